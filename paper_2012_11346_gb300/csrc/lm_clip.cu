@@ -1,0 +1,383 @@
+// The global norm of many gradients, and their clipping by it.  Contract:
+// include/slim_lm.h.
+//
+//   norm = sqrt(sum g^2),  out = min(1, max_norm / norm) * g
+//
+// Two launches: one reads every gradient and leaves one partial sum per block,
+// one adds the partial sums (every block all of them, in the same order),
+// scales and writes.  HBM bounds both; a set that fits L2 is read from HBM once,
+// and of a larger set the second launch starts with the end, which L2 still
+// holds.  The tensors' addresses travel as kernel parameters: no copy and no
+// device table.
+//
+// Range: a thread adds the squares of 64 to 128 elements in fp32 and moves the
+// sum to fp64.  Squares leave fp32's range long before the gradients do, so a
+// thread whose sum overflowed, or is so small that it may have lost squares to
+// underflow, takes its elements again scaled by a power of two, which fits
+// every value of the types.
+#include <float.h>
+#include <stdint.h>
+
+#include "../../include/slim_lm.h"
+#include "common.cuh"
+#include "profiler.h"
+
+namespace slim {
+namespace lm {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kGridNorm = 152 * 8;   // partial sums; blocks of either launch
+constexpr int kChunkBytes = 65536;   // of one tensor, per block and turn
+
+// A launch's tensors.  Tensor t's chunks are numbered [start[t], start[t+1]).
+template <int CAP>
+struct Table {
+  const void* src[CAP];
+  void* dst[CAP];
+  unsigned long long numel[CAP];  // bit 63: bf16
+  unsigned start[CAP + 1];
+  int n;
+};
+constexpr unsigned long long kBf16Bit = 1ull << 63;
+
+template <int CAP>
+__device__ __forceinline__ int find_tensor(const Table<CAP>& tb, unsigned chunk) {
+  int lo = 0, hi = tb.n;  // start[lo] <= chunk < start[hi]
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (tb.start[mid] <= chunk)
+      lo = mid;
+    else
+      hi = mid;
+  }
+  return lo;
+}
+
+// 16 bytes of T as fp32 values.
+template <typename T> struct Pack;
+template <> struct Pack<float> {
+  static constexpr int n = 4;
+  static __device__ __forceinline__ void get(const uint4& u, float* f) {
+    f[0] = __uint_as_float(u.x);
+    f[1] = __uint_as_float(u.y);
+    f[2] = __uint_as_float(u.z);
+    f[3] = __uint_as_float(u.w);
+  }
+  static __device__ __forceinline__ uint4 put(const float* f) {
+    return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]),
+                      __float_as_uint(f[3]));
+  }
+};
+template <> struct Pack<__nv_bfloat16> {
+  static constexpr int n = 8;
+  static __device__ __forceinline__ void get(const uint4& u, float* f) {
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      f[2 * i] = __uint_as_float(w[i] << 16);
+      f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    }
+  }
+  static __device__ __forceinline__ uint4 put(const float* f) {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const __nv_bfloat162 h = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]);
+      w[i] = *reinterpret_cast<const uint32_t*>(&h);
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+  }
+};
+
+// ------------------------------------------------------------------ norm
+// Thresholds of a thread's fp32 sum of squares.  Above kTiny, squares lost to
+// underflow (each below 2^-126) are below its rounding; at or under it every
+// element is below 2^-40, and 2^96 lifts the smallest subnormal's square into
+// the normal range without overflow.
+constexpr float kTiny = 0x1p-80f;
+
+template <typename T>
+__device__ __forceinline__ float square_sum(const T* p, long long lead, long long nvec,
+                                            long long n, float scale, unsigned& any) {
+  constexpr int W = Pack<T>::n;
+  float s = 0.0f;
+  const uint4* v = reinterpret_cast<const uint4*>(p + lead);
+  long long i = threadIdx.x;
+  auto take = [&](const uint4& u) {
+    any |= (u.x | u.y | u.z | u.w);
+    float f[W];
+    Pack<T>::get(u, f);
+#pragma unroll
+    for (int e = 0; e < W; ++e) {
+      const float x = f[e] * scale;
+      s = fmaf(x, x, s);
+    }
+  };
+  for (; i + 3 * kThreads < nvec; i += 4 * kThreads) {
+    uint4 u[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) u[j] = v[i + j * kThreads];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) take(u[j]);
+  }
+  for (; i < nvec; i += kThreads) take(v[i]);
+  // the elements before the first aligned 16 bytes and after the last
+  const long long tail = lead + nvec * W;
+  auto one = [&](long long k) {
+    const float x = Io<T>::load(p, k) * scale;
+    any |= x != 0.0f;
+    s = fmaf(x, x, s);
+  };
+  if (threadIdx.x < lead) one(threadIdx.x);
+  if (tail + threadIdx.x < n) one(tail + threadIdx.x);
+  return s;
+}
+
+template <typename T>
+__device__ __forceinline__ double chunk_squares(const T* p, long long n) {
+  constexpr int W = Pack<T>::n;
+  const unsigned mis = (unsigned)(reinterpret_cast<uintptr_t>(p) & 15u) / sizeof(T);
+  long long lead = mis ? W - mis : 0;
+  if (lead > n) lead = n;
+  const long long nvec = (n - lead) / W;
+  unsigned any = 0, dummy = 0;
+  const float s = square_sum<T>(p, lead, nvec, n, 1.0f, any);
+  if (s >= kTiny && s <= FLT_MAX) return (double)s;
+  if (s < kTiny) {
+    if ((any << 1) == 0) return 0.0;  // nothing but zeros
+    return (double)square_sum<T>(p, lead, nvec, n, 0x1p96f, dummy) * 0x1p-192;
+  }
+  return (double)square_sum<T>(p, lead, nvec, n, 0x1p-96f, dummy) * 0x1p192;
+}
+
+// Sum of x over the block, in a fixed order; every thread gets it.
+__device__ __forceinline__ double block_sum(double x, double* sh) {
+  for (int o = 16; o; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+  if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = x;
+  __syncthreads();
+  double t = 0.0;
+#pragma unroll
+  for (int i = 0; i < kThreads / 32; ++i) t += sh[i];
+  __syncthreads();
+  return t;
+}
+
+template <int CAP>
+__global__ void __launch_bounds__(kThreads) k_norm(const __grid_constant__ Table<CAP> tb,
+                                                   double* part) {
+  __shared__ double sh[kThreads / 32];
+  double acc = 0.0;
+  const unsigned total = tb.start[tb.n];
+  for (unsigned c = blockIdx.x; c < total; c += gridDim.x) {
+    const int t = find_tensor(tb, c);
+    const bool half = tb.numel[t] & kBf16Bit;
+    const long long n = (long long)(tb.numel[t] & ~kBf16Bit);
+    const long long per = kChunkBytes / (half ? 2 : 4);
+    const long long a = (long long)(c - tb.start[t]) * per;
+    const long long m = n - a < per ? n - a : per;
+    if (half)
+      acc += chunk_squares(static_cast<const __nv_bfloat16*>(tb.src[t]) + a, m);
+    else
+      acc += chunk_squares(static_cast<const float*>(tb.src[t]) + a, m);
+  }
+  const double s = block_sum(acc, sh);
+  if (threadIdx.x == 0) part[blockIdx.x] = s;
+}
+
+// ------------------------------------------------------------------ clip
+template <typename T>
+__device__ __forceinline__ void scale_chunk(const T* p, T* q, long long n, float c) {
+  constexpr int W = Pack<T>::n;
+  const unsigned mp = (unsigned)(reinterpret_cast<uintptr_t>(p) & 15u);
+  const unsigned mq = (unsigned)(reinterpret_cast<uintptr_t>(q) & 15u);
+  if (mp != mq) {  // no common alignment: element by element
+    long long i = threadIdx.x;
+    for (; i + 7 * kThreads < n; i += 8 * kThreads) {
+      float x[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) x[j] = Io<T>::load(p, i + j * kThreads);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) Io<T>::store(q, i + j * kThreads, x[j] * c);
+    }
+    for (; i < n; i += kThreads) Io<T>::store(q, i, Io<T>::load(p, i) * c);
+    return;
+  }
+  long long lead = mp ? W - (long long)(mp / sizeof(T)) : 0;
+  if (lead > n) lead = n;
+  const long long nvec = (n - lead) / W, tail = lead + nvec * W;
+  const uint4* v = reinterpret_cast<const uint4*>(p + lead);
+  uint4* o = reinterpret_cast<uint4*>(q + lead);
+  auto put = [&](const uint4& u) {
+    float f[W];
+    Pack<T>::get(u, f);
+#pragma unroll
+    for (int e = 0; e < W; ++e) f[e] *= c;
+    return Pack<T>::put(f);
+  };
+  long long i = threadIdx.x;
+  for (; i + 3 * kThreads < nvec; i += 4 * kThreads) {
+    uint4 u[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) u[j] = v[i + j * kThreads];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) o[i + j * kThreads] = put(u[j]);
+  }
+  for (; i < nvec; i += kThreads) o[i] = put(v[i]);
+  if (threadIdx.x < lead) Io<T>::store(q, threadIdx.x, Io<T>::load(p, threadIdx.x) * c);
+  if (tail + threadIdx.x < n)
+    Io<T>::store(q, tail + threadIdx.x, Io<T>::load(p, tail + threadIdx.x) * c);
+}
+
+template <int CAP>
+__global__ void __launch_bounds__(kThreads) k_clip(const __grid_constant__ Table<CAP> tb,
+                                                   const double* part, int parts, float max_norm,
+                                                   int in_place, float* norm_out) {
+  __shared__ double sh[kThreads / 32];
+  double acc = 0.0;
+  for (int i = threadIdx.x; i < parts; i += kThreads) acc += part[i];
+  const double norm = sqrt(block_sum(acc, sh));
+  if (norm_out && blockIdx.x == 0 && threadIdx.x == 0) *norm_out = (float)norm;
+  // a norm that is not finite scales nothing
+  const float c = norm > (double)max_norm && norm <= DBL_MAX ? (float)((double)max_norm / norm)
+                                                             : 1.0f;
+  if (c == 1.0f && in_place) return;
+  const unsigned total = tb.start[tb.n];
+  for (unsigned x = blockIdx.x; x < total; x += gridDim.x) {
+    const unsigned chunk = total - 1 - x;  // the end first: L2 holds what was read last
+    const int t = find_tensor(tb, chunk);
+    const bool half = tb.numel[t] & kBf16Bit;
+    const long long n = (long long)(tb.numel[t] & ~kBf16Bit);
+    const long long per = kChunkBytes / (half ? 2 : 4);
+    const long long a = (long long)(chunk - tb.start[t]) * per;
+    const long long m = n - a < per ? n - a : per;
+    if (half)
+      scale_chunk(static_cast<const __nv_bfloat16*>(tb.src[t]) + a,
+                  static_cast<__nv_bfloat16*>(tb.dst[t]) + a, m, c);
+    else
+      scale_chunk(static_cast<const float*>(tb.src[t]) + a, static_cast<float*>(tb.dst[t]) + a, m,
+                  c);
+  }
+}
+
+// ------------------------------------------------------------------ host
+// Kernel parameters hold at most 4 KB on the short path and 32,764 bytes on
+// the long one; longer lists take several launches of the latter.
+constexpr int kSmall = 128, kLarge = 1024;
+static_assert(sizeof(Table<kSmall>) <= 3900 && sizeof(Table<kLarge>) <= 32000, "parameters");
+
+struct List {
+  const void* const* src;
+  void* const* dst;
+  const long long* numel;
+  const slim_dtype* dtypes;
+  int n;
+};
+
+// Tensors [a, ..) of the list, as many as fit; returns the next one.
+template <int CAP>
+int fill(const List& l, int a, Table<CAP>* tb, bool* in_place, double* bytes) {
+  tb->n = 0;
+  unsigned long long chunks = 0;
+  *in_place = true;
+  *bytes = 0.0;
+  int t = a;
+  for (; t < l.n && tb->n < CAP; ++t) {
+    if (l.numel[t] == 0) continue;
+    const bool half = l.dtypes[t] == SLIM_BF16;
+    const long long per = kChunkBytes / (half ? 2 : 4);
+    const int i = tb->n++;
+    tb->src[i] = l.src[t];
+    tb->dst[i] = l.dst[t];
+    tb->numel[i] = (unsigned long long)l.numel[t] | (half ? kBf16Bit : 0);
+    tb->start[i] = (unsigned)chunks;
+    chunks += (unsigned long long)((l.numel[t] + per - 1) / per);
+    if (l.src[t] != l.dst[t]) *in_place = false;
+    *bytes += (double)l.numel[t] * (half ? 2 : 4);
+  }
+  tb->start[tb->n] = (unsigned)chunks;
+  return t;
+}
+
+template <int CAP>
+slim_status run(const List& l, float max_norm, float* norm, double* part, cudaStream_t s) {
+  static_assert(sizeof(Table<CAP>) < 32764, "kernel parameters");
+  Table<CAP> tb;
+  tb.n = 0;
+  tb.start[0] = 0;
+  bool in_place;
+  double bytes;
+  int parts = 0;
+  auto grid = [&] {
+    const unsigned c = tb.start[tb.n];
+    return c < 1 ? 1u : c < kGridNorm ? c : (unsigned)kGridNorm;
+  };
+  int a = 0;
+  do {
+    a = fill(l, a, &tb, &in_place, &bytes);
+    prof::Scope ps(prof::K_CLIP, s, 0.0, bytes);
+    k_norm<CAP><<<grid(), kThreads, 0, s>>>(tb, part + parts);
+    if (cudaGetLastError() != cudaSuccess) return SLIM_ERR_CUDA;
+    parts += (int)grid();
+  } while (a < l.n);
+  a = 0;
+  bool first = true;
+  do {
+    a = fill(l, a, &tb, &in_place, &bytes);
+    prof::Scope ps(prof::K_CLIP, s, 0.0, bytes);
+    k_clip<CAP><<<grid(), kThreads, 0, s>>>(tb, part, parts, max_norm, in_place,
+                                            first ? norm : nullptr);
+    if (cudaGetLastError() != cudaSuccess) return SLIM_ERR_CUDA;
+    first = false;
+  } while (a < l.n);
+  return SLIM_OK;
+}
+
+}  // namespace
+}  // namespace lm
+}  // namespace slim
+
+extern "C" slim_status slim_clip_workspace_size(int n, size_t* bytes) {
+  if (!bytes || n < 0) return SLIM_ERR_INVALID_ARG;
+  slim::Carver cv(nullptr);
+  cv.take<int>(4);  // the call's error word (no kernel here sets it)
+  const size_t groups = n == 0 ? 1 : ((size_t)n + slim::lm::kLarge - 1) / slim::lm::kLarge;
+  cv.take<double>(groups * slim::lm::kGridNorm);
+  *bytes = cv.bytes();
+  return SLIM_OK;
+}
+
+extern "C" slim_status slim_clip_grads(const void* const* src, void* const* dst,
+                                       const long long* numel, const slim_dtype* dtypes, int n,
+                                       float max_norm, float* norm, void* workspace,
+                                       size_t workspace_bytes, void* stream) {
+  using namespace slim::lm;
+  if (n < 0 || !(max_norm > 0.0f) || !norm || (reinterpret_cast<uintptr_t>(norm) & 3u))
+    return SLIM_ERR_INVALID_ARG;
+  if (n > 0 && (!src || !dst || !numel || !dtypes)) return SLIM_ERR_INVALID_ARG;
+  long long total = 0;
+  int live = 0;
+  for (int t = 0; t < n; ++t) {
+    if (dtypes[t] != SLIM_F32 && dtypes[t] != SLIM_BF16) return SLIM_ERR_INVALID_ARG;
+    if (numel[t] < 0 || numel[t] > (1LL << 40)) return SLIM_ERR_INVALID_ARG;
+    if (numel[t] == 0) continue;
+    const uintptr_t mask = dtypes[t] == SLIM_BF16 ? 1 : 3;
+    if (!src[t] || !dst[t] || (reinterpret_cast<uintptr_t>(src[t]) & mask) ||
+        (reinterpret_cast<uintptr_t>(dst[t]) & mask))
+      return SLIM_ERR_INVALID_ARG;
+    total += numel[t];
+    ++live;
+    if (total > (1LL << 42)) return SLIM_ERR_INVALID_ARG;  // chunk numbers fit 32 bits
+  }
+  size_t need = 0;
+  slim_clip_workspace_size(n, &need);
+  if (workspace == nullptr || workspace_bytes < need) return SLIM_ERR_WORKSPACE;
+  if (reinterpret_cast<uintptr_t>(workspace) & 255u) return SLIM_ERR_INVALID_ARG;
+  slim::Carver cv(workspace);
+  cv.take<int>(4);
+  double* part = cv.take<double>(0);
+  const List l{src, dst, numel, dtypes, n};
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if (live <= kSmall) return run<kSmall>(l, max_norm, norm, part, s);
+  return run<kLarge>(l, max_norm, norm, part, s);
+}

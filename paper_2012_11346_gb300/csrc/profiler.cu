@@ -15,7 +15,9 @@ const char* kNames[K_COUNT] = {
     "mma_gemm",    "simt_prep",     "simt_scan",      "simt_finalize", "simt_dstat",
     "simt_vjp",    "simt_store",    "simt_reduce",    "simt_state",    "tc_fwd",
     "tc_bwd",      "tc_delta",      "tc_scan",        "tc_bwd_q",      "tc_bwd_kv",
-    "tc_reduce",   "tc_selftest",   "tc_prep",        "stack_rows"};
+    "tc_reduce",   "tc_selftest",   "tc_prep",        "stack_rows",
+    "embed_fwd",   "embed_sort",    "embed_sum",      "clip",          "loss_prep",
+    "loss_stats",  "loss_join",     "loss_softmax",   "loss_grad"};
 
 struct Rec {
   Kid k;

@@ -26,6 +26,15 @@ enum Kid {
   K_TC_SELFTEST,
   K_TC_PREP,
   K_STACK,
+  K_EMBED_FWD,
+  K_EMBED_SORT,
+  K_EMBED_SUM,
+  K_CLIP,
+  K_LOSS_PREP,
+  K_LOSS_STATS,
+  K_LOSS_JOIN,
+  K_LOSS_SOFTMAX,
+  K_LOSS_GRAD,
   K_COUNT
 };
 

@@ -1,11 +1,12 @@
 """Python binding of libslim (ctypes): argument marshalling only.
 
 Every computation runs in the CUDA kernels behind the C ABI declared in
-include/slim.h.  PyTorch supplies device memory (outputs and workspace, so
+include/slim.h and include/slim_lm.h.  PyTorch supplies device memory (outputs and workspace, so
 torch.cuda.max_memory_allocated sees all of it) and the current stream.  There
 is no CPU fallback: if libslim.so is missing or no GPU is present, the calls
 raise.
 """
+import contextlib
 import ctypes
 import os
 
@@ -16,12 +17,14 @@ _lib = None
 
 DTYPES = {torch.float32: 0, torch.bfloat16: 1}
 FEATURES = {"exp": 0, "relu": 1, "square": 2}
+INDEX_DTYPES = {torch.int32: 0, torch.int64: 1}
 STATUS = {0: "SLIM_OK", 1: "SLIM_ERR_INVALID_ARG", 2: "SLIM_ERR_UNSUPPORTED",
           3: "SLIM_ERR_WORKSPACE", 4: "SLIM_ERR_CUDA", 5: "SLIM_ERR_TIMEOUT"}
 
 _i, _p, _sz = ctypes.c_int, ctypes.c_void_p, ctypes.c_size_t
+_ll, _f = ctypes.c_longlong, ctypes.c_float
 
-# (name, argtypes) for every symbol of include/slim.h
+# (name, argtypes) for every symbol of include/slim.h and include/slim_lm.h
 SIGNATURES = {
     "slim_status_string": ([_i], ctypes.c_char_p),
     "slim_version": ([], _i),
@@ -48,6 +51,11 @@ SIGNATURES = {
                           _i),
     "slim_fwd_noalloc": ([_p] * 4 + [_i] * 6 + [_i, _i] + [_p] * 5 + [_p], _i),
     "slim_diag_wait_timeout": ([_p, _p], _i),
+    "slim_embed_fwd": ([_p, _i, _p, _ll, _i, _i, _i, _f, _p, _p], _i),
+    "slim_embed_bwd_workspace_size": ([_ll, _i, _i, _i, ctypes.POINTER(_sz)], _i),
+    "slim_embed_bwd": ([_p, _i, _p, _ll, _i, _i, _i, _f, _i, _p, _p, _sz, _p], _i),
+    "slim_clip_workspace_size": ([_i, ctypes.POINTER(_sz)], _i),
+    "slim_clip_grads": ([_p, _p, _p, _p, _i, _f, _p, _p, _sz, _p], _i),
 }
 
 
@@ -438,3 +446,145 @@ class SlimAttention(torch.autograd.Function):
 
 def slim_attention(q, k, v, omega, C, feature="exp"):
     return SlimAttention.apply(q, k, v, omega, C, feature)
+
+
+# ---------------------------------------------------------------- language-model ends
+def _require(cond, what):
+    if not cond:
+        raise ValueError(what)
+
+
+def _require_ids(ids, what):
+    if ids.dtype not in INDEX_DTYPES:
+        raise TypeError(f"{what} must be int32 or int64, got {ids.dtype}")
+
+
+def _require_dtype(what, *ts):
+    for t in ts:
+        if t.dtype not in DTYPES:
+            raise TypeError(f"{what}: float32 or bfloat16 expected, got {t.dtype}")
+    if len({t.dtype for t in ts}) > 1:
+        raise TypeError(f"{what}: one dtype expected, got {[t.dtype for t in ts]}")
+
+
+def _on(stream):
+    """The context in which a call on `stream` allocates: memory that the
+    caching allocator hands out there is free as far as that stream's order
+    goes, and is given out again only behind the call's work."""
+    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
+
+
+def embed_workspace_size(N, D, V, dtype):
+    n = _sz(0)
+    _check(library().slim_embed_bwd_workspace_size(N, D, V, DTYPES[dtype], ctypes.byref(n)),
+           "slim_embed_bwd_workspace_size")
+    return n.value
+
+
+def embed_forward(ids, table, scale=1.0, out=None, stream=None):
+    """slim_embed_fwd: out [*ids.shape, D] = scale * table[ids], zero rows where
+    an id lies outside [0, V).  ids int32 or int64 of any shape; table [V, D]."""
+    _require_cuda(ids, table)
+    _require_ids(ids, "ids")
+    _require_dtype("embed_forward", table)
+    _require(table.dim() == 2, "table must be [V, D]")
+    V, D = table.shape
+    if out is None:
+        with _on(stream):
+            out = torch.empty(*ids.shape, D, dtype=table.dtype, device=table.device)
+    else:
+        _require_cuda(out)
+        _require(out.dtype == table.dtype and tuple(out.shape) == (*ids.shape, D),
+                 "out must be [*ids.shape, D] in the table's dtype")
+    _check(library().slim_embed_fwd(ids.data_ptr(), INDEX_DTYPES[ids.dtype], table.data_ptr(),
+                                    ids.numel(), D, V, DTYPES[table.dtype], scale,
+                                    out.data_ptr(), _stream_handle(stream)), "slim_embed_fwd")
+    return out
+
+
+def embed_backward(ids, dout, V, scale=1.0, dtable=None, workspace=None, stream=None):
+    """slim_embed_bwd: the gradient of embed_forward with respect to its table,
+    [V, D] in dout's dtype.  With dtable given, the gradient is added to it in
+    place (and it is returned); rows that no id names are then left alone."""
+    _require_cuda(ids, dout)
+    _require_ids(ids, "ids")
+    _require_dtype("embed_backward", dout)
+    _require(tuple(dout.shape[:-1]) == tuple(ids.shape), "dout must be [*ids.shape, D]")
+    D, N = dout.shape[-1], ids.numel()
+    accumulate = dtable is not None
+    if accumulate:
+        _require_cuda(dtable)
+        _require(dtable.dtype == dout.dtype and tuple(dtable.shape) == (V, D),
+                 "dtable must be [V, D] in dout's dtype")
+    with _on(stream):
+        if not accumulate:
+            dtable = torch.empty(V, D, dtype=dout.dtype, device=dout.device)
+        ws = workspace if workspace is not None else _workspace(
+            embed_workspace_size(N, D, V, dout.dtype), dout.device)
+    _check(library().slim_embed_bwd(ids.data_ptr(), INDEX_DTYPES[ids.dtype], dout.data_ptr(), N, D,
+                                    V, DTYPES[dout.dtype], scale, int(accumulate),
+                                    dtable.data_ptr(), ws.data_ptr(), ws.numel(),
+                                    _stream_handle(stream)), "slim_embed_bwd")
+    return dtable
+
+
+def clip_workspace_size(n):
+    """Workspace bytes of clip_grad_norm for n gradients."""
+    b = _sz(0)
+    _check(library().slim_clip_workspace_size(n, ctypes.byref(b)), "slim_clip_workspace_size")
+    return b.value
+
+
+def clip_grad_norm(grads, max_norm, out=None, workspace=None, stream=None):
+    """slim_clip_grads: scales the gradients by min(1, max_norm / norm), norm
+    being their global 2-norm, and returns norm ([1] fp32, on the device).
+    In place, or into the tensors of `out` (same shapes and dtypes).  If the
+    norm is not finite nothing is scaled: read it and skip the step."""
+    grads = list(grads)
+    dst = grads if out is None else list(out)
+    _require(len(dst) == len(grads), "out must have one tensor per gradient")
+    _require(len(grads) > 0, "no gradients")
+    _require_cuda(*grads)
+    if out is not None:
+        _require_cuda(*dst)
+        for g, o in zip(grads, dst):
+            _require(o.shape == g.shape and o.dtype == g.dtype,
+                     "out must have the gradients' shapes and dtypes")
+    n = len(grads)
+    for g in grads:
+        if g.dtype not in DTYPES:
+            raise TypeError(f"gradients must be float32 or bfloat16, got {g.dtype}")
+    ptr = ctypes.c_void_p * n
+    src_p = ptr(*[g.data_ptr() for g in grads])
+    _require(len({a for a, g in zip(src_p, grads) if g.numel()}) ==
+             sum(g.numel() > 0 for g in grads), "a gradient is listed twice")
+    dst_p = src_p if out is None else ptr(*[o.data_ptr() for o in dst])
+    numel = (_ll * n)(*[g.numel() for g in grads])
+    dts = (_i * n)(*[DTYPES[g.dtype] for g in grads])
+    with _on(stream):
+        norm = torch.empty(1, dtype=torch.float32, device=grads[0].device)
+        ws = workspace if workspace is not None else _workspace(clip_workspace_size(n),
+                                                                norm.device)
+    _check(library().slim_clip_grads(src_p, dst_p, numel, dts, n, max_norm, norm.data_ptr(),
+                                     ws.data_ptr(), ws.numel(), _stream_handle(stream)),
+           "slim_clip_grads")
+    return norm
+
+
+class Embedding(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, ids, table, scale):
+        ids = ids.contiguous()
+        ctx.save_for_backward(ids)
+        ctx.V, ctx.scale = table.shape[0], scale
+        return embed_forward(ids, table.contiguous(), scale)
+
+    @staticmethod
+    def backward(ctx, dout):
+        (ids,) = ctx.saved_tensors
+        return None, embed_backward(ids, dout.contiguous(), ctx.V, ctx.scale), None
+
+
+def embedding(ids, table, scale=1.0):
+    """Differentiable embed_forward (gradient with respect to the table)."""
+    return Embedding.apply(ids, table, scale)

@@ -1,0 +1,105 @@
+"""Host-only checks of the language-model entry points (include/slim_lm.h):
+sizes, and refusals before anything is enqueued.  No call here reaches a CUDA
+launch; the pointers are never dereferenced."""
+import ctypes
+
+import pytest
+import torch
+
+from paper_2012_11346_gb300 import slim
+
+OK, INVALID, UNSUPPORTED, WORKSPACE = 0, 1, 2, 3
+FAKE = 0x10000
+F32, BF16, I32, I64 = 0, 1, 0, 1
+
+
+@pytest.fixture(scope="module")
+def lib():
+    import os
+    if not os.path.exists(slim._LIB_PATH):
+        from paper_2012_11346_gb300 import build
+        build.build()
+    return slim.library()
+
+
+# ---------------------------------------------------------------- embedding
+def embed_fwd(lib, ids=FAKE, it=I64, table=FAKE, N=4, D=8, V=16, dt=F32, out=FAKE):
+    return lib.slim_embed_fwd(ids, it, table, N, D, V, dt, 1.0, out, None)
+
+
+def embed_bwd(lib, ids=FAKE, it=I64, dout=FAKE, N=4, D=8, V=16, dt=F32, acc=0, dtable=FAKE,
+              ws=FAKE, nbytes=1 << 40):
+    return lib.slim_embed_bwd(ids, it, dout, N, D, V, dt, 1.0, acc, dtable, ws, nbytes, None)
+
+
+@pytest.mark.parametrize("kw", [dict(N=-1), dict(N=1 << 31), dict(D=0), dict(V=0), dict(dt=2),
+                                dict(it=2), dict(ids=None), dict(ids=FAKE + 4),
+                                dict(it=I32, ids=FAKE + 2)])
+def test_embed_rejects(lib, kw):
+    assert embed_fwd(lib, **kw) == INVALID
+    assert embed_bwd(lib, **kw) == INVALID
+
+
+def test_embed_rejects_tensors(lib):
+    for bad in (None, FAKE + 8):
+        assert embed_fwd(lib, table=bad) == INVALID
+        assert embed_fwd(lib, out=bad) == INVALID
+        assert embed_bwd(lib, dout=bad) == INVALID
+        assert embed_bwd(lib, dtable=bad) == INVALID
+    assert embed_bwd(lib, acc=2) == INVALID
+
+
+def test_embed_workspace(lib):
+    need = slim.embed_workspace_size(1000, 64, 300, torch.float32)
+    assert embed_bwd(lib, N=1000, D=64, V=300, nbytes=need - 1) == WORKSPACE
+    assert embed_bwd(lib, N=1000, D=64, V=300, ws=None) == WORKSPACE
+    assert embed_bwd(lib, N=1000, D=64, V=300, ws=FAKE + 16, nbytes=need) == INVALID
+    assert lib.slim_embed_bwd_workspace_size(4, 8, 16, F32, None) == INVALID
+    # grows with the tokens, not with the table (beyond the sort's second buffer)
+    a = slim.embed_workspace_size(100000, 64, 300, torch.float32)
+    b = slim.embed_workspace_size(100000, 64, 60000, torch.float32)
+    assert a == b
+
+
+def test_embed_no_tokens_enqueues_nothing(lib):
+    assert embed_fwd(lib, N=0, ids=None, out=None) == OK
+    assert embed_bwd(lib, N=0, ids=None, dout=None, acc=1, ws=None, nbytes=0) == OK
+
+
+# ---------------------------------------------------------------- clipping
+def clip(lib, n=2, src=(FAKE, FAKE), dst=(FAKE, FAKE), numel=(8, 8), dts=(F32, BF16), max_norm=1.0,
+         norm=FAKE, ws=FAKE, nbytes=1 << 40):
+    p = ctypes.c_void_p * len(src)
+    return lib.slim_clip_grads(p(*src), p(*dst), (ctypes.c_longlong * len(numel))(*numel),
+                               (ctypes.c_int * len(dts))(*dts), n, max_norm, norm, ws, nbytes,
+                               None)
+
+
+@pytest.mark.parametrize("kw", [dict(n=-1), dict(max_norm=0.0), dict(max_norm=-1.0),
+                                dict(max_norm=float("nan")), dict(norm=None),
+                                dict(norm=FAKE + 2), dict(dts=(F32, 2)), dict(numel=(8, -1)),
+                                dict(src=(FAKE, None)), dict(dst=(None, FAKE)),
+                                dict(src=(FAKE + 2, FAKE)), dict(dst=(FAKE, FAKE + 1)),
+                                dict(numel=(1 << 41, 8)), dict(ws=FAKE + 8)])
+def test_clip_rejects(lib, kw):
+    assert clip(lib, **kw) == INVALID
+
+
+def test_clip_workspace(lib):
+    need = slim.clip_workspace_size(2)
+    assert clip(lib, nbytes=need - 1) == WORKSPACE
+    assert clip(lib, ws=None) == WORKSPACE
+    assert lib.slim_clip_workspace_size(2, None) == INVALID
+    assert lib.slim_clip_grads(None, None, None, None, 1, 1.0, FAKE, FAKE, 1 << 40, None) == INVALID
+
+
+# ---------------------------------------------------------------- the binding
+def test_binding_refuses_cpu_tensors():
+    with pytest.raises(RuntimeError):
+        slim.embed_forward(torch.zeros(3, dtype=torch.long), torch.zeros(4, 8))
+    with pytest.raises(RuntimeError):
+        slim.embed_backward(torch.zeros(3, dtype=torch.long), torch.zeros(3, 8), 4)
+    with pytest.raises(RuntimeError):
+        slim.clip_grad_norm([torch.zeros(3)], 1.0)
+    with pytest.raises(ValueError):
+        slim.clip_grad_norm([], 1.0)
