@@ -57,6 +57,61 @@ slim_status slim_embed_bwd(const void* ids, slim_index itype, const void* dout, 
                            void* workspace, size_t workspace_bytes, void* stream);
 
 /*
+ * Softmax cross entropy of the rows of x against a vocabulary w:
+ *     z_iv   = sum_d x_id w_vd
+ *     lse_i  = log sum_v exp(z_iv)
+ *     loss_i = lse_i - z_i,target(i)
+ * The logits z live in tiles on the chip; what is kept is O(N).
+ *   x       [N, D] dtype;  w [V, D] dtype;  targets [N] itype, aligned to its
+ *           own size.  A row whose target is ignore_index has loss 0 (its lse
+ *           is written all the same).  Any other target outside [0, V) is an
+ *           error of the caller's data and makes the row's loss NaN.
+ *   loss    [N] fp32, written.  Computed as log1p of the other words' weight
+ *           against the target's, so that a small loss keeps its digits.
+ *   lse     [N] fp32, written; slim_vocab_loss_bwd reads it.
+ *   total   [2] fp32, written: the sum of the losses, and the number of rows
+ *           that are not ignored (their quotient is the mean loss).
+ * bf16 operands are multiplied exactly and summed in fp32.  fp32 operands are
+ * split into three bf16 pieces (24 bits) and multiplied piece by piece, six
+ * products each, smallest first, on the tensor cores.
+ * 0 <= N < 2^31, D >= 1, V >= 1.  N = 0 only zeroes `total`.
+ *
+ * slim_vocab_loss_workspace_size: workspace bytes of the forward (backward =
+ * 0, piece is not read) or of the backward with this piece.
+ */
+slim_status slim_vocab_loss_workspace_size(long long N, int D, int V, slim_dtype dtype, int piece,
+                                           int backward, size_t* bytes);
+slim_status slim_vocab_loss_fwd(const void* x, const void* w, const void* targets,
+                                slim_index itype, long long N, int D, int V, slim_dtype dtype,
+                                long long ignore_index, float* loss, float* lse, float* total,
+                                void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * The gradients of sum_i c_i loss_i with respect to x and w:
+ *     g_iv = c_i (exp(z_iv - lse_i) - [v = target(i)]),  c_i = dloss_i / count
+ *     dx = g w  [N, D] dtype,   dw = g^T x  [V, D] dtype
+ * in pieces of `piece` words (rounded up to a multiple of 256): a piece's
+ * logits are computed again and its g is held only until both products have
+ * read it, so memory grows with N * piece and not with N * V.
+ *   lse          [N] fp32 from the forward on the same x, w and targets.
+ *   dloss        fp32: [N] with dloss_stride 1, or [1] for every row with
+ *                dloss_stride 0.
+ *   count        [1] fp32 or null (1): for the mean loss, the forward's
+ *                total[1].  Where it is 0 there is no row to divide among and
+ *                the gradients are zero.
+ * An ignored row passes nothing on: its dx is zero, and its x, whatever it
+ * holds, does not reach dw.  A row whose target is out of range passes NaN.
+ * g is rounded once for the products: to bf16 for bf16 problems (2^-9
+ * relative, like the rounding of the gradients themselves), to three bf16
+ * pieces for fp32 ones.  Sums are fp32; dx and dw are rounded once.
+ */
+slim_status slim_vocab_loss_bwd(const void* x, const void* w, const void* targets,
+                                slim_index itype, const float* lse, const float* dloss,
+                                int dloss_stride, const float* count, long long N, int D, int V,
+                                slim_dtype dtype, int piece, long long ignore_index, void* dx,
+                                void* dw, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * The global 2-norm of n gradients and their clipping by it:
  *     norm = sqrt(sum over all tensors and elements of g^2)
  *     out  = min(1, max_norm / norm) * g, rounded to nearest even.

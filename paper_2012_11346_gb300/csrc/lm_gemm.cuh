@@ -1,0 +1,335 @@
+// Tile products of the vocabulary loss on the tcgen05 tensor cores: the roles
+// of a persistent, warp-specialised kernel that computes D = A B^T tiles with
+// an epilogue of its caller's.
+//
+// A block (or a pair of blocks, CG = 2, on one tile of twice the height) runs
+// three roles side by side: one thread copies operand tiles into a ring of
+// shared-memory stages by TMA, one thread issues the MMAs on them, and eight
+// warps read finished accumulators from TMEM and run the epilogue.  Two
+// accumulators alternate, so a tile's epilogue runs under the next tile's MMAs.
+//
+// Operands are planes of bf16 matrices, K-major ([rows][K]) or MN-major
+// ([K][rows]); coordinates past an edge read as zero.  NP = 3: a value is the
+// sum of its three planes' values, and the product is the sum of the six plane
+// products of order below 2^-16, smallest first.  The tensor core adds to a
+// 32-bit accumulator with a truncation per step, so for NP = 3 a sum is cut
+// into short chains that the epilogue's registers join in fp32.
+#pragma once
+#include "common.cuh"
+#include "tc_common.cuh"
+
+namespace slim {
+namespace lm {
+
+constexpr int kTM = 128;  // rows of a block's tile
+constexpr int kTK = 64;   // reduction per stage
+constexpr int kGemmThreads = 384;  // warps: TMA, MMA, TMEM, spare, 8 of epilogue
+constexpr int kEpiWarps = 8;
+
+template <int NP, int CG>
+struct Tile {
+  // With three planes the epilogue holds a tile's sums in registers: half the
+  // columns, 64 per thread.
+  static constexpr int N = NP == 1 ? 256 : 128;
+  static constexpr int HALF = N / 2;      // columns of an epilogue warp
+  static constexpr int BROWS = N / CG;    // rows of B that a block holds
+  static constexpr int A_BYTES = kTM * kTK * 2, B_BYTES = BROWS * kTK * 2;
+  static constexpr int STAGE = A_BYTES + B_BYTES;
+  static constexpr int STAGES = 192 * 1024 / STAGE < 8 ? 192 * 1024 / STAGE : 8;
+  static constexpr int PAIRS = NP == 1 ? 1 : 6;
+  static constexpr size_t smem() { return 1024 + (size_t)STAGES * STAGE; }
+};
+
+// One product: D [M, N] = sum over K of A and B.
+struct Product {
+  CUtensorMap a, b;
+  int a_mn, b_mn;  // operand layouts: 0 K-major, 1 MN-major
+  int M, N;
+  int tm, tn;      // tiles each way (tm in tiles of kTM * CG rows)
+  int kb;          // stages (of kTK) of the reduction
+  int chain;       // stage products per accumulator chain
+};
+
+struct GemmShared {
+  uint64_t full[8], empty[8], tfull[2], tempty[2];
+  uint32_t tmem;
+};
+
+// ------------------------------------------------------------------ cluster
+__device__ __forceinline__ uint32_t cluster_rank() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ uint32_t map_to_rank(uint32_t addr, uint32_t rank) {
+  uint32_t r;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
+  return r;
+}
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+template <int CG>
+__device__ __forceinline__ void arrive_at_leader(uint32_t bar) {
+  if (CG == 1)
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+  else
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(
+                     map_to_rank(bar, 0))
+                 : "memory");
+}
+
+// ------------------------------------------------------------------ CG forms
+template <int CG>
+__device__ __forceinline__ void gemm_tmem_alloc(uint32_t dst, uint32_t cols) {
+  if (CG == 1) {
+    tc::tmem_alloc(dst, cols);
+  } else {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(dst),
+                 "r"(cols)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+  }
+}
+template <int CG>
+__device__ __forceinline__ void gemm_tmem_free(uint32_t t, uint32_t cols) {
+  if (CG == 1)
+    tc::tmem_dealloc(t, cols);
+  else
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(t), "r"(cols)
+                 : "memory");
+}
+template <int CG>
+__device__ __forceinline__ void gemm_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc,
+                                         uint32_t acc) {
+  if (CG == 1) {
+    tc::mma(d, a, b, idesc, acc);
+  } else {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"(acc)
+        : "memory");
+  }
+}
+// Arrives on the mbarrier (of both blocks of a pair) once this thread's MMAs
+// so far are done.
+template <int CG>
+__device__ __forceinline__ void gemm_commit(uint32_t bar) {
+  if (CG == 1) {
+    tc::mma_commit(bar);
+  } else {
+    asm volatile(
+        "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 "
+        "[%0], %1;" ::"r"(bar),
+        "h"((uint16_t)3)
+        : "memory");
+  }
+}
+// One box of a tensor map to shared memory; x is a multiple of 64 elements
+// (128 bytes).  With CG = 2 the bytes are counted on the leader's barrier.
+template <int CG>
+__device__ __forceinline__ void gemm_tma(uint32_t dst, const CUtensorMap* map, int x, int y, int z,
+                                         uint32_t bar) {
+  if (CG == 1)
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes "
+        "[%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
+        "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(bar)
+        : "memory");
+  else
+    asm volatile(
+        "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes "
+        "[%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
+        "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(bar)
+        : "memory");
+}
+
+// ------------------------------------------------------------------ roles
+// The planes of the i-th product of a stage, smallest products first.
+template <int NP>
+__device__ __forceinline__ void plane_pair(int i, int& pa, int& pb) {
+  if (NP == 1) {
+    pa = pb = 0;
+  } else {
+    // (2,0) (1,1) (0,2) (1,0) (0,1) (0,0), two bits each
+    pa = (0x046 >> (2 * i)) & 3;
+    pb = (0x124 >> (2 * i)) & 3;
+  }
+}
+
+// Sets the ring up and allocates TMEM; every thread of the block (of the pair).
+template <int NP, int CG>
+__device__ __forceinline__ void gemm_begin(GemmShared& sh) {
+  using T = Tile<NP, CG>;
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < T::STAGES; ++i) {
+      tc::mbar_init(tc::smem_u32(&sh.full[i]), 1);
+      tc::mbar_init(tc::smem_u32(&sh.empty[i]), 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      tc::mbar_init(tc::smem_u32(&sh.tfull[i]), 1);
+      tc::mbar_init(tc::smem_u32(&sh.tempty[i]), kEpiWarps * CG);
+    }
+    tc::mbar_fence_init();
+  }
+  if (threadIdx.x / 32 == 2) gemm_tmem_alloc<CG>(tc::smem_u32(&sh.tmem), 2 * T::N);
+  tc::tc_fence_before();
+  if (CG == 1)
+    __syncthreads();
+  else
+    cluster_sync();
+  tc::tc_fence_after();
+}
+
+template <int NP, int CG>
+__device__ __forceinline__ void gemm_end(GemmShared& sh, bool failed) {
+  // a role that gave up may leave copies in flight: let them land
+  if (failed)
+    for (int i = 0; i < 1000; ++i) __nanosleep(10000);
+  tc::tc_fence_before();
+  if (CG == 1)
+    __syncthreads();
+  else
+    cluster_sync();
+  if (threadIdx.x / 32 == 2) gemm_tmem_free<CG>(sh.tmem, 2 * Tile<NP, CG>::N);
+}
+
+// The copying thread.  `next(p, m, n)` yields this worker's tiles in order:
+// the same sequence in every role.  False if a wait gave up.
+template <int NP, int CG, typename Next>
+__device__ bool gemm_copy(GemmShared& sh, uint8_t* stages, Next next, int* err) {
+  using T = Tile<NP, CG>;
+  const uint32_t rank = CG == 1 ? 0 : cluster_rank();
+  const Product* p;
+  int m, n;
+  uint32_t it = 0;
+  while (next(p, m, n)) {
+    const int row = (m * CG + (int)rank) * kTM, col = n * T::N + (int)rank * T::BROWS;
+    for (int kb = 0; kb < p->kb; ++kb) {
+#pragma unroll 1
+      for (int i = 0; i < T::PAIRS; ++i, ++it) {
+        const int st = it % T::STAGES;
+        int pa, pb;
+        plane_pair<NP>(i, pa, pb);
+        if (!tc::mbar_wait(tc::smem_u32(&sh.empty[st]), ((it / T::STAGES) & 1) ^ 1, err))
+          return false;
+        uint32_t full = tc::smem_u32(&sh.full[st]);
+        if (rank == 0) tc::mbar_expect_tx(full, CG * T::STAGE);
+        if (CG == 2) full = map_to_rank(full, 0);
+        const uint32_t sa = tc::smem_u32(stages) + st * T::STAGE, sb = sa + T::A_BYTES;
+        const int k = kb * kTK;
+        if (p->a_mn) {
+#pragma unroll
+          for (int j = 0; j < kTM / 64; ++j)
+            gemm_tma<CG>(sa + j * 8192, &p->a, row + 64 * j, k, pa, full);
+        } else {
+          gemm_tma<CG>(sa, &p->a, k, row, pa, full);
+        }
+        if (p->b_mn) {
+#pragma unroll
+          for (int j = 0; j < T::BROWS / 64; ++j)
+            gemm_tma<CG>(sb + j * 8192, &p->b, col + 64 * j, k, pb, full);
+        } else {
+          gemm_tma<CG>(sb, &p->b, k, col, pb, full);
+        }
+      }
+    }
+  }
+  return true;
+}
+
+// The thread that issues MMAs (of the leading block of a pair).
+template <int NP, int CG, typename Next>
+__device__ bool gemm_multiply(GemmShared& sh, uint8_t* stages, Next next, int* err) {
+  using T = Tile<NP, CG>;
+  const Product* p;
+  int m, n;
+  uint32_t it = 0, acc = 0;
+  while (next(p, m, n)) {
+    const uint32_t idesc = tc::idesc_bf16(kTM * CG, T::N, p->a_mn, p->b_mn);
+    const uint32_t a_lbo = p->a_mn ? 8192 : 16, b_lbo = p->b_mn ? 8192 : 16;
+    const uint32_t a_step = p->a_mn ? 128 : 2, b_step = p->b_mn ? 128 : 2;
+    const int total = p->kb * T::PAIRS;
+    for (int k0 = 0; k0 < total; k0 += p->chain, ++acc) {
+      const int buf = acc & 1;
+      if (!tc::mbar_wait(tc::smem_u32(&sh.tempty[buf]), ((acc >> 1) & 1) ^ 1, err)) return false;
+      tc::tc_fence_after();
+      const uint32_t d = sh.tmem + buf * T::N;
+      const int k1 = min(k0 + p->chain, total);
+      for (int k = k0; k < k1; ++k, ++it) {
+        const int st = it % T::STAGES;
+        if (!tc::mbar_wait(tc::smem_u32(&sh.full[st]), (it / T::STAGES) & 1, err)) return false;
+        tc::tc_fence_after();
+        const uint32_t sa = tc::smem_u32(stages) + st * T::STAGE, sb = sa + T::A_BYTES;
+        const uint64_t da = tc::sdesc(sa, a_lbo, 1024), db = tc::sdesc(sb, b_lbo, 1024);
+#pragma unroll
+        for (int j = 0; j < kTK / 16; ++j)
+          gemm_mma<CG>(d, da + j * a_step, db + j * b_step, idesc, k > k0 || j > 0);
+        gemm_commit<CG>(tc::smem_u32(&sh.empty[st]));
+      }
+      gemm_commit<CG>(tc::smem_u32(&sh.tfull[buf]));
+    }
+  }
+  return true;
+}
+
+// An epilogue warp.  For every tile, epi.begin(p, m, n, row, col0) once, then
+// epi.chunk(c, v) for each 32 columns col0 + c .. of row `row` (of this thread)
+// that lie inside the product, then epi.end().  Reads past the product's rows
+// still run (their values are zero sums); the epilogue drops them.
+template <int NP, int CG, typename Next, typename Epi>
+__device__ bool gemm_finish(GemmShared& sh, Next next, Epi& epi, int* err) {
+  using T = Tile<NP, CG>;
+  const uint32_t rank = CG == 1 ? 0 : cluster_rank();
+  const int w = threadIdx.x / 32 - 4, lane = threadIdx.x & 31;
+  const int quarter = w & 3, half = w >> 2;
+  const Product* p;
+  int m, n;
+  uint32_t acc = 0;
+  while (next(p, m, n)) {
+    const int row = (m * CG + (int)rank) * kTM + quarter * 32 + lane;
+    const int col = n * T::N + half * T::HALF;
+    const int total = p->kb * T::PAIRS;
+    float sum[NP == 1 ? 1 : T::HALF];
+    epi.begin(*p, m, n, row, col);
+    for (int k0 = 0; k0 < total; k0 += p->chain, ++acc) {
+      const int buf = acc & 1;
+      if (!tc::mbar_wait(tc::smem_u32(&sh.tfull[buf]), (acc >> 1) & 1, err)) return false;
+      tc::tc_fence_after();
+      const uint32_t t = sh.tmem + buf * T::N + half * T::HALF + ((uint32_t)(quarter * 32) << 16);
+      if (NP > 1) {
+#pragma unroll
+        for (int c = 0; c < T::HALF; c += 16) {
+          float v[16];
+          tc::tmem_ld16(t + c, v);
+#pragma unroll
+          for (int i = 0; i < 16; ++i) sum[c + i] = k0 == 0 ? v[i] : sum[c + i] + v[i];
+        }
+      } else {
+#pragma unroll 1
+        for (int c = 0; c < T::HALF && col + c < p->N; c += 32) {
+          float v[32];
+          __syncwarp();
+          tc::tmem_ld32(t + c, v);
+          epi.chunk(c, v);
+        }
+      }
+      tc::tc_fence_before();
+      __syncwarp();
+      if (lane == 0) arrive_at_leader<CG>(tc::smem_u32(&sh.tempty[buf]));
+    }
+    if (NP > 1) {
+#pragma unroll
+      for (int c = 0; c < T::HALF; c += 32)
+        if (col + c < p->N) epi.chunk(c, &sum[c]);
+    }
+    epi.end();
+  }
+  return true;
+}
+
+}  // namespace lm
+}  // namespace slim

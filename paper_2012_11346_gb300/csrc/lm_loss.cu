@@ -1,0 +1,918 @@
+// Softmax cross entropy over a vocabulary in pieces, without keeping the
+// logits, and its gradients.  Contract: include/slim_lm.h.
+//
+// Forward: z = x w^T by tiles on the tensor cores; a tile's epilogue folds its
+// columns into a running (maximum, sum of exponentials) per row, which stays in
+// registers while a worker walks along the vocabulary for the same rows.  The
+// row's own target is left out of the sum and its logit kept apart: the loss is
+// log1p(rest / target), which keeps its digits when it is small.  A second
+// kernel joins the workers' partial statistics of each row in a fixed order.
+//
+// Backward, for each piece of the vocabulary: the logits again, with an epilogue
+// that turns them into g = c (p - onehot), kept for this piece only, and then one
+// launch with both products, dx += g w and dw = g^T x.
+#include <stdint.h>
+
+#include "../../include/slim_lm.h"
+#include "common.cuh"
+#include "lm_gemm.cuh"
+#include "profiler.h"
+#include "report.h"
+#include "tma_map.h"
+
+namespace slim {
+namespace lm {
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr int kPieceStep = 256;  // pieces are multiples of this
+
+__device__ __forceinline__ long long load_target(const void* t, int i64, long long i) {
+  return i64 ? static_cast<const long long*>(t)[i] : static_cast<const int*>(t)[i];
+}
+
+// 2^x.  The fast form is within a few units of 2^-22; fp32 problems take the
+// accurate one.
+template <int NP>
+__device__ __forceinline__ float exp2_of(float x) {
+  return NP == 1 ? tc::ex2_approx(x) : exp2f(x);
+}
+
+// Packs the leading bf16 plane of two values and leaves their remainders (both
+// exact).  With one plane there is no remainder to keep.
+template <int NP>
+__device__ __forceinline__ float lead_bf16(float v) {
+  const float h = __bfloat162float(__float2bfloat16_rn(v));
+  // a finite value that rounds up to infinity is cut off instead
+  return NP > 1 && isinf(h) && !isinf(v) ? __uint_as_float(__float_as_uint(v) & 0xffff0000u) : h;
+}
+template <int NP>
+__device__ __forceinline__ uint32_t take_plane(float& a, float& b) {
+  if (NP == 1) return tc::pack_bf16(a, b);
+  const float ha = lead_bf16<NP>(a), hb = lead_bf16<NP>(b);
+  // an infinity or NaN is all in its first plane
+  a = isfinite(a) ? a - ha : 0.0f;
+  b = isfinite(b) ? b - hb : 0.0f;
+  return tc::pack_bf16(ha, hb);
+}
+
+// ------------------------------------------------------------------ staging
+// Rows as bf16 planes [NP][R][ld]: fp32 values split into three, rows padded to
+// a multiple of 8 elements so that TMA can step over them.  Rows that `targets`
+// marks as ignored become zero.
+template <typename T, int NP>
+__global__ void __launch_bounds__(256) k_stage(const T* src, long long R, int D, int ld,
+                                               const void* targets, int i64, long long ignore,
+                                               __nv_bfloat16* dst) {
+  const int per = ld / 8;
+  const long long total = R * per, plane = R * ld;
+  for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < total;
+       i += (long long)gridDim.x * 256) {
+    const long long r = i / per;
+    const int c = (int)(i - r * per) * 8;
+    const bool live = !targets || load_target(targets, i64, r) != ignore;
+    float v[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      v[j] = live && c + j < D ? Io<T>::load(src, (size_t)r * D + c + j) : 0.0f;
+#pragma unroll
+    for (int p = 0; p < NP; ++p) {
+      uint32_t u[4];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) u[q] = take_plane<NP>(v[2 * q], v[2 * q + 1]);
+      *reinterpret_cast<uint4*>(dst + p * plane + r * ld + c) = make_uint4(u[0], u[1], u[2], u[3]);
+    }
+  }
+}
+
+// ------------------------------------------------------------------ logits
+// A worker (a block, or a pair) takes a contiguous run of the tiles, columns
+// fastest, so that it stays with the same rows as long as it can.
+struct RunNext {
+  const Product* p;
+  long long t, end;
+  __device__ bool operator()(const Product*& q, int& m, int& n) {
+    if (t >= end) return false;
+    q = p;
+    m = (int)(t / p->tn);
+    n = (int)(t % p->tn);
+    ++t;
+    return true;
+  }
+};
+__host__ __device__ inline long long run_begin(long long worker, long long tiles, long long workers) {
+  return worker * tiles / workers;
+}
+// The worker that has tile t.
+__host__ __device__ inline long long run_owner(long long t, long long tiles, long long workers) {
+  return ((t + 1) * workers - 1) / tiles;
+}
+
+struct StatJob {
+  Product p;
+  const void* targets;
+  int i64;
+  long long ignore;
+  int V;
+  int slots;       // partial statistics per row: 2 per worker that shares it
+  float2* part;    // [tm][slots][rows of a tile]: maximum, sum
+  float* zt;       // [N] target logits
+  int* err;
+  unsigned* rep;
+};
+
+// (maximum, sum) of a row's logits but the target's, over a worker's run.
+template <int NP, int CG>
+struct StatEpi {
+  const StatJob& j;
+  long long worker, workers;
+  int m_now = -1;
+  float top = -INFINITY, sum = 0.0f;
+  int row = 0, col = 0, target = -1, slot_row = 0;
+  __device__ StatEpi(const StatJob& job, long long w, long long ws)
+      : j(job), worker(w), workers(ws) {}
+  __device__ void begin(const Product& p, int m, int n, int r, int c) {
+    if (m != m_now) {
+      flush();
+      m_now = m;
+      top = -INFINITY;
+      sum = 0.0f;
+      row = r;
+      slot_row = r - m * kTM * CG;
+      target = -1;
+      if (r < p.M) {
+        const long long t = load_target(j.targets, j.i64, r);
+        if (t != j.ignore && t >= 0 && t < j.V) target = (int)t;
+      }
+    }
+    col = c;
+  }
+  __device__ void chunk(int c, const float* v) {
+    float z[32];
+    const int left = j.V - (col + c), at = target - (col + c);
+#pragma unroll
+    for (int i = 0; i < 32; ++i) z[i] = v[i];
+    if (at >= 0 && at < 32) {
+#pragma unroll
+      for (int i = 0; i < 32; ++i)
+        if (i == at) {
+          j.zt[row] = z[i];
+          z[i] = -INFINITY;
+        }
+    }
+    if (left < 32) {
+#pragma unroll
+      for (int i = 0; i < 32; ++i)
+        if (i >= left) z[i] = -INFINITY;
+    }
+    float t = top;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) t = fmaxf(t, z[i]);
+    // with nothing but -inf so far the sum stays 0: 2^(-inf - 0)
+    const float base = t == -INFINITY ? 0.0f : t * kLog2e;
+    float s = sum * exp2_of<NP>(top * kLog2e - base);
+#pragma unroll
+    for (int i = 0; i < 32; ++i) s += exp2_of<NP>(fmaf(z[i], kLog2e, -base));
+    top = t;
+    sum = s;
+  }
+  __device__ void end() {}
+  __device__ void flush() {
+    if (m_now < 0) return;
+    const long long tiles = (long long)j.p.tm * j.p.tn;
+    const int slot = (int)(worker - run_owner((long long)m_now * j.p.tn, tiles, workers)) * 2 +
+                     (threadIdx.x / 32 - 4) / 4;
+    j.part[((size_t)m_now * j.slots + slot) * (kTM * CG) + slot_row] = make_float2(top, sum);
+  }
+};
+
+struct SoftJob {
+  Product p;
+  const void* targets;
+  int i64;
+  long long ignore;
+  int V, v0;                  // vocabulary, and the piece's first word
+  const float *lse, *dloss, *count;
+  int dstride;
+  __nv_bfloat16* g;           // [NP][M][ld]
+  long long plane;
+  int ld;
+  int* err;
+  unsigned* rep;
+};
+
+// g = c (exp(z - lse) - onehot), rounded to NP bf16 pieces.
+template <int NP, int CG>
+struct SoftEpi {
+  const SoftJob& j;
+  int row = 0, col = 0, target = -1;
+  float coef = 0.0f, lse2 = 0.0f;
+  bool in = false, live = false;
+  __device__ explicit SoftEpi(const SoftJob& job) : j(job) {}
+  __device__ void begin(const Product& p, int m, int n, int r, int c) {
+    row = r;
+    col = c;
+    in = r < p.M;
+    live = false;
+    target = -1;
+    if (!in) return;
+    const long long t = load_target(j.targets, j.i64, r);
+    live = t != j.ignore;
+    coef = j.dloss[(size_t)r * j.dstride];
+    if (j.count) {
+      const float k = *j.count;
+      if (k == 0.0f) live = false;
+      coef /= k;
+    }
+    if (t >= 0 && t < j.V)
+      target = (int)t - j.v0;
+    else
+      coef = __int_as_float(0x7fffffff);
+    lse2 = j.lse[r] * kLog2e;
+  }
+  __device__ void chunk(int c, const float* v) {
+    if (!in) return;
+    const int at = target - (col + c);
+    float g[32];
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+      const float p = exp2_of<NP>(fmaf(v[i], kLog2e, -lse2));
+      g[i] = live ? coef * (i == at ? p - 1.0f : p) : 0.0f;
+    }
+    __nv_bfloat16* dst = j.g + (size_t)row * j.ld + col + c;
+#pragma unroll
+    for (int q = 0; q < NP; ++q) {
+#pragma unroll
+      for (int i = 0; i < 32; i += 8) {
+        uint32_t u[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) u[e] = take_plane<NP>(g[i + 2 * e], g[i + 2 * e + 1]);
+        *reinterpret_cast<uint4*>(dst + q * j.plane + i) = make_uint4(u[0], u[1], u[2], u[3]);
+      }
+    }
+  }
+  __device__ void end() {}
+};
+
+template <int NP, int CG, typename Job, typename Epi>
+__device__ __forceinline__ void logits_roles(const Job& job, long long worker, long long workers,
+                                             Epi& epi) {
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ GemmShared sh;
+  uint8_t* stages = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
+                                               ~uintptr_t(1023));
+  if (blockIdx.x == 0 && threadIdx.x == 0) tc::set_report(job.err, job.rep);
+  gemm_begin<NP, CG>(sh);
+  const long long tiles = (long long)job.p.tm * job.p.tn;
+  const RunNext next{&job.p, run_begin(worker, tiles, workers),
+                     run_begin(worker + 1, tiles, workers)};
+  const int warp = threadIdx.x / 32, lane = threadIdx.x & 31;
+  bool ok = true;
+  if (warp == 0) {
+    if (lane == 0) ok = gemm_copy<NP, CG>(sh, stages, next, job.err);
+  } else if (warp == 1) {
+    if (lane == 0 && (CG == 1 || cluster_rank() == 0))
+      ok = gemm_multiply<NP, CG>(sh, stages, next, job.err);
+  } else if (warp >= 4) {
+    ok = gemm_finish<NP, CG>(sh, next, epi, job.err);
+  }
+  __syncwarp();
+  gemm_end<NP, CG>(sh, !ok);
+}
+
+template <int NP, int CG>
+__global__ void __launch_bounds__(kGemmThreads, 1)
+    k_loss_stats(const __grid_constant__ StatJob job) {
+  const long long worker = blockIdx.x / CG, workers = gridDim.x / CG;
+  StatEpi<NP, CG> epi(job, worker, workers);
+  logits_roles<NP, CG>(job, worker, workers, epi);
+  if (threadIdx.x >= 128) epi.flush();
+}
+
+template <int NP, int CG>
+__global__ void __launch_bounds__(kGemmThreads, 1)
+    k_loss_softmax(const __grid_constant__ SoftJob job) {
+  SoftEpi<NP, CG> epi(job);
+  logits_roles<NP, CG>(job, blockIdx.x / CG, gridDim.x / CG, epi);
+}
+
+// ------------------------------------------------------------------ join
+struct JoinJob {
+  const float2* part;
+  const float* zt;
+  const void* targets;
+  int i64;
+  long long ignore, N;
+  int V, tn, slots, tile_rows;
+  long long tiles, workers;
+  int lanes_log2;  // threads per row
+  float *loss, *lse;
+  float* block_sum;  // [blocks][2]
+  unsigned* done;
+  float* total;
+};
+
+// One row by 2^lanes_log2 threads: the partial statistics joined, the loss and
+// its log-sum; then the sums over rows, by block and, by the block that is done
+// last, over blocks in order.
+__global__ void __launch_bounds__(256) k_loss_join(JoinJob j) {
+  const int lanes = 1 << j.lanes_log2, lane = threadIdx.x & (lanes - 1);
+  const long long row = (long long)blockIdx.x * (256 >> j.lanes_log2) + (threadIdx.x >> j.lanes_log2);
+  const bool in = row < j.N;
+  float top = -INFINITY, sum = 0.0f;
+  if (in) {
+    const long long m = row / j.tile_rows;
+    const long long first = run_owner(m * j.tn, j.tiles, j.workers);
+    const long long last = run_owner(m * j.tn + j.tn - 1, j.tiles, j.workers);
+    const int n = (int)(last - first + 1) * 2;
+    for (int s = lane; s < n; s += lanes) {
+      const float2 a = j.part[((size_t)m * j.slots + s) * j.tile_rows + (row - m * j.tile_rows)];
+      const float t = fmaxf(top, a.x), base = t == -INFINITY ? 0.0f : t;
+      sum = sum * expf(top - base) + a.y * expf(a.x - base);
+      top = t;
+    }
+  }
+  for (int o = lanes >> 1; o; o >>= 1) {
+    const float ot = __shfl_xor_sync(0xffffffffu, top, o), os = __shfl_xor_sync(0xffffffffu, sum, o);
+    const float t = fmaxf(top, ot), base = t == -INFINITY ? 0.0f : t;
+    sum = sum * expf(top - base) + os * expf(ot - base);
+    top = t;
+  }
+  float loss = 0.0f, counted = 0.0f;
+  if (in && lane == 0) {
+    const float rest = top + logf(sum);  // log of the weight of every word but the target
+    const long long t = load_target(j.targets, j.i64, row);
+    float lse = rest;
+    if (t != j.ignore) {
+      counted = 1.0f;
+      if (t >= 0 && t < j.V) {
+        const float z = j.zt[row], d = rest - z;
+        if (rest == -INFINITY && z > -INFINITY) {  // the target is all there is
+          lse = z;
+        } else {
+          const float small = log1pf(expf(-fabsf(d)));
+          loss = d > 0.0f ? d + small : small;
+          lse = d > 0.0f ? rest + small : z + small;
+          if (d != d) lse = loss = d;
+        }
+      } else {
+        loss = __int_as_float(0x7fffffff);
+      }
+    }
+    j.loss[row] = loss;
+    j.lse[row] = lse;
+  }
+  // sums over the block's rows, in a fixed order
+  __shared__ float sl[8], sc[8];
+  __shared__ bool last;
+  float a = loss, b = counted;
+  for (int o = 16; o; o >>= 1) {
+    a += __shfl_xor_sync(0xffffffffu, a, o);
+    b += __shfl_xor_sync(0xffffffffu, b, o);
+  }
+  if ((threadIdx.x & 31) == 0) {
+    sl[threadIdx.x >> 5] = a;
+    sc[threadIdx.x >> 5] = b;
+  }
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    a = b = 0.0f;
+    for (int i = 0; i < 8; ++i) {
+      a += sl[i];
+      b += sc[i];
+    }
+    j.block_sum[2 * blockIdx.x] = a;
+    j.block_sum[2 * blockIdx.x + 1] = b;
+    __threadfence();
+    last = atomicAdd(j.done, 1u) == gridDim.x - 1;
+  }
+  __syncthreads();
+  if (!last) return;
+  __threadfence();
+  double da = 0.0, db = 0.0;
+  for (unsigned i = threadIdx.x; i < gridDim.x; i += 256) {
+    da += __ldcg(j.block_sum + 2 * i);
+    db += __ldcg(j.block_sum + 2 * i + 1);
+  }
+  __shared__ double dl[8], dc[8];
+  for (int o = 16; o; o >>= 1) {
+    da += __shfl_xor_sync(0xffffffffu, da, o);
+    db += __shfl_xor_sync(0xffffffffu, db, o);
+  }
+  if ((threadIdx.x & 31) == 0) {
+    dl[threadIdx.x >> 5] = da;
+    dc[threadIdx.x >> 5] = db;
+  }
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    da = db = 0.0;
+    for (int i = 0; i < 8; ++i) {
+      da += dl[i];
+      db += dc[i];
+    }
+    j.total[0] = (float)da;
+    j.total[1] = (float)db;
+  }
+}
+
+// ------------------------------------------------------------------ gradients
+// Tiles of two products in one list: dw's (long reductions) first, then dx's,
+// dealt out in turn.
+struct DealNext {
+  const Product *p0, *p1;
+  long long t, step, n0, n1;
+  __device__ bool operator()(const Product*& q, int& m, int& n) {
+    if (t >= n0 + n1) return false;
+    const bool second = t >= n0;
+    q = second ? p1 : p0;
+    const long long x = second ? t - n0 : t;
+    m = (int)(x / q->tn);
+    n = (int)(x % q->tn);
+    t += step;
+    return true;
+  }
+};
+
+struct GradJob {
+  Product dw, dx;
+  void *dw_out, *dx_out;   // the piece's rows of dw; dx
+  float* acc;              // [N][acc_ld] running sum of dx over pieces
+  int acc_ld;
+  int first, last;         // of the pieces
+  int f32;
+  const void* targets;
+  int i64;
+  long long ignore;
+  int* err;
+  unsigned* rep;
+};
+
+template <int NP, int CG>
+struct GradEpi {
+  using T = typename std::conditional<NP == 1, __nv_bfloat16, float>::type;
+  const GradJob& j;
+  const Product* p = nullptr;
+  int row = 0, col = 0;
+  bool in = false, is_dw = false, live = true;
+  __device__ explicit GradEpi(const GradJob& job) : j(job) {}
+  __device__ void begin(const Product& q, int m, int n, int r, int c) {
+    p = &q;
+    row = r;
+    col = c;
+    in = r < q.M;
+    is_dw = p == &j.dw;
+    live = true;
+    if (in && !is_dw && j.last) live = load_target(j.targets, j.i64, r) != j.ignore;
+  }
+  __device__ void chunk(int c, const float* v) {
+    if (!in) return;
+    const int D = p->N, left = D - (col + c);
+    const size_t at = (size_t)row * D + col + c;
+    float f[32];
+#pragma unroll
+    for (int i = 0; i < 32; ++i) f[i] = v[i];
+    if (!is_dw) {
+      float* acc = j.acc + (size_t)row * j.acc_ld + col + c;
+      if (!j.first) {
+#pragma unroll
+        for (int i = 0; i < 32; i += 4) {
+          if (i < left) {
+            const float4 o = *reinterpret_cast<const float4*>(acc + i);
+            f[i] += o.x;
+            f[i + 1] += o.y;
+            f[i + 2] += o.z;
+            f[i + 3] += o.w;
+          }
+        }
+      }
+      if (!j.last) {
+#pragma unroll
+        for (int i = 0; i < 32; i += 4)
+          if (i < left)
+            *reinterpret_cast<float4*>(acc + i) = make_float4(f[i], f[i + 1], f[i + 2], f[i + 3]);
+        return;
+      }
+      if (!live) {
+#pragma unroll
+        for (int i = 0; i < 32; ++i) f[i] = 0.0f;
+      }
+    }
+    T* out = static_cast<T*>(is_dw ? j.dw_out : j.dx_out) + at;
+    constexpr int W = 16 / sizeof(T);
+    if (left >= 32 && D % W == 0) {
+#pragma unroll
+      for (int i = 0; i < 32; i += W) {
+        uint4 u;
+        if (NP == 1)
+          u = make_uint4(tc::pack_bf16(f[i], f[i + 1]), tc::pack_bf16(f[i + 2], f[i + 3]),
+                         tc::pack_bf16(f[i + 4 * (NP == 1)], f[i + 5 * (NP == 1)]),
+                         tc::pack_bf16(f[i + 6 * (NP == 1)], f[i + 7 * (NP == 1)]));
+        else
+          u = make_uint4(__float_as_uint(f[i]), __float_as_uint(f[i + 1]),
+                         __float_as_uint(f[i + 2]), __float_as_uint(f[i + 3]));
+        *reinterpret_cast<uint4*>(out + i) = u;
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 32; ++i)
+        if (i < left) Io<T>::store(out, i, f[i]);
+    }
+  }
+  __device__ void end() {}
+};
+
+template <int NP, int CG>
+__global__ void __launch_bounds__(kGemmThreads, 1)
+    k_loss_grad(const __grid_constant__ GradJob job) {
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ GemmShared sh;
+  uint8_t* stages = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
+                                               ~uintptr_t(1023));
+  gemm_begin<NP, CG>(sh);
+  const DealNext next{&job.dw, &job.dx, blockIdx.x / CG, gridDim.x / CG,
+                      (long long)job.dw.tm * job.dw.tn, (long long)job.dx.tm * job.dx.tn};
+  const int warp = threadIdx.x / 32, lane = threadIdx.x & 31;
+  bool ok = true;
+  if (warp == 0) {
+    if (lane == 0) ok = gemm_copy<NP, CG>(sh, stages, next, job.err);
+  } else if (warp == 1) {
+    if (lane == 0 && (CG == 1 || cluster_rank() == 0))
+      ok = gemm_multiply<NP, CG>(sh, stages, next, job.err);
+  } else if (warp >= 4) {
+    GradEpi<NP, CG> epi(job);
+    ok = gemm_finish<NP, CG>(sh, next, epi, job.err);
+  }
+  __syncwarp();
+  gemm_end<NP, CG>(sh, !ok);
+}
+
+// ------------------------------------------------------------------ host
+struct Sizes {
+  long long N;
+  int D, V;
+  slim_dtype dtype;
+  int np() const { return dtype == SLIM_F32 ? 3 : 1; }
+  int ld() const { return (D + 7) / 8 * 8; }  // of a staged row
+  // bf16 rows that TMA can step over are read where they are
+  bool stage_w() const { return dtype == SLIM_F32 || D % 8 != 0; }
+  bool stage_x(bool bwd) const { return bwd || stage_w(); }
+};
+
+bool sizes_ok(long long N, int D, int V, slim_dtype dtype) {
+  if (N < 0 || N >= (1LL << 31) - 512 || D < 1 || V < 1 || V > (1 << 30)) return false;
+  if (dtype != SLIM_F32 && dtype != SLIM_BF16) return false;
+  return (long long)D <= (1LL << 40) / (N > 0 ? N : 1) && (long long)D <= (1LL << 40) / V;
+}
+
+int sm_count() {
+  static const int n = [] {
+    int dev = 0, v = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess ||
+        cudaDeviceGetAttribute(&v, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || v < 2)
+      v = 152;
+    cudaGetLastError();
+    return v;
+  }();
+  return n;
+}
+
+// Workspace sizes do not depend on the device: statistics of up to this many
+// workers.
+constexpr int kMaxWorkers = 152;
+int workers(int cg) {
+  const int n = sm_count() < kMaxWorkers ? sm_count() : kMaxWorkers;
+  return n / cg;
+}
+
+constexpr int CGv = 1;
+
+int cdiv(long long a, long long b) { return (int)((a + b - 1) / b); }
+
+// Partial statistics per row of a forward on `tm` x `tn` tiles.
+int stat_slots(long long tm, long long tn, long long w) {
+  long long s = w / tm + 2;
+  if (s > tn) s = tn;
+  if (s > w) s = w;
+  return (int)s * 2;
+}
+
+struct Ws {
+  int* header;        // error word, report address; [4]: the join's counter
+  __nv_bfloat16 *x, *w;
+  float2* part;
+  float *zt, *block_sum;
+  __nv_bfloat16* g;
+  float* acc;
+};
+constexpr size_t kHeaderInts = 32;
+
+int round_piece(int piece, int V) {
+  const long long p = ((long long)(piece < V ? piece : V) + kPieceStep - 1) / kPieceStep * kPieceStep;
+  return (int)p;
+}
+int acc_ld(int D) { return (D + 31) / 32 * 32; }
+
+Ws carve(Carver& cv, const Sizes& z, int piece, bool bwd) {
+  Ws w{};
+  const int np = z.np();
+  w.header = cv.take<int>(kHeaderInts);
+  if (z.stage_x(bwd)) w.x = cv.take<__nv_bfloat16>((size_t)np * z.N * z.ld());
+  if (z.stage_w()) w.w = cv.take<__nv_bfloat16>((size_t)np * z.V * z.ld());
+  if (!bwd) {
+    const int rows = kTM * CGv;
+    const long long tm = cdiv(z.N, rows), tn = cdiv(z.V, np == 1 ? 256 : 128);
+    w.part = cv.take<float2>((size_t)tm * stat_slots(tm, tn, kMaxWorkers / CGv) * rows);
+    w.zt = cv.take<float>(z.N);
+    w.block_sum = cv.take<float>(2 * (size_t)cdiv(z.N, 8));
+  } else {
+    const int p = round_piece(piece, z.V);
+    w.g = cv.take<__nv_bfloat16>((size_t)np * z.N * p);
+    if (p < z.V) w.acc = cv.take<float>((size_t)z.N * acc_ld(z.D));
+  }
+  return w;
+}
+
+// A tensor map over planes of [rows][cols] bf16 (row stride ld elements),
+// boxes of 64 columns x box_rows rows, 128-byte swizzle.
+bool plane_map(CUtensorMap* m, const __nv_bfloat16* base, long long rows, long long cols,
+               long long ld, long long plane, int np, int box_rows) {
+  const EncodeTiledFn fn = encode_tiled();
+  if (!fn) return false;
+  const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)np};
+  const cuuint64_t strides[2] = {(cuuint64_t)ld * 2, (cuuint64_t)plane * 2};
+  const cuuint32_t box[3] = {(cuuint32_t)kTK, (cuuint32_t)box_rows, 1};
+  const cuuint32_t es[3] = {1, 1, 1};
+  return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<__nv_bfloat16*>(base), dims, strides,
+            box, es, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+struct Planes {
+  const __nv_bfloat16* p;
+  long long rows, cols, ld, plane;
+};
+
+template <int NP, int CG>
+bool make_product(Product* p, const Planes& a, bool a_mn, const Planes& b, bool b_mn, long long M,
+                  long long N, long long K) {
+  using T = Tile<NP, CG>;
+  if (!plane_map(&p->a, a.p, a.rows, a.cols, a.ld, a.plane, NP, a_mn ? kTK : kTM) ||
+      !plane_map(&p->b, b.p, b.rows, b.cols, b.ld, b.plane, NP, b_mn ? kTK : T::BROWS))
+    return false;
+  p->a_mn = a_mn;
+  p->b_mn = b_mn;
+  p->M = (int)M;
+  p->N = (int)N;
+  p->tm = cdiv(M, kTM * CG);
+  p->tn = cdiv(N, T::N);
+  p->kb = cdiv(K, kTK);
+  // one chain for bf16 problems; 128 of the reduction (48 steps) for fp32 ones
+  p->chain = NP == 1 ? p->kb : 2 * T::PAIRS;
+  return true;
+}
+
+template <int NP>
+slim_status stage(const void* src, long long R, int D, int ld, const void* targets, slim_index it,
+                  long long ignore, __nv_bfloat16* dst, cudaStream_t s) {
+  using T = typename std::conditional<NP == 1, __nv_bfloat16, float>::type;
+  const long long n = R * (ld / 8);
+  const unsigned blocks = (unsigned)(cdiv(n, 256) < 152 * 16 ? cdiv(n, 256) : 152 * 16);
+  prof::Scope ps(prof::K_LOSS_PREP, s);
+  k_stage<T, NP><<<blocks, 256, 0, s>>>((const T*)src, R, D, ld, targets, it == SLIM_I64, ignore,
+                                        dst);
+  return cudaGetLastError() == cudaSuccess ? SLIM_OK : SLIM_ERR_CUDA;
+}
+
+// Launches a kernel of the tile products on `blocks` blocks, in pairs for CG = 2.
+template <int NP, int CG, typename Job>
+bool launch(void (*k)(Job), unsigned blocks, cudaStream_t s, const Job& job, bool* ready) {
+  constexpr size_t smem = Tile<NP, CG>::smem();
+  if (ready == nullptr || !*ready) {
+    if (cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) !=
+        cudaSuccess)
+      return false;
+    if (ready) *ready = true;
+  }
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(blocks);
+  cfg.blockDim = dim3(kGemmThreads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeClusterDimension;
+  at[0].val.clusterDim.x = CG;
+  at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = CG > 1 ? 1 : 0;
+  return cudaLaunchKernelEx(&cfg, k, job) == cudaSuccess;
+}
+
+template <typename T>
+bool* once() {
+  static bool flags[kMaxDevices];
+  return device_flag(flags);
+}
+
+template <int NP, int CG>
+slim_status fwd(const Sizes& z, const void* x, const void* w, const void* targets, slim_index it,
+                long long ignore, float* loss, float* lse, float* total, const Ws& ws,
+                unsigned* rep, cudaStream_t s) {
+  using T = Tile<NP, CG>;
+  const int ld = z.ld();
+  const __nv_bfloat16* xp = ws.x ? ws.x : static_cast<const __nv_bfloat16*>(x);
+  const __nv_bfloat16* wp = ws.w ? ws.w : static_cast<const __nv_bfloat16*>(w);
+  StatJob j{};
+  if (!make_product<NP, CG>(&j.p, Planes{xp, z.N, z.D, ld, z.N * ld}, false,
+                            Planes{wp, z.V, z.D, ld, (long long)z.V * ld}, false, z.N, z.V, z.D))
+    return SLIM_ERR_CUDA;
+  if (cudaMemsetAsync(ws.header, 0, kHeaderInts * sizeof(int), s) != cudaSuccess)
+    return SLIM_ERR_CUDA;
+  slim_status st;
+  if (ws.x && (st = stage<NP>(x, z.N, z.D, ld, nullptr, it, 0, ws.x, s)) != SLIM_OK) return st;
+  if (ws.w && (st = stage<NP>(w, z.V, z.D, ld, nullptr, it, 0, ws.w, s)) != SLIM_OK) return st;
+  const long long tiles = (long long)j.p.tm * j.p.tn;
+  const long long wk = tiles < workers(CG) ? tiles : workers(CG);
+  j.targets = targets;
+  j.i64 = it == SLIM_I64;
+  j.ignore = ignore;
+  j.V = z.V;
+  j.slots = stat_slots(j.p.tm, j.p.tn, wk);
+  j.part = ws.part;
+  j.zt = ws.zt;
+  j.err = ws.header;
+  j.rep = rep;
+  {
+    prof::Scope ps(prof::K_LOSS_STATS, s, 2.0 * z.N * z.D * z.V, ((double)z.N + z.V) * z.D * 2 * NP);
+    if (!launch<NP, CG>(k_loss_stats<NP, CG>, (unsigned)wk * CG, s, j, once<StatEpi<NP, CG>>()))
+      return SLIM_ERR_CUDA;
+  }
+  JoinJob q{};
+  q.part = ws.part;
+  q.zt = ws.zt;
+  q.targets = targets;
+  q.i64 = j.i64;
+  q.ignore = ignore;
+  q.N = z.N;
+  q.V = z.V;
+  q.tn = j.p.tn;
+  q.slots = j.slots;
+  q.tile_rows = kTM * CG;
+  q.tiles = tiles;
+  q.workers = wk;
+  while (q.lanes_log2 < 5 && (1 << q.lanes_log2) < j.slots) ++q.lanes_log2;
+  q.loss = loss;
+  q.lse = lse;
+  q.block_sum = ws.block_sum;
+  q.done = reinterpret_cast<unsigned*>(ws.header + 4);
+  q.total = total;
+  prof::Scope ps(prof::K_LOSS_JOIN, s);
+  k_loss_join<<<(unsigned)cdiv(z.N, 256 >> q.lanes_log2), 256, 0, s>>>(q);
+  return cudaGetLastError() == cudaSuccess ? SLIM_OK : SLIM_ERR_CUDA;
+}
+
+template <int NP, int CG>
+slim_status bwd(const Sizes& z, const void* x, const void* w, const void* targets, slim_index it,
+                long long ignore, const float* lse, const float* dloss, int dstride,
+                const float* count, int piece, void* dx, void* dw, const Ws& ws, unsigned* rep,
+                cudaStream_t s) {
+  using T = typename std::conditional<NP == 1, __nv_bfloat16, float>::type;
+  const int ld = z.ld(), ps = round_piece(piece, z.V);
+  const int pieces = cdiv(z.V, ps);
+  const __nv_bfloat16* wp = ws.w ? ws.w : static_cast<const __nv_bfloat16*>(w);
+  if (cudaMemsetAsync(ws.header, 0, kHeaderInts * sizeof(int), s) != cudaSuccess)
+    return SLIM_ERR_CUDA;
+  slim_status st = stage<NP>(x, z.N, z.D, ld, targets, it, ignore, ws.x, s);
+  if (st != SLIM_OK) return st;
+  if (ws.w && (st = stage<NP>(w, z.V, z.D, ld, nullptr, it, 0, ws.w, s)) != SLIM_OK) return st;
+  const Planes xm{ws.x, z.N, z.D, ld, z.N * ld};
+  for (int i = 0; i < pieces; ++i) {
+    const int v0 = i * ps, n = z.V - v0 < ps ? z.V - v0 : ps;
+    const Planes wm{wp + (size_t)v0 * ld, n, z.D, ld, (long long)z.V * ld};
+    const Planes gm{ws.g, z.N, n, ps, z.N * ps};
+    SoftJob j{};
+    GradJob q{};
+    if (!make_product<NP, CG>(&j.p, xm, false, wm, false, z.N, n, z.D) ||
+        !make_product<NP, CG>(&q.dw, gm, true, xm, true, n, z.D, z.N) ||
+        !make_product<NP, CG>(&q.dx, gm, false, wm, true, z.N, z.D, n))
+      return SLIM_ERR_CUDA;
+    j.targets = q.targets = targets;
+    j.i64 = q.i64 = it == SLIM_I64;
+    j.ignore = q.ignore = ignore;
+    j.V = z.V;
+    j.v0 = v0;
+    j.lse = lse;
+    j.dloss = dloss;
+    j.dstride = dstride;
+    j.count = count;
+    j.g = ws.g;
+    j.plane = z.N * ps;
+    j.ld = ps;
+    j.err = q.err = ws.header;
+    j.rep = q.rep = rep;
+    const double fl = 2.0 * z.N * z.D * n, gb = 2.0 * NP * z.N * n;
+    const long long tiles = (long long)j.p.tm * j.p.tn;
+    {
+      const long long wk = tiles < workers(CG) ? tiles : workers(CG);
+      prof::Scope sc(prof::K_LOSS_SOFTMAX, s, fl, ((double)z.N + n) * z.D * 2 * NP + gb);
+      if (!launch<NP, CG>(k_loss_softmax<NP, CG>, (unsigned)wk * CG, s, j, once<SoftEpi<NP, CG>>()))
+        return SLIM_ERR_CUDA;
+    }
+    q.dw_out = static_cast<T*>(dw) + (size_t)v0 * z.D;
+    q.dx_out = dx;
+    q.acc = ws.acc;
+    q.acc_ld = acc_ld(z.D);
+    q.first = i == 0;
+    q.last = i == pieces - 1;
+    const long long all = (long long)q.dw.tm * q.dw.tn + (long long)q.dx.tm * q.dx.tn;
+    const long long wk = all < workers(CG) ? all : workers(CG);
+    prof::Scope sc(prof::K_LOSS_GRAD, s, 2 * fl, ((double)z.N + n) * z.D * 2 * NP + 2 * gb);
+    if (!launch<NP, CG>(k_loss_grad<NP, CG>, (unsigned)wk * CG, s, q, once<GradEpi<NP, CG>>()))
+      return SLIM_ERR_CUDA;
+  }
+  return SLIM_OK;
+}
+
+bool aligned(const void* p, size_t to) {
+  return p != nullptr && (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0;
+}
+
+}  // namespace
+}  // namespace lm
+}  // namespace slim
+
+extern "C" slim_status slim_vocab_loss_workspace_size(long long N, int D, int V, slim_dtype dtype,
+                                                      int piece, int backward, size_t* bytes) {
+  using namespace slim::lm;
+  if (!bytes || !sizes_ok(N, D, V, dtype) || (backward && piece < 1)) return SLIM_ERR_INVALID_ARG;
+  slim::Carver cv(nullptr);
+  carve(cv, Sizes{N, D, V, dtype}, piece, backward != 0);
+  *bytes = cv.bytes();
+  return SLIM_OK;
+}
+
+extern "C" slim_status slim_vocab_loss_fwd(const void* x, const void* w, const void* targets,
+                                           slim_index itype, long long N, int D, int V,
+                                           slim_dtype dtype, long long ignore_index, float* loss,
+                                           float* lse, float* total, void* workspace,
+                                           size_t workspace_bytes, void* stream) {
+  using namespace slim::lm;
+  if (!sizes_ok(N, D, V, dtype) || (itype != SLIM_I32 && itype != SLIM_I64))
+    return SLIM_ERR_INVALID_ARG;
+  if (!aligned(w, 16) || !aligned(total, 4)) return SLIM_ERR_INVALID_ARG;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if (N == 0)
+    return cudaMemsetAsync(total, 0, 2 * sizeof(float), s) == cudaSuccess ? SLIM_OK : SLIM_ERR_CUDA;
+  if (!aligned(x, 16) || !aligned(targets, itype == SLIM_I64 ? 8 : 4) || !aligned(loss, 4) ||
+      !aligned(lse, 4))
+    return SLIM_ERR_INVALID_ARG;
+  size_t need = 0;
+  slim_vocab_loss_workspace_size(N, D, V, dtype, 1, 0, &need);
+  if (workspace == nullptr || workspace_bytes < need) return SLIM_ERR_WORKSPACE;
+  if (!aligned(workspace, 256)) return SLIM_ERR_INVALID_ARG;
+  unsigned* rep = nullptr;
+  const slim_status st = slim::report::begin(workspace, true, &rep);
+  if (st != SLIM_OK) return st;
+  const Sizes z{N, D, V, dtype};
+  slim::Carver cv(workspace);
+  const Ws ws = carve(cv, z, 1, false);
+  if (dtype == SLIM_BF16)
+    return fwd<1, CGv>(z, x, w, targets, itype, ignore_index, loss, lse, total, ws, rep, s);
+  return fwd<3, CGv>(z, x, w, targets, itype, ignore_index, loss, lse, total, ws, rep, s);
+}
+
+extern "C" slim_status slim_vocab_loss_bwd(const void* x, const void* w, const void* targets,
+                                           slim_index itype, const float* lse, const float* dloss,
+                                           int dloss_stride, const float* count, long long N, int D,
+                                           int V, slim_dtype dtype, int piece,
+                                           long long ignore_index, void* dx, void* dw,
+                                           void* workspace, size_t workspace_bytes, void* stream) {
+  using namespace slim::lm;
+  if (!sizes_ok(N, D, V, dtype) || (itype != SLIM_I32 && itype != SLIM_I64) || piece < 1 ||
+      (dloss_stride & ~1))
+    return SLIM_ERR_INVALID_ARG;
+  if (!aligned(w, 16) || !aligned(dw, 16) || (count && !aligned(count, 4)))
+    return SLIM_ERR_INVALID_ARG;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if (N == 0) {
+    const size_t n = (size_t)V * D * (dtype == SLIM_F32 ? 4 : 2);
+    return cudaMemsetAsync(dw, 0, n, s) == cudaSuccess ? SLIM_OK : SLIM_ERR_CUDA;
+  }
+  if (!aligned(x, 16) || !aligned(targets, itype == SLIM_I64 ? 8 : 4) || !aligned(lse, 4) ||
+      !aligned(dloss, 4) || !aligned(dx, 16))
+    return SLIM_ERR_INVALID_ARG;
+  size_t need = 0;
+  slim_vocab_loss_workspace_size(N, D, V, dtype, piece, 1, &need);
+  if (workspace == nullptr || workspace_bytes < need) return SLIM_ERR_WORKSPACE;
+  if (!aligned(workspace, 256)) return SLIM_ERR_INVALID_ARG;
+  unsigned* rep = nullptr;
+  const slim_status st = slim::report::begin(workspace, true, &rep);
+  if (st != SLIM_OK) return st;
+  const Sizes z{N, D, V, dtype};
+  slim::Carver cv(workspace);
+  const Ws ws = carve(cv, z, piece, true);
+  if (dtype == SLIM_BF16)
+    return bwd<1, CGv>(z, x, w, targets, itype, ignore_index, lse, dloss, dloss_stride, count,
+                       piece, dx, dw, ws, rep, s);
+  return bwd<3, CGv>(z, x, w, targets, itype, ignore_index, lse, dloss, dloss_stride, count, piece,
+                     dx, dw, ws, rep, s);
+}

@@ -35,6 +35,7 @@
 #include "common.cuh"
 #include "profiler.h"
 #include "tc_common.cuh"
+#include "tma_map.h"
 #include "tc_path.h"
 
 namespace slim {
@@ -2009,25 +2010,6 @@ cudaError_t configure() {
   return cudaSuccess;
 }
 
-// cuTensorMapEncodeTiled from the driver (through the runtime's entry-point
-// query, so the library needs no link against libcuda).
-using EncodeTiledFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*,
-                                   const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
-                                   const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
-                                   CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-EncodeTiledFn encode_tiled() {
-  static const EncodeTiledFn fn = [] {
-    void* p = nullptr;
-    cudaDriverEntryPointQueryResult q;
-    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault,
-                                         &q) != cudaSuccess ||
-        q != cudaDriverEntryPointSuccess)
-      p = nullptr;
-    cudaGetLastError();
-    return reinterpret_cast<EncodeTiledFn>(p);
-  }();
-  return fn;
-}
 // [chains][L][64] bf16 rows, 128 bytes each: box {64, 128, 1} (one row tile),
 // 128-byte swizzle; rows at or past L read as zero.
 bool rows_map(CUtensorMap* m, const void* base, int chains, int L) {

@@ -54,6 +54,10 @@ SIGNATURES = {
     "slim_embed_fwd": ([_p, _i, _p, _ll, _i, _i, _i, _f, _p, _p], _i),
     "slim_embed_bwd_workspace_size": ([_ll, _i, _i, _i, ctypes.POINTER(_sz)], _i),
     "slim_embed_bwd": ([_p, _i, _p, _ll, _i, _i, _i, _f, _i, _p, _p, _sz, _p], _i),
+    "slim_vocab_loss_workspace_size": ([_ll, _i, _i, _i, _i, _i, ctypes.POINTER(_sz)], _i),
+    "slim_vocab_loss_fwd": ([_p, _p, _p, _i, _ll, _i, _i, _i, _ll, _p, _p, _p, _p, _sz, _p], _i),
+    "slim_vocab_loss_bwd": ([_p, _p, _p, _i, _p, _p, _i, _p, _ll, _i, _i, _i, _i, _ll, _p, _p, _p,
+                             _sz, _p], _i),
     "slim_clip_workspace_size": ([_i, ctypes.POINTER(_sz)], _i),
     "slim_clip_grads": ([_p, _p, _p, _p, _i, _f, _p, _p, _sz, _p], _i),
 }
@@ -588,3 +592,101 @@ class Embedding(torch.autograd.Function):
 def embedding(ids, table, scale=1.0):
     """Differentiable embed_forward (gradient with respect to the table)."""
     return Embedding.apply(ids, table, scale)
+
+
+# Words per piece of the vocabulary in vocab_loss_backward, unless the caller
+# says otherwise.
+VOCAB_PIECE = 8192
+
+
+def vocab_loss_workspace_size(N, D, V, dtype, backward, piece=VOCAB_PIECE):
+    n = _sz(0)
+    _check(library().slim_vocab_loss_workspace_size(N, D, V, DTYPES[dtype], piece, int(backward),
+                                                    ctypes.byref(n)),
+           "slim_vocab_loss_workspace_size")
+    return n.value
+
+
+def _loss_dims(x, w, targets, what):
+    _require_cuda(x, w, targets)
+    _require_ids(targets, "targets")
+    _require_dtype(what, x, w)
+    _require(w.dim() == 2 and x.shape[-1] == w.shape[1], "x must be [..., D] and w [V, D]")
+    _require(tuple(x.shape[:-1]) == tuple(targets.shape), "targets must have one entry per row of x")
+    return targets.numel(), w.shape[1], w.shape[0]
+
+
+def vocab_loss_forward(x, w, targets, ignore_index=-100, workspace=None, stream=None):
+    """slim_vocab_loss_fwd: softmax cross entropy of the rows of x [..., D]
+    against the words w [V, D], without materialising the logits.  Returns
+    (loss, lse, total): per row the loss (0 where the target is ignore_index)
+    and the log-sum, both fp32 in targets' shape, and total = [sum of the
+    losses, number of rows not ignored]."""
+    N, D, V = _loss_dims(x, w, targets, "vocab_loss_forward")
+    with _on(stream):
+        loss = torch.empty(targets.shape, dtype=torch.float32, device=x.device)
+        lse = torch.empty_like(loss)
+        total = torch.empty(2, dtype=torch.float32, device=x.device)
+        ws = workspace if workspace is not None else _workspace(
+            vocab_loss_workspace_size(N, D, V, x.dtype, False), x.device)
+    _check(library().slim_vocab_loss_fwd(x.data_ptr(), w.data_ptr(), targets.data_ptr(),
+                                         INDEX_DTYPES[targets.dtype], N, D, V, DTYPES[x.dtype],
+                                         ignore_index, loss.data_ptr(), lse.data_ptr(),
+                                         total.data_ptr(), ws.data_ptr(), ws.numel(),
+                                         _stream_handle(stream)), "slim_vocab_loss_fwd")
+    return loss, lse, total
+
+
+def vocab_loss_backward(x, w, targets, lse, dloss, count=None, ignore_index=-100,
+                        piece=VOCAB_PIECE, workspace=None, stream=None):
+    """slim_vocab_loss_bwd: returns (dx, dw), the gradients of sum_i c_i loss_i,
+    c_i = dloss_i / count.  lse: from vocab_loss_forward on the same inputs.
+    dloss: fp32 on the device, one value per row or a single one for all rows.
+    count: None, or one fp32 value on the device (total[1:] of the forward for
+    the mean loss).  Memory grows with rows x piece."""
+    N, D, V = _loss_dims(x, w, targets, "vocab_loss_backward")
+    _require_cuda(lse, dloss)
+    _require(lse.dtype == torch.float32 and lse.numel() == N, "lse must be the forward's")
+    _require(dloss.dtype == torch.float32 and dloss.numel() in (1, N),
+             "dloss must be fp32, one value or one per row")
+    if count is not None:
+        _require_cuda(count)
+        _require(count.dtype == torch.float32 and count.numel() == 1, "count must be one fp32 value")
+    with _on(stream):
+        dx, dw = torch.empty_like(x), torch.empty_like(w)
+        ws = workspace if workspace is not None else _workspace(
+            vocab_loss_workspace_size(N, D, V, x.dtype, True, piece), x.device)
+    _check(library().slim_vocab_loss_bwd(x.data_ptr(), w.data_ptr(), targets.data_ptr(),
+                                         INDEX_DTYPES[targets.dtype], lse.data_ptr(),
+                                         dloss.data_ptr(), int(dloss.numel() > 1), _ptr(count), N,
+                                         D, V, DTYPES[x.dtype], piece, ignore_index, dx.data_ptr(),
+                                         dw.data_ptr(), ws.data_ptr(), ws.numel(),
+                                         _stream_handle(stream)), "slim_vocab_loss_bwd")
+    return dx, dw
+
+
+class VocabLoss(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, w, targets, reduction, ignore_index, piece):
+        x, w, targets = x.contiguous(), w.contiguous(), targets.contiguous()
+        loss, lse, total = vocab_loss_forward(x, w, targets, ignore_index)
+        ctx.save_for_backward(x, w, targets, lse, total)
+        ctx.mean, ctx.ignore_index, ctx.piece = reduction == "mean", ignore_index, piece
+        if reduction == "none":
+            return loss
+        return total[0] / total[1] if ctx.mean else total[0].clone()
+
+    @staticmethod
+    def backward(ctx, dloss):
+        x, w, targets, lse, total = ctx.saved_tensors
+        dx, dw = vocab_loss_backward(x, w, targets, lse, dloss.float().contiguous(),
+                                     count=total[1:] if ctx.mean else None,
+                                     ignore_index=ctx.ignore_index, piece=ctx.piece)
+        return dx, dw, None, None, None, None
+
+
+def vocab_loss(x, w, targets, reduction="mean", ignore_index=-100, piece=VOCAB_PIECE):
+    """Differentiable softmax cross entropy of x [..., D] against the words w
+    [V, D]; reduction "mean" (over the rows not ignored), "sum" or "none"."""
+    _require(reduction in ("mean", "sum", "none"), "reduction must be 'mean', 'sum' or 'none'")
+    return VocabLoss.apply(x, w, targets, reduction, ignore_index, piece)

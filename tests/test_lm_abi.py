@@ -66,6 +66,53 @@ def test_embed_no_tokens_enqueues_nothing(lib):
     assert embed_bwd(lib, N=0, ids=None, dout=None, acc=1, ws=None, nbytes=0) == OK
 
 
+# ---------------------------------------------------------------- vocabulary loss
+def loss_fwd(lib, x=FAKE, w=FAKE, t=FAKE, it=I64, N=4, D=8, V=16, dt=F32, loss=FAKE, lse=FAKE,
+             total=FAKE, ws=FAKE, nbytes=1 << 40):
+    return lib.slim_vocab_loss_fwd(x, w, t, it, N, D, V, dt, -100, loss, lse, total, ws, nbytes, None)
+
+
+def loss_bwd(lib, x=FAKE, w=FAKE, t=FAKE, it=I64, lse=FAKE, dloss=FAKE, stride=1, count=None, N=4,
+             D=8, V=16, dt=F32, piece=256, dx=FAKE, dw=FAKE, ws=FAKE, nbytes=1 << 40):
+    return lib.slim_vocab_loss_bwd(x, w, t, it, lse, dloss, stride, count, N, D, V, dt, piece, -100,
+                                   dx, dw, ws, nbytes, None)
+
+
+@pytest.mark.parametrize("kw", [dict(N=-1), dict(N=1 << 31), dict(D=0), dict(V=0), dict(V=1 << 30 | 1),
+                                dict(dt=2), dict(it=2), dict(x=None), dict(w=None), dict(t=None),
+                                dict(lse=None), dict(x=FAKE + 8), dict(w=FAKE + 8),
+                                dict(t=FAKE + 4), dict(it=I32, t=FAKE + 2), dict(lse=FAKE + 2),
+                                dict(ws=FAKE + 16)])
+def test_loss_rejects(lib, kw):
+    assert loss_fwd(lib, **kw) == INVALID
+    assert loss_bwd(lib, **kw) == INVALID
+
+
+def test_loss_rejects_more(lib):
+    for bad in (None, FAKE + 2):
+        assert loss_fwd(lib, loss=bad) == INVALID
+        assert loss_fwd(lib, total=bad) == INVALID
+        assert loss_bwd(lib, dloss=bad) == INVALID
+    assert loss_bwd(lib, dx=None) == INVALID and loss_bwd(lib, dw=FAKE + 8) == INVALID
+    assert loss_bwd(lib, stride=2) == INVALID and loss_bwd(lib, piece=0) == INVALID
+    assert loss_bwd(lib, count=FAKE + 1) == INVALID
+
+
+def test_loss_workspace(lib):
+    for bwd, call in ((False, loss_fwd), (True, loss_bwd)):
+        need = slim.vocab_loss_workspace_size(4, 8, 16, torch.float32, bwd, piece=256)
+        assert call(lib, nbytes=need - 1) == WORKSPACE
+        assert call(lib, ws=None) == WORKSPACE
+    assert lib.slim_vocab_loss_workspace_size(4, 8, 16, F32, 256, 1, None) == INVALID
+    assert lib.slim_vocab_loss_workspace_size(4, 8, 16, F32, 0, 1, ctypes.byref(ctypes.c_size_t())) == INVALID
+    # bf16 rows that need no staging: the forward keeps O(N), the backward N x piece
+    N, D, bf = 32768, 512, torch.bfloat16
+    size = lambda V, bwd, piece=8192: slim.vocab_loss_workspace_size(N, D, V, bf, bwd, piece)
+    assert size(65536, False) < 64 * N and size(16384, False) <= size(65536, False) * 1.1
+    assert size(65536, True) == size(32768, True)
+    assert size(65536, True, 16384) - size(65536, True) == 2 * N * 8192
+
+
 # ---------------------------------------------------------------- clipping
 def clip(lib, n=2, src=(FAKE, FAKE), dst=(FAKE, FAKE), numel=(8, 8), dts=(F32, BF16), max_norm=1.0,
          norm=FAKE, ws=FAKE, nbytes=1 << 40):
@@ -101,5 +148,7 @@ def test_binding_refuses_cpu_tensors():
         slim.embed_backward(torch.zeros(3, dtype=torch.long), torch.zeros(3, 8), 4)
     with pytest.raises(RuntimeError):
         slim.clip_grad_norm([torch.zeros(3)], 1.0)
+    with pytest.raises(RuntimeError):
+        slim.vocab_loss_forward(torch.zeros(3, 8), torch.zeros(4, 8), torch.zeros(3, dtype=torch.long))
     with pytest.raises(ValueError):
         slim.clip_grad_norm([], 1.0)
