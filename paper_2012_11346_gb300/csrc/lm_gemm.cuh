@@ -238,6 +238,10 @@ __device__ bool gemm_copy(GemmShared& sh, uint8_t* stages, Next next, int* err) 
       }
     }
   }
+  // every stage handed back: no arrival is on its way when the block leaves
+  for (int i = 0; i < T::STAGES; ++i, ++it)
+    if (!tc::mbar_wait(tc::smem_u32(&sh.empty[it % T::STAGES]), ((it / T::STAGES) & 1) ^ 1, err))
+      return false;
   return true;
 }
 

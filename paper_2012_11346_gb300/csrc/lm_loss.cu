@@ -115,19 +115,22 @@ struct StatJob {
   long long ignore;
   int V;
   int slots;       // partial statistics per row: 2 per worker that shares it
-  float2* part;    // [tm][slots][rows of a tile]: maximum, sum
+  float2* part;    // [tm][slots][rows of a tile]: base, sum of 2^(z log2 e - base)
   float* zt;       // [N] target logits
   int* err;
   unsigned* rep;
 };
 
-// (maximum, sum) of a row's logits but the target's, over a worker's run.
+// A row's logits but the target's, over a worker's run, as (base, sum): sum =
+// sum_v 2^(z_v log2 e - base), base the largest exponent so far.  The base is
+// kept as it was used, in units of log2, so that it means the same to every
+// term and to the join.
 template <int NP, int CG>
 struct StatEpi {
   const StatJob& j;
   long long worker, workers;
   int m_now = -1;
-  float top = -INFINITY, sum = 0.0f;
+  float base = -INFINITY, sum = 0.0f;
   int row = 0, col = 0, target = -1, slot_row = 0;
   __device__ StatEpi(const StatJob& job, long long w, long long ws)
       : j(job), worker(w), workers(ws) {}
@@ -135,7 +138,7 @@ struct StatEpi {
     if (m != m_now) {
       flush();
       m_now = m;
-      top = -INFINITY;
+      base = -INFINITY;
       sum = 0.0f;
       row = r;
       slot_row = r - m * kTM * CG;
@@ -165,16 +168,18 @@ struct StatEpi {
       for (int i = 0; i < 32; ++i)
         if (i >= left) z[i] = -INFINITY;
     }
-    float t = top;
+    float q[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-    for (int i = 0; i < 32; ++i) t = fmaxf(t, z[i]);
+    for (int i = 0; i < 32; ++i) q[i & 3] = fmaxf(q[i & 3], z[i]);
+    const float to = fmaxf(base, fmaxf(fmaxf(q[0], q[1]), fmaxf(q[2], q[3])) * kLog2e);
     // with nothing but -inf so far the sum stays 0: 2^(-inf - 0)
-    const float base = t == -INFINITY ? 0.0f : t * kLog2e;
-    float s = sum * exp2_of<NP>(top * kLog2e - base);
+    const float ref = to == -INFINITY ? 0.0f : to;
+    // 32 terms are added among themselves first: a run is tens of thousands long
+    float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-    for (int i = 0; i < 32; ++i) s += exp2_of<NP>(fmaf(z[i], kLog2e, -base));
-    top = t;
-    sum = s;
+    for (int i = 0; i < 32; ++i) s[i & 3] += exp2_of<NP>(fmaf(z[i], kLog2e, -ref));
+    sum = fmaf(sum, exp2_of<NP>(base - ref), (s[0] + s[1]) + (s[2] + s[3]));
+    base = to;
   }
   __device__ void end() {}
   __device__ void flush() {
@@ -182,7 +187,7 @@ struct StatEpi {
     const long long tiles = (long long)j.p.tm * j.p.tn;
     const int slot = (int)(worker - run_owner((long long)m_now * j.p.tn, tiles, workers)) * 2 +
                      (threadIdx.x / 32 - 4) / 4;
-    j.part[((size_t)m_now * j.slots + slot) * (kTM * CG) + slot_row] = make_float2(top, sum);
+    j.part[((size_t)m_now * j.slots + slot) * (kTM * CG) + slot_row] = make_float2(base, sum);
   }
 };
 
@@ -192,8 +197,7 @@ struct SoftJob {
   int i64;
   long long ignore;
   int V, v0;                  // vocabulary, and the piece's first word
-  const float *lse, *dloss, *count;
-  int dstride;
+  const float *lse, *dloss;   // dloss: per row, or null (1; the products are scaled)
   __nv_bfloat16* g;           // [NP][M][ld]
   long long plane;
   int ld;
@@ -201,12 +205,15 @@ struct SoftJob {
   unsigned* rep;
 };
 
-// g = c (exp(z - lse) - onehot), rounded to NP bf16 pieces.
+// g = c (exp(z - lse) - onehot), rounded to NP bf16 pieces.  A factor that all
+// rows share is left to the products' epilogues: rounded into g it would put the
+// same error on every row, and without it a target with little weight is -1
+// exactly.
 template <int NP, int CG>
 struct SoftEpi {
   const SoftJob& j;
   int row = 0, col = 0, target = -1;
-  float coef = 0.0f, lse2 = 0.0f;
+  float coef = 0.0f, lse = 0.0f;
   bool in = false, live = false;
   __device__ explicit SoftEpi(const SoftJob& job) : j(job) {}
   __device__ void begin(const Product& p, int m, int n, int r, int c) {
@@ -218,17 +225,12 @@ struct SoftEpi {
     if (!in) return;
     const long long t = load_target(j.targets, j.i64, r);
     live = t != j.ignore;
-    coef = j.dloss[(size_t)r * j.dstride];
-    if (j.count) {
-      const float k = *j.count;
-      if (k == 0.0f) live = false;
-      coef /= k;
-    }
+    coef = j.dloss ? j.dloss[r] : 1.0f;
     if (t >= 0 && t < j.V)
       target = (int)t - j.v0;
     else
       coef = __int_as_float(0x7fffffff);
-    lse2 = j.lse[r] * kLog2e;
+    lse = j.lse[r];
   }
   __device__ void chunk(int c, const float* v) {
     if (!in) return;
@@ -236,7 +238,7 @@ struct SoftEpi {
     float g[32];
 #pragma unroll
     for (int i = 0; i < 32; ++i) {
-      const float p = exp2_of<NP>(fmaf(v[i], kLog2e, -lse2));
+      const float p = NP == 1 ? tc::ex2_approx((v[i] - lse) * kLog2e) : expf(v[i] - lse);
       g[i] = live ? coef * (i == at ? p - 1.0f : p) : 0.0f;
     }
     __nv_bfloat16* dst = j.g + (size_t)row * j.ld + col + c;
@@ -319,7 +321,12 @@ __global__ void __launch_bounds__(256) k_loss_join(JoinJob j) {
   const int lanes = 1 << j.lanes_log2, lane = threadIdx.x & (lanes - 1);
   const long long row = (long long)blockIdx.x * (256 >> j.lanes_log2) + (threadIdx.x >> j.lanes_log2);
   const bool in = row < j.N;
-  float top = -INFINITY, sum = 0.0f;
+  float base = -INFINITY, sum = 0.0f;
+  auto add = [&](float b, float x) {
+    const float to = fmaxf(base, b), ref = to == -INFINITY ? 0.0f : to;
+    sum = sum * exp2f(base - ref) + x * exp2f(b - ref);
+    base = to;
+  };
   if (in) {
     const long long m = row / j.tile_rows;
     const long long first = run_owner(m * j.tn, j.tiles, j.workers);
@@ -327,26 +334,23 @@ __global__ void __launch_bounds__(256) k_loss_join(JoinJob j) {
     const int n = (int)(last - first + 1) * 2;
     for (int s = lane; s < n; s += lanes) {
       const float2 a = j.part[((size_t)m * j.slots + s) * j.tile_rows + (row - m * j.tile_rows)];
-      const float t = fmaxf(top, a.x), base = t == -INFINITY ? 0.0f : t;
-      sum = sum * expf(top - base) + a.y * expf(a.x - base);
-      top = t;
+      add(a.x, a.y);
     }
   }
-  for (int o = lanes >> 1; o; o >>= 1) {
-    const float ot = __shfl_xor_sync(0xffffffffu, top, o), os = __shfl_xor_sync(0xffffffffu, sum, o);
-    const float t = fmaxf(top, ot), base = t == -INFINITY ? 0.0f : t;
-    sum = sum * expf(top - base) + os * expf(ot - base);
-    top = t;
-  }
+  for (int o = lanes >> 1; o; o >>= 1)
+    add(__shfl_xor_sync(0xffffffffu, base, o), __shfl_xor_sync(0xffffffffu, sum, o));
   float loss = 0.0f, counted = 0.0f;
   if (in && lane == 0) {
-    const float rest = top + logf(sum);  // log of the weight of every word but the target
+    // log of the weight of every word but the target: a base of some tens and a
+    // logarithm, joined in fp64 so that only the result is rounded
+    const double rest64 = ((double)base + (double)log2f(sum)) * 0.69314718055994531;
+    const float rest = (float)rest64;
     const long long t = load_target(j.targets, j.i64, row);
     float lse = rest;
     if (t != j.ignore) {
       counted = 1.0f;
       if (t >= 0 && t < j.V) {
-        const float z = j.zt[row], d = rest - z;
+        const float z = j.zt[row], d = (float)(rest64 - (double)z);
         if (rest == -INFINITY && z > -INFINITY) {  // the target is all there is
           lse = z;
         } else {
@@ -439,7 +443,7 @@ struct GradJob {
   float* acc;              // [N][acc_ld] running sum of dx over pieces
   int acc_ld;
   int first, last;         // of the pieces
-  int f32;
+  const float *scale, *count;  // the results' factor: (scale or 1) / (count or 1)
   const void* targets;
   int i64;
   long long ignore;
@@ -454,7 +458,11 @@ struct GradEpi {
   const Product* p = nullptr;
   int row = 0, col = 0;
   bool in = false, is_dw = false, live = true;
-  __device__ explicit GradEpi(const GradJob& job) : j(job) {}
+  float scale = 1.0f;
+  __device__ explicit GradEpi(const GradJob& job) : j(job) {
+    if (j.scale) scale = *j.scale;
+    if (j.count) scale = *j.count == 0.0f ? 0.0f : scale / *j.count;
+  }
   __device__ void begin(const Product& q, int m, int n, int r, int c) {
     p = &q;
     row = r;
@@ -492,11 +500,9 @@ struct GradEpi {
             *reinterpret_cast<float4*>(acc + i) = make_float4(f[i], f[i + 1], f[i + 2], f[i + 3]);
         return;
       }
-      if (!live) {
-#pragma unroll
-        for (int i = 0; i < 32; ++i) f[i] = 0.0f;
-      }
     }
+#pragma unroll
+    for (int i = 0; i < 32; ++i) f[i] = live ? f[i] * scale : 0.0f;
     T* out = static_cast<T*>(is_dw ? j.dw_out : j.dx_out) + at;
     constexpr int W = 16 / sizeof(T);
     if (left >= 32 && D % W == 0) {
@@ -584,7 +590,7 @@ int workers(int cg) {
   return n / cg;
 }
 
-constexpr int CGv = 1;
+constexpr int CGv = 2;
 
 int cdiv(long long a, long long b) { return (int)((a + b - 1) / b); }
 
@@ -801,9 +807,9 @@ slim_status bwd(const Sizes& z, const void* x, const void* w, const void* target
     j.V = z.V;
     j.v0 = v0;
     j.lse = lse;
-    j.dloss = dloss;
-    j.dstride = dstride;
-    j.count = count;
+    j.dloss = dstride ? dloss : nullptr;
+    q.scale = dstride ? nullptr : dloss;
+    q.count = count;
     j.g = ws.g;
     j.plane = z.N * ps;
     j.ld = ps;
