@@ -26,8 +26,11 @@ constexpr int kTK = 64;   // reduction per stage
 constexpr int kGemmThreads = 384;  // warps: TMA, MMA, TMEM, spare, 8 of epilogue
 constexpr int kEpiWarps = 8;
 
-template <int NP, int CG>
+// OUT: bytes of shared memory per epilogue warp from which it stores by TMA.
+constexpr int kSmemBytes = 227 * 1024 - 1024 - 512;  // after alignment and barriers
+template <int NP, int CG, int OUT = 0>
 struct Tile {
+  static constexpr int PLANES = NP, GROUP = CG;
   // With three planes the epilogue holds a tile's sums in registers: half the
   // columns, 64 per thread.
   static constexpr int N = NP == 1 ? 256 : 128;
@@ -35,9 +38,11 @@ struct Tile {
   static constexpr int BROWS = N / CG;    // rows of B that a block holds
   static constexpr int A_BYTES = kTM * kTK * 2, B_BYTES = BROWS * kTK * 2;
   static constexpr int STAGE = A_BYTES + B_BYTES;
-  static constexpr int STAGES = 192 * 1024 / STAGE < 8 ? 192 * 1024 / STAGE : 8;
+  static constexpr int FIT = (kSmemBytes - kEpiWarps * OUT) / STAGE;
+  static constexpr int STAGES = FIT < 8 ? FIT : 8;
   static constexpr int PAIRS = NP == 1 ? 1 : 6;
-  static constexpr size_t smem() { return 1024 + (size_t)STAGES * STAGE; }
+  static constexpr int OUT_BYTES = OUT;
+  static constexpr size_t smem() { return 1024 + (size_t)STAGES * STAGE + kEpiWarps * OUT; }
 };
 
 // One product: D [M, N] = sum over K of A and B.
@@ -161,9 +166,9 @@ __device__ __forceinline__ void plane_pair(int i, int& pa, int& pb) {
 }
 
 // Sets the ring up and allocates TMEM; every thread of the block (of the pair).
-template <int NP, int CG>
+template <typename T>
 __device__ __forceinline__ void gemm_begin(GemmShared& sh) {
-  using T = Tile<NP, CG>;
+  constexpr int CG = T::GROUP;
   if (threadIdx.x == 0) {
     for (int i = 0; i < T::STAGES; ++i) {
       tc::mbar_init(tc::smem_u32(&sh.full[i]), 1);
@@ -184,8 +189,9 @@ __device__ __forceinline__ void gemm_begin(GemmShared& sh) {
   tc::tc_fence_after();
 }
 
-template <int NP, int CG>
+template <typename T>
 __device__ __forceinline__ void gemm_end(GemmShared& sh, bool failed) {
+  constexpr int CG = T::GROUP;
   // a role that gave up may leave copies in flight: let them land
   if (failed)
     for (int i = 0; i < 1000; ++i) __nanosleep(10000);
@@ -194,14 +200,14 @@ __device__ __forceinline__ void gemm_end(GemmShared& sh, bool failed) {
     __syncthreads();
   else
     cluster_sync();
-  if (threadIdx.x / 32 == 2) gemm_tmem_free<CG>(sh.tmem, 2 * Tile<NP, CG>::N);
+  if (threadIdx.x / 32 == 2) gemm_tmem_free<CG>(sh.tmem, 2 * T::N);
 }
 
 // The copying thread.  `next(p, m, n)` yields this worker's tiles in order:
 // the same sequence in every role.  False if a wait gave up.
-template <int NP, int CG, typename Next>
+template <typename T, typename Next>
 __device__ bool gemm_copy(GemmShared& sh, uint8_t* stages, Next next, int* err) {
-  using T = Tile<NP, CG>;
+  constexpr int NP = T::PLANES, CG = T::GROUP;
   const uint32_t rank = CG == 1 ? 0 : cluster_rank();
   const Product* p;
   int m, n;
@@ -246,9 +252,9 @@ __device__ bool gemm_copy(GemmShared& sh, uint8_t* stages, Next next, int* err) 
 }
 
 // The thread that issues MMAs (of the leading block of a pair).
-template <int NP, int CG, typename Next>
+template <typename T, typename Next>
 __device__ bool gemm_multiply(GemmShared& sh, uint8_t* stages, Next next, int* err) {
-  using T = Tile<NP, CG>;
+  constexpr int CG = T::GROUP;
   const Product* p;
   int m, n;
   uint32_t it = 0, acc = 0;
@@ -284,9 +290,9 @@ __device__ bool gemm_multiply(GemmShared& sh, uint8_t* stages, Next next, int* e
 // epi.chunk(c, v) for each 32 columns col0 + c .. of row `row` (of this thread)
 // that lie inside the product, then epi.end().  Reads past the product's rows
 // still run (their values are zero sums); the epilogue drops them.
-template <int NP, int CG, typename Next, typename Epi>
+template <typename T, typename Next, typename Epi>
 __device__ bool gemm_finish(GemmShared& sh, Next next, Epi& epi, int* err) {
-  using T = Tile<NP, CG>;
+  constexpr int NP = T::PLANES, CG = T::GROUP;
   const uint32_t rank = CG == 1 ? 0 : cluster_rank();
   const int w = threadIdx.x / 32 - 4, lane = threadIdx.x & 31;
   const int quarter = w & 3, half = w >> 2;
@@ -333,6 +339,74 @@ __device__ bool gemm_finish(GemmShared& sh, Next next, Epi& epi, int* err) {
     epi.end();
   }
   return true;
+}
+
+// All roles of a kernel's block.  Epi is made by the caller; workers iterate with
+// `next`.
+template <typename T, typename Next, typename Epi>
+__device__ __forceinline__ void gemm_roles(GemmShared& sh, uint8_t* stages, const Next& next,
+                                           Epi& epi, int* err) {
+  gemm_begin<T>(sh);
+  const int warp = threadIdx.x / 32, lane = threadIdx.x & 31;
+  bool ok = true;
+  if (warp == 0) {
+    if (lane == 0) ok = gemm_copy<T>(sh, stages, next, err);
+  } else if (warp == 1) {
+    if (lane == 0 && (T::GROUP == 1 || cluster_rank() == 0))
+      ok = gemm_multiply<T>(sh, stages, next, err);
+  } else if (warp >= 4) {
+    ok = gemm_finish<T>(sh, next, epi, err);
+  }
+  __syncwarp();
+  gemm_end<T>(sh, !ok);
+}
+
+// ------------------------------------------------------------------ output boxes
+// An epilogue warp's 32 rows x 32 columns go out as one box: every lane writes
+// its row's 16-byte pieces into shared memory, swizzled so that eight lanes fill
+// all banks, and one lane starts the copy.  A row-by-row store from registers
+// would touch 32 lines with every instruction.
+//   bf16: rows of 64 bytes, 64-byte swizzle;  fp32: 128 bytes, 128-byte swizzle.
+__device__ __forceinline__ uint32_t box_piece16(int row, int c) {  // bf16, c in 0..3
+  return (uint32_t)(row * 64 + ((c ^ ((row >> 1) & 3)) << 4));
+}
+__device__ __forceinline__ uint32_t box_piece32(int row, int c) {  // fp32, c in 0..7
+  return (uint32_t)(row * 128 + ((c ^ (row & 7)) << 4));
+}
+// Before a box in shared memory is written again: all but the newest KEEP
+// groups of this lane's stores have read theirs.
+template <int KEEP>
+__device__ __forceinline__ void box_reuse() {
+  if ((threadIdx.x & 31) == 0)
+    asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(KEEP) : "memory");
+  __syncwarp();
+}
+__device__ __forceinline__ void box_written() {
+  tc::fence_async_smem();
+  __syncwarp();
+}
+// By one lane: stores (or adds, fp32) a box, and closes a group.
+__device__ __forceinline__ void box_store(const CUtensorMap* map, uint32_t src, int x, int y,
+                                          int z) {
+  asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%1, %2, %3}], [%4];" ::
+                   "l"(reinterpret_cast<uint64_t>(map)),
+               "r"(x), "r"(y), "r"(z), "r"(src)
+               : "memory");
+}
+__device__ __forceinline__ void box_add(const CUtensorMap* map, uint32_t src, int x, int y, int z) {
+  asm volatile(
+      "cp.reduce.async.bulk.tensor.3d.global.shared::cta.add.bulk_group [%0, {%1, %2, %3}], "
+      "[%4];" ::"l"(reinterpret_cast<uint64_t>(map)),
+      "r"(x), "r"(y), "r"(z), "r"(src)
+      : "memory");
+}
+__device__ __forceinline__ void box_commit() {
+  asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+}
+// The lane's stores are complete.
+__device__ __forceinline__ void box_drain() {
+  if ((threadIdx.x & 31) == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+  __syncwarp();
 }
 
 }  // namespace lm

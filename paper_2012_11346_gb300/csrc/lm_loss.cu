@@ -198,9 +198,7 @@ struct SoftJob {
   long long ignore;
   int V, v0;                  // vocabulary, and the piece's first word
   const float *lse, *dloss;   // dloss: per row, or null (1; the products are scaled)
-  __nv_bfloat16* g;           // [NP][M][ld]
-  long long plane;
-  int ld;
+  CUtensorMap g;              // planes of g, boxes of 32 x 32
   int* err;
   unsigned* rep;
 };
@@ -215,33 +213,50 @@ struct SoftEpi {
   int row = 0, col = 0, target = -1;
   float coef = 0.0f, lse = 0.0f;
   bool in = false, live = false;
-  __device__ explicit SoftEpi(const SoftJob& job) : j(job) {}
+  uint8_t* box;  // this warp's output boxes
+  uint32_t turn = 0;
+  static constexpr int kBox = 2048, kBoxes = NP == 1 ? 4 : 3, kOut = kBoxes * kBox;
+  __device__ SoftEpi(const SoftJob& job, uint8_t* b) : j(job), box(b) {}
   __device__ void begin(const Product& p, int m, int n, int r, int c) {
     row = r;
     col = c;
     in = r < p.M;
     live = false;
     target = -1;
+    coef = 0.0f;
+    lse = INFINITY;  // exp(z - inf) = 0: nothing from rows that are ignored
     if (!in) return;
     const long long t = load_target(j.targets, j.i64, r);
-    live = t != j.ignore;
+    if (t == j.ignore) return;
+    live = true;
+    lse = j.lse[r];
     coef = j.dloss ? j.dloss[r] : 1.0f;
     if (t >= 0 && t < j.V)
       target = (int)t - j.v0;
     else
       coef = __int_as_float(0x7fffffff);
-    lse = j.lse[r];
   }
   __device__ void chunk(int c, const float* v) {
-    if (!in) return;
-    const int at = target - (col + c);
+    const int at = target - (col + c), lane = threadIdx.x & 31;
     float g[32];
+    if (NP == 1) {
+      const float l2 = lse * kLog2e;
 #pragma unroll
-    for (int i = 0; i < 32; ++i) {
-      const float p = NP == 1 ? tc::ex2_approx((v[i] - lse) * kLog2e) : expf(v[i] - lse);
-      g[i] = live ? coef * (i == at ? p - 1.0f : p) : 0.0f;
+      for (int i = 0; i < 32; ++i) g[i] = tc::ex2_approx(fmaf(v[i], kLog2e, -l2));
+    } else {
+#pragma unroll
+      for (int i = 0; i < 32; ++i) g[i] = expf(v[i] - lse);
     }
-    __nv_bfloat16* dst = j.g + (size_t)row * j.ld + col + c;
+    if (live && at >= 0 && at < 32) {
+#pragma unroll
+      for (int i = 0; i < 32; ++i)
+        if (i == at) g[i] -= 1.0f;
+    }
+#pragma unroll
+    for (int i = 0; i < 32; ++i) g[i] = live ? g[i] * coef : 0.0f;
+    // NP = 1: four boxes in turn; NP = 3: the planes' three at once
+    box_reuse<NP == 1 ? kBoxes - 1 : 0>();
+    uint8_t* to = box + (NP == 1 ? (turn++ % kBoxes) * kBox : 0);
 #pragma unroll
     for (int q = 0; q < NP; ++q) {
 #pragma unroll
@@ -249,53 +264,62 @@ struct SoftEpi {
         uint32_t u[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) u[e] = take_plane<NP>(g[i + 2 * e], g[i + 2 * e + 1]);
-        *reinterpret_cast<uint4*>(dst + q * j.plane + i) = make_uint4(u[0], u[1], u[2], u[3]);
+        *reinterpret_cast<uint4*>(to + q * kBox + box_piece16(lane, i / 8)) =
+            make_uint4(u[0], u[1], u[2], u[3]);
       }
+    }
+    box_written();
+    if (lane == 0 && in) {
+#pragma unroll
+      for (int q = 0; q < NP; ++q)
+        box_store(&j.g, tc::smem_u32(to + q * kBox), col + c, row, q);
+      box_commit();
     }
   }
   __device__ void end() {}
 };
 
-template <int NP, int CG, typename Job, typename Epi>
-__device__ __forceinline__ void logits_roles(const Job& job, long long worker, long long workers,
-                                             Epi& epi) {
+template <typename T>
+__device__ __forceinline__ uint8_t* stage_memory() {
   extern __shared__ uint8_t smem_raw[];
-  __shared__ GemmShared sh;
-  uint8_t* stages = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
-                                               ~uintptr_t(1023));
-  if (blockIdx.x == 0 && threadIdx.x == 0) tc::set_report(job.err, job.rep);
-  gemm_begin<NP, CG>(sh);
-  const long long tiles = (long long)job.p.tm * job.p.tn;
-  const RunNext next{&job.p, run_begin(worker, tiles, workers),
-                     run_begin(worker + 1, tiles, workers)};
-  const int warp = threadIdx.x / 32, lane = threadIdx.x & 31;
-  bool ok = true;
-  if (warp == 0) {
-    if (lane == 0) ok = gemm_copy<NP, CG>(sh, stages, next, job.err);
-  } else if (warp == 1) {
-    if (lane == 0 && (CG == 1 || cluster_rank() == 0))
-      ok = gemm_multiply<NP, CG>(sh, stages, next, job.err);
-  } else if (warp >= 4) {
-    ok = gemm_finish<NP, CG>(sh, next, epi, job.err);
-  }
-  __syncwarp();
-  gemm_end<NP, CG>(sh, !ok);
+  return reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
+                                    ~uintptr_t(1023));
 }
+// The epilogue warp's output boxes, behind the stages.
+template <typename T>
+__device__ __forceinline__ uint8_t* out_memory(uint8_t* stages) {
+  return stages + T::STAGES * T::STAGE + ((int)(threadIdx.x / 32) - 4) * T::OUT_BYTES;
+}
+template <int CG>
+__device__ __forceinline__ RunNext run_of(const Product& p) {
+  const long long tiles = (long long)p.tm * p.tn, worker = blockIdx.x / CG, workers = gridDim.x / CG;
+  return RunNext{&p, run_begin(worker, tiles, workers), run_begin(worker + 1, tiles, workers)};
+}
+
+template <int NP, int CG> using StatTile = Tile<NP, CG>;
+template <int NP, int CG> using SoftTile = Tile<NP, CG, SoftEpi<NP, CG>::kOut>;
 
 template <int NP, int CG>
 __global__ void __launch_bounds__(kGemmThreads, 1)
     k_loss_stats(const __grid_constant__ StatJob job) {
-  const long long worker = blockIdx.x / CG, workers = gridDim.x / CG;
-  StatEpi<NP, CG> epi(job, worker, workers);
-  logits_roles<NP, CG>(job, worker, workers, epi);
+  using T = StatTile<NP, CG>;
+  __shared__ GemmShared sh;
+  if (blockIdx.x == 0 && threadIdx.x == 0) tc::set_report(job.err, job.rep);
+  StatEpi<NP, CG> epi(job, blockIdx.x / CG, gridDim.x / CG);
+  gemm_roles<T>(sh, stage_memory<T>(), run_of<CG>(job.p), epi, job.err);
   if (threadIdx.x >= 128) epi.flush();
 }
 
 template <int NP, int CG>
 __global__ void __launch_bounds__(kGemmThreads, 1)
     k_loss_softmax(const __grid_constant__ SoftJob job) {
-  SoftEpi<NP, CG> epi(job);
-  logits_roles<NP, CG>(job, blockIdx.x / CG, gridDim.x / CG, epi);
+  using T = SoftTile<NP, CG>;
+  __shared__ GemmShared sh;
+  if (blockIdx.x == 0 && threadIdx.x == 0) tc::set_report(job.err, job.rep);
+  uint8_t* stages = stage_memory<T>();
+  SoftEpi<NP, CG> epi(job, out_memory<T>(stages));
+  gemm_roles<T>(sh, stages, run_of<CG>(job.p), epi, job.err);
+  if (threadIdx.x >= 128) box_drain();
 }
 
 // ------------------------------------------------------------------ join
@@ -420,26 +444,37 @@ __global__ void __launch_bounds__(256) k_loss_join(JoinJob j) {
 }
 
 // ------------------------------------------------------------------ gradients
-// Tiles of two products in one list: dw's (long reductions) first, then dx's,
-// dealt out in turn.
+// A worker's tiles of the two products: a contiguous range of each, dealt on the
+// host so that the workers' reductions come out even.
+constexpr int kMaxWorkers = 152;
+struct Deal {
+  unsigned lo[2][kMaxWorkers + 1];
+};
 struct DealNext {
-  const Product *p0, *p1;
-  long long t, step, n0, n1;
+  const Product* p[2];
+  unsigned t, end0, t1, end1;
+  int which;
   __device__ bool operator()(const Product*& q, int& m, int& n) {
-    if (t >= n0 + n1) return false;
-    const bool second = t >= n0;
-    q = second ? p1 : p0;
-    const long long x = second ? t - n0 : t;
-    m = (int)(x / q->tn);
-    n = (int)(x % q->tn);
-    t += step;
+    if (which == 0 && t >= end0) {
+      which = 1;
+      t = t1;
+    }
+    if (which == 1 && t >= end1) return false;
+    q = which ? p[1] : p[0];
+    m = (int)(t / q->tn);
+    n = (int)(t % q->tn);
+    ++t;
     return true;
   }
 };
 
 struct GradJob {
-  Product dw, dx;
-  void *dw_out, *dx_out;   // the piece's rows of dw; dx
+  Product p[2];            // dw of the piece's words, and dx
+  CUtensorMap out[2];      // their results, boxes of 32 x 32 (where `boxes`)
+  CUtensorMap sum;         // the running sum of dx, fp32
+  Deal deal;
+  void* to[2];
+  int boxes;               // rows that TMA can step over
   float* acc;              // [N][acc_ld] running sum of dx over pieces
   int acc_ld;
   int first, last;         // of the pieces
@@ -454,12 +489,15 @@ struct GradJob {
 template <int NP, int CG>
 struct GradEpi {
   using T = typename std::conditional<NP == 1, __nv_bfloat16, float>::type;
+  static constexpr int kBox = 4096, kBoxes = 2, kOut = kBoxes * kBox;
   const GradJob& j;
+  uint8_t* box;
+  uint32_t turn = 0;
   const Product* p = nullptr;
-  int row = 0, col = 0;
-  bool in = false, is_dw = false, live = true;
+  int row = 0, col = 0, which = 0;
+  bool in = false, live = true;
   float scale = 1.0f;
-  __device__ explicit GradEpi(const GradJob& job) : j(job) {
+  __device__ GradEpi(const GradJob& job, uint8_t* b) : j(job), box(b) {
     if (j.scale) scale = *j.scale;
     if (j.count) scale = *j.count == 0.0f ? 0.0f : scale / *j.count;
   }
@@ -468,57 +506,74 @@ struct GradEpi {
     row = r;
     col = c;
     in = r < q.M;
-    is_dw = p == &j.dw;
+    which = p == &j.p[1];
     live = true;
-    if (in && !is_dw && j.last) live = load_target(j.targets, j.i64, r) != j.ignore;
+    if (in && which == 1 && j.last) live = load_target(j.targets, j.i64, r) != j.ignore;
+  }
+  // 32 fp32 values of every lane's row into a box
+  __device__ uint8_t* put32(const float* f) {
+    const int lane = threadIdx.x & 31;
+    box_reuse<kBoxes - 1>();
+    uint8_t* to = box + (turn++ % kBoxes) * kBox;
+#pragma unroll
+    for (int i = 0; i < 32; i += 4)
+      *reinterpret_cast<float4*>(to + box_piece32(lane, i / 4)) =
+          make_float4(f[i], f[i + 1], f[i + 2], f[i + 3]);
+    box_written();
+    return to;
+  }
+  __device__ uint8_t* put16(const float* f) {
+    const int lane = threadIdx.x & 31;
+    box_reuse<kBoxes - 1>();
+    uint8_t* to = box + (turn++ % kBoxes) * kBox;
+#pragma unroll
+    for (int i = 0; i < 32; i += 8)
+      *reinterpret_cast<uint4*>(to + box_piece16(lane, i / 8)) =
+          make_uint4(tc::pack_bf16(f[i], f[i + 1]), tc::pack_bf16(f[i + 2], f[i + 3]),
+                     tc::pack_bf16(f[i + 4], f[i + 5]), tc::pack_bf16(f[i + 6], f[i + 7]));
+    box_written();
+    return to;
   }
   __device__ void chunk(int c, const float* v) {
-    if (!in) return;
-    const int D = p->N, left = D - (col + c);
-    const size_t at = (size_t)row * D + col + c;
+    const int D = p->N, left = D - (col + c), lane = threadIdx.x & 31;
     float f[32];
 #pragma unroll
     for (int i = 0; i < 32; ++i) f[i] = v[i];
-    if (!is_dw) {
-      float* acc = j.acc + (size_t)row * j.acc_ld + col + c;
-      if (!j.first) {
+    if (which == 1) {
+      if (!j.last) {
+        // the pieces' sums of dx, added where they lie; a launch adds once
+        uint8_t* b = put32(f);
+        if (lane == 0 && in) {
+          if (j.first)
+            box_store(&j.sum, tc::smem_u32(b), col + c, row, 0);
+          else
+            box_add(&j.sum, tc::smem_u32(b), col + c, row, 0);
+          box_commit();
+        }
+        return;
+      }
+      if (!j.first && in) {
+        const float* acc = j.acc + (size_t)row * j.acc_ld + col + c;
 #pragma unroll
         for (int i = 0; i < 32; i += 4) {
-          if (i < left) {
-            const float4 o = *reinterpret_cast<const float4*>(acc + i);
-            f[i] += o.x;
-            f[i + 1] += o.y;
-            f[i + 2] += o.z;
-            f[i + 3] += o.w;
-          }
+          const float4 o = *reinterpret_cast<const float4*>(acc + i);
+          f[i] += o.x;
+          f[i + 1] += o.y;
+          f[i + 2] += o.z;
+          f[i + 3] += o.w;
         }
-      }
-      if (!j.last) {
-#pragma unroll
-        for (int i = 0; i < 32; i += 4)
-          if (i < left)
-            *reinterpret_cast<float4*>(acc + i) = make_float4(f[i], f[i + 1], f[i + 2], f[i + 3]);
-        return;
       }
     }
 #pragma unroll
     for (int i = 0; i < 32; ++i) f[i] = live ? f[i] * scale : 0.0f;
-    T* out = static_cast<T*>(is_dw ? j.dw_out : j.dx_out) + at;
-    constexpr int W = 16 / sizeof(T);
-    if (left >= 32 && D % W == 0) {
-#pragma unroll
-      for (int i = 0; i < 32; i += W) {
-        uint4 u;
-        if (NP == 1)
-          u = make_uint4(tc::pack_bf16(f[i], f[i + 1]), tc::pack_bf16(f[i + 2], f[i + 3]),
-                         tc::pack_bf16(f[i + 4 * (NP == 1)], f[i + 5 * (NP == 1)]),
-                         tc::pack_bf16(f[i + 6 * (NP == 1)], f[i + 7 * (NP == 1)]));
-        else
-          u = make_uint4(__float_as_uint(f[i]), __float_as_uint(f[i + 1]),
-                         __float_as_uint(f[i + 2]), __float_as_uint(f[i + 3]));
-        *reinterpret_cast<uint4*>(out + i) = u;
+    if (j.boxes) {
+      uint8_t* b = NP == 1 ? put16(f) : put32(f);
+      if (lane == 0 && in) {
+        box_store(&j.out[which], tc::smem_u32(b), col + c, row, 0);
+        box_commit();
       }
-    } else {
+    } else if (in) {
+      T* out = static_cast<T*>(j.to[which]) + (size_t)row * D + col + c;
 #pragma unroll
       for (int i = 0; i < 32; ++i)
         if (i < left) Io<T>::store(out, i, f[i]);
@@ -527,29 +582,20 @@ struct GradEpi {
   __device__ void end() {}
 };
 
+template <int NP, int CG> using GradTile = Tile<NP, CG, GradEpi<NP, CG>::kOut>;
+
 template <int NP, int CG>
 __global__ void __launch_bounds__(kGemmThreads, 1)
     k_loss_grad(const __grid_constant__ GradJob job) {
-  extern __shared__ uint8_t smem_raw[];
+  using T = GradTile<NP, CG>;
   __shared__ GemmShared sh;
-  uint8_t* stages = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
-                                               ~uintptr_t(1023));
-  gemm_begin<NP, CG>(sh);
-  const DealNext next{&job.dw, &job.dx, blockIdx.x / CG, gridDim.x / CG,
-                      (long long)job.dw.tm * job.dw.tn, (long long)job.dx.tm * job.dx.tn};
-  const int warp = threadIdx.x / 32, lane = threadIdx.x & 31;
-  bool ok = true;
-  if (warp == 0) {
-    if (lane == 0) ok = gemm_copy<NP, CG>(sh, stages, next, job.err);
-  } else if (warp == 1) {
-    if (lane == 0 && (CG == 1 || cluster_rank() == 0))
-      ok = gemm_multiply<NP, CG>(sh, stages, next, job.err);
-  } else if (warp >= 4) {
-    GradEpi<NP, CG> epi(job);
-    ok = gemm_finish<NP, CG>(sh, next, epi, job.err);
-  }
-  __syncwarp();
-  gemm_end<NP, CG>(sh, !ok);
+  const int w = blockIdx.x / CG;
+  const DealNext next{{&job.p[0], &job.p[1]}, job.deal.lo[0][w],     job.deal.lo[0][w + 1],
+                      job.deal.lo[1][w],      job.deal.lo[1][w + 1], 0};
+  uint8_t* stages = stage_memory<T>();
+  GradEpi<NP, CG> epi(job, out_memory<T>(stages));
+  gemm_roles<T>(sh, stages, next, epi, job.err);
+  if (threadIdx.x >= 128) box_drain();
 }
 
 // ------------------------------------------------------------------ host
@@ -582,9 +628,7 @@ int sm_count() {
   return n;
 }
 
-// Workspace sizes do not depend on the device: statistics of up to this many
-// workers.
-constexpr int kMaxWorkers = 152;
+// Workspace sizes do not depend on the device: they are for kMaxWorkers blocks.
 int workers(int cg) {
   const int n = sm_count() < kMaxWorkers ? sm_count() : kMaxWorkers;
   return n / cg;
@@ -653,6 +697,62 @@ bool plane_map(CUtensorMap* m, const __nv_bfloat16* base, long long rows, long l
             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// A map for output boxes of 32 x 32 over planes of T, row stride ld elements.
+template <typename T>
+bool box_map(CUtensorMap* m, T* base, long long rows, long long cols, long long ld, long long plane,
+             int np) {
+  const EncodeTiledFn fn = encode_tiled();
+  if (!fn) return false;
+  constexpr bool f32 = sizeof(T) == 4;
+  const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)np};
+  const cuuint64_t strides[2] = {(cuuint64_t)ld * sizeof(T), (cuuint64_t)plane * sizeof(T)};
+  const cuuint32_t box[3] = {32, 32, 1};
+  const cuuint32_t es[3] = {1, 1, 1};
+  return fn(m, f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, base,
+            dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            f32 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+            CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// Tiles 0 .. n[k]-1 of two products, costing cost[k] each, to w workers in
+// contiguous ranges: the dearer product's tiles evenly, then the other's so that
+// the workers' totals come level.
+void deal_tiles(const long long n[2], const long long cost[2], int w, Deal* d) {
+  const int a = cost[0] >= cost[1] ? 0 : 1, b = 1 - a;
+  long long load[kMaxWorkers], give[kMaxWorkers], most = 0;
+  d->lo[a][0] = 0;
+  for (int i = 0; i < w; ++i) {
+    const long long k = n[a] / w + (i < n[a] % w);
+    d->lo[a][i + 1] = d->lo[a][i] + (unsigned)k;
+    load[i] = k * cost[a];
+    if (load[i] > most) most = load[i];
+  }
+  // the lowest level at which all of b's tiles fit
+  auto fits = [&](long long level) {
+    long long s = 0;
+    for (int i = 0; i < w; ++i)
+      if (level > load[i]) s += (level - load[i]) / cost[b];
+    return s >= n[b];
+  };
+  long long lo = 0, hi = most + (n[b] / w + 1) * cost[b];
+  while (lo < hi) {
+    const long long mid = (lo + hi) / 2;
+    if (fits(mid))
+      hi = mid;
+    else
+      lo = mid + 1;
+  }
+  long long left = n[b];
+  for (int i = w - 1; i >= 0; --i) {  // those with the least of a first
+    long long k = lo > load[i] ? (lo - load[i]) / cost[b] : 0;
+    if (k > left) k = left;
+    give[i] = k;
+    left -= k;
+  }
+  d->lo[b][0] = 0;
+  for (int i = 0; i < w; ++i) d->lo[b][i + 1] = d->lo[b][i] + (unsigned)give[i];
+}
+
 struct Planes {
   const __nv_bfloat16* p;
   long long rows, cols, ld, plane;
@@ -690,9 +790,10 @@ slim_status stage(const void* src, long long R, int D, int ld, const void* targe
 }
 
 // Launches a kernel of the tile products on `blocks` blocks, in pairs for CG = 2.
-template <int NP, int CG, typename Job>
+template <typename T, typename Job>
 bool launch(void (*k)(Job), unsigned blocks, cudaStream_t s, const Job& job, bool* ready) {
-  constexpr size_t smem = Tile<NP, CG>::smem();
+  constexpr size_t smem = T::smem();
+  constexpr int CG = T::GROUP;
   if (ready == nullptr || !*ready) {
     if (cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) !=
         cudaSuccess)
@@ -749,7 +850,8 @@ slim_status fwd(const Sizes& z, const void* x, const void* w, const void* target
   j.rep = rep;
   {
     prof::Scope ps(prof::K_LOSS_STATS, s, 2.0 * z.N * z.D * z.V, ((double)z.N + z.V) * z.D * 2 * NP);
-    if (!launch<NP, CG>(k_loss_stats<NP, CG>, (unsigned)wk * CG, s, j, once<StatEpi<NP, CG>>()))
+    if (!launch<StatTile<NP, CG>>(k_loss_stats<NP, CG>, (unsigned)wk * CG, s, j,
+                                  once<StatEpi<NP, CG>>()))
       return SLIM_ERR_CUDA;
   }
   JoinJob q{};
@@ -798,8 +900,17 @@ slim_status bwd(const Sizes& z, const void* x, const void* w, const void* target
     SoftJob j{};
     GradJob q{};
     if (!make_product<NP, CG>(&j.p, xm, false, wm, false, z.N, n, z.D) ||
-        !make_product<NP, CG>(&q.dw, gm, true, xm, true, n, z.D, z.N) ||
-        !make_product<NP, CG>(&q.dx, gm, false, wm, true, z.N, z.D, n))
+        !make_product<NP, CG>(&q.p[0], gm, true, xm, true, n, z.D, z.N) ||
+        !make_product<NP, CG>(&q.p[1], gm, false, wm, true, z.N, z.D, n) ||
+        !box_map(&j.g, ws.g, z.N, n, ps, z.N * ps, NP))
+      return SLIM_ERR_CUDA;
+    q.to[0] = static_cast<T*>(dw) + (size_t)v0 * z.D;
+    q.to[1] = dx;
+    q.boxes = z.D * sizeof(T) % 16 == 0;
+    if (q.boxes && (!box_map(&q.out[0], (T*)q.to[0], n, z.D, z.D, (long long)n * z.D, 1) ||
+                    !box_map(&q.out[1], (T*)q.to[1], z.N, z.D, z.D, z.N * z.D, 1)))
+      return SLIM_ERR_CUDA;
+    if (ws.acc && !box_map(&q.sum, ws.acc, z.N, z.D, acc_ld(z.D), z.N * acc_ld(z.D), 1))
       return SLIM_ERR_CUDA;
     j.targets = q.targets = targets;
     j.i64 = q.i64 = it == SLIM_I64;
@@ -810,9 +921,6 @@ slim_status bwd(const Sizes& z, const void* x, const void* w, const void* target
     j.dloss = dstride ? dloss : nullptr;
     q.scale = dstride ? nullptr : dloss;
     q.count = count;
-    j.g = ws.g;
-    j.plane = z.N * ps;
-    j.ld = ps;
     j.err = q.err = ws.header;
     j.rep = q.rep = rep;
     const double fl = 2.0 * z.N * z.D * n, gb = 2.0 * NP * z.N * n;
@@ -820,19 +928,21 @@ slim_status bwd(const Sizes& z, const void* x, const void* w, const void* target
     {
       const long long wk = tiles < workers(CG) ? tiles : workers(CG);
       prof::Scope sc(prof::K_LOSS_SOFTMAX, s, fl, ((double)z.N + n) * z.D * 2 * NP + gb);
-      if (!launch<NP, CG>(k_loss_softmax<NP, CG>, (unsigned)wk * CG, s, j, once<SoftEpi<NP, CG>>()))
+      if (!launch<SoftTile<NP, CG>>(k_loss_softmax<NP, CG>, (unsigned)wk * CG, s, j,
+                                    once<SoftEpi<NP, CG>>()))
         return SLIM_ERR_CUDA;
     }
-    q.dw_out = static_cast<T*>(dw) + (size_t)v0 * z.D;
-    q.dx_out = dx;
     q.acc = ws.acc;
     q.acc_ld = acc_ld(z.D);
     q.first = i == 0;
     q.last = i == pieces - 1;
-    const long long all = (long long)q.dw.tm * q.dw.tn + (long long)q.dx.tm * q.dx.tn;
-    const long long wk = all < workers(CG) ? all : workers(CG);
+    const long long nt[2] = {(long long)q.p[0].tm * q.p[0].tn, (long long)q.p[1].tm * q.p[1].tn};
+    const long long cost[2] = {q.p[0].kb, q.p[1].kb};
+    const int wk = (int)(nt[0] + nt[1] < workers(CG) ? nt[0] + nt[1] : workers(CG));
+    deal_tiles(nt, cost, wk, &q.deal);
     prof::Scope sc(prof::K_LOSS_GRAD, s, 2 * fl, ((double)z.N + n) * z.D * 2 * NP + 2 * gb);
-    if (!launch<NP, CG>(k_loss_grad<NP, CG>, (unsigned)wk * CG, s, q, once<GradEpi<NP, CG>>()))
+    if (!launch<GradTile<NP, CG>>(k_loss_grad<NP, CG>, (unsigned)wk * CG, s, q,
+                                 once<GradEpi<NP, CG>>()))
       return SLIM_ERR_CUDA;
   }
   return SLIM_OK;

@@ -594,13 +594,16 @@ def embedding(ids, table, scale=1.0):
     return Embedding.apply(ids, table, scale)
 
 
-# Words per piece of the vocabulary in vocab_loss_backward, unless the caller
-# says otherwise.
-VOCAB_PIECE = 8192
+def vocab_piece(N, V):
+    """Words per piece of the vocabulary in vocab_loss_backward, unless the
+    caller says otherwise: as many as keep rows x piece within 2^28, and at
+    least 1024."""
+    return min(V, max(1024, (1 << 28) // max(N, 1)))
 
 
-def vocab_loss_workspace_size(N, D, V, dtype, backward, piece=VOCAB_PIECE):
+def vocab_loss_workspace_size(N, D, V, dtype, backward, piece=None):
     n = _sz(0)
+    piece = vocab_piece(N, V) if piece is None else piece
     _check(library().slim_vocab_loss_workspace_size(N, D, V, DTYPES[dtype], piece, int(backward),
                                                     ctypes.byref(n)),
            "slim_vocab_loss_workspace_size")
@@ -638,13 +641,14 @@ def vocab_loss_forward(x, w, targets, ignore_index=-100, workspace=None, stream=
 
 
 def vocab_loss_backward(x, w, targets, lse, dloss, count=None, ignore_index=-100,
-                        piece=VOCAB_PIECE, workspace=None, stream=None):
+                        piece=None, workspace=None, stream=None):
     """slim_vocab_loss_bwd: returns (dx, dw), the gradients of sum_i c_i loss_i,
     c_i = dloss_i / count.  lse: from vocab_loss_forward on the same inputs.
     dloss: fp32 on the device, one value per row or a single one for all rows.
     count: None, or one fp32 value on the device (total[1:] of the forward for
     the mean loss).  Memory grows with rows x piece."""
     N, D, V = _loss_dims(x, w, targets, "vocab_loss_backward")
+    piece = vocab_piece(N, V) if piece is None else piece
     _require_cuda(lse, dloss)
     _require(lse.dtype == torch.float32 and lse.numel() == N, "lse must be the forward's")
     _require(dloss.dtype == torch.float32 and dloss.numel() in (1, N),
@@ -685,7 +689,7 @@ class VocabLoss(torch.autograd.Function):
         return dx, dw, None, None, None, None
 
 
-def vocab_loss(x, w, targets, reduction="mean", ignore_index=-100, piece=VOCAB_PIECE):
+def vocab_loss(x, w, targets, reduction="mean", ignore_index=-100, piece=None):
     """Differentiable softmax cross entropy of x [..., D] against the words w
     [V, D]; reduction "mean" (over the rows not ignored), "sum" or "none"."""
     _require(reduction in ("mean", "sum", "none"), "reduction must be 'mean', 'sum' or 'none'")

@@ -54,7 +54,7 @@ def rel(a, b):
     return float((a.double() - b).norm() / b.norm().clamp(min=1e-300))
 
 
-def check(x, w, t, c, piece=slim.VOCAB_PIECE, mean=False):
+def check(x, w, t, c, piece=None, mean=False):
     dt = x.dtype
     loss, lse, total = slim.vocab_loss_forward(x, w, t)
     count = (t != -100).sum().item()
