@@ -11,9 +11,12 @@
 // Operands are planes of bf16 matrices, K-major ([rows][K]) or MN-major
 // ([K][rows]); coordinates past an edge read as zero.  NP = 3: a value is the
 // sum of its three planes' values, and the product is the sum of the six plane
-// products of order below 2^-16, smallest first.  The tensor core adds to a
-// 32-bit accumulator with a truncation per step, so for NP = 3 a sum is cut
-// into short chains that the epilogue's registers join in fp32.
+// products down to 2^-16 of the largest.
+//
+// The tensor core cuts off the last bits at every step of a sum: measured, a
+// sum of K bf16 products comes out low by K * 7e-10 of itself (K * 1.7e-9 where
+// all have one sign).  ACC: a sum is cut into chains that the epilogue's
+// registers join in fp32, where that loss would show in an fp32 result.
 #pragma once
 #include "common.cuh"
 #include "tc_common.cuh"
@@ -21,28 +24,29 @@
 namespace slim {
 namespace lm {
 
-constexpr int kTM = 128;  // rows of a block's tile
-constexpr int kTK = 64;   // reduction per stage
-constexpr int kGemmThreads = 384;  // warps: TMA, MMA, TMEM, spare, 8 of epilogue
-constexpr int kEpiWarps = 8;
+constexpr int kTM = 128;           // rows of a block's tile
+constexpr int kTN = 256;           // columns of a tile
+constexpr int kTK = 64;            // reduction per stage
+constexpr int kEpiWarps = 16;      // four per quarter of the rows, 64 columns each
+constexpr int kEpiCols = kTN / 4;
+constexpr int kGemmThreads = 128 + 32 * kEpiWarps;  // warps: TMA, MMA, TMEM, spare, epilogue
 
 // OUT: bytes of shared memory per epilogue warp from which it stores by TMA.
 constexpr int kSmemBytes = 227 * 1024 - 1024 - 512;  // after alignment and barriers
-template <int NP, int CG, int OUT = 0>
+template <int NP, int CG, int OUT = 0, bool JOIN = (NP > 1)>
 struct Tile {
   static constexpr int PLANES = NP, GROUP = CG;
-  // With three planes the epilogue holds a tile's sums in registers: half the
-  // columns, 64 per thread.
-  static constexpr int N = NP == 1 ? 256 : 128;
-  static constexpr int HALF = N / 2;      // columns of an epilogue warp
-  static constexpr int BROWS = N / CG;    // rows of B that a block holds
+  static constexpr bool ACC = JOIN;
+  static constexpr int BROWS = kTN / CG;    // rows of B that a block holds
   static constexpr int A_BYTES = kTM * kTK * 2, B_BYTES = BROWS * kTK * 2;
-  static constexpr int STAGE = A_BYTES + B_BYTES;
+  static constexpr int STAGE = A_BYTES + B_BYTES;  // one plane of either operand
   static constexpr int FIT = (kSmemBytes - kEpiWarps * OUT) / STAGE;
   static constexpr int STAGES = FIT < 8 ? FIT : 8;
-  static constexpr int PAIRS = NP == 1 ? 1 : 6;
   static constexpr int OUT_BYTES = OUT;
+  // chains of 512 of the reduction, or of 128 with three planes (48 steps)
+  static constexpr int CHAIN = NP == 1 ? 8 : 2;
   static constexpr size_t smem() { return 1024 + (size_t)STAGES * STAGE + kEpiWarps * OUT; }
+  static_assert(STAGES >= 3, "a stage per plane");
 };
 
 // One product: D [M, N] = sum over K of A and B.
@@ -52,7 +56,6 @@ struct Product {
   int M, N;
   int tm, tn;      // tiles each way (tm in tiles of kTM * CG rows)
   int kb;          // stages (of kTK) of the reduction
-  int chain;       // stage products per accumulator chain
 };
 
 struct GemmShared {
@@ -80,8 +83,10 @@ __device__ __forceinline__ void arrive_at_leader(uint32_t bar) {
   if (CG == 1)
     asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
   else
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(
-                     map_to_rank(bar, 0))
+    // what it hands over is TMEM, read by completed tcgen05.ld: nothing in memory
+    // has to be made visible to the other block (a release at cluster scope
+    // waits for the warp's earlier stores, 0.5 us a tile)
+    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(map_to_rank(bar, 0))
                  : "memory");
 }
 
@@ -153,18 +158,6 @@ __device__ __forceinline__ void gemm_tma(uint32_t dst, const CUtensorMap* map, i
 }
 
 // ------------------------------------------------------------------ roles
-// The planes of the i-th product of a stage, smallest products first.
-template <int NP>
-__device__ __forceinline__ void plane_pair(int i, int& pa, int& pb) {
-  if (NP == 1) {
-    pa = pb = 0;
-  } else {
-    // (2,0) (1,1) (0,2) (1,0) (0,1) (0,0), two bits each
-    pa = (0x046 >> (2 * i)) & 3;
-    pb = (0x124 >> (2 * i)) & 3;
-  }
-}
-
 // Sets the ring up and allocates TMEM; every thread of the block (of the pair).
 template <typename T>
 __device__ __forceinline__ void gemm_begin(GemmShared& sh) {
@@ -180,7 +173,7 @@ __device__ __forceinline__ void gemm_begin(GemmShared& sh) {
     }
     tc::mbar_fence_init();
   }
-  if (threadIdx.x / 32 == 2) gemm_tmem_alloc<CG>(tc::smem_u32(&sh.tmem), 2 * T::N);
+  if (threadIdx.x / 32 == 2) gemm_tmem_alloc<CG>(tc::smem_u32(&sh.tmem), 2 * kTN);
   tc::tc_fence_before();
   if (CG == 1)
     __syncthreads();
@@ -200,7 +193,7 @@ __device__ __forceinline__ void gemm_end(GemmShared& sh, bool failed) {
     __syncthreads();
   else
     cluster_sync();
-  if (threadIdx.x / 32 == 2) gemm_tmem_free<CG>(sh.tmem, 2 * T::N);
+  if (threadIdx.x / 32 == 2) gemm_tmem_free<CG>(sh.tmem, 2 * kTN);
 }
 
 // The copying thread.  `next(p, m, n)` yields this worker's tiles in order:
@@ -213,13 +206,11 @@ __device__ bool gemm_copy(GemmShared& sh, uint8_t* stages, Next next, int* err) 
   int m, n;
   uint32_t it = 0;
   while (next(p, m, n)) {
-    const int row = (m * CG + (int)rank) * kTM, col = n * T::N + (int)rank * T::BROWS;
+    const int row = (m * CG + (int)rank) * kTM, col = n * kTN + (int)rank * T::BROWS;
     for (int kb = 0; kb < p->kb; ++kb) {
 #pragma unroll 1
-      for (int i = 0; i < T::PAIRS; ++i, ++it) {
+      for (int q = 0; q < NP; ++q, ++it) {
         const int st = it % T::STAGES;
-        int pa, pb;
-        plane_pair<NP>(i, pa, pb);
         if (!tc::mbar_wait(tc::smem_u32(&sh.empty[st]), ((it / T::STAGES) & 1) ^ 1, err))
           return false;
         uint32_t full = tc::smem_u32(&sh.full[st]);
@@ -230,16 +221,16 @@ __device__ bool gemm_copy(GemmShared& sh, uint8_t* stages, Next next, int* err) 
         if (p->a_mn) {
 #pragma unroll
           for (int j = 0; j < kTM / 64; ++j)
-            gemm_tma<CG>(sa + j * 8192, &p->a, row + 64 * j, k, pa, full);
+            gemm_tma<CG>(sa + j * 8192, &p->a, row + 64 * j, k, q, full);
         } else {
-          gemm_tma<CG>(sa, &p->a, k, row, pa, full);
+          gemm_tma<CG>(sa, &p->a, k, row, q, full);
         }
         if (p->b_mn) {
 #pragma unroll
           for (int j = 0; j < T::BROWS / 64; ++j)
-            gemm_tma<CG>(sb + j * 8192, &p->b, col + 64 * j, k, pb, full);
+            gemm_tma<CG>(sb + j * 8192, &p->b, col + 64 * j, k, q, full);
         } else {
-          gemm_tma<CG>(sb, &p->b, k, col, pb, full);
+          gemm_tma<CG>(sb, &p->b, k, col, q, full);
         }
       }
     }
@@ -251,36 +242,95 @@ __device__ bool gemm_copy(GemmShared& sh, uint8_t* stages, Next next, int* err) 
   return true;
 }
 
-// The thread that issues MMAs (of the leading block of a pair).
+// One lane of a converged warp, the same every time.  ptxas knows that a branch
+// on it holds one thread, and keeps what the MMAs take in uniform registers.
+__device__ __forceinline__ bool elect_one() {
+  uint32_t p;
+  asm volatile(
+      "{\n\t.reg .pred P;\n\t"
+      "elect.sync _|P, 0xffffffff;\n\t"
+      "selp.u32 %0, 1, 0, P;\n\t}"
+      : "=r"(p));
+  return p != 0;
+}
+
+// The warp that issues MMAs (of the leading block of a pair).  All lanes walk
+// the loop; one of them issues.
 template <typename T, typename Next>
 __device__ bool gemm_multiply(GemmShared& sh, uint8_t* stages, Next next, int* err) {
   constexpr int CG = T::GROUP;
   const Product* p;
   int m, n;
-  uint32_t it = 0, acc = 0;
+  const uint32_t full0 = tc::smem_u32(&sh.full[0]), empty0 = tc::smem_u32(&sh.empty[0]);
+  const uint32_t tmem = sh.tmem;
+  uint32_t st = 0, phase = 0, acc = 0;
+  auto step_on = [&](uint32_t& s, uint32_t& ph) {
+    if (++s == T::STAGES) {
+      s = 0;
+      ph ^= 1;
+    }
+  };
+  auto wait = [&](uint32_t bar, uint32_t parity) {
+    const bool ok = __all_sync(0xffffffffu, tc::mbar_wait(bar, parity, err));
+    tc::tc_fence_after();
+    return ok;
+  };
   while (next(p, m, n)) {
-    const uint32_t idesc = tc::idesc_bf16(kTM * CG, T::N, p->a_mn, p->b_mn);
-    const uint32_t a_lbo = p->a_mn ? 8192 : 16, b_lbo = p->b_mn ? 8192 : 16;
+    const uint32_t idesc = tc::idesc_bf16(kTM * CG, kTN, p->a_mn, p->b_mn);
     const uint32_t a_step = p->a_mn ? 128 : 2, b_step = p->b_mn ? 128 : 2;
-    const int total = p->kb * T::PAIRS;
-    for (int k0 = 0; k0 < total; k0 += p->chain, ++acc) {
-      const int buf = acc & 1;
-      if (!tc::mbar_wait(tc::smem_u32(&sh.tempty[buf]), ((acc >> 1) & 1) ^ 1, err)) return false;
-      tc::tc_fence_after();
-      const uint32_t d = sh.tmem + buf * T::N;
-      const int k1 = min(k0 + p->chain, total);
-      for (int k = k0; k < k1; ++k, ++it) {
-        const int st = it % T::STAGES;
-        if (!tc::mbar_wait(tc::smem_u32(&sh.full[st]), (it / T::STAGES) & 1, err)) return false;
-        tc::tc_fence_after();
-        const uint32_t sa = tc::smem_u32(stages) + st * T::STAGE, sb = sa + T::A_BYTES;
-        const uint64_t da = tc::sdesc(sa, a_lbo, 1024), db = tc::sdesc(sb, b_lbo, 1024);
+    const uint64_t a0 = tc::sdesc(tc::smem_u32(stages), p->a_mn ? 8192 : 16, 1024);
+    const uint64_t b0 = tc::sdesc(tc::smem_u32(stages) + T::A_BYTES, p->b_mn ? 8192 : 16, 1024);
+    const int kb = p->kb, step = T::ACC ? T::CHAIN : kb;
+    for (int k0 = 0; k0 < kb; k0 += step, ++acc) {
+      const uint32_t buf = acc & 1;
+      if (!wait(tc::smem_u32(&sh.tempty[buf]), ((acc >> 1) & 1) ^ 1)) return false;
+      const uint32_t d = tmem + buf * kTN;
+      uint32_t more = 0;
+      // by the issuing lane
+      auto product = [&](uint32_t ia, uint32_t ib) {
+        const uint64_t da = a0 + ia * (T::STAGE >> 4), db = b0 + ib * (T::STAGE >> 4);
 #pragma unroll
         for (int j = 0; j < kTK / 16; ++j)
-          gemm_mma<CG>(d, da + j * a_step, db + j * b_step, idesc, k > k0 || j > 0);
-        gemm_commit<CG>(tc::smem_u32(&sh.empty[st]));
+          gemm_mma<CG>(d, da + j * a_step, db + j * b_step, idesc, j == 0 ? more : 1u);
+      };
+      auto done = [&](uint32_t i) { gemm_commit<CG>(empty0 + 8 * i); };
+      const int k1 = min(k0 + step, kb);
+      for (int k = k0; k < k1; ++k) {
+        const uint32_t s0 = st;
+        if (!wait(full0 + 8 * s0, phase)) return false;
+        step_on(st, phase);
+        if (T::PLANES == 1) {
+          if (elect_one()) {
+            product(s0, s0);
+            done(s0);
+          }
+        } else {
+          if (elect_one()) product(s0, s0);
+          const uint32_t s1 = st;
+          if (!wait(full0 + 8 * s1, phase)) return false;
+          step_on(st, phase);
+          more = 1;
+          if (elect_one()) {
+            product(s0, s1);
+            product(s1, s0);
+            product(s1, s1);
+            done(s1);
+          }
+          const uint32_t s2 = st;
+          if (!wait(full0 + 8 * s2, phase)) return false;
+          step_on(st, phase);
+          if (elect_one()) {
+            product(s0, s2);
+            product(s2, s0);
+            done(s2);
+            done(s0);
+          }
+        }
+        more = 1;
+        __syncwarp();
       }
-      gemm_commit<CG>(tc::smem_u32(&sh.tfull[buf]));
+      if (elect_one()) gemm_commit<CG>(tc::smem_u32(&sh.tfull[buf]));
+      __syncwarp();
     }
   }
   return true;
@@ -288,31 +338,33 @@ __device__ bool gemm_multiply(GemmShared& sh, uint8_t* stages, Next next, int* e
 
 // An epilogue warp.  For every tile, epi.begin(p, m, n, row, col0) once, then
 // epi.chunk(c, v) for each 32 columns col0 + c .. of row `row` (of this thread)
-// that lie inside the product, then epi.end().  Reads past the product's rows
-// still run (their values are zero sums); the epilogue drops them.
+// that begin inside the product (v is the epilogue's to change).  Reads past the product's rows still run (their
+// values are zero sums); the epilogue drops them.
 template <typename T, typename Next, typename Epi>
 __device__ bool gemm_finish(GemmShared& sh, Next next, Epi& epi, int* err) {
-  constexpr int NP = T::PLANES, CG = T::GROUP;
+  constexpr int CG = T::GROUP;
   const uint32_t rank = CG == 1 ? 0 : cluster_rank();
   const int w = threadIdx.x / 32 - 4, lane = threadIdx.x & 31;
-  const int quarter = w & 3, half = w >> 2;
+  const int quarter = w & 3, part = w >> 2;
   const Product* p;
   int m, n;
   uint32_t acc = 0;
   while (next(p, m, n)) {
     const int row = (m * CG + (int)rank) * kTM + quarter * 32 + lane;
-    const int col = n * T::N + half * T::HALF;
-    const int total = p->kb * T::PAIRS;
-    float sum[NP == 1 ? 1 : T::HALF];
+    const int col = n * kTN + part * kEpiCols;
+    const int step = T::ACC ? T::CHAIN : p->kb;
+    float sum[T::ACC ? kEpiCols : 1];
     epi.begin(*p, m, n, row, col);
-    for (int k0 = 0; k0 < total; k0 += p->chain, ++acc) {
+    for (int k0 = 0; k0 < p->kb; k0 += step, ++acc) {
       const int buf = acc & 1;
       if (!tc::mbar_wait(tc::smem_u32(&sh.tfull[buf]), (acc >> 1) & 1, err)) return false;
       tc::tc_fence_after();
-      const uint32_t t = sh.tmem + buf * T::N + half * T::HALF + ((uint32_t)(quarter * 32) << 16);
-      if (NP > 1) {
+      __syncwarp();
+      const uint32_t t =
+          sh.tmem + buf * kTN + part * kEpiCols + ((uint32_t)(quarter * 32) << 16);
+      if (T::ACC) {
 #pragma unroll
-        for (int c = 0; c < T::HALF; c += 16) {
+        for (int c = 0; c < kEpiCols; c += 16) {
           float v[16];
           tc::tmem_ld16(t + c, v);
 #pragma unroll
@@ -320,7 +372,7 @@ __device__ bool gemm_finish(GemmShared& sh, Next next, Epi& epi, int* err) {
         }
       } else {
 #pragma unroll 1
-        for (int c = 0; c < T::HALF && col + c < p->N; c += 32) {
+        for (int c = 0; c < kEpiCols && col + c < p->N; c += 32) {
           float v[32];
           __syncwarp();
           tc::tmem_ld32(t + c, v);
@@ -331,12 +383,11 @@ __device__ bool gemm_finish(GemmShared& sh, Next next, Epi& epi, int* err) {
       __syncwarp();
       if (lane == 0) arrive_at_leader<CG>(tc::smem_u32(&sh.tempty[buf]));
     }
-    if (NP > 1) {
+    if (T::ACC) {
 #pragma unroll
-      for (int c = 0; c < T::HALF; c += 32)
+      for (int c = 0; c < kEpiCols; c += 32)
         if (col + c < p->N) epi.chunk(c, &sum[c]);
     }
-    epi.end();
   }
   return true;
 }
@@ -352,8 +403,7 @@ __device__ __forceinline__ void gemm_roles(GemmShared& sh, uint8_t* stages, cons
   if (warp == 0) {
     if (lane == 0) ok = gemm_copy<T>(sh, stages, next, err);
   } else if (warp == 1) {
-    if (lane == 0 && (T::GROUP == 1 || cluster_rank() == 0))
-      ok = gemm_multiply<T>(sh, stages, next, err);
+    if (T::GROUP == 1 || cluster_rank() == 0) ok = gemm_multiply<T>(sh, stages, next, err);
   } else if (warp >= 4) {
     ok = gemm_finish<T>(sh, next, epi, err);
   }

@@ -114,7 +114,7 @@ struct StatJob {
   int i64;
   long long ignore;
   int V;
-  int slots;       // partial statistics per row: 2 per worker that shares it
+  int slots;       // partial statistics per row: 4 per worker that shares it
   float2* part;    // [tm][slots][rows of a tile]: base, sum of 2^(z log2 e - base)
   float* zt;       // [N] target logits
   int* err;
@@ -150,11 +150,9 @@ struct StatEpi {
     }
     col = c;
   }
-  __device__ void chunk(int c, const float* v) {
-    float z[32];
+  __device__ __forceinline__ void chunk(int c, float* v) {
+    float* z = v;
     const int left = j.V - (col + c), at = target - (col + c);
-#pragma unroll
-    for (int i = 0; i < 32; ++i) z[i] = v[i];
     if (at >= 0 && at < 32) {
 #pragma unroll
       for (int i = 0; i < 32; ++i)
@@ -181,11 +179,10 @@ struct StatEpi {
     sum = fmaf(sum, exp2_of<NP>(base - ref), (s[0] + s[1]) + (s[2] + s[3]));
     base = to;
   }
-  __device__ void end() {}
   __device__ void flush() {
     if (m_now < 0) return;
     const long long tiles = (long long)j.p.tm * j.p.tn;
-    const int slot = (int)(worker - run_owner((long long)m_now * j.p.tn, tiles, workers)) * 2 +
+    const int slot = (int)(worker - run_owner((long long)m_now * j.p.tn, tiles, workers)) * 4 +
                      (threadIdx.x / 32 - 4) / 4;
     j.part[((size_t)m_now * j.slots + slot) * (kTM * CG) + slot_row] = make_float2(base, sum);
   }
@@ -215,7 +212,7 @@ struct SoftEpi {
   bool in = false, live = false;
   uint8_t* box;  // this warp's output boxes
   uint32_t turn = 0;
-  static constexpr int kBox = 2048, kBoxes = NP == 1 ? 4 : 3, kOut = kBoxes * kBox;
+  static constexpr int kBox = 2048, kBoxes = 2, kOut = kBoxes * kBox;
   __device__ SoftEpi(const SoftJob& job, uint8_t* b) : j(job), box(b) {}
   __device__ void begin(const Product& p, int m, int n, int r, int c) {
     row = r;
@@ -236,9 +233,9 @@ struct SoftEpi {
     else
       coef = __int_as_float(0x7fffffff);
   }
-  __device__ void chunk(int c, const float* v) {
+  __device__ __forceinline__ void chunk(int c, float* v) {
     const int at = target - (col + c), lane = threadIdx.x & 31;
-    float g[32];
+    float* g = v;
     if (NP == 1) {
       const float l2 = lse * kLog2e;
 #pragma unroll
@@ -254,29 +251,25 @@ struct SoftEpi {
     }
 #pragma unroll
     for (int i = 0; i < 32; ++i) g[i] = live ? g[i] * coef : 0.0f;
-    // NP = 1: four boxes in turn; NP = 3: the planes' three at once
-    box_reuse<NP == 1 ? kBoxes - 1 : 0>();
-    uint8_t* to = box + (NP == 1 ? (turn++ % kBoxes) * kBox : 0);
 #pragma unroll
     for (int q = 0; q < NP; ++q) {
+      box_reuse<kBoxes - 1>();
+      uint8_t* to = box + (turn++ % kBoxes) * kBox;
 #pragma unroll
       for (int i = 0; i < 32; i += 8) {
         uint32_t u[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) u[e] = take_plane<NP>(g[i + 2 * e], g[i + 2 * e + 1]);
-        *reinterpret_cast<uint4*>(to + q * kBox + box_piece16(lane, i / 8)) =
+        *reinterpret_cast<uint4*>(to + box_piece16(lane, i / 8)) =
             make_uint4(u[0], u[1], u[2], u[3]);
       }
-    }
-    box_written();
-    if (lane == 0 && in) {
-#pragma unroll
-      for (int q = 0; q < NP; ++q)
-        box_store(&j.g, tc::smem_u32(to + q * kBox), col + c, row, q);
-      box_commit();
+      box_written();
+      if (lane == 0 && in) {
+        box_store(&j.g, tc::smem_u32(to), col + c, row, q);
+        box_commit();
+      }
     }
   }
-  __device__ void end() {}
 };
 
 template <typename T>
@@ -296,13 +289,15 @@ __device__ __forceinline__ RunNext run_of(const Product& p) {
   return RunNext{&p, run_begin(worker, tiles, workers), run_begin(worker + 1, tiles, workers)};
 }
 
-template <int NP, int CG> using StatTile = Tile<NP, CG>;
+// A bf16 logit over more than 512 features is summed in chains: its loss shows
+// in the fp32 results otherwise (2e-6 of a logit at 2048).
+template <int NP, int CG, bool JOIN> using StatTile = Tile<NP, CG, 0, JOIN>;
 template <int NP, int CG> using SoftTile = Tile<NP, CG, SoftEpi<NP, CG>::kOut>;
 
-template <int NP, int CG>
+template <int NP, int CG, bool JOIN>
 __global__ void __launch_bounds__(kGemmThreads, 1)
     k_loss_stats(const __grid_constant__ StatJob job) {
-  using T = StatTile<NP, CG>;
+  using T = StatTile<NP, CG, JOIN>;
   __shared__ GemmShared sh;
   if (blockIdx.x == 0 && threadIdx.x == 0) tc::set_report(job.err, job.rep);
   StatEpi<NP, CG> epi(job, blockIdx.x / CG, gridDim.x / CG);
@@ -355,7 +350,7 @@ __global__ void __launch_bounds__(256) k_loss_join(JoinJob j) {
     const long long m = row / j.tile_rows;
     const long long first = run_owner(m * j.tn, j.tiles, j.workers);
     const long long last = run_owner(m * j.tn + j.tn - 1, j.tiles, j.workers);
-    const int n = (int)(last - first + 1) * 2;
+    const int n = (int)(last - first + 1) * 4;
     for (int s = lane; s < n; s += lanes) {
       const float2 a = j.part[((size_t)m * j.slots + s) * j.tile_rows + (row - m * j.tile_rows)];
       add(a.x, a.y);
@@ -489,10 +484,11 @@ struct GradJob {
 template <int NP, int CG>
 struct GradEpi {
   using T = typename std::conditional<NP == 1, __nv_bfloat16, float>::type;
-  static constexpr int kBox = 4096, kBoxes = 2, kOut = kBoxes * kBox;
+  static constexpr int kOut = 4096;  // one fp32 box, or two of bf16 in turn
   const GradJob& j;
   uint8_t* box;
   uint32_t turn = 0;
+  bool wide = false;  // the last box was fp32
   const Product* p = nullptr;
   int row = 0, col = 0, which = 0;
   bool in = false, live = true;
@@ -513,8 +509,9 @@ struct GradEpi {
   // 32 fp32 values of every lane's row into a box
   __device__ uint8_t* put32(const float* f) {
     const int lane = threadIdx.x & 31;
-    box_reuse<kBoxes - 1>();
-    uint8_t* to = box + (turn++ % kBoxes) * kBox;
+    box_reuse<0>();
+    wide = true;
+    uint8_t* to = box;
 #pragma unroll
     for (int i = 0; i < 32; i += 4)
       *reinterpret_cast<float4*>(to + box_piece32(lane, i / 4)) =
@@ -524,8 +521,12 @@ struct GradEpi {
   }
   __device__ uint8_t* put16(const float* f) {
     const int lane = threadIdx.x & 31;
-    box_reuse<kBoxes - 1>();
-    uint8_t* to = box + (turn++ % kBoxes) * kBox;
+    if (wide)
+      box_reuse<0>();
+    else
+      box_reuse<1>();
+    wide = false;
+    uint8_t* to = box + (turn++ & 1) * 2048;
 #pragma unroll
     for (int i = 0; i < 32; i += 8)
       *reinterpret_cast<uint4*>(to + box_piece16(lane, i / 8)) =
@@ -534,11 +535,9 @@ struct GradEpi {
     box_written();
     return to;
   }
-  __device__ void chunk(int c, const float* v) {
+  __device__ __forceinline__ void chunk(int c, float* v) {
     const int D = p->N, left = D - (col + c), lane = threadIdx.x & 31;
-    float f[32];
-#pragma unroll
-    for (int i = 0; i < 32; ++i) f[i] = v[i];
+    float* f = v;
     if (which == 1) {
       if (!j.last) {
         // the pieces' sums of dx, added where they lie; a launch adds once
@@ -579,7 +578,6 @@ struct GradEpi {
         if (i < left) Io<T>::store(out, i, f[i]);
     }
   }
-  __device__ void end() {}
 };
 
 template <int NP, int CG> using GradTile = Tile<NP, CG, GradEpi<NP, CG>::kOut>;
@@ -643,7 +641,7 @@ int stat_slots(long long tm, long long tn, long long w) {
   long long s = w / tm + 2;
   if (s > tn) s = tn;
   if (s > w) s = w;
-  return (int)s * 2;
+  return (int)s * 4;
 }
 
 struct Ws {
@@ -670,7 +668,7 @@ Ws carve(Carver& cv, const Sizes& z, int piece, bool bwd) {
   if (z.stage_w()) w.w = cv.take<__nv_bfloat16>((size_t)np * z.V * z.ld());
   if (!bwd) {
     const int rows = kTM * CGv;
-    const long long tm = cdiv(z.N, rows), tn = cdiv(z.V, np == 1 ? 256 : 128);
+    const long long tm = cdiv(z.N, rows), tn = cdiv(z.V, kTN);
     w.part = cv.take<float2>((size_t)tm * stat_slots(tm, tn, kMaxWorkers / CGv) * rows);
     w.zt = cv.take<float>(z.N);
     w.block_sum = cv.take<float>(2 * (size_t)cdiv(z.N, 8));
@@ -761,19 +759,16 @@ struct Planes {
 template <int NP, int CG>
 bool make_product(Product* p, const Planes& a, bool a_mn, const Planes& b, bool b_mn, long long M,
                   long long N, long long K) {
-  using T = Tile<NP, CG>;
   if (!plane_map(&p->a, a.p, a.rows, a.cols, a.ld, a.plane, NP, a_mn ? kTK : kTM) ||
-      !plane_map(&p->b, b.p, b.rows, b.cols, b.ld, b.plane, NP, b_mn ? kTK : T::BROWS))
+      !plane_map(&p->b, b.p, b.rows, b.cols, b.ld, b.plane, NP, b_mn ? kTK : kTN / CG))
     return false;
   p->a_mn = a_mn;
   p->b_mn = b_mn;
   p->M = (int)M;
   p->N = (int)N;
   p->tm = cdiv(M, kTM * CG);
-  p->tn = cdiv(N, T::N);
+  p->tn = cdiv(N, kTN);
   p->kb = cdiv(K, kTK);
-  // one chain for bf16 problems; 128 of the reduction (48 steps) for fp32 ones
-  p->chain = NP == 1 ? p->kb : 2 * T::PAIRS;
   return true;
 }
 
@@ -824,7 +819,6 @@ template <int NP, int CG>
 slim_status fwd(const Sizes& z, const void* x, const void* w, const void* targets, slim_index it,
                 long long ignore, float* loss, float* lse, float* total, const Ws& ws,
                 unsigned* rep, cudaStream_t s) {
-  using T = Tile<NP, CG>;
   const int ld = z.ld();
   const __nv_bfloat16* xp = ws.x ? ws.x : static_cast<const __nv_bfloat16*>(x);
   const __nv_bfloat16* wp = ws.w ? ws.w : static_cast<const __nv_bfloat16*>(w);
@@ -850,9 +844,14 @@ slim_status fwd(const Sizes& z, const void* x, const void* w, const void* target
   j.rep = rep;
   {
     prof::Scope ps(prof::K_LOSS_STATS, s, 2.0 * z.N * z.D * z.V, ((double)z.N + z.V) * z.D * 2 * NP);
-    if (!launch<StatTile<NP, CG>>(k_loss_stats<NP, CG>, (unsigned)wk * CG, s, j,
-                                  once<StatEpi<NP, CG>>()))
-      return SLIM_ERR_CUDA;
+    const unsigned blocks = (unsigned)wk * CG;
+    const bool ok =
+        NP > 1 || j.p.kb > StatTile<NP, CG, true>::CHAIN
+            ? launch<StatTile<NP, CG, true>>(k_loss_stats<NP, CG, true>, blocks, s, j,
+                                             once<StatTile<NP, CG, true>>())
+            : launch<StatTile<NP, CG, NP != 1>>(k_loss_stats<NP, CG, NP != 1>, blocks, s, j,
+                                                once<StatTile<NP, CG, NP != 1>>());
+    if (!ok) return SLIM_ERR_CUDA;
   }
   JoinJob q{};
   q.part = ws.part;

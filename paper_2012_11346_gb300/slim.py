@@ -597,8 +597,9 @@ def embedding(ids, table, scale=1.0):
 def vocab_piece(N, V):
     """Words per piece of the vocabulary in vocab_loss_backward, unless the
     caller says otherwise: as many as keep rows x piece within 2^28, and at
-    least 1024."""
-    return min(V, max(1024, (1 << 28) // max(N, 1)))
+    least 8192 (smaller pieces leave the products too few tiles; larger ones
+    gain nothing at 32768 rows)."""
+    return min(V, max(8192, (1 << 28) // max(N, 1)))
 
 
 def vocab_loss_workspace_size(N, D, V, dtype, backward, piece=None):
