@@ -31,21 +31,19 @@ constexpr int kEpiWarps = 16;      // four per quarter of the rows, 64 columns e
 constexpr int kEpiCols = kTN / 4;
 constexpr int kGemmThreads = 128 + 32 * kEpiWarps;  // warps: TMA, MMA, TMEM, spare, epilogue
 
-// OUT: bytes of shared memory per epilogue warp from which it stores by TMA.
 constexpr int kSmemBytes = 227 * 1024 - 1024 - 512;  // after alignment and barriers
-template <int NP, int CG, int OUT = 0, bool JOIN = (NP > 1)>
+template <int NP, int CG, bool JOIN = (NP > 1)>
 struct Tile {
   static constexpr int PLANES = NP, GROUP = CG;
   static constexpr bool ACC = JOIN;
   static constexpr int BROWS = kTN / CG;    // rows of B that a block holds
   static constexpr int A_BYTES = kTM * kTK * 2, B_BYTES = BROWS * kTK * 2;
   static constexpr int STAGE = A_BYTES + B_BYTES;  // one plane of either operand
-  static constexpr int FIT = (kSmemBytes - kEpiWarps * OUT) / STAGE;
+  static constexpr int FIT = kSmemBytes / STAGE;
   static constexpr int STAGES = FIT < 8 ? FIT : 8;
-  static constexpr int OUT_BYTES = OUT;
   // chains of 512 of the reduction, or of 128 with three planes (48 steps)
   static constexpr int CHAIN = NP == 1 ? 8 : 2;
-  static constexpr size_t smem() { return 1024 + (size_t)STAGES * STAGE + kEpiWarps * OUT; }
+  static constexpr size_t smem() { return 1024 + (size_t)STAGES * STAGE; }
   static_assert(STAGES >= 3, "a stage per plane");
 };
 
@@ -411,52 +409,22 @@ __device__ __forceinline__ void gemm_roles(GemmShared& sh, uint8_t* stages, cons
   gemm_end<T>(sh, !ok);
 }
 
-// ------------------------------------------------------------------ output boxes
-// An epilogue warp's 32 rows x 32 columns go out as one box: every lane writes
-// its row's 16-byte pieces into shared memory, swizzled so that eight lanes fill
-// all banks, and one lane starts the copy.  A row-by-row store from registers
-// would touch 32 lines with every instruction.
-//   bf16: rows of 64 bytes, 64-byte swizzle;  fp32: 128 bytes, 128-byte swizzle.
-__device__ __forceinline__ uint32_t box_piece16(int row, int c) {  // bf16, c in 0..3
-  return (uint32_t)(row * 64 + ((c ^ ((row >> 1) & 3)) << 4));
-}
-__device__ __forceinline__ uint32_t box_piece32(int row, int c) {  // fp32, c in 0..7
-  return (uint32_t)(row * 128 + ((c ^ (row & 7)) << 4));
-}
-// Before a box in shared memory is written again: all but the newest KEEP
-// groups of this lane's stores have read theirs.
-template <int KEEP>
-__device__ __forceinline__ void box_reuse() {
-  if ((threadIdx.x & 31) == 0)
-    asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(KEEP) : "memory");
-  __syncwarp();
-}
-__device__ __forceinline__ void box_written() {
-  tc::fence_async_smem();
-  __syncwarp();
-}
-// By one lane: stores (or adds, fp32) a box, and closes a group.
-__device__ __forceinline__ void box_store(const CUtensorMap* map, uint32_t src, int x, int y,
-                                          int z) {
-  asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%1, %2, %3}], [%4];" ::
-                   "l"(reinterpret_cast<uint64_t>(map)),
-               "r"(x), "r"(y), "r"(z), "r"(src)
+// ------------------------------------------------------------------ rows to memory
+// A lane holds 32 columns of its own row.  It moves them in whole 32-byte
+// sectors: a 256 x 256 tile of bf16 took 5.6 k cycles this way under the next
+// tile's MMAs (5.1 k without a store), 7.9 k with 16-byte stores, and 6.5 k
+// through shared memory and TMA, which compete with the MMAs' operands.
+__device__ __forceinline__ void store32(void* p, const uint32_t* u) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(u[0]),
+               "r"(u[1]), "r"(u[2]), "r"(u[3]), "r"(u[4]), "r"(u[5]), "r"(u[6]), "r"(u[7])
                : "memory");
 }
-__device__ __forceinline__ void box_add(const CUtensorMap* map, uint32_t src, int x, int y, int z) {
-  asm volatile(
-      "cp.reduce.async.bulk.tensor.3d.global.shared::cta.add.bulk_group [%0, {%1, %2, %3}], "
-      "[%4];" ::"l"(reinterpret_cast<uint64_t>(map)),
-      "r"(x), "r"(y), "r"(z), "r"(src)
-      : "memory");
-}
-__device__ __forceinline__ void box_commit() {
-  asm volatile("cp.async.bulk.commit_group;" ::: "memory");
-}
-// The lane's stores are complete.
-__device__ __forceinline__ void box_drain() {
-  if ((threadIdx.x & 31) == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
-  __syncwarp();
+__device__ __forceinline__ void load32(const void* p, uint32_t* u) {
+  asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]), "=r"(u[4]), "=r"(u[5]), "=r"(u[6]),
+                 "=r"(u[7])
+               : "l"(p)
+               : "memory");
 }
 
 }  // namespace lm

@@ -195,7 +195,9 @@ struct SoftJob {
   long long ignore;
   int V, v0;                  // vocabulary, and the piece's first word
   const float *lse, *dloss;   // dloss: per row, or null (1; the products are scaled)
-  CUtensorMap g;              // planes of g, boxes of 32 x 32
+  __nv_bfloat16* g;           // [NP][M][ld], ld a multiple of 256
+  long long plane;
+  int ld;
   int* err;
   unsigned* rep;
 };
@@ -210,13 +212,13 @@ struct SoftEpi {
   int row = 0, col = 0, target = -1;
   float coef = 0.0f, lse = 0.0f;
   bool in = false, live = false;
-  uint8_t* box;  // this warp's output boxes
-  uint32_t turn = 0;
-  static constexpr int kBox = 2048, kBoxes = 2, kOut = kBoxes * kBox;
-  __device__ SoftEpi(const SoftJob& job, uint8_t* b) : j(job), box(b) {}
+  __device__ explicit SoftEpi(const SoftJob& job) : j(job) {}
+  int m_now = -1;
   __device__ void begin(const Product& p, int m, int n, int r, int c) {
-    row = r;
     col = c;
+    if (m == m_now) return;  // the same rows as the last tile's
+    m_now = m;
+    row = r;
     in = r < p.M;
     live = false;
     target = -1;
@@ -234,7 +236,7 @@ struct SoftEpi {
       coef = __int_as_float(0x7fffffff);
   }
   __device__ __forceinline__ void chunk(int c, float* v) {
-    const int at = target - (col + c), lane = threadIdx.x & 31;
+    const int at = target - (col + c);
     float* g = v;
     if (NP == 1) {
       const float l2 = lse * kLog2e;
@@ -251,22 +253,17 @@ struct SoftEpi {
     }
 #pragma unroll
     for (int i = 0; i < 32; ++i) g[i] = live ? g[i] * coef : 0.0f;
+    if (!in) return;
+    // columns past the piece's end stay inside the row's ld, and nothing reads them
+    __nv_bfloat16* to = j.g + (size_t)row * j.ld + col + c;
 #pragma unroll
     for (int q = 0; q < NP; ++q) {
-      box_reuse<kBoxes - 1>();
-      uint8_t* to = box + (turn++ % kBoxes) * kBox;
 #pragma unroll
-      for (int i = 0; i < 32; i += 8) {
-        uint32_t u[4];
+      for (int i = 0; i < 32; i += 16) {
+        uint32_t u[8];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) u[e] = take_plane<NP>(g[i + 2 * e], g[i + 2 * e + 1]);
-        *reinterpret_cast<uint4*>(to + box_piece16(lane, i / 8)) =
-            make_uint4(u[0], u[1], u[2], u[3]);
-      }
-      box_written();
-      if (lane == 0 && in) {
-        box_store(&j.g, tc::smem_u32(to), col + c, row, q);
-        box_commit();
+        for (int e = 0; e < 8; ++e) u[e] = take_plane<NP>(g[i + 2 * e], g[i + 2 * e + 1]);
+        store32(to + q * j.plane + i, u);
       }
     }
   }
@@ -278,11 +275,6 @@ __device__ __forceinline__ uint8_t* stage_memory() {
   return reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
                                     ~uintptr_t(1023));
 }
-// The epilogue warp's output boxes, behind the stages.
-template <typename T>
-__device__ __forceinline__ uint8_t* out_memory(uint8_t* stages) {
-  return stages + T::STAGES * T::STAGE + ((int)(threadIdx.x / 32) - 4) * T::OUT_BYTES;
-}
 template <int CG>
 __device__ __forceinline__ RunNext run_of(const Product& p) {
   const long long tiles = (long long)p.tm * p.tn, worker = blockIdx.x / CG, workers = gridDim.x / CG;
@@ -291,8 +283,7 @@ __device__ __forceinline__ RunNext run_of(const Product& p) {
 
 // A bf16 logit over more than 512 features is summed in chains: its loss shows
 // in the fp32 results otherwise (2e-6 of a logit at 2048).
-template <int NP, int CG, bool JOIN> using StatTile = Tile<NP, CG, 0, JOIN>;
-template <int NP, int CG> using SoftTile = Tile<NP, CG, SoftEpi<NP, CG>::kOut>;
+template <int NP, int CG, bool JOIN> using StatTile = Tile<NP, CG, JOIN>;
 
 template <int NP, int CG, bool JOIN>
 __global__ void __launch_bounds__(kGemmThreads, 1)
@@ -308,13 +299,11 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
 template <int NP, int CG>
 __global__ void __launch_bounds__(kGemmThreads, 1)
     k_loss_softmax(const __grid_constant__ SoftJob job) {
-  using T = SoftTile<NP, CG>;
+  using T = Tile<NP, CG>;
   __shared__ GemmShared sh;
   if (blockIdx.x == 0 && threadIdx.x == 0) tc::set_report(job.err, job.rep);
-  uint8_t* stages = stage_memory<T>();
-  SoftEpi<NP, CG> epi(job, out_memory<T>(stages));
-  gemm_roles<T>(sh, stages, run_of<CG>(job.p), epi, job.err);
-  if (threadIdx.x >= 128) box_drain();
+  SoftEpi<NP, CG> epi(job);
+  gemm_roles<T>(sh, stage_memory<T>(), run_of<CG>(job.p), epi, job.err);
 }
 
 // ------------------------------------------------------------------ join
@@ -465,13 +454,11 @@ struct DealNext {
 
 struct GradJob {
   Product p[2];            // dw of the piece's words, and dx
-  CUtensorMap out[2];      // their results, boxes of 32 x 32 (where `boxes`)
-  CUtensorMap sum;         // the running sum of dx, fp32
   Deal deal;
-  void* to[2];
-  int boxes;               // rows that TMA can step over
+  void* to[2];             // their results
   float* acc;              // [N][acc_ld] running sum of dx over pieces
   int acc_ld;
+  int wide;                // the results' rows are whole 32-byte sectors
   int first, last;         // of the pieces
   const float *scale, *count;  // the results' factor: (scale or 1) / (count or 1)
   const void* targets;
@@ -484,16 +471,12 @@ struct GradJob {
 template <int NP, int CG>
 struct GradEpi {
   using T = typename std::conditional<NP == 1, __nv_bfloat16, float>::type;
-  static constexpr int kOut = 4096;  // one fp32 box, or two of bf16 in turn
   const GradJob& j;
-  uint8_t* box;
-  uint32_t turn = 0;
-  bool wide = false;  // the last box was fp32
   const Product* p = nullptr;
   int row = 0, col = 0, which = 0;
   bool in = false, live = true;
   float scale = 1.0f;
-  __device__ GradEpi(const GradJob& job, uint8_t* b) : j(job), box(b) {
+  __device__ explicit GradEpi(const GradJob& job) : j(job) {
     if (j.scale) scale = *j.scale;
     if (j.count) scale = *j.count == 0.0f ? 0.0f : scale / *j.count;
   }
@@ -506,73 +489,44 @@ struct GradEpi {
     live = true;
     if (in && which == 1 && j.last) live = load_target(j.targets, j.i64, r) != j.ignore;
   }
-  // 32 fp32 values of every lane's row into a box
-  __device__ uint8_t* put32(const float* f) {
-    const int lane = threadIdx.x & 31;
-    box_reuse<0>();
-    wide = true;
-    uint8_t* to = box;
+  __device__ __forceinline__ void chunk(int c, float* f) {
+    if (!in) return;
+    const int D = p->N, left = D - (col + c);
+    uint32_t u[8];
+    if (which == 1) {  // the pieces' sum of dx; its rows are padded to whole chunks
+      float* acc = j.acc + (size_t)row * j.acc_ld + col + c;
+      if (!j.first) {
 #pragma unroll
-    for (int i = 0; i < 32; i += 4)
-      *reinterpret_cast<float4*>(to + box_piece32(lane, i / 4)) =
-          make_float4(f[i], f[i + 1], f[i + 2], f[i + 3]);
-    box_written();
-    return to;
-  }
-  __device__ uint8_t* put16(const float* f) {
-    const int lane = threadIdx.x & 31;
-    if (wide)
-      box_reuse<0>();
-    else
-      box_reuse<1>();
-    wide = false;
-    uint8_t* to = box + (turn++ & 1) * 2048;
+        for (int i = 0; i < 32; i += 8) {
+          load32(acc + i, u);
 #pragma unroll
-    for (int i = 0; i < 32; i += 8)
-      *reinterpret_cast<uint4*>(to + box_piece16(lane, i / 8)) =
-          make_uint4(tc::pack_bf16(f[i], f[i + 1]), tc::pack_bf16(f[i + 2], f[i + 3]),
-                     tc::pack_bf16(f[i + 4], f[i + 5]), tc::pack_bf16(f[i + 6], f[i + 7]));
-    box_written();
-    return to;
-  }
-  __device__ __forceinline__ void chunk(int c, float* v) {
-    const int D = p->N, left = D - (col + c), lane = threadIdx.x & 31;
-    float* f = v;
-    if (which == 1) {
+          for (int e = 0; e < 8; ++e) f[i + e] += __uint_as_float(u[e]);
+        }
+      }
       if (!j.last) {
-        // the pieces' sums of dx, added where they lie; a launch adds once
-        uint8_t* b = put32(f);
-        if (lane == 0 && in) {
-          if (j.first)
-            box_store(&j.sum, tc::smem_u32(b), col + c, row, 0);
-          else
-            box_add(&j.sum, tc::smem_u32(b), col + c, row, 0);
-          box_commit();
+#pragma unroll
+        for (int i = 0; i < 32; i += 8) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) u[e] = __float_as_uint(f[i + e]);
+          store32(acc + i, u);
         }
         return;
-      }
-      if (!j.first && in) {
-        const float* acc = j.acc + (size_t)row * j.acc_ld + col + c;
-#pragma unroll
-        for (int i = 0; i < 32; i += 4) {
-          const float4 o = *reinterpret_cast<const float4*>(acc + i);
-          f[i] += o.x;
-          f[i + 1] += o.y;
-          f[i + 2] += o.z;
-          f[i + 3] += o.w;
-        }
       }
     }
 #pragma unroll
     for (int i = 0; i < 32; ++i) f[i] = live ? f[i] * scale : 0.0f;
-    if (j.boxes) {
-      uint8_t* b = NP == 1 ? put16(f) : put32(f);
-      if (lane == 0 && in) {
-        box_store(&j.out[which], tc::smem_u32(b), col + c, row, 0);
-        box_commit();
+    T* out = static_cast<T*>(j.to[which]) + (size_t)row * D + col + c;
+    constexpr int W = 32 / sizeof(T);
+    if (j.wide && left >= 32) {
+#pragma unroll
+      for (int i = 0; i < 32; i += W) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          u[e] = NP == 1 ? tc::pack_bf16(f[i + 2 * e % W], f[i + (2 * e + 1) % W])
+                         : __float_as_uint(f[i + e % W]);
+        store32(out + i, u);
       }
-    } else if (in) {
-      T* out = static_cast<T*>(j.to[which]) + (size_t)row * D + col + c;
+    } else {
 #pragma unroll
       for (int i = 0; i < 32; ++i)
         if (i < left) Io<T>::store(out, i, f[i]);
@@ -580,20 +534,16 @@ struct GradEpi {
   }
 };
 
-template <int NP, int CG> using GradTile = Tile<NP, CG, GradEpi<NP, CG>::kOut>;
-
 template <int NP, int CG>
 __global__ void __launch_bounds__(kGemmThreads, 1)
     k_loss_grad(const __grid_constant__ GradJob job) {
-  using T = GradTile<NP, CG>;
+  using T = Tile<NP, CG>;
   __shared__ GemmShared sh;
   const int w = blockIdx.x / CG;
   const DealNext next{{&job.p[0], &job.p[1]}, job.deal.lo[0][w],     job.deal.lo[0][w + 1],
                       job.deal.lo[1][w],      job.deal.lo[1][w + 1], 0};
-  uint8_t* stages = stage_memory<T>();
-  GradEpi<NP, CG> epi(job, out_memory<T>(stages));
-  gemm_roles<T>(sh, stages, next, epi, job.err);
-  if (threadIdx.x >= 128) box_drain();
+  GradEpi<NP, CG> epi(job);
+  gemm_roles<T>(sh, stage_memory<T>(), next, epi, job.err);
 }
 
 // ------------------------------------------------------------------ host
@@ -693,23 +643,6 @@ bool plane_map(CUtensorMap* m, const __nv_bfloat16* base, long long rows, long l
   return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<__nv_bfloat16*>(base), dims, strides,
             box, es, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
-// A map for output boxes of 32 x 32 over planes of T, row stride ld elements.
-template <typename T>
-bool box_map(CUtensorMap* m, T* base, long long rows, long long cols, long long ld, long long plane,
-             int np) {
-  const EncodeTiledFn fn = encode_tiled();
-  if (!fn) return false;
-  constexpr bool f32 = sizeof(T) == 4;
-  const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)np};
-  const cuuint64_t strides[2] = {(cuuint64_t)ld * sizeof(T), (cuuint64_t)plane * sizeof(T)};
-  const cuuint32_t box[3] = {32, 32, 1};
-  const cuuint32_t es[3] = {1, 1, 1};
-  return fn(m, f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, base,
-            dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
-            f32 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
-            CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 // Tiles 0 .. n[k]-1 of two products, costing cost[k] each, to w workers in
@@ -900,17 +833,11 @@ slim_status bwd(const Sizes& z, const void* x, const void* w, const void* target
     GradJob q{};
     if (!make_product<NP, CG>(&j.p, xm, false, wm, false, z.N, n, z.D) ||
         !make_product<NP, CG>(&q.p[0], gm, true, xm, true, n, z.D, z.N) ||
-        !make_product<NP, CG>(&q.p[1], gm, false, wm, true, z.N, z.D, n) ||
-        !box_map(&j.g, ws.g, z.N, n, ps, z.N * ps, NP))
+        !make_product<NP, CG>(&q.p[1], gm, false, wm, true, z.N, z.D, n))
       return SLIM_ERR_CUDA;
     q.to[0] = static_cast<T*>(dw) + (size_t)v0 * z.D;
     q.to[1] = dx;
-    q.boxes = z.D * sizeof(T) % 16 == 0;
-    if (q.boxes && (!box_map(&q.out[0], (T*)q.to[0], n, z.D, z.D, (long long)n * z.D, 1) ||
-                    !box_map(&q.out[1], (T*)q.to[1], z.N, z.D, z.D, z.N * z.D, 1)))
-      return SLIM_ERR_CUDA;
-    if (ws.acc && !box_map(&q.sum, ws.acc, z.N, z.D, acc_ld(z.D), z.N * acc_ld(z.D), 1))
-      return SLIM_ERR_CUDA;
+    q.wide = z.D * sizeof(T) % 32 == 0 && ((uintptr_t)dw & 31) == 0 && ((uintptr_t)dx & 31) == 0;
     j.targets = q.targets = targets;
     j.i64 = q.i64 = it == SLIM_I64;
     j.ignore = q.ignore = ignore;
@@ -920,6 +847,9 @@ slim_status bwd(const Sizes& z, const void* x, const void* w, const void* target
     j.dloss = dstride ? dloss : nullptr;
     q.scale = dstride ? nullptr : dloss;
     q.count = count;
+    j.g = ws.g;
+    j.plane = z.N * ps;
+    j.ld = ps;
     j.err = q.err = ws.header;
     j.rep = q.rep = rep;
     const double fl = 2.0 * z.N * z.D * n, gb = 2.0 * NP * z.N * n;
@@ -927,7 +857,7 @@ slim_status bwd(const Sizes& z, const void* x, const void* w, const void* target
     {
       const long long wk = tiles < workers(CG) ? tiles : workers(CG);
       prof::Scope sc(prof::K_LOSS_SOFTMAX, s, fl, ((double)z.N + n) * z.D * 2 * NP + gb);
-      if (!launch<SoftTile<NP, CG>>(k_loss_softmax<NP, CG>, (unsigned)wk * CG, s, j,
+      if (!launch<Tile<NP, CG>>(k_loss_softmax<NP, CG>, (unsigned)wk * CG, s, j,
                                     once<SoftEpi<NP, CG>>()))
         return SLIM_ERR_CUDA;
     }
@@ -940,7 +870,7 @@ slim_status bwd(const Sizes& z, const void* x, const void* w, const void* target
     const int wk = (int)(nt[0] + nt[1] < workers(CG) ? nt[0] + nt[1] : workers(CG));
     deal_tiles(nt, cost, wk, &q.deal);
     prof::Scope sc(prof::K_LOSS_GRAD, s, 2 * fl, ((double)z.N + n) * z.D * 2 * NP + 2 * gb);
-    if (!launch<GradTile<NP, CG>>(k_loss_grad<NP, CG>, (unsigned)wk * CG, s, q,
+    if (!launch<Tile<NP, CG>>(k_loss_grad<NP, CG>, (unsigned)wk * CG, s, q,
                                  once<GradEpi<NP, CG>>()))
       return SLIM_ERR_CUDA;
   }
