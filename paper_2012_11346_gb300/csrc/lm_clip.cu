@@ -165,7 +165,8 @@ __device__ __forceinline__ double block_sum(double x, double* sh) {
 
 template <int CAP>
 __global__ void __launch_bounds__(kThreads) k_norm(const __grid_constant__ Table<CAP> tb,
-                                                   double* part) {
+                                                   double* part, int* header) {
+  if (header && blockIdx.x == 0 && threadIdx.x < 4) header[threadIdx.x] = 0;
   __shared__ double sh[kThreads / 32];
   double acc = 0.0;
   const unsigned total = tb.start[tb.n];
@@ -300,7 +301,8 @@ int fill(const List& l, int a, Table<CAP>* tb, bool* in_place, double* bytes) {
 }
 
 template <int CAP>
-slim_status run(const List& l, float max_norm, float* norm, double* part, cudaStream_t s) {
+slim_status run(const List& l, float max_norm, float* norm, int* header, double* part,
+                cudaStream_t s) {
   static_assert(sizeof(Table<CAP>) < 32764, "kernel parameters");
   Table<CAP> tb;
   tb.n = 0;
@@ -316,7 +318,7 @@ slim_status run(const List& l, float max_norm, float* norm, double* part, cudaSt
   do {
     a = fill(l, a, &tb, &in_place, &bytes);
     prof::Scope ps(prof::K_CLIP, s, 0.0, bytes);
-    k_norm<CAP><<<grid(), kThreads, 0, s>>>(tb, part + parts);
+    k_norm<CAP><<<grid(), kThreads, 0, s>>>(tb, part + parts, parts == 0 ? header : nullptr);
     if (cudaGetLastError() != cudaSuccess) return SLIM_ERR_CUDA;
     parts += (int)grid();
   } while (a < l.n);
@@ -340,7 +342,7 @@ slim_status run(const List& l, float max_norm, float* norm, double* part, cudaSt
 extern "C" slim_status slim_clip_workspace_size(int n, size_t* bytes) {
   if (!bytes || n < 0) return SLIM_ERR_INVALID_ARG;
   slim::Carver cv(nullptr);
-  cv.take<int>(4);  // the call's error word (no kernel here sets it)
+  cv.take<int>(4);
   const size_t groups = n == 0 ? 1 : ((size_t)n + slim::lm::kLarge - 1) / slim::lm::kLarge;
   cv.take<double>(groups * slim::lm::kGridNorm);
   *bytes = cv.bytes();
@@ -374,10 +376,10 @@ extern "C" slim_status slim_clip_grads(const void* const* src, void* const* dst,
   if (workspace == nullptr || workspace_bytes < need) return SLIM_ERR_WORKSPACE;
   if (reinterpret_cast<uintptr_t>(workspace) & 255u) return SLIM_ERR_INVALID_ARG;
   slim::Carver cv(workspace);
-  cv.take<int>(4);
+  int* header = cv.take<int>(4);  // the call's error word (no kernel here waits)
   double* part = cv.take<double>(0);
   const List l{src, dst, numel, dtypes, n};
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  if (live <= kSmall) return run<kSmall>(l, max_norm, norm, part, s);
-  return run<kLarge>(l, max_norm, norm, part, s);
+  if (live <= kSmall) return run<kSmall>(l, max_norm, norm, header, part, s);
+  return run<kLarge>(l, max_norm, norm, header, part, s);
 }

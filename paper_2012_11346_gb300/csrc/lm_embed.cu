@@ -196,8 +196,10 @@ __device__ void scatter_range(const SortSrc& s, long long a, long long e, int sh
 }
 
 __global__ void __launch_bounds__(kSortThreads) k_sort_count(SortSrc s, long long N, int tile,
-                                                             int shift, uint32_t* cnt) {
+                                                             int shift, uint32_t* cnt,
+                                                             int* header) {
   __shared__ uint32_t hist[kRadix];
+  if (blockIdx.x == 0 && threadIdx.x < 4) header[threadIdx.x] = 0;
   if (threadIdx.x < kRadix) hist[threadIdx.x] = 0;
   __syncthreads();
   const long long a = (long long)blockIdx.x * tile, e = a + tile < N ? a + tile : N;
@@ -244,7 +246,9 @@ __global__ void __launch_bounds__(kSortThreads) k_sort_scatter(SortSrc s, long l
 // The whole sort of a short list by one block, all passes in one launch.
 __global__ void __launch_bounds__(kSortThreads) k_sort_one(SortSrc s, long long N, int passes,
                                                            uint32_t* k0, uint32_t* p0,
-                                                           uint32_t* k1, uint32_t* p1) {
+                                                           uint32_t* k1, uint32_t* p1,
+                                                           int* header) {
+  if (threadIdx.x < 4) header[threadIdx.x] = 0;
   __shared__ uint32_t wh[kSortWarps][kRadix];
   __shared__ uint32_t base[kRadix], sums[kRadix / 32];
   for (int p = 0; p < passes; ++p) {
@@ -477,12 +481,13 @@ Plan plan(long long N, int V) {
 }
 
 struct Ws {
+  int* header;  // the call's error word (no kernel here waits)
   uint32_t *k0, *p0, *k1, *p1, *cnt;
   float* part;
 };
 Ws carve(Carver& cv, long long N, int D, const Plan& p) {
   Ws w;
-  cv.take<int>(4);  // the call's error word (no kernel here sets it)
+  w.header = cv.take<int>(4);
   w.k0 = cv.take<uint32_t>(N);
   w.p0 = cv.take<uint32_t>(N);
   w.k1 = cv.take<uint32_t>(p.passes > 1 ? N : 0);
@@ -510,13 +515,15 @@ slim_status sort(const void* ids, slim_index itype, long long N, int V, const Pl
   SortSrc src{ids, itype == SLIM_I64, V, nullptr, nullptr};
   if (N <= kOneBlock) {
     prof::Scope ps(prof::K_EMBED_SORT, s);
-    k_sort_one<<<1, kSortThreads, 0, s>>>(src, N, p.passes, w.k0, w.p0, w.k1, w.p1);
+    k_sort_one<<<1, kSortThreads, 0, s>>>(src, N, p.passes, w.k0, w.p0, w.k1, w.p1,
+                                       w.header);
     if (!launched()) return SLIM_ERR_CUDA;
   } else {
     for (int i = 0; i < p.passes; ++i) {
       {
         prof::Scope ps(prof::K_EMBED_SORT, s);
-        k_sort_count<<<p.tiles, kSortThreads, 0, s>>>(src, N, p.tile, i * kRadixBits, w.cnt);
+        k_sort_count<<<p.tiles, kSortThreads, 0, s>>>(src, N, p.tile, i * kRadixBits, w.cnt,
+                                                     w.header);
         if (!launched()) return SLIM_ERR_CUDA;
       }
       uint32_t *ko = i & 1 ? w.k1 : w.k0, *po = i & 1 ? w.p1 : w.p0;

@@ -16,6 +16,8 @@
 #include "../../include/slim_lm.h"
 #include "common.cuh"
 #include "lm_gemm.cuh"
+#include "lm_loss_dev.cuh"
+#include "lm_loss_rows.h"
 #include "profiler.h"
 #include "report.h"
 #include "tma_map.h"
@@ -24,12 +26,7 @@ namespace slim {
 namespace lm {
 namespace {
 
-constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kPieceStep = 256;  // pieces are multiples of this
-
-__device__ __forceinline__ long long load_target(const void* t, int i64, long long i) {
-  return i64 ? static_cast<const long long*>(t)[i] : static_cast<const int*>(t)[i];
-}
 
 // 2^x.  The fast form is within a few units of 2^-22; fp32 problems take the
 // accurate one.
@@ -329,72 +326,49 @@ __global__ void __launch_bounds__(256) k_loss_join(JoinJob j) {
   const int lanes = 1 << j.lanes_log2, lane = threadIdx.x & (lanes - 1);
   const long long row = (long long)blockIdx.x * (256 >> j.lanes_log2) + (threadIdx.x >> j.lanes_log2);
   const bool in = row < j.N;
-  float base = -INFINITY, sum = 0.0f;
-  auto add = [&](float b, float x) {
-    const float to = fmaxf(base, b), ref = to == -INFINITY ? 0.0f : to;
-    sum = sum * exp2f(base - ref) + x * exp2f(b - ref);
-    base = to;
-  };
+  LogSum a;
   if (in) {
     const long long m = row / j.tile_rows;
     const long long first = run_owner(m * j.tn, j.tiles, j.workers);
     const long long last = run_owner(m * j.tn + j.tn - 1, j.tiles, j.workers);
     const int n = (int)(last - first + 1) * 4;
+    const float2* p = j.part + (size_t)m * j.slots * j.tile_rows + (row - m * j.tile_rows);
     for (int s = lane; s < n; s += lanes) {
-      const float2 a = j.part[((size_t)m * j.slots + s) * j.tile_rows + (row - m * j.tile_rows)];
-      add(a.x, a.y);
+      const float2 x = p[(size_t)s * j.tile_rows];
+      a.add(x.x, x.y);
     }
   }
   for (int o = lanes >> 1; o; o >>= 1)
-    add(__shfl_xor_sync(0xffffffffu, base, o), __shfl_xor_sync(0xffffffffu, sum, o));
+    a.add(__shfl_xor_sync(0xffffffffu, a.base, o), __shfl_xor_sync(0xffffffffu, a.sum, o));
   float loss = 0.0f, counted = 0.0f;
   if (in && lane == 0) {
-    // log of the weight of every word but the target: a base of some tens and a
-    // logarithm, joined in fp64 so that only the result is rounded
-    const double rest64 = ((double)base + (double)log2f(sum)) * 0.69314718055994531;
-    const float rest = (float)rest64;
-    const long long t = load_target(j.targets, j.i64, row);
-    float lse = rest;
-    if (t != j.ignore) {
+    float lse;
+    if (finish_loss(a, load_target(j.targets, j.i64, row), j.ignore, j.V, j.zt + row, loss, lse))
       counted = 1.0f;
-      if (t >= 0 && t < j.V) {
-        const float z = j.zt[row], d = (float)(rest64 - (double)z);
-        if (rest == -INFINITY && z > -INFINITY) {  // the target is all there is
-          lse = z;
-        } else {
-          const float small = log1pf(expf(-fabsf(d)));
-          loss = d > 0.0f ? d + small : small;
-          lse = d > 0.0f ? rest + small : z + small;
-          if (d != d) lse = loss = d;
-        }
-      } else {
-        loss = __int_as_float(0x7fffffff);
-      }
-    }
     j.loss[row] = loss;
     j.lse[row] = lse;
   }
   // sums over the block's rows, in a fixed order
   __shared__ float sl[8], sc[8];
   __shared__ bool last;
-  float a = loss, b = counted;
+  float ls = loss, cs = counted;
   for (int o = 16; o; o >>= 1) {
-    a += __shfl_xor_sync(0xffffffffu, a, o);
-    b += __shfl_xor_sync(0xffffffffu, b, o);
+    ls += __shfl_xor_sync(0xffffffffu, ls, o);
+    cs += __shfl_xor_sync(0xffffffffu, cs, o);
   }
   if ((threadIdx.x & 31) == 0) {
-    sl[threadIdx.x >> 5] = a;
-    sc[threadIdx.x >> 5] = b;
+    sl[threadIdx.x >> 5] = ls;
+    sc[threadIdx.x >> 5] = cs;
   }
   __syncthreads();
   if (threadIdx.x == 0) {
-    a = b = 0.0f;
+    ls = cs = 0.0f;
     for (int i = 0; i < 8; ++i) {
-      a += sl[i];
-      b += sc[i];
+      ls += sl[i];
+      cs += sc[i];
     }
-    j.block_sum[2 * blockIdx.x] = a;
-    j.block_sum[2 * blockIdx.x + 1] = b;
+    j.block_sum[2 * blockIdx.x] = ls;
+    j.block_sum[2 * blockIdx.x + 1] = cs;
     __threadfence();
     last = atomicAdd(j.done, 1u) == gridDim.x - 1;
   }
@@ -799,7 +773,10 @@ slim_status fwd(const Sizes& z, const void* x, const void* w, const void* target
   q.tile_rows = kTM * CG;
   q.tiles = tiles;
   q.workers = wk;
-  while (q.lanes_log2 < 5 && (1 << q.lanes_log2) < j.slots) ++q.lanes_log2;
+  // neighbouring threads take neighbouring rows (their statistics lie side by
+  // side); several per row only where the rows alone are too few
+  while (q.lanes_log2 < 5 && (1 << q.lanes_log2) < j.slots && (z.N << q.lanes_log2) < 65536)
+    ++q.lanes_log2;
   q.loss = loss;
   q.lse = lse;
   q.block_sum = ws.block_sum;
@@ -889,6 +866,10 @@ extern "C" slim_status slim_vocab_loss_workspace_size(long long N, int D, int V,
                                                       int piece, int backward, size_t* bytes) {
   using namespace slim::lm;
   if (!bytes || !sizes_ok(N, D, V, dtype) || (backward && piece < 1)) return SLIM_ERR_INVALID_ARG;
+  if (rows_fit(N, D)) {
+    *bytes = rows_workspace((int)N, D, V, backward != 0);
+    return SLIM_OK;
+  }
   slim::Carver cv(nullptr);
   carve(cv, Sizes{N, D, V, dtype}, piece, backward != 0);
   *bytes = cv.bytes();
@@ -914,6 +895,9 @@ extern "C" slim_status slim_vocab_loss_fwd(const void* x, const void* w, const v
   slim_vocab_loss_workspace_size(N, D, V, dtype, 1, 0, &need);
   if (workspace == nullptr || workspace_bytes < need) return SLIM_ERR_WORKSPACE;
   if (!aligned(workspace, 256)) return SLIM_ERR_INVALID_ARG;
+  if (rows_fit(N, D))
+    return rows_fwd(x, w, targets, itype, (int)N, D, V, dtype, ignore_index, loss, lse, total,
+                    workspace, s);
   unsigned* rep = nullptr;
   const slim_status st = slim::report::begin(workspace, true, &rep);
   if (st != SLIM_OK) return st;
@@ -949,6 +933,9 @@ extern "C" slim_status slim_vocab_loss_bwd(const void* x, const void* w, const v
   slim_vocab_loss_workspace_size(N, D, V, dtype, piece, 1, &need);
   if (workspace == nullptr || workspace_bytes < need) return SLIM_ERR_WORKSPACE;
   if (!aligned(workspace, 256)) return SLIM_ERR_INVALID_ARG;
+  if (rows_fit(N, D))
+    return rows_bwd(x, w, targets, itype, lse, dloss, dloss_stride, count, (int)N, D, V, dtype,
+                    ignore_index, dx, dw, workspace, s);
   unsigned* rep = nullptr;
   const slim_status st = slim::report::begin(workspace, true, &rep);
   if (st != SLIM_OK) return st;

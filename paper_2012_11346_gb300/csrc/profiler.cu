@@ -17,7 +17,8 @@ const char* kNames[K_COUNT] = {
     "tc_bwd",      "tc_delta",      "tc_scan",        "tc_bwd_q",      "tc_bwd_kv",
     "tc_reduce",   "tc_selftest",   "tc_prep",        "stack_rows",
     "embed_fwd",   "embed_sort",    "embed_sum",      "clip",          "loss_prep",
-    "loss_stats",  "loss_join",     "loss_softmax",   "loss_grad"};
+    "loss_stats",  "loss_join",     "loss_softmax",   "loss_grad",
+    "loss_rows"};
 
 struct Rec {
   Kid k;

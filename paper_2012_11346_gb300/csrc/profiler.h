@@ -35,6 +35,7 @@ enum Kid {
   K_LOSS_JOIN,
   K_LOSS_SOFTMAX,
   K_LOSS_GRAD,
+  K_LOSS_ROWS,
   K_COUNT
 };
 

@@ -8,6 +8,7 @@ raise.
 """
 import contextlib
 import ctypes
+import functools
 import os
 
 import torch
@@ -138,6 +139,13 @@ def bwd_schedule(B, H, L, d, M, C, dtype, feature):
 def _stream_handle(stream):
     s = torch.cuda.current_stream() if stream is None else stream
     return ctypes.c_void_p(s.cuda_stream)
+
+
+def _stream_of(t, stream):
+    """The raw stream of a call on tensor t: `stream`, or the current one."""
+    if stream is not None:
+        return stream.cuda_stream
+    return torch._C._cuda_getCurrentRawStream(t.get_device())
 
 
 def _workspace(nbytes, device):
@@ -471,13 +479,17 @@ def _require_dtype(what, *ts):
         raise TypeError(f"{what}: one dtype expected, got {[t.dtype for t in ts]}")
 
 
+_HERE = contextlib.nullcontext()
+
+
 def _on(stream):
     """The context in which a call on `stream` allocates: memory that the
     caching allocator hands out there is free as far as that stream's order
     goes, and is given out again only behind the call's work."""
-    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
+    return _HERE if stream is None else torch.cuda.stream(stream)
 
 
+@functools.lru_cache(maxsize=1024)
 def embed_workspace_size(N, D, V, dtype):
     n = _sz(0)
     _check(library().slim_embed_bwd_workspace_size(N, D, V, DTYPES[dtype], ctypes.byref(n)),
@@ -502,7 +514,7 @@ def embed_forward(ids, table, scale=1.0, out=None, stream=None):
                  "out must be [*ids.shape, D] in the table's dtype")
     _check(library().slim_embed_fwd(ids.data_ptr(), INDEX_DTYPES[ids.dtype], table.data_ptr(),
                                     ids.numel(), D, V, DTYPES[table.dtype], scale,
-                                    out.data_ptr(), _stream_handle(stream)), "slim_embed_fwd")
+                                    out.data_ptr(), _stream_of(table, stream)), "slim_embed_fwd")
     return out
 
 
@@ -528,10 +540,11 @@ def embed_backward(ids, dout, V, scale=1.0, dtable=None, workspace=None, stream=
     _check(library().slim_embed_bwd(ids.data_ptr(), INDEX_DTYPES[ids.dtype], dout.data_ptr(), N, D,
                                     V, DTYPES[dout.dtype], scale, int(accumulate),
                                     dtable.data_ptr(), ws.data_ptr(), ws.numel(),
-                                    _stream_handle(stream)), "slim_embed_bwd")
+                                    _stream_of(dout, stream)), "slim_embed_bwd")
     return dtable
 
 
+@functools.lru_cache(maxsize=1024)
 def clip_workspace_size(n):
     """Workspace bytes of clip_grad_norm for n gradients."""
     b = _sz(0)
@@ -542,35 +555,36 @@ def clip_workspace_size(n):
 def clip_grad_norm(grads, max_norm, out=None, workspace=None, stream=None):
     """slim_clip_grads: scales the gradients by min(1, max_norm / norm), norm
     being their global 2-norm, and returns norm ([1] fp32, on the device).
-    In place, or into the tensors of `out` (same shapes and dtypes).  If the
+    In place, or into the tensors of `out` (same sizes and dtypes).  If the
     norm is not finite nothing is scaled: read it and skip the step."""
     grads = list(grads)
-    dst = grads if out is None else list(out)
-    _require(len(dst) == len(grads), "out must have one tensor per gradient")
-    _require(len(grads) > 0, "no gradients")
-    _require_cuda(*grads)
-    if out is not None:
-        _require_cuda(*dst)
-        for g, o in zip(grads, dst):
-            _require(o.shape == g.shape and o.dtype == g.dtype,
-                     "out must have the gradients' shapes and dtypes")
     n = len(grads)
-    for g in grads:
-        if g.dtype not in DTYPES:
-            raise TypeError(f"gradients must be float32 or bfloat16, got {g.dtype}")
+    _require(n > 0, "no gradients")
+    _require_cuda(*grads)
+    try:
+        dts = [DTYPES[g.dtype] for g in grads]
+    except KeyError as e:
+        raise TypeError(f"gradients must be float32 or bfloat16, got {e.args[0]}") from None
+    sizes = [g.numel() for g in grads]
+    src = [g.data_ptr() for g in grads]
+    _require(len(set(src)) == n or len({p for p, k in zip(src, sizes) if k}) ==
+             sum(k > 0 for k in sizes), "a gradient is listed twice")
     ptr = ctypes.c_void_p * n
-    src_p = ptr(*[g.data_ptr() for g in grads])
-    _require(len({a for a, g in zip(src_p, grads) if g.numel()}) ==
-             sum(g.numel() > 0 for g in grads), "a gradient is listed twice")
-    dst_p = src_p if out is None else ptr(*[o.data_ptr() for o in dst])
-    numel = (_ll * n)(*[g.numel() for g in grads])
-    dts = (_i * n)(*[DTYPES[g.dtype] for g in grads])
+    src_p = dst_p = ptr(*src)
+    if out is not None:
+        dst = list(out)
+        _require_cuda(*dst)
+        _require([o.numel() for o in dst] == sizes and
+                 [o.dtype for o in dst] == [g.dtype for g in grads],
+                 "out must hold one tensor of the same size and dtype per gradient")
+        dst_p = ptr(*[o.data_ptr() for o in dst])
     with _on(stream):
         norm = torch.empty(1, dtype=torch.float32, device=grads[0].device)
         ws = workspace if workspace is not None else _workspace(clip_workspace_size(n),
                                                                 norm.device)
-    _check(library().slim_clip_grads(src_p, dst_p, numel, dts, n, max_norm, norm.data_ptr(),
-                                     ws.data_ptr(), ws.numel(), _stream_handle(stream)),
+    _check(library().slim_clip_grads(src_p, dst_p, (_ll * n)(*sizes), (_i * n)(*dts), n, max_norm,
+                                     norm.data_ptr(),
+                                     ws.data_ptr(), ws.numel(), _stream_of(norm, stream)),
            "slim_clip_grads")
     return norm
 
@@ -602,6 +616,7 @@ def vocab_piece(N, V):
     return min(V, max(8192, (1 << 28) // max(N, 1)))
 
 
+@functools.lru_cache(maxsize=1024)
 def vocab_loss_workspace_size(N, D, V, dtype, backward, piece=None):
     n = _sz(0)
     piece = vocab_piece(N, V) if piece is None else piece
@@ -637,7 +652,7 @@ def vocab_loss_forward(x, w, targets, ignore_index=-100, workspace=None, stream=
                                          INDEX_DTYPES[targets.dtype], N, D, V, DTYPES[x.dtype],
                                          ignore_index, loss.data_ptr(), lse.data_ptr(),
                                          total.data_ptr(), ws.data_ptr(), ws.numel(),
-                                         _stream_handle(stream)), "slim_vocab_loss_fwd")
+                                         _stream_of(x, stream)), "slim_vocab_loss_fwd")
     return loss, lse, total
 
 
@@ -666,7 +681,7 @@ def vocab_loss_backward(x, w, targets, lse, dloss, count=None, ignore_index=-100
                                          dloss.data_ptr(), int(dloss.numel() > 1), _ptr(count), N,
                                          D, V, DTYPES[x.dtype], piece, ignore_index, dx.data_ptr(),
                                          dw.data_ptr(), ws.data_ptr(), ws.numel(),
-                                         _stream_handle(stream)), "slim_vocab_loss_bwd")
+                                         _stream_of(x, stream)), "slim_vocab_loss_bwd")
     return dx, dw
 
 

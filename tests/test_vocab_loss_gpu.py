@@ -99,6 +99,39 @@ def test_loss_and_gradients(cuda_device, N, D, V, dt, mean):
     check(x, w, t, c, mean=mean)
 
 
+FEW = [(1, 512, 5000), (2, 96, 4097), (3, 1000, 333), (4, 4096, 50), (1, 16384, 40), (8, 2048, 65),
+       (5, 100, 20001), (8, 37, 1000), (7, 515, 200), (8, 2056, 40), (9, 64, 3000), (6, 8, 3)]
+
+
+@pytest.mark.parametrize("dt", [F32, BF16])
+@pytest.mark.parametrize("N,D,V", FEW)
+@pytest.mark.parametrize("mean", [False, True])
+def test_few_rows(cuda_device, N, D, V, dt, mean):
+    """Up to eight rows take kernels of their own (fp32 products in either type)."""
+    x, w, t, c = make(cuda_device, N, D, V, dt, ignored=0.3)
+    a, b = check(x, w, t, c, mean=mean), check(x, w, t, c, mean=mean)
+    for u, v in zip(a, b):
+        assert torch.equal(u, v)
+
+
+@pytest.mark.parametrize("dt", [F32, BF16])
+def test_few_rows_ignored_and_bad(cuda_device, dt):
+    x, w, t, c = make(cuda_device, 6, 64, 500, dt, ignored=0.0)
+    t[2] = -100
+    clean = check(x, w, t, c)
+    y, d = x.clone(), c.clone()
+    y[2], d[2] = float("nan"), float("inf")
+    loss, lse, total = slim.vocab_loss_forward(y, w, t)
+    dx, dw = slim.vocab_loss_backward(y, w, t, lse, d)
+    for a, b in zip((loss, total, dx, dw), (clean[0], clean[2], clean[3], clean[4])):
+        assert torch.equal(a, b)
+    t[4] = 500
+    loss, lse, total = slim.vocab_loss_forward(x, w, t)
+    dx, dw = slim.vocab_loss_backward(x, w, t, lse, c)
+    assert torch.isnan(loss).tolist() == [i == 4 for i in range(6)]
+    assert torch.isnan(dx[4]).all() and torch.isfinite(dx[:4]).all() and torch.isnan(dw).all()
+
+
 @pytest.mark.parametrize("dt", [F32, BF16])
 @pytest.mark.parametrize("piece", [1, 256, 300, 768, 1 << 20])
 def test_pieces(cuda_device, dt, piece):
