@@ -54,6 +54,49 @@ struct Product {
   int M, N;
   int tm, tn;      // tiles each way (tm in tiles of kTM * CG rows)
   int kb;          // stages (of kTK) of the reduction
+  int splits;      // parts of the reduction, computed as tiles of their own
+};
+
+// One tile: stages [k0, k1) of product p's reduction.
+struct Work {
+  const Product* p;
+  int m, n, split, k0, k1;
+};
+// A contiguous range of a product's tiles, columns and splits fastest.  It is
+// walked by counting: a division per tile would hold up every role.
+struct TileRange {
+  const Product* p;
+  int m, n, split;
+  long long left;
+  __device__ __forceinline__ TileRange(const Product* q, long long begin, long long end)
+      : p(q), left(end - begin) {
+    const long long tile = begin / q->splits;
+    split = (int)(begin - tile * q->splits);
+    m = (int)(tile / q->tn);
+    n = (int)(tile - (long long)m * q->tn);
+  }
+  __device__ __forceinline__ bool next(Work& w) {
+    if (left <= 0) return false;
+    --left;
+    w.p = p;
+    w.m = m;
+    w.n = n;
+    w.split = split;
+    w.k0 = 0;
+    w.k1 = p->kb;
+    if (p->splits > 1) {
+      w.k0 = (int)((long long)split * p->kb / p->splits);
+      w.k1 = (int)((long long)(split + 1) * p->kb / p->splits);
+    }
+    if (++split == p->splits) {
+      split = 0;
+      if (++n == p->tn) {
+        n = 0;
+        ++m;
+      }
+    }
+    return true;
+  }
 };
 
 struct GemmShared {
@@ -194,52 +237,6 @@ __device__ __forceinline__ void gemm_end(GemmShared& sh, bool failed) {
   if (threadIdx.x / 32 == 2) gemm_tmem_free<CG>(sh.tmem, 2 * kTN);
 }
 
-// The copying thread.  `next(p, m, n)` yields this worker's tiles in order:
-// the same sequence in every role.  False if a wait gave up.
-template <typename T, typename Next>
-__device__ bool gemm_copy(GemmShared& sh, uint8_t* stages, Next next, int* err) {
-  constexpr int NP = T::PLANES, CG = T::GROUP;
-  const uint32_t rank = CG == 1 ? 0 : cluster_rank();
-  const Product* p;
-  int m, n;
-  uint32_t it = 0;
-  while (next(p, m, n)) {
-    const int row = (m * CG + (int)rank) * kTM, col = n * kTN + (int)rank * T::BROWS;
-    for (int kb = 0; kb < p->kb; ++kb) {
-#pragma unroll 1
-      for (int q = 0; q < NP; ++q, ++it) {
-        const int st = it % T::STAGES;
-        if (!tc::mbar_wait(tc::smem_u32(&sh.empty[st]), ((it / T::STAGES) & 1) ^ 1, err))
-          return false;
-        uint32_t full = tc::smem_u32(&sh.full[st]);
-        if (rank == 0) tc::mbar_expect_tx(full, CG * T::STAGE);
-        if (CG == 2) full = map_to_rank(full, 0);
-        const uint32_t sa = tc::smem_u32(stages) + st * T::STAGE, sb = sa + T::A_BYTES;
-        const int k = kb * kTK;
-        if (p->a_mn) {
-#pragma unroll
-          for (int j = 0; j < kTM / 64; ++j)
-            gemm_tma<CG>(sa + j * 8192, &p->a, row + 64 * j, k, q, full);
-        } else {
-          gemm_tma<CG>(sa, &p->a, k, row, q, full);
-        }
-        if (p->b_mn) {
-#pragma unroll
-          for (int j = 0; j < T::BROWS / 64; ++j)
-            gemm_tma<CG>(sb + j * 8192, &p->b, col + 64 * j, k, q, full);
-        } else {
-          gemm_tma<CG>(sb, &p->b, k, col, q, full);
-        }
-      }
-    }
-  }
-  // every stage handed back: no arrival is on its way when the block leaves
-  for (int i = 0; i < T::STAGES; ++i, ++it)
-    if (!tc::mbar_wait(tc::smem_u32(&sh.empty[it % T::STAGES]), ((it / T::STAGES) & 1) ^ 1, err))
-      return false;
-  return true;
-}
-
 // One lane of a converged warp, the same every time.  ptxas knows that a branch
 // on it holds one thread, and keeps what the MMAs take in uniform registers.
 __device__ __forceinline__ bool elect_one() {
@@ -252,13 +249,88 @@ __device__ __forceinline__ bool elect_one() {
   return p != 0;
 }
 
+// A value that all lanes agree on, told to the compiler as such: what an MMA and
+// its loop take comes from uniform registers.
+template <typename V>
+__device__ __forceinline__ V uniform(V x) {
+  return __shfl_sync(0xffffffffu, x, 0);
+}
+__device__ __forceinline__ const CUtensorMap* uniform(const CUtensorMap* x) {
+  return reinterpret_cast<const CUtensorMap*>(
+      __shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(x), 0));
+}
+
+// The copying warp.  `next(work)` yields this worker's tiles in order: the same
+// sequence in every role.  All lanes walk the loop and one of them issues, as for
+// the MMAs: a lone thread with its operands in ordinary registers took 600
+// cycles for a stage's four copies, more than the stage's MMAs.  False if a wait
+// gave up.
+template <typename T, typename Next>
+__device__ bool gemm_copy(GemmShared& sh, uint8_t* stages, Next next, int* err) {
+  constexpr int NP = T::PLANES, CG = T::GROUP;
+  const int rank = CG == 1 ? 0 : uniform((int)cluster_rank());
+  const uint32_t full0 = tc::smem_u32(&sh.full[0]), empty0 = tc::smem_u32(&sh.empty[0]);
+  const uint32_t count0 = CG == 2 ? map_to_rank(full0, 0) : full0;  // the leader's
+  const uint32_t smem = tc::smem_u32(stages);
+  uint32_t st = 0, phase = 1;
+  auto step_on = [&] {
+    if (++st == T::STAGES) {
+      st = 0;
+      phase ^= 1;
+    }
+  };
+  auto free = [&] {
+    return __all_sync(0xffffffffu, tc::mbar_wait(empty0 + 8 * st, phase, err));
+  };
+  Work w;
+  while (next(w)) {
+    const CUtensorMap* map_a = uniform(&w.p->a);
+    const CUtensorMap* map_b = uniform(&w.p->b);
+    const int a_mn = uniform(w.p->a_mn), b_mn = uniform(w.p->b_mn);
+    const int row = uniform((w.m * CG + rank) * kTM), col = uniform(w.n * kTN + rank * T::BROWS);
+    const int k1 = uniform(w.k1) * kTK;
+    for (int k = uniform(w.k0) * kTK; k < k1; k += kTK) {
+#pragma unroll 1
+      for (int q = 0; q < NP; ++q) {
+        if (!free()) return false;
+        if (elect_one()) {
+          if (rank == 0) tc::mbar_expect_tx(full0 + 8 * st, CG * T::STAGE);
+          const uint32_t full = count0 + 8 * st;
+          const uint32_t sa = smem + st * T::STAGE, sb = sa + T::A_BYTES;
+          if (a_mn) {
+#pragma unroll
+            for (int j = 0; j < kTM / 64; ++j)
+              gemm_tma<CG>(sa + j * 8192, map_a, row + 64 * j, k, q, full);
+          } else {
+            gemm_tma<CG>(sa, map_a, k, row, q, full);
+          }
+          if (b_mn) {
+#pragma unroll
+            for (int j = 0; j < T::BROWS / 64; ++j)
+              gemm_tma<CG>(sb + j * 8192, map_b, col + 64 * j, k, q, full);
+          } else {
+            gemm_tma<CG>(sb, map_b, k, col, q, full);
+          }
+        }
+        __syncwarp();
+        step_on();
+      }
+    }
+  }
+  // every stage handed back: no arrival is on its way when the block leaves
+  for (int i = 0; i < T::STAGES; ++i) {
+    if (!free()) return false;
+    step_on();
+  }
+  return true;
+}
+
 // The warp that issues MMAs (of the leading block of a pair).  All lanes walk
 // the loop; one of them issues.
 template <typename T, typename Next>
 __device__ bool gemm_multiply(GemmShared& sh, uint8_t* stages, Next next, int* err) {
   constexpr int CG = T::GROUP;
-  const Product* p;
-  int m, n;
+  Work w;
   const uint32_t full0 = tc::smem_u32(&sh.full[0]), empty0 = tc::smem_u32(&sh.empty[0]);
   const uint32_t tmem = sh.tmem;
   uint32_t st = 0, phase = 0, acc = 0;
@@ -273,13 +345,15 @@ __device__ bool gemm_multiply(GemmShared& sh, uint8_t* stages, Next next, int* e
     tc::tc_fence_after();
     return ok;
   };
-  while (next(p, m, n)) {
-    const uint32_t idesc = tc::idesc_bf16(kTM * CG, kTN, p->a_mn, p->b_mn);
-    const uint32_t a_step = p->a_mn ? 128 : 2, b_step = p->b_mn ? 128 : 2;
-    const uint64_t a0 = tc::sdesc(tc::smem_u32(stages), p->a_mn ? 8192 : 16, 1024);
-    const uint64_t b0 = tc::sdesc(tc::smem_u32(stages) + T::A_BYTES, p->b_mn ? 8192 : 16, 1024);
-    const int kb = p->kb, step = T::ACC ? T::CHAIN : kb;
-    for (int k0 = 0; k0 < kb; k0 += step, ++acc) {
+  while (next(w)) {
+    const int a_mn = uniform(w.p->a_mn), b_mn = uniform(w.p->b_mn);
+    const int first = uniform(w.k0), last = uniform(w.k1);
+    const uint32_t idesc = tc::idesc_bf16(kTM * CG, kTN, a_mn, b_mn);
+    const uint32_t a_step = a_mn ? 128 : 2, b_step = b_mn ? 128 : 2;
+    const uint64_t a0 = tc::sdesc(tc::smem_u32(stages), a_mn ? 8192 : 16, 1024);
+    const uint64_t b0 = tc::sdesc(tc::smem_u32(stages) + T::A_BYTES, b_mn ? 8192 : 16, 1024);
+    const int step = T::ACC ? T::CHAIN : last - first;
+    for (int k0 = first; k0 < last; k0 += step, ++acc) {
       const uint32_t buf = acc & 1;
       if (!wait(tc::smem_u32(&sh.tempty[buf]), ((acc >> 1) & 1) ^ 1)) return false;
       const uint32_t d = tmem + buf * kTN;
@@ -292,7 +366,7 @@ __device__ bool gemm_multiply(GemmShared& sh, uint8_t* stages, Next next, int* e
           gemm_mma<CG>(d, da + j * a_step, db + j * b_step, idesc, j == 0 ? more : 1u);
       };
       auto done = [&](uint32_t i) { gemm_commit<CG>(empty0 + 8 * i); };
-      const int k1 = min(k0 + step, kb);
+      const int k1 = min(k0 + step, last);
       for (int k = k0; k < k1; ++k) {
         const uint32_t s0 = st;
         if (!wait(full0 + 8 * s0, phase)) return false;
@@ -334,7 +408,7 @@ __device__ bool gemm_multiply(GemmShared& sh, uint8_t* stages, Next next, int* e
   return true;
 }
 
-// An epilogue warp.  For every tile, epi.begin(p, m, n, row, col0) once, then
+// An epilogue warp.  For every tile, epi.begin(work, row, col0) once, then
 // epi.chunk(c, v) for each 32 columns col0 + c .. of row `row` (of this thread)
 // that begin inside the product (v is the epilogue's to change).  Reads past the product's rows still run (their
 // values are zero sums); the epilogue drops them.
@@ -342,18 +416,18 @@ template <typename T, typename Next, typename Epi>
 __device__ bool gemm_finish(GemmShared& sh, Next next, Epi& epi, int* err) {
   constexpr int CG = T::GROUP;
   const uint32_t rank = CG == 1 ? 0 : cluster_rank();
-  const int w = threadIdx.x / 32 - 4, lane = threadIdx.x & 31;
-  const int quarter = w & 3, part = w >> 2;
-  const Product* p;
-  int m, n;
+  const int warp = threadIdx.x / 32 - 4, lane = threadIdx.x & 31;
+  const int quarter = warp & 3, part = warp >> 2;
+  Work w;
   uint32_t acc = 0;
-  while (next(p, m, n)) {
-    const int row = (m * CG + (int)rank) * kTM + quarter * 32 + lane;
-    const int col = n * kTN + part * kEpiCols;
-    const int step = T::ACC ? T::CHAIN : p->kb;
+  while (next(w)) {
+    const Product* p = w.p;
+    const int row = (w.m * CG + (int)rank) * kTM + quarter * 32 + lane;
+    const int col = w.n * kTN + part * kEpiCols;
+    const int step = T::ACC ? T::CHAIN : w.k1 - w.k0;
     float sum[T::ACC ? kEpiCols : 1];
-    epi.begin(*p, m, n, row, col);
-    for (int k0 = 0; k0 < p->kb; k0 += step, ++acc) {
+    epi.begin(w, row, col);
+    for (int k0 = w.k0; k0 < w.k1; k0 += step, ++acc) {
       const int buf = acc & 1;
       if (!tc::mbar_wait(tc::smem_u32(&sh.tfull[buf]), (acc >> 1) & 1, err)) return false;
       tc::tc_fence_after();
@@ -366,7 +440,7 @@ __device__ bool gemm_finish(GemmShared& sh, Next next, Epi& epi, int* err) {
           float v[16];
           tc::tmem_ld16(t + c, v);
 #pragma unroll
-          for (int i = 0; i < 16; ++i) sum[c + i] = k0 == 0 ? v[i] : sum[c + i] + v[i];
+          for (int i = 0; i < 16; ++i) sum[c + i] = k0 == w.k0 ? v[i] : sum[c + i] + v[i];
         }
       } else {
 #pragma unroll 1
@@ -396,10 +470,11 @@ template <typename T, typename Next, typename Epi>
 __device__ __forceinline__ void gemm_roles(GemmShared& sh, uint8_t* stages, const Next& next,
                                            Epi& epi, int* err) {
   gemm_begin<T>(sh);
-  const int warp = threadIdx.x / 32, lane = threadIdx.x & 31;
+  tc::grid_dependency_wait();  // set up under the previous kernel's end
+  const int warp = uniform((int)threadIdx.x / 32);
   bool ok = true;
   if (warp == 0) {
-    if (lane == 0) ok = gemm_copy<T>(sh, stages, next, err);
+    ok = gemm_copy<T>(sh, stages, next, err);
   } else if (warp == 1) {
     if (T::GROUP == 1 || cluster_rank() == 0) ok = gemm_multiply<T>(sh, stages, next, err);
   } else if (warp >= 4) {

@@ -57,27 +57,57 @@ __device__ __forceinline__ uint32_t take_plane(float& a, float& b) {
 // Rows as bf16 planes [NP][R][ld]: fp32 values split into three, rows padded to
 // a multiple of 8 elements so that TMA can step over them.  Rows that `targets`
 // marks as ignored become zero.
+struct StageJob {
+  const void* src[2];
+  __nv_bfloat16* dst[2];
+  long long rows[2];
+  int D, ld;
+  const void* targets;  // of the first source's rows, or null
+  int i64;
+  long long ignore;
+  int* header;          // cleared: the call's first kernel
+  unsigned* rep;
+};
 template <typename T, int NP>
-__global__ void __launch_bounds__(256) k_stage(const T* src, long long R, int D, int ld,
-                                               const void* targets, int i64, long long ignore,
-                                               __nv_bfloat16* dst) {
-  const int per = ld / 8;
-  const long long total = R * per, plane = R * ld;
+__global__ void __launch_bounds__(256) k_stage(StageJob j) {
+  tc::grid_dependency_wait();  // (of nothing) lets the next kernel set up meanwhile
+  if (blockIdx.x == 0 && threadIdx.x < 8) j.header[threadIdx.x] = 0;
+  __syncthreads();
+  if (blockIdx.x == 0 && threadIdx.x == 0) tc::set_report(j.header, j.rep);
+  const int per = j.ld / 8;
+  const long long n0 = j.rows[0] * per, total = n0 + j.rows[1] * per;
   for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < total;
        i += (long long)gridDim.x * 256) {
-    const long long r = i / per;
-    const int c = (int)(i - r * per) * 8;
-    const bool live = !targets || load_target(targets, i64, r) != ignore;
+    const int which = i >= n0;
+    const long long k = which ? i - n0 : i, r = k / per;
+    const int c = (int)(k - r * per) * 8;
+    const bool live = which || !j.targets || load_target(j.targets, j.i64, r) != j.ignore;
+    const T* src = static_cast<const T*>(j.src[which]) + (size_t)r * j.D + c;
     float v[8];
+    if (live && c + 8 <= j.D && (j.D * sizeof(T)) % 16 == 0) {
+      constexpr int W = 16 / sizeof(T);
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
-      v[j] = live && c + j < D ? Io<T>::load(src, (size_t)r * D + c + j) : 0.0f;
+      for (int q = 0; q < 8; q += W) {
+        union {
+          uint4 u;
+          T e[W];
+        } x;
+        x.u = *reinterpret_cast<const uint4*>(src + q);
+#pragma unroll
+        for (int e = 0; e < W; ++e) v[q + e] = Io<T>::load(x.e, e);
+      }
+    } else {
+#pragma unroll
+      for (int q = 0; q < 8; ++q) v[q] = live && c + q < j.D ? Io<T>::load(src, q) : 0.0f;
+    }
+    __nv_bfloat16* dst = j.dst[which] + r * j.ld + c;
+    const long long plane = j.rows[which] * j.ld;
 #pragma unroll
     for (int p = 0; p < NP; ++p) {
       uint32_t u[4];
 #pragma unroll
       for (int q = 0; q < 4; ++q) u[q] = take_plane<NP>(v[2 * q], v[2 * q + 1]);
-      *reinterpret_cast<uint4*>(dst + p * plane + r * ld + c) = make_uint4(u[0], u[1], u[2], u[3]);
+      *reinterpret_cast<uint4*>(dst + p * plane) = make_uint4(u[0], u[1], u[2], u[3]);
     }
   }
 }
@@ -86,16 +116,8 @@ __global__ void __launch_bounds__(256) k_stage(const T* src, long long R, int D,
 // A worker (a block, or a pair) takes a contiguous run of the tiles, columns
 // fastest, so that it stays with the same rows as long as it can.
 struct RunNext {
-  const Product* p;
-  long long t, end;
-  __device__ bool operator()(const Product*& q, int& m, int& n) {
-    if (t >= end) return false;
-    q = p;
-    m = (int)(t / p->tn);
-    n = (int)(t % p->tn);
-    ++t;
-    return true;
-  }
+  TileRange r;
+  __device__ __forceinline__ bool operator()(Work& w) { return r.next(w); }
 };
 __host__ __device__ inline long long run_begin(long long worker, long long tiles, long long workers) {
   return worker * tiles / workers;
@@ -116,6 +138,7 @@ struct StatJob {
   float* zt;       // [N] target logits
   int* err;
   unsigned* rep;
+  int first;       // the call's first kernel: clears its header
 };
 
 // A row's logits but the target's, over a worker's run, as (base, sum): sum =
@@ -131,16 +154,16 @@ struct StatEpi {
   int row = 0, col = 0, target = -1, slot_row = 0;
   __device__ StatEpi(const StatJob& job, long long w, long long ws)
       : j(job), worker(w), workers(ws) {}
-  __device__ void begin(const Product& p, int m, int n, int r, int c) {
-    if (m != m_now) {
+  __device__ void begin(const Work& w, int r, int c) {
+    if (w.m != m_now) {
       flush();
-      m_now = m;
+      m_now = w.m;
       base = -INFINITY;
       sum = 0.0f;
       row = r;
-      slot_row = r - m * kTM * CG;
+      slot_row = r - w.m * kTM * CG;
       target = -1;
-      if (r < p.M) {
+      if (r < w.p->M) {
         const long long t = load_target(j.targets, j.i64, r);
         if (t != j.ignore && t >= 0 && t < j.V) target = (int)t;
       }
@@ -211,12 +234,12 @@ struct SoftEpi {
   bool in = false, live = false;
   __device__ explicit SoftEpi(const SoftJob& job) : j(job) {}
   int m_now = -1;
-  __device__ void begin(const Product& p, int m, int n, int r, int c) {
+  __device__ void begin(const Work& w, int r, int c) {
     col = c;
-    if (m == m_now) return;  // the same rows as the last tile's
-    m_now = m;
+    if (w.m == m_now) return;  // the same rows as the last tile's
+    m_now = w.m;
     row = r;
-    in = r < p.M;
+    in = r < w.p->M;
     live = false;
     target = -1;
     coef = 0.0f;
@@ -275,7 +298,8 @@ __device__ __forceinline__ uint8_t* stage_memory() {
 template <int CG>
 __device__ __forceinline__ RunNext run_of(const Product& p) {
   const long long tiles = (long long)p.tm * p.tn, worker = blockIdx.x / CG, workers = gridDim.x / CG;
-  return RunNext{&p, run_begin(worker, tiles, workers), run_begin(worker + 1, tiles, workers)};
+  return RunNext{
+      TileRange(&p, run_begin(worker, tiles, workers), run_begin(worker + 1, tiles, workers))};
 }
 
 // A bf16 logit over more than 512 features is summed in chains: its loss shows
@@ -287,7 +311,11 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
     k_loss_stats(const __grid_constant__ StatJob job) {
   using T = StatTile<NP, CG, JOIN>;
   __shared__ GemmShared sh;
-  if (blockIdx.x == 0 && threadIdx.x == 0) tc::set_report(job.err, job.rep);
+  if (job.first) {
+    if (blockIdx.x == 0 && threadIdx.x < 8) job.err[threadIdx.x] = 0;
+    __syncthreads();
+    if (blockIdx.x == 0 && threadIdx.x == 0) tc::set_report(job.err, job.rep);
+  }
   StatEpi<NP, CG> epi(job, blockIdx.x / CG, gridDim.x / CG);
   gemm_roles<T>(sh, stage_memory<T>(), run_of<CG>(job.p), epi, job.err);
   if (threadIdx.x >= 128) epi.flush();
@@ -298,7 +326,6 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
     k_loss_softmax(const __grid_constant__ SoftJob job) {
   using T = Tile<NP, CG>;
   __shared__ GemmShared sh;
-  if (blockIdx.x == 0 && threadIdx.x == 0) tc::set_report(job.err, job.rep);
   SoftEpi<NP, CG> epi(job);
   gemm_roles<T>(sh, stage_memory<T>(), run_of<CG>(job.p), epi, job.err);
 }
@@ -323,6 +350,7 @@ struct JoinJob {
 // its log-sum; then the sums over rows, by block and, by the block that is done
 // last, over blocks in order.
 __global__ void __launch_bounds__(256) k_loss_join(JoinJob j) {
+  tc::grid_dependency_wait();
   const int lanes = 1 << j.lanes_log2, lane = threadIdx.x & (lanes - 1);
   const long long row = (long long)blockIdx.x * (256 >> j.lanes_log2) + (threadIdx.x >> j.lanes_log2);
   const bool in = row < j.N;
@@ -409,27 +437,15 @@ struct Deal {
   unsigned lo[2][kMaxWorkers + 1];
 };
 struct DealNext {
-  const Product* p[2];
-  unsigned t, end0, t1, end1;
-  int which;
-  __device__ bool operator()(const Product*& q, int& m, int& n) {
-    if (which == 0 && t >= end0) {
-      which = 1;
-      t = t1;
-    }
-    if (which == 1 && t >= end1) return false;
-    q = which ? p[1] : p[0];
-    m = (int)(t / q->tn);
-    n = (int)(t % q->tn);
-    ++t;
-    return true;
-  }
+  TileRange a, b;
+  __device__ __forceinline__ bool operator()(Work& w) { return a.next(w) || b.next(w); }
 };
 
 struct GradJob {
   Product p[2];            // dw of the piece's words, and dx
   Deal deal;
   void* to[2];             // their results
+  float* part[2];          // with splits: [splits][M][acc_ld] partial sums
   float* acc;              // [N][acc_ld] running sum of dx over pieces
   int acc_ld;
   int wide;                // the results' rows are whole 32-byte sectors
@@ -442,6 +458,12 @@ struct GradJob {
   unsigned* rep;
 };
 
+__device__ __forceinline__ float grad_scale(const GradJob& j) {
+  float s = j.scale ? *j.scale : 1.0f;
+  if (j.count) s = *j.count == 0.0f ? 0.0f : s / *j.count;
+  return s;
+}
+
 template <int NP, int CG>
 struct GradEpi {
   using T = typename std::conditional<NP == 1, __nv_bfloat16, float>::type;
@@ -449,24 +471,32 @@ struct GradEpi {
   const Product* p = nullptr;
   int row = 0, col = 0, which = 0;
   bool in = false, live = true;
-  float scale = 1.0f;
-  __device__ explicit GradEpi(const GradJob& job) : j(job) {
-    if (j.scale) scale = *j.scale;
-    if (j.count) scale = *j.count == 0.0f ? 0.0f : scale / *j.count;
-  }
-  __device__ void begin(const Product& q, int m, int n, int r, int c) {
-    p = &q;
+  float scale;
+  float* part = nullptr;
+  __device__ explicit GradEpi(const GradJob& job) : j(job), scale(grad_scale(job)) {}
+  __device__ void begin(const Work& w, int r, int c) {
+    p = w.p;
     row = r;
     col = c;
-    in = r < q.M;
+    in = r < p->M;
     which = p == &j.p[1];
     live = true;
+    part = p->splits > 1 ? j.part[which] + ((size_t)w.split * p->M + r) * j.acc_ld + c : nullptr;
     if (in && which == 1 && j.last) live = load_target(j.targets, j.i64, r) != j.ignore;
   }
   __device__ __forceinline__ void chunk(int c, float* f) {
     if (!in) return;
     const int D = p->N, left = D - (col + c);
     uint32_t u[8];
+    if (part) {
+#pragma unroll
+      for (int i = 0; i < 32; i += 8) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) u[e] = __float_as_uint(f[i + e]);
+        store32(part + c + i, u);
+      }
+      return;
+    }
     if (which == 1) {  // the pieces' sum of dx; its rows are padded to whole chunks
       float* acc = j.acc + (size_t)row * j.acc_ld + col + c;
       if (!j.first) {
@@ -514,10 +544,53 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
   using T = Tile<NP, CG>;
   __shared__ GemmShared sh;
   const int w = blockIdx.x / CG;
-  const DealNext next{{&job.p[0], &job.p[1]}, job.deal.lo[0][w],     job.deal.lo[0][w + 1],
-                      job.deal.lo[1][w],      job.deal.lo[1][w + 1], 0};
+  const DealNext next{TileRange(&job.p[0], job.deal.lo[0][w], job.deal.lo[0][w + 1]),
+                      TileRange(&job.p[1], job.deal.lo[1][w], job.deal.lo[1][w + 1])};
   GradEpi<NP, CG> epi(job);
   gemm_roles<T>(sh, stage_memory<T>(), next, epi, job.err);
+}
+
+// The split products' partial sums, added in order: four columns a thread.
+template <typename T>
+__global__ void __launch_bounds__(256) k_loss_parts(const __grid_constant__ GradJob j) {
+  tc::grid_dependency_wait();
+  const float scale = grad_scale(j);
+  const int D = j.p[0].N, per = (D + 3) / 4;
+  const long long n0 = j.p[0].splits > 1 ? (long long)j.p[0].M * per : 0;
+  const long long n1 = j.p[1].splits > 1 ? (long long)j.p[1].M * per : 0;
+  for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < n0 + n1;
+       i += (long long)gridDim.x * 256) {
+    const int which = i >= n0;
+    const long long k = which ? i - n0 : i, row = k / per;
+    const int c = (int)(k - row * per) * 4;
+    const Product& p = j.p[which];
+    const float* part = j.part[which] + row * j.acc_ld + c;
+    const size_t step = (size_t)p.M * j.acc_ld;
+    float f[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    auto add = [&](const float* q) {
+      const float4 x = *reinterpret_cast<const float4*>(q);
+      f[0] += x.x;
+      f[1] += x.y;
+      f[2] += x.z;
+      f[3] += x.w;
+    };
+#pragma unroll 4
+    for (int s = 0; s < p.splits; ++s) add(part + s * step);
+    bool live = true;
+    if (which) {
+      float* acc = j.acc + row * j.acc_ld + c;
+      if (!j.first) add(acc);
+      if (!j.last) {
+        *reinterpret_cast<float4*>(acc) = make_float4(f[0], f[1], f[2], f[3]);
+        continue;
+      }
+      live = load_target(j.targets, j.i64, row) != j.ignore;
+    }
+    T* out = static_cast<T*>(j.to[which]) + row * D + c;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (c + e < D) Io<T>::store(out, e, live ? f[e] * scale : 0.0f);
+  }
 }
 
 // ------------------------------------------------------------------ host
@@ -568,13 +641,27 @@ int stat_slots(long long tm, long long tn, long long w) {
   return (int)s * 4;
 }
 
+// A long reduction over few tiles is split, where it would otherwise take more
+// than one and a half times the even share of all workers, into parts of about
+// that share.  100 rows of 1024 against 50000 words: dx is four tiles of 782
+// stages beside 784 tiles of two, and unsplit took all of the launch's 221 us.
+void split_long(const long long tiles[2], const long long kb[2], int np, int w, int splits[2]) {
+  const long long total = tiles[0] * kb[0] + tiles[1] * kb[1];
+  const long long least = np == 1 ? 16 : 4;  // stages worth a tile of their own
+  const long long even = (total + w - 1) / w, share = even > least ? even : least;
+  for (int i = 0; i < 2; ++i) {
+    splits[i] = 1;
+    if (2 * kb[i] >= 3 * share) splits[i] = (int)((kb[i] + share - 1) / share);
+  }
+}
+
 struct Ws {
   int* header;        // error word, report address; [4]: the join's counter
   __nv_bfloat16 *x, *w;
   float2* part;
   float *zt, *block_sum;
   __nv_bfloat16* g;
-  float* acc;
+  float *acc, *split_sum[2];
 };
 constexpr size_t kHeaderInts = 32;
 
@@ -583,6 +670,14 @@ int round_piece(int piece, int V) {
   return (int)p;
 }
 int acc_ld(int D) { return (D + 31) / 32 * 32; }
+
+// Splits of dw and dx for a piece of n words.
+void grad_splits(const Sizes& z, long long n, int w, int splits[2]) {
+  const long long tn = cdiv(z.D, kTN);
+  const long long tiles[2] = {cdiv(n, kTM * CGv) * tn, cdiv(z.N, kTM * CGv) * tn};
+  const long long kb[2] = {cdiv(z.N, kTK), cdiv(n, kTK)};
+  split_long(tiles, kb, z.np(), w, splits);
+}
 
 Ws carve(Carver& cv, const Sizes& z, int piece, bool bwd) {
   Ws w{};
@@ -600,6 +695,18 @@ Ws carve(Carver& cv, const Sizes& z, int piece, bool bwd) {
     const int p = round_piece(piece, z.V);
     w.g = cv.take<__nv_bfloat16>((size_t)np * z.N * p);
     if (p < z.V) w.acc = cv.take<float>((size_t)z.N * acc_ld(z.D));
+    // the largest piece, and the last one if it is shorter
+    size_t need[2] = {0, 0};
+    const int last = z.V - (z.V - 1) / p * p;
+    for (int n : {z.V < p ? z.V : p, last}) {
+      int splits[2];
+      grad_splits(z, n, workers(CGv), splits);
+      for (int i = 0; i < 2; ++i) {
+        const size_t k = splits[i] > 1 ? (size_t)splits[i] * (i ? z.N : n) * acc_ld(z.D) : 0;
+        if (k > need[i]) need[i] = k;
+      }
+    }
+    for (int i = 0; i < 2; ++i) w.split_sum[i] = cv.take<float>(need[i]);
   }
   return w;
 }
@@ -676,24 +783,52 @@ bool make_product(Product* p, const Planes& a, bool a_mn, const Planes& b, bool 
   p->tm = cdiv(M, kTM * CG);
   p->tn = cdiv(N, kTN);
   p->kb = cdiv(K, kTK);
+  p->splits = 1;
   return true;
 }
 
 template <int NP>
-slim_status stage(const void* src, long long R, int D, int ld, const void* targets, slim_index it,
-                  long long ignore, __nv_bfloat16* dst, cudaStream_t s) {
+slim_status stage(StageJob j, cudaStream_t s) {
   using T = typename std::conditional<NP == 1, __nv_bfloat16, float>::type;
-  const long long n = R * (ld / 8);
-  const unsigned blocks = (unsigned)(cdiv(n, 256) < 152 * 16 ? cdiv(n, 256) : 152 * 16);
-  prof::Scope ps(prof::K_LOSS_PREP, s);
-  k_stage<T, NP><<<blocks, 256, 0, s>>>((const T*)src, R, D, ld, targets, it == SLIM_I64, ignore,
-                                        dst);
+  const long long n = (j.rows[0] + j.rows[1]) * (j.ld / 8);
+  const unsigned blocks = (unsigned)(cdiv(n, 256) < 152 * 8 ? cdiv(n, 256) : 152 * 8);
+  prof::Scope ps(prof::K_LOSS_PREP, s, 0.0, (double)n * 8 * (sizeof(T) + 2 * NP));
+  k_stage<T, NP><<<blocks, 256, 0, s>>>(j);
   return cudaGetLastError() == cudaSuccess ? SLIM_OK : SLIM_ERR_CUDA;
+}
+
+// Launches a kernel on the call's stream; `after`: as a dependent of the call's
+// previous kernel, which it waits for itself.
+template <typename Job>
+bool launch_on(void (*k)(Job), unsigned blocks, int threads, size_t smem, int cluster, bool after,
+               cudaStream_t s, const Job& job) {
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(blocks);
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cudaLaunchAttribute at[2];
+  unsigned n = 0;
+  if (cluster > 1) {
+    at[n].id = cudaLaunchAttributeClusterDimension;
+    at[n].val.clusterDim.x = cluster;
+    at[n].val.clusterDim.y = at[n].val.clusterDim.z = 1;
+    ++n;
+  }
+  if (after) {
+    at[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[n].val.programmaticStreamSerializationAllowed = 1;
+    ++n;
+  }
+  cfg.attrs = at;
+  cfg.numAttrs = n;
+  return cudaLaunchKernelEx(&cfg, k, job) == cudaSuccess;
 }
 
 // Launches a kernel of the tile products on `blocks` blocks, in pairs for CG = 2.
 template <typename T, typename Job>
-bool launch(void (*k)(Job), unsigned blocks, cudaStream_t s, const Job& job, bool* ready) {
+bool launch(void (*k)(Job), unsigned blocks, bool after, cudaStream_t s, const Job& job,
+            bool* ready) {
   constexpr size_t smem = T::smem();
   constexpr int CG = T::GROUP;
   if (ready == nullptr || !*ready) {
@@ -702,18 +837,7 @@ bool launch(void (*k)(Job), unsigned blocks, cudaStream_t s, const Job& job, boo
       return false;
     if (ready) *ready = true;
   }
-  cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3(blocks);
-  cfg.blockDim = dim3(kGemmThreads);
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = s;
-  cudaLaunchAttribute at[1];
-  at[0].id = cudaLaunchAttributeClusterDimension;
-  at[0].val.clusterDim.x = CG;
-  at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
-  cfg.attrs = at;
-  cfg.numAttrs = CG > 1 ? 1 : 0;
-  return cudaLaunchKernelEx(&cfg, k, job) == cudaSuccess;
+  return launch_on(k, blocks, kGemmThreads, smem, CG, after, s, job);
 }
 
 template <typename T>
@@ -733,11 +857,12 @@ slim_status fwd(const Sizes& z, const void* x, const void* w, const void* target
   if (!make_product<NP, CG>(&j.p, Planes{xp, z.N, z.D, ld, z.N * ld}, false,
                             Planes{wp, z.V, z.D, ld, (long long)z.V * ld}, false, z.N, z.V, z.D))
     return SLIM_ERR_CUDA;
-  if (cudaMemsetAsync(ws.header, 0, kHeaderInts * sizeof(int), s) != cudaSuccess)
-    return SLIM_ERR_CUDA;
-  slim_status st;
-  if (ws.x && (st = stage<NP>(x, z.N, z.D, ld, nullptr, it, 0, ws.x, s)) != SLIM_OK) return st;
-  if (ws.w && (st = stage<NP>(w, z.V, z.D, ld, nullptr, it, 0, ws.w, s)) != SLIM_OK) return st;
+  if (ws.w) {
+    const slim_status st = stage<NP>(
+        StageJob{{x, w}, {ws.x, ws.w}, {z.N, z.V}, z.D, ld, nullptr, 0, 0, ws.header, rep}, s);
+    if (st != SLIM_OK) return st;
+  }
+  j.first = ws.w == nullptr;
   const long long tiles = (long long)j.p.tm * j.p.tn;
   const long long wk = tiles < workers(CG) ? tiles : workers(CG);
   j.targets = targets;
@@ -754,9 +879,9 @@ slim_status fwd(const Sizes& z, const void* x, const void* w, const void* target
     const unsigned blocks = (unsigned)wk * CG;
     const bool ok =
         NP > 1 || j.p.kb > StatTile<NP, CG, true>::CHAIN
-            ? launch<StatTile<NP, CG, true>>(k_loss_stats<NP, CG, true>, blocks, s, j,
+            ? launch<StatTile<NP, CG, true>>(k_loss_stats<NP, CG, true>, blocks, !j.first, s, j,
                                              once<StatTile<NP, CG, true>>())
-            : launch<StatTile<NP, CG, NP != 1>>(k_loss_stats<NP, CG, NP != 1>, blocks, s, j,
+            : launch<StatTile<NP, CG, NP != 1>>(k_loss_stats<NP, CG, NP != 1>, blocks, !j.first, s, j,
                                                 once<StatTile<NP, CG, NP != 1>>());
     if (!ok) return SLIM_ERR_CUDA;
   }
@@ -783,8 +908,9 @@ slim_status fwd(const Sizes& z, const void* x, const void* w, const void* target
   q.done = reinterpret_cast<unsigned*>(ws.header + 4);
   q.total = total;
   prof::Scope ps(prof::K_LOSS_JOIN, s);
-  k_loss_join<<<(unsigned)cdiv(z.N, 256 >> q.lanes_log2), 256, 0, s>>>(q);
-  return cudaGetLastError() == cudaSuccess ? SLIM_OK : SLIM_ERR_CUDA;
+  return launch_on(k_loss_join, (unsigned)cdiv(z.N, 256 >> q.lanes_log2), 256, 0, 1, true, s, q)
+             ? SLIM_OK
+             : SLIM_ERR_CUDA;
 }
 
 template <int NP, int CG>
@@ -796,11 +922,11 @@ slim_status bwd(const Sizes& z, const void* x, const void* w, const void* target
   const int ld = z.ld(), ps = round_piece(piece, z.V);
   const int pieces = cdiv(z.V, ps);
   const __nv_bfloat16* wp = ws.w ? ws.w : static_cast<const __nv_bfloat16*>(w);
-  if (cudaMemsetAsync(ws.header, 0, kHeaderInts * sizeof(int), s) != cudaSuccess)
-    return SLIM_ERR_CUDA;
-  slim_status st = stage<NP>(x, z.N, z.D, ld, targets, it, ignore, ws.x, s);
+  const slim_status st =
+      stage<NP>(StageJob{{x, w}, {ws.x, ws.w}, {z.N, ws.w ? z.V : 0}, z.D, ld, targets,
+                         it == SLIM_I64, ignore, ws.header, rep},
+                s);
   if (st != SLIM_OK) return st;
-  if (ws.w && (st = stage<NP>(w, z.V, z.D, ld, nullptr, it, 0, ws.w, s)) != SLIM_OK) return st;
   const Planes xm{ws.x, z.N, z.D, ld, z.N * ld};
   for (int i = 0; i < pieces; ++i) {
     const int v0 = i * ps, n = z.V - v0 < ps ? z.V - v0 : ps;
@@ -834,7 +960,7 @@ slim_status bwd(const Sizes& z, const void* x, const void* w, const void* target
     {
       const long long wk = tiles < workers(CG) ? tiles : workers(CG);
       prof::Scope sc(prof::K_LOSS_SOFTMAX, s, fl, ((double)z.N + n) * z.D * 2 * NP + gb);
-      if (!launch<Tile<NP, CG>>(k_loss_softmax<NP, CG>, (unsigned)wk * CG, s, j,
+      if (!launch<Tile<NP, CG>>(k_loss_softmax<NP, CG>, (unsigned)wk * CG, true, s, j,
                                     once<SoftEpi<NP, CG>>()))
         return SLIM_ERR_CUDA;
     }
@@ -842,14 +968,28 @@ slim_status bwd(const Sizes& z, const void* x, const void* w, const void* target
     q.acc_ld = acc_ld(z.D);
     q.first = i == 0;
     q.last = i == pieces - 1;
-    const long long nt[2] = {(long long)q.p[0].tm * q.p[0].tn, (long long)q.p[1].tm * q.p[1].tn};
-    const long long cost[2] = {q.p[0].kb, q.p[1].kb};
+    int splits[2];
+    grad_splits(z, n, workers(CG), splits);
+    long long nt[2], cost[2];
+    for (int k = 0; k < 2; ++k) {
+      q.p[k].splits = splits[k];
+      q.part[k] = ws.split_sum[k];
+      nt[k] = (long long)q.p[k].tm * q.p[k].tn * splits[k];
+      cost[k] = cdiv(q.p[k].kb, splits[k]);
+    }
     const int wk = (int)(nt[0] + nt[1] < workers(CG) ? nt[0] + nt[1] : workers(CG));
     deal_tiles(nt, cost, wk, &q.deal);
     prof::Scope sc(prof::K_LOSS_GRAD, s, 2 * fl, ((double)z.N + n) * z.D * 2 * NP + 2 * gb);
-    if (!launch<Tile<NP, CG>>(k_loss_grad<NP, CG>, (unsigned)wk * CG, s, q,
-                                 once<GradEpi<NP, CG>>()))
+    if (!launch<Tile<NP, CG>>(k_loss_grad<NP, CG>, (unsigned)wk * CG, true, s, q,
+                              once<GradEpi<NP, CG>>()))
       return SLIM_ERR_CUDA;
+    if (splits[0] > 1 || splits[1] > 1) {
+      const long long e = ((splits[0] > 1 ? n : 0) + (splits[1] > 1 ? z.N : 0)) * cdiv(z.D, 4);
+      prof::Scope sp(prof::K_LOSS_PARTS, s);
+      if (!launch_on(k_loss_parts<T>, (unsigned)(cdiv(e, 256) < 152 * 8 ? cdiv(e, 256) : 152 * 8),
+                     256, 0, 1, true, s, q))
+        return SLIM_ERR_CUDA;
+    }
   }
   return SLIM_OK;
 }

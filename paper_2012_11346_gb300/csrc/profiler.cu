@@ -18,7 +18,7 @@ const char* kNames[K_COUNT] = {
     "tc_reduce",   "tc_selftest",   "tc_prep",        "stack_rows",
     "embed_fwd",   "embed_sort",    "embed_sum",      "clip",          "loss_prep",
     "loss_stats",  "loss_join",     "loss_softmax",   "loss_grad",
-    "loss_rows"};
+    "loss_rows",   "loss_parts"};
 
 struct Rec {
   Kid k;

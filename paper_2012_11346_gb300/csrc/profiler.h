@@ -36,6 +36,7 @@ enum Kid {
   K_LOSS_SOFTMAX,
   K_LOSS_GRAD,
   K_LOSS_ROWS,
+  K_LOSS_PARTS,
   K_COUNT
 };
 
