@@ -17,7 +17,9 @@
 
 #include "../../include/slim_lm.h"
 #include "common.cuh"
+#include "launch.h"
 #include "profiler.h"
+#include "tc_common.cuh"
 
 namespace slim {
 namespace lm {
@@ -102,19 +104,25 @@ __global__ void __launch_bounds__(256) k_embed_fwd(const void* ids, int i64, con
 }
 
 // ------------------------------------------------------------------ sort
-// Keys are ids, with every id outside the table mapped to V, so that padding
-// sorts behind all rows.
+// Keys are ids.  The first pass reads the caller's ids and drops those outside
+// the table, so the key takes only the bits that V - 1 has; the number that
+// remains stays on the device (`count`).
 constexpr int kRadixBits = 8, kRadix = 1 << kRadixBits;
 constexpr int kSortThreads = 1024, kSortWarps = kSortThreads / 32;
+constexpr uint32_t kNoKey = 0xffffffffu;
 
 struct SortSrc {
   const void* ids;  // first pass: the caller's ids; later passes: null
   int i64, V;
   const uint32_t *key, *pos;
+  const int* count;  // of the later passes' items
+  __device__ __forceinline__ long long items(long long N) const {
+    return ids ? N : (long long)*count;
+  }
   __device__ __forceinline__ uint32_t key_at(long long i) const {
     if (!ids) return key[i];
     const long long id = load_id(ids, i64, i);
-    return id >= 0 && id < V ? (uint32_t)id : (uint32_t)V;
+    return id >= 0 && id < V ? (uint32_t)id : kNoKey;
   }
   __device__ __forceinline__ uint32_t pos_at(long long i) const {
     return ids ? (uint32_t)i : pos[i];
@@ -127,17 +135,19 @@ __device__ void count_digits(const SortSrc& s, long long a, long long e, int shi
                              uint32_t* hist) {
   for (long long i0 = a; i0 < e; i0 += kSortThreads) {
     const long long i = i0 + threadIdx.x;
-    const uint32_t d = i < e ? (s.key_at(i) >> shift) & (kRadix - 1) : kRadix;
+    const uint32_t key = i < e ? s.key_at(i) : kNoKey;
+    const uint32_t d = key == kNoKey ? kRadix : (key >> shift) & (kRadix - 1);
     const unsigned peers = __match_any_sync(0xffffffffu, d);
     if (d < kRadix && (peers & ((1u << (threadIdx.x & 31)) - 1)) == 0)
       atomicAdd(&hist[d], (uint32_t)__popc(peers));
   }
 }
 
-// Exclusive prefix sum of x[kRadix] (shared memory) in place, by all threads.
-__device__ void scan_digits(uint32_t* x, uint32_t* warp_sum) {
+// Exclusive prefix sum of x[kRadix] (shared memory) in place, by all threads;
+// returns the total to thread kRadix - 1.
+__device__ uint32_t scan_digits(uint32_t* x, uint32_t* warp_sum) {
   const int t = threadIdx.x, lane = t & 31, w = t >> 5;
-  uint32_t v = 0, inc = 0;
+  uint32_t v = 0, inc = 0, before = 0;
   if (t < kRadix) {
     v = inc = x[t];
     for (int o = 1; o < 32; o <<= 1) {
@@ -148,11 +158,11 @@ __device__ void scan_digits(uint32_t* x, uint32_t* warp_sum) {
   }
   __syncthreads();
   if (t < kRadix) {
-    uint32_t before = 0;
     for (int i = 0; i < w; ++i) before += warp_sum[i];
     x[t] = before + inc - v;
   }
   __syncthreads();
+  return before + inc;
 }
 
 // Scatters [a, e) stably by digit; base[d] is where this range's first item
@@ -163,21 +173,21 @@ __device__ void scatter_range(const SortSrc& s, long long a, long long e, int sh
   const int t = threadIdx.x, lane = t & 31, w = t >> 5;
   for (long long i0 = a; i0 < e; i0 += kSortThreads) {
     for (int x = t; x < kSortWarps * kRadix; x += kSortThreads) (&wh[0][0])[x] = 0;
-    __syncthreads();
     const long long i = i0 + t;
-    const bool on = i < e;
-    uint32_t key = 0, pos = 0, d = kRadix;
-    if (on) {
+    uint32_t key = kNoKey, pos = 0, d = kRadix;
+    if (i < e) {
       key = s.key_at(i);
       pos = s.pos_at(i);
-      d = (key >> shift) & (kRadix - 1);
+      if (key != kNoKey) d = (key >> shift) & (kRadix - 1);
     }
+    __syncthreads();
     const unsigned peers = __match_any_sync(0xffffffffu, d);
     const uint32_t rank = __popc(peers & ((1u << lane) - 1));
-    if (on && rank == 0) wh[w][d] = __popc(peers);
+    if (d < kRadix && rank == 0) wh[w][d] = __popc(peers);
     __syncthreads();
     if (t < kRadix) {  // counts of the warps -> first place of each warp's items
       uint32_t run = base[t];
+#pragma unroll 8
       for (int x = 0; x < kSortWarps; ++x) {
         const uint32_t c = wh[x][t];
         wh[x][t] = run;
@@ -186,7 +196,7 @@ __device__ void scatter_range(const SortSrc& s, long long a, long long e, int sh
       base[t] = run;
     }
     __syncthreads();
-    if (on) {
+    if (d < kRadix) {
       const uint32_t at = wh[w][d] + rank;
       key_out[at] = key;
       pos_out[at] = pos;
@@ -199,10 +209,12 @@ __global__ void __launch_bounds__(kSortThreads) k_sort_count(SortSrc s, long lon
                                                              int shift, uint32_t* cnt,
                                                              int* header) {
   __shared__ uint32_t hist[kRadix];
-  if (blockIdx.x == 0 && threadIdx.x < 4) header[threadIdx.x] = 0;
   if (threadIdx.x < kRadix) hist[threadIdx.x] = 0;
+  tc::grid_dependency_wait();
+  if (s.ids && blockIdx.x == 0 && threadIdx.x < 4) header[threadIdx.x] = 0;
   __syncthreads();
-  const long long a = (long long)blockIdx.x * tile, e = a + tile < N ? a + tile : N;
+  const long long n = s.items(N);
+  const long long a = (long long)blockIdx.x * tile, e = a + tile < n ? a + tile : n;
   count_digits(s, a, e, shift, hist);
   __syncthreads();
   if (threadIdx.x < kRadix) cnt[blockIdx.x * kRadix + threadIdx.x] = hist[threadIdx.x];
@@ -211,13 +223,15 @@ __global__ void __launch_bounds__(kSortThreads) k_sort_count(SortSrc s, long lon
 __global__ void __launch_bounds__(kSortThreads) k_sort_scatter(SortSrc s, long long N, int tile,
                                                                int shift, const uint32_t* cnt,
                                                                uint32_t* key_out,
-                                                               uint32_t* pos_out) {
+                                                               uint32_t* pos_out, int* count) {
   __shared__ uint32_t wh[kSortWarps][kRadix];
   __shared__ uint32_t base[kRadix], before[kRadix], sums[kRadix / 32];
   const int t = threadIdx.x, d = t & (kRadix - 1);
+  tc::grid_dependency_wait();
   // every tile's counts: the total of each digit, and that of the tiles before
   constexpr int kQ = kSortThreads / kRadix;
   uint32_t total = 0, prior = 0;
+#pragma unroll 8
   for (int x = t / kRadix; x < (int)gridDim.x; x += kQ) {
     const uint32_t c = cnt[x * kRadix + d];
     total += c;
@@ -236,45 +250,58 @@ __global__ void __launch_bounds__(kSortThreads) k_sort_scatter(SortSrc s, long l
     before[t] = b;
   }
   __syncthreads();
-  scan_digits(base, sums);
+  const uint32_t all = scan_digits(base, sums);
+  if (s.ids && blockIdx.x == 0 && t == kRadix - 1) *count = (int)all;
   if (t < kRadix) base[t] += before[t];
   __syncthreads();
-  const long long a = (long long)blockIdx.x * tile, e = a + tile < N ? a + tile : N;
+  const long long n = s.items(N);
+  const long long a = (long long)blockIdx.x * tile, e = a + tile < n ? a + tile : n;
   scatter_range(s, a, e, shift, wh, base, key_out, pos_out);
 }
 
 // The whole sort of a short list by one block, all passes in one launch.
 __global__ void __launch_bounds__(kSortThreads) k_sort_one(SortSrc s, long long N, int passes,
                                                            uint32_t* k0, uint32_t* p0,
-                                                           uint32_t* k1, uint32_t* p1,
+                                                           uint32_t* k1, uint32_t* p1, int* count,
                                                            int* header) {
-  if (threadIdx.x < 4) header[threadIdx.x] = 0;
   __shared__ uint32_t wh[kSortWarps][kRadix];
   __shared__ uint32_t base[kRadix], sums[kRadix / 32];
+  __shared__ uint32_t left;
+  tc::grid_dependency_wait();  // (of nothing) lets the next kernel set up meanwhile
+  if (threadIdx.x < 4) header[threadIdx.x] = 0;
   for (int p = 0; p < passes; ++p) {
     if (threadIdx.x < kRadix) base[threadIdx.x] = 0;
     __syncthreads();
-    count_digits(s, 0, N, p * kRadixBits, base);
+    const long long n = p == 0 ? N : left;
+    count_digits(s, 0, n, p * kRadixBits, base);
     __syncthreads();
-    scan_digits(base, sums);
+    const uint32_t all = scan_digits(base, sums);
+    if (threadIdx.x == kRadix - 1) {
+      left = all;
+      *count = (int)all;
+    }
     uint32_t *ko = p & 1 ? k1 : k0, *po = p & 1 ? p1 : p0;
-    scatter_range(s, 0, N, p * kRadixBits, wh, base, ko, po);
+    scatter_range(s, 0, n, p * kRadixBits, wh, base, ko, po);
     s.ids = nullptr;
     s.key = ko;
     s.pos = po;
+    __syncthreads();
   }
 }
 
 // ------------------------------------------------------------------ sums
+constexpr int kMaxChunk = 64;
 struct SumJob {
   const uint32_t *key, *pos;  // sorted
-  long long N;
+  const int* count;           // of them
   int D, V, U, gl;            // U vectors a row, 2^gl threads a group
+  int colblocks;              // groups that share a chunk's columns
   int chunk;                  // sorted tokens per chunk
   long long chunks;
   float scale;
   int accumulate;
-  float* part;                // [chunks][2][D]: a run that came in, one that goes on
+  float* part;                // [chunks][2][ld]: a run that came in, one that goes on
+  long long ld;               // a multiple of 4
 };
 
 template <typename T, int VB>
@@ -291,11 +318,40 @@ __device__ __forceinline__ void finish_row(const SumJob& j, const float* acc, T*
   o.store(dst);
 }
 
+// n floats of a partial row.
+template <int n>
+__device__ __forceinline__ void part_store(float* p, const float* f) {
+  if constexpr (n % 4 == 0) {
+#pragma unroll
+    for (int i = 0; i < n; i += 4)
+      *reinterpret_cast<float4*>(p + i) = make_float4(f[i], f[i + 1], f[i + 2], f[i + 3]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < n; ++i) p[i] = f[i];
+  }
+}
+template <int n>
+__device__ __forceinline__ void part_add(const float* p, float* f) {
+  if constexpr (n % 4 == 0) {
+#pragma unroll
+    for (int i = 0; i < n; i += 4) {
+      const float4 x = *reinterpret_cast<const float4*>(p + i);
+      f[i] += x.x;
+      f[i + 1] += x.y;
+      f[i + 2] += x.z;
+      f[i + 3] += x.w;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < n; ++i) f[i] += p[i];
+  }
+}
+
 // Whether `row` is among the sorted keys.
-__device__ __forceinline__ bool has_key(const uint32_t* key, long long N, uint32_t row) {
-  long long lo = 0, hi = N;
+__device__ __forceinline__ bool has_key(const uint32_t* key, int N, uint32_t row) {
+  int lo = 0, hi = N;
   while (lo < hi) {
-    const long long mid = (lo + hi) >> 1;
+    const int mid = (int)(((unsigned)lo + (unsigned)hi) >> 1);
     if (key[mid] < row)
       lo = mid + 1;
     else
@@ -313,11 +369,15 @@ template <typename T, int VB>
 __global__ void __launch_bounds__(256) k_embed_sum(SumJob j, const T* dout, T* dtable,
                                                    unsigned sum_blocks) {
   constexpr int n = Vec<T, VB>::n;
+  // a chunk's tokens, fetched once: the rows' loads then wait for no index
+  __shared__ uint32_t sk[256], sp[256];
+  tc::grid_dependency_wait();
+  const int N = *j.count;
   if (blockIdx.x >= sum_blocks) {
     const int lane = threadIdx.x & 31;
     const long long r0 =
         ((long long)(blockIdx.x - sum_blocks) * 8 + (threadIdx.x >> 5)) * 32;
-    const bool empty = r0 + lane < j.V && !has_key(j.key, j.N, (uint32_t)(r0 + lane));
+    const bool empty = r0 + lane < j.V && !has_key(j.key, N, (uint32_t)(r0 + lane));
     unsigned rows = __ballot_sync(0xffffffffu, empty);
     Vec<T, VB> z;
 #pragma unroll
@@ -330,117 +390,127 @@ __global__ void __launch_bounds__(256) k_embed_sum(SumJob j, const T* dout, T* d
     }
     return;
   }
-  const int g = 1 << j.gl;
-  const long long groups = (long long)blockIdx.x * (256 >> j.gl) + (threadIdx.x >> j.gl);
-  const int colblocks = (j.U + g - 1) >> j.gl;
-  const long long c = groups / colblocks;
-  const int u = (int)(groups % colblocks) * g + (threadIdx.x & (g - 1));
-  if (c >= j.chunks || u >= j.U) return;
-  const long long a = c * j.chunk, e = a + j.chunk < j.N ? a + j.chunk : j.N;
-  const uint32_t V = (uint32_t)j.V;
-  const bool came = a > 0 && j.key[a - 1] == j.key[a];    // the first run started earlier
-  const bool goes = e < j.N && j.key[e - 1] == j.key[e];  // the last run goes on
+  const int g = 1 << j.gl, lane = threadIdx.x & (g - 1);
+  const long long group = (long long)blockIdx.x * (256 >> j.gl) + (threadIdx.x >> j.gl);
+  const long long c = group / j.colblocks;
+  const int u = (int)(group - c * j.colblocks) * g + lane;
+  const long long a = c * j.chunk;
+  const int len = c < j.chunks && a < N ? (int)(a + j.chunk < N ? j.chunk : N - a) : 0;
+  // (a group keeps them at its own threads' places; narrower groups than a chunk
+  // read them where they are)
+  const bool staged = g >= j.chunk;
+  if (staged && lane < len) {
+    sk[threadIdx.x] = j.key[a + lane];
+    sp[threadIdx.x] = j.pos[a + lane];
+  }
+  __syncthreads();
+  if (len == 0 || u >= j.U) return;
+  const uint32_t* key = staged ? sk + (threadIdx.x - lane) : j.key + a;
+  const uint32_t* pos = staged ? sp + (threadIdx.x - lane) : j.pos + a;
+  uint32_t cur = key[0];
+  const bool came = a > 0 && j.key[a - 1] == cur;                  // its run started earlier
+  const bool goes = a + len < N && j.key[a + len] == key[len - 1];  // the last run goes on
   float acc[n];
 #pragma unroll
   for (int x = 0; x < n; ++x) acc[x] = 0.0f;
-  uint32_t cur = j.key[a];
   bool first = true;
+  float* part = j.part + (size_t)c * 2 * j.ld + (size_t)u * n;
+  const T* rows = dout + (size_t)u * n;
   auto flush = [&](bool last) {
-    if (cur < V) {
-      float* p = nullptr;
-      if (first && came)
-        p = j.part + ((size_t)c * 2) * j.D;
-      else if (last && goes)
-        p = j.part + ((size_t)c * 2 + 1) * j.D;
-      if (p) {
-#pragma unroll
-        for (int x = 0; x < n; ++x) p[(size_t)u * n + x] = acc[x];
-      } else {
-        finish_row<T, VB>(j, acc, dtable + (size_t)cur * j.D + (size_t)u * n);
-      }
-    }
+    if (first && came)
+      part_store<n>(part, acc);
+    else if (last && goes)
+      part_store<n>(part + j.ld, acc);
+    else
+      finish_row<T, VB>(j, acc, dtable + (size_t)cur * j.D + (size_t)u * n);
     first = false;
 #pragma unroll
     for (int x = 0; x < n; ++x) acc[x] = 0.0f;
   };
-  for (long long i = a; i < e; i += kSumAhead) {
-    uint32_t k[kSumAhead];
+  for (int i = 0; i < len; i += kSumAhead) {
     Vec<T, VB> v[kSumAhead];
 #pragma unroll
-    for (int x = 0; x < kSumAhead; ++x) {
-      k[x] = i + x < e ? j.key[i + x] : V;
-      if (k[x] < V) v[x].load(dout + (size_t)j.pos[i + x] * j.D + (size_t)u * n);
-    }
+    for (int x = 0; x < kSumAhead; ++x)
+      if (i + x < len) v[x].load(rows + (size_t)pos[i + x] * j.D);
 #pragma unroll
     for (int x = 0; x < kSumAhead; ++x) {
-      if (i + x >= e) break;
-      if (k[x] != cur) {
+      if (i + x >= len) break;
+      const uint32_t k = key[i + x];
+      if (k != cur) {
         flush(false);
-        cur = k[x];
+        cur = k;
       }
-      if (cur < V) {
 #pragma unroll
-        for (int y = 0; y < n; ++y) acc[y] += v[x].get(y);
-      }
+      for (int y = 0; y < n; ++y) acc[y] += v[x].get(y);
     }
   }
   flush(true);
 }
 
 // Joins the runs that cross chunks.  A block looks at one chunk; if a run
-// starts in it and goes on, its groups of threads add the later chunks'
-// partial rows (each group a contiguous share of them, in order), and the
-// groups' sums are added in order.
-constexpr int kJoinThreads = 512;
+// starts in it and goes on, it adds the later chunks' partial rows in order.
+// Most such runs reach one chunk further, and all threads go side by side along
+// the columns.  A long run (a frequent token) is cut into 16 shares of 32 threads
+// a column block, whose sums are added in order.
+constexpr int kJoinThreads = 512, kJoinGroups = kJoinThreads / 32;
 template <typename T, int VB>
 __global__ void __launch_bounds__(kJoinThreads) k_embed_join(SumJob j, T* dtable) {
   constexpr int n = Vec<T, VB>::n;
-  __shared__ float sh[kJoinThreads * n];
+  __shared__ float sh[kJoinGroups][n][32];
+  tc::grid_dependency_wait();
+  const int N = *j.count;
   const long long c = blockIdx.x;
   const long long a = c * j.chunk, e = a + j.chunk;
-  if (e >= j.N) return;
-  const uint32_t key = j.key[e - 1];
-  if (key != j.key[e] || key >= (uint32_t)j.V) return;
+  if (e >= N) return;
+  const uint32_t key = j.key[e - 1], next = j.key[e], head = j.key[a],
+                 before = a > 0 ? j.key[a - 1] : kNoKey;
+  if (key != next) return;
   // the run came into this chunk from an earlier one, which joins it
-  if (a > 0 && j.key[a] == key && j.key[a - 1] == key) return;
-  // the run's last token, then the last chunk that holds some of it
-  long long lo = e, hi = j.N;  // key[lo] == key, key[hi] != key
-  while (hi - lo > 1) {
-    const long long mid = (lo + hi) >> 1;
-    if (j.key[mid] == key)
-      lo = mid;
-    else
-      hi = mid;
+  if (head == key && before == key) return;
+  const int lane = threadIdx.x & 31, grp = threadIdx.x >> 5;
+  // chunks c+1 .. c+more begin inside the run (and are in their slot 0)
+  int more = 0;
+  for (;;) {
+    const long long at = e + (long long)(more + (int)threadIdx.x) * j.chunk;
+    const int in = __syncthreads_count(at < N && j.key[at] == key);
+    more += in;  // a run is contiguous: the threads in it are the first ones
+    if (in < kJoinThreads) break;
   }
-  const long long more = lo / j.chunk - c;  // chunks c+1 .. c+more, in their slot 0
-  const int g = 1 << j.gl, lane = threadIdx.x & (g - 1), grp = threadIdx.x >> j.gl;
-  const int groups = kJoinThreads >> j.gl;
-  const long long share = (more + groups - 1) / groups;
-  const long long b0 = grp * share < more ? grp * share : more;
-  const long long b1 = b0 + share < more ? b0 + share : more;
-  for (int u0 = 0; u0 < j.U; u0 += g) {
+  const float* first = j.part + ((size_t)c * 2 + 1) * j.ld;
+  const float* rest = j.part + (size_t)(c + 1) * 2 * j.ld;
+  T* out = dtable + (size_t)key * j.D;
+  if (more < kJoinGroups) {
+    for (int u = threadIdx.x; u < j.U; u += kJoinThreads) {
+      float acc[n];
+#pragma unroll
+      for (int x = 0; x < n; ++x) acc[x] = 0.0f;
+      part_add<n>(first + (size_t)u * n, acc);
+      for (int b = 0; b < more; ++b) part_add<n>(rest + (size_t)b * 2 * j.ld + (size_t)u * n, acc);
+      finish_row<T, VB>(j, acc, out + (size_t)u * n);
+    }
+    return;
+  }
+  const int share = (more + kJoinGroups - 1) / kJoinGroups;
+  const int b0 = min(grp * share, more), b1 = min(b0 + share, more);
+  for (int u0 = 0; u0 < j.U; u0 += 32) {
     const int u = u0 + lane;
     const bool on = u < j.U;
     float acc[n];
 #pragma unroll
-    for (int x = 0; x < n; ++x)
-      acc[x] = on && grp == 0 ? j.part[((size_t)c * 2 + 1) * j.D + (size_t)u * n + x] : 0.0f;
+    for (int x = 0; x < n; ++x) acc[x] = 0.0f;
     if (on) {
-#pragma unroll 4
-      for (long long b = b0; b < b1; ++b) {
-        const float* p = j.part + ((size_t)(c + 1 + b) * 2) * j.D + (size_t)u * n;
-#pragma unroll
-        for (int x = 0; x < n; ++x) acc[x] += p[x];
-      }
+      if (grp == 0) part_add<n>(first + (size_t)u * n, acc);
+#pragma unroll 8
+      for (int b = b0; b < b1; ++b) part_add<n>(rest + (size_t)b * 2 * j.ld + (size_t)u * n, acc);
     }
 #pragma unroll
-    for (int x = 0; x < n; ++x) sh[x * kJoinThreads + threadIdx.x] = acc[x];
+    for (int x = 0; x < n; ++x) sh[grp][x][lane] = acc[x];
     __syncthreads();
     if (grp == 0 && on) {
-      for (int q = 1; q < groups; ++q)
+      for (int q = 1; q < kJoinGroups; ++q)
 #pragma unroll
-        for (int x = 0; x < n; ++x) acc[x] += sh[x * kJoinThreads + (q << j.gl) + lane];
-      finish_row<T, VB>(j, acc, dtable + (size_t)key * j.D + (size_t)u * n);
+        for (int x = 0; x < n; ++x) acc[x] += sh[q][x][lane];
+      finish_row<T, VB>(j, acc, out + (size_t)u * n);
     }
     __syncthreads();
   }
@@ -459,23 +529,28 @@ bool aligned(const void* p, size_t to) {
   return p != nullptr && (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0;
 }
 
-constexpr long long kOneBlock = 4096;  // longest list one block sorts alone
+// Longest list that one block sorts alone: 13 us for 1000 ids in two passes, 33
+// for 4096, which four launches sort in about 15.
+constexpr long long kOneBlock = 1024;
 
 struct Plan {
   int passes, tiles, tile;
   int chunk;
   long long chunks;
 };
-Plan plan(long long N, int V) {
+Plan plan(long long N, int D, int V, int es) {
   Plan p;
   int bits = 1;
-  while ((1LL << bits) < (long long)V + 1) ++bits;
+  while ((1LL << bits) < (long long)V) ++bits;
   p.passes = (bits + kRadixBits - 1) / kRadixBits;
   const long long want = (N + 2047) / 2048;
   p.tiles = (int)(want < kSMs ? (want > 0 ? want : 1) : kSMs);
   p.tile = (int)((N + p.tiles - 1) / p.tiles);
-  long long k = (N + 1023) / 1024;
-  p.chunk = (int)(k < 16 ? 16 : k > 64 ? 64 : k);
+  // chunks short enough for some waves of blocks, long enough that their
+  // partial rows (two each) stay small beside the rows they sum; longer for
+  // narrow rows, of which a block takes several chunks
+  long long k = N / ((long long)D * es > 1024 ? 2048 : 1024);
+  p.chunk = (int)(k < 16 ? 16 : k > kMaxChunk ? kMaxChunk : k);
   p.chunks = (N + p.chunk - 1) / p.chunk;
   return p;
 }
@@ -483,8 +558,10 @@ Plan plan(long long N, int V) {
 struct Ws {
   int* header;  // the call's error word (no kernel here waits)
   uint32_t *k0, *p0, *k1, *p1, *cnt;
+  int* count;
   float* part;
 };
+long long part_ld(int D) { return (D + 3) / 4 * 4; }
 Ws carve(Carver& cv, long long N, int D, const Plan& p) {
   Ws w;
   w.header = cv.take<int>(4);
@@ -493,7 +570,8 @@ Ws carve(Carver& cv, long long N, int D, const Plan& p) {
   w.k1 = cv.take<uint32_t>(p.passes > 1 ? N : 0);
   w.p1 = cv.take<uint32_t>(p.passes > 1 ? N : 0);
   w.cnt = cv.take<uint32_t>((size_t)p.tiles * kRadix);
-  w.part = cv.take<float>((size_t)p.chunks * 2 * D);
+  w.count = cv.take<int>(1);
+  w.part = cv.take<float>((size_t)p.chunks * 2 * part_ld(D));
   return w;
 }
 
@@ -512,26 +590,29 @@ slim_status fwd(const void* ids, slim_index itype, const void* table, long long 
 
 slim_status sort(const void* ids, slim_index itype, long long N, int V, const Plan& p, const Ws& w,
                  cudaStream_t s, const uint32_t** key, const uint32_t** pos) {
-  SortSrc src{ids, itype == SLIM_I64, V, nullptr, nullptr};
+  SortSrc src{ids, itype == SLIM_I64, V, nullptr, nullptr, w.count};
   if (N <= kOneBlock) {
     prof::Scope ps(prof::K_EMBED_SORT, s);
-    k_sort_one<<<1, kSortThreads, 0, s>>>(src, N, p.passes, w.k0, w.p0, w.k1, w.p1,
-                                       w.header);
+    k_sort_one<<<1, kSortThreads, 0, s>>>(src, N, p.passes, w.k0, w.p0, w.k1, w.p1, w.count,
+                                          w.header);
     if (!launched()) return SLIM_ERR_CUDA;
   } else {
     for (int i = 0; i < p.passes; ++i) {
+      const int shift = i * kRadixBits;
       {
         prof::Scope ps(prof::K_EMBED_SORT, s);
-        k_sort_count<<<p.tiles, kSortThreads, 0, s>>>(src, N, p.tile, i * kRadixBits, w.cnt,
-                                                     w.header);
-        if (!launched()) return SLIM_ERR_CUDA;
+        if (!launch_on<SortSrc, long long, int, int, uint32_t*, int*>(
+                k_sort_count, p.tiles, kSortThreads, 0, 1, i > 0, s, src, N, p.tile, shift, w.cnt,
+                w.header))
+          return SLIM_ERR_CUDA;
       }
       uint32_t *ko = i & 1 ? w.k1 : w.k0, *po = i & 1 ? w.p1 : w.p0;
       prof::Scope ps(prof::K_EMBED_SORT, s);
-      k_sort_scatter<<<p.tiles, kSortThreads, 0, s>>>(src, N, p.tile, i * kRadixBits, w.cnt, ko,
-                                                      po);
-      if (!launched()) return SLIM_ERR_CUDA;
-      src = SortSrc{nullptr, 0, V, ko, po};
+      if (!launch_on<SortSrc, long long, int, int, const uint32_t*, uint32_t*, uint32_t*, int*>(
+              k_sort_scatter, p.tiles, kSortThreads, 0, 1, true, s, src, N, p.tile, shift, w.cnt,
+              ko, po, w.count))
+        return SLIM_ERR_CUDA;
+      src = SortSrc{nullptr, 0, V, ko, po, w.count};
     }
   }
   *key = p.passes & 1 ? w.k0 : w.k1;
@@ -542,37 +623,40 @@ slim_status sort(const void* ids, slim_index itype, long long N, int V, const Pl
 template <typename T, int VB>
 slim_status bwd(const void* ids, slim_index itype, const void* dout, long long N, int D, int V,
                 float scale, int accumulate, void* dtable, void* ws, cudaStream_t s) {
-  const Plan p = plan(N, V);
+  const Plan p = plan(N, D, V, (int)sizeof(T));
   Carver cv(ws);
   const Ws w = carve(cv, N, D, p);
   SumJob j{};
-  const slim_status st = sort(ids, itype, N, V, p, w, s, &j.key, &j.pos);
-  if (st != SLIM_OK) return st;
-  j.N = N;
-  j.D = D;
-  j.V = V;
   j.U = D / Vec<T, VB>::n;
   j.gl = group_log2(j.U, 1);
+  j.colblocks = (j.U + (1 << j.gl) - 1) >> j.gl;
+  const long long per = 256 >> j.gl;
+  const long long sum_blocks = (p.chunks * j.colblocks + per - 1) / per;
+  const long long zero_blocks = accumulate ? 0 : ((long long)V + 255) / 256;
+  if (sum_blocks + zero_blocks >= (1LL << 31)) return SLIM_ERR_UNSUPPORTED;
+  const slim_status st = sort(ids, itype, N, V, p, w, s, &j.key, &j.pos);
+  if (st != SLIM_OK) return st;
+  j.count = w.count;
+  j.D = D;
+  j.V = V;
   j.chunk = p.chunk;
   j.chunks = p.chunks;
   j.scale = scale;
   j.accumulate = accumulate;
   j.part = w.part;
-  const long long colblocks = (j.U + (1 << j.gl) - 1) >> j.gl;
-  const long long per = 256 >> j.gl;
-  const long long sum_blocks = (p.chunks * colblocks + per - 1) / per;
-  const long long zero_blocks = accumulate ? 0 : ((long long)V + 255) / 256;
-  if (sum_blocks + zero_blocks >= (1LL << 31)) return SLIM_ERR_UNSUPPORTED;
+  j.ld = part_ld(D);
   {
     prof::Scope ps(prof::K_EMBED_SUM, s, 0.0, ((double)N + V) * D * sizeof(T));
-    k_embed_sum<T, VB><<<(unsigned)(sum_blocks + zero_blocks), 256, 0, s>>>(
-        j, (const T*)dout, (T*)dtable, (unsigned)sum_blocks);
-    if (!launched()) return SLIM_ERR_CUDA;
+    if (!launch_on<SumJob, const T*, T*, unsigned>(
+            k_embed_sum<T, VB>, (unsigned)(sum_blocks + zero_blocks), 256, 0, 1, true, s, j,
+            (const T*)dout, (T*)dtable, (unsigned)sum_blocks))
+      return SLIM_ERR_CUDA;
   }
   if (p.chunks > 1) {
-    prof::Scope ps(prof::K_EMBED_SUM, s);
-    k_embed_join<T, VB><<<(unsigned)(p.chunks - 1), kJoinThreads, 0, s>>>(j, (T*)dtable);
-    if (!launched()) return SLIM_ERR_CUDA;
+    prof::Scope ps(prof::K_EMBED_JOIN, s);
+    if (!launch_on<SumJob, T*>(k_embed_join<T, VB>, (unsigned)(p.chunks - 1), kJoinThreads, 0, 1,
+                               true, s, j, (T*)dtable))
+      return SLIM_ERR_CUDA;
   }
   return SLIM_OK;
 }
@@ -615,7 +699,7 @@ extern "C" slim_status slim_embed_bwd_workspace_size(long long N, int D, int V, 
   using namespace slim::lm;
   if (!bytes || !sizes_ok(N, D, V, dtype, SLIM_I64)) return SLIM_ERR_INVALID_ARG;
   slim::Carver cv(nullptr);
-  carve(cv, N, D, plan(N, V));
+  carve(cv, N, D, plan(N, D, V, dtype == SLIM_F32 ? 4 : 2));
   *bytes = cv.bytes();
   return SLIM_OK;
 }

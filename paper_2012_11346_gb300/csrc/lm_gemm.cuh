@@ -488,9 +488,10 @@ __device__ __forceinline__ void gemm_roles(GemmShared& sh, uint8_t* stages, cons
 // A lane holds 32 columns of its own row.  It moves them in whole 32-byte
 // sectors: a 256 x 256 tile of bf16 took 5.6 k cycles this way under the next
 // tile's MMAs (5.1 k without a store), 7.9 k with 16-byte stores, and 6.5 k
-// through shared memory and TMA, which compete with the MMAs' operands.
+// through shared memory and TMA, which compete with the MMAs' operands.  Past
+// L1, whose lines are the same memory: 6 % of the softmax kernel.
 __device__ __forceinline__ void store32(void* p, const uint32_t* u) {
-  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(u[0]),
+  asm volatile("st.global.L1::no_allocate.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(u[0]),
                "r"(u[1]), "r"(u[2]), "r"(u[3]), "r"(u[4]), "r"(u[5]), "r"(u[6]), "r"(u[7])
                : "memory");
 }

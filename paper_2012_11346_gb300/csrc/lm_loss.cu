@@ -15,6 +15,7 @@
 
 #include "../../include/slim_lm.h"
 #include "common.cuh"
+#include "launch.h"
 #include "lm_gemm.cuh"
 #include "lm_loss_dev.cuh"
 #include "lm_loss_rows.h"
@@ -795,34 +796,6 @@ slim_status stage(StageJob j, cudaStream_t s) {
   prof::Scope ps(prof::K_LOSS_PREP, s, 0.0, (double)n * 8 * (sizeof(T) + 2 * NP));
   k_stage<T, NP><<<blocks, 256, 0, s>>>(j);
   return cudaGetLastError() == cudaSuccess ? SLIM_OK : SLIM_ERR_CUDA;
-}
-
-// Launches a kernel on the call's stream; `after`: as a dependent of the call's
-// previous kernel, which it waits for itself.
-template <typename Job>
-bool launch_on(void (*k)(Job), unsigned blocks, int threads, size_t smem, int cluster, bool after,
-               cudaStream_t s, const Job& job) {
-  cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3(blocks);
-  cfg.blockDim = dim3(threads);
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = s;
-  cudaLaunchAttribute at[2];
-  unsigned n = 0;
-  if (cluster > 1) {
-    at[n].id = cudaLaunchAttributeClusterDimension;
-    at[n].val.clusterDim.x = cluster;
-    at[n].val.clusterDim.y = at[n].val.clusterDim.z = 1;
-    ++n;
-  }
-  if (after) {
-    at[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at[n].val.programmaticStreamSerializationAllowed = 1;
-    ++n;
-  }
-  cfg.attrs = at;
-  cfg.numAttrs = n;
-  return cudaLaunchKernelEx(&cfg, k, job) == cudaSuccess;
 }
 
 // Launches a kernel of the tile products on `blocks` blocks, in pairs for CG = 2.

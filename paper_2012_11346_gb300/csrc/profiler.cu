@@ -16,7 +16,7 @@ const char* kNames[K_COUNT] = {
     "simt_vjp",    "simt_store",    "simt_reduce",    "simt_state",    "tc_fwd",
     "tc_bwd",      "tc_delta",      "tc_scan",        "tc_bwd_q",      "tc_bwd_kv",
     "tc_reduce",   "tc_selftest",   "tc_prep",        "stack_rows",
-    "embed_fwd",   "embed_sort",    "embed_sum",      "clip",          "loss_prep",
+    "embed_fwd",   "embed_sort",    "embed_sum",  "embed_join",    "clip",          "loss_prep",
     "loss_stats",  "loss_join",     "loss_softmax",   "loss_grad",
     "loss_rows",   "loss_parts"};
 

@@ -29,6 +29,7 @@ enum Kid {
   K_EMBED_FWD,
   K_EMBED_SORT,
   K_EMBED_SUM,
+  K_EMBED_JOIN,
   K_CLIP,
   K_LOSS_PREP,
   K_LOSS_STATS,
