@@ -41,8 +41,9 @@ struct Tile {
   static constexpr int STAGE = A_BYTES + B_BYTES;  // one plane of either operand
   static constexpr int FIT = kSmemBytes / STAGE;
   static constexpr int STAGES = FIT < 8 ? FIT : 8;
-  // chains of 512 of the reduction, or of 128 with three planes (48 steps)
-  static constexpr int CHAIN = NP == 1 ? 8 : 2;
+  // chains of 512 of the reduction, or of 64 with three planes: there only the
+  // last four steps, the large planes', work on a large sum
+  static constexpr int CHAIN = NP == 1 ? 8 : 1;
   static constexpr size_t smem() { return 1024 + (size_t)STAGES * STAGE; }
   static_assert(STAGES >= 3, "a stage per plane");
 };
@@ -67,9 +68,9 @@ struct Work {
 struct TileRange {
   const Product* p;
   int m, n, split;
-  long long left;
+  int left;
   __device__ __forceinline__ TileRange(const Product* q, long long begin, long long end)
-      : p(q), left(end - begin) {
+      : p(q), left((int)(end - begin)) {
     const long long tile = begin / q->splits;
     split = (int)(begin - tile * q->splits);
     m = (int)(tile / q->tn);
@@ -368,35 +369,28 @@ __device__ bool gemm_multiply(GemmShared& sh, uint8_t* stages, Next next, int* e
       auto done = [&](uint32_t i) { gemm_commit<CG>(empty0 + 8 * i); };
       const int k1 = min(k0 + step, last);
       for (int k = k0; k < k1; ++k) {
-        const uint32_t s0 = st;
-        if (!wait(full0 + 8 * s0, phase)) return false;
-        step_on(st, phase);
-        if (T::PLANES == 1) {
-          if (elect_one()) {
-            product(s0, s0);
-            done(s0);
-          }
-        } else {
-          if (elect_one()) product(s0, s0);
-          const uint32_t s1 = st;
-          if (!wait(full0 + 8 * s1, phase)) return false;
+        uint32_t s[3];
+#pragma unroll
+        for (int q = 0; q < T::PLANES; ++q) {
+          s[q] = st;
+          if (!wait(full0 + 8 * st, phase)) return false;
           step_on(st, phase);
-          more = 1;
-          if (elect_one()) {
-            product(s0, s1);
-            product(s1, s0);
-            product(s1, s1);
-            done(s1);
+        }
+        if (elect_one()) {
+          if (T::PLANES > 1) {
+            // smallest products first: what each step cuts off is in
+            // proportion to the sum so far
+            product(s[0], s[2]);
+            more = 1;
+            product(s[2], s[0]);
+            done(s[2]);
+            product(s[1], s[1]);
+            product(s[0], s[1]);
+            product(s[1], s[0]);
+            done(s[1]);
           }
-          const uint32_t s2 = st;
-          if (!wait(full0 + 8 * s2, phase)) return false;
-          step_on(st, phase);
-          if (elect_one()) {
-            product(s0, s2);
-            product(s2, s0);
-            done(s2);
-            done(s0);
-          }
+          product(s[0], s[0]);
+          done(s[0]);
         }
         more = 1;
         __syncwarp();
@@ -426,6 +420,10 @@ __device__ bool gemm_finish(GemmShared& sh, Next next, Epi& epi, int* err) {
     const int col = w.n * kTN + part * kEpiCols;
     const int step = T::ACC ? T::CHAIN : w.k1 - w.k0;
     float sum[T::ACC ? kEpiCols : 1];
+    if (T::ACC) {
+#pragma unroll
+      for (int c = 0; c < kEpiCols; ++c) sum[c] = 0.0f;
+    }
     epi.begin(w, row, col);
     for (int k0 = w.k0; k0 < w.k1; k0 += step, ++acc) {
       const int buf = acc & 1;
@@ -440,7 +438,7 @@ __device__ bool gemm_finish(GemmShared& sh, Next next, Epi& epi, int* err) {
           float v[16];
           tc::tmem_ld16(t + c, v);
 #pragma unroll
-          for (int i = 0; i < 16; ++i) sum[c + i] = k0 == w.k0 ? v[i] : sum[c + i] + v[i];
+          for (int i = 0; i < 16; ++i) sum[c + i] += v[i];
         }
       } else {
 #pragma unroll 1
@@ -473,11 +471,17 @@ __device__ __forceinline__ void gemm_roles(GemmShared& sh, uint8_t* stages, cons
   tc::grid_dependency_wait();  // set up under the previous kernel's end
   const int warp = uniform((int)threadIdx.x / 32);
   bool ok = true;
-  if (warp == 0) {
-    ok = gemm_copy<T>(sh, stages, next, err);
-  } else if (warp == 1) {
-    if (T::GROUP == 1 || cluster_rank() == 0) ok = gemm_multiply<T>(sh, stages, next, err);
-  } else if (warp >= 4) {
+  // With ACC the epilogue holds 64 sums a thread: the first warpgroup hands its
+  // registers over.  A block starts with 640 x 96 = 61440; 128 x 32 + 512 x 112 are
+  // as many after the split.
+  if (warp < 4) {
+    if (T::ACC) asm volatile("setmaxnreg.dec.sync.aligned.u32 32;");
+    if (warp == 0)
+      ok = gemm_copy<T>(sh, stages, next, err);
+    else if (warp == 1 && (T::GROUP == 1 || cluster_rank() == 0))
+      ok = gemm_multiply<T>(sh, stages, next, err);
+  } else {
+    if (T::ACC) asm volatile("setmaxnreg.inc.sync.aligned.u32 112;");
     ok = gemm_finish<T>(sh, next, epi, err);
   }
   __syncwarp();

@@ -979,7 +979,7 @@ extern "C" slim_status slim_vocab_loss_workspace_size(long long N, int D, int V,
                                                       int piece, int backward, size_t* bytes) {
   using namespace slim::lm;
   if (!bytes || !sizes_ok(N, D, V, dtype) || (backward && piece < 1)) return SLIM_ERR_INVALID_ARG;
-  if (rows_fit(N, D)) {
+  if (rows_fit(N, D, dtype)) {
     *bytes = rows_workspace((int)N, D, V, backward != 0);
     return SLIM_OK;
   }
@@ -1008,7 +1008,7 @@ extern "C" slim_status slim_vocab_loss_fwd(const void* x, const void* w, const v
   slim_vocab_loss_workspace_size(N, D, V, dtype, 1, 0, &need);
   if (workspace == nullptr || workspace_bytes < need) return SLIM_ERR_WORKSPACE;
   if (!aligned(workspace, 256)) return SLIM_ERR_INVALID_ARG;
-  if (rows_fit(N, D))
+  if (rows_fit(N, D, dtype))
     return rows_fwd(x, w, targets, itype, (int)N, D, V, dtype, ignore_index, loss, lse, total,
                     workspace, s);
   unsigned* rep = nullptr;
@@ -1046,7 +1046,7 @@ extern "C" slim_status slim_vocab_loss_bwd(const void* x, const void* w, const v
   slim_vocab_loss_workspace_size(N, D, V, dtype, piece, 1, &need);
   if (workspace == nullptr || workspace_bytes < need) return SLIM_ERR_WORKSPACE;
   if (!aligned(workspace, 256)) return SLIM_ERR_INVALID_ARG;
-  if (rows_fit(N, D))
+  if (rows_fit(N, D, dtype))
     return rows_bwd(x, w, targets, itype, lse, dloss, dloss_stride, count, (int)N, D, V, dtype,
                     ignore_index, dx, dw, workspace, s);
   unsigned* rep = nullptr;

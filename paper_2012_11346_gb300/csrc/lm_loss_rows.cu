@@ -1,7 +1,7 @@
 // The vocabulary loss of a few rows (one drafted token, a handful of requests),
 // forward and backward.  Contract: include/slim_lm.h.
 //
-// With N <= 8 the products are far below the memory traffic: w is read once and,
+// With N <= 8 (fp32) or 4 (bf16) the products are far below the memory traffic: w is read once and,
 // backward, dw written once.  So the rows of x sit on the chip in fp32, w
 // streams past them in 16-byte loads, and the products are fp32 FMA in either
 // type: no staging, no split, g never rounded.
@@ -462,8 +462,10 @@ template <typename T, int VB>
 slim_status by_rows(const Job& j, bool bwd, cudaStream_t s) {
   if (j.N == 1) return run<T, VB, 1>(j, bwd, s);
   if (j.N == 2) return run<T, VB, 2>(j, bwd, s);
-  if (j.N <= 4) return run<T, VB, 4>(j, bwd, s);
-  return run<T, VB, 8>(j, bwd, s);
+  if constexpr (sizeof(T) == 4) {
+    if (j.N > 4) return run<T, VB, 8>(j, bwd, s);
+  }
+  return run<T, VB, 4>(j, bwd, s);
 }
 
 slim_status dispatch(const Job& j, slim_dtype dtype, bool bwd, cudaStream_t s) {
@@ -475,8 +477,12 @@ slim_status dispatch(const Job& j, slim_dtype dtype, bool bwd, cudaStream_t s) {
 
 }  // namespace
 
-bool rows_fit(long long N, int D) {
-  if (N < 1 || N > kMaxRows) return false;
+// Measured against the tile kernels at nine rows (forward / backward, us): bf16,
+// 512 x 32768, 3 rows 16.7/43 and 8 rows 20.7/86 here, 23.8/53 there; 1024 x
+// 50000, 33/110 and 54/212 against 41/118.  fp32, which the tile kernels have to
+// split first: 512 x 32768, 8 rows 24.7/82 here, 73.9/159 there.
+bool rows_fit(long long N, int D, slim_dtype dtype) {
+  if (N < 1 || N > (dtype == SLIM_BF16 ? kMaxRows / 2 : kMaxRows)) return false;
   const int nt = N == 1 ? 1 : N == 2 ? 2 : N <= 4 ? 4 : 8;
   return (long long)nt * D <= kMaxElems;
 }

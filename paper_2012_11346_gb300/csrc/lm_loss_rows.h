@@ -8,7 +8,7 @@ namespace slim {
 namespace lm {
 
 // Whether these sizes take this path.
-bool rows_fit(long long N, int D);
+bool rows_fit(long long N, int D, slim_dtype dtype);
 size_t rows_workspace(int N, int D, int V, bool bwd);
 // Arguments as in slim_vocab_loss_fwd / slim_vocab_loss_bwd, already checked.
 slim_status rows_fwd(const void* x, const void* w, const void* targets, slim_index it, int N, int D,
