@@ -6,6 +6,7 @@ torch.cuda.max_memory_allocated sees all of it) and the current stream.  There
 is no CPU fallback: if libslim.so is missing or no GPU is present, the calls
 raise.
 """
+import array
 import contextlib
 import ctypes
 import functools
@@ -466,17 +467,18 @@ def _require(cond, what):
         raise ValueError(what)
 
 
-def _require_ids(ids, what):
-    if ids.dtype not in INDEX_DTYPES:
+def _index_code(ids, what):
+    code = INDEX_DTYPES.get(ids.dtype)
+    if code is None:
         raise TypeError(f"{what} must be int32 or int64, got {ids.dtype}")
+    return code
 
 
-def _require_dtype(what, *ts):
-    for t in ts:
-        if t.dtype not in DTYPES:
-            raise TypeError(f"{what}: float32 or bfloat16 expected, got {t.dtype}")
-    if len({t.dtype for t in ts}) > 1:
-        raise TypeError(f"{what}: one dtype expected, got {[t.dtype for t in ts]}")
+def _dtype_code(t, what):
+    code = DTYPES.get(t.dtype)
+    if code is None:
+        raise TypeError(f"{what}: float32 or bfloat16 expected, got {t.dtype}")
+    return code
 
 
 _HERE = contextlib.nullcontext()
@@ -501,9 +503,9 @@ def embed_forward(ids, table, scale=1.0, out=None, stream=None):
     """slim_embed_fwd: out [*ids.shape, D] = scale * table[ids], zero rows where
     an id lies outside [0, V).  ids int32 or int64 of any shape; table [V, D]."""
     _require_cuda(ids, table)
-    _require_ids(ids, "ids")
-    _require_dtype("embed_forward", table)
-    _require(table.dim() == 2, "table must be [V, D]")
+    it, dt = _index_code(ids, "ids"), _dtype_code(table, "embed_forward")
+    if table.dim() != 2:
+        raise ValueError("table must be [V, D]")
     V, D = table.shape
     if out is None:
         with _on(stream):
@@ -512,9 +514,8 @@ def embed_forward(ids, table, scale=1.0, out=None, stream=None):
         _require_cuda(out)
         _require(out.dtype == table.dtype and tuple(out.shape) == (*ids.shape, D),
                  "out must be [*ids.shape, D] in the table's dtype")
-    _check(library().slim_embed_fwd(ids.data_ptr(), INDEX_DTYPES[ids.dtype], table.data_ptr(),
-                                    ids.numel(), D, V, DTYPES[table.dtype], scale,
-                                    out.data_ptr(), _stream_of(table, stream)), "slim_embed_fwd")
+    _check(library().slim_embed_fwd(ids.data_ptr(), it, table.data_ptr(), ids.numel(), D, V, dt,
+                                    scale, out.data_ptr(), _stream_of(table, stream)), "slim_embed_fwd")
     return out
 
 
@@ -523,9 +524,9 @@ def embed_backward(ids, dout, V, scale=1.0, dtable=None, workspace=None, stream=
     [V, D] in dout's dtype.  With dtable given, the gradient is added to it in
     place (and it is returned); rows that no id names are then left alone."""
     _require_cuda(ids, dout)
-    _require_ids(ids, "ids")
-    _require_dtype("embed_backward", dout)
-    _require(tuple(dout.shape[:-1]) == tuple(ids.shape), "dout must be [*ids.shape, D]")
+    it, dt = _index_code(ids, "ids"), _dtype_code(dout, "embed_backward")
+    if dout.shape[:-1] != ids.shape:
+        raise ValueError("dout must be [*ids.shape, D]")
     D, N = dout.shape[-1], ids.numel()
     accumulate = dtable is not None
     if accumulate:
@@ -537,8 +538,7 @@ def embed_backward(ids, dout, V, scale=1.0, dtable=None, workspace=None, stream=
             dtable = torch.empty(V, D, dtype=dout.dtype, device=dout.device)
         ws = workspace if workspace is not None else _workspace(
             embed_workspace_size(N, D, V, dout.dtype), dout.device)
-    _check(library().slim_embed_bwd(ids.data_ptr(), INDEX_DTYPES[ids.dtype], dout.data_ptr(), N, D,
-                                    V, DTYPES[dout.dtype], scale, int(accumulate),
+    _check(library().slim_embed_bwd(ids.data_ptr(), it, dout.data_ptr(), N, D, V, dt, scale, int(accumulate),
                                     dtable.data_ptr(), ws.data_ptr(), ws.numel(),
                                     _stream_of(dout, stream)), "slim_embed_bwd")
     return dtable
@@ -561,31 +561,30 @@ def clip_grad_norm(grads, max_norm, out=None, workspace=None, stream=None):
     n = len(grads)
     _require(n > 0, "no gradients")
     _require_cuda(*grads)
-    try:
-        dts = [DTYPES[g.dtype] for g in grads]
-    except KeyError as e:
-        raise TypeError(f"gradients must be float32 or bfloat16, got {e.args[0]}") from None
-    sizes = [g.numel() for g in grads]
-    src = [g.data_ptr() for g in grads]
+    types = [g.dtype for g in grads]
+    for t in set(types):
+        if t not in DTYPES:
+            raise TypeError(f"gradients must be float32 or bfloat16, got {t}")
+    bf16 = torch.bfloat16
+    dts = array.array("i", [1 if t is bf16 else 0 for t in types])
+    sizes = array.array("q", [g.numel() for g in grads])
+    src = dst = array.array("Q", [g.data_ptr() for g in grads])
     _require(len(set(src)) == n or len({p for p, k in zip(src, sizes) if k}) ==
              sum(k > 0 for k in sizes), "a gradient is listed twice")
-    ptr = ctypes.c_void_p * n
-    src_p = dst_p = ptr(*src)
     if out is not None:
-        dst = list(out)
-        _require_cuda(*dst)
-        _require([o.numel() for o in dst] == sizes and
-                 [o.dtype for o in dst] == [g.dtype for g in grads],
+        out = list(out)
+        _require_cuda(*out)
+        _require([o.numel() for o in out] == sizes.tolist() and [o.dtype for o in out] == types,
                  "out must hold one tensor of the same size and dtype per gradient")
-        dst_p = ptr(*[o.data_ptr() for o in dst])
+        dst = array.array("Q", [o.data_ptr() for o in out])
     with _on(stream):
         norm = torch.empty(1, dtype=torch.float32, device=grads[0].device)
         ws = workspace if workspace is not None else _workspace(clip_workspace_size(n),
                                                                 norm.device)
-    _check(library().slim_clip_grads(src_p, dst_p, (_ll * n)(*sizes), (_i * n)(*dts), n, max_norm,
-                                     norm.data_ptr(),
-                                     ws.data_ptr(), ws.numel(), _stream_of(norm, stream)),
-           "slim_clip_grads")
+    _check(library().slim_clip_grads(src.buffer_info()[0], dst.buffer_info()[0],
+                                     sizes.buffer_info()[0], dts.buffer_info()[0], n, max_norm,
+                                     norm.data_ptr(), ws.data_ptr(), ws.numel(),
+                                     _stream_of(norm, stream)), "slim_clip_grads")
     return norm
 
 
@@ -628,11 +627,15 @@ def vocab_loss_workspace_size(N, D, V, dtype, backward, piece=None):
 
 def _loss_dims(x, w, targets, what):
     _require_cuda(x, w, targets)
-    _require_ids(targets, "targets")
-    _require_dtype(what, x, w)
-    _require(w.dim() == 2 and x.shape[-1] == w.shape[1], "x must be [..., D] and w [V, D]")
-    _require(tuple(x.shape[:-1]) == tuple(targets.shape), "targets must have one entry per row of x")
-    return targets.numel(), w.shape[1], w.shape[0]
+    it, dt = _index_code(targets, "targets"), _dtype_code(x, what)
+    if w.dtype != x.dtype:
+        raise TypeError(f"{what}: one dtype expected, got {x.dtype} and {w.dtype}")
+    shape, rows = w.shape, x.shape
+    if len(shape) != 2 or rows[-1] != shape[1]:
+        raise ValueError("x must be [..., D] and w [V, D]")
+    if rows[:-1] != targets.shape:
+        raise ValueError("targets must have one entry per row of x")
+    return targets.numel(), shape[1], shape[0], it, dt
 
 
 def vocab_loss_forward(x, w, targets, ignore_index=-100, workspace=None, stream=None):
@@ -641,16 +644,16 @@ def vocab_loss_forward(x, w, targets, ignore_index=-100, workspace=None, stream=
     (loss, lse, total): per row the loss (0 where the target is ignore_index)
     and the log-sum, both fp32 in targets' shape, and total = [sum of the
     losses, number of rows not ignored]."""
-    N, D, V = _loss_dims(x, w, targets, "vocab_loss_forward")
+    N, D, V, it, dt = _loss_dims(x, w, targets, "vocab_loss_forward")
     with _on(stream):
-        loss = torch.empty(targets.shape, dtype=torch.float32, device=x.device)
+        dev = x.device
+        loss = torch.empty(targets.shape, dtype=torch.float32, device=dev)
         lse = torch.empty_like(loss)
-        total = torch.empty(2, dtype=torch.float32, device=x.device)
+        total = torch.empty(2, dtype=torch.float32, device=dev)
         ws = workspace if workspace is not None else _workspace(
-            vocab_loss_workspace_size(N, D, V, x.dtype, False), x.device)
-    _check(library().slim_vocab_loss_fwd(x.data_ptr(), w.data_ptr(), targets.data_ptr(),
-                                         INDEX_DTYPES[targets.dtype], N, D, V, DTYPES[x.dtype],
-                                         ignore_index, loss.data_ptr(), lse.data_ptr(),
+            vocab_loss_workspace_size(N, D, V, x.dtype, False), dev)
+    _check(library().slim_vocab_loss_fwd(x.data_ptr(), w.data_ptr(), targets.data_ptr(), it, N, D,
+                                         V, dt, ignore_index, loss.data_ptr(), lse.data_ptr(),
                                          total.data_ptr(), ws.data_ptr(), ws.numel(),
                                          _stream_of(x, stream)), "slim_vocab_loss_fwd")
     return loss, lse, total
@@ -663,12 +666,15 @@ def vocab_loss_backward(x, w, targets, lse, dloss, count=None, ignore_index=-100
     dloss: fp32 on the device, one value per row or a single one for all rows.
     count: None, or one fp32 value on the device (total[1:] of the forward for
     the mean loss).  Memory grows with rows x piece."""
-    N, D, V = _loss_dims(x, w, targets, "vocab_loss_backward")
-    piece = vocab_piece(N, V) if piece is None else piece
+    N, D, V, it, dt = _loss_dims(x, w, targets, "vocab_loss_backward")
     _require_cuda(lse, dloss)
-    _require(lse.dtype == torch.float32 and lse.numel() == N, "lse must be the forward's")
-    _require(dloss.dtype == torch.float32 and dloss.numel() in (1, N),
-             "dloss must be fp32, one value or one per row")
+    if piece is None:
+        piece = vocab_piece(N, V)
+    per_row = dloss.numel()
+    if lse.dtype != torch.float32 or lse.numel() != N:
+        raise ValueError("lse must be the forward's")
+    if dloss.dtype != torch.float32 or (per_row != 1 and per_row != N):
+        raise ValueError("dloss must be fp32, one value or one per row")
     if count is not None:
         _require_cuda(count)
         _require(count.dtype == torch.float32 and count.numel() == 1, "count must be one fp32 value")
@@ -677,10 +683,9 @@ def vocab_loss_backward(x, w, targets, lse, dloss, count=None, ignore_index=-100
         ws = workspace if workspace is not None else _workspace(
             vocab_loss_workspace_size(N, D, V, x.dtype, True, piece), x.device)
     _check(library().slim_vocab_loss_bwd(x.data_ptr(), w.data_ptr(), targets.data_ptr(),
-                                         INDEX_DTYPES[targets.dtype], lse.data_ptr(),
-                                         dloss.data_ptr(), int(dloss.numel() > 1), _ptr(count), N,
-                                         D, V, DTYPES[x.dtype], piece, ignore_index, dx.data_ptr(),
-                                         dw.data_ptr(), ws.data_ptr(), ws.numel(),
+                                         it, lse.data_ptr(), dloss.data_ptr(), int(per_row > 1),
+                                         _ptr(count), N, D, V, dt, piece, ignore_index,
+                                         dx.data_ptr(), dw.data_ptr(), ws.data_ptr(), ws.numel(),
                                          _stream_of(x, stream)), "slim_vocab_loss_bwd")
     return dx, dw
 
