@@ -450,21 +450,22 @@ __global__ void __launch_bounds__(256) k_embed_sum(SumJob j, const T* dout, T* d
 // Joins the runs that cross chunks.  A block looks at one chunk; if a run
 // starts in it and goes on, it adds the later chunks' partial rows in order.
 // Most such runs reach one chunk further, and all threads go side by side along
-// the columns.  A long run (a frequent token) is cut into 16 shares of 32 threads
-// a column block, whose sums are added in order.
-constexpr int kJoinThreads = 512, kJoinGroups = kJoinThreads / 32;
+// the columns.  A long run (a frequent token) is cut into 16 shares, a warp each,
+// whose sums are added in order; a warp goes along 64 vectors of the columns at a
+// time.
+constexpr int kJoinThreads = 512, kJoinGroups = kJoinThreads / 32, kJoinCols = 2;
 template <typename T, int VB>
 __global__ void __launch_bounds__(kJoinThreads) k_embed_join(SumJob j, T* dtable) {
   constexpr int n = Vec<T, VB>::n;
-  __shared__ float sh[kJoinGroups][n][32];
+  __shared__ float sh[kJoinGroups][kJoinCols][n][32];
   tc::grid_dependency_wait();
-  const int N = *j.count;
   const long long c = blockIdx.x;
-  const long long a = c * j.chunk, e = a + j.chunk;
-  if (e >= N) return;
+  const long long a = c * j.chunk, e = a + j.chunk;  // inside the list as the host knows it
+  // (read beside the count, which says whether they mean anything)
   const uint32_t key = j.key[e - 1], next = j.key[e], head = j.key[a],
                  before = a > 0 ? j.key[a - 1] : kNoKey;
-  if (key != next) return;
+  const int N = *j.count;
+  if (e >= N || key != next) return;
   // the run came into this chunk from an earlier one, which joins it
   if (head == key && before == key) return;
   const int lane = threadIdx.x & 31, grp = threadIdx.x >> 5;
@@ -485,6 +486,7 @@ __global__ void __launch_bounds__(kJoinThreads) k_embed_join(SumJob j, T* dtable
 #pragma unroll
       for (int x = 0; x < n; ++x) acc[x] = 0.0f;
       part_add<n>(first + (size_t)u * n, acc);
+#pragma unroll 4
       for (int b = 0; b < more; ++b) part_add<n>(rest + (size_t)b * 2 * j.ld + (size_t)u * n, acc);
       finish_row<T, VB>(j, acc, out + (size_t)u * n);
     }
@@ -492,25 +494,36 @@ __global__ void __launch_bounds__(kJoinThreads) k_embed_join(SumJob j, T* dtable
   }
   const int share = (more + kJoinGroups - 1) / kJoinGroups;
   const int b0 = min(grp * share, more), b1 = min(b0 + share, more);
-  for (int u0 = 0; u0 < j.U; u0 += 32) {
-    const int u = u0 + lane;
-    const bool on = u < j.U;
-    float acc[n];
+  for (int u0 = 0; u0 < j.U; u0 += 32 * kJoinCols) {
+    float acc[kJoinCols][n];
 #pragma unroll
-    for (int x = 0; x < n; ++x) acc[x] = 0.0f;
-    if (on) {
-      if (grp == 0) part_add<n>(first + (size_t)u * n, acc);
-#pragma unroll 8
-      for (int b = b0; b < b1; ++b) part_add<n>(rest + (size_t)b * 2 * j.ld + (size_t)u * n, acc);
-    }
+    for (int k = 0; k < kJoinCols; ++k)
 #pragma unroll
-    for (int x = 0; x < n; ++x) sh[grp][x][lane] = acc[x];
+      for (int x = 0; x < n; ++x) acc[k][x] = 0.0f;
+    auto add = [&](const float* row) {
+#pragma unroll
+      for (int k = 0; k < kJoinCols; ++k) {
+        const int u = u0 + 32 * k + lane;
+        if (u < j.U) part_add<n>(row + (size_t)u * n, acc[k]);
+      }
+    };
+    if (grp == 0) add(first);
+#pragma unroll 4
+    for (int b = b0; b < b1; ++b) add(rest + (size_t)b * 2 * j.ld);
+#pragma unroll
+    for (int k = 0; k < kJoinCols; ++k)
+#pragma unroll
+      for (int x = 0; x < n; ++x) sh[grp][k][x][lane] = acc[k][x];
     __syncthreads();
-    if (grp == 0 && on) {
+    if (grp < kJoinCols) {  // one warp per block of 32 vectors
+      const int u = u0 + 32 * grp + lane;
+      float sum[n];
+#pragma unroll
+      for (int x = 0; x < n; ++x) sum[x] = sh[0][grp][x][lane];
       for (int q = 1; q < kJoinGroups; ++q)
 #pragma unroll
-        for (int x = 0; x < n; ++x) acc[x] += sh[q][x][lane];
-      finish_row<T, VB>(j, acc, out + (size_t)u * n);
+        for (int x = 0; x < n; ++x) sum[x] += sh[q][grp][x][lane];
+      if (u < j.U) finish_row<T, VB>(j, sum, out + (size_t)u * n);
     }
     __syncthreads();
   }
@@ -538,7 +551,7 @@ struct Plan {
   int chunk;
   long long chunks;
 };
-Plan plan(long long N, int D, int V, int es) {
+Plan plan(long long N, int V) {
   Plan p;
   int bits = 1;
   while ((1LL << bits) < (long long)V) ++bits;
@@ -547,9 +560,9 @@ Plan plan(long long N, int D, int V, int es) {
   p.tiles = (int)(want < kSMs ? (want > 0 ? want : 1) : kSMs);
   p.tile = (int)((N + p.tiles - 1) / p.tiles);
   // chunks short enough for some waves of blocks, long enough that their
-  // partial rows (two each) stay small beside the rows they sum; longer for
-  // narrow rows, of which a block takes several chunks
-  long long k = N / ((long long)D * es > 1024 ? 2048 : 1024);
+  // partial rows (two each) stay small beside the rows they sum: 65536 x 768
+  // fp32 in chunks of 16, 32, 64 took 107, 101, 96 us
+  const long long k = N / 1024;
   p.chunk = (int)(k < 16 ? 16 : k > kMaxChunk ? kMaxChunk : k);
   p.chunks = (N + p.chunk - 1) / p.chunk;
   return p;
@@ -623,7 +636,7 @@ slim_status sort(const void* ids, slim_index itype, long long N, int V, const Pl
 template <typename T, int VB>
 slim_status bwd(const void* ids, slim_index itype, const void* dout, long long N, int D, int V,
                 float scale, int accumulate, void* dtable, void* ws, cudaStream_t s) {
-  const Plan p = plan(N, D, V, (int)sizeof(T));
+  const Plan p = plan(N, V);
   Carver cv(ws);
   const Ws w = carve(cv, N, D, p);
   SumJob j{};
@@ -699,7 +712,7 @@ extern "C" slim_status slim_embed_bwd_workspace_size(long long N, int D, int V, 
   using namespace slim::lm;
   if (!bytes || !sizes_ok(N, D, V, dtype, SLIM_I64)) return SLIM_ERR_INVALID_ARG;
   slim::Carver cv(nullptr);
-  carve(cv, N, D, plan(N, D, V, dtype == SLIM_F32 ? 4 : 2));
+  carve(cv, N, D, plan(N, V));
   *bytes = cv.bytes();
   return SLIM_OK;
 }
