@@ -446,10 +446,13 @@ struct GradJob {
   Product p[2];            // dw of the piece's words, and dx
   Deal deal;
   void* to[2];             // their results
-  float* part[2];          // with splits: [splits][M][acc_ld] partial sums
+  int parts[2];            // whether a product's tiles go to `part`:
+  float* part[2];          // [splits][M][acc_ld] partial sums
   float* acc;              // [N][acc_ld] running sum of dx over pieces
   int acc_ld;
-  int wide;                // the results' rows are whole 32-byte sectors
+  // 2: the results' rows are whole 32-byte sectors, 1: 16-byte pieces, 0: neither;
+  // their values then go to `part` and out from there
+  int wide;
   int first, last;         // of the pieces
   const float *scale, *count;  // the results' factor: (scale or 1) / (count or 1)
   const void* targets;
@@ -482,7 +485,7 @@ struct GradEpi {
     in = r < p->M;
     which = p == &j.p[1];
     live = true;
-    part = p->splits > 1 ? j.part[which] + ((size_t)w.split * p->M + r) * j.acc_ld + c : nullptr;
+    part = j.parts[which] ? j.part[which] + ((size_t)w.split * p->M + r) * j.acc_ld + c : nullptr;
     if (in && which == 1 && j.last) live = load_target(j.targets, j.i64, r) != j.ignore;
   }
   __device__ __forceinline__ void chunk(int c, float* f) {
@@ -522,19 +525,19 @@ struct GradEpi {
     for (int i = 0; i < 32; ++i) f[i] = live ? f[i] * scale : 0.0f;
     T* out = static_cast<T*>(j.to[which]) + (size_t)row * D + col + c;
     constexpr int W = 32 / sizeof(T);
-    if (j.wide && left >= 32) {
 #pragma unroll
-      for (int i = 0; i < 32; i += W) {
+    for (int i = 0; i < 32; i += W) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-          u[e] = NP == 1 ? tc::pack_bf16(f[i + 2 * e % W], f[i + (2 * e + 1) % W])
-                         : __float_as_uint(f[i + e % W]);
-        store32(out + i, u);
+      for (int e = 0; e < 8; ++e)
+        u[e] = NP == 1 ? tc::pack_bf16(f[i + 2 * e % W], f[i + (2 * e + 1) % W])
+                       : __float_as_uint(f[i + e % W]);
+      if (j.wide == 2) {
+        if (i < left) store32(out + i, u);
+      } else {
+        if (i < left) *reinterpret_cast<uint4*>(out + i) = make_uint4(u[0], u[1], u[2], u[3]);
+        if (i + W / 2 < left)
+          *reinterpret_cast<uint4*>(out + i + W / 2) = make_uint4(u[4], u[5], u[6], u[7]);
       }
-    } else {
-#pragma unroll
-      for (int i = 0; i < 32; ++i)
-        if (i < left) Io<T>::store(out, i, f[i]);
     }
   }
 };
@@ -551,14 +554,16 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
   gemm_roles<T>(sh, stage_memory<T>(), next, epi, job.err);
 }
 
-// The split products' partial sums, added in order: four columns a thread.
+// The split products' partial sums, added in order, and the way out for rows that
+// the tiles cannot store in aligned pieces (a scalar store per column and row took
+// 449 us of a 551 us step at 60000 x 300 x 100 bf16): four columns a thread.
 template <typename T>
 __global__ void __launch_bounds__(256) k_loss_parts(const __grid_constant__ GradJob j) {
   tc::grid_dependency_wait();
   const float scale = grad_scale(j);
   const int D = j.p[0].N, per = (D + 3) / 4;
-  const long long n0 = j.p[0].splits > 1 ? (long long)j.p[0].M * per : 0;
-  const long long n1 = j.p[1].splits > 1 ? (long long)j.p[1].M * per : 0;
+  const long long n0 = j.parts[0] ? (long long)j.p[0].M * per : 0;
+  const long long n1 = j.parts[1] ? (long long)j.p[1].M * per : 0;
   for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < n0 + n1;
        i += (long long)gridDim.x * 256) {
     const int which = i >= n0;
@@ -589,8 +594,18 @@ __global__ void __launch_bounds__(256) k_loss_parts(const __grid_constant__ Grad
     }
     T* out = static_cast<T*>(j.to[which]) + row * D + c;
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
-      if (c + e < D) Io<T>::store(out, e, live ? f[e] * scale : 0.0f);
+    for (int e = 0; e < 4; ++e) f[e] = live ? f[e] * scale : 0.0f;
+    if (D % 4 == 0) {
+      if constexpr (sizeof(T) == 4)
+        *reinterpret_cast<float4*>(out) = make_float4(f[0], f[1], f[2], f[3]);
+      else
+        *reinterpret_cast<uint2*>(out) =
+            make_uint2(tc::pack_bf16(f[0], f[1]), tc::pack_bf16(f[2], f[3]));
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (c + e < D) Io<T>::store(out, e, f[e]);
+    }
   }
 }
 
@@ -601,8 +616,9 @@ struct Sizes {
   slim_dtype dtype;
   int np() const { return dtype == SLIM_F32 ? 3 : 1; }
   int ld() const { return (D + 7) / 8 * 8; }  // of a staged row
+  bool even_rows() const { return D % (dtype == SLIM_F32 ? 4 : 8) == 0; }  // 16-byte pieces
   // bf16 rows that TMA can step over are read where they are
-  bool stage_w() const { return dtype == SLIM_F32 || D % 8 != 0; }
+  bool stage_w() const { return dtype == SLIM_F32 || !even_rows(); }
   bool stage_x(bool bwd) const { return bwd || stage_w(); }
 };
 
@@ -704,7 +720,8 @@ Ws carve(Carver& cv, const Sizes& z, int piece, bool bwd) {
       int splits[2];
       grad_splits(z, n, workers(CGv), splits);
       for (int i = 0; i < 2; ++i) {
-        const size_t k = splits[i] > 1 ? (size_t)splits[i] * (i ? z.N : n) * acc_ld(z.D) : 0;
+        const bool parts = splits[i] > 1 || !z.even_rows();
+        const size_t k = parts ? (size_t)splits[i] * (i ? z.N : n) * acc_ld(z.D) : 0;
         if (k > need[i]) need[i] = k;
       }
     }
@@ -914,7 +931,8 @@ slim_status bwd(const Sizes& z, const void* x, const void* w, const void* target
       return SLIM_ERR_CUDA;
     q.to[0] = static_cast<T*>(dw) + (size_t)v0 * z.D;
     q.to[1] = dx;
-    q.wide = z.D * sizeof(T) % 32 == 0 && ((uintptr_t)dw & 31) == 0 && ((uintptr_t)dx & 31) == 0;
+    q.wide = !z.even_rows() ? 0
+             : z.D * sizeof(T) % 32 == 0 && (((uintptr_t)dw | (uintptr_t)dx) & 31) == 0 ? 2 : 1;
     j.targets = q.targets = targets;
     j.i64 = q.i64 = it == SLIM_I64;
     j.ignore = q.ignore = ignore;
@@ -944,6 +962,8 @@ slim_status bwd(const Sizes& z, const void* x, const void* w, const void* target
     q.last = i == pieces - 1;
     int splits[2];
     grad_splits(z, n, workers(CG), splits);
+    q.parts[0] = splits[0] > 1 || !q.wide;
+    q.parts[1] = splits[1] > 1 || (!q.wide && q.last);
     long long nt[2], cost[2];
     for (int k = 0; k < 2; ++k) {
       q.p[k].splits = splits[k];
@@ -957,8 +977,8 @@ slim_status bwd(const Sizes& z, const void* x, const void* w, const void* target
     if (!launch<Tile<NP, CG>>(k_loss_grad<NP, CG>, (unsigned)wk * CG, true, s, q,
                               once<GradEpi<NP, CG>>()))
       return SLIM_ERR_CUDA;
-    if (splits[0] > 1 || splits[1] > 1) {
-      const long long e = ((splits[0] > 1 ? n : 0) + (splits[1] > 1 ? z.N : 0)) * cdiv(z.D, 4);
+    if (q.parts[0] || q.parts[1]) {
+      const long long e = ((q.parts[0] ? n : 0) + (q.parts[1] ? z.N : 0)) * cdiv(z.D, 4);
       prof::Scope sp(prof::K_LOSS_PARTS, s);
       if (!launch_on(k_loss_parts<T>, (unsigned)(cdiv(e, 256) < 152 * 8 ? cdiv(e, 256) : 152 * 8),
                      256, 0, 1, true, s, q))
