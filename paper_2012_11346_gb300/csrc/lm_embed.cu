@@ -366,7 +366,7 @@ constexpr int kSumAhead = 8;  // rows in flight per thread
 // from sum_blocks on write the rows that no token names as zero, 32 rows a
 // warp.
 template <typename T, int VB>
-__global__ void __launch_bounds__(256) k_embed_sum(SumJob j, const T* dout, T* dtable,
+__global__ void __launch_bounds__(256, 4) k_embed_sum(SumJob j, const T* dout, T* dtable,
                                                    unsigned sum_blocks) {
   constexpr int n = Vec<T, VB>::n;
   // a chunk's tokens, fetched once: the rows' loads then wait for no index
@@ -556,7 +556,7 @@ Plan plan(long long N, int V) {
   int bits = 1;
   while ((1LL << bits) < (long long)V) ++bits;
   p.passes = (bits + kRadixBits - 1) / kRadixBits;
-  const long long want = (N + 2047) / 2048;
+  const long long want = (N + kSortThreads - 1) / kSortThreads;  // one round of a block's threads
   p.tiles = (int)(want < kSMs ? (want > 0 ? want : 1) : kSMs);
   p.tile = (int)((N + p.tiles - 1) / p.tiles);
   // chunks short enough for some waves of blocks, long enough that their
