@@ -11,6 +11,14 @@
 // Backward, for each piece of the vocabulary: the logits again, with an epilogue
 // that turns them into g = c (p - onehot), kept for this piece only, and then one
 // launch with both products, dx += g w and dw = g^T x.
+//
+// What bounds them, on GB300 (kernel times; peak = 1978 TFLOP/s bf16):
+//   statistics  16384 x 512 x 50021 bf16  430-445 us, 1.9 PFLOP/s: the tensor
+//               pipe; 8192 x 768 x 10000 fp32 359 us, 2.1 P plane products/s.
+//   softmax     32768 x 512 x 32768 bf16  740 us (580 without g's stores).
+//   products    the same sizes            1296 us, 1.7 PFLOP/s at 1.7 GHz: power.
+// The logits are computed twice because a row's statistics are not known until
+// its last word; keeping them would be N x V, the thing to avoid.
 #include <stdint.h>
 
 #include "../../include/slim_lm.h"
