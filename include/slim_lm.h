@@ -14,6 +14,11 @@
  * 16-byte aligned unless their line below says otherwise; workspaces are
  * 256-byte aligned.  Results do not depend on the order in which blocks run:
  * two calls on the same inputs agree bit for bit.
+ *
+ * The vocabulary loss has device-side waits (its tile kernels'); they are bounded
+ * and reported like those of slim_fwd: the next slim_vocab_loss_* call on the same
+ * workspace returns SLIM_ERR_TIMEOUT, and slim_check_device_error reads the
+ * failure by blocking.  The other entry points have none.
  */
 #ifndef SLIM_LM_H_
 #define SLIM_LM_H_

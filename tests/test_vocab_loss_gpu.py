@@ -107,7 +107,7 @@ FEW = [(1, 512, 5000), (2, 96, 4097), (3, 1000, 333), (4, 4096, 50), (1, 16384, 
 @pytest.mark.parametrize("N,D,V", FEW)
 @pytest.mark.parametrize("mean", [False, True])
 def test_few_rows(cuda_device, N, D, V, dt, mean):
-    """Up to eight rows take kernels of their own (fp32 products in either type)."""
+    """Up to eight fp32 or four bf16 rows take kernels of their own."""
     x, w, t, c = make(cuda_device, N, D, V, dt, ignored=0.3)
     a, b = check(x, w, t, c, mean=mean), check(x, w, t, c, mean=mean)
     for u, v in zip(a, b):
@@ -137,6 +137,19 @@ def test_few_rows_ignored_and_bad(cuda_device, dt):
 def test_pieces(cuda_device, dt, piece):
     x, w, t, c = make(cuda_device, 333, 136, 1900, dt, it=torch.int32)
     check(x, w, t, c, piece=piece)
+
+
+@pytest.mark.parametrize("dt", [F32, BF16])
+@pytest.mark.parametrize("N,D,V,piece", [(333, 131, 1900, 256), (333, 132, 1900, 768),
+                                         (100, 77, 30000, 8192), (12000, 20, 300, 256),
+                                         (9000, 50, 40, None), (20, 1000, 9000, 2048)])
+def test_pieces_of_uneven_rows_and_split_sums(cuda_device, N, D, V, piece, dt):
+    """Rows that are no whole 16 bytes, several pieces, and reductions long enough
+    to be split, together."""
+    x, w, t, c = make(cuda_device, N, D, V, dt)
+    a, b = check(x, w, t, c, piece=piece, mean=True), check(x, w, t, c, piece=piece, mean=True)
+    for u, v in zip(a, b):
+        assert torch.equal(u, v)
 
 
 @pytest.mark.parametrize("dt", [F32, BF16])
@@ -314,6 +327,19 @@ def test_another_stream_and_given_workspace(cuda_device):
     s.synchronize()
     for a, b in zip(base, (loss, lse, total, dx, dw)):
         assert torch.equal(a, b)
+    slim.check_device_error(ws)
+
+
+@pytest.mark.parametrize("N", [3, 300])
+def test_error_word_is_cleared(cuda_device, N):
+    """Whatever a workspace held, a call leaves its error word clear."""
+    x, w, t, c = make(cuda_device, N, 64, 500, F32)
+    n = max(slim.vocab_loss_workspace_size(N, 64, 500, F32, b) for b in (False, True))
+    ws = torch.full((n,), 255, dtype=torch.uint8, device=cuda_device)
+    _, lse, _ = slim.vocab_loss_forward(x, w, t, workspace=ws)
+    slim.check_device_error(ws)
+    ws.fill_(255)
+    slim.vocab_loss_backward(x, w, t, lse, c, workspace=ws)
     slim.check_device_error(ws)
 
 
