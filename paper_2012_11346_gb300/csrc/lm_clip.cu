@@ -19,6 +19,8 @@
 #include <float.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "../../include/slim_lm.h"
 #include "common.cuh"
 #include "launch.h"
@@ -100,6 +102,15 @@ template <> struct Pack<__nv_bfloat16> {
   }
 };
 
+// Elements from p to its next 128-byte boundary, at most n: a warp's 512 bytes
+// then cover whole lines (16-byte alignment alone cost a slice that starts one
+// element into its buffer 17 % of the norm's rate).
+template <typename T>
+__device__ __forceinline__ long long to_line(const T* p, long long n) {
+  const long long lead = (long long)(-(intptr_t)p & 127) / (long long)sizeof(T);
+  return lead < n ? lead : n;
+}
+
 // ------------------------------------------------------------------ norm
 // Thresholds of a thread's fp32 sum of squares.  Above kTiny, squares lost to
 // underflow (each below 2^-126) are below its rounding; at or under it every
@@ -147,9 +158,7 @@ __device__ __forceinline__ float square_sum(const T* p, long long lead, long lon
 template <typename T>
 __device__ __forceinline__ double chunk_squares(const T* p, long long n) {
   constexpr int W = Pack<T>::n;
-  const unsigned mis = (unsigned)(reinterpret_cast<uintptr_t>(p) & 15u) / sizeof(T);
-  long long lead = mis ? W - mis : 0;
-  if (lead > n) lead = n;
+  const long long lead = to_line(p, n);
   const long long nvec = (n - lead) / W;
   unsigned any = 0, dummy = 0;
   const float s = square_sum<T>(p, lead, nvec, n, 1.0f, any);
@@ -200,27 +209,19 @@ __global__ void __launch_bounds__(kThreads) k_norm(const __grid_constant__ Table
 }
 
 // ------------------------------------------------------------------ clip
+// Bytes k .. k+15 of the 32 bytes (a, b), k = 4 W + r / 8.
+template <int W>
+__device__ __forceinline__ uint4 shifted(const uint4& a, const uint4& b, unsigned r) {
+  const uint32_t c[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+  return make_uint4(__funnelshift_r(c[W], c[W + 1], r), __funnelshift_r(c[W + 1], c[W + 2], r),
+                    __funnelshift_r(c[W + 2], c[W + 3], r), __funnelshift_r(c[W + 3], c[W + 4], r));
+}
+
 template <typename T>
 __device__ __forceinline__ void scale_chunk(const T* p, T* q, long long n, float c) {
   constexpr int W = Pack<T>::n;
-  const unsigned mp = (unsigned)(reinterpret_cast<uintptr_t>(p) & 15u);
-  const unsigned mq = (unsigned)(reinterpret_cast<uintptr_t>(q) & 15u);
-  if (mp != mq) {  // no common alignment: element by element
-    long long i = threadIdx.x;
-    for (; i + 7 * kThreads < n; i += 8 * kThreads) {
-      float x[8];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) x[j] = Io<T>::load(p, i + j * kThreads);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) Io<T>::store(q, i + j * kThreads, x[j] * c);
-    }
-    for (; i < n; i += kThreads) Io<T>::store(q, i, Io<T>::load(p, i) * c);
-    return;
-  }
-  long long lead = mp ? W - (long long)(mp / sizeof(T)) : 0;
-  if (lead > n) lead = n;
+  const long long lead = to_line(q, n);  // the stores' lines
   const long long nvec = (n - lead) / W, tail = lead + nvec * W;
-  const uint4* v = reinterpret_cast<const uint4*>(p + lead);
   uint4* o = reinterpret_cast<uint4*>(q + lead);
   auto put = [&](const uint4& u) {
     float f[W];
@@ -229,15 +230,44 @@ __device__ __forceinline__ void scale_chunk(const T* p, T* q, long long n, float
     for (int e = 0; e < W; ++e) f[e] *= c;
     return Pack<T>::put(f);
   };
+  // the source may lie otherwise: then every 16 bytes come from the two aligned
+  // pieces that hold them (each holds some, so neither leaves the buffer)
+  const uintptr_t src = reinterpret_cast<uintptr_t>(p + lead);
+  const unsigned k = (unsigned)(src & 15u);
+  const uint4* v = reinterpret_cast<const uint4*>(src - k);
   long long i = threadIdx.x;
-  for (; i + 7 * kThreads < nvec; i += 8 * kThreads) {
-    uint4 u[8];
+  if (k == 0) {
+    for (; i + 7 * kThreads < nvec; i += 8 * kThreads) {
+      uint4 u[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) u[j] = v[i + j * kThreads];
+      for (int j = 0; j < 8; ++j) u[j] = v[i + j * kThreads];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) o[i + j * kThreads] = put(u[j]);
+      for (int j = 0; j < 8; ++j) o[i + j * kThreads] = put(u[j]);
+    }
+    for (; i < nvec; i += kThreads) o[i] = put(v[i]);
+  } else {
+    const unsigned r = (k & 3u) * 8;
+    auto all = [&](auto word) {
+      constexpr int w = decltype(word)::value;
+      for (; i + 3 * kThreads < nvec; i += 4 * kThreads) {
+        uint4 a[4], b[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          a[j] = v[i + j * kThreads];
+          b[j] = v[i + j * kThreads + 1];
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) o[i + j * kThreads] = put(shifted<w>(a[j], b[j], r));
+      }
+      for (; i < nvec; i += kThreads) o[i] = put(shifted<w>(v[i], v[i + 1], r));
+    };
+    switch (k >> 2) {
+      case 0: all(std::integral_constant<int, 0>()); break;
+      case 1: all(std::integral_constant<int, 1>()); break;
+      case 2: all(std::integral_constant<int, 2>()); break;
+      default: all(std::integral_constant<int, 3>()); break;
+    }
   }
-  for (; i < nvec; i += kThreads) o[i] = put(v[i]);
   if (threadIdx.x < lead) Io<T>::store(q, threadIdx.x, Io<T>::load(p, threadIdx.x) * c);
   if (tail + threadIdx.x < n)
     Io<T>::store(q, tail + threadIdx.x, Io<T>::load(p, tail + threadIdx.x) * c);
