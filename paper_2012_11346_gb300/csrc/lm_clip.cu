@@ -8,8 +8,8 @@
 // scales and writes.  HBM bounds both; a set that fits L2 is read from HBM once,
 // and of a larger set the second launch starts with the end, which L2 still
 // holds.  The tensors' addresses travel as kernel parameters: no copy and no
-// device table.  279 M fp32 gradients into a second list: 516 us, of which the
-// norm 170 (6.5 TB/s) and the scaling 346 (6.4 TB/s read and written).
+// device table.  279 M fp32 gradients into a second list: 505-516 us, of which
+// the norm 165 (6.8 TB/s) and the scaling 340 (6.5 TB/s read and written).
 //
 // Range: a thread adds the squares of 64 to 128 elements in fp32 and moves the
 // sum to fp64.  Squares leave fp32's range long before the gradients do, so a
@@ -41,7 +41,11 @@ constexpr int kGridNorm = 152 * 4, kGridClip = 152 * 8;
 // gradients of 4.3 MB in all: 16 -> 12 us with the chained launches).
 constexpr int kChunkMost = 65536, kChunkLeast = 4096;
 
-// A launch's tensors.  Tensor t's chunks are numbered [start[t], start[t+1]).
+// A launch's tensors.  Tensor t's chunks are numbered [start[t], start[t+1]); they
+// begin at its first 128-byte boundary (of the source for the norm, of the target
+// for the scaling), and the first one also takes the elements before that: a
+// warp's 512 bytes then cover whole lines, and no chunk but a tensor's last leaves
+// a few threads with loads of their own.
 template <int CAP>
 struct Table {
   const void* src[CAP];
@@ -102,13 +106,23 @@ template <> struct Pack<__nv_bfloat16> {
   }
 };
 
-// Elements from p to its next 128-byte boundary, at most n: a warp's 512 bytes
-// then cover whole lines (16-byte alignment alone cost a slice that starts one
-// element into its buffer 17 % of the norm's rate).
-template <typename T>
-__device__ __forceinline__ long long to_line(const T* p, long long n) {
-  const long long lead = (long long)(-(intptr_t)p & 127) / (long long)sizeof(T);
+// Elements of 2^ls bytes from address p to its next 128-byte boundary, at most n.
+__host__ __device__ __forceinline__ long long to_line(const void* p, long long n, int ls) {
+  const long long lead = (long long)(-(intptr_t)p & 127) >> ls;
   return lead < n ? lead : n;
+}
+
+// A chunk: elements [at, at + m) of the tensor, and [0, lead) beside them.
+struct Chunk {
+  long long at, m, lead;
+};
+template <int CAP>
+__device__ __forceinline__ Chunk find_chunk(const Table<CAP>& tb, int t, unsigned chunk,
+                                            const void* p, long long n, int ls) {
+  const long long per = tb.chunk >> ls, lead = to_line(p, n, ls);
+  const long long x = chunk - tb.start[t], a = x * per;
+  const long long left = n - lead - a;
+  return Chunk{lead + a, left < per ? left : per, x == 0 ? lead : 0};
 }
 
 // ------------------------------------------------------------------ norm
@@ -119,11 +133,12 @@ __device__ __forceinline__ long long to_line(const T* p, long long n) {
 constexpr float kTiny = 0x1p-80f;
 
 template <typename T>
-__device__ __forceinline__ float square_sum(const T* p, long long lead, long long nvec,
-                                            long long n, float scale, unsigned& any) {
+__device__ __forceinline__ float square_sum(const T* p, const Chunk& c, float scale,
+                                            unsigned& any) {
   constexpr int W = Pack<T>::n;
   float s = 0.0f;
-  const uint4* v = reinterpret_cast<const uint4*>(p + lead);
+  const uint4* v = reinterpret_cast<const uint4*>(p + c.at);
+  const long long nvec = c.m / W;
   long long i = threadIdx.x;
   auto take = [&](const uint4& u) {
     any |= (u.x | u.y | u.z | u.w);
@@ -143,31 +158,33 @@ __device__ __forceinline__ float square_sum(const T* p, long long lead, long lon
     for (int j = 0; j < 8; ++j) take(u[j]);
   }
   for (; i < nvec; i += kThreads) take(v[i]);
-  // the elements before the first aligned 16 bytes and after the last
-  const long long tail = lead + nvec * W;
+  // the elements before the first line and after the last 16 bytes
   auto one = [&](long long k) {
     const float x = Io<T>::load(p, k) * scale;
     any |= x != 0.0f;
     s = fmaf(x, x, s);
   };
-  if (threadIdx.x < lead) one(threadIdx.x);
-  if (tail + threadIdx.x < n) one(tail + threadIdx.x);
+  if (threadIdx.x < c.lead) one(threadIdx.x);
+  if (nvec * W + threadIdx.x < c.m) one(c.at + nvec * W + threadIdx.x);
   return s;
 }
 
+// Once more, scaled; out of line, as it hardly ever runs.
 template <typename T>
-__device__ __forceinline__ double chunk_squares(const T* p, long long n) {
-  constexpr int W = Pack<T>::n;
-  const long long lead = to_line(p, n);
-  const long long nvec = (n - lead) / W;
-  unsigned any = 0, dummy = 0;
-  const float s = square_sum<T>(p, lead, nvec, n, 1.0f, any);
+__device__ __noinline__ double scaled_squares(const T* p, long long at, long long m,
+                                              long long lead, bool up) {
+  unsigned any = 0;
+  const double s = (double)square_sum<T>(p, Chunk{at, m, lead}, up ? 0x1p96f : 0x1p-96f, any);
+  return s * (up ? 0x1p-192 : 0x1p192);
+}
+template <typename T>
+__device__ __forceinline__ double chunk_squares(const T* p, const Chunk& c) {
+  unsigned any = 0;
+  const float s = square_sum<T>(p, c, 1.0f, any);
   if (s >= kTiny && s <= FLT_MAX) return (double)s;
-  if (s < kTiny) {
-    if ((any << 1) == 0) return 0.0;  // nothing but zeros
-    return (double)square_sum<T>(p, lead, nvec, n, 0x1p96f, dummy) * 0x1p-192;
-  }
-  return (double)square_sum<T>(p, lead, nvec, n, 0x1p-96f, dummy) * 0x1p192;
+  const bool up = s < kTiny;  // else an overflow, an infinity or NaN
+  if (up && (any << 1) == 0) return 0.0;  // nothing but zeros
+  return scaled_squares<T>(p, c.at, c.m, c.lead, up);
 }
 
 // Sum of x over the block, in a fixed order, for thread 0.  By one warp: fp64
@@ -196,13 +213,11 @@ __global__ void __launch_bounds__(kThreads) k_norm(const __grid_constant__ Table
     const int t = find_tensor(tb, c);
     const bool half = tb.numel[t] & kBf16Bit;
     const long long n = (long long)(tb.numel[t] & ~kBf16Bit);
-    const long long per = tb.chunk >> (half ? 1 : 2);
-    const long long a = (long long)(c - tb.start[t]) * per;
-    const long long m = n - a < per ? n - a : per;
+    const Chunk ch = find_chunk(tb, t, c, tb.src[t], n, half ? 1 : 2);
     if (half)
-      acc += chunk_squares(static_cast<const __nv_bfloat16*>(tb.src[t]) + a, m);
+      acc += chunk_squares(static_cast<const __nv_bfloat16*>(tb.src[t]), ch);
     else
-      acc += chunk_squares(static_cast<const float*>(tb.src[t]) + a, m);
+      acc += chunk_squares(static_cast<const float*>(tb.src[t]), ch);
   }
   const double s = block_sum(acc, sh);
   if (threadIdx.x == 0) part[blockIdx.x] = s;
@@ -218,11 +233,10 @@ __device__ __forceinline__ uint4 shifted(const uint4& a, const uint4& b, unsigne
 }
 
 template <typename T>
-__device__ __forceinline__ void scale_chunk(const T* p, T* q, long long n, float c) {
+__device__ __forceinline__ void scale_chunk(const T* p, T* q, const Chunk& ch, float c) {
   constexpr int W = Pack<T>::n;
-  const long long lead = to_line(q, n);  // the stores' lines
-  const long long nvec = (n - lead) / W, tail = lead + nvec * W;
-  uint4* o = reinterpret_cast<uint4*>(q + lead);
+  const long long nvec = ch.m / W;
+  uint4* o = reinterpret_cast<uint4*>(q + ch.at);
   auto put = [&](const uint4& u) {
     float f[W];
     Pack<T>::get(u, f);
@@ -232,7 +246,7 @@ __device__ __forceinline__ void scale_chunk(const T* p, T* q, long long n, float
   };
   // the source may lie otherwise: then every 16 bytes come from the two aligned
   // pieces that hold them (each holds some, so neither leaves the buffer)
-  const uintptr_t src = reinterpret_cast<uintptr_t>(p + lead);
+  const uintptr_t src = reinterpret_cast<uintptr_t>(p + ch.at);
   const unsigned k = (unsigned)(src & 15u);
   const uint4* v = reinterpret_cast<const uint4*>(src - k);
   long long i = threadIdx.x;
@@ -268,9 +282,11 @@ __device__ __forceinline__ void scale_chunk(const T* p, T* q, long long n, float
       default: all(std::integral_constant<int, 3>()); break;
     }
   }
-  if (threadIdx.x < lead) Io<T>::store(q, threadIdx.x, Io<T>::load(p, threadIdx.x) * c);
-  if (tail + threadIdx.x < n)
-    Io<T>::store(q, tail + threadIdx.x, Io<T>::load(p, tail + threadIdx.x) * c);
+  if (threadIdx.x < ch.lead) Io<T>::store(q, threadIdx.x, Io<T>::load(p, threadIdx.x) * c);
+  if (nvec * W + threadIdx.x < ch.m) {
+    const long long k = ch.at + nvec * W + threadIdx.x;
+    Io<T>::store(q, k, Io<T>::load(p, k) * c);
+  }
 }
 
 template <int CAP>
@@ -299,15 +315,12 @@ __global__ void __launch_bounds__(kThreads) k_clip(const __grid_constant__ Table
     const int t = find_tensor(tb, chunk);
     const bool half = tb.numel[t] & kBf16Bit;
     const long long n = (long long)(tb.numel[t] & ~kBf16Bit);
-    const long long per = tb.chunk >> (half ? 1 : 2);
-    const long long a = (long long)(chunk - tb.start[t]) * per;
-    const long long m = n - a < per ? n - a : per;
+    const Chunk ch = find_chunk(tb, t, chunk, tb.dst[t], n, half ? 1 : 2);
     if (half)
-      scale_chunk(static_cast<const __nv_bfloat16*>(tb.src[t]) + a,
-                  static_cast<__nv_bfloat16*>(tb.dst[t]) + a, m, c);
+      scale_chunk(static_cast<const __nv_bfloat16*>(tb.src[t]),
+                  static_cast<__nv_bfloat16*>(tb.dst[t]), ch, c);
     else
-      scale_chunk(static_cast<const float*>(tb.src[t]) + a, static_cast<float*>(tb.dst[t]) + a, m,
-                  c);
+      scale_chunk(static_cast<const float*>(tb.src[t]), static_cast<float*>(tb.dst[t]), ch, c);
   }
 }
 
@@ -325,9 +338,10 @@ struct List {
   int n;
 };
 
-// Tensors [a, ..) of the list, as many as fit; returns the next one.
+// Tensors [a, ..) of the list, as many as fit; returns the next one.  The chunks
+// begin where `by_dst` says.
 template <int CAP>
-int fill(const List& l, int a, Table<CAP>* tb, bool* in_place, double* bytes) {
+int fill(const List& l, int a, bool by_dst, Table<CAP>* tb, bool* in_place, double* bytes) {
   tb->n = 0;
   unsigned long long chunks = 0;
   *in_place = true;
@@ -336,13 +350,15 @@ int fill(const List& l, int a, Table<CAP>* tb, bool* in_place, double* bytes) {
   for (; t < l.n && tb->n < CAP; ++t) {
     if (l.numel[t] == 0) continue;
     const bool half = l.dtypes[t] == SLIM_BF16;
-    const long long per = tb->chunk >> (half ? 1 : 2);
+    const int ls = half ? 1 : 2;
+    const long long per = tb->chunk >> ls;
+    const long long body = l.numel[t] - to_line(by_dst ? l.dst[t] : l.src[t], l.numel[t], ls);
     const int i = tb->n++;
     tb->src[i] = l.src[t];
     tb->dst[i] = l.dst[t];
     tb->numel[i] = (unsigned long long)l.numel[t] | (half ? kBf16Bit : 0);
     tb->start[i] = (unsigned)chunks;
-    chunks += (unsigned long long)((l.numel[t] + per - 1) / per);
+    chunks += body > 0 ? (unsigned long long)((body + per - 1) / per) : 1;
     if (l.src[t] != l.dst[t]) *in_place = false;
     *bytes += (double)l.numel[t] * (half ? 2 : 4);
   }
@@ -370,7 +386,7 @@ slim_status run(const List& l, float max_norm, float* norm, int* header, double*
   };
   int a = 0;
   do {
-    a = fill(l, a, &tb, &in_place, &bytes);
+    a = fill(l, a, false, &tb, &in_place, &bytes);
     prof::Scope ps(prof::K_CLIP, s, 0.0, bytes);
     if (!launch_on<Table<CAP>, double*, int*>(k_norm<CAP>, grid(kGridNorm), kThreads, 0, 1, parts > 0, s, tb,
                                               part + parts, parts == 0 ? header : nullptr))
@@ -380,7 +396,7 @@ slim_status run(const List& l, float max_norm, float* norm, int* header, double*
   a = 0;
   bool first = true;
   do {
-    a = fill(l, a, &tb, &in_place, &bytes);
+    a = fill(l, a, true, &tb, &in_place, &bytes);
     prof::Scope ps(prof::K_CLIP, s, 0.0, bytes);
     if (!launch_on<Table<CAP>, const double*, int, float, int, float*>(
             k_clip<CAP>, grid(kGridClip), kThreads, 0, 1, true, s, tb, part, parts, max_norm, in_place,

@@ -594,12 +594,19 @@ class Embedding(torch.autograd.Function):
         ids = ids.contiguous()
         ctx.save_for_backward(ids)
         ctx.V, ctx.scale = table.shape[0], scale
-        return embed_forward(ids, table.contiguous(), scale)
+        return embed_forward(ids, _ready(table), scale)
 
     @staticmethod
     def backward(ctx, dout):
         (ids,) = ctx.saved_tensors
-        return None, embed_backward(ids, dout.contiguous(), ctx.V, ctx.scale), None
+        return None, embed_backward(ids, _ready(dout), ctx.V, ctx.scale), None
+
+
+def _ready(t):
+    """t as the entry points take it: contiguous, on a 16-byte boundary (a slice
+    of rows may begin anywhere)."""
+    t = t.contiguous()
+    return t if t.data_ptr() % 16 == 0 else t.clone()
 
 
 def embedding(ids, table, scale=1.0):
@@ -693,7 +700,7 @@ def vocab_loss_backward(x, w, targets, lse, dloss, count=None, ignore_index=-100
 class VocabLoss(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, w, targets, reduction, ignore_index, piece):
-        x, w, targets = x.contiguous(), w.contiguous(), targets.contiguous()
+        x, w, targets = _ready(x), _ready(w), targets.contiguous()
         loss, lse, total = vocab_loss_forward(x, w, targets, ignore_index)
         ctx.save_for_backward(x, w, targets, lse, total)
         ctx.mean, ctx.ignore_index, ctx.piece = reduction == "mean", ignore_index, piece

@@ -313,6 +313,23 @@ def test_autograd(cuda_device):
         assert rel(x.grad, r["dx"]) <= 1e-5 and rel(w.grad, r["dw"]) <= 1e-5
 
 
+def test_autograd_takes_slices_and_transposes(cuda_device):
+    """Rows that begin off a 16-byte boundary and transposed operands: refused by
+    the plain calls, copied by the differentiable one."""
+    x, w, t, c = make(cuda_device, 201, 33, 120, F32)
+    with pytest.raises(slim.SlimError) as e:
+        slim.vocab_loss_forward(x[1:], w, t[1:])
+    assert e.value.status == 1
+    with pytest.raises(RuntimeError):
+        slim.vocab_loss_forward(x, w.t().contiguous().t(), t)
+    x.requires_grad_(), w.requires_grad_()
+    slim.vocab_loss(x[1:], w.t().contiguous().t(), t[1:]).backward()
+    n = (t[1:] != -100).sum()
+    r = ref64(x.detach()[1:], w.detach(), t[1:], (1.0 / n).expand(200).contiguous())
+    assert rel(x.grad[1:], r["dx"]) <= 1e-5 and rel(w.grad, r["dw"]) <= 1e-5
+    assert (x.grad[0] == 0).all()
+
+
 def test_another_stream_and_given_workspace(cuda_device):
     x, w, t, c = make(cuda_device, 500, 64, 3000, BF16)
     base = check(x, w, t, c)
