@@ -32,19 +32,25 @@ constexpr int kEpiCols = kTN / 4;
 constexpr int kGemmThreads = 128 + 32 * kEpiWarps;  // warps: TMA, MMA, TMEM, spare, epilogue
 
 constexpr int kSmemBytes = 227 * 1024 - 1024 - 512;  // after alignment and barriers
-template <int NP, int CG, bool JOIN = (NP > 1)>
+// HOLD: a block keeps its rows of a short A (up to kHeld stages, K-major) in
+// shared memory while it stays with the same tile row, and the ring carries B
+// alone.  Worth it where a worker walks along many columns.
+constexpr int kHeld = 8;
+template <int NP, int CG, bool JOIN = (NP > 1), bool HOLD_A = false>
 struct Tile {
   static constexpr int PLANES = NP, GROUP = CG;
-  static constexpr bool ACC = JOIN;
+  static constexpr bool ACC = JOIN, HOLD = HOLD_A;
+  static_assert(!HOLD || NP == 1, "one plane");
   static constexpr int BROWS = kTN / CG;    // rows of B that a block holds
   static constexpr int A_BYTES = kTM * kTK * 2, B_BYTES = BROWS * kTK * 2;
-  static constexpr int STAGE = A_BYTES + B_BYTES;  // one plane of either operand
-  static constexpr int FIT = kSmemBytes / STAGE;
+  static constexpr int HELD_BYTES = HOLD ? kHeld * A_BYTES : 0;
+  static constexpr int STAGE = HOLD ? B_BYTES : A_BYTES + B_BYTES;  // one plane of either operand
+  static constexpr int FIT = (kSmemBytes - HELD_BYTES) / STAGE;
   static constexpr int STAGES = FIT < 8 ? FIT : 8;
   // chains of 512 of the reduction, or of 64 with three planes: there only the
   // last four steps, the large planes', work on a large sum
   static constexpr int CHAIN = NP == 1 ? 8 : 1;
-  static constexpr size_t smem() { return 1024 + (size_t)STAGES * STAGE; }
+  static constexpr size_t smem() { return 1024 + HELD_BYTES + (size_t)STAGES * STAGE; }
   static_assert(STAGES >= 3, "a stage per plane");
 };
 
@@ -102,6 +108,7 @@ struct TileRange {
 
 struct GemmShared {
   uint64_t full[8], empty[8], tfull[2], tempty[2];
+  uint64_t held, unheld;  // HOLD: the rows are there; no MMA reads them any more
   uint32_t tmem;
 };
 
@@ -209,6 +216,8 @@ __device__ __forceinline__ void gemm_begin(GemmShared& sh) {
       tc::mbar_init(tc::smem_u32(&sh.full[i]), 1);
       tc::mbar_init(tc::smem_u32(&sh.empty[i]), 1);
     }
+    tc::mbar_init(tc::smem_u32(&sh.held), 1);
+    tc::mbar_init(tc::smem_u32(&sh.unheld), 1);
     for (int i = 0; i < 2; ++i) {
       tc::mbar_init(tc::smem_u32(&sh.tfull[i]), 1);
       tc::mbar_init(tc::smem_u32(&sh.tempty[i]), kEpiWarps * CG);
@@ -273,7 +282,8 @@ __device__ bool gemm_copy(GemmShared& sh, uint8_t* stages, Next next, int* err) 
   const uint32_t full0 = tc::smem_u32(&sh.full[0]), empty0 = tc::smem_u32(&sh.empty[0]);
   const uint32_t count0 = CG == 2 ? map_to_rank(full0, 0) : full0;  // the leader's
   const uint32_t smem = tc::smem_u32(stages);
-  uint32_t st = 0, phase = 1;
+  uint32_t st = 0, phase = 1, held_phase = 0;
+  int held_row = -1;
   auto step_on = [&] {
     if (++st == T::STAGES) {
       st = 0;
@@ -289,16 +299,35 @@ __device__ bool gemm_copy(GemmShared& sh, uint8_t* stages, Next next, int* err) 
     const CUtensorMap* map_b = uniform(&w.p->b);
     const int a_mn = uniform(w.p->a_mn), b_mn = uniform(w.p->b_mn);
     const int row = uniform((w.m * CG + rank) * kTM), col = uniform(w.n * kTN + rank * T::BROWS);
-    const int k1 = uniform(w.k1) * kTK;
-    for (int k = uniform(w.k0) * kTK; k < k1; k += kTK) {
+    const int k0 = uniform(w.k0) * kTK, k1 = uniform(w.k1) * kTK;
+    if (T::HOLD && row != held_row) {
+      if (held_row >= 0) {
+        if (!__all_sync(0xffffffffu, tc::mbar_wait(tc::smem_u32(&sh.unheld), held_phase, err)))
+          return false;
+        held_phase ^= 1;
+      }
+      held_row = row;
+      if (elect_one()) {
+        const uint32_t held = tc::smem_u32(&sh.held);
+        if (rank == 0) tc::mbar_expect_tx(held, CG * (k1 - k0) / kTK * T::A_BYTES);
+        const uint32_t bar = CG == 2 ? map_to_rank(held, 0) : held;
+        for (int k = k0; k < k1; k += kTK)
+          gemm_tma<CG>(smem + (k - k0) / kTK * T::A_BYTES, map_a, k, row, 0, bar);
+      }
+      __syncwarp();
+    }
+    for (int k = k0; k < k1; k += kTK) {
 #pragma unroll 1
       for (int q = 0; q < NP; ++q) {
         if (!free()) return false;
         if (elect_one()) {
           if (rank == 0) tc::mbar_expect_tx(full0 + 8 * st, CG * T::STAGE);
           const uint32_t full = count0 + 8 * st;
-          const uint32_t sa = smem + st * T::STAGE, sb = sa + T::A_BYTES;
-          if (a_mn) {
+          const uint32_t sa = smem + T::HELD_BYTES + st * T::STAGE;
+          const uint32_t sb = T::HOLD ? sa : sa + T::A_BYTES;
+          if (T::HOLD) {
+            // the rows are held
+          } else if (a_mn) {
 #pragma unroll
             for (int j = 0; j < kTM / 64; ++j)
               gemm_tma<CG>(sa + j * 8192, map_a, row + 64 * j, k, q, full);
@@ -334,7 +363,8 @@ __device__ bool gemm_multiply(GemmShared& sh, uint8_t* stages, Next next, int* e
   Work w;
   const uint32_t full0 = tc::smem_u32(&sh.full[0]), empty0 = tc::smem_u32(&sh.empty[0]);
   const uint32_t tmem = sh.tmem;
-  uint32_t st = 0, phase = 0, acc = 0;
+  uint32_t st = 0, phase = 0, acc = 0, held_phase = 0;
+  int held_m = -1;
   auto step_on = [&](uint32_t& s, uint32_t& ph) {
     if (++s == T::STAGES) {
       s = 0;
@@ -351,8 +381,16 @@ __device__ bool gemm_multiply(GemmShared& sh, uint8_t* stages, Next next, int* e
     const int first = uniform(w.k0), last = uniform(w.k1);
     const uint32_t idesc = tc::idesc_bf16(kTM * CG, kTN, a_mn, b_mn);
     const uint32_t a_step = a_mn ? 128 : 2, b_step = b_mn ? 128 : 2;
+    const uint32_t ring = tc::smem_u32(stages) + T::HELD_BYTES;
     const uint64_t a0 = tc::sdesc(tc::smem_u32(stages), a_mn ? 8192 : 16, 1024);
-    const uint64_t b0 = tc::sdesc(tc::smem_u32(stages) + T::A_BYTES, b_mn ? 8192 : 16, 1024);
+    const uint64_t b0 = tc::sdesc(T::HOLD ? ring : ring + T::A_BYTES, b_mn ? 8192 : 16, 1024);
+    if (T::HOLD && uniform(w.m) != held_m) {
+      if (held_m >= 0 && elect_one()) gemm_commit<CG>(tc::smem_u32(&sh.unheld));
+      __syncwarp();
+      held_m = uniform(w.m);
+      if (!wait(tc::smem_u32(&sh.held), held_phase)) return false;
+      held_phase ^= 1;
+    }
     const int step = T::ACC ? T::CHAIN : last - first;
     for (int k0 = first; k0 < last; k0 += step, ++acc) {
       const uint32_t buf = acc & 1;
@@ -361,7 +399,8 @@ __device__ bool gemm_multiply(GemmShared& sh, uint8_t* stages, Next next, int* e
       uint32_t more = 0;
       // by the issuing lane
       auto product = [&](uint32_t ia, uint32_t ib) {
-        const uint64_t da = a0 + ia * (T::STAGE >> 4), db = b0 + ib * (T::STAGE >> 4);
+        const uint64_t da = a0 + ia * ((T::HOLD ? T::A_BYTES : T::STAGE) >> 4);
+        const uint64_t db = b0 + ib * (T::STAGE >> 4);
 #pragma unroll
         for (int j = 0; j < kTK / 16; ++j)
           gemm_mma<CG>(d, da + j * a_step, db + j * b_step, idesc, j == 0 ? more : 1u);
@@ -389,7 +428,7 @@ __device__ bool gemm_multiply(GemmShared& sh, uint8_t* stages, Next next, int* e
             product(s[1], s[0]);
             done(s[1]);
           }
-          product(s[0], s[0]);
+          product(T::HOLD ? k - first : s[0], s[0]);
           done(s[0]);
         }
         more = 1;

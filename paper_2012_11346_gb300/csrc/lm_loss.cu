@@ -13,9 +13,10 @@
 // launch with both products, dx += g w and dw = g^T x.
 //
 // What bounds them, on GB300 (kernel times; peak = 1978 TFLOP/s bf16):
-//   statistics  16384 x 512 x 50021 bf16  430-445 us, 1.9 PFLOP/s: the tensor
-//               pipe; 8192 x 768 x 10000 fp32 359 us, 2.1 P plane products/s.
-//   softmax     32768 x 512 x 32768 bf16  740 us (580 without g's stores).
+//   statistics  16384 x 512 x 50021 bf16  400 us, 2.1 PFLOP/s: the tensor pipe;
+//               8192 x 768 x 10000 fp32   359 us, 2.1 PFLOP/s of plane products.
+//   softmax     32768 x 512 x 32768 bf16  685 us: g's stores share L1 with the
+//               MMAs' operands (the statistics of the same tiles: 528 us).
 //   products    the same sizes            1296 us, 1.7 PFLOP/s at 1.7 GHz: power.
 // The logits are computed twice because a row's statistics are not known until
 // its last word; keeping them would be N x V, the thing to avoid.
@@ -312,13 +313,17 @@ __device__ __forceinline__ RunNext run_of(const Product& p) {
 }
 
 // A bf16 logit over more than 512 features is summed in chains: its loss shows
-// in the fp32 results otherwise (2e-6 of a logit at 2048).
-template <int NP, int CG, bool JOIN> using StatTile = Tile<NP, CG, JOIN>;
+// in the fp32 results otherwise (2e-6 of a logit at 2048).  Up to 512 features a
+// worker can hold its rows of x while it walks along the vocabulary: 16384 x 512 x
+// 50021 statistics 424 -> 400 us, the softmax kernel of 32768 x 512 x 32768 735 ->
+// 685 us.
+// Changing rows then drains the MMAs, so it has to be for a walk of some tiles.
+bool hold_rows(const Product& p) { return p.kb <= kHeld && p.tn >= 8; }
 
-template <int NP, int CG, bool JOIN>
+template <int NP, int CG, bool JOIN, bool HOLD>
 __global__ void __launch_bounds__(kGemmThreads, 1)
     k_loss_stats(const __grid_constant__ StatJob job) {
-  using T = StatTile<NP, CG, JOIN>;
+  using T = Tile<NP, CG, JOIN, HOLD>;
   __shared__ GemmShared sh;
   if (job.first) {
     if (blockIdx.x == 0 && threadIdx.x < 8) job.err[threadIdx.x] = 0;
@@ -330,10 +335,10 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
   if (threadIdx.x >= 128) epi.flush();
 }
 
-template <int NP, int CG>
+template <int NP, int CG, bool HOLD>
 __global__ void __launch_bounds__(kGemmThreads, 1)
     k_loss_softmax(const __grid_constant__ SoftJob job) {
-  using T = Tile<NP, CG>;
+  using T = Tile<NP, CG, (NP > 1), HOLD>;
   __shared__ GemmShared sh;
   SoftEpi<NP, CG> epi(job);
   gemm_roles<T>(sh, stage_memory<T>(), run_of<CG>(job.p), epi, job.err);
@@ -839,7 +844,7 @@ bool launch(void (*k)(Job), unsigned blocks, bool after, cudaStream_t s, const J
   return launch_on(k, blocks, kGemmThreads, smem, CG, after, s, job);
 }
 
-template <typename T>
+template <typename... T>
 bool* once() {
   static bool flags[kMaxDevices];
   return device_flag(flags);
@@ -876,12 +881,17 @@ slim_status fwd(const Sizes& z, const void* x, const void* w, const void* target
   {
     prof::Scope ps(prof::K_LOSS_STATS, s, 2.0 * z.N * z.D * z.V, ((double)z.N + z.V) * z.D * 2 * NP);
     const unsigned blocks = (unsigned)wk * CG;
-    const bool ok =
-        NP > 1 || j.p.kb > StatTile<NP, CG, true>::CHAIN
-            ? launch<StatTile<NP, CG, true>>(k_loss_stats<NP, CG, true>, blocks, !j.first, s, j,
-                                             once<StatTile<NP, CG, true>>())
-            : launch<StatTile<NP, CG, NP != 1>>(k_loss_stats<NP, CG, NP != 1>, blocks, !j.first, s, j,
-                                                once<StatTile<NP, CG, NP != 1>>());
+    auto go = [&](auto join, auto hold) {
+      using T = Tile<NP, CG, decltype(join)::value, decltype(hold)::value>;
+      return launch<T>(k_loss_stats<NP, CG, T::ACC, T::HOLD>, blocks, !j.first, s, j,
+                       once<StatEpi<NP, CG>, T>());
+    };
+    using Yes = std::true_type;
+    using No = std::integral_constant<bool, (NP > 1)>;  // three planes: always in chains
+    using Hold = std::integral_constant<bool, NP == 1>;
+    const bool ok = j.p.kb > Tile<1, CG>::CHAIN ? go(Yes(), std::false_type())
+                    : hold_rows(j.p)            ? go(No(), Hold())
+                                                : go(No(), std::false_type());
     if (!ok) return SLIM_ERR_CUDA;
   }
   JoinJob q{};
@@ -960,9 +970,13 @@ slim_status bwd(const Sizes& z, const void* x, const void* w, const void* target
     {
       const long long wk = tiles < workers(CG) ? tiles : workers(CG);
       prof::Scope sc(prof::K_LOSS_SOFTMAX, s, fl, ((double)z.N + n) * z.D * 2 * NP + gb);
-      if (!launch<Tile<NP, CG>>(k_loss_softmax<NP, CG>, (unsigned)wk * CG, true, s, j,
-                                    once<SoftEpi<NP, CG>>()))
-        return SLIM_ERR_CUDA;
+      auto go = [&](auto hold) {
+        using T = Tile<NP, CG, (NP > 1), decltype(hold)::value>;
+        return launch<T>(k_loss_softmax<NP, CG, T::HOLD>, (unsigned)wk * CG, true, s, j,
+                         once<SoftEpi<NP, CG>, T>());
+      };
+      using Hold = std::integral_constant<bool, NP == 1>;
+      if (!(hold_rows(j.p) ? go(Hold()) : go(std::false_type()))) return SLIM_ERR_CUDA;
     }
     q.acc = ws.acc;
     q.acc_ld = acc_ld(z.D);
