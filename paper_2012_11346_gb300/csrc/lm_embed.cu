@@ -552,8 +552,8 @@ bool aligned(const void* p, size_t to) {
   return p != nullptr && (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0;
 }
 
-// Longest list that one block sorts alone: 13 us for 1000 ids in two passes, 33
-// for 4096, which four launches sort in about 15.
+// Longest list that one block sorts alone: 9 us for 1000 ids in two passes; at 4096
+// ids four launches are 8 us faster.
 constexpr long long kOneBlock = 1024;
 
 struct Plan {
