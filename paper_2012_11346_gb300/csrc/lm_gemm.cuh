@@ -2,8 +2,8 @@
 // of a persistent, warp-specialised kernel that computes D = A B^T tiles with
 // an epilogue of its caller's.
 //
-// A block (or a pair of blocks, CG = 2, on one tile of twice the height) runs
-// three roles side by side: one thread copies operand tiles into a ring of
+// A pair of blocks works on a tile, each on half of its rows, and runs three roles
+// side by side: one thread copies operand tiles into a ring of
 // shared-memory stages by TMA, one thread issues the MMAs on them, and eight
 // warps read finished accumulators from TMEM and run the epilogue.  Two
 // accumulators alternate, so a tile's epilogue runs under the next tile's MMAs.
@@ -15,8 +15,9 @@
 //
 // The tensor core cuts off the last bits at every step of a sum: measured, a
 // sum of 512 bf16 products comes out low by 4e-7 of itself and one of 2048 by
-// 1.7e-6 (9e-7 and 5.7e-6 where all have one sign).  ACC: a sum is cut into chains that the epilogue's
-// registers join in fp32, where that loss would show in an fp32 result.
+// 1.7e-6 (9e-7 and 5.7e-6 where all have one sign).  ACC: a sum is cut into
+// chains that the epilogue's registers join in fp32, where that loss would show in
+// an fp32 result.
 #pragma once
 #include "common.cuh"
 #include "tc_common.cuh"
@@ -24,7 +25,8 @@
 namespace slim {
 namespace lm {
 
-constexpr int kTM = 128;           // rows of a block's tile
+constexpr int kPair = 2;           // blocks of a tile
+constexpr int kTM = 128;           // rows of a block's half of a tile
 constexpr int kTN = 256;           // columns of a tile
 constexpr int kTK = 64;            // reduction per stage
 constexpr int kEpiWarps = 16;      // four per quarter of the rows, 64 columns each
@@ -36,12 +38,12 @@ constexpr int kSmemBytes = 227 * 1024 - 1024 - 512;  // after alignment and barr
 // shared memory while it stays with the same tile row, and the ring carries B
 // alone.  Worth it where a worker walks along many columns.
 constexpr int kHeld = 8;
-template <int NP, int CG, bool JOIN = (NP > 1), bool HOLD_A = false>
+template <int NP, bool JOIN = (NP > 1), bool HOLD_A = false>
 struct Tile {
-  static constexpr int PLANES = NP, GROUP = CG;
+  static constexpr int PLANES = NP;
   static constexpr bool ACC = JOIN, HOLD = HOLD_A;
   static_assert(!HOLD || NP == 1, "one plane");
-  static constexpr int BROWS = kTN / CG;    // rows of B that a block holds
+  static constexpr int BROWS = kTN / kPair;    // rows of B that a block holds
   static constexpr int A_BYTES = kTM * kTK * 2, B_BYTES = BROWS * kTK * 2;
   static constexpr int HELD_BYTES = HOLD ? kHeld * A_BYTES : 0;
   static constexpr int STAGE = HOLD ? B_BYTES : A_BYTES + B_BYTES;  // one plane of either operand
@@ -59,7 +61,7 @@ struct Product {
   CUtensorMap a, b;
   int a_mn, b_mn;  // operand layouts: 0 K-major, 1 MN-major
   int M, N;
-  int tm, tn;      // tiles each way (tm in tiles of kTM * CG rows)
+  int tm, tn;      // tiles each way (tm in tiles of kTM * kPair rows)
   int kb;          // stages (of kTK) of the reduction
   int splits;      // parts of the reduction, computed as tiles of their own
 };
@@ -127,11 +129,7 @@ __device__ __forceinline__ void cluster_sync() {
   asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
   asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
-template <int CG>
 __device__ __forceinline__ void arrive_at_leader(uint32_t bar) {
-  if (CG == 1)
-    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
-  else
     // what it hands over is TMEM, read by completed tcgen05.ld: nothing in memory
     // has to be made visible to the other block (a release at cluster scope
     // waits for the warp's earlier stores, 0.5 us a tile)
@@ -139,78 +137,49 @@ __device__ __forceinline__ void arrive_at_leader(uint32_t bar) {
                  : "memory");
 }
 
-// ------------------------------------------------------------------ CG forms
-template <int CG>
+// ------------------------------------------------------------------ pair forms
 __device__ __forceinline__ void gemm_tmem_alloc(uint32_t dst, uint32_t cols) {
-  if (CG == 1) {
-    tc::tmem_alloc(dst, cols);
-  } else {
-    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(dst),
-                 "r"(cols)
-                 : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
-  }
+  asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(dst),
+               "r"(cols)
+               : "memory");
+  asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
 }
-template <int CG>
 __device__ __forceinline__ void gemm_tmem_free(uint32_t t, uint32_t cols) {
-  if (CG == 1)
-    tc::tmem_dealloc(t, cols);
-  else
-    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(t), "r"(cols)
-                 : "memory");
+  asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(t), "r"(cols)
+               : "memory");
 }
-template <int CG>
 __device__ __forceinline__ void gemm_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc,
                                          uint32_t acc) {
-  if (CG == 1) {
-    tc::mma(d, a, b, idesc, acc);
-  } else {
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "setp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
-        "l"(a), "l"(b), "r"(idesc), "r"(acc)
-        : "memory");
-  }
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+      "l"(a), "l"(b), "r"(idesc), "r"(acc)
+      : "memory");
 }
-// Arrives on the mbarrier (of both blocks of a pair) once this thread's MMAs
-// so far are done.
-template <int CG>
+// Arrives on the mbarrier of both blocks once this thread's MMAs so far are done.
 __device__ __forceinline__ void gemm_commit(uint32_t bar) {
-  if (CG == 1) {
-    tc::mma_commit(bar);
-  } else {
-    asm volatile(
-        "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 "
-        "[%0], %1;" ::"r"(bar),
-        "h"((uint16_t)3)
-        : "memory");
-  }
+  asm volatile(
+      "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 "
+      "[%0], %1;" ::"r"(bar),
+      "h"((uint16_t)3)
+      : "memory");
 }
 // One box of a tensor map to shared memory; x is a multiple of 64 elements
-// (128 bytes).  With CG = 2 the bytes are counted on the leader's barrier.
-template <int CG>
+// (128 bytes).  The bytes are counted on the leading block's barrier.
 __device__ __forceinline__ void gemm_tma(uint32_t dst, const CUtensorMap* map, int x, int y, int z,
                                          uint32_t bar) {
-  if (CG == 1)
-    asm volatile(
-        "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes "
-        "[%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
-        "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(bar)
-        : "memory");
-  else
-    asm volatile(
-        "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes "
-        "[%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
-        "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(bar)
-        : "memory");
+  asm volatile(
+      "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes "
+      "[%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(bar)
+      : "memory");
 }
 
 // ------------------------------------------------------------------ roles
 // Sets the ring up and allocates TMEM; every thread of the block (of the pair).
 template <typename T>
 __device__ __forceinline__ void gemm_begin(GemmShared& sh) {
-  constexpr int CG = T::GROUP;
   if (threadIdx.x == 0) {
     for (int i = 0; i < T::STAGES; ++i) {
       tc::mbar_init(tc::smem_u32(&sh.full[i]), 1);
@@ -220,31 +189,24 @@ __device__ __forceinline__ void gemm_begin(GemmShared& sh) {
     tc::mbar_init(tc::smem_u32(&sh.unheld), 1);
     for (int i = 0; i < 2; ++i) {
       tc::mbar_init(tc::smem_u32(&sh.tfull[i]), 1);
-      tc::mbar_init(tc::smem_u32(&sh.tempty[i]), kEpiWarps * CG);
+      tc::mbar_init(tc::smem_u32(&sh.tempty[i]), kEpiWarps * kPair);
     }
     tc::mbar_fence_init();
   }
-  if (threadIdx.x / 32 == 2) gemm_tmem_alloc<CG>(tc::smem_u32(&sh.tmem), 2 * kTN);
+  if (threadIdx.x / 32 == 2) gemm_tmem_alloc(tc::smem_u32(&sh.tmem), 2 * kTN);
   tc::tc_fence_before();
-  if (CG == 1)
-    __syncthreads();
-  else
-    cluster_sync();
+  cluster_sync();
   tc::tc_fence_after();
 }
 
 template <typename T>
 __device__ __forceinline__ void gemm_end(GemmShared& sh, bool failed) {
-  constexpr int CG = T::GROUP;
   // a role that gave up may leave copies in flight: let them land
   if (failed)
     for (int i = 0; i < 1000; ++i) __nanosleep(10000);
   tc::tc_fence_before();
-  if (CG == 1)
-    __syncthreads();
-  else
-    cluster_sync();
-  if (threadIdx.x / 32 == 2) gemm_tmem_free<CG>(sh.tmem, 2 * kTN);
+  cluster_sync();
+  if (threadIdx.x / 32 == 2) gemm_tmem_free(sh.tmem, 2 * kTN);
 }
 
 // One lane of a converged warp, the same every time.  ptxas knows that a branch
@@ -277,10 +239,10 @@ __device__ __forceinline__ const CUtensorMap* uniform(const CUtensorMap* x) {
 // gave up.
 template <typename T, typename Next>
 __device__ bool gemm_copy(GemmShared& sh, uint8_t* stages, Next next, int* err) {
-  constexpr int NP = T::PLANES, CG = T::GROUP;
-  const int rank = CG == 1 ? 0 : uniform((int)cluster_rank());
+  constexpr int NP = T::PLANES;
+  const int rank = uniform((int)cluster_rank());
   const uint32_t full0 = tc::smem_u32(&sh.full[0]), empty0 = tc::smem_u32(&sh.empty[0]);
-  const uint32_t count0 = CG == 2 ? map_to_rank(full0, 0) : full0;  // the leader's
+  const uint32_t count0 = map_to_rank(full0, 0);  // the leading block's
   const uint32_t smem = tc::smem_u32(stages);
   uint32_t st = 0, phase = 1, held_phase = 0;
   int held_row = -1;
@@ -298,7 +260,7 @@ __device__ bool gemm_copy(GemmShared& sh, uint8_t* stages, Next next, int* err) 
     const CUtensorMap* map_a = uniform(&w.p->a);
     const CUtensorMap* map_b = uniform(&w.p->b);
     const int a_mn = uniform(w.p->a_mn), b_mn = uniform(w.p->b_mn);
-    const int row = uniform((w.m * CG + rank) * kTM), col = uniform(w.n * kTN + rank * T::BROWS);
+    const int row = uniform((w.m * kPair + rank) * kTM), col = uniform(w.n * kTN + rank * T::BROWS);
     const int k0 = uniform(w.k0) * kTK, k1 = uniform(w.k1) * kTK;
     if (T::HOLD && row != held_row) {
       if (held_row >= 0) {
@@ -309,10 +271,10 @@ __device__ bool gemm_copy(GemmShared& sh, uint8_t* stages, Next next, int* err) 
       held_row = row;
       if (elect_one()) {
         const uint32_t held = tc::smem_u32(&sh.held);
-        if (rank == 0) tc::mbar_expect_tx(held, CG * (k1 - k0) / kTK * T::A_BYTES);
-        const uint32_t bar = CG == 2 ? map_to_rank(held, 0) : held;
+        if (rank == 0) tc::mbar_expect_tx(held, kPair * (k1 - k0) / kTK * T::A_BYTES);
+        const uint32_t bar = map_to_rank(held, 0);
         for (int k = k0; k < k1; k += kTK)
-          gemm_tma<CG>(smem + (k - k0) / kTK * T::A_BYTES, map_a, k, row, 0, bar);
+          gemm_tma(smem + (k - k0) / kTK * T::A_BYTES, map_a, k, row, 0, bar);
       }
       __syncwarp();
     }
@@ -321,7 +283,7 @@ __device__ bool gemm_copy(GemmShared& sh, uint8_t* stages, Next next, int* err) 
       for (int q = 0; q < NP; ++q) {
         if (!free()) return false;
         if (elect_one()) {
-          if (rank == 0) tc::mbar_expect_tx(full0 + 8 * st, CG * T::STAGE);
+          if (rank == 0) tc::mbar_expect_tx(full0 + 8 * st, kPair * T::STAGE);
           const uint32_t full = count0 + 8 * st;
           const uint32_t sa = smem + T::HELD_BYTES + st * T::STAGE;
           const uint32_t sb = T::HOLD ? sa : sa + T::A_BYTES;
@@ -330,16 +292,16 @@ __device__ bool gemm_copy(GemmShared& sh, uint8_t* stages, Next next, int* err) 
           } else if (a_mn) {
 #pragma unroll
             for (int j = 0; j < kTM / 64; ++j)
-              gemm_tma<CG>(sa + j * 8192, map_a, row + 64 * j, k, q, full);
+              gemm_tma(sa + j * 8192, map_a, row + 64 * j, k, q, full);
           } else {
-            gemm_tma<CG>(sa, map_a, k, row, q, full);
+            gemm_tma(sa, map_a, k, row, q, full);
           }
           if (b_mn) {
 #pragma unroll
             for (int j = 0; j < T::BROWS / 64; ++j)
-              gemm_tma<CG>(sb + j * 8192, map_b, col + 64 * j, k, q, full);
+              gemm_tma(sb + j * 8192, map_b, col + 64 * j, k, q, full);
           } else {
-            gemm_tma<CG>(sb, map_b, k, col, q, full);
+            gemm_tma(sb, map_b, k, col, q, full);
           }
         }
         __syncwarp();
@@ -359,7 +321,6 @@ __device__ bool gemm_copy(GemmShared& sh, uint8_t* stages, Next next, int* err) 
 // the loop; one of them issues.
 template <typename T, typename Next>
 __device__ bool gemm_multiply(GemmShared& sh, uint8_t* stages, Next next, int* err) {
-  constexpr int CG = T::GROUP;
   Work w;
   const uint32_t full0 = tc::smem_u32(&sh.full[0]), empty0 = tc::smem_u32(&sh.empty[0]);
   const uint32_t tmem = sh.tmem;
@@ -379,13 +340,13 @@ __device__ bool gemm_multiply(GemmShared& sh, uint8_t* stages, Next next, int* e
   while (next(w)) {
     const int a_mn = uniform(w.p->a_mn), b_mn = uniform(w.p->b_mn);
     const int first = uniform(w.k0), last = uniform(w.k1);
-    const uint32_t idesc = tc::idesc_bf16(kTM * CG, kTN, a_mn, b_mn);
+    const uint32_t idesc = tc::idesc_bf16(kTM * kPair, kTN, a_mn, b_mn);
     const uint32_t a_step = a_mn ? 128 : 2, b_step = b_mn ? 128 : 2;
     const uint32_t ring = tc::smem_u32(stages) + T::HELD_BYTES;
     const uint64_t a0 = tc::sdesc(tc::smem_u32(stages), a_mn ? 8192 : 16, 1024);
     const uint64_t b0 = tc::sdesc(T::HOLD ? ring : ring + T::A_BYTES, b_mn ? 8192 : 16, 1024);
     if (T::HOLD && uniform(w.m) != held_m) {
-      if (held_m >= 0 && elect_one()) gemm_commit<CG>(tc::smem_u32(&sh.unheld));
+      if (held_m >= 0 && elect_one()) gemm_commit(tc::smem_u32(&sh.unheld));
       __syncwarp();
       held_m = uniform(w.m);
       if (!wait(tc::smem_u32(&sh.held), held_phase)) return false;
@@ -403,9 +364,9 @@ __device__ bool gemm_multiply(GemmShared& sh, uint8_t* stages, Next next, int* e
         const uint64_t db = b0 + ib * (T::STAGE >> 4);
 #pragma unroll
         for (int j = 0; j < kTK / 16; ++j)
-          gemm_mma<CG>(d, da + j * a_step, db + j * b_step, idesc, j == 0 ? more : 1u);
+          gemm_mma(d, da + j * a_step, db + j * b_step, idesc, j == 0 ? more : 1u);
       };
-      auto done = [&](uint32_t i) { gemm_commit<CG>(empty0 + 8 * i); };
+      auto done = [&](uint32_t i) { gemm_commit(empty0 + 8 * i); };
       const int k1 = min(k0 + step, last);
       for (int k = k0; k < k1; ++k) {
         uint32_t s[3];
@@ -434,7 +395,7 @@ __device__ bool gemm_multiply(GemmShared& sh, uint8_t* stages, Next next, int* e
         more = 1;
         __syncwarp();
       }
-      if (elect_one()) gemm_commit<CG>(tc::smem_u32(&sh.tfull[buf]));
+      if (elect_one()) gemm_commit(tc::smem_u32(&sh.tfull[buf]));
       __syncwarp();
     }
   }
@@ -443,19 +404,18 @@ __device__ bool gemm_multiply(GemmShared& sh, uint8_t* stages, Next next, int* e
 
 // An epilogue warp.  For every tile, epi.begin(work, row, col0) once, then
 // epi.chunk(c, v) for each 32 columns col0 + c .. of row `row` (of this thread)
-// that begin inside the product (v is the epilogue's to change).  Reads past the product's rows still run (their
-// values are zero sums); the epilogue drops them.
+// that begin inside the product (v is the epilogue's to change).  Reads past the
+// product's rows still run (their values are zero sums); the epilogue drops them.
 template <typename T, typename Next, typename Epi>
 __device__ bool gemm_finish(GemmShared& sh, Next next, Epi& epi, int* err) {
-  constexpr int CG = T::GROUP;
-  const uint32_t rank = CG == 1 ? 0 : cluster_rank();
+  const uint32_t rank = cluster_rank();
   const int warp = threadIdx.x / 32 - 4, lane = threadIdx.x & 31;
   const int quarter = warp & 3, part = warp >> 2;
   Work w;
   uint32_t acc = 0;
   while (next(w)) {
     const Product* p = w.p;
-    const int row = (w.m * CG + (int)rank) * kTM + quarter * 32 + lane;
+    const int row = (w.m * kPair + (int)rank) * kTM + quarter * 32 + lane;
     const int col = w.n * kTN + part * kEpiCols;
     const int step = T::ACC ? T::CHAIN : w.k1 - w.k0;
     float sum[T::ACC ? kEpiCols : 1];
@@ -490,7 +450,7 @@ __device__ bool gemm_finish(GemmShared& sh, Next next, Epi& epi, int* err) {
       }
       tc::tc_fence_before();
       __syncwarp();
-      if (lane == 0) arrive_at_leader<CG>(tc::smem_u32(&sh.tempty[buf]));
+      if (lane == 0) arrive_at_leader(tc::smem_u32(&sh.tempty[buf]));
     }
     if (T::ACC) {
 #pragma unroll
@@ -517,7 +477,7 @@ __device__ __forceinline__ void gemm_roles(GemmShared& sh, uint8_t* stages, cons
     if (T::ACC) asm volatile("setmaxnreg.dec.sync.aligned.u32 32;");
     if (warp == 0)
       ok = gemm_copy<T>(sh, stages, next, err);
-    else if (warp == 1 && (T::GROUP == 1 || cluster_rank() == 0))
+    else if (warp == 1 && (cluster_rank() == 0))
       ok = gemm_multiply<T>(sh, stages, next, err);
   } else {
     if (T::ACC) asm volatile("setmaxnreg.inc.sync.aligned.u32 112;");

@@ -155,7 +155,7 @@ struct StatJob {
 // sum_v 2^(z_v log2 e - base), base the largest exponent so far.  The base is
 // kept as it was used, in units of log2, so that it means the same to every
 // term and to the join.
-template <int NP, int CG>
+template <int NP>
 struct StatEpi {
   const StatJob& j;
   long long worker, workers;
@@ -171,7 +171,7 @@ struct StatEpi {
       base = -INFINITY;
       sum = 0.0f;
       row = r;
-      slot_row = r - w.m * kTM * CG;
+      slot_row = r - w.m * kTM * kPair;
       target = -1;
       if (r < w.p->M) {
         const long long t = load_target(j.targets, j.i64, r);
@@ -214,7 +214,7 @@ struct StatEpi {
     const long long tiles = (long long)j.p.tm * j.p.tn;
     const int slot = (int)(worker - run_owner((long long)m_now * j.p.tn, tiles, workers)) * 4 +
                      (threadIdx.x / 32 - 4) / 4;
-    j.part[((size_t)m_now * j.slots + slot) * (kTM * CG) + slot_row] = make_float2(base, sum);
+    j.part[((size_t)m_now * j.slots + slot) * (kTM * kPair) + slot_row] = make_float2(base, sum);
   }
 };
 
@@ -236,7 +236,7 @@ struct SoftJob {
 // rows share is left to the products' epilogues: rounded into g it would put the
 // same error on every row, and without it a target with little weight is -1
 // exactly.
-template <int NP, int CG>
+template <int NP>
 struct SoftEpi {
   const SoftJob& j;
   int row = 0, col = 0, target = -1;
@@ -305,9 +305,9 @@ __device__ __forceinline__ uint8_t* stage_memory() {
   return reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
                                     ~uintptr_t(1023));
 }
-template <int CG>
 __device__ __forceinline__ RunNext run_of(const Product& p) {
-  const long long tiles = (long long)p.tm * p.tn, worker = blockIdx.x / CG, workers = gridDim.x / CG;
+  const long long tiles = (long long)p.tm * p.tn;
+  const long long worker = blockIdx.x / kPair, workers = gridDim.x / kPair;
   return RunNext{
       TileRange(&p, run_begin(worker, tiles, workers), run_begin(worker + 1, tiles, workers))};
 }
@@ -320,28 +320,28 @@ __device__ __forceinline__ RunNext run_of(const Product& p) {
 // Changing rows then drains the MMAs, so it has to be for a walk of some tiles.
 bool hold_rows(const Product& p) { return p.kb <= kHeld && p.tn >= 8; }
 
-template <int NP, int CG, bool JOIN, bool HOLD>
+template <int NP, bool JOIN, bool HOLD>
 __global__ void __launch_bounds__(kGemmThreads, 1)
     k_loss_stats(const __grid_constant__ StatJob job) {
-  using T = Tile<NP, CG, JOIN, HOLD>;
+  using T = Tile<NP, JOIN, HOLD>;
   __shared__ GemmShared sh;
   if (job.first) {
     if (blockIdx.x == 0 && threadIdx.x < 8) job.err[threadIdx.x] = 0;
     __syncthreads();
     if (blockIdx.x == 0 && threadIdx.x == 0) tc::set_report(job.err, job.rep);
   }
-  StatEpi<NP, CG> epi(job, blockIdx.x / CG, gridDim.x / CG);
-  gemm_roles<T>(sh, stage_memory<T>(), run_of<CG>(job.p), epi, job.err);
+  StatEpi<NP> epi(job, blockIdx.x / kPair, gridDim.x / kPair);
+  gemm_roles<T>(sh, stage_memory<T>(), run_of(job.p), epi, job.err);
   if (threadIdx.x >= 128) epi.flush();
 }
 
-template <int NP, int CG, bool HOLD>
+template <int NP, bool HOLD>
 __global__ void __launch_bounds__(kGemmThreads, 1)
     k_loss_softmax(const __grid_constant__ SoftJob job) {
-  using T = Tile<NP, CG, (NP > 1), HOLD>;
+  using T = Tile<NP, (NP > 1), HOLD>;
   __shared__ GemmShared sh;
-  SoftEpi<NP, CG> epi(job);
-  gemm_roles<T>(sh, stage_memory<T>(), run_of<CG>(job.p), epi, job.err);
+  SoftEpi<NP> epi(job);
+  gemm_roles<T>(sh, stage_memory<T>(), run_of(job.p), epi, job.err);
 }
 
 // ------------------------------------------------------------------ join
@@ -481,7 +481,7 @@ __device__ __forceinline__ float grad_scale(const GradJob& j) {
   return s;
 }
 
-template <int NP, int CG>
+template <int NP>
 struct GradEpi {
   using T = typename std::conditional<NP == 1, __nv_bfloat16, float>::type;
   const GradJob& j;
@@ -555,15 +555,15 @@ struct GradEpi {
   }
 };
 
-template <int NP, int CG>
+template <int NP>
 __global__ void __launch_bounds__(kGemmThreads, 1)
     k_loss_grad(const __grid_constant__ GradJob job) {
-  using T = Tile<NP, CG>;
+  using T = Tile<NP>;
   __shared__ GemmShared sh;
-  const int w = blockIdx.x / CG;
+  const int w = blockIdx.x / kPair;
   const DealNext next{TileRange(&job.p[0], job.deal.lo[0][w], job.deal.lo[0][w + 1]),
                       TileRange(&job.p[1], job.deal.lo[1][w], job.deal.lo[1][w + 1])};
-  GradEpi<NP, CG> epi(job);
+  GradEpi<NP> epi(job);
   gemm_roles<T>(sh, stage_memory<T>(), next, epi, job.err);
 }
 
@@ -655,12 +655,10 @@ int sm_count() {
 }
 
 // Workspace sizes do not depend on the device: they are for kMaxWorkers blocks.
-int workers(int cg) {
+int workers() {  // pairs
   const int n = sm_count() < kMaxWorkers ? sm_count() : kMaxWorkers;
-  return n / cg;
+  return n / kPair;
 }
-
-constexpr int CGv = 2;
 
 int cdiv(long long a, long long b) { return (int)((a + b - 1) / b); }
 
@@ -705,7 +703,7 @@ int acc_ld(int D) { return (D + 31) / 32 * 32; }
 // Splits of dw and dx for a piece of n words.
 void grad_splits(const Sizes& z, long long n, int w, int splits[2]) {
   const long long tn = cdiv(z.D, kTN);
-  const long long tiles[2] = {cdiv(n, kTM * CGv) * tn, cdiv(z.N, kTM * CGv) * tn};
+  const long long tiles[2] = {cdiv(n, kTM * kPair) * tn, cdiv(z.N, kTM * kPair) * tn};
   const long long kb[2] = {cdiv(z.N, kTK), cdiv(n, kTK)};
   split_long(tiles, kb, z.np(), w, splits);
 }
@@ -717,9 +715,9 @@ Ws carve(Carver& cv, const Sizes& z, int piece, bool bwd) {
   if (z.stage_x(bwd)) w.x = cv.take<__nv_bfloat16>((size_t)np * z.N * z.ld());
   if (z.stage_w()) w.w = cv.take<__nv_bfloat16>((size_t)np * z.V * z.ld());
   if (!bwd) {
-    const int rows = kTM * CGv;
+    const int rows = kTM * kPair;
     const long long tm = cdiv(z.N, rows), tn = cdiv(z.V, kTN);
-    w.part = cv.take<float2>((size_t)tm * stat_slots(tm, tn, kMaxWorkers / CGv) * rows);
+    w.part = cv.take<float2>((size_t)tm * stat_slots(tm, tn, kMaxWorkers / kPair) * rows);
     w.zt = cv.take<float>(z.N);
     w.block_sum = cv.take<float>(2 * (size_t)cdiv(z.N, 8));
   } else {
@@ -731,7 +729,7 @@ Ws carve(Carver& cv, const Sizes& z, int piece, bool bwd) {
     const int last = z.V - (z.V - 1) / p * p;
     for (int n : {z.V < p ? z.V : p, last}) {
       int splits[2];
-      grad_splits(z, n, workers(CGv), splits);
+      grad_splits(z, n, workers(), splits);
       for (int i = 0; i < 2; ++i) {
         const bool parts = splits[i] > 1 || !z.even_rows();
         const size_t k = parts ? (size_t)splits[i] * (i ? z.N : n) * acc_ld(z.D) : 0;
@@ -802,17 +800,17 @@ struct Planes {
   long long rows, cols, ld, plane;
 };
 
-template <int NP, int CG>
+template <int NP>
 bool make_product(Product* p, const Planes& a, bool a_mn, const Planes& b, bool b_mn, long long M,
                   long long N, long long K) {
   if (!plane_map(&p->a, a.p, a.rows, a.cols, a.ld, a.plane, NP, a_mn ? kTK : kTM) ||
-      !plane_map(&p->b, b.p, b.rows, b.cols, b.ld, b.plane, NP, b_mn ? kTK : kTN / CG))
+      !plane_map(&p->b, b.p, b.rows, b.cols, b.ld, b.plane, NP, b_mn ? kTK : kTN / kPair))
     return false;
   p->a_mn = a_mn;
   p->b_mn = b_mn;
   p->M = (int)M;
   p->N = (int)N;
-  p->tm = cdiv(M, kTM * CG);
+  p->tm = cdiv(M, kTM * kPair);
   p->tn = cdiv(N, kTN);
   p->kb = cdiv(K, kTK);
   p->splits = 1;
@@ -829,19 +827,18 @@ slim_status stage(StageJob j, cudaStream_t s) {
   return cudaGetLastError() == cudaSuccess ? SLIM_OK : SLIM_ERR_CUDA;
 }
 
-// Launches a kernel of the tile products on `blocks` blocks, in pairs for CG = 2.
+// Launches a kernel of the tile products on `blocks` blocks, in pairs.
 template <typename T, typename Job>
 bool launch(void (*k)(Job), unsigned blocks, bool after, cudaStream_t s, const Job& job,
             bool* ready) {
   constexpr size_t smem = T::smem();
-  constexpr int CG = T::GROUP;
   if (ready == nullptr || !*ready) {
     if (cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) !=
         cudaSuccess)
       return false;
     if (ready) *ready = true;
   }
-  return launch_on(k, blocks, kGemmThreads, smem, CG, after, s, job);
+  return launch_on(k, blocks, kGemmThreads, smem, kPair, after, s, job);
 }
 
 template <typename... T>
@@ -850,7 +847,7 @@ bool* once() {
   return device_flag(flags);
 }
 
-template <int NP, int CG>
+template <int NP>
 slim_status fwd(const Sizes& z, const void* x, const void* w, const void* targets, slim_index it,
                 long long ignore, float* loss, float* lse, float* total, const Ws& ws,
                 unsigned* rep, cudaStream_t s) {
@@ -858,7 +855,7 @@ slim_status fwd(const Sizes& z, const void* x, const void* w, const void* target
   const __nv_bfloat16* xp = ws.x ? ws.x : static_cast<const __nv_bfloat16*>(x);
   const __nv_bfloat16* wp = ws.w ? ws.w : static_cast<const __nv_bfloat16*>(w);
   StatJob j{};
-  if (!make_product<NP, CG>(&j.p, Planes{xp, z.N, z.D, ld, z.N * ld}, false,
+  if (!make_product<NP>(&j.p, Planes{xp, z.N, z.D, ld, z.N * ld}, false,
                             Planes{wp, z.V, z.D, ld, (long long)z.V * ld}, false, z.N, z.V, z.D))
     return SLIM_ERR_CUDA;
   if (ws.w) {
@@ -868,7 +865,7 @@ slim_status fwd(const Sizes& z, const void* x, const void* w, const void* target
   }
   j.first = ws.w == nullptr;
   const long long tiles = (long long)j.p.tm * j.p.tn;
-  const long long wk = tiles < workers(CG) ? tiles : workers(CG);
+  const long long wk = tiles < workers() ? tiles : workers();
   j.targets = targets;
   j.i64 = it == SLIM_I64;
   j.ignore = ignore;
@@ -880,16 +877,16 @@ slim_status fwd(const Sizes& z, const void* x, const void* w, const void* target
   j.rep = rep;
   {
     prof::Scope ps(prof::K_LOSS_STATS, s, 2.0 * z.N * z.D * z.V, ((double)z.N + z.V) * z.D * 2 * NP);
-    const unsigned blocks = (unsigned)wk * CG;
+    const unsigned blocks = (unsigned)wk * kPair;
     auto go = [&](auto join, auto hold) {
-      using T = Tile<NP, CG, decltype(join)::value, decltype(hold)::value>;
-      return launch<T>(k_loss_stats<NP, CG, T::ACC, T::HOLD>, blocks, !j.first, s, j,
-                       once<StatEpi<NP, CG>, T>());
+      using T = Tile<NP, decltype(join)::value, decltype(hold)::value>;
+      return launch<T>(k_loss_stats<NP, T::ACC, T::HOLD>, blocks, !j.first, s, j,
+                       once<StatEpi<NP>, T>());
     };
     using Yes = std::true_type;
     using No = std::integral_constant<bool, (NP > 1)>;  // three planes: always in chains
     using Hold = std::integral_constant<bool, NP == 1>;
-    const bool ok = j.p.kb > Tile<1, CG>::CHAIN ? go(Yes(), std::false_type())
+    const bool ok = j.p.kb > Tile<1>::CHAIN ? go(Yes(), std::false_type())
                     : hold_rows(j.p)            ? go(No(), Hold())
                                                 : go(No(), std::false_type());
     if (!ok) return SLIM_ERR_CUDA;
@@ -904,7 +901,7 @@ slim_status fwd(const Sizes& z, const void* x, const void* w, const void* target
   q.V = z.V;
   q.tn = j.p.tn;
   q.slots = j.slots;
-  q.tile_rows = kTM * CG;
+  q.tile_rows = kTM * kPair;
   q.tiles = tiles;
   q.workers = wk;
   // neighbouring threads take neighbouring rows (their statistics lie side by
@@ -922,7 +919,7 @@ slim_status fwd(const Sizes& z, const void* x, const void* w, const void* target
              : SLIM_ERR_CUDA;
 }
 
-template <int NP, int CG>
+template <int NP>
 slim_status bwd(const Sizes& z, const void* x, const void* w, const void* targets, slim_index it,
                 long long ignore, const float* lse, const float* dloss, int dstride,
                 const float* count, int piece, void* dx, void* dw, const Ws& ws, unsigned* rep,
@@ -943,9 +940,9 @@ slim_status bwd(const Sizes& z, const void* x, const void* w, const void* target
     const Planes gm{ws.g, z.N, n, ps, z.N * ps};
     SoftJob j{};
     GradJob q{};
-    if (!make_product<NP, CG>(&j.p, xm, false, wm, false, z.N, n, z.D) ||
-        !make_product<NP, CG>(&q.p[0], gm, true, xm, true, n, z.D, z.N) ||
-        !make_product<NP, CG>(&q.p[1], gm, false, wm, true, z.N, z.D, n))
+    if (!make_product<NP>(&j.p, xm, false, wm, false, z.N, n, z.D) ||
+        !make_product<NP>(&q.p[0], gm, true, xm, true, n, z.D, z.N) ||
+        !make_product<NP>(&q.p[1], gm, false, wm, true, z.N, z.D, n))
       return SLIM_ERR_CUDA;
     q.to[0] = static_cast<T*>(dw) + (size_t)v0 * z.D;
     q.to[1] = dx;
@@ -968,12 +965,12 @@ slim_status bwd(const Sizes& z, const void* x, const void* w, const void* target
     const double fl = 2.0 * z.N * z.D * n, gb = 2.0 * NP * z.N * n;
     const long long tiles = (long long)j.p.tm * j.p.tn;
     {
-      const long long wk = tiles < workers(CG) ? tiles : workers(CG);
+      const long long wk = tiles < workers() ? tiles : workers();
       prof::Scope sc(prof::K_LOSS_SOFTMAX, s, fl, ((double)z.N + n) * z.D * 2 * NP + gb);
       auto go = [&](auto hold) {
-        using T = Tile<NP, CG, (NP > 1), decltype(hold)::value>;
-        return launch<T>(k_loss_softmax<NP, CG, T::HOLD>, (unsigned)wk * CG, true, s, j,
-                         once<SoftEpi<NP, CG>, T>());
+        using T = Tile<NP, (NP > 1), decltype(hold)::value>;
+        return launch<T>(k_loss_softmax<NP, T::HOLD>, (unsigned)wk * kPair, true, s, j,
+                         once<SoftEpi<NP>, T>());
       };
       using Hold = std::integral_constant<bool, NP == 1>;
       if (!(hold_rows(j.p) ? go(Hold()) : go(std::false_type()))) return SLIM_ERR_CUDA;
@@ -983,7 +980,7 @@ slim_status bwd(const Sizes& z, const void* x, const void* w, const void* target
     q.first = i == 0;
     q.last = i == pieces - 1;
     int splits[2];
-    grad_splits(z, n, workers(CG), splits);
+    grad_splits(z, n, workers(), splits);
     q.parts[0] = splits[0] > 1 || !q.wide;
     q.parts[1] = splits[1] > 1 || (!q.wide && q.last);
     long long nt[2], cost[2];
@@ -993,11 +990,11 @@ slim_status bwd(const Sizes& z, const void* x, const void* w, const void* target
       nt[k] = (long long)q.p[k].tm * q.p[k].tn * splits[k];
       cost[k] = cdiv(q.p[k].kb, splits[k]);
     }
-    const int wk = (int)(nt[0] + nt[1] < workers(CG) ? nt[0] + nt[1] : workers(CG));
+    const int wk = (int)(nt[0] + nt[1] < workers() ? nt[0] + nt[1] : workers());
     deal_tiles(nt, cost, wk, &q.deal);
     prof::Scope sc(prof::K_LOSS_GRAD, s, 2 * fl, ((double)z.N + n) * z.D * 2 * NP + 2 * gb);
-    if (!launch<Tile<NP, CG>>(k_loss_grad<NP, CG>, (unsigned)wk * CG, true, s, q,
-                              once<GradEpi<NP, CG>>()))
+    if (!launch<Tile<NP>>(k_loss_grad<NP>, (unsigned)wk * kPair, true, s, q,
+                              once<GradEpi<NP>>()))
       return SLIM_ERR_CUDA;
     if (q.parts[0] || q.parts[1]) {
       const long long e = ((q.parts[0] ? n : 0) + (q.parts[1] ? z.N : 0)) * cdiv(z.D, 4);
@@ -1061,8 +1058,8 @@ extern "C" slim_status slim_vocab_loss_fwd(const void* x, const void* w, const v
   slim::Carver cv(workspace);
   const Ws ws = carve(cv, z, 1, false);
   if (dtype == SLIM_BF16)
-    return fwd<1, CGv>(z, x, w, targets, itype, ignore_index, loss, lse, total, ws, rep, s);
-  return fwd<3, CGv>(z, x, w, targets, itype, ignore_index, loss, lse, total, ws, rep, s);
+    return fwd<1>(z, x, w, targets, itype, ignore_index, loss, lse, total, ws, rep, s);
+  return fwd<3>(z, x, w, targets, itype, ignore_index, loss, lse, total, ws, rep, s);
 }
 
 extern "C" slim_status slim_vocab_loss_bwd(const void* x, const void* w, const void* targets,
@@ -1099,8 +1096,8 @@ extern "C" slim_status slim_vocab_loss_bwd(const void* x, const void* w, const v
   slim::Carver cv(workspace);
   const Ws ws = carve(cv, z, piece, true);
   if (dtype == SLIM_BF16)
-    return bwd<1, CGv>(z, x, w, targets, itype, ignore_index, lse, dloss, dloss_stride, count,
+    return bwd<1>(z, x, w, targets, itype, ignore_index, lse, dloss, dloss_stride, count,
                        piece, dx, dw, ws, rep, s);
-  return bwd<3, CGv>(z, x, w, targets, itype, ignore_index, lse, dloss, dloss_stride, count, piece,
+  return bwd<3>(z, x, w, targets, itype, ignore_index, lse, dloss, dloss_stride, count, piece,
                      dx, dw, ws, rep, s);
 }
