@@ -338,8 +338,10 @@ struct List {
   int n;
 };
 
-// Tensors [a, ..) of the list, as many as fit; returns the next one.  The chunks
-// begin where `by_dst` says.
+// Tensors [a, ..) of the list, as many as fit; returns the next one that is not
+// empty (or n): only a list without elements makes a launch without tensors, and
+// the launches that leave partial sums are those that the workspace counts.  The
+// chunks begin where `by_dst` says.
 template <int CAP>
 int fill(const List& l, int a, bool by_dst, Table<CAP>* tb, bool* in_place, double* bytes) {
   tb->n = 0;
@@ -362,6 +364,7 @@ int fill(const List& l, int a, bool by_dst, Table<CAP>* tb, bool* in_place, doub
     if (l.src[t] != l.dst[t]) *in_place = false;
     *bytes += (double)l.numel[t] * (half ? 2 : 4);
   }
+  while (t < l.n && l.numel[t] == 0) ++t;
   tb->start[tb->n] = (unsigned)chunks;
   return t;
 }

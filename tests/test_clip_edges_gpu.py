@@ -1,0 +1,43 @@
+"""Clipping by the global norm at the edges of its lists and of fp32's range.
+
+Tolerances as in test_clip_gpu.py: the norm within 67 * 2^-24 of the one in 64
+bits, an element within that, three roundings in fp32 and one to its type."""
+import math
+
+import pytest
+import torch
+
+from paper_2012_11346_gb300 import slim
+
+pytestmark = pytest.mark.gpu
+
+F32, BF16 = torch.float32, torch.bfloat16
+NORM_TOL = 67 * 2.0 ** -24
+
+
+def norm64(ts):
+    return math.sqrt(sum(float((t.double() ** 2).sum()) for t in ts))
+
+
+@pytest.mark.parametrize("live", [127, 128, 129, 1023, 1024, 1025])
+@pytest.mark.parametrize("lead,trail", [(0, 0), (0, 1), (3, 700), (1, 1100)])
+def test_empty_tensors_around_a_full_list(cuda_device, live, lead, trail):
+    """As many tensors as a launch holds, with empty ones around them, and enough
+    elements for every block to leave a partial sum: nothing is written past the
+    workspace, and every element is counted once."""
+    g = torch.Generator(device=cuda_device).manual_seed(live)
+    sizes = [0] * lead + [8192] * live + [0] * trail
+    grads = [torch.randn(n, generator=g, device=cuda_device) for n in sizes]
+    n = norm64(grads)
+    before = [t.clone() for t in grads]
+    need = slim.clip_workspace_size(len(grads))
+    held = torch.full((need + 65536,), 0xA5, dtype=torch.uint8, device=cuda_device)
+    launches = slim.launch_count()
+    norm = slim.clip_grad_norm(grads, 0.5 * n, workspace=held[:need])
+    assert slim.launch_count() - launches == 2 * (1 if live <= 128 else -(-live // 1024))
+    assert (held[need:] == 0xA5).all()
+    assert abs(norm.item() - n) <= NORM_TOL * n
+    tol = NORM_TOL + 5 * 2.0 ** -24
+    for a, b in zip(grads, before):
+        ref = b.double() * 0.5
+        assert ((a.double() - ref).abs() <= tol * ref.abs()).all()
