@@ -588,6 +588,28 @@ def clip_grad_norm(grads, max_norm, out=None, workspace=None, stream=None):
     return norm
 
 
+class _FirstDerivative(torch.autograd.Function):
+    """A gradient that the kernels computed, tied to what it depends on: its own
+    backward refuses."""
+
+    @staticmethod
+    def forward(ctx, grad, *depends):
+        return grad.clone()
+
+    @staticmethod
+    def backward(ctx, *_):
+        raise RuntimeError("libslim's calls can be differentiated only once")
+
+
+def _first_derivatives(grads, *depends):
+    """What a Function's backward returns.  The kernels leave no graph: under
+    create_graph, differentiating the gradients again would drop their terms
+    without a word, and is made an error instead."""
+    if not torch.is_grad_enabled() or not any(t.requires_grad for t in depends):
+        return grads
+    return tuple(_FirstDerivative.apply(g, *depends) for g in grads)
+
+
 class Embedding(torch.autograd.Function):
     @staticmethod
     def forward(ctx, ids, table, scale):
@@ -599,7 +621,8 @@ class Embedding(torch.autograd.Function):
     @staticmethod
     def backward(ctx, dout):
         (ids,) = ctx.saved_tensors
-        return None, embed_backward(ids, _ready(dout), ctx.V, ctx.scale), None
+        dtable = embed_backward(ids, _ready(dout), ctx.V, ctx.scale)
+        return None, *_first_derivatives((dtable,), dout), None
 
 
 def _ready(t):
@@ -610,7 +633,7 @@ def _ready(t):
 
 
 def embedding(ids, table, scale=1.0):
-    """Differentiable embed_forward (gradient with respect to the table)."""
+    """Differentiable embed_forward (gradient with respect to the table, once)."""
     return Embedding.apply(ids, table, scale)
 
 
@@ -699,10 +722,10 @@ def vocab_loss_backward(x, w, targets, lse, dloss, count=None, ignore_index=-100
 
 class VocabLoss(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, w, targets, reduction, ignore_index, piece):
-        x, w, targets = _ready(x), _ready(w), targets.contiguous()
+    def forward(ctx, x_in, w_in, targets, reduction, ignore_index, piece):
+        x, w, targets = _ready(x_in), _ready(w_in), targets.contiguous()
         loss, lse, total = vocab_loss_forward(x, w, targets, ignore_index)
-        ctx.save_for_backward(x, w, targets, lse, total)
+        ctx.save_for_backward(x_in, w_in, x, w, targets, lse, total)
         ctx.mean, ctx.ignore_index, ctx.piece = reduction == "mean", ignore_index, piece
         if reduction == "none":
             return loss
@@ -710,15 +733,15 @@ class VocabLoss(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, dloss):
-        x, w, targets, lse, total = ctx.saved_tensors
-        dx, dw = vocab_loss_backward(x, w, targets, lse, dloss.float().contiguous(),
-                                     count=total[1:] if ctx.mean else None,
-                                     ignore_index=ctx.ignore_index, piece=ctx.piece)
-        return dx, dw, None, None, None, None
+        x_in, w_in, x, w, targets, lse, total = ctx.saved_tensors
+        grads = vocab_loss_backward(x, w, targets, lse, dloss.float().contiguous(),
+                                    count=total[1:] if ctx.mean else None,
+                                    ignore_index=ctx.ignore_index, piece=ctx.piece)
+        return *_first_derivatives(grads, x_in, w_in, dloss), None, None, None, None
 
 
 def vocab_loss(x, w, targets, reduction="mean", ignore_index=-100, piece=None):
-    """Differentiable softmax cross entropy of x [..., D] against the words w
+    """Differentiable (once) softmax cross entropy of x [..., D] against the words w
     [V, D]; reduction "mean" (over the rows not ignored), "sum" or "none"."""
     _require(reduction in ("mean", "sum", "none"), "reduction must be 'mean', 'sum' or 'none'")
-    return VocabLoss.apply(x, w, targets, reduction, ignore_index, piece)
+    return VocabLoss.apply(_ready(x), _ready(w), targets, reduction, ignore_index, piece)
