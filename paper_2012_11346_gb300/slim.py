@@ -436,9 +436,32 @@ def tc_selftest(A, B, a_mn, b_mn):
     return D, err
 
 
+class _FirstDerivative(torch.autograd.Function):
+    """A gradient that the kernels computed, tied to what it depends on: its own
+    backward refuses."""
+
+    @staticmethod
+    def forward(ctx, grad, *depends):
+        return grad.clone()
+
+    @staticmethod
+    def backward(ctx, *_):
+        raise RuntimeError("libslim's calls can be differentiated only once")
+
+
+def _first_derivatives(grads, *depends):
+    """What a Function's backward returns.  The kernels leave no graph: under
+    create_graph, differentiating the gradients again would drop their terms
+    without a word, and is made an error instead."""
+    if not torch.is_grad_enabled() or not any(t.requires_grad for t in depends):
+        return grads
+    return tuple(_FirstDerivative.apply(g, *depends) for g in grads)
+
+
 class SlimAttention(torch.autograd.Function):
     """Causal linear attention with the SLiM forward/backward (state carried
-    across slices of C rows; backward by rollback, no stored activations)."""
+    across slices of C rows; backward by rollback, no stored activations).
+    Differentiable once."""
 
     @staticmethod
     def forward(ctx, q, k, v, omega, C, feature):
@@ -451,10 +474,9 @@ class SlimAttention(torch.autograd.Function):
     @staticmethod
     def backward(ctx, dout):
         q, k, v, omega, out, S, z, S_lo, z_lo = ctx.saved_tensors
-        dq, dk, dv, domega = backward(q.contiguous(), k.contiguous(), v.contiguous(),
-                                      omega.contiguous(), out, dout.contiguous(), S, z, ctx.C,
-                                      ctx.feature, S_lo=S_lo, z_lo=z_lo)
-        return dq, dk, dv, domega, None, None
+        grads = backward(q.contiguous(), k.contiguous(), v.contiguous(), omega.contiguous(), out,
+                         dout.contiguous(), S, z, ctx.C, ctx.feature, S_lo=S_lo, z_lo=z_lo)
+        return *_first_derivatives(grads, q, k, v, omega, dout), None, None
 
 
 def slim_attention(q, k, v, omega, C, feature="exp"):
@@ -586,28 +608,6 @@ def clip_grad_norm(grads, max_norm, out=None, workspace=None, stream=None):
                                      norm.data_ptr(), ws.data_ptr(), ws.numel(),
                                      _stream_of(norm, stream)), "slim_clip_grads")
     return norm
-
-
-class _FirstDerivative(torch.autograd.Function):
-    """A gradient that the kernels computed, tied to what it depends on: its own
-    backward refuses."""
-
-    @staticmethod
-    def forward(ctx, grad, *depends):
-        return grad.clone()
-
-    @staticmethod
-    def backward(ctx, *_):
-        raise RuntimeError("libslim's calls can be differentiated only once")
-
-
-def _first_derivatives(grads, *depends):
-    """What a Function's backward returns.  The kernels leave no graph: under
-    create_graph, differentiating the gradients again would drop their terms
-    without a word, and is made an error instead."""
-    if not torch.is_grad_enabled() or not any(t.requires_grad for t in depends):
-        return grads
-    return tuple(_FirstDerivative.apply(g, *depends) for g in grads)
 
 
 class Embedding(torch.autograd.Function):

@@ -101,3 +101,25 @@ def test_first_derivatives_are_as_before(on_cpu):
     dx, du = torch.autograd.grad(y, (x, u), create_graph=True)
     (ddu,) = torch.autograd.grad(du.sum(), u)
     assert torch.allclose(ddu, 6 * u)
+
+
+def test_attention_refuses_second_derivatives(monkeypatch):
+    """slim_attention's kernels, stood in for by out = q omega_00."""
+    def forward(q, k, v, omega, C, feature, residuals):
+        return ((q * omega[0, 0]).detach(),) + tuple(torch.zeros(1) for _ in range(4))
+
+    def backward(q, k, v, omega, out, dout, S, z, C, feature, S_lo, z_lo):
+        with torch.no_grad():
+            return dout * omega[0, 0], torch.zeros_like(k), torch.zeros_like(v), \
+                torch.zeros_like(omega).index_put_((torch.tensor(0), torch.tensor(0)), (dout * q).sum())
+
+    monkeypatch.setattr(slim, "forward", forward)
+    monkeypatch.setattr(slim, "backward", backward)
+    q, omega = leaf(1, 1, 4, 2), leaf(3, 2, seed=1)
+    y = slim.slim_attention(q, q.detach(), q.detach(), omega, 2)
+    plain = torch.autograd.grad(y.pow(2).sum(), q, retain_graph=True)[0]
+    assert torch.allclose(plain, 2 * q * omega[0, 0] ** 2) and not plain.requires_grad
+    (dq,) = torch.autograd.grad(y.pow(2).sum(), q, create_graph=True)
+    assert torch.equal(dq.detach(), plain)
+    with pytest.raises(RuntimeError, match=REFUSAL):
+        torch.autograd.grad(dq.sum() + q.sum() + omega.sum(), (q, omega))
