@@ -333,7 +333,9 @@ slim_status slim_bwd_schedule(int B, int H, int L, int d, int M, int C, slim_dty
  * Reads the device error word that bounded waits in the kernels set when they
  * give up, and clears it.  Copies 4 bytes from the workspace on `stream` and
  * synchronises that stream (this call, unlike the others, blocks).  A failure
- * it reports is not reported again by the next call on the workspace.
+ * that was counted (see above) and not yet reported is reported even if a later
+ * call on the workspace has cleared the word.  A failure it reports is not
+ * reported again by the next call on the workspace.
  * Returns SLIM_OK, SLIM_ERR_TIMEOUT, or SLIM_ERR_CUDA.
  */
 slim_status slim_check_device_error(void* workspace, void* stream);

@@ -114,13 +114,16 @@ slim_status begin(const void* workspace, bool enabled, unsigned** counter) {
   return SLIM_OK;
 }
 
-void mark_seen(const void* workspace) {
+bool mark_seen(const void* workspace) {
   int dev = -1;
-  if (cudaGetDevice(&dev) != cudaSuccess) return;
+  if (cudaGetDevice(&dev) != cudaSuccess) return false;
   std::lock_guard<std::mutex> lock(g_mu);
-  if (g_state != 1) return;
+  if (g_state != 1) return false;
   const int slot = find_slot(workspace, dev);
-  if (slot >= 0) g_seen[slot] = load_counter(slot);
+  if (slot < 0) return false;
+  const unsigned now = load_counter(slot), before = g_seen[slot];
+  g_seen[slot] = now;
+  return now != before;
 }
 
 }  // namespace report

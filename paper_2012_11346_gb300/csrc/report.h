@@ -17,10 +17,11 @@ namespace report {
 // *counter is null: a wait that gives up is then counted nowhere.
 slim_status begin(const void* workspace, bool enabled, unsigned** counter);
 
-// After a blocking read of a workspace's error word: every failure counted on
-// that workspace so far has been seen, so the next call does not report it
-// again.
-void mark_seen(const void* workspace);
+// At a blocking check of a workspace, its stream drained: whether a failure was
+// counted on it since that was last reported (a later call may have cleared the
+// error word itself).  Every failure so far has then been seen, so the next call
+// does not report it again.
+bool mark_seen(const void* workspace);
 
 }  // namespace report
 }  // namespace slim

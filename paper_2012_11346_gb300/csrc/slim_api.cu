@@ -436,14 +436,12 @@ slim_status slim_check_device_error(void* workspace, void* stream) {
   if (cudaMemcpyAsync(&word, workspace, sizeof(int), cudaMemcpyDeviceToHost, s) != cudaSuccess)
     return SLIM_ERR_CUDA;
   if (cudaStreamSynchronize(s) != cudaSuccess) return SLIM_ERR_CUDA;
-  // the stream is drained: every failure counted on this workspace is in the
-  // word just read, so the next call need not report it again
-  slim::report::mark_seen(workspace);
-  if (word != 0) {
-    if (cudaMemsetAsync(workspace, 0, sizeof(int), s) != cudaSuccess) return SLIM_ERR_CUDA;
-    return SLIM_ERR_TIMEOUT;
-  }
-  return SLIM_OK;
+  // the stream is drained: every failure on this workspace is in the word just
+  // read, or was counted before a later call cleared the word
+  const bool counted = slim::report::mark_seen(workspace);
+  if (word != 0 && cudaMemsetAsync(workspace, 0, sizeof(int), s) != cudaSuccess)
+    return SLIM_ERR_CUDA;
+  return word != 0 || counted ? SLIM_ERR_TIMEOUT : SLIM_OK;
 }
 
 }  // extern "C"
