@@ -1048,12 +1048,14 @@ extern "C" slim_status slim_vocab_loss_fwd(const void* x, const void* w, const v
   slim_vocab_loss_workspace_size(N, D, V, dtype, 1, 0, &need);
   if (workspace == nullptr || workspace_bytes < need) return SLIM_ERR_WORKSPACE;
   if (!aligned(workspace, 256)) return SLIM_ERR_INVALID_ARG;
-  if (rows_fit(N, D, dtype))
+  unsigned* rep = nullptr;
+  const bool rows = rows_fit(N, D, dtype);
+  const slim_status st =
+      rows ? slim::report::pending(workspace) : slim::report::begin(workspace, true, &rep);
+  if (st != SLIM_OK) return st;
+  if (rows)
     return rows_fwd(x, w, targets, itype, (int)N, D, V, dtype, ignore_index, loss, lse, total,
                     workspace, s);
-  unsigned* rep = nullptr;
-  const slim_status st = slim::report::begin(workspace, true, &rep);
-  if (st != SLIM_OK) return st;
   const Sizes z{N, D, V, dtype};
   slim::Carver cv(workspace);
   const Ws ws = carve(cv, z, 1, false);
@@ -1086,12 +1088,14 @@ extern "C" slim_status slim_vocab_loss_bwd(const void* x, const void* w, const v
   slim_vocab_loss_workspace_size(N, D, V, dtype, piece, 1, &need);
   if (workspace == nullptr || workspace_bytes < need) return SLIM_ERR_WORKSPACE;
   if (!aligned(workspace, 256)) return SLIM_ERR_INVALID_ARG;
-  if (rows_fit(N, D, dtype))
+  unsigned* rep = nullptr;
+  const bool rows = rows_fit(N, D, dtype);
+  const slim_status st =
+      rows ? slim::report::pending(workspace) : slim::report::begin(workspace, true, &rep);
+  if (st != SLIM_OK) return st;
+  if (rows)
     return rows_bwd(x, w, targets, itype, lse, dloss, dloss_stride, count, (int)N, D, V, dtype,
                     ignore_index, dx, dw, workspace, s);
-  unsigned* rep = nullptr;
-  const slim_status st = slim::report::begin(workspace, true, &rep);
-  if (st != SLIM_OK) return st;
   const Sizes z{N, D, V, dtype};
   slim::Carver cv(workspace);
   const Ws ws = carve(cv, z, piece, true);

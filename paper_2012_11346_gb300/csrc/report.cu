@@ -126,5 +126,9 @@ bool mark_seen(const void* workspace) {
   return now != before;
 }
 
+slim_status pending(const void* workspace) {
+  return mark_seen(workspace) ? SLIM_ERR_TIMEOUT : SLIM_OK;
+}
+
 }  // namespace report
 }  // namespace slim

@@ -17,6 +17,11 @@ namespace report {
 // *counter is null: a wait that gives up is then counted nowhere.
 slim_status begin(const void* workspace, bool enabled, unsigned** counter);
 
+// For an entry point whose kernels have no waits, at the same place: begin's
+// status.  It takes no slot and sets nothing up: a workspace that has none has
+// no failure to report.
+slim_status pending(const void* workspace);
+
 // At a blocking check of a workspace, its stream drained: whether a failure was
 // counted on it since that was last reported (a later call may have cleared the
 // error word itself).  Every failure so far has then been seen, so the next call

@@ -46,3 +46,29 @@ def test_a_call_without_waits_between_loses_nothing(cuda_device, call):
     slim.check_device_error(ws)
     call(cuda_device, ws)
     slim.check_device_error(ws)
+
+
+@pytest.mark.parametrize("N", [1, 3, 300])
+@pytest.mark.parametrize("backward", [False, True])
+def test_the_next_loss_call_reports_it(cuda_device, N, backward):
+    """Whether it has few rows or many: it launches nothing and returns the error,
+    and the call after it runs."""
+    x, w, t = loss_inputs(cuda_device, N)
+    ref = slim.vocab_loss_forward(x, w, t)
+    one = torch.ones(1, device=cuda_device)
+    ws = torch.zeros(1 << 22, dtype=torch.uint8, device=cuda_device)
+
+    def call():
+        if backward:
+            return slim.vocab_loss_backward(x, w, t, ref[1], one, workspace=ws)
+        return slim.vocab_loss_forward(x, w, t, workspace=ws)
+
+    fail_on(ws)
+    before = slim.launch_count()
+    with pytest.raises(slim.SlimError) as e:
+        call()
+    assert e.value.status == TIMEOUT and slim.launch_count() == before
+    out = call()
+    slim.check_device_error(ws)
+    want = slim.vocab_loss_backward(x, w, t, ref[1], one) if backward else ref
+    assert all(torch.equal(a, b) for a, b in zip(out, want))
