@@ -209,6 +209,13 @@ __device__ __forceinline__ void gemm_end(GemmShared& sh, bool failed) {
   if (threadIdx.x / 32 == 2) gemm_tmem_free(sh.tmem, 2 * kTN);
 }
 
+// A bounded wait of a whole warp: false for all lanes if one of them gave up.
+// What follows takes a full warp (tcgen05.ld, the block's and the pair's
+// barriers), also when the wait ran out.
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, int* err) {
+  return __all_sync(0xffffffffu, tc::mbar_wait(bar, parity, err));
+}
+
 // One lane of a converged warp, the same every time.  ptxas knows that a branch
 // on it holds one thread, and keeps what the MMAs take in uniform registers.
 __device__ __forceinline__ bool elect_one() {
@@ -252,9 +259,7 @@ __device__ bool gemm_copy(GemmShared& sh, uint8_t* stages, Next next, int* err) 
       phase ^= 1;
     }
   };
-  auto free = [&] {
-    return __all_sync(0xffffffffu, tc::mbar_wait(empty0 + 8 * st, phase, err));
-  };
+  auto free = [&] { return warp_wait(empty0 + 8 * st, phase, err); };
   Work w;
   while (next(w)) {
     const CUtensorMap* map_a = uniform(&w.p->a);
@@ -264,8 +269,7 @@ __device__ bool gemm_copy(GemmShared& sh, uint8_t* stages, Next next, int* err) 
     const int k0 = uniform(w.k0) * kTK, k1 = uniform(w.k1) * kTK;
     if (T::HOLD && row != held_row) {
       if (held_row >= 0) {
-        if (!__all_sync(0xffffffffu, tc::mbar_wait(tc::smem_u32(&sh.unheld), held_phase, err)))
-          return false;
+        if (!warp_wait(tc::smem_u32(&sh.unheld), held_phase, err)) return false;
         held_phase ^= 1;
       }
       held_row = row;
@@ -333,7 +337,7 @@ __device__ bool gemm_multiply(GemmShared& sh, uint8_t* stages, Next next, int* e
     }
   };
   auto wait = [&](uint32_t bar, uint32_t parity) {
-    const bool ok = __all_sync(0xffffffffu, tc::mbar_wait(bar, parity, err));
+    const bool ok = warp_wait(bar, parity, err);
     tc::tc_fence_after();
     return ok;
   };
@@ -426,9 +430,8 @@ __device__ bool gemm_finish(GemmShared& sh, Next next, Epi& epi, int* err) {
     epi.begin(w, row, col);
     for (int k0 = w.k0; k0 < w.k1; k0 += step, ++acc) {
       const int buf = acc & 1;
-      if (!tc::mbar_wait(tc::smem_u32(&sh.tfull[buf]), (acc >> 1) & 1, err)) return false;
+      if (!warp_wait(tc::smem_u32(&sh.tfull[buf]), (acc >> 1) & 1, err)) return false;
       tc::tc_fence_after();
-      __syncwarp();
       const uint32_t t =
           sh.tmem + buf * kTN + part * kEpiCols + ((uint32_t)(quarter * 32) << 16);
       if (T::ACC) {
