@@ -128,9 +128,9 @@ slim_status slim_vocab_loss_bwd(const void* x, const void* w, const void* target
  *   norm      [1] fp32, written.  The squares are summed over the whole range
  *             of the types: neither 1e30 nor 1e-30 is lost.
  *   max_norm  > 0; infinity only measures and copies.
- * When the norm is not finite (an infinity or NaN among the gradients) the
- * gradients are passed on unscaled: the caller reads the norm and skips the
- * step.
+ * When the norm written is not finite (an infinity or NaN among the gradients,
+ * or finite ones whose norm passes fp32's range) the gradients are passed on
+ * unscaled: the caller reads the norm and skips the step.
  *   workspace of slim_clip_workspace_size(n) bytes.
  */
 slim_status slim_clip_workspace_size(int n, size_t* bytes);

@@ -301,9 +301,11 @@ __global__ void __launch_bounds__(kThreads) k_clip(const __grid_constant__ Table
     for (int o = 16; o; o >>= 1) acc += __shfl_xor_sync(0xffffffffu, acc, o);
     if (threadIdx.x == 0) {
       const double norm = sqrt(acc);
-      if (norm_out && blockIdx.x == 0) *norm_out = (float)norm;
-      // a norm that is not finite scales nothing
-      factor = norm > (double)max_norm && norm <= DBL_MAX ? (float)((double)max_norm / norm) : 1.0f;
+      const float told = (float)norm;
+      if (norm_out && blockIdx.x == 0) *norm_out = told;
+      // a norm that is not finite scales nothing: the one that the caller reads,
+      // which overflows before the sum in fp64 does
+      factor = norm > (double)max_norm && told <= FLT_MAX ? (float)((double)max_norm / norm) : 1.0f;
     }
   }
   __syncthreads();

@@ -41,3 +41,28 @@ def test_empty_tensors_around_a_full_list(cuda_device, live, lead, trail):
     for a, b in zip(grads, before):
         ref = b.double() * 0.5
         assert ((a.double() - ref).abs() <= tol * ref.abs()).all()
+
+
+@pytest.mark.parametrize("dt", [F32, BF16])
+@pytest.mark.parametrize("in_place", [True, False])
+@pytest.mark.parametrize("n", [20, 100000])
+def test_finite_gradients_whose_norm_passes_fp32(cuda_device, dt, in_place, n):
+    """What the caller reads is an infinity: as for any norm that is not finite,
+    the gradients are passed on as they are.  One step below, they are clipped."""
+    value = 3.0e38 / math.sqrt(n) * 1.5
+    grads = [torch.full((n,), value, dtype=dt, device=cuda_device), torch.ones(9, device=cuda_device)]
+    before = [g.clone() for g in grads]
+    out = None if in_place else [torch.empty_like(g) for g in grads]
+    norm = slim.clip_grad_norm(grads, 1e30, out=out)
+    assert math.isinf(norm.item())
+    for b, o in zip(before, grads if in_place else out):
+        assert torch.equal(b, o)
+    grads[0].copy_(before[0].double() * 0.5)
+    n64 = norm64(grads)
+    assert n64 < torch.finfo(F32).max
+    ref = [g.double() * (1e30 / n64) for g in grads]
+    norm = slim.clip_grad_norm(grads, 1e30, out=out)
+    assert abs(norm.item() - n64) <= NORM_TOL * n64
+    unit = 2.0 ** -24 if dt == F32 else 2.0 ** -8
+    for r, o in zip(ref, grads if in_place else out):
+        assert ((o.double() - r).abs() <= (NORM_TOL + 5 * 2.0 ** -24 + unit) * r.abs()).all()
