@@ -232,8 +232,19 @@ __device__ __forceinline__ uint4 shifted(const uint4& a, const uint4& b, unsigne
                     __funnelshift_r(c[W + 2], c[W + 3], r), __funnelshift_r(c[W + 3], c[W + 4], r));
 }
 
+// max_norm / norm as the product of two, a step each: below fp32's normal range
+// it would lose its digits (1e38 clipped to 1e-3: 13 bits of them left).
+struct Factor {
+  float a, b;
+  __device__ __forceinline__ float operator()(float x) const { return x * a * b; }
+};
+__device__ __forceinline__ Factor make_factor(double f) {
+  if (f >= 0x1p-126) return Factor{(float)f, 1.0f};
+  return Factor{(float)(f * 0x1p126), 0x1p-126f};
+}
+
 template <typename T>
-__device__ __forceinline__ void scale_chunk(const T* p, T* q, const Chunk& ch, float c) {
+__device__ __forceinline__ void scale_chunk(const T* p, T* q, const Chunk& ch, const Factor& c) {
   constexpr int W = Pack<T>::n;
   const long long nvec = ch.m / W;
   uint4* o = reinterpret_cast<uint4*>(q + ch.at);
@@ -241,7 +252,7 @@ __device__ __forceinline__ void scale_chunk(const T* p, T* q, const Chunk& ch, f
     float f[W];
     Pack<T>::get(u, f);
 #pragma unroll
-    for (int e = 0; e < W; ++e) f[e] *= c;
+    for (int e = 0; e < W; ++e) f[e] = c(f[e]);
     return Pack<T>::put(f);
   };
   // the source may lie otherwise: then every 16 bytes come from the two aligned
@@ -282,10 +293,10 @@ __device__ __forceinline__ void scale_chunk(const T* p, T* q, const Chunk& ch, f
       default: all(std::integral_constant<int, 3>()); break;
     }
   }
-  if (threadIdx.x < ch.lead) Io<T>::store(q, threadIdx.x, Io<T>::load(p, threadIdx.x) * c);
+  if (threadIdx.x < ch.lead) Io<T>::store(q, threadIdx.x, c(Io<T>::load(p, threadIdx.x)));
   if (nvec * W + threadIdx.x < ch.m) {
     const long long k = ch.at + nvec * W + threadIdx.x;
-    Io<T>::store(q, k, Io<T>::load(p, k) * c);
+    Io<T>::store(q, k, c(Io<T>::load(p, k)));
   }
 }
 
@@ -293,7 +304,7 @@ template <int CAP>
 __global__ void __launch_bounds__(kThreads) k_clip(const __grid_constant__ Table<CAP> tb,
                                                    const double* part, int parts, float max_norm,
                                                    int in_place, float* norm_out) {
-  __shared__ float factor;
+  __shared__ Factor factor;
   tc::grid_dependency_wait();
   if (threadIdx.x < 32) {
     double acc = 0.0;
@@ -305,12 +316,12 @@ __global__ void __launch_bounds__(kThreads) k_clip(const __grid_constant__ Table
       if (norm_out && blockIdx.x == 0) *norm_out = told;
       // a norm that is not finite scales nothing: the one that the caller reads,
       // which overflows before the sum in fp64 does
-      factor = norm > (double)max_norm && told <= FLT_MAX ? (float)((double)max_norm / norm) : 1.0f;
+      factor = make_factor(norm > (double)max_norm && told <= FLT_MAX ? (double)max_norm / norm : 1.0);
     }
   }
   __syncthreads();
-  const float c = factor;
-  if (c == 1.0f && in_place) return;
+  const Factor c = factor;
+  if (c.a * c.b == 1.0f && in_place) return;
   const unsigned total = tb.start[tb.n];
   for (unsigned x = blockIdx.x; x < total; x += gridDim.x) {
     const unsigned chunk = total - 1 - x;  // the end first: L2 holds what was read last

@@ -66,3 +66,21 @@ def test_finite_gradients_whose_norm_passes_fp32(cuda_device, dt, in_place, n):
     unit = 2.0 ** -24 if dt == F32 else 2.0 ** -8
     for r, o in zip(ref, grads if in_place else out):
         assert ((o.double() - r).abs() <= (NORM_TOL + 5 * 2.0 ** -24 + unit) * r.abs()).all()
+
+
+@pytest.mark.parametrize("dt", [F32, BF16])
+@pytest.mark.parametrize("value,max_norm", [(1e36, 1.0), (1e36, 1e-3), (1e36, 1e-7), (1e33, 1e-9),
+                                            (1e36, 1e-30), (1e36, 1e-37)])
+def test_factors_below_fp32s_normal_range(cuda_device, dt, value, max_norm):
+    """max_norm / norm down to 1e-75: the clipped gradients keep their digits (an
+    element below 2^-126 to a multiple of the type's least number)."""
+    g = torch.Generator(device=cuda_device).manual_seed(1)
+    grads = [(torch.randn(n, generator=g, device=cuda_device) * value).to(dt) for n in (70001, 300)]
+    n64 = norm64(grads)
+    ref = [t.double() * (max_norm / n64) for t in grads]
+    # max_norm reaches the kernel in fp32
+    assert abs(slim.clip_grad_norm(grads, max_norm).item() - n64) <= NORM_TOL * n64
+    unit, least = (2.0 ** -24, 2.0 ** -149) if dt == F32 else (2.0 ** -8, 2.0 ** -133)
+    for r, o in zip(ref, grads):
+        tol = (NORM_TOL + 6 * 2.0 ** -24 + unit) * r.abs() + least
+        assert ((o.double() - r).abs() <= tol).all()
