@@ -313,8 +313,9 @@ __device__ __forceinline__ RunNext run_of(const Product& p) {
 }
 
 // A bf16 logit over more than 512 features is summed in chains: its loss shows
-// in the fp32 results otherwise (2e-6 of a logit at 2048).  Up to 512 features a
-// worker can hold its rows of x while it walks along the vocabulary: 16384 x 512 x
+// in the fp32 results otherwise (2e-6 of a logit at 2048).  The gradients' logits
+// are summed as the statistics' are, to the same bits: where a row is sure of its
+// target, p - 1 is what their difference leaves.  Up to 512 features a worker can hold its rows of x while it walks along the vocabulary: 16384 x 512 x
 // 50021 statistics 424 -> 400 us, the softmax kernel of 32768 x 512 x 32768 735 ->
 // 685 us.
 // Changing rows then drains the MMAs, so it has to be for a walk of some tiles.
@@ -335,10 +336,10 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
   if (threadIdx.x >= 128) epi.flush();
 }
 
-template <int NP, bool HOLD>
+template <int NP, bool JOIN, bool HOLD>
 __global__ void __launch_bounds__(kGemmThreads, 1)
     k_loss_softmax(const __grid_constant__ SoftJob job) {
-  using T = Tile<NP, (NP > 1), HOLD>;
+  using T = Tile<NP, JOIN, HOLD>;
   __shared__ GemmShared sh;
   SoftEpi<NP> epi(job);
   gemm_roles<T>(sh, stage_memory<T>(), run_of(job.p), epi, job.err);
@@ -847,6 +848,16 @@ bool* once() {
   return device_flag(flags);
 }
 
+// Calls go(join, hold) with the form of the tiles that logits `p` take, as types.
+template <int NP, typename Go>
+bool with_form(const Product& p, Go go) {
+  using No = std::integral_constant<bool, (NP > 1)>;  // three planes: always in chains
+  using Hold = std::integral_constant<bool, NP == 1>;
+  return p.kb > Tile<1>::CHAIN ? go(std::true_type(), std::false_type())
+         : hold_rows(p)        ? go(No(), Hold())
+                               : go(No(), std::false_type());
+}
+
 template <int NP>
 slim_status fwd(const Sizes& z, const void* x, const void* w, const void* targets, slim_index it,
                 long long ignore, float* loss, float* lse, float* total, const Ws& ws,
@@ -877,18 +888,11 @@ slim_status fwd(const Sizes& z, const void* x, const void* w, const void* target
   j.rep = rep;
   {
     prof::Scope ps(prof::K_LOSS_STATS, s, 2.0 * z.N * z.D * z.V, ((double)z.N + z.V) * z.D * 2 * NP);
-    const unsigned blocks = (unsigned)wk * kPair;
-    auto go = [&](auto join, auto hold) {
+    const bool ok = with_form<NP>(j.p, [&](auto join, auto hold) {
       using T = Tile<NP, decltype(join)::value, decltype(hold)::value>;
-      return launch<T>(k_loss_stats<NP, T::ACC, T::HOLD>, blocks, !j.first, s, j,
+      return launch<T>(k_loss_stats<NP, T::ACC, T::HOLD>, (unsigned)wk * kPair, !j.first, s, j,
                        once<StatEpi<NP>, T>());
-    };
-    using Yes = std::true_type;
-    using No = std::integral_constant<bool, (NP > 1)>;  // three planes: always in chains
-    using Hold = std::integral_constant<bool, NP == 1>;
-    const bool ok = j.p.kb > Tile<1>::CHAIN ? go(Yes(), std::false_type())
-                    : hold_rows(j.p)            ? go(No(), Hold())
-                                                : go(No(), std::false_type());
+    });
     if (!ok) return SLIM_ERR_CUDA;
   }
   JoinJob q{};
@@ -967,13 +971,12 @@ slim_status bwd(const Sizes& z, const void* x, const void* w, const void* target
     {
       const long long wk = tiles < workers() ? tiles : workers();
       prof::Scope sc(prof::K_LOSS_SOFTMAX, s, fl, ((double)z.N + n) * z.D * 2 * NP + gb);
-      auto go = [&](auto hold) {
-        using T = Tile<NP, (NP > 1), decltype(hold)::value>;
-        return launch<T>(k_loss_softmax<NP, T::HOLD>, (unsigned)wk * kPair, true, s, j,
+      const bool ok = with_form<NP>(j.p, [&](auto join, auto hold) {
+        using T = Tile<NP, decltype(join)::value, decltype(hold)::value>;
+        return launch<T>(k_loss_softmax<NP, T::ACC, T::HOLD>, (unsigned)wk * kPair, true, s, j,
                          once<SoftEpi<NP>, T>());
-      };
-      using Hold = std::integral_constant<bool, NP == 1>;
-      if (!(hold_rows(j.p) ? go(Hold()) : go(std::false_type()))) return SLIM_ERR_CUDA;
+      });
+      if (!ok) return SLIM_ERR_CUDA;
     }
     q.acc = ws.acc;
     q.acc_ld = acc_ld(z.D);
