@@ -675,6 +675,11 @@ int stat_slots(long long tm, long long tn, long long w) {
 // than one and a half times the even share of all workers, into parts of about
 // that share.  100 rows of 1024 against 50000 words: dx is four tiles of 782
 // stages beside 784 tiles of two, and unsplit took all of the launch's 221 us.
+// With one plane a part is also at most 32768 terms long: the longer a sum of one
+// sign, the more of each term the tensor core cuts off.  dw over 2^20 rows came out
+// low by 6.6e-3 of itself unbroken, more than the result's own rounding (2^-9), and
+// in parts of 65536 by 3.8e-4; the parts are joined in fp32.
+constexpr long long kPartMost = 32768 / kTK;
 void split_long(const long long tiles[2], const long long kb[2], int np, int w, int splits[2]) {
   const long long total = tiles[0] * kb[0] + tiles[1] * kb[1];
   const long long least = np == 1 ? 16 : 4;  // stages worth a tile of their own
@@ -682,6 +687,8 @@ void split_long(const long long tiles[2], const long long kb[2], int np, int w, 
   for (int i = 0; i < 2; ++i) {
     splits[i] = 1;
     if (2 * kb[i] >= 3 * share) splits[i] = (int)((kb[i] + share - 1) / share);
+    if (np == 1 && (long long)splits[i] * kPartMost < kb[i])
+      splits[i] = (int)((kb[i] + kPartMost - 1) / kPartMost);
   }
 }
 

@@ -35,3 +35,31 @@ def test_rows_that_are_sure_of_their_target(cuda_device, dt, N, D, V):
     # dx = g_0 w_0, and as little of the other words
     most = bound * w[0].abs().max().item() + rest * w.abs().max().item()
     assert dx.abs().max().item() <= most * (1 + 2.0 ** -7)
+
+
+def test_a_million_terms_of_one_sign(cuda_device):
+    """dw of a bf16 problem over 2^20 rows that all push the same way.  The tensor
+    core cuts the end off what it adds to a long sum, always downwards, so such
+    sums are cut into parts that are joined in fp32.  What may be missing is 2^-12
+    of the result, an eighth of the unit it is rounded to: that shows in the mean
+    over 10^5 elements, from which the results' own rounding (2^-9 / sqrt 3 each)
+    vanishes to below 1e-5; 2e-5 is left to it.  26 tiles of words, so that the
+    work alone gives no reason to split the sums."""
+    g = torch.Generator(device=cuda_device).manual_seed(11)
+    N, D, V = 1 << 20, 16, 26 * 256
+    x = (0.5 + torch.rand(N, D, generator=g, device=cuda_device)).to(BF16)
+    w = (0.5 * torch.randn(V, D, generator=g, device=cuda_device)).to(BF16)
+    t = torch.zeros(N, dtype=torch.long, device=cuda_device)
+    _, lse, _ = slim.vocab_loss_forward(x, w, t)
+    dx, dw = slim.vocab_loss_backward(x, w, t, lse, torch.ones(1, device=cuda_device))
+    ref = torch.zeros(V, D, dtype=torch.float64, device=cuda_device)
+    for a in range(0, N, 1 << 15):
+        rows = x[a:a + (1 << 15)].double()
+        ref += torch.softmax(rows @ w.double().T, 1).T @ rows
+    off = ((dw.double()[1:] - ref[1:]) / ref[1:]).mean().item()
+    assert -(2.0 ** -12 + 2e-5) <= off <= 2e-5
+    # the last row of dx, against the definition
+    p = torch.softmax(x[-1:].double() @ w.double().T, 1)
+    p[0, 0] -= 1
+    last = p @ w.double()
+    assert (dx[-1:].double() - last).norm() <= 5e-3 * last.norm()
