@@ -37,7 +37,8 @@ typedef enum { SLIM_I32 = 0, SLIM_I64 = 1 } slim_index;
  *   ids    [N] itype, aligned to its own size.  An id outside [0, V) marks
  *          padding: its row of out is zero.
  *   table  [V, D] dtype;  out [N, D] dtype.
- * 0 <= N < 2^31, D >= 1, V >= 1.  N = 0 enqueues nothing.
+ * 0 <= N < 2^31, 1 <= D <= 2^30, V >= 1, N D and V D <= 2^42.  N = 0 enqueues
+ * nothing.
  */
 slim_status slim_embed_fwd(const void* ids, slim_index itype, const void* table, long long N,
                            int D, int V, slim_dtype dtype, float scale, void* out, void* stream);

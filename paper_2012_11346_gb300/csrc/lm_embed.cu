@@ -542,6 +542,7 @@ __global__ void __launch_bounds__(kJoinThreads) k_embed_join(SumJob j, T* dtable
 // ------------------------------------------------------------------ host
 bool sizes_ok(long long N, int D, int V, slim_dtype dtype, slim_index itype) {
   if (N < 0 || N >= (1LL << 31) || D < 1 || V < 1) return false;
+  if (D > (1 << 30)) return false;  // a row's 32-bit column indices step past its end
   if (dtype != SLIM_F32 && dtype != SLIM_BF16) return false;
   if (itype != SLIM_I32 && itype != SLIM_I64) return false;
   // element counts stay far inside 64 bits
