@@ -80,7 +80,8 @@ slim_status slim_embed_bwd(const void* ids, slim_index itype, const void* dout, 
  * bf16 operands are multiplied exactly and summed in fp32.  fp32 operands are
  * split into three bf16 pieces (24 bits) and multiplied piece by piece, six
  * products each, smallest first, on the tensor cores.
- * 0 <= N < 2^31 - 512, D >= 1, 1 <= V <= 2^30, N V <= 2^50.  N = 0 only zeroes `total`.
+ * 0 <= N < 2^31 - 512, 1 <= D <= 2^30, 1 <= V <= 2^30, N V <= 2^50, N D and V D
+ * <= 2^40.  N = 0 only zeroes `total`.
  *
  * slim_vocab_loss_workspace_size: workspace bytes of the forward (backward =
  * 0, piece is not read) or of the backward with this piece.

@@ -639,6 +639,7 @@ struct Sizes {
 bool sizes_ok(long long N, int D, int V, slim_dtype dtype) {
   if (N < 0 || N >= (1LL << 31) - 512 || D < 1 || V < 1 || V > (1 << 30)) return false;
   if (dtype != SLIM_F32 && dtype != SLIM_BF16) return false;
+  if (D > (1 << 30)) return false;  // rounded up to whole stages, 32 bits hold it
   if (N > 0 && (long long)V > (1LL << 50) / N) return false;  // a worker's tiles fit 31 bits
   return (long long)D <= (1LL << 40) / (N > 0 ? N : 1) && (long long)D <= (1LL << 40) / V;
 }

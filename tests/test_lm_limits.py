@@ -32,3 +32,17 @@ def test_embedding_width(lib, D, dt):
     assert lib.slim_embed_bwd(FAKE, I64, FAKE, 1, D, 1, dt, 1.0, 0, FAKE, FAKE, 1 << 50, None) == INVALID
     assert lib.slim_embed_bwd_workspace_size(1, D, 1, dt, ctypes.byref(n)) == INVALID
     assert lib.slim_embed_bwd_workspace_size(1, WIDEST, 1, dt, ctypes.byref(n)) == OK
+
+
+@pytest.mark.parametrize("dt", [F32, BF16])
+@pytest.mark.parametrize("D", [WIDEST + 1, (1 << 31) - 64, (1 << 31) - 1])
+def test_loss_width(lib, D, dt):
+    """Rounded up to whole stages, the features have to stay in 32 bits."""
+    n = ctypes.c_size_t()
+    assert lib.slim_vocab_loss_fwd(FAKE, FAKE, FAKE, I64, 9, D, 1, dt, -100, FAKE, FAKE, FAKE, FAKE, 1 << 60,
+                                   None) == INVALID
+    assert lib.slim_vocab_loss_bwd(FAKE, FAKE, FAKE, I64, FAKE, FAKE, 0, None, 9, D, 1, dt, 256, -100, FAKE,
+                                   FAKE, FAKE, 1 << 60, None) == INVALID
+    for backward in (0, 1):
+        size = lambda d: lib.slim_vocab_loss_workspace_size(9, d, 1, dt, 256, backward, ctypes.byref(n))
+        assert size(D) == INVALID and size(WIDEST) == OK
