@@ -46,3 +46,36 @@ def test_loss_width(lib, D, dt):
     for backward in (0, 1):
         size = lambda d: lib.slim_vocab_loss_workspace_size(9, d, 1, dt, 256, backward, ctypes.byref(n))
         assert size(D) == INVALID and size(WIDEST) == OK
+
+
+class NoLibrary:
+    def __getattr__(self, name):
+        raise AssertionError(f"{name} was reached")
+
+
+BIG = (1 << 32) + 5  # 5 as a C int
+
+
+@pytest.mark.parametrize("call", [
+    lambda e, i: slim.embed_workspace_size(4, 8, BIG, torch.float32),
+    lambda e, i: slim.embed_workspace_size(4, BIG, 8, torch.float32),
+    lambda e, i: slim.embed_forward(i, e),
+    lambda e, i: slim.embed_backward(i, torch.zeros(3, 1), BIG, dtable=e),
+    lambda e, i: slim.vocab_loss_workspace_size(4, 8, BIG, torch.float32, False),
+    lambda e, i: slim.vocab_loss_workspace_size(4, BIG, 8, torch.float32, True, 256),
+    lambda e, i: slim.vocab_loss_forward(torch.zeros(3, 1), e, i),
+    lambda e, i: slim.vocab_loss_backward(torch.zeros(3, 1), e, i, torch.zeros(3), torch.zeros(1)),
+    lambda e, i: slim.clip_workspace_size(BIG),
+])
+def test_sizes_past_c_ints_are_refused(monkeypatch, call):
+    """They would reach the library as their low 32 bits: a table of 2^32 + 5 rows
+    as one of 5, with every other id as padding."""
+    monkeypatch.setattr(slim, "library", NoLibrary)
+    monkeypatch.setattr(slim, "_require_cuda", lambda *t: None)
+    with pytest.raises(ValueError):
+        call(torch.zeros(1, 1).expand(BIG, 1), torch.zeros(3, dtype=torch.long))
+
+
+def test_a_piece_of_any_size_is_the_whole_vocabulary(lib):
+    size = lambda piece: slim.vocab_loss_workspace_size(100, 64, 3000, torch.bfloat16, True, piece)
+    assert size((1 << 32) + 256) == size(1 << 20) == size(3000) > size(256)
