@@ -565,6 +565,8 @@ def embed_backward(ids, dout, V, scale=1.0, dtable=None, workspace=None, stream=
         _require_cuda(dtable)
         _require(dtable.dtype == dout.dtype and tuple(dtable.shape) == (V, D),
                  "dtable must be [V, D] in dout's dtype")
+    if workspace is not None:
+        _require_cuda(workspace)
     with _on(stream):
         if not accumulate:
             dtable = torch.empty(V, D, dtype=dout.dtype, device=dout.device)
@@ -610,6 +612,8 @@ def clip_grad_norm(grads, max_norm, out=None, workspace=None, stream=None):
         _require([o.numel() for o in out] == sizes.tolist() and [o.dtype for o in out] == types,
                  "out must hold one tensor of the same size and dtype per gradient")
         dst = array.array("Q", [o.data_ptr() for o in out])
+    if workspace is not None:
+        _require_cuda(workspace)
     with _on(stream):
         norm = torch.empty(1, dtype=torch.float32, device=grads[0].device)
         ws = workspace if workspace is not None else _workspace(clip_workspace_size(n),
@@ -688,6 +692,8 @@ def vocab_loss_forward(x, w, targets, ignore_index=-100, workspace=None, stream=
     and the log-sum, both fp32 in targets' shape, and total = [sum of the
     losses, number of rows not ignored]."""
     N, D, V, it, dt = _loss_dims(x, w, targets, "vocab_loss_forward")
+    if workspace is not None:
+        _require_cuda(workspace)
     with _on(stream):
         dev = x.device
         loss = torch.empty(targets.shape, dtype=torch.float32, device=dev)
@@ -720,6 +726,8 @@ def vocab_loss_backward(x, w, targets, lse, dloss, count=None, ignore_index=-100
     if count is not None:
         _require_cuda(count)
         _require(count.dtype == torch.float32 and count.numel() == 1, "count must be one fp32 value")
+    if workspace is not None:
+        _require_cuda(workspace)
     with _on(stream):
         dx, dw = torch.empty_like(x), torch.empty_like(w)
         ws = workspace if workspace is not None else _workspace(
