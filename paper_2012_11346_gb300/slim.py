@@ -489,11 +489,9 @@ def _require(cond, what):
         raise ValueError(what)
 
 
-def _require_int32(*sizes):
-    """Sizes that the library takes as C ints, of which ctypes would pass the low
-    32 bits on."""
-    for n in sizes:
-        _require(-(1 << 31) <= n < 1 << 31, "a size does not fit 32 bits")
+def _too_large():
+    # the library takes these as C ints, of which ctypes would pass the low 32 bits on
+    raise ValueError("a size does not fit 32 bits")
 
 
 def _index_code(ids, what):
@@ -523,7 +521,8 @@ def _on(stream):
 @functools.lru_cache(maxsize=1024)
 def embed_workspace_size(N, D, V, dtype):
     n = _sz(0)
-    _require_int32(D, V)
+    if (V | D) >> 31:
+        _too_large()
     _check(library().slim_embed_bwd_workspace_size(N, D, V, DTYPES[dtype], ctypes.byref(n)),
            "slim_embed_bwd_workspace_size")
     return n.value
@@ -537,7 +536,8 @@ def embed_forward(ids, table, scale=1.0, out=None, stream=None):
     if table.dim() != 2:
         raise ValueError("table must be [V, D]")
     V, D = table.shape
-    _require_int32(V, D)
+    if (V | D) >> 31:
+        _too_large()
     if out is None:
         with _on(stream):
             out = torch.empty(*ids.shape, D, dtype=table.dtype, device=table.device)
@@ -559,7 +559,8 @@ def embed_backward(ids, dout, V, scale=1.0, dtable=None, workspace=None, stream=
     if dout.shape[:-1] != ids.shape:
         raise ValueError("dout must be [*ids.shape, D]")
     D, N = dout.shape[-1], ids.numel()
-    _require_int32(V, D)
+    if (V | D) >> 31:
+        _too_large()
     accumulate = dtable is not None
     if accumulate:
         _require_cuda(dtable)
@@ -582,7 +583,8 @@ def embed_backward(ids, dout, V, scale=1.0, dtable=None, workspace=None, stream=
 def clip_workspace_size(n):
     """Workspace bytes of clip_grad_norm for n gradients."""
     b = _sz(0)
-    _require_int32(n)
+    if n >> 31:
+        _too_large()
     _check(library().slim_clip_workspace_size(n, ctypes.byref(b)), "slim_clip_workspace_size")
     return b.value
 
@@ -663,8 +665,9 @@ def vocab_piece(N, V):
 @functools.lru_cache(maxsize=1024)
 def vocab_loss_workspace_size(N, D, V, dtype, backward, piece=None):
     n = _sz(0)
-    piece = vocab_piece(N, V) if piece is None else min(piece, V)
-    _require_int32(D, V, piece)
+    piece = vocab_piece(N, V) if piece is None else max(0, min(piece, V))
+    if (V | D) >> 31:
+        _too_large()
     _check(library().slim_vocab_loss_workspace_size(N, D, V, DTYPES[dtype], piece, int(backward),
                                                     ctypes.byref(n)),
            "slim_vocab_loss_workspace_size")
@@ -681,8 +684,10 @@ def _loss_dims(x, w, targets, what):
         raise ValueError("x must be [..., D] and w [V, D]")
     if rows[:-1] != targets.shape:
         raise ValueError("targets must have one entry per row of x")
-    _require_int32(*shape)
-    return targets.numel(), shape[1], shape[0], it, dt
+    V, D = shape
+    if (V | D) >> 31:
+        _too_large()
+    return targets.numel(), D, V, it, dt
 
 
 def vocab_loss_forward(x, w, targets, ignore_index=-100, workspace=None, stream=None):
@@ -717,7 +722,7 @@ def vocab_loss_backward(x, w, targets, lse, dloss, count=None, ignore_index=-100
     the mean loss).  Memory grows with rows x piece."""
     N, D, V, it, dt = _loss_dims(x, w, targets, "vocab_loss_backward")
     _require_cuda(lse, dloss)
-    piece = vocab_piece(N, V) if piece is None else min(piece, V)
+    piece = vocab_piece(N, V) if piece is None else max(0, min(piece, V))
     per_row = dloss.numel()
     if lse.dtype != torch.float32 or lse.numel() != N:
         raise ValueError("lse must be the forward's")
