@@ -5,6 +5,7 @@ import pytest
 import torch
 
 from paper_2012_11346_gb300 import slim
+from test_vocab_loss_gpu import check, make
 
 pytestmark = pytest.mark.gpu
 
@@ -63,3 +64,49 @@ def test_a_million_terms_of_one_sign(cuda_device):
     p[0, 0] -= 1
     last = p @ w.double()
     assert (dx[-1:].double() - last).norm() <= 5e-3 * last.norm()
+
+
+# every row count that takes the few-row kernels, and the first that does not
+FEW = [(BF16, n) for n in (1, 2, 3, 4, 5)] + [(F32, n) for n in (1, 2, 3, 4, 5, 6, 7, 8, 9)]
+
+
+@pytest.mark.parametrize("D,V", [(64, 500), (37, 90), (1000, 33)])
+@pytest.mark.parametrize("dt,N", FEW)
+def test_few_rows_with_an_ignored_one(cuda_device, dt, N, D, V):
+    """What an ignored row and its upstream gradient hold goes nowhere."""
+    for gone in range(N):
+        x, w, t, c = make(cuda_device, N, D, V, dt, it=torch.int32, ignored=0.0, seed=gone)
+        t[gone] = -100
+        clean = check(x, w, t, c)
+        for bad in (float("nan"), float("inf"), torch.finfo(dt).min):
+            y, d = x.clone(), c.clone()
+            y[gone], d[gone] = bad, bad
+            loss, lse, total = slim.vocab_loss_forward(y, w, t)
+            dx, dw = slim.vocab_loss_backward(y, w, t, lse, d)
+            for a, b in zip((loss, total, dx, dw), (clean[0], clean[2], clean[3], clean[4])):
+                assert torch.equal(a, b)
+            assert (dx[gone] == 0).all()
+
+
+@pytest.mark.parametrize("mean", [False, True])
+@pytest.mark.parametrize("dt,N", FEW)
+def test_few_rows_all_ignored(cuda_device, dt, N, mean):
+    x, w, t, c = make(cuda_device, N, 64, 300, dt, ignored=2.0)
+    loss, lse, total = slim.vocab_loss_forward(x, w, t)
+    dx, dw = slim.vocab_loss_backward(x, w, t, lse, c[:1] if mean else c, count=total[1:] if mean else None)
+    assert (loss == 0).all() and (total == 0).all() and (dx == 0).all() and (dw == 0).all()
+    assert ((lse.double() - torch.logsumexp(x.double() @ w.double().T, 1)).abs() <= 1e-4).all()
+
+
+@pytest.mark.parametrize("dt,N", FEW)
+@pytest.mark.parametrize("bad", [-1, 500, 1 << 31])
+def test_few_rows_with_a_target_out_of_range(cuda_device, dt, N, bad):
+    x, w, t, c = make(cuda_device, N, 64, 500, dt, ignored=0.0)
+    at = N // 2
+    t[at] = bad
+    loss, lse, total = slim.vocab_loss_forward(x, w, t)
+    assert torch.isnan(loss).tolist() == [i == at for i in range(N)] and total[1].item() == N
+    assert torch.isnan(total[0]) and torch.isfinite(lse).all()
+    dx, dw = slim.vocab_loss_backward(x, w, t, lse, c)
+    assert torch.isnan(dx).all(1).tolist() == [i == at for i in range(N)]
+    assert torch.isfinite(dx[torch.arange(N, device=cuda_device) != at]).all() and torch.isnan(dw).all()
