@@ -45,6 +45,14 @@ __device__ __forceinline__ float exp2_of(float x) {
   return NP == 1 ? tc::ex2_approx(x) : exp2f(x);
 }
 
+// The fast form that keeps weights below 2^-126: multiplied by a large x they are
+// all that some words' gradients have.
+__device__ __forceinline__ float exp2_small(float x) {
+  float y;
+  asm("ex2.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
 // Packs the leading bf16 plane of two values and leaves their remainders (both
 // exact).  With one plane there is no remainder to keep.
 template <int NP>
@@ -271,7 +279,7 @@ struct SoftEpi {
     if (NP == 1) {
       const float l2 = lse * kLog2e;
 #pragma unroll
-      for (int i = 0; i < 32; ++i) g[i] = tc::ex2_approx(fmaf(v[i], kLog2e, -l2));
+      for (int i = 0; i < 32; ++i) g[i] = exp2_small(fmaf(v[i], kLog2e, -l2));
     } else {
 #pragma unroll
       for (int i = 0; i < 32; ++i) g[i] = expf(v[i] - lse);

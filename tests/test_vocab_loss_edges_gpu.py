@@ -5,7 +5,7 @@ import pytest
 import torch
 
 from paper_2012_11346_gb300 import slim
-from test_vocab_loss_gpu import check, make
+from test_vocab_loss_gpu import U_G, U_OUT, check, make, ref64
 
 pytestmark = pytest.mark.gpu
 
@@ -110,3 +110,24 @@ def test_few_rows_with_a_target_out_of_range(cuda_device, dt, N, bad):
     dx, dw = slim.vocab_loss_backward(x, w, t, lse, c)
     assert torch.isnan(dx).all(1).tolist() == [i == at for i in range(N)]
     assert torch.isfinite(dx[torch.arange(N, device=cuda_device) != at]).all() and torch.isnan(dw).all()
+
+
+@pytest.mark.parametrize("dt", [F32, BF16])
+@pytest.mark.parametrize("big", [30.0, 80.0])
+@pytest.mark.parametrize("N,D", [(140, 128), (140, 700), (3, 128)])
+def test_gradients_at_large_logits(cuda_device, dt, N, D, big):
+    """Logits of several hundred: the elementwise bounds of test_vocab_loss_gpu.py.
+    Errors of the exponents are no longer small there: p is off by a factor of
+    exp(4 dz + ...)."""
+    x, w, t, c = make(cuda_device, N, D, 600, dt)
+    x = (x.float() * big).to(dt)
+    _, lse, _ = slim.vocab_loss_forward(x, w, t)
+    dx, dw = slim.vocab_loss_backward(x, w, t, lse, c)
+    r = ref64(x, w, t, c)
+    soft = torch.expm1(4 * r["dz"] + 2.0 ** -20 * (1 + r["lse"].abs()))[:, None]
+    ge = soft * r["pc"] + U_G[dt] * (r["g"].abs() + soft * r["pc"])
+    x64, w64 = x.double().abs(), w.double().abs()
+    for got, ref, err, mag, n in ((dx, r["dx"], ge @ w64, r["g"].abs() @ w64, w.shape[0]),
+                                  (dw, r["dw"], ge.T @ x64, r["g"].abs().T @ x64, N)):
+        bound = err + (n + 8) * 2.0 ** -23 * mag + U_OUT[dt] * (ref.abs() + err) + 1e-37
+        assert ((got.double() - ref).abs() <= bound).all()
