@@ -323,9 +323,9 @@ __device__ __forceinline__ RunNext run_of(const Product& p) {
 // A bf16 logit over more than 512 features is summed in chains: its loss shows
 // in the fp32 results otherwise (2e-6 of a logit at 2048).  The gradients' logits
 // are summed as the statistics' are, to the same bits: where a row is sure of its
-// target, p - 1 is what their difference leaves.  Up to 512 features a worker can hold its rows of x while it walks along the vocabulary: 16384 x 512 x
-// 50021 statistics 424 -> 400 us, the softmax kernel of 32768 x 512 x 32768 735 ->
-// 685 us.
+// target, p - 1 is what their difference leaves.  Up to 512 features a worker can
+// hold its rows of x while it walks along the vocabulary: 16384 x 512 x 50021
+// statistics 424 -> 400 us, the softmax kernel of 32768 x 512 x 32768 735 -> 685 us.
 // Changing rows then drains the MMAs, so it has to be for a walk of some tiles
 // (65536 x 512, statistics / softmax, ring -> held: 2 tile columns 31 -> 37 / 34 ->
 // 39 us, 4 46 -> 52 / 55 -> 58, 8 78 -> 82 / 98 -> 95, 16 145 -> 146 / 186 -> 174).
@@ -666,7 +666,8 @@ int sm_count() {
   return n;
 }
 
-// Workspace sizes do not depend on the device: they are for kMaxWorkers blocks.
+// Workspace sizes do not depend on the device: they, and the gradients' splits, are
+// for kMaxWorkers blocks.
 int workers() {  // pairs
   const int n = sm_count() < kMaxWorkers ? sm_count() : kMaxWorkers;
   return n / kPair;
@@ -720,11 +721,11 @@ int round_piece(int piece, int V) {
 int acc_ld(int D) { return (D + 31) / 32 * 32; }
 
 // Splits of dw and dx for a piece of n words.
-void grad_splits(const Sizes& z, long long n, int w, int splits[2]) {
+void grad_splits(const Sizes& z, long long n, int splits[2]) {
   const long long tn = cdiv(z.D, kTN);
   const long long tiles[2] = {cdiv(n, kTM * kPair) * tn, cdiv(z.N, kTM * kPair) * tn};
   const long long kb[2] = {cdiv(z.N, kTK), cdiv(n, kTK)};
-  split_long(tiles, kb, z.np(), w, splits);
+  split_long(tiles, kb, z.np(), kMaxWorkers / kPair, splits);
 }
 
 Ws carve(Carver& cv, const Sizes& z, int piece, bool bwd) {
@@ -748,7 +749,7 @@ Ws carve(Carver& cv, const Sizes& z, int piece, bool bwd) {
     const int last = z.V - (z.V - 1) / p * p;
     for (int n : {z.V < p ? z.V : p, last}) {
       int splits[2];
-      grad_splits(z, n, workers(), splits);
+      grad_splits(z, n, splits);
       for (int i = 0; i < 2; ++i) {
         const bool parts = splits[i] > 1 || !z.even_rows();
         const size_t k = parts ? (size_t)splits[i] * (i ? z.N : n) * acc_ld(z.D) : 0;
@@ -1001,7 +1002,7 @@ slim_status bwd(const Sizes& z, const void* x, const void* w, const void* target
     q.first = i == 0;
     q.last = i == pieces - 1;
     int splits[2];
-    grad_splits(z, n, workers(), splits);
+    grad_splits(z, n, splits);
     q.parts[0] = splits[0] > 1 || !q.wide;
     q.parts[1] = splits[1] > 1 || (!q.wide && q.last);
     long long nt[2], cost[2];
