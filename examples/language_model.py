@@ -4,9 +4,10 @@ the tied table and the layers' features.
 
     python examples/language_model.py [--steps 40] [--vocab 4000] [--dtype bf16]
 
-No step keeps anything of size tokens x vocabulary or tokens x layers: the stack
-recomputes its slices and rolls its states back, and the loss recomputes its
-logits piece by piece.  --dtype sets the type at the two ends of the model; the
+No step keeps anything of size tokens x layers: the stack recomputes its slices
+and rolls its states back.  The loss recomputes its logits piece by piece and
+holds one piece's gradient at a time; at the sizes below (8192 tokens, 4000 words)
+the whole vocabulary is one piece.  --dtype sets the type at the two ends of the model; the
 stack runs in fp32 (its bf16 kernels carry no residual of the rolled-back state,
 and after some steps of training a sequence's first rows get gradients thousands
 of times too large).  The data is synthetic: every symbol is followed by one

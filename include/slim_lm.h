@@ -80,6 +80,9 @@ slim_status slim_embed_bwd(const void* ids, slim_index itype, const void* dout, 
  * bf16 operands are multiplied exactly and summed in fp32.  fp32 operands are
  * split into three bf16 pieces (24 bits) and multiplied piece by piece, six
  * products each, smallest first, on the tensor cores.
+ * Values that count are finite: an infinity in w, or in a row that is not ignored,
+ * makes the logits it enters infinite or NaN (among the fp32 pieces, 0 x inf).  A
+ * word is masked through a constant feature of the type's lowest value.
  * 0 <= N < 2^31 - 512, 1 <= D <= 2^30, 1 <= V <= 2^30, N V <= 2^50, N D and V D
  * <= 2^40.  N = 0 only zeroes `total`.
  *
@@ -99,7 +102,8 @@ slim_status slim_vocab_loss_fwd(const void* x, const void* w, const void* target
  *     dx = g w  [N, D] dtype,   dw = g^T x  [V, D] dtype
  * in pieces of `piece` words (rounded up to a multiple of 256): a piece's
  * logits are computed again and its g is held only until both products have
- * read it, so memory grows with N * piece and not with N * V.
+ * read it, so memory grows with N * piece and not with N * V (2 bytes an element for
+ * bf16 problems, 6 for fp32 ones).
  *   lse          [N] fp32 from the forward on the same x, w and targets.
  *   dloss        fp32: [N] with dloss_stride 1, or [1] for every row with
  *                dloss_stride 0.
@@ -110,7 +114,8 @@ slim_status slim_vocab_loss_fwd(const void* x, const void* w, const void* target
  * holds, does not reach dw.  A row whose target is out of range passes NaN.
  * g is rounded once for the products: to bf16 for bf16 problems (2^-9
  * relative, like the rounding of the gradients themselves), to three bf16
- * pieces for fp32 ones.  Sums are fp32; dx and dw are rounded once.
+ * pieces for fp32 ones.  Sums are fp32, and long ones are joined from parts (the
+ * tensor cores cut bits off a long sum); dx and dw are rounded once.
  */
 slim_status slim_vocab_loss_bwd(const void* x, const void* w, const void* targets,
                                 slim_index itype, const float* lse, const float* dloss,

@@ -13,11 +13,11 @@
 // launch with both products, dx += g w and dw = g^T x.
 //
 // What bounds them, on GB300 (kernel times; peak = 1978 TFLOP/s bf16):
-//   statistics  16384 x 512 x 50021 bf16  400 us, 2.1 PFLOP/s: the tensor pipe;
-//               8192 x 768 x 10000 fp32   359 us, 2.1 PFLOP/s of plane products.
-//   softmax     32768 x 512 x 32768 bf16  685 us: g's stores share L1 with the
-//               MMAs' operands (the statistics of the same tiles: 528 us).
-//   products    the same sizes            1296 us, 1.7 PFLOP/s at 1.7 GHz: power.
+//   statistics  16384 x 512 x 50021 bf16  404 us, 2.1 PFLOP/s: the tensor pipe;
+//               8192 x 768 x 10000 fp32   360 us, 2.1 PFLOP/s of plane products.
+//   softmax     32768 x 512 x 32768 bf16  705 us: g's stores share L1 with the
+//               MMAs' operands (the statistics of the same tiles: 540 us).
+//   products    the same sizes            1345 us, 1.6 PFLOP/s at 1.7 GHz: power.
 // The logits are computed twice because a row's statistics are not known until
 // its last word; keeping them would be N x V, the thing to avoid.
 #include <stdint.h>

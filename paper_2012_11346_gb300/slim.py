@@ -658,7 +658,9 @@ def vocab_piece(N, V):
     """Words per piece of the vocabulary in vocab_loss_backward, unless the
     caller says otherwise: as many as keep rows x piece within 2^28, and at
     least 8192 (smaller pieces leave the products too few tiles; larger ones
-    gain nothing at 32768 rows)."""
+    gain nothing at 32768 rows).  So up to 2^28 logits, or 8192 words, one piece
+    is the whole vocabulary, and its gradient (2 bytes an element for bf16, 6 for
+    fp32) as large as the logits: a smaller `piece` holds less."""
     return min(V, max(8192, (1 << 28) // max(N, 1)))
 
 
