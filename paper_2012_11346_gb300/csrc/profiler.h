@@ -38,6 +38,8 @@ enum Kid {
   K_LOSS_GRAD,
   K_LOSS_ROWS,
   K_LOSS_PARTS,
+  K_QK_NORM,
+  K_QK_WEIGHTS,
   K_COUNT
 };
 

@@ -1,7 +1,7 @@
 """Python binding of libslim (ctypes): argument marshalling only.
 
 Every computation runs in the CUDA kernels behind the C ABI declared in
-include/slim.h and include/slim_lm.h.  PyTorch supplies device memory (outputs and workspace, so
+include/slim.h, include/slim_lm.h and include/slim_layer.h.  PyTorch supplies device memory (outputs and workspace, so
 torch.cuda.max_memory_allocated sees all of it) and the current stream.  There
 is no CPU fallback: if libslim.so is missing or no GPU is present, the calls
 raise.
@@ -26,7 +26,7 @@ STATUS = {0: "SLIM_OK", 1: "SLIM_ERR_INVALID_ARG", 2: "SLIM_ERR_UNSUPPORTED",
 _i, _p, _sz = ctypes.c_int, ctypes.c_void_p, ctypes.c_size_t
 _ll, _f = ctypes.c_longlong, ctypes.c_float
 
-# (name, argtypes) for every symbol of include/slim.h and include/slim_lm.h
+# (name, argtypes) for every symbol of include/slim.h, slim_lm.h and slim_layer.h
 SIGNATURES = {
     "slim_status_string": ([_i], ctypes.c_char_p),
     "slim_version": ([], _i),
@@ -62,6 +62,9 @@ SIGNATURES = {
                              _sz, _p], _i),
     "slim_clip_workspace_size": ([_i, ctypes.POINTER(_sz)], _i),
     "slim_clip_grads": ([_p, _p, _p, _p, _i, _f, _p, _p, _sz, _p], _i),
+    "slim_qk_norm_fwd": ([_p] * 7 + [_i, _p] + [_i] * 8 + [_f, _f] + [_p] * 5, _i),
+    "slim_qk_norm_bwd_workspace_size": ([_i] * 5 + [ctypes.POINTER(_sz)], _i),
+    "slim_qk_norm_bwd": ([_p] * 7 + [_i, _p] + [_i] * 8 + [_f, _f] + [_p] * 11 + [_sz, _p], _i),
 }
 
 
@@ -772,3 +775,185 @@ def vocab_loss(x, w, targets, reduction="mean", ignore_index=-100, piece=None):
     [V, D]; reduction "mean" (over the rows not ignored), "sum" or "none"."""
     _require(reduction in ("mean", "sum", "none"), "reduction must be 'mean', 'sum' or 'none'")
     return VocabLoss.apply(_ready(x), _ready(w), targets, reduction, ignore_index, piece)
+
+
+# ---------------------------------------------------------------- around the attention
+def _on_device(t):
+    """The context in which a call on tensor t launches: its device as the current one."""
+    return _HERE if t.get_device() == torch.cuda.current_device() else torch.cuda.device(t.device)
+
+
+def _one_device(*ts):
+    """CUDA tensors (None: left out), all on one device."""
+    dev = None
+    for t in ts:
+        if t is None:
+            continue
+        if not t.is_cuda:
+            raise RuntimeError("libslim runs on CUDA tensors only (no CPU fallback)")
+        if dev is None:
+            dev = t.device
+        elif t.device != dev:
+            raise ValueError("tensors on different devices")
+
+
+def _fp32_or_none(t, shape, what):
+    if t is not None and (t.dtype != torch.float32 or tuple(t.shape) != shape or not t.is_contiguous()):
+        raise ValueError(f"{what} must be contiguous fp32 of shape {list(shape)}")
+    return None if t is None else t.data_ptr()
+
+
+def rotary_frequencies(rotary, base=10000.0):
+    """Radians per position of the rotary / 2 pairs: base^(-2 p / rotary)."""
+    _require(rotary >= 0 and rotary % 2 == 0, "rotary must be even")
+    return array.array("d", [base ** (-2.0 * p / rotary) for p in range(rotary // 2)])
+
+
+class _QkCall:
+    """What both directions of qk_norm marshal alike."""
+
+    def __init__(self, q, k, q_weight, k_weight, positions, inv_freq, what):
+        if q.dim() != 4 or (k is not None and k.dim() != 4):
+            raise ValueError("q and k must be [B, H, L, d]")
+        B, Hq, L, d = self.dims = q.shape
+        Hk = 0 if k is None else k.shape[1]
+        if k is not None and (k.dtype != q.dtype or tuple(k.shape) != (B, Hk, L, d)):
+            raise ValueError("k must be [B, Hk, L, d] in q's dtype")
+        if (B | Hq | Hk | L | d) >> 31:
+            _too_large()
+        if inv_freq is None:
+            inv_freq = ()
+        elif isinstance(inv_freq, torch.Tensor) and inv_freq.is_cuda:
+            raise TypeError("inv_freq is read on the host: give numbers or a CPU tensor")
+        if not (isinstance(inv_freq, array.array) and inv_freq.typecode == "d"):
+            inv_freq = array.array("d", map(float, inv_freq))
+        self.freq, rotary = inv_freq, 2 * len(inv_freq)
+        _require(rotary <= d, "more frequencies than pairs of features")
+        ptype = 0
+        if positions is not None:
+            ptype = _index_code(positions, "positions")
+            if tuple(positions.shape) != (B, L) or not positions.is_contiguous():
+                raise ValueError("positions must be contiguous [B, L]")
+        _one_device(q, k, q_weight, k_weight, positions)
+        self.keep, self.shapes = [], ((B, Hq, L, d), (B, Hk, L, d))
+        self.head = (*self.rows(q, 0), *self.rows(k, 1), _fp32_or_none(q_weight, (d,), "q_weight"),
+                     _fp32_or_none(k_weight, (d,), "k_weight"), _ptr(positions), ptype,
+                     inv_freq.buffer_info()[0] if rotary else None, rotary)
+        self.sizes = (B, Hq, Hk, L, d, _dtype_code(q, what))
+
+    def rows(self, t, side):
+        """A [B, H, L, d] tensor's pointer and strides; the last dimension is contiguous."""
+        if t is None:
+            return None, None
+        b, h, l, one = t.stride()
+        if one != 1 and t.shape[3] > 1:
+            raise RuntimeError("libslim needs rows whose features are contiguous")
+        strides = array.array("q", (b, h, l))
+        self.keep.append(strides)
+        return t.data_ptr(), strides.buffer_info()[0]
+
+    def like(self, t, side, given, what, other):
+        """`given`, checked, or a new contiguous tensor for the side that t is of."""
+        if given is None:
+            return None if t is None else torch.empty(self.shapes[side], dtype=t.dtype, device=t.device)
+        if t is None or given.dtype != other.dtype or tuple(given.shape) != self.shapes[side]:
+            raise ValueError(f"{what} must have the shape and dtype of its input")
+        _one_device(t, given)
+        return given
+
+
+def qk_norm_forward(q, k, q_weight=None, k_weight=None, positions=None, inv_freq=None, interleaved=False,
+                    eps=1e-6, scale=1.0, q_out=None, k_out=None, stream=None):
+    """slim_qk_norm_fwd: the root-mean-square norm of queries and keys per head,
+    times scale and weight ([d] fp32 or None), and the rotation of their first
+    2 * len(inv_freq) features by position.  q [B, Hq, L, d] and k [B, Hk, L, d]
+    (or None) may be slices and transposes of a projection's rows as long as
+    the features are contiguous.  positions: int [B, L], None counts from 0;
+    inv_freq: radians per position on the host (see rotary_frequencies), None:
+    no rotation.  Returns (q_out, k_out), contiguous unless given; they may be q
+    and k themselves."""
+    c = _QkCall(q, k, q_weight, k_weight, positions, inv_freq, "qk_norm_forward")
+    with _on_device(q):
+        with _on(stream):
+            q_out = c.like(q, 0, q_out, "q_out", q)
+            k_out = c.like(k, 1, k_out, "k_out", k)
+        _check(library().slim_qk_norm_fwd(*c.head, int(interleaved), *c.sizes, eps, scale,
+                                          *c.rows(q_out, 0), *c.rows(k_out, 1),
+                                          _stream_of(q, stream)), "slim_qk_norm_fwd")
+    return q_out, k_out
+
+
+@functools.lru_cache(maxsize=1024)
+def qk_norm_workspace_size(B, Hq, Hk, L, d):
+    n = _sz(0)
+    if (B | Hq | Hk | L | d) >> 31:
+        _too_large()
+    _check(library().slim_qk_norm_bwd_workspace_size(B, Hq, Hk, L, d, ctypes.byref(n)),
+           "slim_qk_norm_bwd_workspace_size")
+    return n.value
+
+
+def qk_norm_backward(q, k, q_weight, k_weight, dq_out, dk_out, positions=None, inv_freq=None,
+                     interleaved=False, eps=1e-6, scale=1.0, dq=None, dk=None, weights=True,
+                     workspace=None, stream=None):
+    """slim_qk_norm_bwd: returns (dq, dk, dq_weight, dk_weight), the gradients of
+    <dq_out, q_out> + <dk_out, k_out> for the same arguments as in the forward.
+    dq and dk are contiguous unless given: slices of the projection's gradient,
+    or dq_out and dk_out themselves.  A weight's gradient ([d] fp32) is None
+    where there is no such weight or with weights=False."""
+    c = _QkCall(q, k, q_weight, k_weight, positions, inv_freq, "qk_norm_backward")
+    c.like(q, 0, dq_out, "dq_out", q)
+    c.like(k, 1, dk_out, "dk_out", k)
+    if dq_out is None or (k is not None and dk_out is None):
+        raise ValueError("dq_out and dk_out are needed")
+    if workspace is not None:
+        _require_cuda(workspace)
+    B, Hq, Hk, L, d, _ = c.sizes
+    with _on_device(q):
+        with _on(stream):
+            dq = c.like(q, 0, dq, "dq", q)
+            dk = c.like(k, 1, dk, "dk", k)
+            dwq, dwk = (torch.empty_like(w) if weights and w is not None else None
+                        for w in (q_weight, k_weight))
+            ws = workspace if workspace is not None else _workspace(
+                qk_norm_workspace_size(B, Hq, Hk, L, d), q.device)
+        _check(library().slim_qk_norm_bwd(*c.head, int(interleaved), *c.sizes, eps, scale,
+                                          *c.rows(dq_out, 0), *c.rows(dk_out, 1), *c.rows(dq, 0),
+                                          *c.rows(dk, 1), _ptr(dwq), _ptr(dwk), ws.data_ptr(),
+                                          ws.numel(), _stream_of(q, stream)), "slim_qk_norm_bwd")
+    return dq, dk, dwq, dwk
+
+
+def _dense_rows(t):
+    """t with contiguous features: itself, or a copy."""
+    return t if t is None or t.stride(-1) == 1 or t.shape[-1] == 1 else t.contiguous()
+
+
+class QkNorm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, q_weight, k_weight, positions, inv_freq, interleaved, eps, scale):
+        ctx.save_for_backward(q, k, q_weight, k_weight, positions)
+        ctx.how = dict(inv_freq=inv_freq, interleaved=interleaved, eps=eps, scale=scale)
+        q_out, k_out = qk_norm_forward(_dense_rows(q), _dense_rows(k), q_weight, k_weight,
+                                       positions=positions, **ctx.how)
+        return q_out, k_out
+
+    @staticmethod
+    def backward(ctx, dq_out, dk_out):
+        q, k, q_weight, k_weight, positions = ctx.saved_tensors
+        grads = qk_norm_backward(_dense_rows(q), _dense_rows(k), q_weight, k_weight,
+                                 _dense_rows(dq_out), _dense_rows(dk_out), positions=positions,
+                                 weights=any(ctx.needs_input_grad[2:4]), **ctx.how)
+        there = [i for i, g in enumerate(grads) if g is not None]
+        tied = _first_derivatives(tuple(grads[i] for i in there), *(
+            t for t in (q, k, q_weight, k_weight, dq_out, dk_out) if t is not None))
+        out = [None] * 4
+        for i, g in zip(there, tied):
+            out[i] = g
+        return *out, None, None, None, None, None
+
+
+def qk_norm(q, k, q_weight=None, k_weight=None, positions=None, inv_freq=None, interleaved=False,
+            eps=1e-6, scale=1.0):
+    """Differentiable (once) qk_norm_forward: gradients with respect to q, k and the weights."""
+    return QkNorm.apply(q, k, q_weight, k_weight, positions, inv_freq, interleaved, eps, scale)

@@ -1,0 +1,163 @@
+"""Host-only checks of the entry points around the attention (include/slim_layer.h):
+sizes, and refusals before anything is enqueued.  No call here reaches a CUDA launch;
+the pointers are never dereferenced."""
+import ctypes
+import os
+import re
+
+import pytest
+import torch
+
+import layer_common as ref
+from paper_2012_11346_gb300 import slim
+
+OK, INVALID, UNSUPPORTED, WORKSPACE = 0, 1, 2, 3
+FAKE = 0x10000
+F32, BF16, I32, I64 = 0, 1, 0, 1
+
+
+@pytest.fixture(scope="module")
+def lib():
+    if not os.path.exists(slim._LIB_PATH):
+        from paper_2012_11346_gb300 import build
+        build.build()
+    return slim.library()
+
+
+def test_every_declared_symbol_is_bound(lib):
+    header = open(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include",
+                               "slim_layer.h")).read()
+    names = set(re.findall(r"^slim_status (slim_\w+)\(", header, re.M))
+    assert names
+    for n in names:
+        assert n in slim.SIGNATURES and getattr(lib, n)
+
+
+# ---------------------------------------------------------------- norms of queries and keys
+def strides(*s):
+    return (ctypes.c_longlong * 3)(*s)
+
+
+def freqs(*f):
+    return (ctypes.c_double * max(1, len(f)))(*f)
+
+
+def qk_fwd(lib, q=FAKE, qs=None, k=FAKE, ks=None, wq=FAKE, wk=FAKE, pos=FAKE, pt=I64, freq=freqs(1.0, 0.1), rotary=4,
+           inter=0, B=2, Hq=2, Hk=2, L=3, d=8, dt=F32, eps=1e-6, scale=1.0, qo=FAKE, qos=None, ko=FAKE, kos=None):
+    return lib.slim_qk_norm_fwd(q, qs, k, ks, wq, wk, pos, pt, freq, rotary, inter, B, Hq, Hk, L, d, dt, eps, scale,
+                                qo, qos, ko, kos, None)
+
+
+def qk_bwd(lib, q=FAKE, qs=None, k=FAKE, ks=None, wq=FAKE, wk=FAKE, pos=FAKE, pt=I64, freq=freqs(1.0, 0.1), rotary=4,
+           inter=0, B=2, Hq=2, Hk=2, L=3, d=8, dt=F32, eps=1e-6, scale=1.0, qo=FAKE, qos=None, ko=FAKE, kos=None,
+           dq=FAKE, dqs=None, dk=FAKE, dks=None, dwq=FAKE, dwk=FAKE, ws=FAKE, nbytes=1 << 40):
+    return lib.slim_qk_norm_bwd(q, qs, k, ks, wq, wk, pos, pt, freq, rotary, inter, B, Hq, Hk, L, d, dt, eps, scale,
+                                qo, qos, ko, kos, dq, dqs, dk, dks, dwq, dwk, ws, nbytes, None)
+
+
+BIG = 1 << 40
+QK_BAD = [
+    dict(B=-1), dict(L=-1), dict(B=1 << 16, L=1 << 15), dict(Hq=0), dict(Hk=-1), dict(Hq=4097), dict(Hk=4097),
+    dict(d=0), dict(d=257), dict(dt=2), dict(rotary=-2), dict(rotary=3), dict(rotary=10), dict(inter=2), dict(inter=-1),
+    dict(freq=None), dict(pt=2), dict(freq=freqs(1.0, float("nan"))), dict(freq=freqs(float("inf"), 1.0)),
+    dict(eps=0.0), dict(eps=-1.0), dict(eps=float("nan")), dict(eps=float("inf")), dict(scale=float("nan")),
+    dict(scale=float("inf")), dict(q=None), dict(k=None), dict(qo=None), dict(ko=None), dict(q=FAKE + 2), dict(k=FAKE + 1),
+    dict(qo=FAKE + 2), dict(dt=BF16, ko=FAKE + 1), dict(wq=FAKE + 2), dict(wk=FAKE + 1), dict(pos=FAKE + 4),
+    dict(pt=I32, pos=FAKE + 2), dict(qs=strides(-1, 24, 8)), dict(ks=strides(48, 24, BIG + 1)),
+    dict(qs=strides(BIG, BIG, BIG), B=1 << 22, L=1, Hq=1), dict(B=1 << 15, L=1 << 15, Hq=4096)]
+
+
+@pytest.mark.parametrize("kw", QK_BAD)
+def test_qk_rejects(lib, kw):
+    assert qk_fwd(lib, **kw) == INVALID
+    assert qk_bwd(lib, **kw) == INVALID
+
+
+# written tensors whose elements share places
+@pytest.mark.parametrize("s", [(48, 24, 0), (48, 24, 7), (0, 24, 8), (48, 0, 8), (24, 24, 8), (47, 24, 8), (48, 8, 8),
+                               (8, 16, 16)])
+def test_qk_rejects_shared_places(lib, s):
+    assert qk_fwd(lib, qos=strides(*s)) == INVALID
+    assert qk_fwd(lib, kos=strides(*s)) == INVALID
+    assert qk_bwd(lib, dqs=strides(*s)) == INVALID
+    assert qk_bwd(lib, dks=strides(*s)) == INVALID
+
+
+def test_qk_rejects_more(lib):
+    for bad in (None, FAKE + 2):
+        assert qk_bwd(lib, dq=bad) == INVALID
+        assert qk_bwd(lib, dk=bad) == INVALID
+    assert qk_bwd(lib, dwq=FAKE + 2) == INVALID and qk_bwd(lib, dwk=FAKE + 1) == INVALID
+    need = slim.qk_norm_workspace_size(2, 2, 2, 3, 8)
+    assert qk_bwd(lib, nbytes=need - 1) == WORKSPACE and qk_bwd(lib, ws=None) == WORKSPACE
+    assert qk_bwd(lib, ws=FAKE + 16) == INVALID
+    assert lib.slim_qk_norm_bwd_workspace_size(2, 2, 2, 3, 8, None) == INVALID
+    n = ctypes.c_size_t()
+    assert lib.slim_qk_norm_bwd_workspace_size(2, 0, 2, 3, 8, ctypes.byref(n)) == INVALID
+    # a fixed number of blocks, whatever the length
+    assert slim.qk_norm_workspace_size(1, 1, 1, 1, 8) == slim.qk_norm_workspace_size(8, 8, 8, 1 << 20, 8)
+
+
+def test_qk_without_rows_enqueues_nothing(lib):
+    for kw in (dict(B=0), dict(L=0)):
+        assert qk_fwd(lib, q=None, k=None, qo=None, ko=None, **kw) == OK
+        assert qk_bwd(lib, q=None, k=None, qo=None, ko=None, dq=None, dk=None, dwq=None, dwk=None, ws=None, nbytes=0,
+                      **kw) == OK
+
+
+def test_qk_binding(monkeypatch):
+    q = torch.zeros(1, 2, 3, 8)
+    with pytest.raises(RuntimeError, match="CUDA"):
+        slim.qk_norm_forward(q, q)
+    monkeypatch.setattr(slim, "_one_device", lambda *t: None)
+    bad = [
+        (ValueError, lambda: slim.qk_norm_forward(q[0], q)),
+        (ValueError, lambda: slim.qk_norm_forward(q, q.bfloat16())),
+        (ValueError, lambda: slim.qk_norm_forward(q, q[:, :, :2])),
+        (TypeError, lambda: slim.qk_norm_forward(q.half(), None)),
+        (ValueError, lambda: slim.qk_norm_forward(q, q, torch.ones(7))),
+        (ValueError, lambda: slim.qk_norm_forward(q, q, torch.ones(8).bfloat16())),
+        (ValueError, lambda: slim.qk_norm_forward(q, q, positions=torch.zeros(3, dtype=torch.long))),
+        (TypeError, lambda: slim.qk_norm_forward(q, q, positions=torch.zeros(1, 3))),
+        (ValueError, lambda: slim.qk_norm_forward(q, q, inv_freq=[1.0] * 5)),
+        (RuntimeError, lambda: slim.qk_norm_forward(q.transpose(2, 3).contiguous().transpose(2, 3), q)),
+        (ValueError, lambda: slim.qk_norm_forward(q.expand(1 << 32, 2, 3, 8), None)),
+        (ValueError, lambda: slim.qk_norm_backward(q, q, None, None, q, None)),
+        (ValueError, lambda: slim.qk_norm_backward(q, q, None, None, q, q[:, :1])),
+        (ValueError, lambda: slim.qk_norm_backward(q, None, None, None, q, q)),
+        (ValueError, lambda: slim.rotary_frequencies(3)),
+    ]
+    for kind, call in bad:
+        with pytest.raises(kind):
+            call()
+
+
+# ---------------------------------------------------------------- the formulas themselves
+def test_qk_formula_against_differences():
+    """The gradient that the kernels compute, r (g - n mean(g n)) after turning back,
+    against central differences of the definition."""
+    g = torch.Generator().manual_seed(0)
+    x = torch.randn(1, 2, 3, 6, generator=g, dtype=torch.float64)
+    w = 1 + 0.3 * torch.randn(6, generator=g, dtype=torch.float64)
+    up = torch.randn(1, 2, 3, 6, generator=g, dtype=torch.float64)
+    freq = [1.0, 0.1]
+
+    def f(a, b):
+        return (ref.qk64(a, b, None, freq, False, 1e-6, 0.7) * up).sum()
+
+    back = ref.angles64(None, freq, 1, 3, "cpu")
+    dz = up.clone()
+    i, k = ref.pairs_of(6, 2, False)
+    dz[..., i], dz[..., k] = up[..., i] * back.cos() + up[..., k] * back.sin(), up[..., k] * back.cos() - up[..., i] * back.sin()
+    dz = 0.7 * dz
+    r = 1 / (x.square().mean(-1, keepdim=True) + 1e-6).sqrt()
+    n = x * r
+    dx = r * (dz * w - n * (dz * w * n).mean(-1, keepdim=True))
+    dw = (dz * n).sum((0, 1, 2))
+    h = 1e-6
+    for t, grad, call in ((x, dx, lambda e: f(x + e, w)), (w, dw, lambda e: f(x, w + e))):
+        for j in range(t.numel()):
+            e = torch.zeros_like(t).view(-1)
+            e[j] = h
+            e = e.view_as(t)
+            assert abs((call(e) - call(-e)) / (2 * h) - grad.reshape(-1)[j]) < 1e-7
