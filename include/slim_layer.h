@@ -5,6 +5,9 @@
  *   slim_qk_norm_*     the root-mean-square norm of queries and keys per head
  *                      and their rotation by position, in one pass from a
  *                      projection's rows to the [B, H, L, d] that slim_fwd takes
+ *   slim_gated_scan_*  a gated linear recurrence per channel, the sibling of the
+ *                      attention's prefix state that forgets, with the same
+ *                      carries in and out of a segment
  *
  * The conventions of slim.h hold: device pointers, every buffer owned by the
  * caller, arguments validated before anything is enqueued, all work on
@@ -80,6 +83,62 @@ slim_status slim_qk_norm_bwd(const void* q, const slim_strides* q_strides, const
                              const slim_strides* dq_strides, void* dk,
                              const slim_strides* dk_strides, float* dq_weight, float* dk_weight,
                              void* workspace, size_t workspace_bytes, void* stream);
+
+/* How a gate g and an input x make a step h_t = a_t h_(t-1) + u_t. */
+typedef enum {
+  SLIM_GATE_VALUE = 0,  /* a = g,          u = x */
+  SLIM_GATE_LOG = 1,    /* a = exp(g),     u = x */
+  SLIM_GATE_SIGMOID = 2 /* a = sigmoid(g), u = (1 - a) x = sigmoid(-g) x */
+} slim_gate;
+
+/* Steps between the states that a forward keeps for its backward. */
+#define SLIM_SCAN_CHUNK 64
+
+/*
+ * h_t = a_t h_(t-1) + u_t for every channel of every sequence, from h_0.
+ *   gate, x  [B, L, D] dtype: element (b, t, c) at ((b L + t) pitch + c), aligned
+ *            to their element size; pitch > D reads a slice of a projection's
+ *            rows, pitch 0 one row for all.
+ *   h0       [B, D] fp32, or null (zero): a segment starts from the last state of
+ *            the one before.
+ *   h        [B, L, D] dtype, written.
+ *   last     [B, D] fp32, written (the state after the last step), or null; it may
+ *            be h0 itself.
+ *   kept     [B, ceil(L / SLIM_SCAN_CHUNK), D] fp32, written (the state before each
+ *            chunk), or null: what slim_gated_scan_bwd reads.
+ *   workspace of slim_gated_scan_workspace_size(..., backward = 0) bytes (none up to
+ *            SLIM_SCAN_CHUNK steps).
+ * States and sums are fp32, h is rounded once.  A gate of zero (VALUE 0, LOG or
+ * SIGMOID -inf) starts anew: nothing before it reaches h, finite or not.  A state
+ * that is not finite stays in its channel until such a gate, or until the gates'
+ * product since sinks below fp32's range.  Gates beyond 1 may grow a state past
+ * fp32's range; so may the product of SLIM_SCAN_CHUNK of them alone.
+ * Nothing written overlaps anything else but as said.
+ * 0 <= B < 2^16, 0 <= L <= 2^30, 1 <= D <= 2^30, B D <= 2^36, B L D <= 2^40,
+ * D <= pitch (0 <= pitch for inputs) <= 2^40, offsets below 2^60.  With B L = 0 the
+ * state is passed on.
+ */
+slim_status slim_gated_scan_workspace_size(int B, int L, int D, int backward, size_t* bytes);
+slim_status slim_gated_scan_fwd(const void* gate, long long gate_pitch, const void* x,
+                                long long x_pitch, const float* h0, int B, int L, int D,
+                                slim_dtype dtype, slim_gate kind, void* h, float* last, float* kept,
+                                void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * The gradients of <dh, h> + <dlast, last> with respect to gate, x and h0.
+ *   kept     from the forward on the same gate, x and h0; the states inside a chunk
+ *            are computed again from it, in fp32.
+ *   dh       [B, L, D] dtype;  dlast [B, D] fp32, or null (zero).
+ *   dgate, dx  [B, L, D] dtype with pitches of their own, written.
+ *   dh0      [B, D] fp32, written, or null; it may be dlast itself.
+ * Where a step starts anew its LOG or SIGMOID gate has gradient 0.
+ */
+slim_status slim_gated_scan_bwd(const void* gate, long long gate_pitch, const void* x,
+                                long long x_pitch, const float* kept, const void* dh,
+                                const float* dlast, int B, int L, int D, slim_dtype dtype,
+                                slim_gate kind, void* dgate, long long dgate_pitch, void* dx,
+                                long long dx_pitch, float* dh0, void* workspace,
+                                size_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

@@ -18,7 +18,8 @@ const char* kNames[K_COUNT] = {
     "tc_reduce",   "tc_selftest",   "tc_prep",        "stack_rows",
     "embed_fwd",   "embed_sort",    "embed_sum",  "embed_join",    "clip",          "loss_prep",
     "loss_stats",  "loss_join",     "loss_softmax",   "loss_grad",
-    "loss_rows",   "loss_parts",  "qk_norm",       "qk_weights"};
+    "loss_rows",   "loss_parts",  "qk_norm",       "qk_weights",
+    "scan_sums",   "scan_states",   "scan_fwd",    "scan_bwd"};
 
 struct Rec {
   Kid k;

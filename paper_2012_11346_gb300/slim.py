@@ -64,6 +64,9 @@ SIGNATURES = {
     "slim_clip_grads": ([_p, _p, _p, _p, _i, _f, _p, _p, _sz, _p], _i),
     "slim_qk_norm_fwd": ([_p] * 7 + [_i, _p] + [_i] * 8 + [_f, _f] + [_p] * 5, _i),
     "slim_qk_norm_bwd_workspace_size": ([_i] * 5 + [ctypes.POINTER(_sz)], _i),
+    "slim_gated_scan_workspace_size": ([_i] * 4 + [ctypes.POINTER(_sz)], _i),
+    "slim_gated_scan_fwd": ([_p, _ll, _p, _ll, _p] + [_i] * 5 + [_p] * 4 + [_sz, _p], _i),
+    "slim_gated_scan_bwd": ([_p, _ll, _p, _ll] + [_p] * 3 + [_i] * 5 + [_p, _ll, _p, _ll, _p, _p, _sz, _p], _i),
     "slim_qk_norm_bwd": ([_p] * 7 + [_i, _p] + [_i] * 8 + [_f, _f] + [_p] * 11 + [_sz, _p], _i),
 }
 
@@ -957,3 +960,149 @@ def qk_norm(q, k, q_weight=None, k_weight=None, positions=None, inv_freq=None, i
             eps=1e-6, scale=1.0):
     """Differentiable (once) qk_norm_forward: gradients with respect to q, k and the weights."""
     return QkNorm.apply(q, k, q_weight, k_weight, positions, inv_freq, interleaved, eps, scale)
+
+
+GATES = {"value": 0, "log": 1, "sigmoid": 2}
+SCAN_CHUNK = 64
+
+
+@functools.lru_cache(maxsize=1024)
+def gated_scan_workspace_size(B, L, D, backward):
+    n = _sz(0)
+    if (B | L | D) >> 31:
+        _too_large()
+    _check(library().slim_gated_scan_workspace_size(B, L, D, int(backward), ctypes.byref(n)),
+           "slim_gated_scan_workspace_size")
+    return n.value
+
+
+def _pitch(t, what):
+    """Elements from a row of [B, L, D] to the next; a slice of wider rows has one, too."""
+    B, L, D = t.shape
+    b, l, one = t.stride()
+    if D > 1 and one != 1:
+        raise RuntimeError(f"{what}: libslim needs rows whose channels are contiguous")
+    if L > 1:
+        pitch, whole = l, B <= 1 or b == L * l
+    else:
+        pitch, whole = (b if B > 1 else D), True
+    if not whole:
+        raise RuntimeError(f"{what}: libslim needs rows at one distance from each other")
+    return pitch
+
+
+def _scan_dims(gate, x, kind, what):
+    if gate.dim() != 3 or gate.shape != x.shape:
+        raise ValueError("gate and x must be [B, L, D]")
+    if gate.dtype != x.dtype:
+        raise TypeError(f"{what}: one dtype expected, got {gate.dtype} and {x.dtype}")
+    _require(kind in GATES, f"kind must be one of {', '.join(GATES)}")
+    B, L, D = gate.shape
+    if (B | L | D) >> 31:
+        _too_large()
+    return B, L, D, _dtype_code(gate, what), GATES[kind]
+
+
+def gated_scan_forward(gate, x, kind="sigmoid", h0=None, keep=False, last=None, workspace=None, stream=None):
+    """slim_gated_scan_fwd: h_t = a_t h_(t-1) + u_t per channel, gate and x [B, L, D]
+    (slices of a projection's rows are read where they are).  kind "value": a =
+    gate, u = x; "log": a = exp(gate), u = x; "sigmoid": a = sigmoid(gate), u =
+    (1 - a) x.  h0: the state to start from, [B, D] fp32 or None (zero).  Returns
+    (h, last): all states in x's dtype and the last in fp32 (into `last` if given,
+    which may be h0); with keep=True also what gated_scan_backward needs."""
+    B, L, D, dt, code = _scan_dims(gate, x, kind, "gated_scan_forward")
+    _one_device(gate, x, h0, last)
+    h0p = _fp32_or_none(h0, (B, D), "h0")
+    _fp32_or_none(last, (B, D), "last")
+    if workspace is not None:
+        _require_cuda(workspace)
+    with _on_device(x):
+        with _on(stream):
+            h = torch.empty(B, L, D, dtype=x.dtype, device=x.device)
+            if last is None:
+                last = torch.empty(B, D, dtype=torch.float32, device=x.device)
+            kept = (torch.empty(B, -(-L // SCAN_CHUNK), D, dtype=torch.float32, device=x.device)
+                    if keep else None)
+            ws = workspace
+            if ws is None and L > SCAN_CHUNK:
+                ws = _workspace(gated_scan_workspace_size(B, L, D, False), x.device)
+        _check(library().slim_gated_scan_fwd(gate.data_ptr(), _pitch(gate, "gate"), x.data_ptr(),
+                                             _pitch(x, "x"), h0p, B, L, D, dt, code, h.data_ptr(),
+                                             last.data_ptr(), _ptr(kept), _ptr(ws),
+                                             0 if ws is None else ws.numel(), _stream_of(x, stream)),
+               "slim_gated_scan_fwd")
+    return (h, last, kept) if keep else (h, last)
+
+
+def gated_scan_backward(gate, x, kept, dh, kind="sigmoid", dlast=None, dgate=None, dx=None, dh0=None,
+                        workspace=None, stream=None):
+    """slim_gated_scan_bwd: returns (dgate, dx, dh0), the gradients of <dh, h> +
+    <dlast, last>.  kept: from gated_scan_forward(..., keep=True) on the same inputs;
+    dlast: [B, D] fp32 or None (zero).  dgate and dx are contiguous unless given
+    (slices of the projection's gradient); dh0 may be given, too, also as dlast."""
+    B, L, D, dt, code = _scan_dims(gate, x, kind, "gated_scan_backward")
+    _one_device(gate, x, kept, dh, dlast, dgate, dx, dh0)
+    if tuple(dh.shape) != (B, L, D) or dh.dtype != x.dtype or not dh.is_contiguous():
+        raise ValueError("dh must be contiguous [B, L, D] in x's dtype")
+    dlp = _fp32_or_none(dlast, (B, D), "dlast")
+    _fp32_or_none(dh0, (B, D), "dh0")
+    if kept is None:
+        raise ValueError("kept must be the forward's")
+    _fp32_or_none(kept, (B, -(-L // SCAN_CHUNK), D), "kept")
+    for t in (dgate, dx):
+        if t is not None and (tuple(t.shape) != (B, L, D) or t.dtype != x.dtype):
+            raise ValueError("dgate and dx must be [B, L, D] in x's dtype")
+    if workspace is not None:
+        _require_cuda(workspace)
+    with _on_device(x):
+        with _on(stream):
+            if dgate is None:
+                dgate = torch.empty(B, L, D, dtype=x.dtype, device=x.device)
+            if dx is None:
+                dx = torch.empty(B, L, D, dtype=x.dtype, device=x.device)
+            if dh0 is None:
+                dh0 = torch.empty(B, D, dtype=torch.float32, device=x.device)
+            ws = workspace
+            if ws is None and L > SCAN_CHUNK:
+                ws = _workspace(gated_scan_workspace_size(B, L, D, True), x.device)
+        _check(library().slim_gated_scan_bwd(gate.data_ptr(), _pitch(gate, "gate"), x.data_ptr(),
+                                             _pitch(x, "x"), kept.data_ptr(), dh.data_ptr(), dlp, B,
+                                             L, D, dt, code, dgate.data_ptr(), _pitch(dgate, "dgate"),
+                                             dx.data_ptr(), _pitch(dx, "dx"), dh0.data_ptr(),
+                                             _ptr(ws), 0 if ws is None else ws.numel(),
+                                             _stream_of(x, stream)), "slim_gated_scan_bwd")
+    return dgate, dx, dh0
+
+
+def _even_rows(t):
+    """t with contiguous channels and its rows at one distance: itself, or a copy."""
+    try:
+        return t if _pitch(t, "") >= 0 else t.contiguous()
+    except RuntimeError:
+        return t.contiguous()
+
+
+class GatedScan(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, gate, x, kind, h0):
+        h, last, kept = gated_scan_forward(_even_rows(gate), _even_rows(x), kind,
+                                           None if h0 is None else h0.contiguous(), keep=True)
+        ctx.save_for_backward(gate, x, h0, kept)
+        ctx.kind = kind
+        return h, last
+
+    @staticmethod
+    def backward(ctx, dh, dlast):
+        gate, x, h0, kept = ctx.saved_tensors
+        grads = gated_scan_backward(_even_rows(gate), _even_rows(x), kept, dh.contiguous(), ctx.kind,
+                                    dlast=dlast.contiguous())
+        if h0 is None:
+            grads = grads[:2]
+        tied = _first_derivatives(grads, *(t for t in (gate, x, h0, dh, dlast) if t is not None))
+        return tied[0], tied[1], None, (tied[2] if h0 is not None else None)
+
+
+def gated_scan(gate, x, kind="sigmoid", h0=None):
+    """Differentiable (once) gated_scan_forward: returns (h, last), with gradients with
+    respect to gate, x and h0."""
+    return GatedScan.apply(gate, x, kind, h0)

@@ -66,8 +66,7 @@ def scan64(gate, x, kind, h0=None):
     h = torch.zeros_like(x[:, 0]) if h0 is None else h0
     out = []
     for t in range(x.shape[1]):
-        # a gate of zero forgets whatever the state holds
-        h = torch.where(a[:, t] == 0, 0.0, a[:, t] * torch.where(a[:, t] == 0, 0.0, h)) + b[:, t] * x[:, t]
+        h = a[:, t] * h + b[:, t] * x[:, t]
         out.append(h)
     return torch.stack(out, 1), h
 

@@ -161,3 +161,89 @@ def test_qk_formula_against_differences():
             e[j] = h
             e = e.view_as(t)
             assert abs((call(e) - call(-e)) / (2 * h) - grad.reshape(-1)[j]) < 1e-7
+
+
+# ---------------------------------------------------------------- gated recurrence
+def scan_fwd(lib, gate=FAKE, gp=8, x=FAKE, xp=8, h0=FAKE, B=2, L=100, D=8, dt=F32, kind=0, h=FAKE, last=FAKE, kept=FAKE,
+             ws=FAKE, nbytes=1 << 40):
+    return lib.slim_gated_scan_fwd(gate, gp, x, xp, h0, B, L, D, dt, kind, h, last, kept, ws, nbytes, None)
+
+
+def scan_bwd(lib, gate=FAKE, gp=8, x=FAKE, xp=8, kept=FAKE, h=FAKE, last=FAKE, B=2, L=100, D=8, dt=F32, kind=0, dg=FAKE,
+             dgp=8, dx=FAKE, dxp=8, h0=FAKE, ws=FAKE, nbytes=1 << 40):
+    return lib.slim_gated_scan_bwd(gate, gp, x, xp, kept, h, last, B, L, D, dt, kind, dg, dgp, dx, dxp, h0, ws, nbytes,
+                                   None)
+
+
+@pytest.mark.parametrize("kw", [
+    dict(B=-1), dict(B=1 << 16), dict(L=-1), dict(L=(1 << 30) + 1), dict(D=0), dict(D=(1 << 30) + 1), dict(dt=2),
+    dict(kind=3), dict(kind=-1), dict(gate=None), dict(x=None), dict(h=None), dict(gate=FAKE + 2), dict(x=FAKE + 1),
+    dict(h=FAKE + 2), dict(dt=BF16, h=FAKE + 1), dict(gp=-1), dict(xp=-8), dict(gp=BIG + 1), dict(h0=FAKE + 2),
+    dict(last=FAKE + 1), dict(kept=FAKE + 2), dict(ws=FAKE + 16), dict(B=60000, L=1 << 30, D=1 << 10),
+    dict(B=60000, L=1, D=1 << 25), dict(L=1 << 30, D=1, gp=1 << 35)])
+def test_scan_rejects(lib, kw):
+    assert scan_fwd(lib, **kw) == INVALID
+    assert scan_bwd(lib, **kw) == INVALID
+
+
+def test_scan_rejects_more(lib):
+    for kw in (dict(dg=None), dict(dx=None), dict(dg=FAKE + 2), dict(dx=FAKE + 1), dict(dgp=7), dict(dxp=0), dict(kept=None)):
+        assert scan_bwd(lib, **kw) == INVALID
+    for back, call in ((False, scan_fwd), (True, scan_bwd)):
+        need = slim.gated_scan_workspace_size(2, 100, 8, back)
+        assert call(lib, nbytes=need - 1) == WORKSPACE and call(lib, ws=None) == WORKSPACE
+        assert slim.gated_scan_workspace_size(2, 64, 8, back) == 0
+        # grows with the chunks, not the steps' values
+        assert slim.gated_scan_workspace_size(1, 1 << 16, 512, back) <= (1 << 16) * 512 // 64 * 12 + 512
+    assert lib.slim_gated_scan_workspace_size(2, 100, 8, 0, None) == INVALID
+    assert lib.slim_gated_scan_workspace_size(2, 100, 8, 2, ctypes.byref(ctypes.c_size_t())) == INVALID
+
+
+def test_scan_constant_is_the_headers():
+    header = open(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include",
+                               "slim_layer.h")).read()
+    assert int(re.search(r"#define SLIM_SCAN_CHUNK (\d+)", header).group(1)) == slim.SCAN_CHUNK
+
+
+def test_scan_binding(monkeypatch):
+    x = torch.zeros(2, 70, 8)
+    with pytest.raises(RuntimeError, match="CUDA"):
+        slim.gated_scan_forward(x, x)
+    monkeypatch.setattr(slim, "_one_device", lambda *t: None)
+    monkeypatch.setattr(slim, "_on_device", lambda t: slim._HERE)
+    monkeypatch.setattr(slim, "library", lambda: (_ for _ in ()).throw(AssertionError("reached")))
+    h0, kept = torch.zeros(2, 8), torch.zeros(2, 2, 8)
+    bad = [
+        (ValueError, lambda: slim.gated_scan_forward(x[0], x[0])),
+        (ValueError, lambda: slim.gated_scan_forward(x, x[:, :3])),
+        (TypeError, lambda: slim.gated_scan_forward(x, x.bfloat16())),
+        (TypeError, lambda: slim.gated_scan_forward(x.half(), x.half())),
+        (ValueError, lambda: slim.gated_scan_forward(x, x, "tanh")),
+        (ValueError, lambda: slim.gated_scan_forward(x, x, h0=h0[:1])),
+        (ValueError, lambda: slim.gated_scan_forward(x, x, h0=h0.bfloat16())),
+        (ValueError, lambda: slim.gated_scan_forward(x, x, last=h0.double())),
+        (ValueError, lambda: slim.gated_scan_forward(*[x[:1, :1].expand(1, 1 << 32, 8)] * 2)),
+        (ValueError, lambda: slim.gated_scan_backward(x, x, None, x)),
+        (ValueError, lambda: slim.gated_scan_backward(x, x, kept[:, :1], x)),
+        (ValueError, lambda: slim.gated_scan_backward(x, x, kept, x[:, :3])),
+        (ValueError, lambda: slim.gated_scan_backward(x, x, kept, x.bfloat16())),
+        (ValueError, lambda: slim.gated_scan_backward(x, x, kept, x, dx=x.bfloat16())),
+        (ValueError, lambda: slim.gated_scan_backward(x, x, kept, x, dlast=h0[:1])),
+    ]
+    for kind, call in bad:
+        with pytest.raises(kind):
+            call()
+    for t in (x.transpose(1, 2).contiguous().transpose(1, 2), torch.zeros(4, 70, 8)[::2][:, :35]):
+        with pytest.raises(RuntimeError):
+            slim._pitch(t, "t")
+    assert slim._pitch(torch.zeros(2, 70, 24)[..., 8:16], "t") == 24
+    assert slim._pitch(torch.zeros(5, 3, 8)[:, :1], "t") == 24 and slim._pitch(torch.zeros(1, 1, 8), "t") == 8
+
+
+def test_scan_formula_against_differences():
+    """Autograd on the recurrence, which the kernels are held to, against central differences."""
+    g = torch.Generator().manual_seed(0)
+    gate, x = (torch.randn(1, 4, 3, generator=g, dtype=torch.float64).requires_grad_() for _ in range(2))
+    h0 = torch.randn(1, 3, generator=g, dtype=torch.float64).requires_grad_()
+    for kind in slim.GATES:
+        assert torch.autograd.gradcheck(lambda a, b, c: ref.scan64(a, b, kind, c), (gate, x, h0))
