@@ -106,23 +106,20 @@ typedef enum {
  *            be h0 itself.
  *   kept     [B, ceil(L / SLIM_SCAN_CHUNK), D] fp32, written (the state before each
  *            chunk), or null: what slim_gated_scan_bwd reads.
- *   workspace of slim_gated_scan_workspace_size(..., backward = 0) bytes (none up to
- *            SLIM_SCAN_CHUNK steps).
  * States and sums are fp32, h is rounded once.  A gate of zero (VALUE 0, LOG or
  * SIGMOID -inf) starts anew: nothing before it reaches h, finite or not.  A state
  * that is not finite stays in its channel until such a gate, or until the gates'
  * product since sinks below fp32's range.  Gates beyond 1 may grow a state past
  * fp32's range; so may the product of SLIM_SCAN_CHUNK of them alone.
- * Nothing written overlaps anything else but as said.
- * 0 <= B < 2^16, 0 <= L <= 2^30, 1 <= D <= 2^30, B D <= 2^36, B L D <= 2^40,
+ * Nothing written overlaps anything else but as said.  No workspace.
+ * 0 <= B, 0 <= L <= 2^30, 1 <= D <= 2^30, B D <= 2^32, B L D <= 2^40,
  * D <= pitch (0 <= pitch for inputs) <= 2^40, offsets below 2^60.  With B L = 0 the
  * state is passed on.
  */
-slim_status slim_gated_scan_workspace_size(int B, int L, int D, int backward, size_t* bytes);
 slim_status slim_gated_scan_fwd(const void* gate, long long gate_pitch, const void* x,
                                 long long x_pitch, const float* h0, int B, int L, int D,
                                 slim_dtype dtype, slim_gate kind, void* h, float* last, float* kept,
-                                void* workspace, size_t workspace_bytes, void* stream);
+                                void* stream);
 
 /*
  * The gradients of <dh, h> + <dlast, last> with respect to gate, x and h0.
@@ -137,8 +134,7 @@ slim_status slim_gated_scan_bwd(const void* gate, long long gate_pitch, const vo
                                 long long x_pitch, const float* kept, const void* dh,
                                 const float* dlast, int B, int L, int D, slim_dtype dtype,
                                 slim_gate kind, void* dgate, long long dgate_pitch, void* dx,
-                                long long dx_pitch, float* dh0, void* workspace,
-                                size_t workspace_bytes, void* stream);
+                                long long dx_pitch, float* dh0, void* stream);
 
 #ifdef __cplusplus
 }

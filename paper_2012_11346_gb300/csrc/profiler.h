@@ -40,8 +40,6 @@ enum Kid {
   K_LOSS_PARTS,
   K_QK_NORM,
   K_QK_WEIGHTS,
-  K_SCAN_SUMS,
-  K_SCAN_STATES,
   K_SCAN_FWD,
   K_SCAN_BWD,
   K_COUNT

@@ -64,9 +64,8 @@ SIGNATURES = {
     "slim_clip_grads": ([_p, _p, _p, _p, _i, _f, _p, _p, _sz, _p], _i),
     "slim_qk_norm_fwd": ([_p] * 7 + [_i, _p] + [_i] * 8 + [_f, _f] + [_p] * 5, _i),
     "slim_qk_norm_bwd_workspace_size": ([_i] * 5 + [ctypes.POINTER(_sz)], _i),
-    "slim_gated_scan_workspace_size": ([_i] * 4 + [ctypes.POINTER(_sz)], _i),
-    "slim_gated_scan_fwd": ([_p, _ll, _p, _ll, _p] + [_i] * 5 + [_p] * 4 + [_sz, _p], _i),
-    "slim_gated_scan_bwd": ([_p, _ll, _p, _ll] + [_p] * 3 + [_i] * 5 + [_p, _ll, _p, _ll, _p, _p, _sz, _p], _i),
+    "slim_gated_scan_fwd": ([_p, _ll, _p, _ll, _p] + [_i] * 5 + [_p] * 4, _i),
+    "slim_gated_scan_bwd": ([_p, _ll, _p, _ll] + [_p] * 3 + [_i] * 5 + [_p, _ll, _p, _ll, _p, _p], _i),
     "slim_qk_norm_bwd": ([_p] * 7 + [_i, _p] + [_i] * 8 + [_f, _f] + [_p] * 11 + [_sz, _p], _i),
 }
 
@@ -966,16 +965,6 @@ GATES = {"value": 0, "log": 1, "sigmoid": 2}
 SCAN_CHUNK = 64
 
 
-@functools.lru_cache(maxsize=1024)
-def gated_scan_workspace_size(B, L, D, backward):
-    n = _sz(0)
-    if (B | L | D) >> 31:
-        _too_large()
-    _check(library().slim_gated_scan_workspace_size(B, L, D, int(backward), ctypes.byref(n)),
-           "slim_gated_scan_workspace_size")
-    return n.value
-
-
 def _pitch(t, what):
     """Elements from a row of [B, L, D] to the next; a slice of wider rows has one, too."""
     B, L, D = t.shape
@@ -1003,7 +992,7 @@ def _scan_dims(gate, x, kind, what):
     return B, L, D, _dtype_code(gate, what), GATES[kind]
 
 
-def gated_scan_forward(gate, x, kind="sigmoid", h0=None, keep=False, last=None, workspace=None, stream=None):
+def gated_scan_forward(gate, x, kind="sigmoid", h0=None, keep=False, last=None, stream=None):
     """slim_gated_scan_fwd: h_t = a_t h_(t-1) + u_t per channel, gate and x [B, L, D]
     (slices of a projection's rows are read where they are).  kind "value": a =
     gate, u = x; "log": a = exp(gate), u = x; "sigmoid": a = sigmoid(gate), u =
@@ -1014,8 +1003,6 @@ def gated_scan_forward(gate, x, kind="sigmoid", h0=None, keep=False, last=None, 
     _one_device(gate, x, h0, last)
     h0p = _fp32_or_none(h0, (B, D), "h0")
     _fp32_or_none(last, (B, D), "last")
-    if workspace is not None:
-        _require_cuda(workspace)
     with _on_device(x):
         with _on(stream):
             h = torch.empty(B, L, D, dtype=x.dtype, device=x.device)
@@ -1023,19 +1010,15 @@ def gated_scan_forward(gate, x, kind="sigmoid", h0=None, keep=False, last=None, 
                 last = torch.empty(B, D, dtype=torch.float32, device=x.device)
             kept = (torch.empty(B, -(-L // SCAN_CHUNK), D, dtype=torch.float32, device=x.device)
                     if keep else None)
-            ws = workspace
-            if ws is None and L > SCAN_CHUNK:
-                ws = _workspace(gated_scan_workspace_size(B, L, D, False), x.device)
         _check(library().slim_gated_scan_fwd(gate.data_ptr(), _pitch(gate, "gate"), x.data_ptr(),
                                              _pitch(x, "x"), h0p, B, L, D, dt, code, h.data_ptr(),
-                                             last.data_ptr(), _ptr(kept), _ptr(ws),
-                                             0 if ws is None else ws.numel(), _stream_of(x, stream)),
+                                             last.data_ptr(), _ptr(kept), _stream_of(x, stream)),
                "slim_gated_scan_fwd")
     return (h, last, kept) if keep else (h, last)
 
 
 def gated_scan_backward(gate, x, kept, dh, kind="sigmoid", dlast=None, dgate=None, dx=None, dh0=None,
-                        workspace=None, stream=None):
+                        stream=None):
     """slim_gated_scan_bwd: returns (dgate, dx, dh0), the gradients of <dh, h> +
     <dlast, last>.  kept: from gated_scan_forward(..., keep=True) on the same inputs;
     dlast: [B, D] fp32 or None (zero).  dgate and dx are contiguous unless given
@@ -1052,8 +1035,6 @@ def gated_scan_backward(gate, x, kept, dh, kind="sigmoid", dlast=None, dgate=Non
     for t in (dgate, dx):
         if t is not None and (tuple(t.shape) != (B, L, D) or t.dtype != x.dtype):
             raise ValueError("dgate and dx must be [B, L, D] in x's dtype")
-    if workspace is not None:
-        _require_cuda(workspace)
     with _on_device(x):
         with _on(stream):
             if dgate is None:
@@ -1062,14 +1043,10 @@ def gated_scan_backward(gate, x, kept, dh, kind="sigmoid", dlast=None, dgate=Non
                 dx = torch.empty(B, L, D, dtype=x.dtype, device=x.device)
             if dh0 is None:
                 dh0 = torch.empty(B, D, dtype=torch.float32, device=x.device)
-            ws = workspace
-            if ws is None and L > SCAN_CHUNK:
-                ws = _workspace(gated_scan_workspace_size(B, L, D, True), x.device)
         _check(library().slim_gated_scan_bwd(gate.data_ptr(), _pitch(gate, "gate"), x.data_ptr(),
                                              _pitch(x, "x"), kept.data_ptr(), dh.data_ptr(), dlp, B,
                                              L, D, dt, code, dgate.data_ptr(), _pitch(dgate, "dgate"),
                                              dx.data_ptr(), _pitch(dx, "dx"), dh0.data_ptr(),
-                                             _ptr(ws), 0 if ws is None else ws.numel(),
                                              _stream_of(x, stream)), "slim_gated_scan_bwd")
     return dgate, dx, dh0
 

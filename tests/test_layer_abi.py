@@ -164,22 +164,20 @@ def test_qk_formula_against_differences():
 
 
 # ---------------------------------------------------------------- gated recurrence
-def scan_fwd(lib, gate=FAKE, gp=8, x=FAKE, xp=8, h0=FAKE, B=2, L=100, D=8, dt=F32, kind=0, h=FAKE, last=FAKE, kept=FAKE,
-             ws=FAKE, nbytes=1 << 40):
-    return lib.slim_gated_scan_fwd(gate, gp, x, xp, h0, B, L, D, dt, kind, h, last, kept, ws, nbytes, None)
+def scan_fwd(lib, gate=FAKE, gp=8, x=FAKE, xp=8, h0=FAKE, B=2, L=100, D=8, dt=F32, kind=0, h=FAKE, last=FAKE, kept=FAKE):
+    return lib.slim_gated_scan_fwd(gate, gp, x, xp, h0, B, L, D, dt, kind, h, last, kept, None)
 
 
 def scan_bwd(lib, gate=FAKE, gp=8, x=FAKE, xp=8, kept=FAKE, h=FAKE, last=FAKE, B=2, L=100, D=8, dt=F32, kind=0, dg=FAKE,
-             dgp=8, dx=FAKE, dxp=8, h0=FAKE, ws=FAKE, nbytes=1 << 40):
-    return lib.slim_gated_scan_bwd(gate, gp, x, xp, kept, h, last, B, L, D, dt, kind, dg, dgp, dx, dxp, h0, ws, nbytes,
-                                   None)
+             dgp=8, dx=FAKE, dxp=8, h0=FAKE):
+    return lib.slim_gated_scan_bwd(gate, gp, x, xp, kept, h, last, B, L, D, dt, kind, dg, dgp, dx, dxp, h0, None)
 
 
 @pytest.mark.parametrize("kw", [
-    dict(B=-1), dict(B=1 << 16), dict(L=-1), dict(L=(1 << 30) + 1), dict(D=0), dict(D=(1 << 30) + 1), dict(dt=2),
+    dict(B=-1), dict(L=-1), dict(L=(1 << 30) + 1), dict(D=0), dict(D=(1 << 30) + 1), dict(dt=2),
     dict(kind=3), dict(kind=-1), dict(gate=None), dict(x=None), dict(h=None), dict(gate=FAKE + 2), dict(x=FAKE + 1),
     dict(h=FAKE + 2), dict(dt=BF16, h=FAKE + 1), dict(gp=-1), dict(xp=-8), dict(gp=BIG + 1), dict(h0=FAKE + 2),
-    dict(last=FAKE + 1), dict(kept=FAKE + 2), dict(ws=FAKE + 16), dict(B=60000, L=1 << 30, D=1 << 10),
+    dict(last=FAKE + 1), dict(kept=FAKE + 2), dict(B=60000, L=1 << 30, D=1 << 10),
     dict(B=60000, L=1, D=1 << 25), dict(L=1 << 30, D=1, gp=1 << 35)])
 def test_scan_rejects(lib, kw):
     assert scan_fwd(lib, **kw) == INVALID
@@ -189,14 +187,6 @@ def test_scan_rejects(lib, kw):
 def test_scan_rejects_more(lib):
     for kw in (dict(dg=None), dict(dx=None), dict(dg=FAKE + 2), dict(dx=FAKE + 1), dict(dgp=7), dict(dxp=0), dict(kept=None)):
         assert scan_bwd(lib, **kw) == INVALID
-    for back, call in ((False, scan_fwd), (True, scan_bwd)):
-        need = slim.gated_scan_workspace_size(2, 100, 8, back)
-        assert call(lib, nbytes=need - 1) == WORKSPACE and call(lib, ws=None) == WORKSPACE
-        assert slim.gated_scan_workspace_size(2, 64, 8, back) == 0
-        # grows with the chunks, not the steps' values
-        assert slim.gated_scan_workspace_size(1, 1 << 16, 512, back) <= (1 << 16) * 512 // 64 * 12 + 512
-    assert lib.slim_gated_scan_workspace_size(2, 100, 8, 0, None) == INVALID
-    assert lib.slim_gated_scan_workspace_size(2, 100, 8, 2, ctypes.byref(ctypes.c_size_t())) == INVALID
 
 
 def test_scan_constant_is_the_headers():
