@@ -8,12 +8,19 @@
  *   slim_gated_scan_*  a gated linear recurrence per channel, the sibling of the
  *                      attention's prefix state that forgets, with the same
  *                      carries in and out of a segment
+ *   slim_gated_ff_*    the gated feed-forward's two projections, activation and
+ *                      product in one kernel, and its gradients
  *
  * The conventions of slim.h hold: device pointers, every buffer owned by the
  * caller, arguments validated before anything is enqueued, all work on
  * `stream`, no synchronisation; host arrays are read during the call.
  * Workspaces are 256-byte aligned.  Results do not depend on the order in which
  * blocks run: two calls on the same inputs agree bit for bit.
+ *
+ * The gated feed-forward has device-side waits (its tile kernels'); they are
+ * bounded and reported like those of the vocabulary loss: the next slim_gated_ff_*
+ * call on the same workspace returns SLIM_ERR_TIMEOUT, and slim_check_device_error
+ * reads the failure by blocking.  The other entry points have none.
  */
 #ifndef SLIM_LAYER_H_
 #define SLIM_LAYER_H_
@@ -135,6 +142,50 @@ slim_status slim_gated_scan_bwd(const void* gate, long long gate_pitch, const vo
                                 const float* dlast, int B, int L, int D, slim_dtype dtype,
                                 slim_gate kind, void* dgate, long long dgate_pitch, void* dx,
                                 long long dx_pitch, float* dh0, void* stream);
+
+/* The activation of a gate. */
+typedef enum {
+  SLIM_ACT_SILU = 0,      /* g sigmoid(g) */
+  SLIM_ACT_GELU = 1,      /* g Phi(g), Phi the normal distribution's */
+  SLIM_ACT_GELU_TANH = 2, /* g (1 + tanh(sqrt(2 / pi) (g + 0.044715 g^3))) / 2 */
+  SLIM_ACT_RELU = 3,      /* max(g, 0) */
+  SLIM_ACT_SIGMOID = 4    /* sigmoid(g) */
+} slim_act;
+
+/*
+ * h = act(x w_gate^T) * (x w_up^T), elementwise: what the last projection of a
+ * gated feed-forward reads.
+ *   x  [N, D] dtype;  w [2F, D] dtype: w_gate the first F rows, w_up the others;
+ *   h  [N, F] dtype, written.  16-byte aligned.
+ * Neither projection is written.  bf16 operands are multiplied exactly and summed
+ * in fp32; fp32 operands are split into three bf16 pieces (24 bits) and multiplied
+ * piece by piece, six products each, smallest first, on the tensor cores (up to 8
+ * rows: fp32 FMA in either type).  h is rounded once.
+ * Values are finite: an infinity in a row of x, or of w, makes what it enters
+ * infinite or NaN.
+ * 0 <= N < 2^31 - 512, 1 <= D <= 2^30, 1 <= F <= 2^29, N F <= 2^45, N D and 2 F D
+ * <= 2^40.  N = 0 enqueues nothing.
+ *   workspace of slim_gated_ff_workspace_size(..., backward = 0) bytes.
+ */
+slim_status slim_gated_ff_workspace_size(long long N, int D, int F, slim_dtype dtype, int backward,
+                                         size_t* bytes);
+slim_status slim_gated_ff_fwd(const void* x, const void* w, long long N, int D, int F,
+                              slim_dtype dtype, slim_act act, void* h, void* workspace,
+                              size_t workspace_bytes, void* stream);
+
+/*
+ * The gradients of <dh, h> with respect to x and w.
+ *   dh  [N, F] dtype;  dx [N, D] dtype, dw [2F, D] dtype, written.  16-byte aligned.
+ * With g and u the projections, computed again here,
+ *     dz = [dh u act'(g), dh act(g)],   dx = dz w,   dw = dz^T x.
+ * dz is rounded once for the products: to bf16 for bf16 problems (2^-9 relative,
+ * like the rounding of the gradients themselves), to three bf16 pieces for fp32
+ * ones; the workspace holds it (2 N F elements of 2 or 6 bytes).  Sums are fp32, and
+ * long ones are joined from parts; dx and dw are rounded once.  N = 0 zeroes dw.
+ */
+slim_status slim_gated_ff_bwd(const void* x, const void* w, const void* dh, long long N, int D,
+                              int F, slim_dtype dtype, slim_act act, void* dx, void* dw,
+                              void* workspace, size_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

@@ -39,10 +39,13 @@ constexpr int kSmemBytes = 227 * 1024 - 1024 - 512;  // after alignment and barr
 // shared memory while it stays with the same tile row, and the ring carries B
 // alone.  Worth it where a worker walks along many columns.
 constexpr int kHeld = 8;
-template <int NP, bool JOIN = (NP > 1), bool HOLD_A = false>
+// GATED: B is two matrices of as many rows, one behind the other (`up` rows on);
+// a tile's columns are 128 of the one, from the pair's first block, and the same
+// 128 of the other, from its second.  The epilogue gets both together.
+template <int NP, bool JOIN = (NP > 1), bool HOLD_A = false, bool GATED_B = false>
 struct Tile {
   static constexpr int PLANES = NP;
-  static constexpr bool ACC = JOIN, HOLD = HOLD_A;
+  static constexpr bool ACC = JOIN, HOLD = HOLD_A, GATED = GATED_B;
   static_assert(!HOLD || NP == 1, "one plane");
   static constexpr int BROWS = kTN / kPair;    // rows of B that a block holds
   static constexpr int A_BYTES = kTM * kTK * 2, B_BYTES = BROWS * kTK * 2;
@@ -65,6 +68,7 @@ struct Product {
   int tm, tn;      // tiles each way (tm in tiles of kTM * kPair rows)
   int kb;          // stages (of kTK) of the reduction
   int splits;      // parts of the reduction, computed as tiles of their own
+  int up;          // GATED: rows from B's first matrix to its second
 };
 
 // One tile: stages [k0, k1) of product p's reduction.
@@ -266,7 +270,7 @@ __device__ bool gemm_copy(GemmShared& sh, uint8_t* stages, Next next, int* err) 
     const CUtensorMap* map_a = uniform(&w.p->a);
     const CUtensorMap* map_b = uniform(&w.p->b);
     const int a_mn = uniform(w.p->a_mn), b_mn = uniform(w.p->b_mn);
-    const int row = uniform((w.m * kPair + rank) * kTM), col = uniform(w.n * kTN + rank * T::BROWS);
+    const int row = uniform((w.m * kPair + rank) * kTM), col = uniform(T::GATED ? w.n * T::BROWS + rank * w.p->up : w.n * kTN + rank * T::BROWS);
     const int k0 = uniform(w.k0) * kTK, k1 = uniform(w.k1) * kTK;
     if (T::HOLD && row != held_row) {
       if (held_row >= 0) {
@@ -409,8 +413,10 @@ __device__ bool gemm_multiply(GemmShared& sh, uint8_t* stages, Next next, int* e
 
 // An epilogue warp.  For every tile, epi.begin(work, row, col0) once, then
 // epi.chunk(c, v) for each 32 columns col0 + c .. of row `row` (of this thread)
-// that begin inside the product (v is the epilogue's to change).  Reads past the
-// product's rows still run (their values are zero sums); the epilogue drops them.
+// that begin inside the product (v is the epilogue's to change).  GATED:
+// epi.pair(c, v, u) for each 16 columns, v of the first matrix and u of the second.
+// Reads past the product's rows still run (their values are zero sums); the
+// epilogue drops them.
 template <typename T, typename Next, typename Epi>
 __device__ bool gemm_finish(GemmShared& sh, Next next, Epi& epi, int* err) {
   const uint32_t rank = cluster_rank();
@@ -421,7 +427,8 @@ __device__ bool gemm_finish(GemmShared& sh, Next next, Epi& epi, int* err) {
   while (next(w)) {
     const Product* p = w.p;
     const int row = (w.m * kPair + (int)rank) * kTM + quarter * 32 + lane;
-    const int col = w.n * kTN + part * kEpiCols;
+    constexpr int kCols = T::GATED ? kEpiCols / 2 : kEpiCols;
+    const int col = (T::GATED ? w.n * T::BROWS : w.n * kTN) + part * kCols;
     const int step = T::ACC ? T::CHAIN : w.k1 - w.k0;
     float sum[T::ACC ? kEpiCols : 1];
     if (T::ACC) {
@@ -433,15 +440,23 @@ __device__ bool gemm_finish(GemmShared& sh, Next next, Epi& epi, int* err) {
       const int buf = acc & 1;
       if (!warp_wait(tc::smem_u32(&sh.tfull[buf]), (acc >> 1) & 1, err)) return false;
       tc::tc_fence_after();
-      const uint32_t t =
-          sh.tmem + buf * kTN + part * kEpiCols + ((uint32_t)(quarter * 32) << 16);
+      const uint32_t t = sh.tmem + buf * kTN + part * kCols + ((uint32_t)(quarter * 32) << 16);
       if (T::ACC) {
 #pragma unroll
         for (int c = 0; c < kEpiCols; c += 16) {
           float v[16];
-          tc::tmem_ld16(t + c, v);
+          tc::tmem_ld16(t + c + (T::GATED && c >= kCols ? T::BROWS - kCols : 0), v);
 #pragma unroll
           for (int i = 0; i < 16; ++i) sum[c + i] += v[i];
+        }
+      } else if constexpr (T::GATED) {
+#pragma unroll 1
+        for (int c = 0; c < kCols && col + c < p->N; c += 16) {
+          float v[16], u[16];
+          __syncwarp();
+          tc::tmem_ld16(t + c, v);
+          tc::tmem_ld16(t + c + T::BROWS, u);
+          epi.pair(c, v, u);
         }
       } else {
 #pragma unroll 1
@@ -456,7 +471,11 @@ __device__ bool gemm_finish(GemmShared& sh, Next next, Epi& epi, int* err) {
       __syncwarp();
       if (lane == 0) arrive_at_leader(tc::smem_u32(&sh.tempty[buf]));
     }
-    if (T::ACC) {
+    if constexpr (T::ACC && T::GATED) {
+#pragma unroll
+      for (int c = 0; c < kCols; c += 16)
+        if (col + c < p->N) epi.pair(c, &sum[c], &sum[c + kCols]);
+    } else if constexpr (T::ACC) {
 #pragma unroll
       for (int c = 0; c < kEpiCols; c += 32)
         if (col + c < p->N) epi.chunk(c, &sum[c]);

@@ -42,6 +42,12 @@ enum Kid {
   K_QK_WEIGHTS,
   K_SCAN_FWD,
   K_SCAN_BWD,
+  K_FF,
+  K_FF_DZ,
+  K_FF_PREP,
+  K_FF_GRAD,
+  K_FF_PARTS,
+  K_FF_ROWS,
   K_COUNT
 };
 

@@ -66,6 +66,9 @@ SIGNATURES = {
     "slim_qk_norm_bwd_workspace_size": ([_i] * 5 + [ctypes.POINTER(_sz)], _i),
     "slim_gated_scan_fwd": ([_p, _ll, _p, _ll, _p] + [_i] * 5 + [_p] * 4, _i),
     "slim_gated_scan_bwd": ([_p, _ll, _p, _ll] + [_p] * 3 + [_i] * 5 + [_p, _ll, _p, _ll, _p, _p], _i),
+    "slim_gated_ff_workspace_size": ([_ll, _i, _i, _i, _i, ctypes.POINTER(_sz)], _i),
+    "slim_gated_ff_fwd": ([_p, _p, _ll] + [_i] * 4 + [_p, _p, _sz, _p], _i),
+    "slim_gated_ff_bwd": ([_p, _p, _p, _ll] + [_i] * 4 + [_p, _p, _p, _sz, _p], _i),
     "slim_qk_norm_bwd": ([_p] * 7 + [_i, _p] + [_i] * 8 + [_f, _f] + [_p] * 11 + [_sz, _p], _i),
 }
 
@@ -1083,3 +1086,96 @@ def gated_scan(gate, x, kind="sigmoid", h0=None):
     """Differentiable (once) gated_scan_forward: returns (h, last), with gradients with
     respect to gate, x and h0."""
     return GatedScan.apply(gate, x, kind, h0)
+
+
+ACTIVATIONS = {"silu": 0, "gelu": 1, "gelu_tanh": 2, "relu": 3, "sigmoid": 4}
+
+
+@functools.lru_cache(maxsize=1024)
+def gated_ff_workspace_size(N, D, F, dtype, backward):
+    n = _sz(0)
+    if (D | F) >> 31:
+        _too_large()
+    _check(library().slim_gated_ff_workspace_size(N, D, F, DTYPES[dtype], int(backward), ctypes.byref(n)),
+           "slim_gated_ff_workspace_size")
+    return n.value
+
+
+def _ff_dims(x, w, act, what):
+    _one_device(x, w)
+    _require_cuda(x, w)
+    if w.dtype != x.dtype:
+        raise TypeError(f"{what}: one dtype expected, got {x.dtype} and {w.dtype}")
+    if w.dim() != 2 or w.shape[0] % 2 or x.dim() < 1 or x.shape[-1] != w.shape[1]:
+        raise ValueError("x must be [..., D] and w [2F, D]")
+    _require(act in ACTIVATIONS, f"act must be one of {', '.join(ACTIVATIONS)}")
+    F, D = w.shape[0] // 2, w.shape[1]
+    if (D | F) >> 31:
+        _too_large()
+    return x.numel() // max(D, 1), D, F, _dtype_code(x, what), ACTIVATIONS[act]
+
+
+def gated_ff_forward(x, w, act="silu", keep=False, out=None, workspace=None, stream=None):
+    """slim_gated_ff_fwd: act(x w_gate^T) * (x w_up^T) for x [..., D] and w [2F, D], its
+    first F rows the gate's and the others up's; act one of "silu", "gelu",
+    "gelu_tanh", "relu", "sigmoid".  With keep=True returns (h, z), z being what
+    gated_ff_backward can reuse, or None where computing it again is the faster."""
+    N, D, F, dt, code = _ff_dims(x, w, act, "gated_ff_forward")
+    shape = (*x.shape[:-1], F)
+    if out is not None:
+        _one_device(x, out)
+        _require_cuda(out)
+        _require(out.dtype == x.dtype and tuple(out.shape) == shape, "out must be [..., F] in x's dtype")
+    if workspace is not None:
+        _require_cuda(workspace)
+    with _on_device(x):
+        with _on(stream):
+            h = out if out is not None else torch.empty(shape, dtype=x.dtype, device=x.device)
+            ws = workspace if workspace is not None else _workspace(
+                gated_ff_workspace_size(N, D, F, x.dtype, False), x.device)
+        _check(library().slim_gated_ff_fwd(x.data_ptr(), w.data_ptr(), N, D, F, dt, code, h.data_ptr(),
+                                           ws.data_ptr(), ws.numel(), _stream_of(x, stream)),
+               "slim_gated_ff_fwd")
+    return (h, None) if keep else h
+
+
+def gated_ff_backward(x, w, dh, act="silu", z=None, workspace=None, stream=None):
+    """slim_gated_ff_bwd: returns (dx, dw), the gradients of <dh, h>.  z: from
+    gated_ff_forward(..., keep=True) on the same inputs, or None."""
+    N, D, F, dt, code = _ff_dims(x, w, act, "gated_ff_backward")
+    _one_device(x, dh)
+    _require_cuda(dh)
+    if tuple(dh.shape) != (*x.shape[:-1], F) or dh.dtype != x.dtype:
+        raise ValueError("dh must be [..., F] in x's dtype")
+    if workspace is not None:
+        _require_cuda(workspace)
+    with _on_device(x):
+        with _on(stream):
+            dx, dw = torch.empty_like(x), torch.empty_like(w)
+            ws = workspace if workspace is not None else _workspace(
+                gated_ff_workspace_size(N, D, F, x.dtype, True), x.device)
+        _check(library().slim_gated_ff_bwd(x.data_ptr(), w.data_ptr(), dh.data_ptr(), N, D, F, dt, code,
+                                           dx.data_ptr(), dw.data_ptr(), ws.data_ptr(), ws.numel(),
+                                           _stream_of(x, stream)), "slim_gated_ff_bwd")
+    return dx, dw
+
+
+class GatedFeedForward(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x_in, w_in, act):
+        x, w = _ready(x_in), _ready(w_in)
+        h, z = gated_ff_forward(x, w, act, keep=True)
+        ctx.save_for_backward(x_in, w_in, x, w, z)
+        ctx.act = act
+        return h
+
+    @staticmethod
+    def backward(ctx, dh):
+        x_in, w_in, x, w, z = ctx.saved_tensors
+        grads = gated_ff_backward(x, w, _ready(dh), ctx.act, z=z)
+        return *_first_derivatives(grads, x_in, w_in, dh), None
+
+
+def gated_ff(x, w, act="silu"):
+    """Differentiable (once) gated_ff_forward: gradients with respect to x and w."""
+    return GatedFeedForward.apply(x, w, act)

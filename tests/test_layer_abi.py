@@ -237,3 +237,73 @@ def test_scan_formula_against_differences():
     h0 = torch.randn(1, 3, generator=g, dtype=torch.float64).requires_grad_()
     for kind in slim.GATES:
         assert torch.autograd.gradcheck(lambda a, b, c: ref.scan64(a, b, kind, c), (gate, x, h0))
+
+
+# ---------------------------------------------------------------- gated feed-forward
+def ff_fwd(lib, x=FAKE, w=FAKE, N=20, D=8, F=16, dt=F32, act=0, h=FAKE, ws=FAKE, nbytes=1 << 60):
+    return lib.slim_gated_ff_fwd(x, w, N, D, F, dt, act, h, ws, nbytes, None)
+
+
+def ff_bwd(lib, x=FAKE, w=FAKE, h=FAKE, N=20, D=8, F=16, dt=F32, act=0, dx=FAKE, dw=FAKE, ws=FAKE, nbytes=1 << 60):
+    return lib.slim_gated_ff_bwd(x, w, h, N, D, F, dt, act, dx, dw, ws, nbytes, None)
+
+
+@pytest.mark.parametrize("kw", [
+    dict(N=-1), dict(N=(1 << 31) - 512), dict(D=0), dict(D=(1 << 30) + 1), dict(F=0), dict(F=(1 << 29) + 1), dict(dt=2),
+    dict(act=-1), dict(act=5), dict(N=1 << 20, F=1 << 26), dict(N=1 << 20, D=(1 << 20) + 1), dict(F=1 << 20, D=1 << 20),
+    dict(x=None), dict(w=None), dict(h=None), dict(x=FAKE + 8), dict(w=FAKE + 8), dict(h=FAKE + 4), dict(ws=FAKE + 16),
+    dict(N=3, ws=FAKE + 16), dict(N=3, x=FAKE + 2)])
+def test_ff_rejects(lib, kw):
+    assert ff_fwd(lib, **kw) == INVALID
+    assert ff_bwd(lib, **kw) == INVALID
+
+
+def test_ff_rejects_more(lib):
+    for bad in (None, FAKE + 8):
+        assert ff_bwd(lib, dx=bad) == INVALID and ff_bwd(lib, dw=bad) == INVALID
+    for N in (3, 20):
+        for back, call in ((False, ff_fwd), (True, ff_bwd)):
+            need = slim.gated_ff_workspace_size(N, 8, 16, torch.float32, back)
+            assert call(lib, N=N, nbytes=need - 1) == WORKSPACE and call(lib, N=N, ws=None) == WORKSPACE
+    n = ctypes.c_size_t()
+    assert lib.slim_gated_ff_workspace_size(20, 8, 16, F32, 0, None) == INVALID
+    assert lib.slim_gated_ff_workspace_size(20, 8, 16, F32, 2, ctypes.byref(n)) == INVALID
+    size = lambda N, F, back: slim.gated_ff_workspace_size(N, 512, F, torch.bfloat16, back)
+    # bf16 rows that need no staging: nothing forward, dz backward
+    assert size(32768, 2048, False) <= 256
+    assert 2 * 2 * 32768 * 2048 <= size(32768, 2048, True) <= 2 * 2 * 32768 * 2048 + (1 << 26)
+    assert ff_fwd(lib, N=0, x=None, h=None, ws=None, nbytes=0) == OK
+
+
+def test_ff_binding(monkeypatch):
+    x, w = torch.zeros(4, 8), torch.zeros(12, 8)
+    with pytest.raises(RuntimeError, match="CUDA"):
+        slim.gated_ff_forward(x, w)
+    monkeypatch.setattr(slim, "_one_device", lambda *t: None)
+    monkeypatch.setattr(slim, "_require_cuda", lambda *t: None)
+    monkeypatch.setattr(slim, "_on_device", lambda t: slim._HERE)
+    monkeypatch.setattr(slim, "library", lambda: (_ for _ in ()).throw(AssertionError("reached")))
+    bad = [
+        (TypeError, lambda: slim.gated_ff_forward(x, w.bfloat16())),
+        (TypeError, lambda: slim.gated_ff_forward(x.half(), w.half())),
+        (ValueError, lambda: slim.gated_ff_forward(x, w[:11])),
+        (ValueError, lambda: slim.gated_ff_forward(x, w[:, :7])),
+        (ValueError, lambda: slim.gated_ff_forward(x, w[0])),
+        (ValueError, lambda: slim.gated_ff_forward(x, w, "tanh")),
+        (ValueError, lambda: slim.gated_ff_forward(x, w, out=torch.zeros(4, 7))),
+        (ValueError, lambda: slim.gated_ff_forward(x, w, out=torch.zeros(4, 6).bfloat16())),
+        (ValueError, lambda: slim.gated_ff_forward(x, torch.zeros(1, 8).expand(1 << 33, 8))),
+        (ValueError, lambda: slim.gated_ff_backward(x, w, torch.zeros(4, 12))),
+        (ValueError, lambda: slim.gated_ff_backward(x, w, torch.zeros(4, 6).bfloat16())),
+    ]
+    for kind, call in bad:
+        with pytest.raises(kind):
+            call()
+
+
+@pytest.mark.parametrize("act", list(ref.ACTS))
+def test_ff_formula_against_differences(act):
+    g = torch.Generator().manual_seed(0)
+    x = torch.randn(3, 4, generator=g, dtype=torch.float64).requires_grad_()
+    w = torch.randn(6, 4, generator=g, dtype=torch.float64).requires_grad_()
+    assert torch.autograd.gradcheck(lambda a, b: ref.ff64(a, b, act), (x, w))
