@@ -17,10 +17,11 @@
  * Workspaces are 256-byte aligned.  Results do not depend on the order in which
  * blocks run: two calls on the same inputs agree bit for bit.
  *
- * The gated feed-forward has device-side waits (its tile kernels'); they are
- * bounded and reported like those of the vocabulary loss: the next slim_gated_ff_*
- * call on the same workspace returns SLIM_ERR_TIMEOUT, and slim_check_device_error
- * reads the failure by blocking.  The other entry points have none.
+ * The gated feed-forward has device-side waits (its tile kernels'), and so has the
+ * recurrence where it has a workspace; they are bounded and reported like those of
+ * the vocabulary loss: the next slim_gated_ff_* or slim_gated_scan_* call on the same
+ * workspace returns SLIM_ERR_TIMEOUT, and slim_check_device_error reads the failure
+ * by blocking.  The other entry points have none.
  */
 #ifndef SLIM_LAYER_H_
 #define SLIM_LAYER_H_
@@ -118,15 +119,18 @@ typedef enum {
  * that is not finite stays in its channel until such a gate, or until the gates'
  * product since sinks below fp32's range.  Gates beyond 1 may grow a state past
  * fp32's range; so may the product of SLIM_SCAN_CHUNK of them alone.
- * Nothing written overlaps anything else but as said.  No workspace.
+ * Nothing written overlaps anything else but as said.
+ *   workspace of slim_gated_scan_workspace_size() bytes, for either direction; where
+ *   that is 0 (short sequences, few of them) it is not read and may be null.
  * 0 <= B, 0 <= L <= 2^30, 1 <= D <= 2^30, B D <= 2^32, B L D <= 2^40,
  * D <= pitch (0 <= pitch for inputs) <= 2^40, offsets below 2^60.  With B L = 0 the
  * state is passed on.
  */
+slim_status slim_gated_scan_workspace_size(int B, int L, int D, slim_dtype dtype, size_t* bytes);
 slim_status slim_gated_scan_fwd(const void* gate, long long gate_pitch, const void* x,
                                 long long x_pitch, const float* h0, int B, int L, int D,
                                 slim_dtype dtype, slim_gate kind, void* h, float* last, float* kept,
-                                void* stream);
+                                void* workspace, size_t workspace_bytes, void* stream);
 
 /*
  * The gradients of <dh, h> + <dlast, last> with respect to gate, x and h0.
@@ -141,7 +145,8 @@ slim_status slim_gated_scan_bwd(const void* gate, long long gate_pitch, const vo
                                 long long x_pitch, const float* kept, const void* dh,
                                 const float* dlast, int B, int L, int D, slim_dtype dtype,
                                 slim_gate kind, void* dgate, long long dgate_pitch, void* dx,
-                                long long dx_pitch, float* dh0, void* stream);
+                                long long dx_pitch, float* dh0, void* workspace,
+                                size_t workspace_bytes, void* stream);
 
 /* The activation of a gate. */
 typedef enum {

@@ -19,7 +19,7 @@ const char* kNames[K_COUNT] = {
     "embed_fwd",   "embed_sort",    "embed_sum",  "embed_join",    "clip",          "loss_prep",
     "loss_stats",  "loss_join",     "loss_softmax",   "loss_grad",
     "loss_rows",   "loss_parts",  "qk_norm",       "qk_weights",
-    "scan_fwd",    "scan_bwd",
+    "scan_clear", "scan_fwd",    "scan_bwd",
     "gated_ff",    "gated_ff_dz",   "gated_ff_prep", "gated_ff_grad", "gated_ff_parts", "gated_ff_rows"};
 
 struct Rec {

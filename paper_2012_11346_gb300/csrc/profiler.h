@@ -40,6 +40,7 @@ enum Kid {
   K_LOSS_PARTS,
   K_QK_NORM,
   K_QK_WEIGHTS,
+  K_SCAN_CLEAR,
   K_SCAN_FWD,
   K_SCAN_BWD,
   K_FF,

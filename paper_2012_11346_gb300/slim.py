@@ -64,8 +64,10 @@ SIGNATURES = {
     "slim_clip_grads": ([_p, _p, _p, _p, _i, _f, _p, _p, _sz, _p], _i),
     "slim_qk_norm_fwd": ([_p] * 7 + [_i, _p] + [_i] * 8 + [_f, _f] + [_p] * 5, _i),
     "slim_qk_norm_bwd_workspace_size": ([_i] * 5 + [ctypes.POINTER(_sz)], _i),
-    "slim_gated_scan_fwd": ([_p, _ll, _p, _ll, _p] + [_i] * 5 + [_p] * 4, _i),
-    "slim_gated_scan_bwd": ([_p, _ll, _p, _ll] + [_p] * 3 + [_i] * 5 + [_p, _ll, _p, _ll, _p, _p], _i),
+    "slim_gated_scan_workspace_size": ([_i] * 4 + [ctypes.POINTER(_sz)], _i),
+    "slim_gated_scan_fwd": ([_p, _ll, _p, _ll, _p] + [_i] * 5 + [_p] * 4 + [_sz, _p], _i),
+    "slim_gated_scan_bwd": ([_p, _ll, _p, _ll] + [_p] * 3 + [_i] * 5 + [_p, _ll, _p, _ll, _p, _p, _sz, _p],
+                            _i),
     "slim_gated_ff_workspace_size": ([_ll, _i, _i, _i, _i, ctypes.POINTER(_sz)], _i),
     "slim_gated_ff_fwd": ([_p, _p, _ll] + [_i] * 4 + [_p, _p, _sz, _p], _i),
     "slim_gated_ff_bwd": ([_p, _p, _p, _ll] + [_i] * 4 + [_p, _p, _p, _sz, _p], _i),
@@ -995,7 +997,25 @@ def _scan_dims(gate, x, kind, what):
     return B, L, D, _dtype_code(gate, what), GATES[kind]
 
 
-def gated_scan_forward(gate, x, kind="sigmoid", h0=None, keep=False, last=None, stream=None):
+@functools.lru_cache(maxsize=1024)
+def gated_scan_workspace_size(B, L, D, dtype):
+    n = _sz(0)
+    _check(library().slim_gated_scan_workspace_size(B, L, D, DTYPES[dtype], ctypes.byref(n)),
+           "slim_gated_scan_workspace_size")
+    return n.value
+
+
+def _scan_workspace(given, need, device):
+    """(tensor or None, pointer, bytes): short sequences need none."""
+    if given is None:
+        given = _workspace(need, device) if need else None
+    else:
+        _one_device(given)
+        _require_cuda(given)
+    return given, _ptr(given), 0 if given is None else given.numel()
+
+
+def gated_scan_forward(gate, x, kind="sigmoid", h0=None, keep=False, last=None, workspace=None, stream=None):
     """slim_gated_scan_fwd: h_t = a_t h_(t-1) + u_t per channel, gate and x [B, L, D]
     (slices of a projection's rows are read where they are).  kind "value": a =
     gate, u = x; "log": a = exp(gate), u = x; "sigmoid": a = sigmoid(gate), u =
@@ -1013,15 +1033,16 @@ def gated_scan_forward(gate, x, kind="sigmoid", h0=None, keep=False, last=None, 
                 last = torch.empty(B, D, dtype=torch.float32, device=x.device)
             kept = (torch.empty(B, -(-L // SCAN_CHUNK), D, dtype=torch.float32, device=x.device)
                     if keep else None)
+            ws, wsp, nbytes = _scan_workspace(workspace, gated_scan_workspace_size(B, L, D, x.dtype), x.device)
         _check(library().slim_gated_scan_fwd(gate.data_ptr(), _pitch(gate, "gate"), x.data_ptr(),
                                              _pitch(x, "x"), h0p, B, L, D, dt, code, h.data_ptr(),
-                                             last.data_ptr(), _ptr(kept), _stream_of(x, stream)),
-               "slim_gated_scan_fwd")
+                                             last.data_ptr(), _ptr(kept), wsp, nbytes,
+                                             _stream_of(x, stream)), "slim_gated_scan_fwd")
     return (h, last, kept) if keep else (h, last)
 
 
 def gated_scan_backward(gate, x, kept, dh, kind="sigmoid", dlast=None, dgate=None, dx=None, dh0=None,
-                        stream=None):
+                        workspace=None, stream=None):
     """slim_gated_scan_bwd: returns (dgate, dx, dh0), the gradients of <dh, h> +
     <dlast, last>.  kept: from gated_scan_forward(..., keep=True) on the same inputs;
     dlast: [B, D] fp32 or None (zero).  dgate and dx are contiguous unless given
@@ -1046,11 +1067,12 @@ def gated_scan_backward(gate, x, kept, dh, kind="sigmoid", dlast=None, dgate=Non
                 dx = torch.empty(B, L, D, dtype=x.dtype, device=x.device)
             if dh0 is None:
                 dh0 = torch.empty(B, D, dtype=torch.float32, device=x.device)
+            ws, wsp, nbytes = _scan_workspace(workspace, gated_scan_workspace_size(B, L, D, x.dtype), x.device)
         _check(library().slim_gated_scan_bwd(gate.data_ptr(), _pitch(gate, "gate"), x.data_ptr(),
                                              _pitch(x, "x"), kept.data_ptr(), dh.data_ptr(), dlp, B,
                                              L, D, dt, code, dgate.data_ptr(), _pitch(dgate, "dgate"),
-                                             dx.data_ptr(), _pitch(dx, "dx"), dh0.data_ptr(),
-                                             _stream_of(x, stream)), "slim_gated_scan_bwd")
+                                             dx.data_ptr(), _pitch(dx, "dx"), dh0.data_ptr(), wsp,
+                                             nbytes, _stream_of(x, stream)), "slim_gated_scan_bwd")
     return dgate, dx, dh0
 
 

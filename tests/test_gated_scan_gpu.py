@@ -8,6 +8,7 @@ most once more per step: C = 20 * 2^-24 a step covers them.  With m_t = |a_t| m_
 what meets in h_t, its error follows e_t = |a_t| e_(t-1) + C m_t.  The same from the
 other end for g; a product of two such values takes both errors and C of its size;
 the result's rounding adds U."""
+import ctypes
 import math
 
 import pytest
@@ -238,6 +239,71 @@ def test_nothing_to_do(cuda_device):
     assert (slim.gated_scan_forward(z, z, "log")[1] == 0).all()
     n = torch.zeros(0, 5, 6, device=cuda_device)
     assert slim.gated_scan_forward(n, n)[0].shape == n.shape
+
+
+@pytest.mark.parametrize("dt", [F32, BF16])
+@pytest.mark.parametrize("B,L,D", [(3, 600, 40), (2, 1024, 33), (40, 640, 70), (700, 150, 20), (5, 2049, 100)])
+def test_tiles_of_a_cluster_and_of_the_whole_gpu(cuda_device, B, L, D, dt):
+    """Sequences whose tiles are one cluster (with blocks to spare, and full) and such that
+    look back through the workspace, with too many tiles or too many sequences."""
+    gate, x, h0, dh, dlast = make(cuda_device, B, L, D, "sigmoid", dt, seed=L)
+    check(gate, x, "sigmoid", h0, dh, dlast)
+
+
+def test_a_sequence_does_not_depend_on_its_neighbours(cuda_device):
+    """Alone (a cluster's tiles) and among many (tiles that look back): the same bits."""
+    gate, x, h0, dh, dlast = make(cuda_device, 300, 500, 24, "log", F32)
+    out = slim.gated_scan_forward(gate, x, "log", h0=h0, keep=True)
+    grads = slim.gated_scan_backward(gate, x, out[2], dh, "log", dlast=dlast)
+    assert slim.gated_scan_workspace_size(300, 500, 24, F32) and not slim.gated_scan_workspace_size(1, 500, 24, F32)
+    for b in (0, 7, 299):
+        one = [t[b:b + 1].contiguous() for t in (gate, x, h0, dh, dlast)]
+        a = slim.gated_scan_forward(one[0], one[1], "log", h0=one[2], keep=True)
+        g = slim.gated_scan_backward(one[0], one[1], a[2], one[3], "log", dlast=one[4])
+        assert all(torch.equal(p[0], q[b]) for p, q in zip((*a, *g), (*out, *grads)))
+
+
+def test_two_calls_at_once(cuda_device):
+    """Two streams whose tiles share the GPU, each with a workspace of its own."""
+    sets = [make(cuda_device, 2, 9000, 96, "sigmoid", BF16, seed=i) for i in range(2)]
+    ref = [slim.gated_scan_forward(s[0], s[1], "sigmoid", h0=s[2], keep=True) for s in sets]
+    streams = [torch.cuda.Stream() for _ in sets]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        got = []
+        for s, stream in zip(sets, streams):
+            a = slim.gated_scan_forward(s[0], s[1], "sigmoid", h0=s[2], keep=True, stream=stream)
+            got.append(a + slim.gated_scan_backward(s[0], s[1], a[2], s[3], "sigmoid", dlast=s[4], stream=stream))
+        torch.cuda.synchronize()
+        for s, r, a in zip(sets, ref, got):
+            assert all(torch.equal(p, q) for p, q in zip(a, r))
+            g = slim.gated_scan_backward(s[0], s[1], r[2], s[3], "sigmoid", dlast=s[4])
+            assert all(torch.equal(p, q) for p, q in zip(a[3:], g))
+
+
+@pytest.mark.parametrize("backward", [False, True])
+def test_a_wait_that_gave_up_is_reported(cuda_device, backward):
+    """The next call on the workspace launches nothing and says so; the one after it runs.
+    The wait runs out on a barrier that nothing arrives at."""
+    gate, x, h0, dh, dlast = make(cuda_device, 1, 5000, 16, "log", F32)
+    ref = slim.gated_scan_forward(gate, x, "log", h0=h0, keep=True)
+    ws = torch.full((1 << 21,), 255, dtype=torch.uint8, device=cuda_device)
+
+    def call():
+        if backward:
+            return slim.gated_scan_backward(gate, x, ref[2], dh, "log", dlast=dlast, workspace=ws)
+        return slim.gated_scan_forward(gate, x, "log", h0=h0, workspace=ws)
+
+    want = call()  # whatever the workspace held
+    stream = ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
+    assert slim.library().slim_diag_wait_timeout(ws.data_ptr(), stream) == 0
+    torch.cuda.synchronize()
+    before = slim.launch_count()
+    with pytest.raises(slim.SlimError) as e:
+        call()
+    assert e.value.status == 5 and slim.launch_count() == before
+    assert all(torch.equal(a, b) for a, b in zip(call(), want))
+    slim.check_device_error(ws)
 
 
 def test_same_bits_streams_and_graphs(cuda_device):

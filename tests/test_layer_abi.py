@@ -164,13 +164,14 @@ def test_qk_formula_against_differences():
 
 
 # ---------------------------------------------------------------- gated recurrence
-def scan_fwd(lib, gate=FAKE, gp=8, x=FAKE, xp=8, h0=FAKE, B=2, L=100, D=8, dt=F32, kind=0, h=FAKE, last=FAKE, kept=FAKE):
-    return lib.slim_gated_scan_fwd(gate, gp, x, xp, h0, B, L, D, dt, kind, h, last, kept, None)
+def scan_fwd(lib, gate=FAKE, gp=8, x=FAKE, xp=8, h0=FAKE, B=2, L=100, D=8, dt=F32, kind=0, h=FAKE, last=FAKE, kept=FAKE, ws=FAKE,
+             nbytes=1 << 60):
+    return lib.slim_gated_scan_fwd(gate, gp, x, xp, h0, B, L, D, dt, kind, h, last, kept, ws, nbytes, None)
 
 
 def scan_bwd(lib, gate=FAKE, gp=8, x=FAKE, xp=8, kept=FAKE, h=FAKE, last=FAKE, B=2, L=100, D=8, dt=F32, kind=0, dg=FAKE,
-             dgp=8, dx=FAKE, dxp=8, h0=FAKE):
-    return lib.slim_gated_scan_bwd(gate, gp, x, xp, kept, h, last, B, L, D, dt, kind, dg, dgp, dx, dxp, h0, None)
+             dgp=8, dx=FAKE, dxp=8, h0=FAKE, ws=FAKE, nbytes=1 << 60):
+    return lib.slim_gated_scan_bwd(gate, gp, x, xp, kept, h, last, B, L, D, dt, kind, dg, dgp, dx, dxp, h0, ws, nbytes, None)
 
 
 @pytest.mark.parametrize("kw", [
@@ -187,6 +188,27 @@ def test_scan_rejects(lib, kw):
 def test_scan_rejects_more(lib):
     for kw in (dict(dg=None), dict(dx=None), dict(dg=FAKE + 2), dict(dx=FAKE + 1), dict(dgp=7), dict(dxp=0), dict(kept=None)):
         assert scan_bwd(lib, **kw) == INVALID
+
+
+def test_scan_workspace(lib):
+    """None for short and few sequences; else it is asked for, aligned, and its size does
+    not depend on what the channels' alignment is."""
+    def size(B, L, D, dt=F32):
+        n = ctypes.c_size_t(7)
+        assert lib.slim_gated_scan_workspace_size(B, L, D, dt, ctypes.byref(n)) == 0
+        return n.value
+
+    assert size(2, 100, 8) == size(0, 1 << 20, 8) == size(1 << 20, 8, 512) == size(1 << 20, 64, 512) == 0
+    assert size(1, 512, 8) == 0 and size(2, 3000, 8) > 0 and size(1 << 10, 200, 512) > 0
+    for kw in (dict(B=-1), dict(D=0), dict(L=-1), dict(dt=2)):
+        n = ctypes.c_size_t(7)
+        a = {**dict(B=1, L=5000, D=8, dt=F32), **kw}
+        assert lib.slim_gated_scan_workspace_size(a["B"], a["L"], a["D"], a["dt"], ctypes.byref(n)) == INVALID
+    assert lib.slim_gated_scan_workspace_size(1, 5000, 8, F32, None) == INVALID
+    need = size(2, 5000, 8)
+    for call in (scan_fwd, scan_bwd):
+        assert call(lib, L=5000, ws=None) == call(lib, L=5000, nbytes=need - 1) == WORKSPACE
+        assert call(lib, L=5000, ws=FAKE + 128) == INVALID
 
 
 def test_scan_constant_is_the_headers():
