@@ -170,7 +170,8 @@ typedef enum {
  * infinite or NaN.
  * 0 <= N < 2^31 - 512, 1 <= D <= 2^30, 1 <= F <= 2^29, N F <= 2^45, N D and 2 F D
  * <= 2^40.  N = 0 enqueues nothing.
- *   workspace of slim_gated_ff_workspace_size(..., backward = 0) bytes.
+ *   workspace of slim_gated_ff_workspace_size(..., backward = 0) bytes; where that is
+ *   0 (up to 8 rows) it may be null.
  */
 slim_status slim_gated_ff_workspace_size(long long N, int D, int F, slim_dtype dtype, int backward,
                                          size_t* bytes);

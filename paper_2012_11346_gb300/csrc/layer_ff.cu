@@ -365,6 +365,8 @@ extern "C" slim_status slim_gated_ff_workspace_size(long long N, int D, int F, s
                                                     int backward, size_t* bytes) {
   using namespace slim::lm;
   if (!bytes || !ff_sizes_ok(N, D, F, dtype, SLIM_ACT_SILU) || (backward & ~1)) return SLIM_ERR_INVALID_ARG;
+  *bytes = 0;
+  if (!backward && slim::layer::ff_rows_fit(N, D, dtype)) return SLIM_OK;
   slim::Carver cv(nullptr);
   ff_carve(cv, FfSizes{N, D, F, dtype}, backward != 0);
   *bytes = cv.bytes();
@@ -377,6 +379,7 @@ slim_status ff_begin(long long N, int D, int F, slim_dtype dtype, int backward, 
                      size_t bytes, bool waits, unsigned** rep) {
   size_t need = 0;
   slim_gated_ff_workspace_size(N, D, F, dtype, backward, &need);
+  if (need == 0 && workspace == nullptr) return SLIM_OK;
   if (workspace == nullptr || bytes < need) return SLIM_ERR_WORKSPACE;
   if (!slim::lm::aligned(workspace, 256)) return SLIM_ERR_INVALID_ARG;
   return waits ? slim::report::begin(workspace, true, rep) : slim::report::pending(workspace);
@@ -395,7 +398,11 @@ extern "C" slim_status slim_gated_ff_fwd(const void* x, const void* w, long long
   unsigned* rep = nullptr;
   const slim_status st = ff_begin(N, D, F, dtype, 0, workspace, workspace_bytes, !rows, &rep);
   if (st != SLIM_OK) return st;
-  if (rows) return slim::layer::ff_rows_fwd(x, w, (int)N, D, F, dtype, act, h, static_cast<int*>(workspace), s);
+  if (rows) {
+    // nothing waits; a workspace given all the same starts anew
+    if (workspace && cudaMemsetAsync(workspace, 0, 16, s) != cudaSuccess) return SLIM_ERR_CUDA;
+    return slim::layer::ff_rows_fwd(x, w, (int)N, D, F, dtype, act, h, s);
+  }
   const FfSizes z{N, D, F, dtype};
   slim::Carver cv(workspace);
   const FfWs ws = ff_carve(cv, z, false);

@@ -45,8 +45,7 @@ template <typename T, bool VEC> struct Piece {
 
 template <typename T, bool VEC, int NT>
 __global__ void __launch_bounds__(kThreads) k_ff_rows(const T* x, const T* w, int N, int D, int F,
-                                                      int act, T* h, int* header) {
-  if (blockIdx.x == 0 && threadIdx.x < 4) header[threadIdx.x] = 0;  // nothing here waits
+                                                      int act, T* h) {
   using P = Piece<T, VEC>;
   constexpr int C = 2 * NT;
   const int lane = threadIdx.x & 31;
@@ -96,21 +95,19 @@ __global__ void __launch_bounds__(kThreads) k_ff_rows(const T* x, const T* w, in
 }
 
 template <typename T, bool VEC, int NT>
-bool run(const void* x, const void* w, int N, int D, int F, int act, void* h, int* header,
-         cudaStream_t s) {
+bool run(const void* x, const void* w, int N, int D, int F, int act, void* h, cudaStream_t s) {
   const int want = (F + kWarps - 1) / kWarps, most = 152 * 8;
   prof::Scope ps(prof::K_FF_ROWS, s, 4.0 * N * D * F, 2.0 * F * D * sizeof(T));
   k_ff_rows<T, VEC, NT><<<want < most ? want : most, kThreads, 0, s>>>(
-      static_cast<const T*>(x), static_cast<const T*>(w), N, D, F, act, static_cast<T*>(h), header);
+      static_cast<const T*>(x), static_cast<const T*>(w), N, D, F, act, static_cast<T*>(h));
   return cudaGetLastError() == cudaSuccess;
 }
 template <typename T, bool VEC>
-bool by_rows(const void* x, const void* w, int N, int D, int F, int act, void* h, int* header,
-         cudaStream_t s) {
-  if (N == 1) return run<T, VEC, 1>(x, w, N, D, F, act, h, header, s);
-  if (N == 2) return run<T, VEC, 2>(x, w, N, D, F, act, h, header, s);
-  if (N <= 4) return run<T, VEC, 4>(x, w, N, D, F, act, h, header, s);
-  return run<T, VEC, 8>(x, w, N, D, F, act, h, header, s);
+bool by_rows(const void* x, const void* w, int N, int D, int F, int act, void* h, cudaStream_t s) {
+  if (N == 1) return run<T, VEC, 1>(x, w, N, D, F, act, h, s);
+  if (N == 2) return run<T, VEC, 2>(x, w, N, D, F, act, h, s);
+  if (N <= 4) return run<T, VEC, 4>(x, w, N, D, F, act, h, s);
+  return run<T, VEC, 8>(x, w, N, D, F, act, h, s);
 }
 
 }  // namespace
@@ -118,13 +115,13 @@ bool by_rows(const void* x, const void* w, int N, int D, int F, int act, void* h
 bool ff_rows_fit(long long N, int, slim_dtype) { return N >= 1 && N <= kMaxRows; }
 
 slim_status ff_rows_fwd(const void* x, const void* w, int N, int D, int F, slim_dtype dtype,
-                        slim_act act, void* h, int* header, cudaStream_t s) {
+                        slim_act act, void* h, cudaStream_t s) {
   using B = __nv_bfloat16;
   const bool ok = dtype == SLIM_F32
-                      ? (D % 4 == 0 ? by_rows<float, true>(x, w, N, D, F, act, h, header, s)
-                                    : by_rows<float, false>(x, w, N, D, F, act, h, header, s))
-                      : (D % 8 == 0 ? by_rows<B, true>(x, w, N, D, F, act, h, header, s)
-                                    : by_rows<B, false>(x, w, N, D, F, act, h, header, s));
+                      ? (D % 4 == 0 ? by_rows<float, true>(x, w, N, D, F, act, h, s)
+                                    : by_rows<float, false>(x, w, N, D, F, act, h, s))
+                      : (D % 8 == 0 ? by_rows<B, true>(x, w, N, D, F, act, h, s)
+                                    : by_rows<B, false>(x, w, N, D, F, act, h, s));
   return ok ? SLIM_OK : SLIM_ERR_CUDA;
 }
 

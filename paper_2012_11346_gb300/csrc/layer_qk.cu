@@ -1,10 +1,10 @@
 // Norms of queries and keys per head with the rotation by position, and their
 // gradients.  Contract: include/slim_layer.h.
 //
-// A row of one token and head is held by 1 to 32 lanes, eight features each, as
-// two vectors of four: in the split layout the lower and upper member of four
-// pairs, so that a pair never leaves its lane.  The row's sums (of squares, and
-// backward of g x) go over its lanes by shuffles; nothing else is exchanged.
+// A row of one token and head is held by 1 to 32 lanes, two vectors of up to 16 bytes
+// each: in the split layout the lower and upper members of some pairs, so that a pair
+// never leaves its lane.  The row's sums (of squares, and backward of g x) go over its
+// lanes by shuffles; nothing else is exchanged.
 //
 // Angles are fractions of a turn in 64-bit fixed point: position * frequency
 // mod 1 is one integer product whose overflow is the reduction.  A block takes
@@ -20,6 +20,8 @@
 #include <math.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "../../include/slim_layer.h"
 #include "common.cuh"
 #include "launch.h"
@@ -34,7 +36,7 @@ constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kMaxD = 256, kMaxPairs = kMaxD / 2;
 constexpr int kMaxTokens = 16;       // of a tile
 constexpr int kMaxHeads = 4096;
-constexpr int kBwdBlocks = 152 * 4;  // all of them resident; the workspace is for as many
+constexpr int kBwdBlocks = 152 * 3;  // most that are resident; the workspace is for as many
 
 struct Side {
   const void *x, *dy;  // dy: backward
@@ -51,6 +53,7 @@ struct Job {
   const void* positions;
   int i64, tokens, L, d, half, interleaved;
   int tile;            // tokens of a tile
+  unsigned by_heads, by_half;  // ceil(2^32 / (both sides' heads)), / half
   float eps, scale;
   unsigned long long turn[kMaxPairs];  // frequencies, 2^64 = one turn per position
 };
@@ -75,83 +78,101 @@ __device__ __forceinline__ float2 cos_sin(unsigned long long turn) {
   return q & 2 ? make_float2(-c, -s) : make_float2(c, s);
 }
 
-// MODE 0: any layout and alignment, by elements; 1: split pairs, 2: interleaved
-// pairs, both in vectors of four.
+// How a lane holds its 2 W values, two vectors of W: SPLIT, the lower and the upper
+// members of W pairs; INTER, W pairs one behind the other; ANY, by elements, any layout
+// and alignment.  Behind the turned features both are 2 W of them in a row.
 enum { ANY = 0, SPLIT = 1, INTER = 2 };
-template <typename T, int MODE> struct Row {
-  // feature of the lane's value i, lanes holding pairs 4 g ..
+template <typename T, int MODE, int W> struct Row {
+  static constexpr int N = 2 * W;
+  using Raw = typename std::conditional<W * sizeof(T) == 16, uint4, uint2>::type;
+  struct Held {  // a row as it lies in memory
+    Raw v[MODE == ANY ? 1 : 2];
+    T e[MODE == ANY ? N : 1];
+  };
+  // feature of the lane's value i, lanes holding pairs W g ..
   static __device__ __forceinline__ int at(const Job& j, int g, int i) {
-    if (MODE == INTER) return 8 * g + i;
-    if (MODE == SPLIT) return 4 * g < j.half ? 4 * g + (i & 3) + (i & 4 ? j.half : 0) : 8 * g + i;
-    const int p = 4 * g + (i & 3), up = i >> 2;
+    if (MODE == INTER) return N * g + i;
+    if (MODE == SPLIT) return W * g < j.half ? W * g + i % W + (i >= W ? j.half : 0) : N * g + i;
+    const int p = W * g + i % W, up = i / W;
     if (p >= j.half || j.interleaved) return 2 * p + up;
     return p + (up ? j.half : 0);
   }
-  static __device__ __forceinline__ void load4(const T* p, float* v) {
-    if constexpr (sizeof(T) == 4) {
-      const float4 u = *reinterpret_cast<const float4*>(p);
-      v[0] = u.x;
-      v[1] = u.y;
-      v[2] = u.z;
-      v[3] = u.w;
-    } else {
-      const uint2 u = *reinterpret_cast<const uint2*>(p);
-      tc::unpack_bf16(u.x, v[0], v[1]);
-      tc::unpack_bf16(u.y, v[2], v[3]);
-    }
+  static __device__ __forceinline__ bool turned(const Job& j, int g, int i) {
+    return W * g + (MODE == ANY ? i : 0) < j.half;
   }
-  static __device__ __forceinline__ void store4(T* p, const float* v) {
-    if constexpr (sizeof(T) == 4)
-      *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
-    else
-      *reinterpret_cast<uint2*>(p) =
-          make_uint2(tc::pack_bf16(v[0], v[1]), tc::pack_bf16(v[2], v[3]));
-  }
-  static __device__ __forceinline__ void load(const Job& j, const T* row, int g, bool on, float* v) {
-    if (MODE == ANY) {
+  static __device__ __forceinline__ void fetch(const Job& j, const T* row, int g, bool on, Held& h) {
+    if constexpr (MODE == ANY) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
+      for (int i = 0; i < N; ++i) {
         const int e = at(j, g, i);
-        v[i] = on && e < j.d ? Io<T>::load(row, e) : 0.0f;
+        h.e[i] = on && e < j.d ? row[e] : T(0.0f);
       }
     } else if (on) {
-      load4(row + at(j, g, 0), v);
-      load4(row + at(j, g, 4), v + 4);
+      h.v[0] = *reinterpret_cast<const Raw*>(row + at(j, g, 0));
+      h.v[1] = *reinterpret_cast<const Raw*>(row + at(j, g, W));
+    } else {
+      h.v[0] = h.v[1] = Raw{};
+    }
+  }
+  static __device__ __forceinline__ void values(const Held& h, float* v) {
+    if constexpr (MODE == ANY) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) v[i] = Io<T>::load(h.e, i);
     } else {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = 0.0f;
+      for (int k = 0; k < 2; ++k) {
+        const uint32_t* u = reinterpret_cast<const uint32_t*>(&h.v[k]);
+#pragma unroll
+        for (int i = 0; i < (int)(W * sizeof(T) / 4); ++i) {
+          if constexpr (sizeof(T) == 4)
+            v[W * k + i] = __uint_as_float(u[i]);
+          else
+            tc::unpack_bf16(u[i], v[W * k + 2 * i], v[W * k + 2 * i + 1]);
+        }
+      }
     }
   }
   static __device__ __forceinline__ void store(const Job& j, T* row, int g, const float* v) {
-    if (MODE == ANY) {
+    if constexpr (MODE == ANY) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
+      for (int i = 0; i < N; ++i) {
         const int e = at(j, g, i);
         if (e < j.d) Io<T>::store(row, e, v[i]);
       }
     } else {
-      store4(row + at(j, g, 0), v);
-      store4(row + at(j, g, 4), v + 4);
-    }
-  }
-  // the lane's pairs turned (sign 1) or turned back (-1)
-  static __device__ __forceinline__ void rotate(const Job& j, const float2* turns, int g, float sign,
-                                                float* v) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if (4 * g + (MODE == ANY ? i : 0) >= j.half) break;
-      const float2 cs = turns[4 * g + i];
-      float& a = MODE == INTER ? v[2 * i] : v[i];
-      float& b = MODE == INTER ? v[2 * i + 1] : v[i + 4];
-      const float s = sign * cs.y, x = a;
-      a = fmaf(x, cs.x, -b * s);
-      b = fmaf(x, s, b * cs.x);
+      for (int k = 0; k < 2; ++k) {
+        Raw r;
+        uint32_t* u = reinterpret_cast<uint32_t*>(&r);
+#pragma unroll
+        for (int i = 0; i < (int)(W * sizeof(T) / 4); ++i)
+          u[i] = sizeof(T) == 4 ? __float_as_uint(v[W * k + i]) : tc::pack_bf16(v[W * k + 2 * i], v[W * k + 2 * i + 1]);
+        *reinterpret_cast<Raw*>(row + at(j, g, W * k)) = r;
+      }
     }
   }
+  // sum of a b: by four pairs at a time, as lanes of narrower vectors hold them, so that
+  // a row's bits do not depend on its alignment
+  static __device__ __forceinline__ float dot(const float* a, const float* b) {
+    float sum[W / 4];
+#pragma unroll
+    for (int k = 0; k < W / 4; ++k) {
+      sum[k] = 0.0f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int e = MODE == INTER ? 8 * k + i : 4 * k + i % 4 + (i >= 4 ? W : 0);
+        sum[k] = fmaf(a[e], b[e], sum[k]);
+      }
+    }
+    return W == 8 ? sum[0] + sum[W / 4 - 1] : sum[0];
+  }
+  // the members of the lane's pair i
+  static __device__ __forceinline__ float& low(float* v, int i) { return v[MODE == INTER ? 2 * i : i]; }
+  static __device__ __forceinline__ float& high(float* v, int i) { return v[MODE == INTER ? 2 * i + 1 : i + W]; }
 };
 
 __device__ __forceinline__ float over_lanes(float v, int G) {
-  for (int o = G >> 1; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  for (int o = 1; o < G; o <<= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
   return v;
 }
 
@@ -159,103 +180,169 @@ struct TokenAt {
   long long x, dy, out;
 };
 
-template <typename T, int MODE, bool BWD>
-__global__ void __launch_bounds__(kThreads) k_qk_norm(const __grid_constant__ Job j, int lanes_log2) {
-  using R = Row<T, MODE>;
-  extern __shared__ float2 turns[];  // [tile][half]
-  __shared__ TokenAt token[kMaxTokens];
-  const int which = blockIdx.x >= j.side[0].blocks;
-  const Side& s = j.side[which];
-  const int block = blockIdx.x - (which ? j.side[0].blocks : 0);
+// Of an SM: two vectors of 8 values, their gradients and sums fill a thread's registers.
+constexpr int bwd_blocks(int W) { return W == 8 ? 2 : 3; }
+
+// The turns of a tile's tokens lie in shared memory, for all heads.  Forward, a block has
+// both sides' heads; backward one side's, whose weights' sums it keeps.  The next row is
+// on its way while one is at work, the first under the turns.
+//
+// A token's turns are in the order in which lanes read them, two pairs at a time: the
+// lanes of a row side by side (pair after pair, four lanes met in one bank).
+template <typename T, int MODE, int W, bool BWD>
+__global__ void __launch_bounds__(kThreads, BWD ? bwd_blocks(W) : 3) k_qk_norm(const __grid_constant__ Job j, int lanes_log2) {
+  using R = Row<T, MODE, W>;
+  constexpr int N = 2 * W;
+  extern __shared__ float4 turns[];  // [tile][W / 2][rim]
+  __shared__ TokenAt token[BWD ? 1 : 2][kMaxTokens];
+  __shared__ long long position[kMaxTokens];
+  __shared__ __align__(16) float weight[BWD ? 1 : 2][kMaxD];  // times scale
+  __shared__ unsigned long long frequency[kMaxPairs];
+  const int mine = BWD && blockIdx.x >= j.side[0].blocks;
+  const Side& s = j.side[mine];
+  const int block = blockIdx.x - (mine ? j.side[0].blocks : 0);
+  const int H = BWD ? s.H : j.side[0].H + j.side[1].H;
   const int G = 1 << lanes_log2, g = threadIdx.x & (G - 1);
   const int first = threadIdx.x >> lanes_log2, step = kThreads >> lanes_log2;
-  const bool lane_on = 8 * g < j.d;
+  const int rim = (j.half + W - 1) / W;  // lanes with turned pairs
+  const bool lane_on = N * g < j.d;
   const float over_d = 1.0f / j.d;
-  float w[8], dw[8];
+  // (lanes that read different parameters wait for each other: once a block, not a turn)
+  if (threadIdx.x < j.half) frequency[threadIdx.x] = j.turn[threadIdx.x];
+  if (!BWD && threadIdx.x < j.d)
+    for (int k = 0; k < 2; ++k) weight[k][threadIdx.x] = (j.side[k].w ? j.side[k].w[threadIdx.x] : 1.0f) * j.scale;
+  float w[BWD ? N : 1], dw[BWD ? N : 1];
+  if (BWD) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int e = R::at(j, g, i);
-    w[i] = (lane_on && e < j.d ? (s.w ? s.w[e] : 1.0f) : 0.0f) * j.scale;
-    dw[i] = 0.0f;
+    for (int i = 0; i < N; ++i) {
+      const int e = R::at(j, g, i);
+      w[i] = (lane_on && e < j.d ? (s.w ? s.w[e] : 1.0f) : 0.0f) * j.scale;
+      dw[i] = 0.0f;
+    }
   }
   const int tiles = (j.tokens + j.tile - 1) / j.tile;
   for (int tile = block; tile < tiles; tile += s.blocks) {
     const int n0 = tile * j.tile, count = min(j.tile, j.tokens - n0);
+    const int rows = count * H;
     __syncthreads();
     if (threadIdx.x < count) {
       const int n = n0 + threadIdx.x, b = n / j.L, l = n - b * j.L;
-      token[threadIdx.x] = TokenAt{b * s.xs.b + l * s.xs.l, BWD ? b * s.dys.b + l * s.dys.l : 0,
-                                   b * s.os.b + l * s.os.l};
-    }
-    for (int i = threadIdx.x; i < count * j.half; i += kThreads) {
-      const int t = i / j.half, p = i - t * j.half, n = n0 + t;
-      long long pos = n % j.L;
-      if (j.positions)
-        pos = j.i64 ? static_cast<const long long*>(j.positions)[n]
-                    : static_cast<const int*>(j.positions)[n];
-      turns[i] = cos_sin((unsigned long long)pos * j.turn[p]);
+      position[threadIdx.x] = !j.positions ? l
+                              : j.i64      ? static_cast<const long long*>(j.positions)[n]
+                                           : static_cast<const int*>(j.positions)[n];
+      for (int k = 0; k < (BWD ? 1 : 2); ++k) {
+        const Side& t = j.side[BWD ? mine : k];
+        token[k][threadIdx.x] = TokenAt{b * t.xs.b + l * t.xs.l, BWD ? b * t.dys.b + l * t.dys.l : 0,
+                                        b * t.os.b + l * t.os.l};
+      }
     }
     __syncthreads();
-    const int rows = count * s.H;
+    // a row's token, side (of the block's) and head
+    auto place = [&](int r, int& t, int& k, int& h) {
+      r = r < rows ? r : 0;
+      t = H == 1 ? r : (int)__umulhi((unsigned)r, BWD ? s.by_head : j.by_heads);
+      h = r - t * H;
+      k = !BWD && h >= j.side[0].H;
+      if (k) h -= j.side[0].H;
+    };
+    typename R::Held hx, hy;
+    auto fetch = [&](int r) {
+      int t, k, h;
+      place(r, t, k, h);
+      const bool on = r < rows && lane_on;
+      const Side& of = BWD ? s : k ? j.side[1] : j.side[0];
+      R::fetch(j, static_cast<const T*>(of.x) + token[k][t].x + h * of.xs.h, g, on, hx);
+      if (BWD) R::fetch(j, static_cast<const T*>(s.dy) + token[0][t].dy + h * s.dys.h, g, on, hy);
+    };
+    fetch(first);
+    for (int i = threadIdx.x; i < count * j.half; i += kThreads) {
+      const int t = j.half == 1 ? i : (int)__umulhi((unsigned)i, j.by_half), p = i - t * j.half, v = p % W;
+      const float2 cs = cos_sin((unsigned long long)position[t] * frequency[p]);
+      reinterpret_cast<float2*>(turns)[(t * (W / 2) + v / 2) * rim * 2 + p / W * 2 + v % 2] = cs;
+    }
+    __syncthreads();
     // whole warps walk together: their lanes exchange sums
     for (int r0 = first; r0 - first < rows; r0 += step) {
-      const bool on = r0 < rows;
-      const int r = on ? r0 : 0;
-      const int t = s.H == 1 ? r : (int)__umulhi((unsigned)r, s.by_head), h = r - t * s.H;
-      const TokenAt at = token[t];
-      float x[8], dz[8];
-      R::load(j, static_cast<const T*>(s.x) + at.x + h * s.xs.h, g, on && lane_on, x);
-      if (BWD) R::load(j, static_cast<const T*>(s.dy) + at.dy + h * s.dys.h, g, on && lane_on, dz);
-      float ss = 0.0f;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) ss = fmaf(x[i], x[i], ss);
-      ss = over_lanes(ss, G);
+      float x[N], dz[BWD ? N : 1];
+      R::values(hx, x);
+      if constexpr (BWD) R::values(hy, dz);
+      if (r0 + step - first < rows) fetch(r0 + step);
+      int t, k, h;
+      place(r0, t, k, h);
+      float ss = over_lanes(R::dot(x, x), G);
       float fit = 1.0f;
       if (__any_sync(0xffffffffu, !(ss <= 1e38f))) {
         // squares past fp32's range: the row in smaller units, next to which eps is nothing
         if (!(ss <= 1e38f)) fit = 0x1p-80f;
-        ss = 0.0f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          x[i] *= fit;
-          ss = fmaf(x[i], x[i], ss);
-        }
-        ss = over_lanes(ss, G);
+        for (int i = 0; i < N; ++i) x[i] *= fit;
+        ss = over_lanes(R::dot(x, x), G);
       }
       const float rms = rsqrtf(fmaf(ss, over_d, j.eps * (fit * fit)));
 #pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] *= rms;
-      const float2* cs = turns + t * j.half;
-      if (!BWD) {
+      for (int i = 0; i < N; ++i) x[i] *= rms;
+      if constexpr (!BWD) {
+        if (MODE == ANY) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] *= w[i];
-        R::rotate(j, cs, g, 1.0f, x);
-      } else {
-        R::rotate(j, cs, g, -1.0f, dz);
-        float gn = 0.0f;
+          for (int i = 0; i < N; ++i) x[i] *= weight[k][min(R::at(j, g, i), kMaxD - 1)];
+        } else if (lane_on) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+          for (int i = 0; i < N; i += 4) {
+            const float4 f = *reinterpret_cast<const float4*>(&weight[k][R::at(j, g, i)]);
+            x[i] *= f.x;
+            x[i + 1] *= f.y;
+            x[i + 2] *= f.z;
+            x[i + 3] *= f.w;
+          }
+        }
+      }
+      if (W * g < j.half) {
+        const float4* turn = turns + t * (W / 2) * rim + g;
+#pragma unroll
+        for (int i = 0; i < W; i += 2) {
+          const float4 two = turn[i / 2 * rim];
+#pragma unroll
+          for (int v = 0; v < 2; ++v) {
+            const float c = v ? two.z : two.x, sn = (v ? two.w : two.y) * (BWD ? -1.0f : 1.0f);
+            float* y;
+            if constexpr (BWD)
+              y = dz;
+            else
+              y = x;
+            if (MODE == ANY && !R::turned(j, g, i + v)) continue;
+            float &a = R::low(y, i + v), &b = R::high(y, i + v);
+            const float u = a;
+            a = fmaf(u, c, -b * sn);
+            b = fmaf(u, sn, b * c);
+          }
+        }
+      }
+      if constexpr (BWD) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
           dw[i] = fmaf(dz[i], x[i], dw[i]);
           dz[i] *= w[i];
-          gn = fmaf(dz[i], x[i], gn);
         }
-        gn = over_lanes(gn, G) * over_d;
+        const float gn = over_lanes(R::dot(dz, x), G) * over_d;
         const float out = fit * rms;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = out * fmaf(-x[i], gn, dz[i]);
+        for (int i = 0; i < N; ++i) x[i] = out * fmaf(-x[i], gn, dz[i]);
       }
-      if (on && lane_on) R::store(j, static_cast<T*>(s.out) + at.out + h * s.os.h, g, x);
+      const Side& of = BWD ? s : k ? j.side[1] : j.side[0];
+      if (r0 < rows && lane_on) R::store(j, static_cast<T*>(of.out) + token[k][t].out + h * of.os.h, g, x);
     }
   }
   if (!BWD || !s.part) return;
   // the block's sums: rows of a warp, then warps in order
   __shared__ float sum[kWarps][kMaxD];
   const int warp = threadIdx.x >> 5;
+  if constexpr (BWD) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    for (int o = 16; o >= G; o >>= 1) dw[i] += __shfl_xor_sync(0xffffffffu, dw[i], o);
-    const int e = R::at(j, g, i);
-    if ((threadIdx.x & 31) < G && lane_on && e < j.d) sum[warp][e] = dw[i] * j.scale;
+    for (int i = 0; i < N; ++i) {
+      for (int o = 16; o >= G; o >>= 1) dw[i] += __shfl_xor_sync(0xffffffffu, dw[i], o);
+      const int e = R::at(j, g, i);
+      if ((threadIdx.x & 31) < G && lane_on && e < j.d) sum[warp][e] = dw[i] * j.scale;
+    }
   }
   __syncthreads();
   if (threadIdx.x < j.d) {
@@ -266,25 +353,25 @@ __global__ void __launch_bounds__(kThreads) k_qk_norm(const __grid_constant__ Jo
   }
 }
 
-// The weights' gradients from the blocks' sums: 32 features a block, eight threads each.
-__global__ void __launch_bounds__(kThreads) k_qk_weights(WeightJob j) {
+// The weights' gradients from the blocks' sums: 32 features a block, 32 threads each.
+__global__ void __launch_bounds__(1024) k_qk_weights(WeightJob j) {
   tc::grid_dependency_wait();
-  __shared__ float sh[8][32];
+  __shared__ float sh[32][33];
   const int which = blockIdx.y, col = threadIdx.x & 31, q = threadIdx.x >> 5;
   const int e = blockIdx.x * 32 + col, n = j.blocks[which];
   if (!j.out[which]) return;
   float v = 0.0f;
-  const int per = (n + 7) / 8, to = min((q + 1) * per, n);
+  const int per = (n + 31) / 32, to = min((q + 1) * per, n);
   if (e < j.d) {
 #pragma unroll 8
     for (int b = q * per; b < to; ++b) v += j.part[which][(size_t)b * j.d + e];
   }
-  sh[q][col] = v;
+  sh[col][q] = v;
   __syncthreads();
-  if (q == 0 && e < j.d) {
-    for (int i = 1; i < 8; ++i) v += sh[i][col];
-    j.out[which][e] = v;
-  }
+  // a warp a feature: its lanes' sums in a fixed tree
+  v = sh[q][col];
+  for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  if (col == 0 && blockIdx.x * 32 + q < j.d) j.out[which][blockIdx.x * 32 + q] = v;
 }
 
 // ------------------------------------------------------------------ host
@@ -330,16 +417,24 @@ struct Operand {  // of a side: x, dy or out
   const slim_strides* s;
 };
 
-// Whether every row of the tensor can be moved in vectors of four elements.
-bool in_fours(const void* p, const slim_strides& s, int es) {
-  return (reinterpret_cast<uintptr_t>(p) & (4 * es - 1)) == 0 && ((s.b | s.h | s.l) & 3) == 0;
+// What all rows of all tensors can be moved in: elements, up to 16 bytes.
+struct Layout {
+  int together;
+};
+void fit(Layout* in, const void* p, const slim_strides& s, int es) {
+  while (in->together > 1 && ((reinterpret_cast<uintptr_t>(p) & (in->together * es - 1)) ||
+                              ((s.b | s.h | s.l) & (in->together - 1))))
+    in->together /= 2;
 }
 
+// i / n is the upper half of i * by(n) for small i, n > 1.
+unsigned by(int n) { return n <= 1 ? 0u : (unsigned)(((1ull << 32) + n - 1) / n); }
+
 bool fill_side(Side* t, const Operand& x, const Operand* dy, const Operand& out, const float* w, int B,
-               int H, int L, int d, int es, bool* fours) {
+               int H, int L, int d, int es, Layout* in) {
   t->H = H;
   if (H == 0) return true;
-  t->by_head = H == 1 ? 0u : (unsigned)(((1ull << 32) + H - 1) / H);
+  t->by_head = by(H);
   const Operand none{nullptr, nullptr};
   const Operand* all[3] = {&x, dy ? dy : &none, &out};
   slim_strides* to[3] = {&t->xs, &t->dys, &t->os};
@@ -348,7 +443,7 @@ bool fill_side(Side* t, const Operand& x, const Operand* dy, const Operand& out,
     if (!all[i]->p || (reinterpret_cast<uintptr_t>(all[i]->p) & (es - 1))) return false;
     *to[i] = strides_of(all[i]->s, H, L, d);
     if (!strides_ok(*to[i], B, H, L)) return false;
-    *fours = *fours && in_fours(all[i]->p, *to[i], es);
+    fit(in, all[i]->p, *to[i], es);
   }
   if (!apart(t->os, B, H, L, d)) return false;
   if (w && (reinterpret_cast<uintptr_t>(w) & 3)) return false;
@@ -359,16 +454,32 @@ bool fill_side(Side* t, const Operand& x, const Operand* dy, const Operand& out,
   return true;
 }
 
+template <typename T, int MODE, int W, bool BWD>
+void start(const Job& j, unsigned blocks, cudaStream_t s) {
+  int lanes_log2 = 0;
+  while ((2 * W << lanes_log2) < j.d) ++lanes_log2;
+  const size_t smem = (size_t)j.tile * ((j.half + W - 1) / W) * (W / 2) * sizeof(float4);
+  k_qk_norm<T, MODE, W, BWD><<<blocks, kThreads, smem, s>>>(j, lanes_log2);
+}
+// Values of a vector that all rows can be moved in, 0: elements.
+template <typename T>
+int vectors(const Job& j, const Layout& in) {
+  constexpr int whole = 16 / sizeof(T);
+  if (in.together < 4 || j.d % 8 || j.half % 4) return 0;
+  return in.together >= whole && j.d % (2 * whole) == 0 && j.half % whole == 0 ? whole : 4;
+}
 template <typename T, bool BWD>
-bool run(const Job& j, int mode, int lanes_log2, cudaStream_t s) {
-  const unsigned blocks = (unsigned)(j.side[0].blocks + j.side[1].blocks);
-  const size_t smem = (size_t)j.tile * j.half * sizeof(float2);
+bool run(const Job& j, const Layout& in, cudaStream_t s) {
+  const unsigned blocks = (unsigned)(j.side[0].blocks + (BWD ? j.side[1].blocks : 0));
   const double n = (double)j.tokens * (j.side[0].H + j.side[1].H) * j.d;
   prof::Scope ps(prof::K_QK_NORM, s, n * (BWD ? 20 : 8), n * sizeof(T) * (BWD ? 3 : 2));
-  auto k = mode == SPLIT ? k_qk_norm<T, SPLIT, BWD>
-           : mode == INTER ? k_qk_norm<T, INTER, BWD>
-                           : k_qk_norm<T, ANY, BWD>;
-  k<<<blocks, kThreads, smem, s>>>(j, lanes_log2);
+  const int w = vectors<T>(j, in);
+  if (w == 0)
+    start<T, ANY, 4, BWD>(j, blocks, s);
+  else if (w == 4)
+    j.interleaved ? start<T, INTER, 4, BWD>(j, blocks, s) : start<T, SPLIT, 4, BWD>(j, blocks, s);
+  else
+    j.interleaved ? start<T, INTER, 16 / sizeof(T), BWD>(j, blocks, s) : start<T, SPLIT, 16 / sizeof(T), BWD>(j, blocks, s);
   return cudaGetLastError() == cudaSuccess;
 }
 
@@ -412,7 +523,7 @@ namespace {
 int set_up(Job* j, const Operand q[3], const Operand k[3], bool bwd, const float* wq, const float* wk,
            const void* positions, slim_index ptype, const double* inv_freq, int rotary,
            int interleaved, int B, int Hq, int Hk, int L, int d, slim_dtype dtype, float eps,
-           float scale, int* mode, int* lanes_log2) {
+           float scale, Layout* in) {
   if (!sizes_ok(B, Hq, Hk, L, d) || (dtype != SLIM_F32 && dtype != SLIM_BF16)) return -1;
   if (rotary < 0 || rotary > d || (rotary & 1) || (interleaved & ~1)) return -1;
   if (rotary > 0 && (!inv_freq || (ptype != SLIM_I32 && ptype != SLIM_I64))) return -1;
@@ -427,9 +538,9 @@ int set_up(Job* j, const Operand q[3], const Operand k[3], bool bwd, const float
   }
   if ((long long)B * L == 0) return 0;
   const int es = dtype == SLIM_F32 ? 4 : 2;
-  bool fours = true;
-  if (!fill_side(&j->side[0], q[0], bwd ? &q[1] : nullptr, q[2], wq, B, Hq, L, d, es, &fours) ||
-      !fill_side(&j->side[1], k[0], bwd ? &k[1] : nullptr, k[2], wk, B, Hk, L, d, es, &fours))
+  in->together = 16 / es;
+  if (!fill_side(&j->side[0], q[0], bwd ? &q[1] : nullptr, q[2], wq, B, Hq, L, d, es, in) ||
+      !fill_side(&j->side[1], k[0], bwd ? &k[1] : nullptr, k[2], wk, B, Hk, L, d, es, in))
     return -1;
   if (positions && (reinterpret_cast<uintptr_t>(positions) & (ptype == SLIM_I64 ? 7 : 3))) return -1;
   j->positions = positions;
@@ -438,12 +549,11 @@ int set_up(Job* j, const Operand q[3], const Operand k[3], bool bwd, const float
   j->L = L;
   j->d = d;
   j->half = rotary / 2;
+  j->by_heads = by(Hq + Hk);
+  j->by_half = by(rotary / 2);
   j->interleaved = interleaved;
   j->eps = eps;
   j->scale = scale;
-  *mode = !fours || d % 8 || rotary % 8 ? ANY : interleaved ? INTER : SPLIT;
-  *lanes_log2 = 0;
-  while ((8 << *lanes_log2) < d) ++*lanes_log2;
   return 1;
 }
 }  // namespace
@@ -460,16 +570,16 @@ extern "C" slim_status slim_qk_norm_fwd(const void* q, const slim_strides* q_str
                                         const slim_strides* k_out_strides, void* stream) {
   using namespace slim::layer;
   Job j{};
-  int mode, lanes;
+  Layout in;
   const Operand qs[3] = {{q, q_strides}, {}, {q_out, q_out_strides}};
   const Operand ks[3] = {{k, k_strides}, {}, {k_out, k_out_strides}};
   const int go = set_up(&j, qs, ks, false, q_weight, k_weight, positions, ptype, inv_freq, rotary,
-                        interleaved, B, Hq, Hk, L, d, dtype, eps, scale, &mode, &lanes);
+                        interleaved, B, Hq, Hk, L, d, dtype, eps, scale, &in);
   if (go <= 0) return go < 0 ? SLIM_ERR_INVALID_ARG : SLIM_OK;
   deal(&j, 0);
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  const bool ok = dtype == SLIM_F32 ? run<float, false>(j, mode, lanes, s)
-                                    : run<__nv_bfloat16, false>(j, mode, lanes, s);
+  const bool ok = dtype == SLIM_F32 ? run<float, false>(j, in, s)
+                                    : run<__nv_bfloat16, false>(j, in, s);
   return ok ? SLIM_OK : SLIM_ERR_CUDA;
 }
 
@@ -483,13 +593,13 @@ extern "C" slim_status slim_qk_norm_bwd(
     size_t workspace_bytes, void* stream) {
   using namespace slim::layer;
   Job j{};
-  int mode, lanes;
+  Layout in;
   const Operand qs[3] = {{q, q_strides}, {dq_out, dq_out_strides}, {dq, dq_strides}};
   const Operand ks[3] = {{k, k_strides}, {dk_out, dk_out_strides}, {dk, dk_strides}};
   for (const float* p : {dq_weight, dk_weight})
     if (reinterpret_cast<uintptr_t>(p) & 3) return SLIM_ERR_INVALID_ARG;
   const int go = set_up(&j, qs, ks, true, q_weight, k_weight, positions, ptype, inv_freq, rotary,
-                        interleaved, B, Hq, Hk, L, d, dtype, eps, scale, &mode, &lanes);
+                        interleaved, B, Hq, Hk, L, d, dtype, eps, scale, &in);
   if (go < 0) return SLIM_ERR_INVALID_ARG;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   if (go == 0 || Hk == 0) {
@@ -503,7 +613,8 @@ extern "C" slim_status slim_qk_norm_bwd(
   slim_qk_norm_bwd_workspace_size(B, Hq, Hk, L, d, &need);
   if (!workspace || workspace_bytes < need) return SLIM_ERR_WORKSPACE;
   if (reinterpret_cast<uintptr_t>(workspace) & 255) return SLIM_ERR_INVALID_ARG;
-  deal(&j, kBwdBlocks);
+  const int width = dtype == SLIM_F32 ? vectors<float>(j, in) : vectors<__nv_bfloat16>(j, in);
+  deal(&j, 152 * bwd_blocks(width));
   float* part = static_cast<float*>(workspace);
   WeightJob wj{};
   wj.d = d;
@@ -515,12 +626,12 @@ extern "C" slim_status slim_qk_norm_bwd(
     j.side[i].part = out[i] ? part : nullptr;
     part += (size_t)j.side[i].blocks * d;
   }
-  const bool ok = dtype == SLIM_F32 ? run<float, true>(j, mode, lanes, s)
-                                    : run<__nv_bfloat16, true>(j, mode, lanes, s);
+  const bool ok = dtype == SLIM_F32 ? run<float, true>(j, in, s)
+                                    : run<__nv_bfloat16, true>(j, in, s);
   if (!ok) return SLIM_ERR_CUDA;
   if (out[0] || out[1]) {
     slim::prof::Scope ps(slim::prof::K_QK_WEIGHTS, s);
-    if (!slim::launch_on(k_qk_weights, dim3((d + 31) / 32, 2), kThreads, 0, 1, true, s, wj))
+    if (!slim::launch_on(k_qk_weights, dim3((d + 31) / 32, 2), 1024, 0, 1, true, s, wj))
       return SLIM_ERR_CUDA;
   }
   return SLIM_OK;

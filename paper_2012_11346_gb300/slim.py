@@ -10,6 +10,7 @@ import array
 import contextlib
 import ctypes
 import functools
+import math
 import os
 
 import torch
@@ -785,29 +786,42 @@ def vocab_loss(x, w, targets, reduction="mean", ignore_index=-100, piece=None):
 
 
 # ---------------------------------------------------------------- around the attention
-def _on_device(t):
-    """The context in which a call on tensor t launches: its device as the current one."""
-    return _HERE if t.get_device() == torch.cuda.current_device() else torch.cuda.device(t.device)
+# A call's Python is most of a decoding step's time: what depends on sizes, strides and
+# types alone is checked once for each of them and kept.
+def _at(dev, stream):
+    """The context in which a call allocates and launches: tensors' device as the current
+    one, and what _on says of `stream`."""
+    if stream is None:
+        return _HERE if dev == torch._C._cuda_getDevice() else torch.cuda.device(dev)
+    # (it makes the stream's device the current one, too)
+    return torch.cuda.stream(stream)
 
 
-def _one_device(*ts):
-    """CUDA tensors (None: left out), all on one device."""
-    dev = None
-    for t in ts:
-        if t is None:
-            continue
-        if not t.is_cuda:
-            raise RuntimeError("libslim runs on CUDA tensors only (no CPU fallback)")
-        if dev is None:
-            dev = t.device
-        elif t.device != dev:
-            raise ValueError("tensors on different devices")
+def _raw(dev, stream):
+    """The raw stream of a call on device `dev`: `stream`, or the current one."""
+    return torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
+
+
+def _device_of(t, *others):
+    """The index of the one device that CUDA tensors (None: left out) are on."""
+    dev = t.get_device()
+    cuda = dev >= 0
+    for o in others:
+        if o is not None and o.get_device() != dev:
+            if cuda and o.is_cuda:
+                raise ValueError("tensors on different devices")
+            cuda = False
+    if not cuda:
+        raise RuntimeError("libslim runs on CUDA tensors only (no CPU fallback)")
+    return dev
 
 
 def _fp32_or_none(t, shape, what):
-    if t is not None and (t.dtype != torch.float32 or tuple(t.shape) != shape or not t.is_contiguous()):
+    if t is None:
+        return None
+    if t.dtype != torch.float32 or t.shape != shape or not t.is_contiguous():
         raise ValueError(f"{what} must be contiguous fp32 of shape {list(shape)}")
-    return None if t is None else t.data_ptr()
+    return t.data_ptr()
 
 
 def rotary_frequencies(rotary, base=10000.0):
@@ -816,56 +830,76 @@ def rotary_frequencies(rotary, base=10000.0):
     return array.array("d", [base ** (-2.0 * p / rotary) for p in range(rotary // 2)])
 
 
+@functools.lru_cache(maxsize=1024)
+def _qk_sizes(q, k, positions, rotary, dtype, k_dtype, what):
+    """(B, Hq, Hk, L, d, dtype code) of checked shapes."""
+    if len(q) != 4 or (k is not None and len(k) != 4):
+        raise ValueError("q and k must be [B, H, L, d]")
+    B, Hq, L, d = q
+    Hk = 0 if k is None else k[1]
+    if k is not None and (k_dtype != dtype or tuple(k) != (B, Hk, L, d)):
+        raise ValueError("k must be [B, Hk, L, d] in q's dtype")
+    if (B | Hq | Hk | L | d) >> 31:
+        _too_large()
+    _require(rotary <= d, "more frequencies than pairs of features")
+    if positions is not None and tuple(positions) != (B, L):
+        raise ValueError("positions must be contiguous [B, L]")
+    if dtype not in DTYPES:
+        raise TypeError(f"{what}: float32 or bfloat16 expected, got {dtype}")
+    return B, Hq, Hk, L, d, DTYPES[dtype]
+
+
+@functools.lru_cache(maxsize=1024)
+def _strides(stride, d):
+    """A [B, H, L, d] tensor's slim_strides; the last dimension is contiguous."""
+    if stride[3] != 1 and d > 1:
+        raise RuntimeError("libslim needs rows whose features are contiguous")
+    return array.array("q", stride[:3])
+
+
 class _QkCall:
     """What both directions of qk_norm marshal alike."""
 
     def __init__(self, q, k, q_weight, k_weight, positions, inv_freq, what):
-        if q.dim() != 4 or (k is not None and k.dim() != 4):
-            raise ValueError("q and k must be [B, H, L, d]")
-        B, Hq, L, d = self.dims = q.shape
-        Hk = 0 if k is None else k.shape[1]
-        if k is not None and (k.dtype != q.dtype or tuple(k.shape) != (B, Hk, L, d)):
-            raise ValueError("k must be [B, Hk, L, d] in q's dtype")
-        if (B | Hq | Hk | L | d) >> 31:
-            _too_large()
         if inv_freq is None:
             inv_freq = ()
         elif isinstance(inv_freq, torch.Tensor) and inv_freq.is_cuda:
             raise TypeError("inv_freq is read on the host: give numbers or a CPU tensor")
         if not (isinstance(inv_freq, array.array) and inv_freq.typecode == "d"):
             inv_freq = array.array("d", map(float, inv_freq))
-        self.freq, rotary = inv_freq, 2 * len(inv_freq)
-        _require(rotary <= d, "more frequencies than pairs of features")
-        ptype = 0
+        rotary = 2 * len(inv_freq)
+        self.q, self.k = q, k
+        self.sizes = _qk_sizes(q.shape, None if k is None else k.shape,
+                               None if positions is None else positions.shape, rotary, q.dtype,
+                               None if k is None else k.dtype, what)
+        B, Hq, Hk, L, self.d, _ = self.sizes
+        pp, ptype = None, 0
         if positions is not None:
             ptype = _index_code(positions, "positions")
-            if tuple(positions.shape) != (B, L) or not positions.is_contiguous():
+            if not positions.is_contiguous():
                 raise ValueError("positions must be contiguous [B, L]")
-        _one_device(q, k, q_weight, k_weight, positions)
-        self.keep, self.shapes = [], ((B, Hq, L, d), (B, Hk, L, d))
-        self.head = (*self.rows(q, 0), *self.rows(k, 1), _fp32_or_none(q_weight, (d,), "q_weight"),
-                     _fp32_or_none(k_weight, (d,), "k_weight"), _ptr(positions), ptype,
+            pp = positions.data_ptr()
+        self.dev = _device_of(q, k, q_weight, k_weight, positions)
+        self.kept = [inv_freq]  # until the call is made
+        self.head = (*self.rows(q), *self.rows(k), _fp32_or_none(q_weight, (self.d,), "q_weight"),
+                     _fp32_or_none(k_weight, (self.d,), "k_weight"), pp, ptype,
                      inv_freq.buffer_info()[0] if rotary else None, rotary)
-        self.sizes = (B, Hq, Hk, L, d, _dtype_code(q, what))
 
-    def rows(self, t, side):
-        """A [B, H, L, d] tensor's pointer and strides; the last dimension is contiguous."""
+    def rows(self, t):
+        """A [B, H, L, d] tensor's pointer and strides."""
         if t is None:
             return None, None
-        b, h, l, one = t.stride()
-        if one != 1 and t.shape[3] > 1:
-            raise RuntimeError("libslim needs rows whose features are contiguous")
-        strides = array.array("q", (b, h, l))
-        self.keep.append(strides)
+        strides = _strides(t.stride(), self.d)
+        self.kept.append(strides)
         return t.data_ptr(), strides.buffer_info()[0]
 
-    def like(self, t, side, given, what, other):
-        """`given`, checked, or a new contiguous tensor for the side that t is of."""
+    def like(self, t, given, what):
+        """`given`, checked, or a new contiguous tensor of t's shape (None: without t)."""
         if given is None:
-            return None if t is None else torch.empty(self.shapes[side], dtype=t.dtype, device=t.device)
-        if t is None or given.dtype != other.dtype or tuple(given.shape) != self.shapes[side]:
+            return None if t is None else t.new_empty(t.shape)
+        if t is None or given.dtype != t.dtype or given.shape != t.shape:
             raise ValueError(f"{what} must have the shape and dtype of its input")
-        _one_device(t, given)
+        _device_of(t, given)
         return given
 
 
@@ -880,13 +914,12 @@ def qk_norm_forward(q, k, q_weight=None, k_weight=None, positions=None, inv_freq
     no rotation.  Returns (q_out, k_out), contiguous unless given; they may be q
     and k themselves."""
     c = _QkCall(q, k, q_weight, k_weight, positions, inv_freq, "qk_norm_forward")
-    with _on_device(q):
-        with _on(stream):
-            q_out = c.like(q, 0, q_out, "q_out", q)
-            k_out = c.like(k, 1, k_out, "k_out", k)
-        _check(library().slim_qk_norm_fwd(*c.head, int(interleaved), *c.sizes, eps, scale,
-                                          *c.rows(q_out, 0), *c.rows(k_out, 1),
-                                          _stream_of(q, stream)), "slim_qk_norm_fwd")
+    with _at(c.dev, stream):
+        q_out = c.like(q, q_out, "q_out")
+        k_out = c.like(k, k_out, "k_out")
+        status = library().slim_qk_norm_fwd(*c.head, int(interleaved), *c.sizes, eps, scale, *c.rows(q_out),
+                                            *c.rows(k_out), _raw(c.dev, stream))
+    _check(status, "slim_qk_norm_fwd")
     return q_out, k_out
 
 
@@ -909,25 +942,21 @@ def qk_norm_backward(q, k, q_weight, k_weight, dq_out, dk_out, positions=None, i
     or dq_out and dk_out themselves.  A weight's gradient ([d] fp32) is None
     where there is no such weight or with weights=False."""
     c = _QkCall(q, k, q_weight, k_weight, positions, inv_freq, "qk_norm_backward")
-    c.like(q, 0, dq_out, "dq_out", q)
-    c.like(k, 1, dk_out, "dk_out", k)
     if dq_out is None or (k is not None and dk_out is None):
         raise ValueError("dq_out and dk_out are needed")
+    c.like(q, dq_out, "dq_out")
+    c.like(k, dk_out, "dk_out")
     if workspace is not None:
         _require_cuda(workspace)
-    B, Hq, Hk, L, d, _ = c.sizes
-    with _on_device(q):
-        with _on(stream):
-            dq = c.like(q, 0, dq, "dq", q)
-            dk = c.like(k, 1, dk, "dk", k)
-            dwq, dwk = (torch.empty_like(w) if weights and w is not None else None
-                        for w in (q_weight, k_weight))
-            ws = workspace if workspace is not None else _workspace(
-                qk_norm_workspace_size(B, Hq, Hk, L, d), q.device)
-        _check(library().slim_qk_norm_bwd(*c.head, int(interleaved), *c.sizes, eps, scale,
-                                          *c.rows(dq_out, 0), *c.rows(dk_out, 1), *c.rows(dq, 0),
-                                          *c.rows(dk, 1), _ptr(dwq), _ptr(dwk), ws.data_ptr(),
-                                          ws.numel(), _stream_of(q, stream)), "slim_qk_norm_bwd")
+    with _at(c.dev, stream):
+        dq = c.like(q, dq, "dq")
+        dk = c.like(k, dk, "dk")
+        dwq, dwk = (w.new_empty(w.shape) if weights and w is not None else None for w in (q_weight, k_weight))
+        ws = workspace if workspace is not None else _workspace(qk_norm_workspace_size(*c.sizes[:5]), q.device)
+        status = library().slim_qk_norm_bwd(*c.head, int(interleaved), *c.sizes, eps, scale, *c.rows(dq_out),
+                                            *c.rows(dk_out), *c.rows(dq), *c.rows(dk), _ptr(dwq), _ptr(dwk),
+                                            ws.data_ptr(), ws.numel(), _raw(c.dev, stream))
+    _check(status, "slim_qk_norm_bwd")
     return dq, dk, dwq, dwk
 
 
@@ -970,10 +999,11 @@ GATES = {"value": 0, "log": 1, "sigmoid": 2}
 SCAN_CHUNK = 64
 
 
-def _pitch(t, what):
+@functools.lru_cache(maxsize=1024)
+def _pitch(shape, stride, what):
     """Elements from a row of [B, L, D] to the next; a slice of wider rows has one, too."""
-    B, L, D = t.shape
-    b, l, one = t.stride()
+    B, L, D = shape
+    b, l, one = stride
     if D > 1 and one != 1:
         raise RuntimeError(f"{what}: libslim needs rows whose channels are contiguous")
     if L > 1:
@@ -985,16 +1015,20 @@ def _pitch(t, what):
     return pitch
 
 
-def _scan_dims(gate, x, kind, what):
-    if gate.dim() != 3 or gate.shape != x.shape:
+@functools.lru_cache(maxsize=1024)
+def _scan_sizes(gate, x, gate_stride, x_stride, gate_dtype, dtype, kind, what):
+    """(B, L, D, dtype code, kind code) of checked shapes, and both inputs' pitches."""
+    if len(gate) != 3 or gate != x:
         raise ValueError("gate and x must be [B, L, D]")
-    if gate.dtype != x.dtype:
-        raise TypeError(f"{what}: one dtype expected, got {gate.dtype} and {x.dtype}")
+    if gate_dtype != dtype:
+        raise TypeError(f"{what}: one dtype expected, got {gate_dtype} and {dtype}")
+    if dtype not in DTYPES:
+        raise TypeError(f"{what}: float32 or bfloat16 expected, got {dtype}")
     _require(kind in GATES, f"kind must be one of {', '.join(GATES)}")
-    B, L, D = gate.shape
+    B, L, D = gate
     if (B | L | D) >> 31:
         _too_large()
-    return B, L, D, _dtype_code(gate, what), GATES[kind]
+    return (B, L, D, DTYPES[dtype], GATES[kind]), _pitch(gate, gate_stride, "gate"), _pitch(x, x_stride, "x")
 
 
 @functools.lru_cache(maxsize=1024)
@@ -1005,14 +1039,17 @@ def gated_scan_workspace_size(B, L, D, dtype):
     return n.value
 
 
-def _scan_workspace(given, need, device):
+def _scan_workspace(given, sizes, t):
     """(tensor or None, pointer, bytes): short sequences need none."""
     if given is None:
-        given = _workspace(need, device) if need else None
+        need = gated_scan_workspace_size(*sizes[:3], t.dtype)
+        if not need:
+            return None, None, 0
+        given = _workspace(need, t.device)
     else:
-        _one_device(given)
+        _device_of(t, given)
         _require_cuda(given)
-    return given, _ptr(given), 0 if given is None else given.numel()
+    return given, given.data_ptr(), given.numel()
 
 
 def gated_scan_forward(gate, x, kind="sigmoid", h0=None, keep=False, last=None, workspace=None, stream=None):
@@ -1022,22 +1059,24 @@ def gated_scan_forward(gate, x, kind="sigmoid", h0=None, keep=False, last=None, 
     (1 - a) x.  h0: the state to start from, [B, D] fp32 or None (zero).  Returns
     (h, last): all states in x's dtype and the last in fp32 (into `last` if given,
     which may be h0); with keep=True also what gated_scan_backward needs."""
-    B, L, D, dt, code = _scan_dims(gate, x, kind, "gated_scan_forward")
-    _one_device(gate, x, h0, last)
+    sizes, gp, xp = _scan_sizes(gate.shape, x.shape, gate.stride(), x.stride(), gate.dtype, x.dtype, kind,
+                                "gated_scan_forward")
+    B, L, D, _, _ = sizes
+    dev = _device_of(x, gate, h0, last)
     h0p = _fp32_or_none(h0, (B, D), "h0")
-    _fp32_or_none(last, (B, D), "last")
-    with _on_device(x):
-        with _on(stream):
-            h = torch.empty(B, L, D, dtype=x.dtype, device=x.device)
-            if last is None:
-                last = torch.empty(B, D, dtype=torch.float32, device=x.device)
-            kept = (torch.empty(B, -(-L // SCAN_CHUNK), D, dtype=torch.float32, device=x.device)
-                    if keep else None)
-            ws, wsp, nbytes = _scan_workspace(workspace, gated_scan_workspace_size(B, L, D, x.dtype), x.device)
-        _check(library().slim_gated_scan_fwd(gate.data_ptr(), _pitch(gate, "gate"), x.data_ptr(),
-                                             _pitch(x, "x"), h0p, B, L, D, dt, code, h.data_ptr(),
-                                             last.data_ptr(), _ptr(kept), wsp, nbytes,
-                                             _stream_of(x, stream)), "slim_gated_scan_fwd")
+    lastp = _fp32_or_none(last, (B, D), "last")
+    kept = None
+    with _at(dev, stream):
+        h = x.new_empty(x.shape)
+        if last is None:
+            last = x.new_empty((B, D), dtype=torch.float32)
+            lastp = last.data_ptr()
+        if keep:
+            kept = x.new_empty((B, -(-L // SCAN_CHUNK), D), dtype=torch.float32)
+        ws, wsp, nbytes = _scan_workspace(workspace, sizes, x)
+        status = library().slim_gated_scan_fwd(gate.data_ptr(), gp, x.data_ptr(), xp, h0p, *sizes, h.data_ptr(),
+                                               lastp, _ptr(kept), wsp, nbytes, _raw(dev, stream))
+    _check(status, "slim_gated_scan_fwd")
     return (h, last, kept) if keep else (h, last)
 
 
@@ -1047,39 +1086,41 @@ def gated_scan_backward(gate, x, kept, dh, kind="sigmoid", dlast=None, dgate=Non
     <dlast, last>.  kept: from gated_scan_forward(..., keep=True) on the same inputs;
     dlast: [B, D] fp32 or None (zero).  dgate and dx are contiguous unless given
     (slices of the projection's gradient); dh0 may be given, too, also as dlast."""
-    B, L, D, dt, code = _scan_dims(gate, x, kind, "gated_scan_backward")
-    _one_device(gate, x, kept, dh, dlast, dgate, dx, dh0)
-    if tuple(dh.shape) != (B, L, D) or dh.dtype != x.dtype or not dh.is_contiguous():
+    sizes, gp, xp = _scan_sizes(gate.shape, x.shape, gate.stride(), x.stride(), gate.dtype, x.dtype, kind,
+                                "gated_scan_backward")
+    B, L, D, _, _ = sizes
+    if kept is None:
+        raise ValueError("kept must be the forward's")
+    dev = _device_of(x, gate, kept, dh, dlast, dgate, dx, dh0)
+    if dh.shape != x.shape or dh.dtype != x.dtype or not dh.is_contiguous():
         raise ValueError("dh must be contiguous [B, L, D] in x's dtype")
     dlp = _fp32_or_none(dlast, (B, D), "dlast")
     _fp32_or_none(dh0, (B, D), "dh0")
-    if kept is None:
-        raise ValueError("kept must be the forward's")
-    _fp32_or_none(kept, (B, -(-L // SCAN_CHUNK), D), "kept")
+    keptp = _fp32_or_none(kept, (B, -(-L // SCAN_CHUNK), D), "kept")
     for t in (dgate, dx):
-        if t is not None and (tuple(t.shape) != (B, L, D) or t.dtype != x.dtype):
+        if t is not None and (t.shape != x.shape or t.dtype != x.dtype):
             raise ValueError("dgate and dx must be [B, L, D] in x's dtype")
-    with _on_device(x):
-        with _on(stream):
-            if dgate is None:
-                dgate = torch.empty(B, L, D, dtype=x.dtype, device=x.device)
-            if dx is None:
-                dx = torch.empty(B, L, D, dtype=x.dtype, device=x.device)
-            if dh0 is None:
-                dh0 = torch.empty(B, D, dtype=torch.float32, device=x.device)
-            ws, wsp, nbytes = _scan_workspace(workspace, gated_scan_workspace_size(B, L, D, x.dtype), x.device)
-        _check(library().slim_gated_scan_bwd(gate.data_ptr(), _pitch(gate, "gate"), x.data_ptr(),
-                                             _pitch(x, "x"), kept.data_ptr(), dh.data_ptr(), dlp, B,
-                                             L, D, dt, code, dgate.data_ptr(), _pitch(dgate, "dgate"),
-                                             dx.data_ptr(), _pitch(dx, "dx"), dh0.data_ptr(), wsp,
-                                             nbytes, _stream_of(x, stream)), "slim_gated_scan_bwd")
+    dgp = D if dgate is None else _pitch(dgate.shape, dgate.stride(), "dgate")
+    dxp = D if dx is None else _pitch(dx.shape, dx.stride(), "dx")
+    with _at(dev, stream):
+        if dgate is None:
+            dgate = x.new_empty(x.shape)
+        if dx is None:
+            dx = x.new_empty(x.shape)
+        if dh0 is None:
+            dh0 = x.new_empty((B, D), dtype=torch.float32)
+        ws, wsp, nbytes = _scan_workspace(workspace, sizes, x)
+        status = library().slim_gated_scan_bwd(gate.data_ptr(), gp, x.data_ptr(), xp, keptp, dh.data_ptr(), dlp,
+                                               *sizes, dgate.data_ptr(), dgp, dx.data_ptr(), dxp, dh0.data_ptr(),
+                                               wsp, nbytes, _raw(dev, stream))
+    _check(status, "slim_gated_scan_bwd")
     return dgate, dx, dh0
 
 
 def _even_rows(t):
     """t with contiguous channels and its rows at one distance: itself, or a copy."""
     try:
-        return t if _pitch(t, "") >= 0 else t.contiguous()
+        return t if _pitch(t.shape, t.stride(), "") >= 0 else t.contiguous()
     except RuntimeError:
         return t.contiguous()
 
@@ -1123,18 +1164,30 @@ def gated_ff_workspace_size(N, D, F, dtype, backward):
     return n.value
 
 
-def _ff_dims(x, w, act, what):
-    _one_device(x, w)
-    _require_cuda(x, w)
-    if w.dtype != x.dtype:
-        raise TypeError(f"{what}: one dtype expected, got {x.dtype} and {w.dtype}")
-    if w.dim() != 2 or w.shape[0] % 2 or x.dim() < 1 or x.shape[-1] != w.shape[1]:
+@functools.lru_cache(maxsize=1024)
+def _ff_sizes(x, w, dtype, w_dtype, act, what):
+    """(N, D, F, dtype code, act code) of checked shapes."""
+    if w_dtype != dtype:
+        raise TypeError(f"{what}: one dtype expected, got {dtype} and {w_dtype}")
+    if dtype not in DTYPES:
+        raise TypeError(f"{what}: float32 or bfloat16 expected, got {dtype}")
+    if len(w) != 2 or w[0] % 2 or len(x) < 1 or x[-1] != w[1]:
         raise ValueError("x must be [..., D] and w [2F, D]")
     _require(act in ACTIVATIONS, f"act must be one of {', '.join(ACTIVATIONS)}")
-    F, D = w.shape[0] // 2, w.shape[1]
+    F, D = w[0] // 2, w[1]
     if (D | F) >> 31:
         _too_large()
-    return x.numel() // max(D, 1), D, F, _dtype_code(x, what), ACTIVATIONS[act]
+    return math.prod(x[:-1]), D, F, DTYPES[dtype], ACTIVATIONS[act]
+
+
+def _ff_workspace(given, sizes, t, backward):
+    """(tensor or None, pointer, bytes): a few rows need none."""
+    if given is None:
+        need = gated_ff_workspace_size(*sizes[:3], t.dtype, backward)
+        if not need:
+            return None, None, 0
+        given = _workspace(need, t.device)
+    return given, given.data_ptr(), given.numel()
 
 
 def gated_ff_forward(x, w, act="silu", keep=False, out=None, workspace=None, stream=None):
@@ -1142,43 +1195,40 @@ def gated_ff_forward(x, w, act="silu", keep=False, out=None, workspace=None, str
     first F rows the gate's and the others up's; act one of "silu", "gelu",
     "gelu_tanh", "relu", "sigmoid".  With keep=True returns (h, z), z being what
     gated_ff_backward can reuse, or None where computing it again is the faster."""
-    N, D, F, dt, code = _ff_dims(x, w, act, "gated_ff_forward")
-    shape = (*x.shape[:-1], F)
+    dev = _device_of(x, w, out)
+    _require_cuda(x, w)
+    sizes = _ff_sizes(x.shape, w.shape, x.dtype, w.dtype, act, "gated_ff_forward")
+    shape = (*x.shape[:-1], sizes[2])
     if out is not None:
-        _one_device(x, out)
         _require_cuda(out)
-        _require(out.dtype == x.dtype and tuple(out.shape) == shape, "out must be [..., F] in x's dtype")
+        _require(out.dtype == x.dtype and out.shape == shape, "out must be [..., F] in x's dtype")
     if workspace is not None:
         _require_cuda(workspace)
-    with _on_device(x):
-        with _on(stream):
-            h = out if out is not None else torch.empty(shape, dtype=x.dtype, device=x.device)
-            ws = workspace if workspace is not None else _workspace(
-                gated_ff_workspace_size(N, D, F, x.dtype, False), x.device)
-        _check(library().slim_gated_ff_fwd(x.data_ptr(), w.data_ptr(), N, D, F, dt, code, h.data_ptr(),
-                                           ws.data_ptr(), ws.numel(), _stream_of(x, stream)),
-               "slim_gated_ff_fwd")
+    with _at(dev, stream):
+        h = out if out is not None else x.new_empty(shape)
+        ws, wsp, nbytes = _ff_workspace(workspace, sizes, x, False)
+        status = library().slim_gated_ff_fwd(x.data_ptr(), w.data_ptr(), *sizes, h.data_ptr(), wsp, nbytes,
+                                             _raw(dev, stream))
+    _check(status, "slim_gated_ff_fwd")
     return (h, None) if keep else h
 
 
 def gated_ff_backward(x, w, dh, act="silu", z=None, workspace=None, stream=None):
     """slim_gated_ff_bwd: returns (dx, dw), the gradients of <dh, h>.  z: from
     gated_ff_forward(..., keep=True) on the same inputs, or None."""
-    N, D, F, dt, code = _ff_dims(x, w, act, "gated_ff_backward")
-    _one_device(x, dh)
-    _require_cuda(dh)
-    if tuple(dh.shape) != (*x.shape[:-1], F) or dh.dtype != x.dtype:
+    dev = _device_of(x, w, dh)
+    _require_cuda(x, w, dh)
+    sizes = _ff_sizes(x.shape, w.shape, x.dtype, w.dtype, act, "gated_ff_backward")
+    if dh.shape != (*x.shape[:-1], sizes[2]) or dh.dtype != x.dtype:
         raise ValueError("dh must be [..., F] in x's dtype")
     if workspace is not None:
         _require_cuda(workspace)
-    with _on_device(x):
-        with _on(stream):
-            dx, dw = torch.empty_like(x), torch.empty_like(w)
-            ws = workspace if workspace is not None else _workspace(
-                gated_ff_workspace_size(N, D, F, x.dtype, True), x.device)
-        _check(library().slim_gated_ff_bwd(x.data_ptr(), w.data_ptr(), dh.data_ptr(), N, D, F, dt, code,
-                                           dx.data_ptr(), dw.data_ptr(), ws.data_ptr(), ws.numel(),
-                                           _stream_of(x, stream)), "slim_gated_ff_bwd")
+    with _at(dev, stream):
+        dx, dw = x.new_empty(x.shape), w.new_empty(w.shape)
+        ws, wsp, nbytes = _ff_workspace(workspace, sizes, x, True)
+        status = library().slim_gated_ff_bwd(x.data_ptr(), w.data_ptr(), dh.data_ptr(), *sizes, dx.data_ptr(),
+                                             dw.data_ptr(), wsp, nbytes, _raw(dev, stream))
+    _check(status, "slim_gated_ff_bwd")
     return dx, dw
 
 
