@@ -868,7 +868,6 @@ class _QkCall:
         if not (isinstance(inv_freq, array.array) and inv_freq.typecode == "d"):
             inv_freq = array.array("d", map(float, inv_freq))
         rotary = 2 * len(inv_freq)
-        self.q, self.k = q, k
         self.sizes = _qk_sizes(q.shape, None if k is None else k.shape,
                                None if positions is None else positions.shape, rotary, q.dtype,
                                None if k is None else k.dtype, what)
@@ -896,7 +895,7 @@ class _QkCall:
     def like(self, t, given, what):
         """`given`, checked, or a new contiguous tensor of t's shape (None: without t)."""
         if given is None:
-            return None if t is None else t.new_empty(t.shape)
+            return None if t is None else torch.empty(t.shape, dtype=t.dtype, device=t.device)
         if t is None or given.dtype != t.dtype or given.shape != t.shape:
             raise ValueError(f"{what} must have the shape and dtype of its input")
         _device_of(t, given)
@@ -951,7 +950,7 @@ def qk_norm_backward(q, k, q_weight, k_weight, dq_out, dk_out, positions=None, i
     with _at(c.dev, stream):
         dq = c.like(q, dq, "dq")
         dk = c.like(k, dk, "dk")
-        dwq, dwk = (w.new_empty(w.shape) if weights and w is not None else None for w in (q_weight, k_weight))
+        dwq, dwk = (torch.empty(w.shape, dtype=w.dtype, device=w.device) if weights and w is not None else None for w in (q_weight, k_weight))
         ws = workspace if workspace is not None else _workspace(qk_norm_workspace_size(*c.sizes[:5]), q.device)
         status = library().slim_qk_norm_bwd(*c.head, int(interleaved), *c.sizes, eps, scale, *c.rows(dq_out),
                                             *c.rows(dk_out), *c.rows(dq), *c.rows(dk), _ptr(dwq), _ptr(dwk),
@@ -1067,12 +1066,12 @@ def gated_scan_forward(gate, x, kind="sigmoid", h0=None, keep=False, last=None, 
     lastp = _fp32_or_none(last, (B, D), "last")
     kept = None
     with _at(dev, stream):
-        h = x.new_empty(x.shape)
+        h = torch.empty(x.shape, dtype=x.dtype, device=x.device)
         if last is None:
-            last = x.new_empty((B, D), dtype=torch.float32)
+            last = torch.empty((B, D), dtype=torch.float32, device=x.device)
             lastp = last.data_ptr()
         if keep:
-            kept = x.new_empty((B, -(-L // SCAN_CHUNK), D), dtype=torch.float32)
+            kept = torch.empty((B, -(-L // SCAN_CHUNK), D), dtype=torch.float32, device=x.device)
         ws, wsp, nbytes = _scan_workspace(workspace, sizes, x)
         status = library().slim_gated_scan_fwd(gate.data_ptr(), gp, x.data_ptr(), xp, h0p, *sizes, h.data_ptr(),
                                                lastp, _ptr(kept), wsp, nbytes, _raw(dev, stream))
@@ -1104,11 +1103,11 @@ def gated_scan_backward(gate, x, kept, dh, kind="sigmoid", dlast=None, dgate=Non
     dxp = D if dx is None else _pitch(dx.shape, dx.stride(), "dx")
     with _at(dev, stream):
         if dgate is None:
-            dgate = x.new_empty(x.shape)
+            dgate = torch.empty(x.shape, dtype=x.dtype, device=x.device)
         if dx is None:
-            dx = x.new_empty(x.shape)
+            dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
         if dh0 is None:
-            dh0 = x.new_empty((B, D), dtype=torch.float32)
+            dh0 = torch.empty((B, D), dtype=torch.float32, device=x.device)
         ws, wsp, nbytes = _scan_workspace(workspace, sizes, x)
         status = library().slim_gated_scan_bwd(gate.data_ptr(), gp, x.data_ptr(), xp, keptp, dh.data_ptr(), dlp,
                                                *sizes, dgate.data_ptr(), dgp, dx.data_ptr(), dxp, dh0.data_ptr(),
@@ -1205,7 +1204,7 @@ def gated_ff_forward(x, w, act="silu", keep=False, out=None, workspace=None, str
     if workspace is not None:
         _require_cuda(workspace)
     with _at(dev, stream):
-        h = out if out is not None else x.new_empty(shape)
+        h = out if out is not None else torch.empty(shape, dtype=x.dtype, device=x.device)
         ws, wsp, nbytes = _ff_workspace(workspace, sizes, x, False)
         status = library().slim_gated_ff_fwd(x.data_ptr(), w.data_ptr(), *sizes, h.data_ptr(), wsp, nbytes,
                                              _raw(dev, stream))
@@ -1224,7 +1223,7 @@ def gated_ff_backward(x, w, dh, act="silu", z=None, workspace=None, stream=None)
     if workspace is not None:
         _require_cuda(workspace)
     with _at(dev, stream):
-        dx, dw = x.new_empty(x.shape), w.new_empty(w.shape)
+        dx, dw = torch.empty(x.shape, dtype=x.dtype, device=x.device), torch.empty(w.shape, dtype=w.dtype, device=w.device)
         ws, wsp, nbytes = _ff_workspace(workspace, sizes, x, True)
         status = library().slim_gated_ff_bwd(x.data_ptr(), w.data_ptr(), dh.data_ptr(), *sizes, dx.data_ptr(),
                                              dw.data_ptr(), wsp, nbytes, _raw(dev, stream))
