@@ -118,16 +118,35 @@ struct FfBwdEpi {
   const FfJob& j;
   int row = 0, col = 0;
   bool in = false;
+  // bf16: dh is on its way before the tile's products are done (16 registers)
+  static constexpr bool AHEAD = NP == 1;
+  uint4 ahead[AHEAD ? 4 : 1];
   __device__ explicit FfBwdEpi(const FfJob& job) : j(job) {}
   __device__ void begin(const Work& w, int r, int c) {
     row = r;
     col = c;
     in = r < w.p->M;
+    if (AHEAD && in && j.wide) {
+      const T* from = static_cast<const T*>(j.dh) + (size_t)r * j.F + c;
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        ahead[i] = c + 8 * i < j.F ? *reinterpret_cast<const uint4*>(from + 8 * i) : make_uint4(0, 0, 0, 0);
+    }
   }
   __device__ __forceinline__ void pair(int c, float* g, float* u) {
     if (!in) return;
     float dh[16];
-    load16(static_cast<const T*>(j.dh) + (size_t)row * j.F, col + c, j.F, j.wide, dh);
+    if (AHEAD && j.wide) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const uint4 a = c ? ahead[AHEAD ? 2 + i : 0] : ahead[AHEAD ? i : 0];
+        const uint32_t v[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) tc::unpack_bf16(v[e], dh[8 * i + 2 * e], dh[8 * i + 2 * e + 1]);
+      }
+    } else {
+      load16(static_cast<const T*>(j.dh) + (size_t)row * j.F, col + c, j.F, j.wide, dh);
+    }
     layer::with_act(j.act, [&](auto act) {
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
@@ -156,9 +175,9 @@ struct FfBwdEpi {
   }
 };
 
-template <int NP, bool HOLD, bool BWD>
+template <int NP, bool HOLD, bool BWD, int COLS>
 __global__ void __launch_bounds__(kGemmThreads, 1) k_ff(const __grid_constant__ FfJob job) {
-  using T = Tile<NP, (NP > 1), HOLD, true>;
+  using T = Tile<NP, (NP > 1), HOLD, true, COLS>;
   __shared__ GemmShared sh;
   if (job.first) {
     if (blockIdx.x == 0 && threadIdx.x < 8) job.err[threadIdx.x] = 0;
@@ -235,14 +254,24 @@ int row_steps(const FfSizes& z, const void* p) {
   return bytes % 32 || (reinterpret_cast<uintptr_t>(p) & 31) ? 1 : 2;
 }
 
+template <int NP, bool HOLD, bool BWD, int COLS>
+bool ff_launch(long long wk, bool staged, cudaStream_t s, const FfJob& j) {
+  using T = Tile<NP, (NP > 1), HOLD, true, COLS>;
+  return launch<T>(k_ff<NP, HOLD, BWD, COLS>, (unsigned)wk * kPair, staged, s, j,
+                   once<T, std::integral_constant<bool, BWD>>());
+}
+
 template <int NP, bool BWD>
 slim_status ff_tiles(const FfSizes& z, FfJob& j, const Planes& x, const Planes& w, const FfWs& ws,
                      bool staged, unsigned* rep, cudaStream_t s) {
-  // B's box covers both matrices; the second begins w_half rows on
   const int columns = BWD ? z.half() : z.F;
-  if (!make_product<NP>(&j.p, x, false, w, false, z.N, columns, z.D)) return SLIM_ERR_CUDA;
-  using Ring = Tile<NP, (NP > 1), false, true>;
-  j.p.tn = cdiv(columns, Ring::BROWS);
+  // Few tiles: of half the columns, for twice the SMs (1021 x 200 x 533 fp32, 20 tiles of
+  // 128 features for 76 pairs of blocks).
+  const bool narrow = 2LL * cdiv(z.N, kTM * kPair) * cdiv(columns, kTN / kPair) <= workers();
+  const int tile_n = narrow ? kTN / 2 : kTN;
+  // B's box covers both matrices; the second begins w_half rows on
+  if (!make_product<NP>(&j.p, x, false, w, false, z.N, columns, z.D, tile_n)) return SLIM_ERR_CUDA;
+  j.p.tn = cdiv(columns, tile_n / kPair);
   j.p.up = z.w_half(BWD);
   j.F = z.F;
   j.half = z.half();
@@ -255,14 +284,12 @@ slim_status ff_tiles(const FfSizes& z, FfJob& j, const Planes& x, const Planes& 
   prof::Scope ps(BWD ? prof::K_FF_DZ : prof::K_FF, s, 4.0 * n * z.D * f,
                  (n + 2 * f) * z.D * 2 * NP + n * f * (z.es() + (BWD ? 4.0 * NP : 0.0)));
   bool ok;
-  if (NP == 1 && hold_rows(j.p)) {
-    using Hold = Tile<1, false, true, true>;
-    ok = launch<Hold>(k_ff<1, true, BWD>, (unsigned)wk * kPair, staged, s, j,
-                      once<Hold, std::integral_constant<bool, BWD>>());
-  } else {
-    ok = launch<Ring>(k_ff<NP, false, BWD>, (unsigned)wk * kPair, staged, s, j,
-                      once<Ring, std::integral_constant<bool, BWD>>());
-  }
+  if (narrow)
+    ok = ff_launch<NP, false, BWD, kTN / 2>(wk, staged, s, j);
+  else if (NP == 1 && hold_rows(j.p))
+    ok = ff_launch<1, true, BWD, kTN>(wk, staged, s, j);
+  else
+    ok = ff_launch<NP, false, BWD, kTN>(wk, staged, s, j);
   return ok ? SLIM_OK : SLIM_ERR_CUDA;
 }
 

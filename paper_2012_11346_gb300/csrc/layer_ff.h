@@ -7,16 +7,25 @@
 
 #include "../../include/slim_layer.h"
 #include "common.cuh"
+#include "tc_common.cuh"
 
 namespace slim {
 namespace layer {
 
-// sigmoid(y) and 1 - sigmoid(y), each to its own digits.  FAST: within some units
-// of 2^-22 of either, for results that are rounded to bf16.
-template <bool FAST>
+// sigmoid(y), and with REST 1 - sigmoid(y), each to its own digits.  FAST: within some
+// units of 2^-22 of either, for results that are rounded to bf16.
+template <bool FAST, bool REST>
 __device__ __forceinline__ void sigmoids(float y, float& s, float& rest) {
-  const float e = FAST ? __expf(-fabsf(y)) : expf(-fabsf(y));
-  const float big = FAST ? __fdividef(1.0f, 1.0f + e) : 1.0f / (1.0f + e), small = e * big;
+  if (FAST) {
+    // from -88 on e^-y is infinite, and s = 0 right; rest takes it as the largest number
+    float e = tc::ex2_approx(-1.44269504f * y);
+    if (REST) e = fminf(e, 3.0e38f);
+    s = __fdividef(1.0f, 1.0f + e);
+    if (REST) rest = e > 1e37f ? 1.0f : e * s;
+    if (y != y) s = rest = y;
+    return;
+  }
+  const float e = expf(-fabsf(y)), big = 1.0f / (1.0f + e), small = e * big;
   s = y >= 0.0f ? big : small;
   rest = y >= 0.0f ? small : big;
   if (y != y) s = rest = y;
@@ -42,7 +51,7 @@ __device__ __forceinline__ void activate(float g, float& a, float& da) {
       y = k * t * fmaf(m * t, t, 1.0f);
     }
     float s, rest;
-    sigmoids<FAST>(y, s, rest);
+    sigmoids<FAST, GRAD>(y, s, rest);
     a = ACT == SLIM_ACT_SIGMOID ? s : g * s;
     if (GRAD) {
       if (ACT == SLIM_ACT_SIGMOID)

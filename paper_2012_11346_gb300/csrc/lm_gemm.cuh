@@ -30,8 +30,7 @@ constexpr int kPair = 2;           // blocks of a tile
 constexpr int kTM = 128;           // rows of a block's half of a tile
 constexpr int kTN = 256;           // columns of a tile
 constexpr int kTK = 64;            // reduction per stage
-constexpr int kEpiWarps = 16;      // four per quarter of the rows, 64 columns each
-constexpr int kEpiCols = kTN / 4;
+constexpr int kEpiWarps = 16;      // four per quarter of the rows
 constexpr int kGemmThreads = 128 + 32 * kEpiWarps;  // warps: TMA, MMA, TMEM, spare, epilogue
 
 constexpr int kSmemBytes = 227 * 1024 - 1024 - 512;  // after alignment and barriers
@@ -42,12 +41,13 @@ constexpr int kHeld = 8;
 // GATED: B is two matrices of as many rows, one behind the other (`up` rows on);
 // a tile's columns are 128 of the one, from the pair's first block, and the same
 // 128 of the other, from its second.  The epilogue gets both together.
-template <int NP, bool JOIN = (NP > 1), bool HOLD_A = false, bool GATED_B = false>
+template <int NP, bool JOIN = (NP > 1), bool HOLD_A = false, bool GATED_B = false, int COLS = kTN>
 struct Tile {
+  static constexpr int TN = COLS, EPI = TN / 4;  // columns, and those of an epilogue warp
   static constexpr int PLANES = NP;
   static constexpr bool ACC = JOIN, HOLD = HOLD_A, GATED = GATED_B;
   static_assert(!HOLD || NP == 1, "one plane");
-  static constexpr int BROWS = kTN / kPair;    // rows of B that a block holds
+  static constexpr int BROWS = TN / kPair;    // rows of B that a block holds
   static constexpr int A_BYTES = kTM * kTK * 2, B_BYTES = BROWS * kTK * 2;
   static constexpr int HELD_BYTES = HOLD ? kHeld * A_BYTES : 0;
   static constexpr int STAGE = HOLD ? B_BYTES : A_BYTES + B_BYTES;  // one plane of either operand
@@ -270,7 +270,7 @@ __device__ bool gemm_copy(GemmShared& sh, uint8_t* stages, Next next, int* err) 
     const CUtensorMap* map_a = uniform(&w.p->a);
     const CUtensorMap* map_b = uniform(&w.p->b);
     const int a_mn = uniform(w.p->a_mn), b_mn = uniform(w.p->b_mn);
-    const int row = uniform((w.m * kPair + rank) * kTM), col = uniform(T::GATED ? w.n * T::BROWS + rank * w.p->up : w.n * kTN + rank * T::BROWS);
+    const int row = uniform((w.m * kPair + rank) * kTM), col = uniform(T::GATED ? w.n * T::BROWS + rank * w.p->up : w.n * T::TN + rank * T::BROWS);
     const int k0 = uniform(w.k0) * kTK, k1 = uniform(w.k1) * kTK;
     if (T::HOLD && row != held_row) {
       if (held_row >= 0) {
@@ -349,7 +349,7 @@ __device__ bool gemm_multiply(GemmShared& sh, uint8_t* stages, Next next, int* e
   while (next(w)) {
     const int a_mn = uniform(w.p->a_mn), b_mn = uniform(w.p->b_mn);
     const int first = uniform(w.k0), last = uniform(w.k1);
-    const uint32_t idesc = tc::idesc_bf16(kTM * kPair, kTN, a_mn, b_mn);
+    const uint32_t idesc = tc::idesc_bf16(kTM * kPair, T::TN, a_mn, b_mn);
     const uint32_t a_step = a_mn ? 128 : 2, b_step = b_mn ? 128 : 2;
     const uint32_t ring = tc::smem_u32(stages) + T::HELD_BYTES;
     const uint64_t a0 = tc::sdesc(tc::smem_u32(stages), a_mn ? 8192 : 16, 1024);
@@ -427,13 +427,13 @@ __device__ bool gemm_finish(GemmShared& sh, Next next, Epi& epi, int* err) {
   while (next(w)) {
     const Product* p = w.p;
     const int row = (w.m * kPair + (int)rank) * kTM + quarter * 32 + lane;
-    constexpr int kCols = T::GATED ? kEpiCols / 2 : kEpiCols;
-    const int col = (T::GATED ? w.n * T::BROWS : w.n * kTN) + part * kCols;
+    constexpr int kCols = T::GATED ? T::EPI / 2 : T::EPI;
+    const int col = (T::GATED ? w.n * T::BROWS : w.n * T::TN) + part * kCols;
     const int step = T::ACC ? T::CHAIN : w.k1 - w.k0;
-    float sum[T::ACC ? kEpiCols : 1];
+    float sum[T::ACC ? T::EPI : 1];
     if (T::ACC) {
 #pragma unroll
-      for (int c = 0; c < kEpiCols; ++c) sum[c] = 0.0f;
+      for (int c = 0; c < T::EPI; ++c) sum[c] = 0.0f;
     }
     epi.begin(w, row, col);
     for (int k0 = w.k0; k0 < w.k1; k0 += step, ++acc) {
@@ -443,7 +443,7 @@ __device__ bool gemm_finish(GemmShared& sh, Next next, Epi& epi, int* err) {
       const uint32_t t = sh.tmem + buf * kTN + part * kCols + ((uint32_t)(quarter * 32) << 16);
       if (T::ACC) {
 #pragma unroll
-        for (int c = 0; c < kEpiCols; c += 16) {
+        for (int c = 0; c < T::EPI; c += 16) {
           float v[16];
           tc::tmem_ld16(t + c + (T::GATED && c >= kCols ? T::BROWS - kCols : 0), v);
 #pragma unroll
@@ -454,13 +454,12 @@ __device__ bool gemm_finish(GemmShared& sh, Next next, Epi& epi, int* err) {
         for (int c = 0; c < kCols && col + c < p->N; c += 16) {
           float v[16], u[16];
           __syncwarp();
-          tc::tmem_ld16(t + c, v);
-          tc::tmem_ld16(t + c + T::BROWS, u);
+          tc::tmem_ld16x2(t + c, v, t + c + T::BROWS, u);
           epi.pair(c, v, u);
         }
       } else {
 #pragma unroll 1
-        for (int c = 0; c < kEpiCols && col + c < p->N; c += 32) {
+        for (int c = 0; c < T::EPI && col + c < p->N; c += 32) {
           float v[32];
           __syncwarp();
           tc::tmem_ld32(t + c, v);
@@ -477,7 +476,7 @@ __device__ bool gemm_finish(GemmShared& sh, Next next, Epi& epi, int* err) {
         if (col + c < p->N) epi.pair(c, &sum[c], &sum[c + kCols]);
     } else if constexpr (T::ACC) {
 #pragma unroll
-      for (int c = 0; c < kEpiCols; c += 32)
+      for (int c = 0; c < T::EPI; c += 32)
         if (col + c < p->N) epi.chunk(c, &sum[c]);
     }
   }

@@ -434,16 +434,16 @@ struct Planes {
 
 template <int NP>
 bool make_product(Product* p, const Planes& a, bool a_mn, const Planes& b, bool b_mn, long long M,
-                  long long N, long long K) {
+                  long long N, long long K, int tile_n = kTN) {
   if (!plane_map(&p->a, a.p, a.rows, a.cols, a.ld, a.plane, NP, a_mn ? kTK : kTM) ||
-      !plane_map(&p->b, b.p, b.rows, b.cols, b.ld, b.plane, NP, b_mn ? kTK : kTN / kPair))
+      !plane_map(&p->b, b.p, b.rows, b.cols, b.ld, b.plane, NP, b_mn ? kTK : tile_n / kPair))
     return false;
   p->a_mn = a_mn;
   p->b_mn = b_mn;
   p->M = (int)M;
   p->N = (int)N;
   p->tm = cdiv(M, kTM * kPair);
-  p->tn = cdiv(N, kTN);
+  p->tn = cdiv(N, tile_n);
   p->kb = cdiv(K, kTK);
   p->splits = 1;
   p->up = 0;

@@ -229,6 +229,25 @@ __device__ __forceinline__ void tmem_ld16(uint32_t taddr, float* v) {
 #pragma unroll
   for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
 }
+// 16 columns at either address, both under way before the wait.
+__device__ __forceinline__ void tmem_ld16x2(uint32_t ta, float* a, uint32_t tb, float* b) {
+  uint32_t r[32];
+#pragma unroll
+  for (int k = 0; k < 32; k += 16)
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : "=r"(r[k]), "=r"(r[k + 1]), "=r"(r[k + 2]), "=r"(r[k + 3]), "=r"(r[k + 4]), "=r"(r[k + 5]),
+          "=r"(r[k + 6]), "=r"(r[k + 7]), "=r"(r[k + 8]), "=r"(r[k + 9]), "=r"(r[k + 10]),
+          "=r"(r[k + 11]), "=r"(r[k + 12]), "=r"(r[k + 13]), "=r"(r[k + 14]), "=r"(r[k + 15])
+        : "r"(k ? tb : ta));
+  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    a[i] = __uint_as_float(r[i]);
+    b[i] = __uint_as_float(r[16 + i]);
+  }
+}
 __device__ __forceinline__ void tmem_ld1(uint32_t taddr, float& v) {
   uint32_t r;
   asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];" : "=r"(r) : "r"(taddr));
