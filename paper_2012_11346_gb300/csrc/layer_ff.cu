@@ -131,6 +131,8 @@ struct FfBwdEpi {
 #pragma unroll
       for (int i = 0; i < 4; ++i)
         ahead[i] = c + 8 * i < j.F ? *reinterpret_cast<const uint4*>(from + 8 * i) : make_uint4(0, 0, 0, 0);
+      // the next tile's, most often of the same rows
+      if (c + kTN / kPair < j.F) asm volatile("prefetch.global.L2 [%0];" ::"l"(from + kTN / kPair));
     }
   }
   __device__ __forceinline__ void pair(int c, float* g, float* u) {
