@@ -162,7 +162,10 @@ typedef enum {
  * gated feed-forward reads.
  *   x  [N, D] dtype;  w [2F, D] dtype: w_gate the first F rows, w_up the others;
  *   h  [N, F] dtype, written.  16-byte aligned.
- * Neither projection is written.  bf16 operands are multiplied exactly and summed
+ *   kept  [N, 2F] fp32, written (both projections, x w^T), or null; only where
+ *         slim_gated_ff_kept_size says more than 0 (wide fp32 rows): there the
+ *         backward reads it sooner than it computes it again.  16-byte aligned.
+ * Without kept, neither projection is written.  bf16 operands are multiplied exactly and summed
  * in fp32; fp32 operands are split into three bf16 pieces (24 bits) and multiplied
  * piece by piece, six products each, smallest first, on the tensor cores (up to 8
  * rows: fp32 FMA in either type).  h is rounded once.
@@ -175,14 +178,16 @@ typedef enum {
  */
 slim_status slim_gated_ff_workspace_size(long long N, int D, int F, slim_dtype dtype, int backward,
                                          size_t* bytes);
+slim_status slim_gated_ff_kept_size(long long N, int D, int F, slim_dtype dtype, size_t* bytes);
 slim_status slim_gated_ff_fwd(const void* x, const void* w, long long N, int D, int F,
-                              slim_dtype dtype, slim_act act, void* h, void* workspace,
-                              size_t workspace_bytes, void* stream);
+                              slim_dtype dtype, slim_act act, void* h, float* kept,
+                              void* workspace, size_t workspace_bytes, void* stream);
 
 /*
  * The gradients of <dh, h> with respect to x and w.
  *   dh  [N, F] dtype;  dx [N, D] dtype, dw [2F, D] dtype, written.  16-byte aligned.
- * With g and u the projections, computed again here,
+ *   kept  from the forward on the same x and w, or null.
+ * With g and u the projections, from kept or computed again here,
  *     dz = [dh u act'(g), dh act(g)],   dx = dz w,   dw = dz^T x.
  * dz is rounded once for the products: to bf16 for bf16 problems (2^-9 relative,
  * like the rounding of the gradients themselves), to three bf16 pieces for fp32
@@ -190,8 +195,8 @@ slim_status slim_gated_ff_fwd(const void* x, const void* w, long long N, int D, 
  * long ones are joined from parts; dx and dw are rounded once.  N = 0 zeroes dw.
  */
 slim_status slim_gated_ff_bwd(const void* x, const void* w, const void* dh, long long N, int D,
-                              int F, slim_dtype dtype, slim_act act, void* dx, void* dw,
-                              void* workspace, size_t workspace_bytes, void* stream);
+                              int F, slim_dtype dtype, slim_act act, const float* kept, void* dx,
+                              void* dw, void* workspace, size_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

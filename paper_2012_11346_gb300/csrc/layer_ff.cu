@@ -28,6 +28,8 @@ struct FfJob {
   int F, act;
   int wide;          // h's (dh's) rows in 2: 32-byte sectors, 1: 16-byte pieces, 0: elements
   void* h;           // forward
+  float* z;          // both projections [N][2 F], or null
+  int z_wide;
   const void* dh;    // backward
   __nv_bfloat16* dz; // [NP][N][2 half]
   long long plane;
@@ -100,6 +102,11 @@ struct FfFwdEpi {
   }
   __device__ __forceinline__ void pair(int c, float* g, float* u) {
     if (!in) return;
+    if (NP > 1 && j.z) {
+      float* row_z = j.z + (size_t)row * (2 * j.F);
+      store16(row_z, col + c, j.F, j.z_wide, g);
+      store16(row_z + j.F, col + c, j.F, j.z_wide, u);
+    }
     layer::with_act(j.act, [&](auto act) {
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
@@ -190,7 +197,68 @@ __global__ void __launch_bounds__(kGemmThreads, 1) k_ff(const __grid_constant__ 
   gemm_roles<T>(sh, stage_memory<T>(), run_of(job.p), epi, job.err);
 }
 
+// dz from projections that the forward kept: eight features a thread.  z and dh are
+// read, dz's three planes written: 24 bytes a feature and row, where computing the
+// projections again takes 24 D operations on the tensor cores.
+__global__ void __launch_bounds__(256) k_ff_kept(const __grid_constant__ FfJob j, long long N) {
+  tc::grid_dependency_wait();
+  if (j.first && blockIdx.x == 0) {
+    if (threadIdx.x < 8) j.err[threadIdx.x] = 0;
+    __syncthreads();
+    if (threadIdx.x == 0) tc::set_report(j.err, j.rep);
+  }
+  const int per = j.half / 8;
+  for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < N * per; i += (long long)gridDim.x * 256) {
+    const long long row = i / per;
+    const int c = (int)(i - row * per) * 8;
+    float v[3][8];  // g, u, dh
+    const float* from[3] = {j.z + row * (2 * j.F), j.z + row * (2 * j.F) + j.F,
+                            static_cast<const float*>(j.dh) + row * j.F};
+#pragma unroll
+    for (int k = 0; k < 3; ++k) {
+      if (j.wide && j.z_wide) {
+#pragma unroll
+        for (int e = 0; e < 8; e += 4) {
+          const float4 f = c + e < j.F ? *reinterpret_cast<const float4*>(from[k] + c + e) : make_float4(0, 0, 0, 0);
+          v[k][e] = f.x;
+          v[k][e + 1] = f.y;
+          v[k][e + 2] = f.z;
+          v[k][e + 3] = f.w;
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[k][e] = c + e < j.F ? from[k][c + e] : 0.0f;
+      }
+    }
+    layer::with_act(j.act, [&](auto act) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        float a, da;
+        layer::activate<decltype(act)::value, false, true>(v[0][e], a, da);
+        v[0][e] = c + e < j.F ? v[2][e] * v[1][e] * da : 0.0f;
+        v[1][e] = c + e < j.F ? v[2][e] * a : 0.0f;
+      }
+    });
+    __nv_bfloat16* to = j.dz + row * (2 * j.half) + c;
+#pragma unroll
+    for (int q = 0; q < 3; ++q)
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        uint32_t u[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) u[e] = take_plane<3>(v[k][2 * e], v[k][2 * e + 1]);
+        *reinterpret_cast<uint4*>(to + q * j.plane + k * j.half) = make_uint4(u[0], u[1], u[2], u[3]);
+      }
+  }
+}
+
 // ------------------------------------------------------------------ host
+// From D on, keeping both projections of fp32 rows is the quicker.
+constexpr int kKeepFrom = 384;
+bool keeps(long long N, int D, int, slim_dtype dtype) {
+  return dtype == SLIM_F32 && D >= kKeepFrom && N > 0 && !layer::ff_rows_fit(N, D, dtype);
+}
+
 struct FfSizes {
   long long N;
   int D, F;
@@ -306,7 +374,7 @@ slim_status ff_stage(const FfSizes& z, const void* x, const void* w, const FfWs&
 }
 
 template <int NP>
-slim_status ff_fwd(const FfSizes& z, const void* x, const void* w, slim_act act, void* h,
+slim_status ff_fwd(const FfSizes& z, const void* x, const void* w, slim_act act, void* h, float* kept,
                    const FfWs& ws, unsigned* rep, cudaStream_t s) {
   if (ws.w) {
     const slim_status st = ff_stage<NP>(z, x, w, ws, false, rep, s);
@@ -319,12 +387,14 @@ slim_status ff_fwd(const FfSizes& z, const void* x, const void* w, slim_act act,
   j.act = act;
   j.h = h;
   j.wide = row_steps(z, h);
+  j.z = kept;
+  j.z_wide = kept ? row_steps(z, kept) : 0;
   return ff_tiles<NP, false>(z, j, xm, wm, ws, ws.w != nullptr, rep, s);
 }
 
 template <int NP>
 slim_status ff_bwd(const FfSizes& z, const void* x, const void* w, const void* dh, slim_act act,
-                   void* dx, void* dw, const FfWs& ws, unsigned* rep, cudaStream_t s) {
+                   const float* kept, void* dx, void* dw, const FfWs& ws, unsigned* rep, cudaStream_t s) {
   using T = typename std::conditional<NP == 1, __nv_bfloat16, float>::type;
   if (ws.w) {
     const slim_status st = ff_stage<NP>(z, x, w, ws, true, rep, s);
@@ -340,8 +410,22 @@ slim_status ff_bwd(const FfSizes& z, const void* x, const void* w, const void* d
   j.wide = row_steps(z, dh);
   j.dz = ws.dz;
   j.plane = z.N * wide;
-  const slim_status st = ff_tiles<NP, true>(z, j, xm, wm, ws, ws.w != nullptr, rep, s);
-  if (st != SLIM_OK) return st;
+  if (kept) {
+    j.z = const_cast<float*>(kept);
+    j.z_wide = row_steps(z, kept);
+    j.F = z.F;
+    j.half = z.half();
+    j.err = ws.header;
+    j.rep = rep;
+    j.first = ws.w == nullptr;
+    const long long n = z.N * (z.half() / 8);
+    prof::Scope sd(prof::K_FF_DZ, s, 20.0 * z.N * z.F, 24.0 * z.N * z.F);
+    if (!launch_on(k_ff_kept, (unsigned)(cdiv(n, 256) < 152 * 8 ? cdiv(n, 256) : 152 * 8), 256, 0, 1, true, s, j, z.N))
+      return SLIM_ERR_CUDA;
+  } else {
+    const slim_status st = ff_tiles<NP, true>(z, j, xm, wm, ws, ws.w != nullptr, rep, s);
+    if (st != SLIM_OK) return st;
+  }
   GradJob q{};
   if (!make_product<NP>(&q.p[0], zm, true, xm, true, wide, z.D, z.N) ||
       !make_product<NP>(&q.p[1], zm, false, wm, true, z.N, z.D, wide))
@@ -402,6 +486,13 @@ extern "C" slim_status slim_gated_ff_workspace_size(long long N, int D, int F, s
   return SLIM_OK;
 }
 
+extern "C" slim_status slim_gated_ff_kept_size(long long N, int D, int F, slim_dtype dtype, size_t* bytes) {
+  using namespace slim::lm;
+  if (!bytes || !ff_sizes_ok(N, D, F, dtype, SLIM_ACT_SILU)) return SLIM_ERR_INVALID_ARG;
+  *bytes = keeps(N, D, F, dtype) ? (size_t)N * 2 * F * sizeof(float) : 0;
+  return SLIM_OK;
+}
+
 namespace {
 // The call's workspace: checked, and its earlier waits' failures reported.
 slim_status ff_begin(long long N, int D, int F, slim_dtype dtype, int backward, void* workspace,
@@ -416,10 +507,11 @@ slim_status ff_begin(long long N, int D, int F, slim_dtype dtype, int backward, 
 }  // namespace
 
 extern "C" slim_status slim_gated_ff_fwd(const void* x, const void* w, long long N, int D, int F,
-                                         slim_dtype dtype, slim_act act, void* h, void* workspace,
-                                         size_t workspace_bytes, void* stream) {
+                                         slim_dtype dtype, slim_act act, void* h, float* kept,
+                                         void* workspace, size_t workspace_bytes, void* stream) {
   using namespace slim::lm;
   if (!ff_sizes_ok(N, D, F, dtype, act) || !aligned(w, 16)) return SLIM_ERR_INVALID_ARG;
+  if (kept && (!keeps(N, D, F, dtype) || !aligned(kept, 16))) return SLIM_ERR_INVALID_ARG;
   if (N == 0) return SLIM_OK;
   if (!aligned(x, 16) || !aligned(h, 16)) return SLIM_ERR_INVALID_ARG;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
@@ -435,15 +527,17 @@ extern "C" slim_status slim_gated_ff_fwd(const void* x, const void* w, long long
   const FfSizes z{N, D, F, dtype};
   slim::Carver cv(workspace);
   const FfWs ws = ff_carve(cv, z, false);
-  return dtype == SLIM_BF16 ? ff_fwd<1>(z, x, w, act, h, ws, rep, s) : ff_fwd<3>(z, x, w, act, h, ws, rep, s);
+  return dtype == SLIM_BF16 ? ff_fwd<1>(z, x, w, act, h, kept, ws, rep, s)
+                            : ff_fwd<3>(z, x, w, act, h, kept, ws, rep, s);
 }
 
 extern "C" slim_status slim_gated_ff_bwd(const void* x, const void* w, const void* dh, long long N,
-                                         int D, int F, slim_dtype dtype, slim_act act, void* dx,
-                                         void* dw, void* workspace, size_t workspace_bytes,
+                                         int D, int F, slim_dtype dtype, slim_act act,
+                                         const float* kept, void* dx, void* dw, void* workspace, size_t workspace_bytes,
                                          void* stream) {
   using namespace slim::lm;
   if (!ff_sizes_ok(N, D, F, dtype, act) || !aligned(w, 16) || !aligned(dw, 16)) return SLIM_ERR_INVALID_ARG;
+  if (kept && (!keeps(N, D, F, dtype) || !aligned(kept, 16))) return SLIM_ERR_INVALID_ARG;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   if (N == 0) {
     const size_t n = 2 * (size_t)F * D * (dtype == SLIM_F32 ? 4 : 2);
@@ -456,6 +550,6 @@ extern "C" slim_status slim_gated_ff_bwd(const void* x, const void* w, const voi
   const FfSizes z{N, D, F, dtype};
   slim::Carver cv(workspace);
   const FfWs ws = ff_carve(cv, z, true);
-  return dtype == SLIM_BF16 ? ff_bwd<1>(z, x, w, dh, act, dx, dw, ws, rep, s)
-                            : ff_bwd<3>(z, x, w, dh, act, dx, dw, ws, rep, s);
+  return dtype == SLIM_BF16 ? ff_bwd<1>(z, x, w, dh, act, nullptr, dx, dw, ws, rep, s)
+                            : ff_bwd<3>(z, x, w, dh, act, kept, dx, dw, ws, rep, s);
 }

@@ -70,8 +70,9 @@ SIGNATURES = {
     "slim_gated_scan_bwd": ([_p, _ll, _p, _ll] + [_p] * 3 + [_i] * 5 + [_p, _ll, _p, _ll, _p, _p, _sz, _p],
                             _i),
     "slim_gated_ff_workspace_size": ([_ll, _i, _i, _i, _i, ctypes.POINTER(_sz)], _i),
-    "slim_gated_ff_fwd": ([_p, _p, _ll] + [_i] * 4 + [_p, _p, _sz, _p], _i),
-    "slim_gated_ff_bwd": ([_p, _p, _p, _ll] + [_i] * 4 + [_p, _p, _p, _sz, _p], _i),
+    "slim_gated_ff_kept_size": ([_ll, _i, _i, _i, ctypes.POINTER(_sz)], _i),
+    "slim_gated_ff_fwd": ([_p, _p, _ll] + [_i] * 4 + [_p, _p, _p, _sz, _p], _i),
+    "slim_gated_ff_bwd": ([_p, _p, _p, _ll] + [_i] * 4 + [_p] * 4 + [_sz, _p], _i),
     "slim_qk_norm_bwd": ([_p] * 7 + [_i, _p] + [_i] * 8 + [_f, _f] + [_p] * 11 + [_sz, _p], _i),
 }
 
@@ -1179,6 +1180,14 @@ def _ff_sizes(x, w, dtype, w_dtype, act, what):
     return math.prod(x[:-1]), D, F, DTYPES[dtype], ACTIVATIONS[act]
 
 
+@functools.lru_cache(maxsize=1024)
+def gated_ff_kept_size(N, D, F, dtype):
+    """Bytes of both projections where keeping them makes the backward quicker, else 0."""
+    n = _sz(0)
+    _check(library().slim_gated_ff_kept_size(N, D, F, DTYPES[dtype], ctypes.byref(n)), "slim_gated_ff_kept_size")
+    return n.value
+
+
 def _ff_workspace(given, sizes, t, backward):
     """(tensor or None, pointer, bytes): a few rows need none."""
     if given is None:
@@ -1192,8 +1201,9 @@ def _ff_workspace(given, sizes, t, backward):
 def gated_ff_forward(x, w, act="silu", keep=False, out=None, workspace=None, stream=None):
     """slim_gated_ff_fwd: act(x w_gate^T) * (x w_up^T) for x [..., D] and w [2F, D], its
     first F rows the gate's and the others up's; act one of "silu", "gelu",
-    "gelu_tanh", "relu", "sigmoid".  With keep=True returns (h, z), z being what
-    gated_ff_backward can reuse, or None where computing it again is the faster."""
+    "gelu_tanh", "relu", "sigmoid".  With keep=True returns (h, z), z being both
+    projections in fp32, [N, 2F], for gated_ff_backward, or None where computing them
+    again is the quicker (bf16, and narrow fp32 rows: see gated_ff_kept_size)."""
     dev = _device_of(x, w, out)
     _require_cuda(x, w)
     sizes = _ff_sizes(x.shape, w.shape, x.dtype, w.dtype, act, "gated_ff_forward")
@@ -1205,27 +1215,31 @@ def gated_ff_forward(x, w, act="silu", keep=False, out=None, workspace=None, str
         _require_cuda(workspace)
     with _at(dev, stream):
         h = out if out is not None else torch.empty(shape, dtype=x.dtype, device=x.device)
+        z = None
+        if keep and gated_ff_kept_size(*sizes[:3], x.dtype):
+            z = torch.empty((sizes[0], 2 * sizes[2]), dtype=torch.float32, device=x.device)
         ws, wsp, nbytes = _ff_workspace(workspace, sizes, x, False)
-        status = library().slim_gated_ff_fwd(x.data_ptr(), w.data_ptr(), *sizes, h.data_ptr(), wsp, nbytes,
-                                             _raw(dev, stream))
+        status = library().slim_gated_ff_fwd(x.data_ptr(), w.data_ptr(), *sizes, h.data_ptr(), _ptr(z), wsp,
+                                             nbytes, _raw(dev, stream))
     _check(status, "slim_gated_ff_fwd")
-    return (h, None) if keep else h
+    return (h, z) if keep else h
 
 
 def gated_ff_backward(x, w, dh, act="silu", z=None, workspace=None, stream=None):
     """slim_gated_ff_bwd: returns (dx, dw), the gradients of <dh, h>.  z: from
     gated_ff_forward(..., keep=True) on the same inputs, or None."""
-    dev = _device_of(x, w, dh)
+    dev = _device_of(x, w, dh, z)
     _require_cuda(x, w, dh)
     sizes = _ff_sizes(x.shape, w.shape, x.dtype, w.dtype, act, "gated_ff_backward")
     if dh.shape != (*x.shape[:-1], sizes[2]) or dh.dtype != x.dtype:
         raise ValueError("dh must be [..., F] in x's dtype")
+    zp = _fp32_or_none(z, (sizes[0], 2 * sizes[2]), "z")
     if workspace is not None:
         _require_cuda(workspace)
     with _at(dev, stream):
         dx, dw = torch.empty(x.shape, dtype=x.dtype, device=x.device), torch.empty(w.shape, dtype=w.dtype, device=w.device)
         ws, wsp, nbytes = _ff_workspace(workspace, sizes, x, True)
-        status = library().slim_gated_ff_bwd(x.data_ptr(), w.data_ptr(), dh.data_ptr(), *sizes, dx.data_ptr(),
+        status = library().slim_gated_ff_bwd(x.data_ptr(), w.data_ptr(), dh.data_ptr(), *sizes, zp, dx.data_ptr(),
                                              dw.data_ptr(), wsp, nbytes, _raw(dev, stream))
     _check(status, "slim_gated_ff_bwd")
     return dx, dw

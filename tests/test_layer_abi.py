@@ -262,19 +262,21 @@ def test_scan_formula_against_differences():
 
 
 # ---------------------------------------------------------------- gated feed-forward
-def ff_fwd(lib, x=FAKE, w=FAKE, N=20, D=8, F=16, dt=F32, act=0, h=FAKE, ws=FAKE, nbytes=1 << 60):
-    return lib.slim_gated_ff_fwd(x, w, N, D, F, dt, act, h, ws, nbytes, None)
+def ff_fwd(lib, x=FAKE, w=FAKE, N=20, D=8, F=16, dt=F32, act=0, h=FAKE, z=None, ws=FAKE, nbytes=1 << 60):
+    return lib.slim_gated_ff_fwd(x, w, N, D, F, dt, act, h, z, ws, nbytes, None)
 
 
-def ff_bwd(lib, x=FAKE, w=FAKE, h=FAKE, N=20, D=8, F=16, dt=F32, act=0, dx=FAKE, dw=FAKE, ws=FAKE, nbytes=1 << 60):
-    return lib.slim_gated_ff_bwd(x, w, h, N, D, F, dt, act, dx, dw, ws, nbytes, None)
+def ff_bwd(lib, x=FAKE, w=FAKE, h=FAKE, N=20, D=8, F=16, dt=F32, act=0, z=None, dx=FAKE, dw=FAKE, ws=FAKE,
+           nbytes=1 << 60):
+    return lib.slim_gated_ff_bwd(x, w, h, N, D, F, dt, act, z, dx, dw, ws, nbytes, None)
 
 
 @pytest.mark.parametrize("kw", [
     dict(N=-1), dict(N=(1 << 31) - 512), dict(D=0), dict(D=(1 << 30) + 1), dict(F=0), dict(F=(1 << 29) + 1), dict(dt=2),
     dict(act=-1), dict(act=5), dict(N=1 << 20, F=1 << 26), dict(N=1 << 20, D=(1 << 20) + 1), dict(F=1 << 20, D=1 << 20),
     dict(x=None), dict(w=None), dict(h=None), dict(x=FAKE + 8), dict(w=FAKE + 8), dict(h=FAKE + 4), dict(ws=FAKE + 16),
-    dict(N=3, ws=FAKE + 16), dict(N=3, x=FAKE + 2)])
+    dict(N=3, ws=FAKE + 16), dict(N=3, x=FAKE + 2), dict(D=512, z=FAKE + 4), dict(z=FAKE), dict(D=512, dt=BF16, z=FAKE),
+    dict(N=8, D=512, z=FAKE)])
 def test_ff_rejects(lib, kw):
     assert ff_fwd(lib, **kw) == INVALID
     assert ff_bwd(lib, **kw) == INVALID
