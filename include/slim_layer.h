@@ -162,9 +162,10 @@ typedef enum {
  * gated feed-forward reads.
  *   x  [N, D] dtype;  w [2F, D] dtype: w_gate the first F rows, w_up the others;
  *   h  [N, F] dtype, written.  16-byte aligned.
- *   kept  [N, 2F] fp32, written (both projections, x w^T), or null; only where
- *         slim_gated_ff_kept_size says more than 0 (wide fp32 rows): there the
- *         backward reads it sooner than it computes it again.  16-byte aligned.
+ *   kept  written, or null: both projections, x w^T, [N, 2 F'] fp32, F' being F
+ *         rounded up to 16 (columns past F hold anything), 32-byte aligned; only
+ *         where slim_gated_ff_kept_size says more than 0 (fp32, from 9 rows on):
+ *         there the backward reads them sooner than it computes them again.
  * Without kept, neither projection is written.  bf16 operands are multiplied exactly and summed
  * in fp32; fp32 operands are split into three bf16 pieces (24 bits) and multiplied
  * piece by piece, six products each, smallest first, on the tensor cores (up to 8

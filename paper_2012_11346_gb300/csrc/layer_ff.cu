@@ -28,8 +28,7 @@ struct FfJob {
   int F, act;
   int wide;          // h's (dh's) rows in 2: 32-byte sectors, 1: 16-byte pieces, 0: elements
   void* h;           // forward
-  float* z;          // both projections [N][2 F], or null
-  int z_wide;
+  float* z;          // both projections [N][2 half], or null
   const void* dh;    // backward
   __nv_bfloat16* dz; // [NP][N][2 half]
   long long plane;
@@ -103,9 +102,10 @@ struct FfFwdEpi {
   __device__ __forceinline__ void pair(int c, float* g, float* u) {
     if (!in) return;
     if (NP > 1 && j.z) {
-      float* row_z = j.z + (size_t)row * (2 * j.F);
-      store16(row_z, col + c, j.F, j.z_wide, g);
-      store16(row_z + j.F, col + c, j.F, j.z_wide, u);
+      // (columns past F are of no use, and are not used)
+      float* row_z = j.z + (size_t)row * (2 * j.half);
+      store16(row_z, col + c, j.half, 2, g);
+      store16(row_z + j.half, col + c, j.half, 2, u);
     }
     layer::with_act(j.act, [&](auto act) {
 #pragma unroll
@@ -212,22 +212,27 @@ __global__ void __launch_bounds__(256) k_ff_kept(const __grid_constant__ FfJob j
     const long long row = i / per;
     const int c = (int)(i - row * per) * 8;
     float v[3][8];  // g, u, dh
-    const float* from[3] = {j.z + row * (2 * j.F), j.z + row * (2 * j.F) + j.F,
-                            static_cast<const float*>(j.dh) + row * j.F};
+    const float* z = j.z + row * (2 * j.half) + c;
+    const float* dh = static_cast<const float*>(j.dh) + row * j.F + c;
 #pragma unroll
-    for (int k = 0; k < 3; ++k) {
-      if (j.wide && j.z_wide) {
-#pragma unroll
-        for (int e = 0; e < 8; e += 4) {
-          const float4 f = c + e < j.F ? *reinterpret_cast<const float4*>(from[k] + c + e) : make_float4(0, 0, 0, 0);
-          v[k][e] = f.x;
-          v[k][e + 1] = f.y;
-          v[k][e + 2] = f.z;
-          v[k][e + 3] = f.w;
-        }
+    for (int e = 0; e < 8; e += 4) {
+      const float4 g = *reinterpret_cast<const float4*>(z + e), u = *reinterpret_cast<const float4*>(z + j.half + e);
+      float4 d = make_float4(0, 0, 0, 0);
+      if (j.wide) {
+        if (c + e < j.F) d = *reinterpret_cast<const float4*>(dh + e);
       } else {
+        if (c + e < j.F) d.x = dh[e];
+        if (c + e + 1 < j.F) d.y = dh[e + 1];
+        if (c + e + 2 < j.F) d.z = dh[e + 2];
+        if (c + e + 3 < j.F) d.w = dh[e + 3];
+      }
+      const float4 all[3] = {g, u, d};
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[k][e] = c + e < j.F ? from[k][c + e] : 0.0f;
+      for (int k = 0; k < 3; ++k) {
+        v[k][e] = all[k].x;
+        v[k][e + 1] = all[k].y;
+        v[k][e + 2] = all[k].z;
+        v[k][e + 3] = all[k].w;
       }
     }
     layer::with_act(j.act, [&](auto act) {
@@ -253,10 +258,11 @@ __global__ void __launch_bounds__(256) k_ff_kept(const __grid_constant__ FfJob j
 }
 
 // ------------------------------------------------------------------ host
-// From D on, keeping both projections of fp32 rows is the quicker.
-constexpr int kKeepFrom = 384;
-bool keeps(long long N, int D, int, slim_dtype dtype) {
-  return dtype == SLIM_F32 && D >= kKeepFrom && N > 0 && !layer::ff_rows_fit(N, D, dtype);
+// Keeping both projections is the quicker for fp32 rows: 8192 x 1024 x 2048, a step of 805
+// us (1002 with them computed again), 32768 x 64 x 1024 462 (506).  bf16 would have to
+// round them to gain.
+bool keeps(long long N, int D, slim_dtype dtype) {
+  return dtype == SLIM_F32 && N > 0 && !layer::ff_rows_fit(N, D, dtype);
 }
 
 struct FfSizes {
@@ -388,7 +394,6 @@ slim_status ff_fwd(const FfSizes& z, const void* x, const void* w, slim_act act,
   j.h = h;
   j.wide = row_steps(z, h);
   j.z = kept;
-  j.z_wide = kept ? row_steps(z, kept) : 0;
   return ff_tiles<NP, false>(z, j, xm, wm, ws, ws.w != nullptr, rep, s);
 }
 
@@ -412,7 +417,6 @@ slim_status ff_bwd(const FfSizes& z, const void* x, const void* w, const void* d
   j.plane = z.N * wide;
   if (kept) {
     j.z = const_cast<float*>(kept);
-    j.z_wide = row_steps(z, kept);
     j.F = z.F;
     j.half = z.half();
     j.err = ws.header;
@@ -489,7 +493,7 @@ extern "C" slim_status slim_gated_ff_workspace_size(long long N, int D, int F, s
 extern "C" slim_status slim_gated_ff_kept_size(long long N, int D, int F, slim_dtype dtype, size_t* bytes) {
   using namespace slim::lm;
   if (!bytes || !ff_sizes_ok(N, D, F, dtype, SLIM_ACT_SILU)) return SLIM_ERR_INVALID_ARG;
-  *bytes = keeps(N, D, F, dtype) ? (size_t)N * 2 * F * sizeof(float) : 0;
+  *bytes = keeps(N, D, dtype) ? (size_t)N * 2 * FfSizes{N, D, F, dtype}.half() * sizeof(float) : 0;
   return SLIM_OK;
 }
 
@@ -511,7 +515,7 @@ extern "C" slim_status slim_gated_ff_fwd(const void* x, const void* w, long long
                                          void* workspace, size_t workspace_bytes, void* stream) {
   using namespace slim::lm;
   if (!ff_sizes_ok(N, D, F, dtype, act) || !aligned(w, 16)) return SLIM_ERR_INVALID_ARG;
-  if (kept && (!keeps(N, D, F, dtype) || !aligned(kept, 16))) return SLIM_ERR_INVALID_ARG;
+  if (kept && (!keeps(N, D, dtype) || !aligned(kept, 32))) return SLIM_ERR_INVALID_ARG;
   if (N == 0) return SLIM_OK;
   if (!aligned(x, 16) || !aligned(h, 16)) return SLIM_ERR_INVALID_ARG;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
@@ -537,7 +541,7 @@ extern "C" slim_status slim_gated_ff_bwd(const void* x, const void* w, const voi
                                          void* stream) {
   using namespace slim::lm;
   if (!ff_sizes_ok(N, D, F, dtype, act) || !aligned(w, 16) || !aligned(dw, 16)) return SLIM_ERR_INVALID_ARG;
-  if (kept && (!keeps(N, D, F, dtype) || !aligned(kept, 16))) return SLIM_ERR_INVALID_ARG;
+  if (kept && (!keeps(N, D, dtype) || !aligned(kept, 32))) return SLIM_ERR_INVALID_ARG;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   if (N == 0) {
     const size_t n = 2 * (size_t)F * D * (dtype == SLIM_F32 ? 4 : 2);

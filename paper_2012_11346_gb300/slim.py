@@ -1202,8 +1202,8 @@ def gated_ff_forward(x, w, act="silu", keep=False, out=None, workspace=None, str
     """slim_gated_ff_fwd: act(x w_gate^T) * (x w_up^T) for x [..., D] and w [2F, D], its
     first F rows the gate's and the others up's; act one of "silu", "gelu",
     "gelu_tanh", "relu", "sigmoid".  With keep=True returns (h, z), z being both
-    projections in fp32, [N, 2F], for gated_ff_backward, or None where computing them
-    again is the quicker (bf16, and narrow fp32 rows: see gated_ff_kept_size)."""
+    projections in fp32 for gated_ff_backward, or None where computing them again is
+    the quicker (bf16, and a few rows: see gated_ff_kept_size)."""
     dev = _device_of(x, w, out)
     _require_cuda(x, w)
     sizes = _ff_sizes(x.shape, w.shape, x.dtype, w.dtype, act, "gated_ff_forward")
@@ -1216,8 +1216,9 @@ def gated_ff_forward(x, w, act="silu", keep=False, out=None, workspace=None, str
     with _at(dev, stream):
         h = out if out is not None else torch.empty(shape, dtype=x.dtype, device=x.device)
         z = None
-        if keep and gated_ff_kept_size(*sizes[:3], x.dtype):
-            z = torch.empty((sizes[0], 2 * sizes[2]), dtype=torch.float32, device=x.device)
+        if keep:
+            need = gated_ff_kept_size(*sizes[:3], x.dtype)
+            z = torch.empty(need // 4, dtype=torch.float32, device=x.device) if need else None
         ws, wsp, nbytes = _ff_workspace(workspace, sizes, x, False)
         status = library().slim_gated_ff_fwd(x.data_ptr(), w.data_ptr(), *sizes, h.data_ptr(), _ptr(z), wsp,
                                              nbytes, _raw(dev, stream))
@@ -1233,7 +1234,7 @@ def gated_ff_backward(x, w, dh, act="silu", z=None, workspace=None, stream=None)
     sizes = _ff_sizes(x.shape, w.shape, x.dtype, w.dtype, act, "gated_ff_backward")
     if dh.shape != (*x.shape[:-1], sizes[2]) or dh.dtype != x.dtype:
         raise ValueError("dh must be [..., F] in x's dtype")
-    zp = _fp32_or_none(z, (sizes[0], 2 * sizes[2]), "z")
+    zp = None if z is None else _fp32_or_none(z, (gated_ff_kept_size(*sizes[:3], x.dtype) // 4,), "z")
     if workspace is not None:
         _require_cuda(workspace)
     with _at(dev, stream):
