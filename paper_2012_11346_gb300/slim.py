@@ -798,6 +798,29 @@ def _at(dev, stream):
     return torch.cuda.stream(stream)
 
 
+try:
+    # (size, stride, dtype) on the current device, without the dispatcher: half of
+    # torch.empty's time
+    from torch._C._dynamo.guards import _empty_strided_cuda as _allocate
+except ImportError:
+    def _allocate(size, stride, dtype):
+        return torch.empty_strided(size, stride, dtype=dtype, device="cuda")
+
+
+@functools.lru_cache(maxsize=1024)
+def _dense(shape):
+    stride, n = [], 1
+    for size in reversed(shape):
+        stride.append(n)
+        n *= max(size, 1)
+    return tuple(shape), tuple(reversed(stride))
+
+
+def _new(shape, dtype):
+    """A contiguous tensor on the current device, to be written."""
+    return _allocate(*_dense(shape), dtype)
+
+
 def _raw(dev, stream):
     """The raw stream of a call on device `dev`: `stream`, or the current one."""
     return torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
@@ -893,14 +916,22 @@ class _QkCall:
         self.kept.append(strides)
         return t.data_ptr(), strides.buffer_info()[0]
 
-    def like(self, t, given, what):
-        """`given`, checked, or a new contiguous tensor of t's shape (None: without t)."""
-        if given is None:
-            return None if t is None else torch.empty(t.shape, dtype=t.dtype, device=t.device)
+    def check(self, t, given, what):
+        """`given` is like t, or None where t is."""
         if t is None or given.dtype != t.dtype or given.shape != t.shape:
             raise ValueError(f"{what} must have the shape and dtype of its input")
         _device_of(t, given)
-        return given
+
+    def like(self, t, given, what):
+        """(tensor, pointer, strides): `given`, checked, or a new contiguous one like t
+        (None without t)."""
+        if given is not None:
+            self.check(t, given, what)
+            return given, *self.rows(given)
+        if t is None:
+            return None, None, None
+        out = _new(t.shape, t.dtype)
+        return out, out.data_ptr(), None
 
 
 def qk_norm_forward(q, k, q_weight=None, k_weight=None, positions=None, inv_freq=None, interleaved=False,
@@ -915,10 +946,10 @@ def qk_norm_forward(q, k, q_weight=None, k_weight=None, positions=None, inv_freq
     and k themselves."""
     c = _QkCall(q, k, q_weight, k_weight, positions, inv_freq, "qk_norm_forward")
     with _at(c.dev, stream):
-        q_out = c.like(q, q_out, "q_out")
-        k_out = c.like(k, k_out, "k_out")
-        status = library().slim_qk_norm_fwd(*c.head, int(interleaved), *c.sizes, eps, scale, *c.rows(q_out),
-                                            *c.rows(k_out), _raw(c.dev, stream))
+        q_out, qp, qs = c.like(q, q_out, "q_out")
+        k_out, kp, ks = c.like(k, k_out, "k_out")
+        status = library().slim_qk_norm_fwd(*c.head, int(interleaved), *c.sizes, eps, scale, qp, qs, kp, ks,
+                                            _raw(c.dev, stream))
     _check(status, "slim_qk_norm_fwd")
     return q_out, k_out
 
@@ -944,17 +975,19 @@ def qk_norm_backward(q, k, q_weight, k_weight, dq_out, dk_out, positions=None, i
     c = _QkCall(q, k, q_weight, k_weight, positions, inv_freq, "qk_norm_backward")
     if dq_out is None or (k is not None and dk_out is None):
         raise ValueError("dq_out and dk_out are needed")
-    c.like(q, dq_out, "dq_out")
-    c.like(k, dk_out, "dk_out")
+    c.check(q, dq_out, "dq_out")
+    if dk_out is not None:
+        c.check(k, dk_out, "dk_out")
     if workspace is not None:
         _require_cuda(workspace)
     with _at(c.dev, stream):
-        dq = c.like(q, dq, "dq")
-        dk = c.like(k, dk, "dk")
-        dwq, dwk = (torch.empty(w.shape, dtype=w.dtype, device=w.device) if weights and w is not None else None for w in (q_weight, k_weight))
-        ws = workspace if workspace is not None else _workspace(qk_norm_workspace_size(*c.sizes[:5]), q.device)
+        dq, qp, qs = c.like(q, dq, "dq")
+        dk, kp, ks = c.like(k, dk, "dk")
+        dwq, dwk = (_new(w.shape, w.dtype) if weights and w is not None else None
+                    for w in (q_weight, k_weight))
+        ws = workspace if workspace is not None else _new((qk_norm_workspace_size(*c.sizes[:5]),), torch.uint8)
         status = library().slim_qk_norm_bwd(*c.head, int(interleaved), *c.sizes, eps, scale, *c.rows(dq_out),
-                                            *c.rows(dk_out), *c.rows(dq), *c.rows(dk), _ptr(dwq), _ptr(dwk),
+                                            *c.rows(dk_out), qp, qs, kp, ks, _ptr(dwq), _ptr(dwk),
                                             ws.data_ptr(), ws.numel(), _raw(c.dev, stream))
     _check(status, "slim_qk_norm_bwd")
     return dq, dk, dwq, dwk
@@ -1045,7 +1078,7 @@ def _scan_workspace(given, sizes, t):
         need = gated_scan_workspace_size(*sizes[:3], t.dtype)
         if not need:
             return None, None, 0
-        given = _workspace(need, t.device)
+        given = _new((need,), torch.uint8)
     else:
         _device_of(t, given)
         _require_cuda(given)
@@ -1067,12 +1100,12 @@ def gated_scan_forward(gate, x, kind="sigmoid", h0=None, keep=False, last=None, 
     lastp = _fp32_or_none(last, (B, D), "last")
     kept = None
     with _at(dev, stream):
-        h = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        h = _new(x.shape, x.dtype)
         if last is None:
-            last = torch.empty((B, D), dtype=torch.float32, device=x.device)
+            last = _new((B, D), torch.float32)
             lastp = last.data_ptr()
         if keep:
-            kept = torch.empty((B, -(-L // SCAN_CHUNK), D), dtype=torch.float32, device=x.device)
+            kept = _new((B, -(-L // SCAN_CHUNK), D), torch.float32)
         ws, wsp, nbytes = _scan_workspace(workspace, sizes, x)
         status = library().slim_gated_scan_fwd(gate.data_ptr(), gp, x.data_ptr(), xp, h0p, *sizes, h.data_ptr(),
                                                lastp, _ptr(kept), wsp, nbytes, _raw(dev, stream))
@@ -1104,11 +1137,11 @@ def gated_scan_backward(gate, x, kept, dh, kind="sigmoid", dlast=None, dgate=Non
     dxp = D if dx is None else _pitch(dx.shape, dx.stride(), "dx")
     with _at(dev, stream):
         if dgate is None:
-            dgate = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+            dgate = _new(x.shape, x.dtype)
         if dx is None:
-            dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+            dx = _new(x.shape, x.dtype)
         if dh0 is None:
-            dh0 = torch.empty((B, D), dtype=torch.float32, device=x.device)
+            dh0 = _new((B, D), torch.float32)
         ws, wsp, nbytes = _scan_workspace(workspace, sizes, x)
         status = library().slim_gated_scan_bwd(gate.data_ptr(), gp, x.data_ptr(), xp, keptp, dh.data_ptr(), dlp,
                                                *sizes, dgate.data_ptr(), dgp, dx.data_ptr(), dxp, dh0.data_ptr(),
@@ -1194,7 +1227,7 @@ def _ff_workspace(given, sizes, t, backward):
         need = gated_ff_workspace_size(*sizes[:3], t.dtype, backward)
         if not need:
             return None, None, 0
-        given = _workspace(need, t.device)
+        given = _new((need,), torch.uint8)
     return given, given.data_ptr(), given.numel()
 
 
@@ -1214,11 +1247,11 @@ def gated_ff_forward(x, w, act="silu", keep=False, out=None, workspace=None, str
     if workspace is not None:
         _require_cuda(workspace)
     with _at(dev, stream):
-        h = out if out is not None else torch.empty(shape, dtype=x.dtype, device=x.device)
+        h = out if out is not None else _new(shape, x.dtype)
         z = None
         if keep:
             need = gated_ff_kept_size(*sizes[:3], x.dtype)
-            z = torch.empty(need // 4, dtype=torch.float32, device=x.device) if need else None
+            z = _new((need // 4,), torch.float32) if need else None
         ws, wsp, nbytes = _ff_workspace(workspace, sizes, x, False)
         status = library().slim_gated_ff_fwd(x.data_ptr(), w.data_ptr(), *sizes, h.data_ptr(), _ptr(z), wsp,
                                              nbytes, _raw(dev, stream))
@@ -1238,7 +1271,7 @@ def gated_ff_backward(x, w, dh, act="silu", z=None, workspace=None, stream=None)
     if workspace is not None:
         _require_cuda(workspace)
     with _at(dev, stream):
-        dx, dw = torch.empty(x.shape, dtype=x.dtype, device=x.device), torch.empty(w.shape, dtype=w.dtype, device=w.device)
+        dx, dw = _new(x.shape, x.dtype), _new(w.shape, w.dtype)
         ws, wsp, nbytes = _ff_workspace(workspace, sizes, x, True)
         status = library().slim_gated_ff_bwd(x.data_ptr(), w.data_ptr(), dh.data_ptr(), *sizes, zp, dx.data_ptr(),
                                              dw.data_ptr(), wsp, nbytes, _raw(dev, stream))
