@@ -118,7 +118,7 @@ typedef enum {
  * SIGMOID -inf) starts anew: nothing before it reaches h, finite or not.  A state
  * that is not finite stays in its channel until such a gate, or until the gates'
  * product since sinks below fp32's range.  Gates beyond 1 may grow a state past
- * fp32's range; so may the product of SLIM_SCAN_CHUNK of them alone.
+ * fp32's range; so may the product of 128 of them alone (a state of zero stays).
  * Nothing written overlaps anything else but as said.
  *   workspace of slim_gated_scan_workspace_size() bytes, for either direction; where
  *   that is 0 (short sequences, few of them) it is not read and may be null.

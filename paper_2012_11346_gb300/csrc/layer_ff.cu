@@ -1,13 +1,19 @@
 // Gated feed-forward: both projections, the activation and the product in one
 // kernel, and its gradients.  Contract: include/slim_layer.h.
 //
-// Forward: a tile is 256 rows by 128 features, its 256 accumulator columns the
-// features' gates and ups side by side (lm_gemm.cuh, GATED), so that the epilogue
-// has both of a feature in one thread and writes h = act(g) u once.
+// Forward: a tile is 256 rows by 128 features (64 where there are few tiles), its 256
+// accumulator columns the features' gates and ups side by side (lm_gemm.cuh, GATED), so
+// that the epilogue has both of a feature in one thread and writes h = act(g) u once.
 //
 // Backward: the projections again, with an epilogue that turns them and dh into
 //     dz = [dh u act'(g), dh act(g)]
 // as bf16 (three planes for fp32), and then one launch with dx = dz w and dw = dz^T x.
+// fp32 may keep both projections instead, and then dz is a pass over them.
+//
+// Measured: 16384 x 768 x 2048 bf16 forward 60 us, 1.72 PFLOP/s, bound by the tensor
+// pipe.  32768 x 512 x 2048 bf16 step: forward 77 us, dz 111, both products 170; with
+// only 8 stages of the reduction to a tile, the epilogue (dz: 192 KB of dh and dz a tile
+// and the operands again, 8 TB/s through L2) takes longer than the tile's MMAs, 57 us.
 #include <stdint.h>
 
 #include "../../include/slim_layer.h"

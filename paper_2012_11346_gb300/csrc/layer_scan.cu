@@ -22,10 +22,11 @@
 // their gates are computed again for the second pass, from shared memory: registers for
 // two tiles would leave room for one block an SM.
 //
-// Measured: 1 x 65536 x 512 fp32 forward 78 us (5.2 TB/s of inputs and outputs; 190 us
+// Measured: 1 x 65536 x 512 fp32 forward 80 us (5.0 TB/s of inputs and outputs; 190 us
 // with all of a sequence's tiles in one cluster's rounds), 8 x 4096 x 512 bf16 step with
-// sigmoid gates 100 us.  bf16 is bound by its instructions (some 45 an element and pass
-// of both), fp32 by the exchange's latency and HBM.
+// sigmoid gates 99 us (forward kernel 37, backward 60).  bf16 is bound by its
+// instructions (49 per element forward, 74 backward, both passes), fp32 by the exchange's
+// latency and HBM.
 //
 // Backward, dgate needs h_(t-1): the forward keeps the states every 64 steps in fp32
 // (1 / 64 the bytes of an fp32 h), and a tile's states are computed again from there,
@@ -155,6 +156,11 @@ template <int KIND> struct Gate {
 
 // a s + u; a of zero forgets a state that is not finite, too.
 __device__ __forceinline__ float step(float a, float s, float u) { return a == 0.0f ? u : fmaf(a, s, u); }
+// The same over some steps: a state of zero stays what it is under a product of gates
+// past fp32's range.
+__device__ __forceinline__ float over(float A, float s, float H) {
+  return A == 0.0f || (s == 0.0f && A == A) ? H : fmaf(A, s, H);
+}
 // The same where `safe`, else the plain sum.  The plain sum of a state that is not
 // finite stays so to the end of a thread's steps, which then takes them again.
 template <bool SAFE>
@@ -175,7 +181,7 @@ __device__ __forceinline__ bool finite(const float* s) {
 }
 // (A, H) of two runs of steps, one behind the other.
 __device__ __forceinline__ float2 join(float2 first, float2 then) {
-  return make_float2(first.x * then.x, step(then.x, first.y, then.y));
+  return make_float2(then.x == 0.0f ? 0.0f : first.x * then.x, over(then.x, first.y, then.y));
 }
 
 // A thread's S steps of V channels.  Those from n on do not exist: a = 1, u = 0 (FULL:
@@ -244,6 +250,11 @@ template <typename T, int V, int S> struct Steps {
       A[v] = a[0][v];
 #pragma unroll
       for (int i = 1; i < S; ++i) A[v] *= a[i][v];
+      if (!(fabsf(A[v]) < INFINITY)) {  // past fp32's range, but not over a new start
+        A[v] = a[0][v];
+#pragma unroll
+        for (int i = 1; i < S; ++i) A[v] = a[i][v] == 0.0f ? 0.0f : A[v] * a[i][v];
+      }
     }
   }
   template <bool SAFE>
@@ -293,7 +304,7 @@ template <typename T, int V, int S> struct Steps {
       write<true, false>(p, pitch, n, a, u, s);
     }
   }
-  // The state behind the steps, from s (ZERO: from zero).
+  // The state behind the steps, from s (`zero`: from zero).
   template <bool SAFE, int KIND>
   static __device__ __forceinline__ void run_over(const float (*a)[V], const float (*b)[V], const float (*x)[V],
                                                   float* s, bool zero) {
@@ -400,7 +411,7 @@ __device__ __forceinline__ float2 load_of(const float2* p, uint32_t rank) {
 }
 
 // ------------------------------------------------------------------ between the tiles
-// LOOK, tiles that do not fit one cluster or one wave of blocks: for each tile and
+// LOOK, tiles that do not fit one cluster or two waves of blocks: for each tile and
 // channel, the tile's sum (A, H) and the state behind it, as soon as they are known.  A
 // word is its own flag: it starts as kNone, a NaN that arithmetic does not make, and is
 // written once and whole.  So no fence is needed, which would wait for its warp's copies
@@ -437,7 +448,7 @@ __device__ __forceinline__ void show(unsigned* p, float f) {
   asm volatile("st.relaxed.gpu.global.b32 [%0], %1;" ::"l"(p), "r"(v) : "memory");
 }
 __device__ __forceinline__ float fold(unsigned long long f, float s) {
-  return step(__uint_as_float((unsigned)f), s, __uint_as_float((unsigned)(f >> 32)));
+  return over(__uint_as_float((unsigned)f), s, __uint_as_float((unsigned)(f >> 32)));
 }
 
 // A wait's polls (see tc_common.cuh): false once it has to give up.
@@ -541,9 +552,9 @@ __device__ __forceinline__ Place next_place(const Job& j) {
 }
 
 // What a block's warps hand each other.  The running ones (a part of the tile's steps
-// each) put their sums; the first of them put the tile's; the folding ones (a thread has
-// a channel) put the state that enters the tile.  All twice, in turn: whoever writes the
-// next but one tile's has met all readers of the first.
+// each) put their sums; the first of them put the tile's and what stands before each
+// part; the folding one puts the state that enters the tile.  What is there twice goes in
+// turn: whoever writes the next but one tile's has met all readers of the first.
 template <int CH> struct Exchange {
   float2 sum[kParts][CH];        // (A, H); backward (A, G)
   float2 before[2][kParts][CH];  // of the parts run before
@@ -551,7 +562,8 @@ template <int CH> struct Exchange {
   float enter[2][CH];
   Place start[3], place[2];      // the first tiles; the third behind the one that runs
 };
-// Running warps among each other; the folding warps' states are there; the tile's sum is.
+// Barriers: the running warps among each other; the entering state is there; the tile's
+// sum is.  (Two each of the last, in turn.)
 enum { SUMS = 1, ENTER = 2, WHOLE = 4 };
 __device__ __forceinline__ void arrive(int id, int threads) {
   __syncwarp();
@@ -590,7 +602,7 @@ __device__ __forceinline__ void fold_tiles(const Job& j, Exchange<32 * V>& ex, P
         for (int z = 0; z < 8; ++z)
 #pragma unroll
           for (int v = 0; v < V; ++v)
-            if (z0 + z < at.q) s[v] = step(f[z][v].x, s[v], f[z][v].y);
+            if (z0 + z < at.q) s[v] = over(f[z][v].x, s[v], f[z][v].y);
       }
     }
 #pragma unroll
@@ -612,7 +624,7 @@ __device__ __forceinline__ void fold_tiles(const Job& j, Exchange<32 * V>& ex, P
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       const float2 f = ex.whole[k][ch + v];
-      if (at.q + 1 < j.tiles) show(j.state + tile0 + (size_t)at.q * CH + v, step(f.x, s[v], f.y));
+      if (at.q + 1 < j.tiles) show(j.state + tile0 + (size_t)at.q * CH + v, over(f.x, s[v], f.y));
       ex.enter[k][ch + v] = s[v];
     }
     if (threadIdx.x == kRun) ex.place[k] = last;
@@ -649,7 +661,7 @@ __device__ __forceinline__ void enter_part(const Exchange<32 * V>& ex, int k, in
 #pragma unroll
   for (int v = 0; v < V; ++v) {
     const float2 f = ex.before[k][part][at + v];
-    s[v] = step(f.x, ex.enter[k][at + v], f.y);
+    s[v] = over(f.x, ex.enter[k][at + v], f.y);
   }
 }
 
@@ -872,7 +884,7 @@ __global__ void __launch_bounds__(kRun + 32, kBlocks) k_scan_bwd(const __grid_co
 #pragma unroll
       for (int i = 0; i < per; ++i) {
         run_enter[k][p0 + i][own] = before;
-        before = step(ex.sum[p0 + i][own].x, before, run[p0 + i][own]);
+        before = over(ex.sum[p0 + i][own].x, before, run[p0 + i][own]);
       }
     }
   };

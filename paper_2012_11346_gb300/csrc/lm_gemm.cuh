@@ -39,8 +39,9 @@ constexpr int kSmemBytes = 227 * 1024 - 1024 - 512;  // after alignment and barr
 // alone.  Worth it where a worker walks along many columns.
 constexpr int kHeld = 8;
 // GATED: B is two matrices of as many rows, one behind the other (`up` rows on);
-// a tile's columns are 128 of the one, from the pair's first block, and the same
-// 128 of the other, from its second.  The epilogue gets both together.
+// half of a tile's columns are of the one, from the pair's first block, and the other
+// half the same ones of the other, from its second.  The epilogue gets both together.
+// COLS: fewer columns, for products of few tiles.
 template <int NP, bool JOIN = (NP > 1), bool HOLD_A = false, bool GATED_B = false, int COLS = kTN>
 struct Tile {
   static constexpr int TN = COLS, EPI = TN / 4;  // columns, and those of an epilogue warp
@@ -270,7 +271,8 @@ __device__ bool gemm_copy(GemmShared& sh, uint8_t* stages, Next next, int* err) 
     const CUtensorMap* map_a = uniform(&w.p->a);
     const CUtensorMap* map_b = uniform(&w.p->b);
     const int a_mn = uniform(w.p->a_mn), b_mn = uniform(w.p->b_mn);
-    const int row = uniform((w.m * kPair + rank) * kTM), col = uniform(T::GATED ? w.n * T::BROWS + rank * w.p->up : w.n * T::TN + rank * T::BROWS);
+    const int row = uniform((w.m * kPair + rank) * kTM);
+    const int col = uniform(T::GATED ? w.n * T::BROWS + rank * w.p->up : w.n * T::TN + rank * T::BROWS);
     const int k0 = uniform(w.k0) * kTK, k1 = uniform(w.k1) * kTK;
     if (T::HOLD && row != held_row) {
       if (held_row >= 0) {

@@ -1,10 +1,10 @@
 """Python binding of libslim (ctypes): argument marshalling only.
 
 Every computation runs in the CUDA kernels behind the C ABI declared in
-include/slim.h, include/slim_lm.h and include/slim_layer.h.  PyTorch supplies device memory (outputs and workspace, so
-torch.cuda.max_memory_allocated sees all of it) and the current stream.  There
-is no CPU fallback: if libslim.so is missing or no GPU is present, the calls
-raise.
+include/slim.h, include/slim_lm.h and include/slim_layer.h.  PyTorch supplies device
+memory (outputs and workspace, so torch.cuda.max_memory_allocated sees all of it) and the
+current stream.  There is no CPU fallback: if libslim.so is missing or no GPU is present,
+the calls raise.
 """
 import array
 import contextlib
@@ -1296,5 +1296,6 @@ class GatedFeedForward(torch.autograd.Function):
 
 
 def gated_ff(x, w, act="silu"):
-    """Differentiable (once) gated_ff_forward: gradients with respect to x and w."""
+    """Differentiable (once) gated_ff_forward: gradients with respect to x and w.  fp32
+    keeps both projections (8 F bytes a row) for its backward."""
     return GatedFeedForward.apply(x, w, act)
