@@ -118,7 +118,9 @@ typedef enum {
  * SIGMOID -inf) starts anew: nothing before it reaches h, finite or not.  A state
  * that is not finite stays in its channel until such a gate, or until the gates'
  * product since sinks below fp32's range.  Gates beyond 1 may grow a state past
- * fp32's range; so may the product of 128 of them alone (a state of zero stays).
+ * fp32's range; so may the product of 128 of them alone,
+ * whatever the state is: the channel is then not finite until such a gate (backward,
+ * its gradient before them).
  * Nothing written overlaps anything else but as said.
  *   workspace of slim_gated_scan_workspace_size() bytes, for either direction; where
  *   that is 0 (short sequences, few of them) it is not read and may be null.
@@ -169,13 +171,13 @@ typedef enum {
  * Without kept, neither projection is written.  bf16 operands are multiplied exactly and summed
  * in fp32; fp32 operands are split into three bf16 pieces (24 bits) and multiplied
  * piece by piece, six products each, smallest first, on the tensor cores (up to 8
- * rows: fp32 FMA in either type).  h is rounded once.
+ * rows, where that is quicker: fp32 FMA in either type).  h is rounded once.
  * Values are finite: an infinity in a row of x, or of w, makes what it enters
  * infinite or NaN.
  * 0 <= N < 2^31 - 512, 1 <= D <= 2^30, 1 <= F <= 2^29, N F <= 2^45, N D and 2 F D
  * <= 2^40.  N = 0 enqueues nothing.
  *   workspace of slim_gated_ff_workspace_size(..., backward = 0) bytes; where that is
- *   0 (up to 8 rows) it may be null.
+ *   0 (a few rows) it may be null.
  */
 slim_status slim_gated_ff_workspace_size(long long N, int D, int F, slim_dtype dtype, int backward,
                                          size_t* bytes);

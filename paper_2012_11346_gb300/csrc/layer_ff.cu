@@ -267,8 +267,8 @@ __global__ void __launch_bounds__(256) k_ff_kept(const __grid_constant__ FfJob j
 // Keeping both projections is the quicker for fp32 rows: 8192 x 1024 x 2048, a step of 805
 // us (1002 with them computed again), 32768 x 64 x 1024 462 (506).  bf16 would have to
 // round them to gain.
-bool keeps(long long N, int D, slim_dtype dtype) {
-  return dtype == SLIM_F32 && N > 0 && !layer::ff_rows_fit(N, D, dtype);
+bool keeps(long long N, int D, int F, slim_dtype dtype) {
+  return dtype == SLIM_F32 && N > 0 && !layer::ff_rows_fit(N, D, F, dtype);
 }
 
 struct FfSizes {
@@ -489,7 +489,7 @@ extern "C" slim_status slim_gated_ff_workspace_size(long long N, int D, int F, s
   using namespace slim::lm;
   if (!bytes || !ff_sizes_ok(N, D, F, dtype, SLIM_ACT_SILU) || (backward & ~1)) return SLIM_ERR_INVALID_ARG;
   *bytes = 0;
-  if (!backward && slim::layer::ff_rows_fit(N, D, dtype)) return SLIM_OK;
+  if (!backward && slim::layer::ff_rows_fit(N, D, F, dtype)) return SLIM_OK;
   slim::Carver cv(nullptr);
   ff_carve(cv, FfSizes{N, D, F, dtype}, backward != 0);
   *bytes = cv.bytes();
@@ -499,7 +499,7 @@ extern "C" slim_status slim_gated_ff_workspace_size(long long N, int D, int F, s
 extern "C" slim_status slim_gated_ff_kept_size(long long N, int D, int F, slim_dtype dtype, size_t* bytes) {
   using namespace slim::lm;
   if (!bytes || !ff_sizes_ok(N, D, F, dtype, SLIM_ACT_SILU)) return SLIM_ERR_INVALID_ARG;
-  *bytes = keeps(N, D, dtype) ? (size_t)N * 2 * FfSizes{N, D, F, dtype}.half() * sizeof(float) : 0;
+  *bytes = keeps(N, D, F, dtype) ? (size_t)N * 2 * FfSizes{N, D, F, dtype}.half() * sizeof(float) : 0;
   return SLIM_OK;
 }
 
@@ -521,11 +521,11 @@ extern "C" slim_status slim_gated_ff_fwd(const void* x, const void* w, long long
                                          void* workspace, size_t workspace_bytes, void* stream) {
   using namespace slim::lm;
   if (!ff_sizes_ok(N, D, F, dtype, act) || !aligned(w, 16)) return SLIM_ERR_INVALID_ARG;
-  if (kept && (!keeps(N, D, dtype) || !aligned(kept, 32))) return SLIM_ERR_INVALID_ARG;
+  if (kept && (!keeps(N, D, F, dtype) || !aligned(kept, 32))) return SLIM_ERR_INVALID_ARG;
   if (N == 0) return SLIM_OK;
   if (!aligned(x, 16) || !aligned(h, 16)) return SLIM_ERR_INVALID_ARG;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  const bool rows = slim::layer::ff_rows_fit(N, D, dtype);
+  const bool rows = slim::layer::ff_rows_fit(N, D, F, dtype);
   unsigned* rep = nullptr;
   const slim_status st = ff_begin(N, D, F, dtype, 0, workspace, workspace_bytes, !rows, &rep);
   if (st != SLIM_OK) return st;
@@ -547,7 +547,7 @@ extern "C" slim_status slim_gated_ff_bwd(const void* x, const void* w, const voi
                                          void* stream) {
   using namespace slim::lm;
   if (!ff_sizes_ok(N, D, F, dtype, act) || !aligned(w, 16) || !aligned(dw, 16)) return SLIM_ERR_INVALID_ARG;
-  if (kept && (!keeps(N, D, dtype) || !aligned(kept, 32))) return SLIM_ERR_INVALID_ARG;
+  if (kept && (!keeps(N, D, F, dtype) || !aligned(kept, 32))) return SLIM_ERR_INVALID_ARG;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   if (N == 0) {
     const size_t n = 2 * (size_t)F * D * (dtype == SLIM_F32 ? 4 : 2);

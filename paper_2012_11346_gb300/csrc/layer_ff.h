@@ -77,7 +77,7 @@ __host__ __device__ __forceinline__ void with_act(int act, Go go) {
 }
 
 // Whether a forward of these sizes takes the form for a few rows.
-bool ff_rows_fit(long long N, int D, slim_dtype dtype);
+bool ff_rows_fit(long long N, int D, int F, slim_dtype dtype);
 // Arguments as in slim_gated_ff_fwd, already checked.  Nothing waits: no workspace.
 slim_status ff_rows_fwd(const void* x, const void* w, int N, int D, int F, slim_dtype dtype,
                         slim_act act, void* h, cudaStream_t s);

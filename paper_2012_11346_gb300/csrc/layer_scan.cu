@@ -156,11 +156,6 @@ template <int KIND> struct Gate {
 
 // a s + u; a of zero forgets a state that is not finite, too.
 __device__ __forceinline__ float step(float a, float s, float u) { return a == 0.0f ? u : fmaf(a, s, u); }
-// The same over some steps: a state of zero stays what it is under a product of gates
-// past fp32's range.
-__device__ __forceinline__ float over(float A, float s, float H) {
-  return A == 0.0f || (s == 0.0f && A == A) ? H : fmaf(A, s, H);
-}
 // The same where `safe`, else the plain sum.  The plain sum of a state that is not
 // finite stays so to the end of a thread's steps, which then takes them again.
 template <bool SAFE>
@@ -179,9 +174,11 @@ __device__ __forceinline__ bool finite(const float* s) {
   for (int v = 0; v < V; ++v) ok = ok && fabsf(s[v]) < INFINITY;
   return ok;
 }
-// (A, H) of two runs of steps, one behind the other.
+// (A, H) of two runs of steps, one behind the other.  A product past fp32's range is not
+// carried over a new start; that a state of zero survives one is not provided for (a
+// select more in each fold: 5 % of a bf16 step).
 __device__ __forceinline__ float2 join(float2 first, float2 then) {
-  return make_float2(then.x == 0.0f ? 0.0f : first.x * then.x, over(then.x, first.y, then.y));
+  return make_float2(then.x == 0.0f ? 0.0f : first.x * then.x, step(then.x, first.y, then.y));
 }
 
 // A thread's S steps of V channels.  Those from n on do not exist: a = 1, u = 0 (FULL:
@@ -244,17 +241,14 @@ template <typename T, int V, int S> struct Steps {
         if (!FULL && i >= n) x[i][v] = 0.0f;
     }
   }
+  // SAFE: past fp32's range it may go, but not over a new start
+  template <bool SAFE>
   static __device__ __forceinline__ void product(const float (*a)[V], float* A) {
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       A[v] = a[0][v];
 #pragma unroll
-      for (int i = 1; i < S; ++i) A[v] *= a[i][v];
-      if (!(fabsf(A[v]) < INFINITY)) {  // past fp32's range, but not over a new start
-        A[v] = a[0][v];
-#pragma unroll
-        for (int i = 1; i < S; ++i) A[v] = a[i][v] == 0.0f ? 0.0f : A[v] * a[i][v];
-      }
+      for (int i = 1; i < S; ++i) A[v] = SAFE && a[i][v] == 0.0f ? 0.0f : A[v] * a[i][v];
     }
   }
   template <bool SAFE>
@@ -448,7 +442,7 @@ __device__ __forceinline__ void show(unsigned* p, float f) {
   asm volatile("st.relaxed.gpu.global.b32 [%0], %1;" ::"l"(p), "r"(v) : "memory");
 }
 __device__ __forceinline__ float fold(unsigned long long f, float s) {
-  return over(__uint_as_float((unsigned)f), s, __uint_as_float((unsigned)(f >> 32)));
+  return step(__uint_as_float((unsigned)f), s, __uint_as_float((unsigned)(f >> 32)));
 }
 
 // A wait's polls (see tc_common.cuh): false once it has to give up.
@@ -602,7 +596,7 @@ __device__ __forceinline__ void fold_tiles(const Job& j, Exchange<32 * V>& ex, P
         for (int z = 0; z < 8; ++z)
 #pragma unroll
           for (int v = 0; v < V; ++v)
-            if (z0 + z < at.q) s[v] = over(f[z][v].x, s[v], f[z][v].y);
+            if (z0 + z < at.q) s[v] = step(f[z][v].x, s[v], f[z][v].y);
       }
     }
 #pragma unroll
@@ -624,7 +618,7 @@ __device__ __forceinline__ void fold_tiles(const Job& j, Exchange<32 * V>& ex, P
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       const float2 f = ex.whole[k][ch + v];
-      if (at.q + 1 < j.tiles) show(j.state + tile0 + (size_t)at.q * CH + v, over(f.x, s[v], f.y));
+      if (at.q + 1 < j.tiles) show(j.state + tile0 + (size_t)at.q * CH + v, step(f.x, s[v], f.y));
       ex.enter[k][ch + v] = s[v];
     }
     if (threadIdx.x == kRun) ex.place[k] = last;
@@ -661,7 +655,7 @@ __device__ __forceinline__ void enter_part(const Exchange<32 * V>& ex, int k, in
 #pragma unroll
   for (int v = 0; v < V; ++v) {
     const float2 f = ex.before[k][part][at + v];
-    s[v] = over(f.x, ex.enter[k][at + v], f.y);
+    s[v] = step(f.x, ex.enter[k][at + v], f.y);
   }
 }
 
@@ -764,9 +758,12 @@ __global__ void __launch_bounds__(kRun + 32, kBlocks) k_scan_fwd(const __grid_co
   auto sums = [&](const Place& p, int slot, int k) {
     float a[S][V], u[S][V], A[V], H[V];
     inputs(steps_of(p), slot, a, u);
-    P::product(a, A);
+    P::template product<false>(a, A);
     P::template forward<false>(a, u, H);
-    if (!finite<V>(H)) P::template forward<true>(a, u, H);
+    if (!finite<V>(H) || !finite<V>(A)) {
+      P::template product<true>(a, A);
+      P::template forward<true>(a, u, H);
+    }
 #pragma unroll
     for (int v = 0; v < V; ++v) ex.sum[part][lane * V + v] = make_float2(A[v], H[v]);
     meet(SUMS, kRun);
@@ -867,9 +864,12 @@ __global__ void __launch_bounds__(kRun + 32, kBlocks) k_scan_bwd(const __grid_co
     const int n = steps_of(p);
     float a[S][V], bb[S][V], y[S][V], dh[S][V], A[V], H[V], G[V];
     front(n, slot, a, bb, y);
-    P::product(a, A);
+    P::template product<false>(a, A);
     P::template run_over<false, KIND>(a, bb, y, H, true);
-    if (!finite<V>(H)) P::template run_over<true, KIND>(a, bb, y, H, true);
+    if (!finite<V>(H) || !finite<V>(A)) {
+      P::template product<true>(a, A);
+      P::template run_over<true, KIND>(a, bb, y, H, true);
+    }
     above(n, slot, dh);
     P::template backward<false>(a, dh, G);
     if (!finite<V>(G)) P::template backward<true>(a, dh, G);
@@ -884,7 +884,7 @@ __global__ void __launch_bounds__(kRun + 32, kBlocks) k_scan_bwd(const __grid_co
 #pragma unroll
       for (int i = 0; i < per; ++i) {
         run_enter[k][p0 + i][own] = before;
-        before = over(ex.sum[p0 + i][own].x, before, run[p0 + i][own]);
+        before = step(ex.sum[p0 + i][own].x, before, run[p0 + i][own]);
       }
     }
   };
