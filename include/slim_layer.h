@@ -139,7 +139,8 @@ slim_status slim_gated_scan_fwd(const void* gate, long long gate_pitch, const vo
  *   kept     from the forward on the same gate, x and h0; the states inside a chunk
  *            are computed again from it, in fp32.
  *   dh       [B, L, D] dtype;  dlast [B, D] fp32, or null (zero).
- *   dgate, dx  [B, L, D] dtype with pitches of their own, written.
+ *   dgate, dx  [B, L, D] dtype with pitches of their own, written; they may be gate
+ *            and x themselves, with the same pitches.
  *   dh0      [B, D] fp32, written, or null; it may be dlast itself.
  * Where a step starts anew its LOG or SIGMOID gate has gradient 0.
  */

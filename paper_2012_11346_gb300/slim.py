@@ -855,8 +855,18 @@ def rotary_frequencies(rotary, base=10000.0):
 
 
 @functools.lru_cache(maxsize=1024)
-def _qk_sizes(q, k, positions, rotary, dtype, k_dtype, what):
-    """(B, Hq, Hk, L, d, dtype code) of checked shapes."""
+def _strides(stride, d):
+    """A [B, H, L, d] tensor's slim_strides and their address; the last dimension is
+    contiguous."""
+    if stride[3] != 1 and d > 1:
+        raise RuntimeError("libslim needs rows whose features are contiguous")
+    a = array.array("q", stride[:3])
+    return a, a.buffer_info()[0]
+
+
+@functools.lru_cache(maxsize=1024)
+def _qk_sizes(q, q_stride, k, k_stride, positions, rotary, dtype, k_dtype, what):
+    """(B, Hq, Hk, L, d, dtype code) of checked shapes, and both sides' strides."""
     if len(q) != 4 or (k is not None and len(k) != 4):
         raise ValueError("q and k must be [B, H, L, d]")
     B, Hq, L, d = q
@@ -870,68 +880,58 @@ def _qk_sizes(q, k, positions, rotary, dtype, k_dtype, what):
         raise ValueError("positions must be contiguous [B, L]")
     if dtype not in DTYPES:
         raise TypeError(f"{what}: float32 or bfloat16 expected, got {dtype}")
-    return B, Hq, Hk, L, d, DTYPES[dtype]
+    return ((B, Hq, Hk, L, d, DTYPES[dtype]), _strides(q_stride, d),
+            (None, None) if k is None else _strides(k_stride, d))
 
 
-@functools.lru_cache(maxsize=1024)
-def _strides(stride, d):
-    """A [B, H, L, d] tensor's slim_strides; the last dimension is contiguous."""
-    if stride[3] != 1 and d > 1:
-        raise RuntimeError("libslim needs rows whose features are contiguous")
-    return array.array("q", stride[:3])
-
-
-class _QkCall:
-    """What both directions of qk_norm marshal alike."""
-
-    def __init__(self, q, k, q_weight, k_weight, positions, inv_freq, what):
-        if inv_freq is None:
-            inv_freq = ()
-        elif isinstance(inv_freq, torch.Tensor) and inv_freq.is_cuda:
+def _qk_call(q, k, q_weight, k_weight, positions, inv_freq, what):
+    """What both directions of qk_norm marshal alike: (device, sizes, the call's first
+    arguments, what they point into)."""
+    if not (isinstance(inv_freq, array.array) and inv_freq.typecode == "d"):
+        if isinstance(inv_freq, torch.Tensor) and inv_freq.is_cuda:
             raise TypeError("inv_freq is read on the host: give numbers or a CPU tensor")
-        if not (isinstance(inv_freq, array.array) and inv_freq.typecode == "d"):
-            inv_freq = array.array("d", map(float, inv_freq))
-        rotary = 2 * len(inv_freq)
-        self.sizes = _qk_sizes(q.shape, None if k is None else k.shape,
-                               None if positions is None else positions.shape, rotary, q.dtype,
-                               None if k is None else k.dtype, what)
-        B, Hq, Hk, L, self.d, _ = self.sizes
-        pp, ptype = None, 0
-        if positions is not None:
-            ptype = _index_code(positions, "positions")
-            if not positions.is_contiguous():
-                raise ValueError("positions must be contiguous [B, L]")
-            pp = positions.data_ptr()
-        self.dev = _device_of(q, k, q_weight, k_weight, positions)
-        self.kept = [inv_freq]  # until the call is made
-        self.head = (*self.rows(q), *self.rows(k), _fp32_or_none(q_weight, (self.d,), "q_weight"),
-                     _fp32_or_none(k_weight, (self.d,), "k_weight"), pp, ptype,
-                     inv_freq.buffer_info()[0] if rotary else None, rotary)
+        inv_freq = array.array("d", () if inv_freq is None else map(float, inv_freq))
+    rotary = 2 * len(inv_freq)
+    at = positions is not None
+    if k is None:
+        plan = _qk_sizes(q.shape, q.stride(), None, None, positions.shape if at else None, rotary, q.dtype, None, what)
+        kp = None
+    else:
+        plan = _qk_sizes(q.shape, q.stride(), k.shape, k.stride(), positions.shape if at else None, rotary, q.dtype,
+                         k.dtype, what)
+        kp = k.data_ptr()
+    sizes, qs, ks = plan
+    pp, ptype = None, 0
+    if at:
+        ptype = _index_code(positions, "positions")
+        if not positions.is_contiguous():
+            raise ValueError("positions must be contiguous [B, L]")
+        pp = positions.data_ptr()
+    weight = (sizes[4],)
+    return (_device_of(q, k, q_weight, k_weight, positions), sizes,
+            (q.data_ptr(), qs[1], kp, ks[1], _fp32_or_none(q_weight, weight, "q_weight"),
+             _fp32_or_none(k_weight, weight, "k_weight"), pp, ptype, inv_freq.buffer_info()[0] if rotary else None,
+             rotary), (plan, inv_freq))
 
-    def rows(self, t):
-        """A [B, H, L, d] tensor's pointer and strides."""
-        if t is None:
-            return None, None
-        strides = _strides(t.stride(), self.d)
-        self.kept.append(strides)
-        return t.data_ptr(), strides.buffer_info()[0]
 
-    def check(self, t, given, what):
-        """`given` is like t, or None where t is."""
-        if t is None or given.dtype != t.dtype or given.shape != t.shape:
-            raise ValueError(f"{what} must have the shape and dtype of its input")
-        _device_of(t, given)
+def _qk_check(t, given, what):
+    """`given` is like t, or None where t is."""
+    if t is None or given.dtype != t.dtype or given.shape != t.shape:
+        raise ValueError(f"{what} must have the shape and dtype of its input")
+    _device_of(t, given)
 
-    def like(self, t, given, what):
-        """(tensor, pointer, strides): `given`, checked, or a new contiguous one like t
-        (None without t)."""
-        if given is not None:
-            self.check(t, given, what)
-            return given, *self.rows(given)
-        if t is None:
-            return None, None, None
-        out = _new(t.shape, t.dtype)
-        return out, out.data_ptr(), None
+
+def _qk_like(t, given, what):
+    """(tensor, pointer, strides' address, strides): `given`, checked, or a new contiguous
+    one like t (None without t)."""
+    if given is not None:
+        _qk_check(t, given, what)
+        strides, address = _strides(given.stride(), t.shape[3])
+        return given, given.data_ptr(), address, strides
+    if t is None:
+        return None, None, None, None
+    out = _new(t.shape, t.dtype)
+    return out, out.data_ptr(), None, None
 
 
 def qk_norm_forward(q, k, q_weight=None, k_weight=None, positions=None, inv_freq=None, interleaved=False,
@@ -944,12 +944,12 @@ def qk_norm_forward(q, k, q_weight=None, k_weight=None, positions=None, inv_freq
     inv_freq: radians per position on the host (see rotary_frequencies), None:
     no rotation.  Returns (q_out, k_out), contiguous unless given; they may be q
     and k themselves."""
-    c = _QkCall(q, k, q_weight, k_weight, positions, inv_freq, "qk_norm_forward")
-    with _at(c.dev, stream):
-        q_out, qp, qs = c.like(q, q_out, "q_out")
-        k_out, kp, ks = c.like(k, k_out, "k_out")
-        status = library().slim_qk_norm_fwd(*c.head, int(interleaved), *c.sizes, eps, scale, qp, qs, kp, ks,
-                                            _raw(c.dev, stream))
+    dev, sizes, head, kept = _qk_call(q, k, q_weight, k_weight, positions, inv_freq, "qk_norm_forward")
+    with _at(dev, stream):
+        q_out, qp, qs, q_strides = _qk_like(q, q_out, "q_out")
+        k_out, kp, ks, k_strides = _qk_like(k, k_out, "k_out")
+        status = library().slim_qk_norm_fwd(*head, int(interleaved), *sizes, eps, scale, qp, qs, kp, ks,
+                                            _raw(dev, stream))
     _check(status, "slim_qk_norm_fwd")
     return q_out, k_out
 
@@ -972,23 +972,24 @@ def qk_norm_backward(q, k, q_weight, k_weight, dq_out, dk_out, positions=None, i
     dq and dk are contiguous unless given: slices of the projection's gradient,
     or dq_out and dk_out themselves.  A weight's gradient ([d] fp32) is None
     where there is no such weight or with weights=False."""
-    c = _QkCall(q, k, q_weight, k_weight, positions, inv_freq, "qk_norm_backward")
+    dev, sizes, head, kept = _qk_call(q, k, q_weight, k_weight, positions, inv_freq, "qk_norm_backward")
     if dq_out is None or (k is not None and dk_out is None):
         raise ValueError("dq_out and dk_out are needed")
-    c.check(q, dq_out, "dq_out")
+    _, up_qp, up_qs, q_above = _qk_like(q, dq_out, "dq_out")
+    up_kp = up_ks = k_above = None
     if dk_out is not None:
-        c.check(k, dk_out, "dk_out")
+        _, up_kp, up_ks, k_above = _qk_like(k, dk_out, "dk_out")
     if workspace is not None:
         _require_cuda(workspace)
-    with _at(c.dev, stream):
-        dq, qp, qs = c.like(q, dq, "dq")
-        dk, kp, ks = c.like(k, dk, "dk")
+    with _at(dev, stream):
+        dq, qp, qs, q_strides = _qk_like(q, dq, "dq")
+        dk, kp, ks, k_strides = _qk_like(k, dk, "dk")
         dwq, dwk = (_new(w.shape, w.dtype) if weights and w is not None else None
                     for w in (q_weight, k_weight))
-        ws = workspace if workspace is not None else _new((qk_norm_workspace_size(*c.sizes[:5]),), torch.uint8)
-        status = library().slim_qk_norm_bwd(*c.head, int(interleaved), *c.sizes, eps, scale, *c.rows(dq_out),
-                                            *c.rows(dk_out), qp, qs, kp, ks, _ptr(dwq), _ptr(dwk),
-                                            ws.data_ptr(), ws.numel(), _raw(c.dev, stream))
+        ws = workspace if workspace is not None else _new((qk_norm_workspace_size(*sizes[:5]),), torch.uint8)
+        status = library().slim_qk_norm_bwd(*head, int(interleaved), *sizes, eps, scale, up_qp, up_qs, up_kp, up_ks,
+                                            qp, qs, kp, ks, _ptr(dwq), _ptr(dwk), ws.data_ptr(), ws.numel(),
+                                            _raw(dev, stream))
     _check(status, "slim_qk_norm_bwd")
     return dq, dk, dwq, dwk
 
@@ -1118,7 +1119,8 @@ def gated_scan_backward(gate, x, kept, dh, kind="sigmoid", dlast=None, dgate=Non
     """slim_gated_scan_bwd: returns (dgate, dx, dh0), the gradients of <dh, h> +
     <dlast, last>.  kept: from gated_scan_forward(..., keep=True) on the same inputs;
     dlast: [B, D] fp32 or None (zero).  dgate and dx are contiguous unless given
-    (slices of the projection's gradient); dh0 may be given, too, also as dlast."""
+    (slices of the projection's gradient, or gate and x themselves); dh0 may be given, too,
+    also as dlast."""
     sizes, gp, xp = _scan_sizes(gate.shape, x.shape, gate.stride(), x.stride(), gate.dtype, x.dtype, kind,
                                 "gated_scan_backward")
     B, L, D, _, _ = sizes

@@ -169,6 +169,16 @@ def test_token_by_token(cuda_device):
     assert rel(state, last) < 1e-5
 
 
+@pytest.mark.parametrize("dt", [F32, BF16])
+@pytest.mark.parametrize("L", [3, 64, 300, 3000])
+def test_gradients_over_their_inputs(cuda_device, L, dt):
+    gate, x, h0, dh, dlast = make(cuda_device, 3, L, 72, "sigmoid", dt)
+    kept = slim.gated_scan_forward(gate, x, "sigmoid", h0=h0, keep=True)[2]
+    ref = slim.gated_scan_backward(gate, x, kept, dh, "sigmoid", dlast=dlast)
+    got = slim.gated_scan_backward(gate, x, kept, dh, "sigmoid", dlast=dlast, dgate=gate, dx=x)
+    assert got[0] is gate and got[1] is x and all(torch.equal(a, b) for a, b in zip(got, ref))
+
+
 @pytest.mark.parametrize("L", [3, 64, 300])
 def test_states_in_place(cuda_device, L):
     gate, x, h0, dh, dlast = make(cuda_device, 2, L, 36, "log", F32)
