@@ -123,7 +123,7 @@ typedef enum {
  * its gradient before them).
  * Nothing written overlaps anything else but as said.
  *   workspace of slim_gated_scan_workspace_size() bytes, for either direction; where
- *   that is 0 (short sequences, few of them) it is not read and may be null.
+ *   that is 0 (short sequences, few of them) it is not used and may be null.
  * 0 <= B, 0 <= L <= 2^30, 1 <= D <= 2^30, B D <= 2^32, B L D <= 2^40,
  * D <= pitch (0 <= pitch for inputs) <= 2^40, offsets below 2^60.  With B L = 0 the
  * state is passed on.

@@ -1119,6 +1119,9 @@ slim_status run(Job& j, slim_dtype dtype, slim_gate kind, int together, bool bwd
     if (reinterpret_cast<uintptr_t>(workspace) & 255) return SLIM_ERR_INVALID_ARG;
     const slim_status st = report::begin(workspace, true, &call.rep);
     if (st != SLIM_OK) return st;
+  } else if (workspace) {
+    const slim_status st = report::pending(workspace);
+    if (st != SLIM_OK) return st;
   }
   const bool ok = dtype == SLIM_F32 ? run_t<float>(j, kind, together, call)
                                     : run_t<__nv_bfloat16>(j, kind, together, call);

@@ -1285,7 +1285,8 @@ class GatedFeedForward(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x_in, w_in, act):
         x, w = _ready(x_in), _ready(w_in)
-        h, z = gated_ff_forward(x, w, act, keep=True)
+        h, z = gated_ff_forward(x, w, act, keep=True) if any(ctx.needs_input_grad) else (
+            gated_ff_forward(x, w, act), None)
         ctx.save_for_backward(x_in, w_in, x, w, z)
         ctx.act = act
         return h
