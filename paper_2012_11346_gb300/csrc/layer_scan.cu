@@ -774,6 +774,7 @@ __global__ void __launch_bounds__(kRun + 32, kBlocks) k_scan_fwd(const __grid_co
   fetch(then, 1);
   fetch_wait();
   sums(at, 0, 0);
+  meet(SUMS, kRun);  // the sums are read: no state is waited for between these and the next
   int slot = 0;
   for (int k = 0; at.q >= 0; k ^= 1) {
     const int slot1 = slot == 2 ? 0 : slot + 1;
@@ -893,6 +894,7 @@ __global__ void __launch_bounds__(kRun + 32, kBlocks) k_scan_bwd(const __grid_co
   fetch(then, 1);
   fetch_wait();
   sums(at, 0, 0);
+  meet(SUMS, kRun);  // the sums are read: no state is waited for between these and the next
   int slot = 0;
   for (int k = 0; at.q >= 0; k ^= 1) {
     const int slot1 = slot == 2 ? 0 : slot + 1;

@@ -294,6 +294,45 @@ def test_a_sequence_does_not_depend_on_its_neighbours(cuda_device):
         assert all(torch.equal(p[0], q[b]) for p, q in zip((*a, *g), (*out, *grads)))
 
 
+@pytest.mark.parametrize("B,L,D,kind,dt", [(8, 4096, 512, "value", F32), (2, 4097, 1000, "sigmoid", BF16),
+                                           (1, 30000, 512, "log", BF16), (1, 9001, 77, "log", F32)])
+def test_the_same_bits_beside_other_work(cuda_device, B, L, D, kind, dt):
+    """Warps that are held up do not read what others have moved on to: the same bits every
+    time, alone and with products on another stream, and those of the same sequence cut
+    into pieces within the roundings of another order."""
+    gate, x, h0, dh, dlast = make(cuda_device, B, L, D, kind, dt)
+    other, side = torch.randn(4096, 4096, device=cuda_device).to(BF16), torch.cuda.Stream()
+
+    def both():
+        a = slim.gated_scan_forward(gate, x, kind, h0=h0, keep=True)
+        return a + slim.gated_scan_backward(gate, x, a[2], dh, kind, dlast=dlast)
+
+    ref = both()
+    torch.cuda.synchronize()
+    for i in range(20):
+        if i % 2:
+            with torch.cuda.stream(side):
+                for _ in range(3):
+                    other @ other
+        out = both()
+        torch.cuda.synchronize()
+        assert all(torch.equal(p, q) for p, q in zip(out, ref)), i
+    # pieces of up to 512 steps are clusters of a few tiles each
+    s, pieces = h0, []
+    for a in range(0, L, 512):
+        g, u = gate[:, a:a + 512].contiguous(), x[:, a:a + 512].contiguous()
+        h, s, kept = slim.gated_scan_forward(g, u, kind, h0=s, keep=True)
+        pieces.append((g, u, h, kept))
+    assert rel(torch.cat([p[2] for p in pieces], 1), ref[0]) < (1e-5 if dt == F32 else 4e-3) and rel(s, ref[1]) < 1e-5
+    d, grads = dlast, []
+    for i, (g, u, _, kept) in reversed(list(enumerate(pieces))):
+        dg, du, d = slim.gated_scan_backward(g, u, kept, dh[:, 512 * i:512 * i + 512].contiguous(), kind, dlast=d)
+        grads.append((dg, du))
+    for k in range(2):
+        assert rel(torch.cat([g[k] for g in reversed(grads)], 1), ref[3 + k]) < (1e-5 if dt == F32 else 4e-3)
+    assert rel(d, ref[5]) < 1e-5
+
+
 def test_two_calls_at_once(cuda_device):
     """Two streams whose tiles share the GPU, each with a workspace of its own."""
     sets = [make(cuda_device, 2, 9000, 96, "sigmoid", BF16, seed=i) for i in range(2)]
