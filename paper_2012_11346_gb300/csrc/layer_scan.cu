@@ -24,7 +24,7 @@
 //
 // Measured: 1 x 65536 x 512 fp32 forward 80 us (5.0 TB/s of inputs and outputs; 190 us
 // with all of a sequence's tiles in one cluster's rounds), 8 x 4096 x 512 bf16 step with
-// sigmoid gates 99 us (forward kernel 37, backward 60).  bf16 is bound by its
+// sigmoid gates 101 us (forward kernel 37, backward 62).  bf16 is bound by its
 // instructions (49 per element forward, 74 backward, both passes), fp32 by the exchange's
 // latency and HBM.
 //
