@@ -854,6 +854,13 @@ def rotary_frequencies(rotary, base=10000.0):
     return array.array("d", [base ** (-2.0 * p / rotary) for p in range(rotary // 2)])
 
 
+def _frequencies(inv_freq):
+    """inv_freq, numbers or None, as an array of its own."""
+    if isinstance(inv_freq, torch.Tensor) and inv_freq.is_cuda:
+        raise TypeError("inv_freq is read on the host: give numbers or a CPU tensor")
+    return array.array("d", () if inv_freq is None else map(float, inv_freq))
+
+
 @functools.lru_cache(maxsize=1024)
 def _strides(stride, d):
     """A [B, H, L, d] tensor's slim_strides and their address; the last dimension is
@@ -888,9 +895,7 @@ def _qk_call(q, k, q_weight, k_weight, positions, inv_freq, what):
     """What both directions of qk_norm marshal alike: (device, sizes, the call's first
     arguments, what they point into)."""
     if not (isinstance(inv_freq, array.array) and inv_freq.typecode == "d"):
-        if isinstance(inv_freq, torch.Tensor) and inv_freq.is_cuda:
-            raise TypeError("inv_freq is read on the host: give numbers or a CPU tensor")
-        inv_freq = array.array("d", () if inv_freq is None else map(float, inv_freq))
+        inv_freq = _frequencies(inv_freq)
     rotary = 2 * len(inv_freq)
     at = positions is not None
     if k is None:
@@ -1025,8 +1030,9 @@ class QkNorm(torch.autograd.Function):
 
 def qk_norm(q, k, q_weight=None, k_weight=None, positions=None, inv_freq=None, interleaved=False,
             eps=1e-6, scale=1.0):
-    """Differentiable (once) qk_norm_forward: gradients with respect to q, k and the weights."""
-    return QkNorm.apply(q, k, q_weight, k_weight, positions, inv_freq, interleaved, eps, scale)
+    """Differentiable (once) qk_norm_forward: gradients with respect to q, k and the weights.
+    inv_freq is read once, for both directions."""
+    return QkNorm.apply(q, k, q_weight, k_weight, positions, _frequencies(inv_freq), interleaved, eps, scale)
 
 
 GATES = {"value": 0, "log": 1, "sigmoid": 2}

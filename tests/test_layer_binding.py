@@ -1,0 +1,38 @@
+"""What the differentiable calls around the attention hand to the library's entry points:
+host-only, with stand-ins in the entry points' place."""
+import array
+
+import pytest
+import torch
+
+from paper_2012_11346_gb300 import slim
+
+
+@pytest.fixture
+def qk_calls(monkeypatch):
+    """What each direction of qk_norm was called with."""
+    calls = []
+
+    def forward(q, k, *weights, **how):
+        calls.append(dict(how, inv_freq=list(how["inv_freq"] or ())))
+        return q.clone(), None if k is None else k.clone()
+
+    def backward(q, k, q_weight, k_weight, dq_out, dk_out, **how):
+        calls.append(dict(how, inv_freq=list(how["inv_freq"] or ())))
+        return dq_out, dk_out, None, None
+
+    monkeypatch.setattr(slim, "qk_norm_forward", forward)
+    monkeypatch.setattr(slim, "qk_norm_backward", backward)
+    return calls
+
+
+@pytest.mark.parametrize("form", [iter, list, torch.tensor, lambda f: array.array("d", f)])
+def test_both_directions_turn_alike(qk_calls, form):
+    """Frequencies that can be read once, or that change between the directions."""
+    q = torch.randn(1, 2, 3, 8, requires_grad=True)
+    freq = form([1.0, 0.5])
+    out, _ = slim.qk_norm(q, None, inv_freq=freq)
+    if hasattr(freq, "__setitem__"):
+        freq[0] = 7.0
+    out.sum().backward()
+    assert [c["inv_freq"] for c in qk_calls] == [[1.0, 0.5]] * 2
