@@ -117,10 +117,10 @@ typedef enum {
  * States and sums are fp32, h is rounded once.  A gate of zero (VALUE 0, LOG or
  * SIGMOID -inf) starts anew: nothing before it reaches h, finite or not.  A state
  * that is not finite stays in its channel until such a gate, or until the gates'
- * product since sinks below fp32's range.  Gates beyond 1 may grow a state past
- * fp32's range; so may the product of 128 of them alone,
- * whatever the state is: the channel is then not finite until such a gate (backward,
- * its gradient before them).
+ * product since sinks below fp32's range.  Gates are finite, but for those infinities.
+ * Beyond 1 they may grow a state past fp32's range; so may the product of up to 128 of
+ * them alone: a state that is not zero is then not finite until such a gate (backward, a
+ * gradient before them), one of zero stays zero.
  * Nothing written overlaps anything else but as said.
  *   workspace of slim_gated_scan_workspace_size() bytes, for either direction; where
  *   that is 0 (short sequences, few of them) it is not used and may be null.

@@ -1098,7 +1098,9 @@ def gated_scan_forward(gate, x, kind="sigmoid", h0=None, keep=False, last=None, 
     gate, u = x; "log": a = exp(gate), u = x; "sigmoid": a = sigmoid(gate), u =
     (1 - a) x.  h0: the state to start from, [B, D] fp32 or None (zero).  Returns
     (h, last): all states in x's dtype and the last in fp32 (into `last` if given,
-    which may be h0); with keep=True also what gated_scan_backward needs."""
+    which may be h0); with keep=True also what gated_scan_backward needs.  Gates beyond 1
+    whose product over up to 128 steps passes fp32's range make a state that is not zero
+    infinite or NaN, even where it alone would not have left that range."""
     sizes, gp, xp = _scan_sizes(gate.shape, x.shape, gate.stride(), x.stride(), gate.dtype, x.dtype, kind,
                                 "gated_scan_forward")
     B, L, D, _, _ = sizes
