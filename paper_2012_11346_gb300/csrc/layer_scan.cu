@@ -163,12 +163,9 @@ __device__ __forceinline__ float next(float a, float s, float u) {
   return SAFE ? step(a, s, u) : fmaf(a, s, u);
 }
 // A s + H over the steps that (A, H) stand for.  Where their gates' product is past fp32's
-// range, a state of zero stays zero as it does step by step.  The plain sum is the same
-// where it is finite, and once it is not stays so over what follows, to be taken again.
-template <bool SAFE>
+// range, a state of zero stays zero, as it does step by step.
 __device__ __forceinline__ float over(float A, float s, float H) {
-  const float r = fmaf(A, s, H);
-  return SAFE && !(fabsf(r) < INFINITY) && (A == 0.0f || (s == 0.0f && A == A)) ? H : r;
+  return A == 0.0f || s == 0.0f ? H : fmaf(A, s, H);
 }
 // What of g passes to the step before a's.
 template <bool SAFE>
@@ -182,29 +179,17 @@ __device__ __forceinline__ bool finite(const float* s) {
   for (int v = 0; v < V; ++v) ok = ok && fabsf(s[v]) < INFINITY;
   return ok;
 }
-// s over some steps by go(s, safe): the plain sums, and again from s where they leave
-// fp32's range.
-template <int V, typename Go>
-__device__ __forceinline__ void over_all(float* s, const Go& go) {
-  float t[V];
+// A gate that is not a number leaves no state one, zero included.
+template <int V>
+__device__ __forceinline__ void poison(const float* A, float* H) {
 #pragma unroll
-  for (int v = 0; v < V; ++v) t[v] = s[v];
-  go(t, std::false_type());
-  if (!finite<V>(t)) {
-#pragma unroll
-    for (int v = 0; v < V; ++v) t[v] = s[v];
-    go(t, std::true_type());
-  }
-#pragma unroll
-  for (int v = 0; v < V; ++v) s[v] = t[v];
+  for (int v = 0; v < V; ++v)
+    if (A[v] != A[v]) H[v] = A[v];
 }
 // (A, H) of two runs of steps, one behind the other.  A product past fp32's range is not
 // carried over a new start, on either side of it.
-template <bool SAFE>
 __device__ __forceinline__ float2 join(float2 first, float2 then) {
-  const float A = first.x * then.x;
-  return make_float2(SAFE && A != A && (first.x == 0.0f || then.x == 0.0f) ? 0.0f : A,
-                     over<SAFE>(then.x, first.y, then.y));
+  return make_float2(then.x == 0.0f || first.x == 0.0f ? 0.0f : first.x * then.x, over(then.x, first.y, then.y));
 }
 
 // A thread's S steps of V channels.  Those from n on do not exist: a = 1, u = 0 (FULL:
@@ -467,9 +452,8 @@ __device__ __forceinline__ void show(unsigned* p, float f) {
   if (v == kNone) v = 0x7fffffffu;
   asm volatile("st.relaxed.gpu.global.b32 [%0], %1;" ::"l"(p), "r"(v) : "memory");
 }
-template <bool SAFE>
 __device__ __forceinline__ float fold(unsigned long long f, float s) {
-  return over<SAFE>(__uint_as_float((unsigned)f), s, __uint_as_float((unsigned)(f >> 32)));
+  return over(__uint_as_float((unsigned)f), s, __uint_as_float((unsigned)(f >> 32)));
 }
 
 // A wait's polls (see tc_common.cuh): false once it has to give up.
@@ -530,17 +514,14 @@ __device__ __forceinline__ void look_back(const unsigned long long* sum, const u
       f[k][0] = kNone2;
       if (m + k < q) look_at<V>(sum + (size_t)(m + k) * CH, f[k]);
     }
-    int n;
-    over_all<V>(s, [&](float* t, auto safe) {
-      n = 0;
+    int n = 0;
 #pragma unroll
-      for (int k = 0; k < N; ++k)
-        if (n == k && there<V>(f[k])) {
+    for (int k = 0; k < N; ++k)
+      if (n == k && there<V>(f[k])) {
 #pragma unroll
-          for (int v = 0; v < V; ++v) t[v] = fold<decltype(safe)::value>(f[k][v], t[v]);
-          n = k + 1;
-        }
-    });
+        for (int v = 0; v < V; ++v) s[v] = fold(f[k][v], s[v]);
+        n = k + 1;
+      }
     m += n;
     if (n == 0) {
       do {
@@ -622,13 +603,11 @@ __device__ __forceinline__ void fold_tiles(const Job& j, Exchange<32 * V>& ex, P
 #pragma unroll
           for (int v = 0; v < V; ++v)
             if (z0 + z < at.q) f[z][v] = load_of(&ex.whole[0][ch + v], z0 + z);
-        over_all<V>(s, [&](float* t, auto safe) {
 #pragma unroll
-          for (int z = 0; z < 8; ++z)
+        for (int z = 0; z < 8; ++z)
 #pragma unroll
-            for (int v = 0; v < V; ++v)
-              if (z0 + z < at.q) t[v] = over<decltype(safe)::value>(f[z][v].x, t[v], f[z][v].y);
-        });
+          for (int v = 0; v < V; ++v)
+            if (z0 + z < at.q) s[v] = over(f[z][v].x, s[v], f[z][v].y);
       }
     }
 #pragma unroll
@@ -650,7 +629,7 @@ __device__ __forceinline__ void fold_tiles(const Job& j, Exchange<32 * V>& ex, P
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       const float2 f = ex.whole[k][ch + v];
-      if (at.q + 1 < j.tiles) show(j.state + tile0 + (size_t)at.q * CH + v, over<true>(f.x, s[v], f.y));
+      if (at.q + 1 < j.tiles) show(j.state + tile0 + (size_t)at.q * CH + v, over(f.x, s[v], f.y));
       ex.enter[k][ch + v] = s[v];
     }
     if (threadIdx.x == kRun) ex.place[k] = last;
@@ -666,18 +645,13 @@ template <int CH, bool BACK>
 __device__ __forceinline__ void join_parts(const Job& j, Exchange<CH>& ex, const Place& at, int k) {
   const int ch = threadIdx.x;
   if (ch < CH) {
-    float2 f;
-    auto go = [&](auto safe) {
-      f = make_float2(1.0f, 0.0f);
+    float2 f = make_float2(1.0f, 0.0f);
 #pragma unroll
-      for (int i = 0; i < kParts; ++i) {
-        const int p = BACK ? kParts - 1 - i : i;
-        ex.before[k][p][ch] = f;
-        f = i ? join<decltype(safe)::value>(f, ex.sum[p][ch]) : ex.sum[p][ch];
-      }
-    };
-    go(std::false_type());
-    if (!finite<2>(&f.x)) go(std::true_type());
+    for (int i = 0; i < kParts; ++i) {
+      const int p = BACK ? kParts - 1 - i : i;
+      ex.before[k][p][ch] = f;
+      f = i ? join(f, ex.sum[p][ch]) : ex.sum[p][ch];
+    }
     ex.whole[k][ch] = f;
     if (j.tickets) {
       if (at.q > 0 && at.q + 1 < j.tiles) show(j.sum + ((size_t)at.stream * j.tiles + at.q) * CH + ch, f);
@@ -692,7 +666,7 @@ __device__ __forceinline__ void enter_part(const Exchange<32 * V>& ex, int k, in
 #pragma unroll
   for (int v = 0; v < V; ++v) {
     const float2 f = ex.before[k][part][at + v];
-    s[v] = over<true>(f.x, ex.enter[k][at + v], f.y);
+    s[v] = over(f.x, ex.enter[k][at + v], f.y);
   }
 }
 
@@ -800,6 +774,7 @@ __global__ void __launch_bounds__(kRun + 32, kBlocks) k_scan_fwd(const __grid_co
     if (!finite<V>(H) || !finite<V>(A)) {
       P::template product<true>(a, A);
       P::template forward<true>(a, u, H);
+      poison<V>(A, H);
     }
 #pragma unroll
     for (int v = 0; v < V; ++v) ex.sum[part][lane * V + v] = make_float2(A[v], H[v]);
@@ -907,10 +882,14 @@ __global__ void __launch_bounds__(kRun + 32, kBlocks) k_scan_bwd(const __grid_co
     if (!finite<V>(H) || !finite<V>(A)) {
       P::template product<true>(a, A);
       P::template run_over<true, KIND>(a, bb, y, H, true);
+      poison<V>(A, H);
     }
     above(n, slot, dh);
     P::template backward<false>(a, dh, G);
-    if (!finite<V>(G)) P::template backward<true>(a, dh, G);
+    if (!finite<V>(G) || !finite<V>(A)) {
+      P::template backward<true>(a, dh, G);
+      poison<V>(A, G);
+    }
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       ex.sum[part][lane * V + v] = make_float2(A[v], G[v]);
@@ -919,13 +898,11 @@ __global__ void __launch_bounds__(kRun + 32, kBlocks) k_scan_bwd(const __grid_co
     meet(SUMS, kRun);
     join_parts<CH, true>(j, ex, p, k);
     if (own < CH) {
-      over_all<1>(&before, [&](float* t, auto safe) {
 #pragma unroll
-        for (int i = 0; i < per; ++i) {
-          run_enter[k][p0 + i][own] = *t;
-          *t = over<decltype(safe)::value>(ex.sum[p0 + i][own].x, *t, run[p0 + i][own]);
-        }
-      });
+      for (int i = 0; i < per; ++i) {
+        run_enter[k][p0 + i][own] = before;
+        before = over(ex.sum[p0 + i][own].x, before, run[p0 + i][own]);
+      }
     }
   };
   Place then = ex.start[1], later = ex.start[2];
