@@ -19,8 +19,8 @@
 // tile's sums are given away before this one's state is waited for: its wait lies under
 // the running warps' work (1 x 65536 x 512 fp32 forward: 120 us with the next tile's
 // sums behind it, 87 before it).  Inputs come by asynchronous copies two tiles ahead, and
-// their gates are computed again for the second pass, from shared memory: registers for
-// two tiles would leave room for one block an SM.
+// their gates are computed again for the second pass, from shared memory (fp32: left there by
+// the first): registers for two tiles would leave room for one block an SM.
 //
 // Measured: 1 x 65536 x 512 fp32 forward 80 us (5.0 TB/s of inputs and outputs; 190 us
 // with all of a sequence's tiles in one cluster's rounds), 8 x 4096 x 512 bf16 step with
@@ -122,20 +122,54 @@ __device__ __forceinline__ float reciprocal(float x) {
   return y;
 }
 
-template <int KIND> struct Gate {
-  // a, and b with u = b x.  The exponential is 2^(g log2 e): off by 2^-22, and by
-  // 1.25 |g| 2^-24 from its argument's rounding.
-  static __device__ __forceinline__ void split(float g, float& a, float& b) {
-    constexpr float log2e = 1.44269504f;
+// A gate multiplies the state at every step, and a state that lasts m steps has its error
+// m times over.  So a gate near 1 is rounded once: LOG gates by the exponential's series,
+// the larger of sigmoid(g) and sigmoid(-g) as 1 less the smaller.  (2^x of the MUFU unit is
+// off by up to 2 units of 2^-24, low by 0.1 to 0.5 on average.)
+template <typename T, int KIND> struct Gate {
+  static constexpr bool WIDE = sizeof(T) == 4;
+  // e^g as 2^(g log2 e), zero below 2^-126.  bf16 inputs: off by 2^-22, and by 1.25 |g|
+  // 2^-24 from its argument's rounding, which fp32 inputs have back.
+  static __device__ __forceinline__ float exponential(float g) {
+    constexpr float log2e = 1.44269504f, ln2 = 0.69314718f;
+    if (!WIDE) return tc::ex2_approx(log2e * g);
+    asm("max.NaN.f32 %0, %0, 0fC3480000;" : "+f"(g));  // -200: an infinity has no remainder
+    const float t = log2e * g, e = tc::ex2_approx(t);
+    return fmaf(e, fmaf(-t, ln2, g), e);
+  }
+  // a, or of a sigmoid the smaller of a and b.
+  static __device__ __forceinline__ float first(float g) {
     if (KIND == SLIM_GATE_SIGMOID) {
-      // sigmoid(g) and sigmoid(-g), each to its own digits
-      const float e = tc::ex2_approx(-log2e * g);
-      a = reciprocal(1.0f + e);
-      b = g < 0.0f ? 1.0f - a : e * a;
-    } else {
-      a = KIND == SLIM_GATE_LOG ? tc::ex2_approx(log2e * g) : g;
-      b = 1.0f;
+      const float e = exponential(-fabsf(g));
+      return e * reciprocal(1.0f + e);
     }
+    if (KIND == SLIM_GATE_LOG) {
+      // up to g^5 / 5! for |g| < 2^-3, the rest below 2^-27; bf16: up to g^3 / 3! for
+      // |g| < 2^-6, the rest below 2^-28
+      constexpr float near = WIDE ? 0x1p-3f : 0x1p-6f;
+      float p = WIDE ? fmaf(g, fmaf(g, 1.0f / 120.0f, 1.0f / 24.0f), 1.0f / 6.0f) : 1.0f / 6.0f;
+      p = fmaf(g, fmaf(g, p, 0.5f), 1.0f);
+      return fabsf(g) < near ? fmaf(g, p, 1.0f) : exponential(g);
+    }
+    return g;
+  }
+  // a, and b with u = b x.
+  static __device__ __forceinline__ void both(float v, bool low, float& a, float& b) {
+    const float large = 1.0f - v;
+    a = KIND != SLIM_GATE_SIGMOID || low ? v : large;
+    b = KIND != SLIM_GATE_SIGMOID ? 1.0f : low ? large : v;
+  }
+  static __device__ __forceinline__ void split(float g, float& a, float& b) { both(first(g), g < 0.0f, a, b); }
+  // fp32: what is held of a gate for the second pass, in its own room, and from there: a,
+  // or the smaller sigmoid with the sign of -g.
+  static __device__ __forceinline__ float hold(float g) {
+    return KIND == SLIM_GATE_SIGMOID ? copysignf(first(g), -g) : first(g);
+  }
+  static __device__ __forceinline__ void open(float held, float& a, float& b) {
+    if (KIND == SLIM_GATE_SIGMOID)
+      both(fabsf(held), __float_as_int(held) >= 0, a, b);
+    else
+      both(held, true, a, b);
   }
   static __device__ __forceinline__ float u(float b, float x) {
     return KIND == SLIM_GATE_SIGMOID ? b * x : x;
@@ -207,12 +241,22 @@ template <typename T, int V, int S> struct Steps {
 #pragma unroll
     for (int i = 0; i < S; ++i) r[i] = slot[i * 32];
   }
+  // Gates: the first pass leaves the second what is held of them.
+  template <int KIND, bool FIRST>
+  static __device__ __forceinline__ void take_gates(R* slot, R* r) {
+    take(slot, r);
+    if constexpr (FIRST && sizeof(T) == 4 && KIND != SLIM_GATE_VALUE) {
+#pragma unroll
+      for (int i = 0; i < S; ++i) slot[i * 32] = r[i] = Gate<T, KIND>::hold(r[i]);
+    }
+  }
   static __device__ __forceinline__ void store(T* p, const float* v) {
     R r;
     pack(v, r);
     *reinterpret_cast<R*>(p) = r;
   }
-  template <int KIND, bool FULL>
+  // HELD: of what take_gates left
+  template <int KIND, bool FULL, bool HELD>
   static __device__ __forceinline__ void gates(const R* g, int n, float (*a)[V], float (*b)[V]) {
 #pragma unroll
     for (int i = 0; i < S; ++i) {
@@ -220,7 +264,10 @@ template <typename T, int V, int S> struct Steps {
       unpack(g[i], f);
 #pragma unroll
       for (int v = 0; v < V; ++v) {
-        Gate<KIND>::split(f[v], a[i][v], b[i][v]);
+        if (HELD && sizeof(T) == 4)
+          Gate<T, KIND>::open(f[v], a[i][v], b[i][v]);
+        else
+          Gate<T, KIND>::split(f[v], a[i][v], b[i][v]);
         if (!FULL && i >= n) {
           a[i][v] = 1.0f;
           b[i][v] = 0.0f;
@@ -232,9 +279,9 @@ template <typename T, int V, int S> struct Steps {
   template <int KIND>
   static __device__ __forceinline__ void gates_of(const R* g, int n, float (*a)[V], float (*b)[V]) {
     if (n == S)
-      gates<KIND, true>(g, n, a, b);
+      gates<KIND, true, true>(g, n, a, b);
     else
-      gates<KIND, false>(g, n, a, b);
+      gates<KIND, false, true>(g, n, a, b);
   }
   static __device__ __forceinline__ void values_of(const R* g, int n, float (*x)[V]) {
     if (n == S)
@@ -315,9 +362,9 @@ template <typename T, int V, int S> struct Steps {
                                                   float* s, bool zero) {
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-      float t = zero ? Gate<KIND>::u(b[0][v], x[0][v]) : next<SAFE>(a[0][v], s[v], Gate<KIND>::u(b[0][v], x[0][v]));
+      float t = zero ? Gate<T, KIND>::u(b[0][v], x[0][v]) : next<SAFE>(a[0][v], s[v], Gate<T, KIND>::u(b[0][v], x[0][v]));
 #pragma unroll
-      for (int i = 1; i < S; ++i) t = next<SAFE>(a[i][v], t, Gate<KIND>::u(b[i][v], x[i][v]));
+      for (int i = 1; i < S; ++i) t = next<SAFE>(a[i][v], t, Gate<T, KIND>::u(b[i][v], x[i][v]));
       s[v] = t;
     }
   }
@@ -331,8 +378,8 @@ template <typename T, int V, int S> struct Steps {
 #pragma unroll
       for (int i = 0; i < S; ++i) {
         const float before = t;
-        if (i + 1 < S) t = next<SAFE>(a[i][v], t, Gate<KIND>::u(b[i][v], x[i][v]));
-        x[i][v] = Gate<KIND>::factor(a[i][v], b[i][v], before, x[i][v]);
+        if (i + 1 < S) t = next<SAFE>(a[i][v], t, Gate<T, KIND>::u(b[i][v], x[i][v]));
+        x[i][v] = Gate<T, KIND>::factor(a[i][v], b[i][v], before, x[i][v]);
       }
     }
   }
@@ -348,8 +395,8 @@ template <typename T, int V, int S> struct Steps {
 #pragma unroll
       for (int v = 0; v < V; ++v) {
         g[v] = i == S - 1 ? __fadd_rn(dh[i][v], r[v]) : next<SAFE>(a[i + 1][v], g[v], dh[i][v]);
-        dg[v] = Gate<KIND>::template grad<SAFE>(g[v], a[i][v], factor[i][v]);
-        dx[v] = Gate<KIND>::u(b[i][v], g[v]);
+        dg[v] = Gate<T, KIND>::template grad<SAFE>(g[v], a[i][v], factor[i][v]);
+        dx[v] = Gate<T, KIND>::u(b[i][v], g[v]);
       }
       if (FULL || i < n) {
         store(pg + i * g_pitch, dg);
@@ -754,21 +801,21 @@ __global__ void __launch_bounds__(kRun + 32, kBlocks) k_scan_fwd(const __grid_co
                         mine + (2 * k + 1) * S * 32);
     fetched();
   };
-  auto inputs = [&](int n, int k, float (*a)[V], float (*u)[V]) {
+  auto inputs = [&](auto first, int n, int k, float (*a)[V], float (*u)[V]) {
     float bb[S][V];
     R in[S];
-    P::take(mine + 2 * k * S * 32 + lane, in);
+    P::template take_gates<KIND, decltype(first)::value>(mine + 2 * k * S * 32 + lane, in);
     P::template gates_of<KIND>(in, n, a, bb);
     P::take(mine + (2 * k + 1) * S * 32 + lane, in);
     P::values_of(in, n, u);
 #pragma unroll
     for (int i = 0; i < S; ++i)
 #pragma unroll
-      for (int v = 0; v < V; ++v) u[i][v] = Gate<KIND>::u(bb[i][v], u[i][v]);
+      for (int v = 0; v < V; ++v) u[i][v] = Gate<T, KIND>::u(bb[i][v], u[i][v]);
   };
   auto sums = [&](const Place& p, int slot, int k) {
     float a[S][V], u[S][V], A[V], H[V];
-    inputs(steps_of(p), slot, a, u);
+    inputs(std::true_type(), steps_of(p), slot, a, u);
     P::template product<false>(a, A);
     P::template forward<false>(a, u, H);
     if (!finite<V>(H) || !finite<V>(A)) {
@@ -800,7 +847,7 @@ __global__ void __launch_bounds__(kRun + 32, kBlocks) k_scan_fwd(const __grid_co
     const int n = steps_of(at), c = at.c0 + lane * V;
     if (n > 0 && c < j.D) {
       float a[S][V], u[S][V], h[V];
-      inputs(n, slot, a, u);
+      inputs(std::false_type(), n, slot, a, u);
       enter_part<V>(ex, k, part, lane * V, h);
       const int t0 = at.q * kTile + part * S;
       if (j.kept && t0 % kChunk == 0)
@@ -854,9 +901,9 @@ __global__ void __launch_bounds__(kRun + 32, kBlocks) k_scan_bwd(const __grid_co
                         mine + (3 * k + 2) * S * 32);
     fetched();
   };
-  auto front = [&](int n, int k, float (*a)[V], float (*bb)[V], float (*y)[V]) {
+  auto front = [&](auto first, int n, int k, float (*a)[V], float (*bb)[V], float (*y)[V]) {
     R in[S];
-    P::take(mine + 3 * k * S * 32 + lane, in);
+    P::template take_gates<KIND, decltype(first)::value>(mine + 3 * k * S * 32 + lane, in);
     P::template gates_of<KIND>(in, n, a, bb);
     P::take(mine + (3 * k + 1) * S * 32 + lane, in);
     P::values_of(in, n, y);
@@ -876,7 +923,7 @@ __global__ void __launch_bounds__(kRun + 32, kBlocks) k_scan_bwd(const __grid_co
     float before = start_of(p);
     const int n = steps_of(p);
     float a[S][V], bb[S][V], y[S][V], dh[S][V], A[V], H[V], G[V];
-    front(n, slot, a, bb, y);
+    front(std::true_type(), n, slot, a, bb, y);
     P::template product<false>(a, A);
     P::template run_over<false, KIND>(a, bb, y, H, true);
     if (!finite<V>(H) || !finite<V>(A)) {
@@ -924,7 +971,7 @@ __global__ void __launch_bounds__(kRun + 32, kBlocks) k_scan_bwd(const __grid_co
     const int n = steps_of(at), c = at.c0 + lane * V, t0 = first_of(at);
     if (n > 0 && c < j.D) {
       float a[S][V], bb[S][V], y[S][V], e[V], h[V];
-      front(n, slot, a, bb, y);
+      front(std::false_type(), n, slot, a, bb, y);
       enter_part<V>(ex, k, part, lane * V, e);
 #pragma unroll
       for (int v = 0; v < V; ++v) h[v] = run_enter[k][part][lane * V + v];
@@ -968,19 +1015,19 @@ __global__ void __launch_bounds__(128) k_scan_short(const __grid_constant__ Job 
 #pragma unroll
     for (int v = 0; v < V; ++v) h[v] = j.start[b * j.D + c + v];
     float a[S][V], bb[S][V], y[S][V];
-    P::template gates<KIND, false>(g, n, a, bb);
+    P::template gates<KIND, false, false>(g, n, a, bb);
     P::template values<false>(x, n, y);
     P::template run_back<KIND>(static_cast<T*>(j.dgate) + row * j.dgate_pitch + c, j.dgate_pitch,
                                static_cast<T*>(j.dx) + row * j.dx_pitch + c, j.dx_pitch, n, a, bb, y, h, s,
                                [&](float (*dh)[V]) { P::template values<false>(up, n, dh); });
   } else {
     float a[S][V], bb[S][V], y[S][V];
-    P::template gates<KIND, false>(g, n, a, bb);
+    P::template gates<KIND, false, false>(g, n, a, bb);
     P::template values<false>(x, n, y);
 #pragma unroll
     for (int k = 0; k < S; ++k)
 #pragma unroll
-      for (int v = 0; v < V; ++v) y[k][v] = Gate<KIND>::u(bb[k][v], y[k][v]);
+      for (int v = 0; v < V; ++v) y[k][v] = Gate<T, KIND>::u(bb[k][v], y[k][v]);
     if (j.kept)
 #pragma unroll
       for (int v = 0; v < V; ++v) j.kept[b * j.D + c + v] = s[v];
