@@ -68,8 +68,8 @@ struct Job {
   int groups, tiles;   // of a sequence
   bool wide;           // inputs' rows come in 16-byte pieces
   long long streams;   // B groups
+  int* err;            // the header of a workspace, where there is one
   // LOOK (else null)
-  int* err;            // the workspace's header
   unsigned long long* tickets;
   unsigned long long* sum;  // [streams][tiles][CH]
   unsigned* state;
@@ -735,6 +735,7 @@ __device__ __forceinline__ Place begin(const Job& j, Exchange<CH>& ex) {
     if (j.tickets) {
       for (int i = 0; i < 3; ++i) ex.start[i] = next_place<CH>(j);
     } else {
+      if (j.err && blockIdx.x == 0) *j.err = 0;
       ex.start[0] = place_of<CH>(j, blockIdx.x / cluster_blocks(), (int)cluster_rank());
       ex.start[1] = ex.start[2] = ex.place[0] = Place{0, 0, -1, 0};
     }
@@ -1184,6 +1185,8 @@ slim_status run(Job& j, slim_dtype dtype, slim_gate kind, int together, bool bwd
     if (reinterpret_cast<uintptr_t>(workspace) & 255) return SLIM_ERR_INVALID_ARG;
     const slim_status st = report::begin(workspace, true, &call.rep);
     if (st != SLIM_OK) return st;
+    // (a direction that does not look back clears the error word, too)
+    j.err = static_cast<int*>(workspace);
   } else if (workspace) {
     const slim_status st = report::pending(workspace);
     if (st != SLIM_OK) return st;
