@@ -58,7 +58,7 @@ typedef struct {
  * whose squares pass fp32's range is normalised all the same; a row that holds
  * an infinity or NaN becomes NaN, and no other.
  * 0 <= B, L and B L < 2^31; Hq >= 1; Hq, Hk <= 4096; 1 <= d <= 256; rotary even,
- * 0 <= rotary <= d; eps > 0 and finite; B L (Hq + Hk) <= 2^40; strides in [0, 2^40],
+ * 0 <= rotary <= d; 0 < eps <= 1e38; B L (Hq + Hk) <= 2^40; strides in [0, 2^40],
  * offsets below 2^60.  B L = 0 enqueues nothing.
  */
 slim_status slim_qk_norm_fwd(const void* q, const slim_strides* q_strides, const void* k,

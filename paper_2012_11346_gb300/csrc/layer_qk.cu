@@ -39,6 +39,7 @@ constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kMaxD = 256, kMaxPairs = kMaxD / 2;
 constexpr int kMaxTokens = 16;       // of a tile
 constexpr int kMaxHeads = 4096;
+constexpr float kMaxEps = 1e38f;     // beside a mean square below 1e38 still in range
 constexpr int kBwdBlocks = 152 * 3;  // most that are resident; the workspace is for as many
 
 struct Side {
@@ -275,13 +276,13 @@ __global__ void __launch_bounds__(kThreads, BWD ? bwd_blocks(W) : 3) k_qk_norm(c
       float ss = over_lanes(R::dot(x, x), G);
       float fit = 1.0f;
       if (__any_sync(0xffffffffu, !(ss <= 1e38f))) {
-        // squares past fp32's range: the row in smaller units, next to which eps is nothing
+        // squares past fp32's range: the row, and eps by their square, in smaller units
         if (!(ss <= 1e38f)) fit = 0x1p-80f;
 #pragma unroll
         for (int i = 0; i < N; ++i) x[i] *= fit;
         ss = over_lanes(R::dot(x, x), G);
       }
-      const float rms = rsqrtf(fmaf(ss, over_d, j.eps * (fit * fit)));
+      const float rms = rsqrtf(fmaf(ss, over_d, j.eps * fit * fit));
 #pragma unroll
       for (int i = 0; i < N; ++i) x[i] *= rms;
       if constexpr (!BWD) {
@@ -530,7 +531,7 @@ int set_up(Job* j, const Operand q[3], const Operand k[3], bool bwd, const float
   if (!sizes_ok(B, Hq, Hk, L, d) || (dtype != SLIM_F32 && dtype != SLIM_BF16)) return -1;
   if (rotary < 0 || rotary > d || (rotary & 1) || (interleaved & ~1)) return -1;
   if (rotary > 0 && (!inv_freq || (ptype != SLIM_I32 && ptype != SLIM_I64))) return -1;
-  if (!(eps > 0.0f) || !isfinite(eps) || !isfinite(scale)) return -1;
+  if (!(eps > 0.0f) || !(eps <= kMaxEps) || !isfinite(scale)) return -1;
   for (int p = 0; p < rotary / 2; ++p) {
     if (!isfinite(inv_freq[p])) return -1;
     double turn = inv_freq[p] * 0.15915494309189533577;

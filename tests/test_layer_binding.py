@@ -1,6 +1,7 @@
 """What the differentiable calls around the attention hand to the library's entry points:
 host-only, with stand-ins in the entry points' place."""
 import array
+import os
 
 import pytest
 import torch
@@ -36,3 +37,13 @@ def test_both_directions_turn_alike(qk_calls, form):
         freq[0] = 7.0
     out.sum().backward()
     assert [c["inv_freq"] for c in qk_calls] == [[1.0, 0.5]] * 2
+
+
+def test_an_eps_past_the_range_is_refused():
+    if not os.path.exists(slim._LIB_PATH):
+        from paper_2012_11346_gb300 import build
+        build.build()
+    one = array.array("d", [1.0]).buffer_info()[0]
+    for eps, status in ((1e38, 0), (1.1e38, 1), (3e38, 1)):  # no rows: nothing is enqueued
+        assert slim.library().slim_qk_norm_fwd(None, None, None, None, None, None, None, 0, one, 2, 0, 0, 1, 1, 3, 4, 0,
+                                               eps, 1.0, None, None, None, None, None) == status
