@@ -1168,12 +1168,18 @@ def _even_rows(t):
         return t.contiguous()
 
 
+def _wants_gradients(*ts):
+    """Whether a differentiable call is recorded (a Function's ctx.needs_input_grad goes by
+    its inputs alone, under torch.no_grad, too)."""
+    return torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in ts)
+
+
 class GatedScan(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, gate, x, kind, h0):
-        h, last, kept = gated_scan_forward(_even_rows(gate), _even_rows(x), kind,
-                                           None if h0 is None else h0.contiguous(), keep=True)
-        ctx.save_for_backward(gate, x, h0, kept)
+    def forward(ctx, gate, x, kind, h0, keep):
+        h, last, *kept = gated_scan_forward(_even_rows(gate), _even_rows(x), kind,
+                                            None if h0 is None else h0.contiguous(), keep=keep)
+        ctx.save_for_backward(gate, x, h0, *kept)
         ctx.kind = kind
         return h, last
 
@@ -1185,13 +1191,13 @@ class GatedScan(torch.autograd.Function):
         if h0 is None:
             grads = grads[:2]
         tied = _first_derivatives(grads, *(t for t in (gate, x, h0, dh, dlast) if t is not None))
-        return tied[0], tied[1], None, (tied[2] if h0 is not None else None)
+        return tied[0], tied[1], None, (tied[2] if h0 is not None else None), None
 
 
 def gated_scan(gate, x, kind="sigmoid", h0=None):
     """Differentiable (once) gated_scan_forward: returns (h, last), with gradients with
     respect to gate, x and h0."""
-    return GatedScan.apply(gate, x, kind, h0)
+    return GatedScan.apply(gate, x, kind, h0, _wants_gradients(gate, x, h0))
 
 
 ACTIVATIONS = {"silu": 0, "gelu": 1, "gelu_tanh": 2, "relu": 3, "sigmoid": 4}
@@ -1291,10 +1297,9 @@ def gated_ff_backward(x, w, dh, act="silu", z=None, workspace=None, stream=None)
 
 class GatedFeedForward(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x_in, w_in, act):
+    def forward(ctx, x_in, w_in, act, keep):
         x, w = _ready(x_in), _ready(w_in)
-        h, z = gated_ff_forward(x, w, act, keep=True) if any(ctx.needs_input_grad) else (
-            gated_ff_forward(x, w, act), None)
+        h, z = gated_ff_forward(x, w, act, keep=True) if keep else (gated_ff_forward(x, w, act), None)
         ctx.save_for_backward(x_in, w_in, x, w, z)
         ctx.act = act
         return h
@@ -1303,10 +1308,10 @@ class GatedFeedForward(torch.autograd.Function):
     def backward(ctx, dh):
         x_in, w_in, x, w, z = ctx.saved_tensors
         grads = gated_ff_backward(x, w, _ready(dh), ctx.act, z=z)
-        return *_first_derivatives(grads, x_in, w_in, dh), None
+        return *_first_derivatives(grads, x_in, w_in, dh), None, None
 
 
 def gated_ff(x, w, act="silu"):
-    """Differentiable (once) gated_ff_forward: gradients with respect to x and w.  fp32
-    keeps both projections (8 F bytes a row) for its backward."""
-    return GatedFeedForward.apply(x, w, act)
+    """Differentiable (once) gated_ff_forward: gradients with respect to x and w.  Where one
+    is wanted, fp32 keeps both projections (8 F bytes a row) for the backward."""
+    return GatedFeedForward.apply(x, w, act, _wants_gradients(x, w))

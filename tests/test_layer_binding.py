@@ -47,3 +47,37 @@ def test_an_eps_past_the_range_is_refused():
     for eps, status in ((1e38, 0), (1.1e38, 1), (3e38, 1)):  # no rows: nothing is enqueued
         assert slim.library().slim_qk_norm_fwd(None, None, None, None, None, None, None, 0, one, 2, 0, 0, 1, 1, 3, 4, 0,
                                                eps, 1.0, None, None, None, None, None) == status
+
+
+@pytest.fixture
+def kept(monkeypatch):
+    """What each forward was asked to keep."""
+    asked = []
+
+    def ff(x, w, act="silu", keep=False):
+        asked.append(keep)
+        h = x.new_zeros(*x.shape[:-1], w.shape[0] // 2)
+        return (h, None) if keep else h
+
+    def scan(gate, x, kind="sigmoid", h0=None, keep=False):
+        asked.append(keep)
+        out = (x.clone(), x[:, -1].float().clone())
+        return (*out, torch.zeros(1)) if keep else out
+
+    monkeypatch.setattr(slim, "gated_ff_forward", ff)
+    monkeypatch.setattr(slim, "gated_scan_forward", scan)
+    return asked
+
+
+@pytest.mark.parametrize("recorded", [False, True])
+@pytest.mark.parametrize("needed", [False, True])
+def test_nothing_is_kept_for_a_gradient_that_is_not_wanted(kept, recorded, needed):
+    """Neither under no_grad with parameters that require gradients nor without any."""
+    x, w, gate = torch.randn(4, 8), torch.randn(12, 8), torch.randn(1, 4, 8)
+    w.requires_grad_(needed)
+    gate.requires_grad_(needed)
+    with torch.set_grad_enabled(recorded):
+        h = slim.gated_ff(x, w)
+        states, last = slim.gated_scan(gate, x[None])
+    assert kept == [recorded and needed] * 2
+    assert h.requires_grad == states.requires_grad == last.requires_grad == (recorded and needed)
