@@ -1176,7 +1176,7 @@ def _wants_gradients(*ts):
 
 class GatedScan(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, gate, x, kind, h0, keep):
+    def forward(ctx, gate, x, kind, h0, keep=True):
         h, last, *kept = gated_scan_forward(_even_rows(gate), _even_rows(x), kind,
                                             None if h0 is None else h0.contiguous(), keep=keep)
         ctx.save_for_backward(gate, x, h0, *kept)
@@ -1297,7 +1297,7 @@ def gated_ff_backward(x, w, dh, act="silu", z=None, workspace=None, stream=None)
 
 class GatedFeedForward(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x_in, w_in, act, keep):
+    def forward(ctx, x_in, w_in, act, keep=True):
         x, w = _ready(x_in), _ready(w_in)
         h, z = gated_ff_forward(x, w, act, keep=True) if keep else (gated_ff_forward(x, w, act), None)
         ctx.save_for_backward(x_in, w_in, x, w, z)

@@ -81,3 +81,10 @@ def test_nothing_is_kept_for_a_gradient_that_is_not_wanted(kept, recorded, neede
         states, last = slim.gated_scan(gate, x[None])
     assert kept == [recorded and needed] * 2
     assert h.requires_grad == states.requires_grad == last.requires_grad == (recorded and needed)
+
+
+def test_the_functions_themselves_keep_unless_told(kept):
+    x, w = torch.randn(4, 8), torch.randn(12, 8, requires_grad=True)
+    slim.GatedFeedForward.apply(x, w, "silu")
+    slim.GatedScan.apply(x[None], x[None].clone().requires_grad_(), "log", None)
+    assert kept == [True, True]
