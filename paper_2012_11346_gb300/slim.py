@@ -1031,7 +1031,9 @@ class QkNorm(torch.autograd.Function):
 def qk_norm(q, k, q_weight=None, k_weight=None, positions=None, inv_freq=None, interleaved=False,
             eps=1e-6, scale=1.0):
     """Differentiable (once) qk_norm_forward: gradients with respect to q, k and the weights.
-    inv_freq is read once, for both directions."""
+    inv_freq is read once, for both directions; positions may be one row expanded."""
+    if positions is not None:
+        positions = positions.contiguous()
     return QkNorm.apply(q, k, q_weight, k_weight, positions, _frequencies(inv_freq), interleaved, eps, scale)
 
 

@@ -88,3 +88,11 @@ def test_the_functions_themselves_keep_unless_told(kept):
     slim.GatedFeedForward.apply(x, w, "silu")
     slim.GatedScan.apply(x[None], x[None].clone().requires_grad_(), "log", None)
     assert kept == [True, True]
+
+
+def test_positions_of_one_row_for_all(qk_calls):
+    q = torch.randn(2, 2, 3, 8, requires_grad=True)
+    slim.qk_norm(q, None, positions=torch.arange(3).expand(2, 3))[0].sum().backward()
+    for call in qk_calls:
+        assert call["positions"].is_contiguous() and call["positions"].tolist() == [[0, 1, 2]] * 2
+    assert len(qk_calls) == 2
