@@ -795,6 +795,7 @@ def _at(dev, stream):
     if stream is None:
         return _HERE if dev == torch._C._cuda_getDevice() else torch.cuda.device(dev)
     # (it makes the stream's device the current one, too)
+    _require(stream.device_index == dev, "the stream is on another device than the tensors")
     return torch.cuda.stream(stream)
 
 

@@ -2,6 +2,7 @@
 host-only, with stand-ins in the entry points' place."""
 import array
 import os
+import types
 
 import pytest
 import torch
@@ -96,3 +97,8 @@ def test_positions_of_one_row_for_all(qk_calls):
     for call in qk_calls:
         assert call["positions"].is_contiguous() and call["positions"].tolist() == [[0, 1, 2]] * 2
     assert len(qk_calls) == 2
+
+
+def test_a_stream_of_another_device_is_refused():
+    with pytest.raises(ValueError):
+        slim._at(0, types.SimpleNamespace(device_index=1))
