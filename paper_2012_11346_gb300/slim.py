@@ -986,6 +986,7 @@ def qk_norm_backward(q, k, q_weight, k_weight, dq_out, dk_out, positions=None, i
     if dk_out is not None:
         _, up_kp, up_ks, k_above = _qk_like(k, dk_out, "dk_out")
     if workspace is not None:
+        _device_of(q, workspace)
         _require_cuda(workspace)
     with _at(dev, stream):
         dq, qp, qs, q_strides = _qk_like(q, dq, "dq")
@@ -1256,7 +1257,7 @@ def gated_ff_forward(x, w, act="silu", keep=False, out=None, workspace=None, str
     "gelu_tanh", "relu", "sigmoid".  With keep=True returns (h, z), z being both
     projections in fp32 for gated_ff_backward, or None where computing them again is
     the quicker (bf16, and a few rows: see gated_ff_kept_size)."""
-    dev = _device_of(x, w, out)
+    dev = _device_of(x, w, out, workspace)
     _require_cuda(x, w)
     sizes = _ff_sizes(x.shape, w.shape, x.dtype, w.dtype, act, "gated_ff_forward")
     shape = (*x.shape[:-1], sizes[2])
@@ -1281,7 +1282,7 @@ def gated_ff_forward(x, w, act="silu", keep=False, out=None, workspace=None, str
 def gated_ff_backward(x, w, dh, act="silu", z=None, workspace=None, stream=None):
     """slim_gated_ff_bwd: returns (dx, dw), the gradients of <dh, h>.  z: from
     gated_ff_forward(..., keep=True) on the same inputs, or None."""
-    dev = _device_of(x, w, dh, z)
+    dev = _device_of(x, w, dh, z, workspace)
     _require_cuda(x, w, dh)
     sizes = _ff_sizes(x.shape, w.shape, x.dtype, w.dtype, act, "gated_ff_backward")
     if dh.shape != (*x.shape[:-1], sizes[2]) or dh.dtype != x.dtype:

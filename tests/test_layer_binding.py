@@ -102,3 +102,29 @@ def test_positions_of_one_row_for_all(qk_calls):
 def test_a_stream_of_another_device_is_refused():
     with pytest.raises(ValueError):
         slim._at(0, types.SimpleNamespace(device_index=1))
+
+
+class Elsewhere(torch.Tensor):
+    """A tensor that gives itself out as one of a GPU."""
+
+    @staticmethod
+    def on(t, index):
+        t = t.as_subclass(Elsewhere)
+        t.index = index
+        return t
+
+    is_cuda = True
+
+    def get_device(self):
+        return self.index
+
+
+def test_a_workspace_of_another_device_is_refused(monkeypatch):
+    monkeypatch.setattr(slim, "library", lambda: (_ for _ in ()).throw(AssertionError("reached")))
+    here = lambda *shape: Elsewhere.on(torch.zeros(*shape), 0)
+    x, w, h, q = here(4, 8), here(12, 8), here(4, 6), here(1, 2, 3, 8)
+    ws = Elsewhere.on(torch.zeros(1 << 20, dtype=torch.uint8), 1)
+    for call in (lambda: slim.gated_ff_forward(x, w, workspace=ws), lambda: slim.gated_ff_backward(x, w, h, workspace=ws),
+                 lambda: slim.qk_norm_backward(q, None, None, None, q, None, workspace=ws)):
+        with pytest.raises(ValueError, match="different devices"):
+            call()
