@@ -177,7 +177,7 @@ typedef enum {
  * piece by piece, six products each, smallest first, on the tensor cores (up to 8
  * rows, where that is quicker: fp32 FMA in either type).  h is rounded once.
  * Values are finite: an infinity in a row of x, or of w, makes what it enters
- * infinite or NaN.
+ * infinite or NaN.  Nothing written overlaps anything else, in either direction.
  * 0 <= N < 2^31 - 512, 1 <= D <= 2^30, 1 <= F <= 2^29, N F <= 2^45, N D and 2 F D
  * <= 2^40.  N = 0 enqueues nothing.
  *   workspace of slim_gated_ff_workspace_size(..., backward = 0) bytes; where that is

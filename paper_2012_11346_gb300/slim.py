@@ -1251,6 +1251,11 @@ def _ff_workspace(given, sizes, t, backward):
     return given, given.data_ptr(), given.numel()
 
 
+def _apart(a, b):
+    """Whether contiguous tensors share no memory."""
+    return a.data_ptr() + a.nbytes <= b.data_ptr() or b.data_ptr() + b.nbytes <= a.data_ptr()
+
+
 def gated_ff_forward(x, w, act="silu", keep=False, out=None, workspace=None, stream=None):
     """slim_gated_ff_fwd: act(x w_gate^T) * (x w_up^T) for x [..., D] and w [2F, D], its
     first F rows the gate's and the others up's; act one of "silu", "gelu",
@@ -1264,6 +1269,7 @@ def gated_ff_forward(x, w, act="silu", keep=False, out=None, workspace=None, str
     if out is not None:
         _require_cuda(out)
         _require(out.dtype == x.dtype and out.shape == shape, "out must be [..., F] in x's dtype")
+        _require(_apart(out, x) and _apart(out, w), "out must not share memory with x or w")
     if workspace is not None:
         _require_cuda(workspace)
     with _at(dev, stream):

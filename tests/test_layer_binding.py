@@ -128,3 +128,16 @@ def test_a_workspace_of_another_device_is_refused(monkeypatch):
                  lambda: slim.qk_norm_backward(q, None, None, None, q, None, workspace=ws)):
         with pytest.raises(ValueError, match="different devices"):
             call()
+
+
+def test_an_output_over_an_input_is_refused(monkeypatch):
+    """Its tiles are written while others still read the rows."""
+    monkeypatch.setattr(slim, "_device_of", lambda *t: 0)
+    monkeypatch.setattr(slim, "_require_cuda", lambda *t: None)
+    monkeypatch.setattr(slim, "_at", lambda dev, stream: slim._HERE)
+    monkeypatch.setattr(slim, "library", lambda: (_ for _ in ()).throw(AssertionError("reached")))
+    rows, w = torch.zeros(10, 8), torch.zeros(16, 8)
+    for out in (rows[:4], rows[2:6], rows[3:7], w[:4], w[12:]):
+        with pytest.raises(ValueError, match="share memory"):
+            slim.gated_ff_forward(rows[:4], w, out=out)
+    assert slim._apart(rows[:4], rows[4:]) and slim._apart(rows[4:], rows[:4])
