@@ -802,10 +802,17 @@ def _at(dev, stream):
 try:
     # (size, stride, dtype) on the current device, without the dispatcher: half of
     # torch.empty's time
-    from torch._C._dynamo.guards import _empty_strided_cuda as _allocate
+    from torch._C import _len_torch_dispatch_stack as _modes
+    from torch._C._dynamo.guards import _empty_strided_cuda as _undispatched
 except ImportError:
-    def _allocate(size, stride, dtype):
+    def _modes():
+        return 1
+
+
+def _allocate(size, stride, dtype):
+    if _modes():  # modes that watch the dispatcher see every tensor
         return torch.empty_strided(size, stride, dtype=dtype, device="cuda")
+    return _undispatched(size, stride, dtype)
 
 
 @functools.lru_cache(maxsize=1024)

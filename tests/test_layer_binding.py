@@ -141,3 +141,19 @@ def test_an_output_over_an_input_is_refused(monkeypatch):
         with pytest.raises(ValueError, match="share memory"):
             slim.gated_ff_forward(rows[:4], w, out=out)
     assert slim._apart(rows[:4], rows[4:]) and slim._apart(rows[4:], rows[:4])
+
+
+def test_modes_see_what_is_allocated(monkeypatch):
+    from torch.utils._python_dispatch import TorchDispatchMode
+
+    class Watching(TorchDispatchMode):
+        def __torch_dispatch__(self, func, types, args=(), kwargs=None):
+            return func(*args, **(kwargs or {}))
+
+    made = []
+    monkeypatch.setattr(torch, "empty_strided", lambda *a, **kw: made.append("dispatched"))
+    monkeypatch.setattr(slim, "_undispatched", lambda *a: made.append("undispatched"), raising=False)
+    slim._allocate((2,), (1,), torch.float32)
+    with Watching():
+        slim._allocate((2,), (1,), torch.float32)
+    assert made[1] == "dispatched" and made[0] == ("dispatched" if slim._modes() else "undispatched")
