@@ -154,6 +154,15 @@ slim_status slim_gated_scan_bwd(const void* gate, long long gate_pitch, const vo
                                 long long dx_pitch, float* dh0, void* workspace,
                                 size_t workspace_bytes, void* stream);
 
+/*
+ * Diagnostic: slim_gated_scan_fwd of one sequence (fp32, LOG, rows one behind the other)
+ * whose tiles look back through the workspace, but whose first tile nobody runs.  The wait
+ * for its state gives up after its limit (about a second), the kernel ends, and the failure
+ * is reported as above.  h holds nothing of use.  Sizes that need no waits are refused.
+ */
+slim_status slim_diag_gated_scan_wait(const float* gate, const float* x, int L, int D, float* h,
+                                      void* workspace, size_t workspace_bytes, void* stream);
+
 /* The activation of a gate. */
 typedef enum {
   SLIM_ACT_SILU = 0,      /* g sigmoid(g) */

@@ -718,12 +718,15 @@ __device__ __forceinline__ void enter_part(const Exchange<32 * V>& ex, int k, in
 }
 
 // ------------------------------------------------------------------ kernels
-// LOOK: clears the words that the scan's blocks wait for, and its header.
-__global__ void __launch_bounds__(256) k_scan_clear(int* header, uint4* words, long long n, unsigned* rep) {
+// LOOK: clears the words that the scan's blocks wait for, and its header; tickets begin
+// with `ticket`.
+__global__ void __launch_bounds__(256) k_scan_clear(int* header, uint4* words, long long n, unsigned* rep,
+                                                    unsigned long long ticket) {
   tc::grid_dependency_wait();
   const uint4 none = make_uint4(kNone, kNone, kNone, kNone);
   for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < n; i += (long long)gridDim.x * 256) words[i] = none;
-  if (blockIdx.x == 0 && threadIdx.x < kHeader && (threadIdx.x < 2 || threadIdx.x > 3)) header[threadIdx.x] = 0;
+  if (blockIdx.x == 0 && threadIdx.x < kHeader && (threadIdx.x < 2 || threadIdx.x > 5)) header[threadIdx.x] = 0;
+  if (blockIdx.x == 0 && threadIdx.x == 4) *reinterpret_cast<unsigned long long*>(header + 4) = ticket;
   if (blockIdx.x == 0 && threadIdx.x == 0) tc::set_report(header, rep);
 }
 
@@ -1088,6 +1091,7 @@ struct Call {
   void* workspace;
   unsigned* rep;
   cudaStream_t s;
+  bool lost;  // diagnostic: nobody runs the sequences' first tiles
 };
 
 template <typename T, int V, int KIND, bool BWD>
@@ -1114,7 +1118,7 @@ bool run_tiles(Job j, const Call& call) {
     prof::Scope ps(prof::K_SCAN_CLEAR, s);
     const long long n = (w.uint4s + 255) / 256;
     k_scan_clear<<<(unsigned)(n < 152 * 8 ? n : 152 * 8), 256, 0, s>>>(w.header, reinterpret_cast<uint4*>(w.sum),
-                                                                       w.uint4s, call.rep);
+                                                                       w.uint4s, call.rep, call.lost ? j.streams : 0);
     if (cudaGetLastError() != cudaSuccess) return false;
   } else if (j.tiles > 1) {
     z = j.tiles <= 8 ? j.tiles : kMaxCluster;
@@ -1174,8 +1178,8 @@ bool run_t(const Job& j, slim_gate kind, int together, const Call& call) {
 }
 // With arguments checked.
 slim_status run(Job& j, slim_dtype dtype, slim_gate kind, int together, bool bwd, void* workspace, size_t bytes,
-                cudaStream_t s) {
-  Call call{bwd, workspace, nullptr, s};
+                cudaStream_t s, bool lost = false) {
+  Call call{bwd, workspace, nullptr, s, lost};
   j.chunks = cdiv(j.L, kChunk);
   j.wide = together == (dtype == SLIM_F32 ? 4 : 8);
   size_t need = 0;
@@ -1304,4 +1308,23 @@ extern "C" slim_status slim_gated_scan_bwd(const void* gate, long long gate_pitc
   j.L = L;
   j.D = D;
   return run(j, dtype, kind, together, true, workspace, workspace_bytes, s);
+}
+
+extern "C" slim_status slim_diag_gated_scan_wait(const float* gate, const float* x, int L, int D, float* h,
+                                                 void* workspace, size_t workspace_bytes, void* stream) {
+  using namespace slim::layer;
+  if (!sizes_ok(1, L, D, SLIM_F32, SLIM_GATE_LOG) || !looks(1, L, D, SLIM_F32, false)) return SLIM_ERR_INVALID_ARG;
+  int together = 4;
+  while (D % together) together /= 2;
+  for (const Rows& r : {Rows{gate, D, false}, Rows{x, D, false}, Rows{h, D, true}})
+    if (!rows_ok(r, 1, L, D, 4, &together)) return SLIM_ERR_INVALID_ARG;
+  Job j{};
+  j.gate = gate;
+  j.x = x;
+  j.gate_pitch = j.x_pitch = j.D = D;
+  j.h = h;
+  j.B = 1;
+  j.L = L;
+  return run(j, SLIM_F32, SLIM_GATE_LOG, together, false, workspace, workspace_bytes,
+             static_cast<cudaStream_t>(stream), true);
 }

@@ -69,6 +69,7 @@ SIGNATURES = {
     "slim_gated_scan_fwd": ([_p, _ll, _p, _ll, _p] + [_i] * 5 + [_p] * 4 + [_sz, _p], _i),
     "slim_gated_scan_bwd": ([_p, _ll, _p, _ll] + [_p] * 3 + [_i] * 5 + [_p, _ll, _p, _ll, _p, _p, _sz, _p],
                             _i),
+    "slim_diag_gated_scan_wait": ([_p, _p, _i, _i, _p, _p, _sz, _p], _i),
     "slim_gated_ff_workspace_size": ([_ll, _i, _i, _i, _i, ctypes.POINTER(_sz)], _i),
     "slim_gated_ff_kept_size": ([_ll, _i, _i, _i, ctypes.POINTER(_sz)], _i),
     "slim_gated_ff_fwd": ([_p, _p, _ll] + [_i] * 4 + [_p, _p, _p, _sz, _p], _i),

@@ -157,3 +157,13 @@ def test_modes_see_what_is_allocated(monkeypatch):
     with Watching():
         slim._allocate((2,), (1,), torch.float32)
     assert made[1] == "dispatched" and made[0] == ("dispatched" if slim._modes() else "undispatched")
+
+
+def test_the_diagnostic_wait_refuses():
+    """Sizes without a wait, and what the forward refuses."""
+    call, ok = slim.library().slim_diag_gated_scan_wait, 0x10000
+    for L, D in ((8, 8), (2048, 8), (-1, 8), (5000, 0)):
+        assert call(ok, ok, L, D, ok, ok, 1 << 40, None) == 1
+    for a in ((None, ok, ok), (ok, None, ok), (ok, ok, None), (ok + 2, ok, ok)):
+        assert call(a[0], a[1], 5000, 8, a[2], ok, 1 << 40, None) == 1
+    assert call(ok, ok, 5000, 8, ok, None, 0, None) == 3

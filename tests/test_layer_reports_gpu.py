@@ -34,3 +34,26 @@ def test_no_failure_that_never_was(cuda_device, L):
         slim.gated_scan_forward(gate, x, "log", workspace=ws)
     slim.gated_scan_forward(gate, x, "log", workspace=ws)
     slim.check_device_error(ws)
+
+
+@pytest.mark.parametrize("L,D", [(2100, 36), (20000, 512)])
+def test_a_look_back_that_gives_up(cuda_device, L, D):
+    """The first tile's state is never there: all blocks come to their end, the next call
+    launches nothing and says so, and the one after it runs."""
+    gate, x = torch.zeros(2, 1, L, D, device=cuda_device)
+    gate -= 0.5
+    x += 1.0
+    want = slim.gated_scan_forward(gate, x, "log")
+    ws = torch.full((slim.gated_scan_workspace_size(1, L, D, F32),), 255, dtype=torch.uint8, device=cuda_device)
+    h = torch.full((L, D), 7.0, device=cuda_device)
+    args = (gate.data_ptr(), x.data_ptr(), L, D, h.data_ptr(), ws.data_ptr(), ws.numel(), stream())
+    assert slim.library().slim_diag_gated_scan_wait(*args) == 0
+    torch.cuda.synchronize()
+    assert (h[:128] == 7.0).all()  # the tile that nobody ran
+    before = slim.launch_count()
+    with pytest.raises(slim.SlimError) as e:
+        slim.gated_scan_forward(gate, x, "log", workspace=ws)
+    assert e.value.status == 5 and slim.launch_count() == before
+    got = slim.gated_scan_forward(gate, x, "log", workspace=ws)
+    slim.check_device_error(ws)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
