@@ -45,7 +45,7 @@ typedef struct {
  * the features (p, p + rotary/2), or (2p, 2p + 1) with `interleaved`.
  *   q [B, Hq, L, d], k [B, Hk, L, d] dtype, with the given strides (null:
  *   contiguous), aligned to their element size; slices of a projection's rows
- *   are read where they are, in 4-element pieces where pointers and strides
+ *   are read where they are, in pieces of up to 16 bytes where pointers and strides
  *   allow it.  Hk = 0: no keys (k, k_out and k_weight are not read).
  *   q_weight, k_weight  [d] fp32, or null (1).
  *   positions  [B, L] ptype, any value, aligned to its own size; null: l.
@@ -55,9 +55,10 @@ typedef struct {
  *   q_out, k_out  as q and k, no two elements in one place.  They may be q and k
  *              themselves, with the same strides.
  * Sums and turns are fp32, y is rounded once.  A row of zeros stays zero; a row
- * whose squares pass fp32's range is normalised all the same; a row that holds
- * an infinity or NaN becomes NaN, and no other.
- * 0 <= B, L and B L < 2^31; Hq >= 1; Hq, Hk <= 4096; 1 <= d <= 256; rotary even,
+ * whose squares pass fp32's range is normalised all the same; a row that holds a
+ * NaN becomes NaN; of a row that holds an infinity, that feature and the other of its
+ * pair become NaN and the rest zero (its gradient is NaN); no other row changes.
+ * 0 <= B, L and B L < 2^31 - 16; Hq >= 1; Hq, Hk <= 4096; 1 <= d <= 256; rotary even,
  * 0 <= rotary <= d; 0 < eps <= 1e38; B L (Hq + Hk) <= 2^40; strides in [0, 2^40],
  * offsets below 2^60.  B L = 0 enqueues nothing.
  */
@@ -205,8 +206,8 @@ slim_status slim_gated_ff_fwd(const void* x, const void* w, long long N, int D, 
  *   kept  from the forward on the same x and w, or null.
  * With g and u the projections, from kept or computed again here,
  *     dz = [dh u act'(g), dh act(g)],   dx = dz w,   dw = dz^T x.
- * dz is rounded once for the products: to bf16 for bf16 problems (2^-9 relative,
- * like the rounding of the gradients themselves), to three bf16 pieces for fp32
+ * dz is rounded once for the products: to bf16 for bf16 problems (by up to 2^-8 of
+ * itself, as the gradients themselves are), to three bf16 pieces for fp32
  * ones; the workspace holds it (2 N F elements of 2 or 6 bytes).  Sums are fp32, and
  * long ones are joined from parts; dx and dw are rounded once.  N = 0 zeroes dw.
  */

@@ -16,9 +16,9 @@
 // The weights' sums stay in registers while a block walks over its rows, leave
 // it once, and are joined over blocks in order by a second kernel.
 //
-// HBM bounds it: each row is read and written once.  Measured: 4 x 12+12 x 8192 x 64 fp32
-// backward 100 us, 6.0 TB/s; 8 x 8+8 x 4096 x 64 bf16 forward 31 us, 4.3 TB/s, its
-// instructions (23 an element, of which 3 for the turns) beside the copies.  With turns
+// Each row is read and written once.  HBM bounds fp32: 4 x 12+12 x 8192 x 64 backward
+// 100 us, 6.0 TB/s.  bf16 waits for its instructions (23 an element, of which 3 for the
+// turns) beside the copies: 8 x 8+8 x 4096 x 64 forward 31 us, 4.3 TB/s.  With turns
 // that four lanes met in one bank for the latter took 49 us.
 #include <math.h>
 #include <stdint.h>
@@ -67,8 +67,9 @@ struct WeightJob {
   int blocks[2], d;
 };
 
-// cos and sin of turn / 2^64 turns: the nearest quarter turn is taken off first,
-// which leaves at most an eighth, exact to 2^-33 of a turn in fp32.
+// cos and sin of turn / 2^64 turns: the nearest quarter turn is taken off first, which
+// leaves at most an eighth, in fp32 off by at most 2^-28 of a turn (its rounding; the
+// lower half of `turn` is cut off, 2^-32).
 __device__ __forceinline__ float2 cos_sin(unsigned long long turn) {
   const unsigned t = (unsigned)(turn >> 32), q = (t + 0x20000000u) >> 30;
   const float rest = (float)(int)(t - (q << 30)) * 0x1p-31f;  // half turns
@@ -156,7 +157,8 @@ template <typename T, int MODE, int W> struct Row {
     }
   }
   // sum of a b: by four pairs at a time, as lanes of narrower vectors hold them, so that
-  // a row's bits do not depend on its alignment
+  // the bits of a row in the split layout that is turned as a whole do not depend on its
+  // alignment (others' features meet in other lanes, or in another order by elements)
   static __device__ __forceinline__ float dot(const float* a, const float* b) {
     float sum[W / 4];
 #pragma unroll

@@ -49,7 +49,9 @@ namespace {
 
 constexpr int kChunk = SLIM_SCAN_CHUNK;  // steps between the states that are kept
 constexpr int kRun = 256, kParts = kRun / 32;  // running threads, and the parts of a tile's steps
-constexpr int kBlocks = 2;               // of an SM; with three, registers spill
+// Of an SM: 96 registers a thread, at which the backward of two bf16 channels a thread
+// spills 108 to 144 bytes, and other backward kernels up to 96; three leave 64.
+constexpr int kBlocks = 2;
 constexpr int kMaxCluster = 16;
 constexpr int kStages = 3;  // tiles of a block whose inputs have slots
 constexpr int kShort = 8;  // sequences up to here need no neighbours: a thread has all steps

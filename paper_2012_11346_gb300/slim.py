@@ -865,6 +865,8 @@ def rotary_frequencies(rotary, base=10000.0):
 
 def _frequencies(inv_freq):
     """inv_freq, numbers or None, as an array of its own."""
+    if isinstance(inv_freq, array.array) and inv_freq.typecode == "d":
+        return inv_freq[:]
     if isinstance(inv_freq, torch.Tensor) and inv_freq.is_cuda:
         raise TypeError("inv_freq is read on the host: give numbers or a CPU tensor")
     return array.array("d", () if inv_freq is None else map(float, inv_freq))
@@ -1295,7 +1297,8 @@ def gated_ff_forward(x, w, act="silu", keep=False, out=None, workspace=None, str
 
 def gated_ff_backward(x, w, dh, act="silu", z=None, workspace=None, stream=None):
     """slim_gated_ff_bwd: returns (dx, dw), the gradients of <dh, h>.  z: from
-    gated_ff_forward(..., keep=True) on the same inputs, or None."""
+    gated_ff_forward(..., keep=True) on the same inputs, or None.  The gradients of bf16
+    projections are rounded to bf16 before their two products."""
     dev = _device_of(x, w, dh, z, workspace)
     _require_cuda(x, w, dh)
     sizes = _ff_sizes(x.shape, w.shape, x.dtype, w.dtype, act, "gated_ff_backward")
