@@ -22,11 +22,12 @@
 // their gates are computed again for the second pass, from shared memory (fp32: left there by
 // the first): registers for two tiles would leave room for one block an SM.
 //
-// Measured: 1 x 65536 x 512 fp32 forward 80 us (5.0 TB/s of inputs and outputs; 190 us
+// Measured: 1 x 65536 x 512 fp32 forward 84 us (4.8 TB/s of inputs and outputs; 190 us
 // with all of a sequence's tiles in one cluster's rounds), 8 x 4096 x 512 bf16 step with
-// sigmoid gates 101 us (forward kernel 37, backward 62).  bf16 is bound by its
-// instructions (49 per element forward, 74 backward, both passes), fp32 by the exchange's
-// latency and HBM.
+// sigmoid gates 109 us (forward kernel 40, backward 68).  bf16 has 51 instructions an
+// element forward and 79 backward, both passes, at 0.6 a cycle and scheduler, and 73 and
+// 136 MB of DRAM traffic: neither is full, and the backward's registers spill.  fp32 waits
+// for the exchange and HBM.
 //
 // Backward, dgate needs h_(t-1): the forward keeps the states every 64 steps in fp32
 // (1 / 64 the bytes of an fp32 h), and a tile's states are computed again from there,
