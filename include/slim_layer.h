@@ -117,14 +117,14 @@ typedef enum {
  *            chunk), or null: what slim_gated_scan_bwd reads.
  * States and sums are fp32, h is rounded once.  A gate near 1, which a state meets many
  * times over, is rounded once: LOG gates within 2^-3 of zero (bf16 2^-6), and the larger
- * of sigmoid(g) and sigmoid(-g).  The others are off by up to 1.5 * 2^-22 of themselves
- * (bf16: and by 1.25 |g| 2^-24), and below 2^-126 they are zero.  A gate of zero (VALUE 0, LOG or
- * SIGMOID -inf) starts anew: nothing before it reaches h, finite or not.  A state
- * that is not finite stays in its channel until such a gate, or until the gates'
- * product since sinks below fp32's range.  Gates are finite, but for those infinities.
- * Beyond 1 they may grow a state past fp32's range; so may the product of up to 128 of
- * them alone: a state that is not zero is then not finite until such a gate (backward, a
- * gradient before them), one of zero stays zero.
+ * of sigmoid(g) and sigmoid(-g).  The others are off by up to 2^-21 of themselves (bf16:
+ * and by 1.25 |g| 2^-24), and below 2^-126 they are zero.  A gate of zero (VALUE 0, LOG
+ * or SIGMOID -inf) starts anew: nothing before it reaches h, finite or not.  A state that
+ * is not finite stays in its channel until such a gate, or until the gates' product since
+ * sinks below fp32's range.  Gates are finite, and LOG gates' exponentials, but for those
+ * infinities.  Beyond 1 they may grow a state past fp32's range; so may the product of up
+ * to 128 of them alone: a state that is not zero is then not finite until such a gate
+ * (backward, a gradient before them), one of zero stays zero.
  * Nothing written overlaps anything else but as said.
  *   workspace of slim_gated_scan_workspace_size() bytes, for either direction; where
  *   that is 0 (short sequences, few of them) it is not used and may be null.

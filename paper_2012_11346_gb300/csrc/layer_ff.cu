@@ -11,9 +11,10 @@
 // fp32 may keep both projections instead, and then dz is a pass over them.
 //
 // Measured: 16384 x 768 x 2048 bf16 forward 60 us, 1.72 PFLOP/s, bound by the tensor
-// pipe (one call's kernels; call after call under the power limit 70 us).  32768 x 512 x 2048 bf16 step: forward 77 us, dz 111, both products 170; with
-// only 8 stages of the reduction to a tile, the epilogue (dz: 192 KB of dh and dz a tile
-// and the operands again, 8 TB/s through L2) takes longer than the tile's MMAs, 57 us.
+// pipe (one call's kernels; call after call under the power limit 70 us).  32768 x 512 x
+// 2048 bf16 step: forward 77 us, dz 111, both products 170; with only 8 stages of the
+// reduction to a tile, the epilogue (dz: 192 KB of dh and dz a tile and the operands
+// again, 8 TB/s through L2) takes longer than the tile's MMAs, 57 us.
 #include <stdint.h>
 
 #include "../../include/slim_layer.h"
