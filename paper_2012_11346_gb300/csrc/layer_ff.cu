@@ -8,6 +8,8 @@
 // Backward: the projections again, with an epilogue that turns them and dh into
 //     dz = [dh u act'(g), dh act(g)]
 // as bf16 (three planes for fp32), and then one launch with dx = dz w and dw = dz^T x.
+// One rounding of a bf16 problem's dz puts dx and dw 2.3e-3 of their norm off where their
+// own rounding is 1.7e-3; a second plane of it would double the MMAs of both products.
 // fp32 may keep both projections instead, and then dz is a pass over them.
 //
 // Measured: 16384 x 768 x 2048 bf16 forward 60 us, 1.72 PFLOP/s, bound by the tensor
